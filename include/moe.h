@@ -297,8 +297,8 @@ moe_status moe_get_last_error(moe_stream_t stream);
  * moe_expert_ffn, moe_combine, moe_layer_forward, moe_layer_forward_dense,
  * moe_layer_forward_experts, moe_prenorm, moe_stack_forward,
  * moe_layer_forward_noalloc, moe_sa_qkv,
- * moe_sa_attend, moe_sa_forward, moe_decoder_forward) returns that status at
- * once without launching.
+ * moe_sa_attend, moe_sa_forward, moe_decoder_forward, moe_paged_append,
+ * moe_paged_attend) returns that status at once without launching.
  * With MOE_WM_SINGLE_CTA=1 the prefill expert GEMMs (batches whose experts
  * hold 128 or more slots on average) run one CTA per tile, the form used on
  * devices that cannot keep CTA pairs resident, instead of CTA pairs. */
@@ -420,6 +420,69 @@ moe_status moe_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe, int
                                const void *const *v1, const void *const *w2,
                                void *const *k_cache, void *const *v_cache, float eps,
                                void *ws, size_t ws_bytes, moe_stream_t stream);
+
+/* ---- paged key/value cache in 8 bits -------------------------------------
+ * The caches of moe_sa_* hold max_len positions of every sequence in bf16.
+ * Here a sequence holds pages of page_size positions, as many as it has
+ * positions for, in any order of one pool, and keys and values are e4m3
+ * numbers with a scale for each (page, key/value head): value = scale x
+ * number.  (The paper keeps its cache in bf16, Sec. 5.1, and says nothing of
+ * its layout.)
+ *
+ * Layouts: k_pages, v_pages [n_pages, Hkv, page_size, 128] e4m3 (a byte each);
+ * k_scale, v_scale [n_pages, Hkv] float32, positive; page_table [n_seq,
+ * max_pages] int32: position p of sequence s lies in page page_table[s, p /
+ * page_size], row p % page_size.  Entries that no position of a call needs may
+ * hold anything.  A page may be in several sequences' tables while nothing is
+ * appended to it.
+ *
+ * Tokens: (seq[t], pos[t]) as in moe_sa_*; the (seq, pos) pairs of a call are
+ * distinct, in any order.  seq[t] < 0 is a padding token: it writes nothing to
+ * the cache, its rows of q and ctx are zero, and it is no error.  A token with
+ * seq >= n_seq or pos outside [0, max_pages page_size) is recorded as
+ * MOE_ERR_DEVICE_INDEX and otherwise treated so; a page_table entry that is
+ * needed and lies outside [0, n_pages) is recorded likewise, its positions are
+ * neither written nor attended to.
+ *
+ * Limits: head_dim 128, up to 8 query heads per key/value head, T <= 65536 (as
+ * moe_sa_*); page_size 16, 32, 64 or 128; n_pages Hkv page_size and max_pages
+ * page_size below 2^31. */
+typedef struct {
+    int32_t page_size; /* positions of a page */
+    int32_t n_pages;   /* pages of the pool */
+    int32_t n_seq;     /* rows of page_table */
+    int32_t max_pages; /* columns of page_table */
+} moe_paged_dims;
+
+/* moe_paged_workspace_size: bytes of scratch moe_paged_attend needs for up to
+ * max_tokens tokens. */
+moe_status moe_paged_workspace_size(const moe_sa_dims *dims, int32_t max_tokens, size_t *bytes);
+
+/* moe_paged_append: the T rows of a QKV projection, qkv [T, (Hq + 2 Hkv) 128]
+ * in qkv_dtype (moe_dtype; query rows, key rows, value rows): queries and keys
+ * turned by the rotary embedding of moe_sa_qkv, q [T, Hq, 128] bf16 out, keys
+ * and values into their pages.  For the rows that a call writes in one page
+ * and head, with a the largest finite magnitude among them,
+ *   need  = the smallest power of two >= a / 448, and >= 2^-100
+ *   scale = need, where the call writes the page's first position (what else
+ *           the page held is void), else max(old scale, need);
+ * the page's other rows are multiplied by old scale / scale and rounded again
+ * where that is not 1; a row's numbers are x / scale rounded to nearest, ties to
+ * even.  A NaN or infinite component is stored as NaN. */
+moe_status moe_paged_append(const moe_sa_dims *dims, const moe_paged_dims *paged, int32_t T,
+                            const void *qkv, int32_t qkv_dtype, const int32_t *seq,
+                            const int32_t *pos, const int32_t *page_table, void *q, void *k_pages,
+                            void *v_pages, float *k_scale, float *v_scale, moe_stream_t stream);
+
+/* moe_paged_attend: ctx[t, h dh .. (h+1) dh) = softmax over positions 0..pos[t]
+ * of q[t,h] . K / sqrt(dh), applied to V, bf16 out; q [T, Hq, 128] bf16.
+ *   ws  workspace of at least moe_paged_workspace_size(dims, T) bytes; calls
+ *       that run at the same time need workspaces of their own. */
+moe_status moe_paged_attend(const moe_sa_dims *dims, const moe_paged_dims *paged, int32_t T,
+                            const void *q, const int32_t *seq, const int32_t *pos,
+                            const int32_t *page_table, const void *k_pages, const void *v_pages,
+                            const float *k_scale, const float *v_scale, void *ctx, void *ws,
+                            size_t ws_bytes, moe_stream_t stream);
 
 #ifdef __cplusplus
 }

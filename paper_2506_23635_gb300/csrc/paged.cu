@@ -1,0 +1,509 @@
+// A paged key/value cache in 8 bits: appending to it, and its entry points.
+//
+// Keys and values lie as e4m3 numbers in pages [n_pages, Hkv, page_size, 128],
+// a scale for each (page, key/value head): value = scale x number.  (The
+// paper's inference keeps its cache in bf16, Sec. 5.1, and prints nothing of
+// its layout.)
+//
+// k_paged_append: rows of a QKV projection -> rotated queries in bf16, rotated
+// keys and values quantised into their pages.  For the rows of one page and
+// head in a call, a = max |x| over them:
+//   need  = the smallest 2^e >= a / 448, e >= -100
+//   scale = need where the call writes the page's first position, otherwise
+//           max(old scale, need); the page's other rows follow a larger scale
+// Powers of two: e4m3 is a floating type, so a finer scale would move only where
+// its range ends, not how it rounds; with them the division is exact, a page
+// that grows rounds its earlier rows again only below the normal range, and
+// the values in a 16-bit type are exact.
+#include <math.h>
+
+#include <algorithm>
+
+#include "paged.cuh"
+
+namespace moe {
+namespace {
+
+// Rotary angles: pair i of position p turns by p base^(-2i/128) =
+// 2 pi (p r_i), r_i in turns as a 64-bit fixed-point fraction, so that p r_i
+// modulo one turn is a product of integers (no 64-bit floating point, of which
+// the SMs do little); its upper 32 bits are the angle to 2^-32 of a turn.
+struct RopeTurns {
+    uint64_t r[kPagedDh / 2];
+};
+
+RopeTurns rope_turns(float base) {
+    RopeTurns t;
+    for (int i = 0; i < kPagedDh / 2; ++i)
+        t.r[i] = (uint64_t)llrint(pow((double)base, -2.0 * i / (double)kPagedDh) /
+                                  6.283185307179586 * 9223372036854775808.0)
+                 << 1;
+    return t;
+}
+
+__device__ __forceinline__ void rope_sincos(uint64_t r, int p, float &sn, float &cs) {
+    const int32_t turns = (int32_t)(((uint64_t)(uint32_t)p * r) >> 32);  // [-1/2, 1/2) x 2^32
+    sincospif((float)turns * 4.656612873077393e-10f, &sn, &cs);          // x 2^-31: in half turns
+}
+
+// The projection's rows: bf16, fp32, or fp32 partial sums that are added in
+// order.
+enum : int { kInBf16 = 0, kInF32 = 1, kInParts = 2 };
+
+struct QkvRows {
+    const void *p;
+    int width;  // (Hq + 2 Hkv) 128
+    int T;
+    int n_part;  // kInParts: parts of each row, 0: as many as `split` says
+    long long part_stride;
+    ProjSplit split;
+};
+
+// Elements i, i + 1 (a) and i + 64, i + 65 (b) of head row hr of token t.
+template <int IN>
+__device__ __forceinline__ void load_pairs(const QkvRows &x, int t, int hr, int i, float2 &a,
+                                           float2 &b) {
+    const size_t at = (size_t)t * x.width + (size_t)hr * kPagedDh + i;
+    if constexpr (IN == kInBf16) {
+        const uint32_t *p = reinterpret_cast<const uint32_t *>(static_cast<const bf16 *>(x.p) + at);
+        const uint32_t u = p[0], v = p[kPagedDh / 4];
+        unpack_bf16x2(u, a.x, a.y);
+        unpack_bf16x2(v, b.x, b.y);
+    } else {
+        const float *p = static_cast<const float *>(x.p) + at;
+        a = *reinterpret_cast<const float2 *>(p);
+        b = *reinterpret_cast<const float2 *>(p + kPagedDh / 2);
+        if constexpr (IN == kInParts) {
+            const int n = x.n_part > 0 ? x.n_part : x.split.parts(x.T, t, hr * kPagedDh);
+            for (int k = 1; k < n; ++k) {
+                const float2 c = *reinterpret_cast<const float2 *>(p + k * x.part_stride);
+                const float2 d =
+                    *reinterpret_cast<const float2 *>(p + k * x.part_stride + kPagedDh / 2);
+                a.x += c.x;
+                a.y += c.y;
+                b.x += d.x;
+                b.y += d.y;
+            }
+        }
+    }
+}
+
+// The smallest power of two that holds magnitudes up to a (finite, >= 0).
+__device__ __forceinline__ float scale_for(float a) {
+    // a = m 2^x, 1 <= m < 2; 448 = 1.75 x 2^8
+    const uint32_t b = __float_as_uint(a);
+    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return __uint_as_float((uint32_t)(max(e, kPagedMinExp) + 127) << 23);
+}
+
+__device__ __forceinline__ float finite_abs(float x) {
+    const float a = fabsf(x);
+    return a <= 3.402823466e38f ? a : 0.f;
+}
+// What is stored of x: an infinity is a NaN (e4m3 has none; 448 would be a
+// number that nobody gave).
+__device__ __forceinline__ float storable(float x) {
+    return fabsf(x) <= 3.402823466e38f ? x : __uint_as_float(0x7fffffffu);
+}
+
+constexpr int kAppThreads = 256;
+constexpr int kAppWarps = kAppThreads / 32;
+constexpr int kAppQTokens = 4;           // tokens x head rows of a block of the queries' part
+constexpr int kAppQRows = kAppWarps;
+constexpr int kAppGroup = 128;           // tokens among which a block looks for its pages' first ones
+
+// Blocks [0, n_qb): queries, kAppQRows head rows of kAppQTokens tokens, a warp
+// a row.  The others: keys and values.  The tokens of a call that lie in one
+// page are found from the first of them: a token leads its page if no earlier
+// token of the call lies there.  Only one that does not follow its
+// predecessor inside the page can (a start); starts look through the whole
+// call's tokens, which may come in any order.  Blocks (group of 128 tokens, rows
+// [rb rpb, (rb + 1) rpb) of the 2 Hkv key and value rows, slot): the starts of the
+// group are shared out among its slots.  A block holds a page's rows in
+// registers, a warp every eighth row, between the maximum and the
+// quantisation.
+template <int IN, int PS>
+__global__ void __launch_bounds__(kAppThreads)
+k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv, const RopeTurns rope,
+               const int32_t *__restrict__ seq, const int32_t *__restrict__ pos,
+               bf16 *__restrict__ q, uint8_t *__restrict__ kp, uint8_t *__restrict__ vp,
+               float *__restrict__ ks, float *__restrict__ vs, int n_qb, int rpb, int slots,
+               unsigned *err) {
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    constexpr int H2 = kPagedDh / 2, R = PS / kAppWarps;
+    const int T = x.T, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int i = 2 * lane;
+    __shared__ __align__(8) float sn_s[kAppQTokens][H2], cs_s[kAppQTokens][H2];
+    __shared__ int tok_at[PS];
+    __shared__ uint32_t starts[kAppGroup / 32];
+    __shared__ float red[kAppWarps];
+    int b = (int)blockIdx.x;
+    if (b < n_qb) {
+        const int nrb = (Hq + kAppQRows - 1) / kAppQRows;
+        const int t0 = b / nrb * kAppQTokens, hr = b % nrb * kAppQRows + warp;
+        const int nt = min(kAppQTokens, T - t0);
+        float2 av[kAppQTokens], bv[kAppQTokens];
+#pragma unroll
+        for (int u = 0; u < kAppQTokens; ++u)
+            if (hr < Hq && u < nt) load_pairs<IN>(x, t0 + u, hr, i, av[u], bv[u]);
+        static_assert(kAppQTokens * H2 == kAppThreads, "an angle a thread");
+        bool in = false;
+        if (tid / H2 < nt) {
+            const int t = t0 + tid / H2, sq = seq[t], p = pos[t];
+            in = pv.inside(sq, p);
+            rope_sincos(rope.r[tid % H2], in ? p : 0, sn_s[tid / H2][tid % H2],
+                        cs_s[tid / H2][tid % H2]);
+            if (!in) {  // a row of zeros
+                sn_s[tid / H2][tid % H2] = 0.f;
+                cs_s[tid / H2][tid % H2] = __uint_as_float(0x7fffffffu);
+            }
+            // (seq < 0: a padding token, no error)
+            if (!in && sq >= 0 && b % nrb == 0 && tid % H2 == 0) set_error(err, kErrIndex);
+        }
+        __syncthreads();
+        if (hr >= Hq) return;
+#pragma unroll
+        for (int u = 0; u < kAppQTokens; ++u) {
+            if (u >= nt) break;
+            const float2 sn = *reinterpret_cast<const float2 *>(&sn_s[u][i]);
+            const float2 cs = *reinterpret_cast<const float2 *>(&cs_s[u][i]);
+            float2 lo = make_float2(av[u].x * cs.x - bv[u].x * sn.x, av[u].y * cs.y - bv[u].y * sn.y);
+            float2 hi = make_float2(bv[u].x * cs.x + av[u].x * sn.x, bv[u].y * cs.y + av[u].y * sn.y);
+            if (isnan(cs.x)) lo = hi = make_float2(0.f, 0.f);
+            bf16 *o = q + ((size_t)(t0 + u) * Hq + hr) * kPagedDh + i;
+            *reinterpret_cast<__nv_bfloat162 *>(o) = __floats2bfloat162_rn(lo.x, lo.y);
+            *reinterpret_cast<__nv_bfloat162 *>(o + H2) = __floats2bfloat162_rn(hi.x, hi.y);
+        }
+        return;
+    }
+    b -= n_qb;
+    const int nrb = (2 * Hkv + rpb - 1) / rpb;
+    const int slot = b % slots, rb = b / slots % nrb, g0 = b / slots / nrb * kAppGroup;
+    if (tid < kAppGroup) {
+        const int t = g0 + tid;
+        bool start = false;
+        if (t < T) {
+            const int sq = seq[t], p = pos[t];
+            start = pv.inside(sq, p) &&
+                    !(t > 0 && (p & (PS - 1)) != 0 && seq[t - 1] == sq && pos[t - 1] == p - 1);
+        }
+        const uint32_t m = __ballot_sync(0xffffffffu, start);
+        if (lane == 0) starts[warp] = m;
+    }
+    __syncthreads();
+    int seen = 0;
+#pragma unroll 1
+    for (int w = 0; w < kAppGroup / 32; ++w) {
+#pragma unroll 1
+        for (uint32_t m = starts[w]; m; m &= m - 1) {
+            if (seen++ % slots != slot) continue;
+            const int t = g0 + w * 32 + __ffs(m) - 1;
+            const int sq = seq[t], pi = pos[t] / PS;
+            const int pg = pv.page(sq, pi);
+            if (pg < 0) {
+                if (rb == 0 && tid == 0) set_error(err, kErrIndex);
+                continue;
+            }
+            __syncthreads();  // (the rows of the start before are done with tok_at)
+            for (int o = tid; o < PS; o += kAppThreads) tok_at[o] = -1;
+            __syncthreads();
+            bool earlier = false;
+            for (int j = tid; j < T; j += kAppThreads) {
+                if (seq[j] != sq) continue;
+                const int p = pos[j];
+                if (p < 0 || p / PS != pi) continue;
+                earlier |= j < t;
+                atomicMax(&tok_at[p & (PS - 1)], j);
+            }
+            if (__syncthreads_or(earlier)) continue;  // another start leads this page
+            int tok[R];
+#pragma unroll
+            for (int k = 0; k < R; ++k) tok[k] = tok_at[warp + k * kAppWarps];
+            const bool fresh = tok_at[0] >= 0;
+#pragma unroll 1
+            for (int hr = rb * rpb; hr < min((rb + 1) * rpb, 2 * Hkv); ++hr) {
+                const bool key = hr < Hkv;
+                const int h = key ? hr : hr - Hkv;
+                float *sp = (key ? ks : vs) + (size_t)pg * Hkv + h;
+                uint8_t *rows = (key ? kp : vp) + ((size_t)pg * Hkv + h) * PS * kPagedDh;
+                const float old = *sp;
+                float2 a[R], c[R];
+                float mx = 0.f;
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    a[k] = c[k] = make_float2(0.f, 0.f);
+                    if (tok[k] >= 0) load_pairs<IN>(x, tok[k], Hq + hr, i, a[k], c[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    if (tok[k] < 0) continue;
+                    if (key) {
+                        const int p = pi * PS + warp + k * kAppWarps;
+                        float s0, c0, s1, c1;
+                        rope_sincos(rope.r[i], p, s0, c0);
+                        rope_sincos(rope.r[i + 1], p, s1, c1);
+                        const float2 u = a[k], v = c[k];
+                        a[k] = make_float2(u.x * c0 - v.x * s0, u.y * c1 - v.y * s1);
+                        c[k] = make_float2(v.x * c0 + u.x * s0, v.y * c1 + u.y * s1);
+                    }
+                    mx = fmaxf(fmaxf(mx, fmaxf(finite_abs(a[k].x), finite_abs(a[k].y))),
+                               fmaxf(finite_abs(c[k].x), finite_abs(c[k].y)));
+                }
+                mx = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(mx)));
+                if (lane == 0) red[warp] = mx;
+                __syncthreads();
+#pragma unroll
+                for (int u = 0; u < kAppWarps; ++u) mx = fmaxf(mx, red[u]);
+                __syncthreads();
+                const float need = scale_for(mx);
+                const float scale = fresh ? need : fmaxf(old, need);
+                if (tid == 0) *sp = scale;
+                const float inv = 1.f / scale;
+                const bool pow2 = (__float_as_uint(scale) & 0x7fffffu) == 0;
+                auto div = [&](float v) { return storable(pow2 ? v * inv : v / scale); };
+                const bool grown = !fresh && scale != old;
+                const float ratio = old / scale;
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    uint8_t *row = rows + (size_t)(warp + k * kAppWarps) * kPagedDh;
+                    if (tok[k] >= 0) {
+                        *reinterpret_cast<uint16_t *>(row + i) =
+                            (uint16_t)e4m3x2(div(a[k].x), div(a[k].y));
+                        *reinterpret_cast<uint16_t *>(row + H2 + i) =
+                            (uint16_t)e4m3x2(div(c[k].x), div(c[k].y));
+                    } else if (grown) {
+                        uint32_t *p4 = reinterpret_cast<uint32_t *>(row + 4 * lane);
+                        const uint32_t v = *p4;
+                        const float2 f0 = e4m3x2_to_float2(v & 0xffffu);
+                        const float2 f1 = e4m3x2_to_float2(v >> 16);
+                        *p4 = e4m3x2(f0.x * ratio, f0.y * ratio) |
+                              e4m3x2(f1.x * ratio, f1.y * ratio) << 16;
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <int IN>
+const void *append_kernel(int ps) {
+    switch (ps) {
+        case 16: return (const void *)k_paged_append<IN, 16>;
+        case 32: return (const void *)k_paged_append<IN, 32>;
+        case 64: return (const void *)k_paged_append<IN, 64>;
+        default: return (const void *)k_paged_append<IN, 128>;
+    }
+}
+
+cudaError_t launch_append(const QkvRows &rows, int in, const moe_sa_dims &d,
+                          const moe_paged_dims &pd, const int32_t *seq, const int32_t *pos,
+                          const int32_t *table, void *q, void *kp, void *vp, float *ks, float *vs,
+                          cudaStream_t st) {
+    int Hq = d.n_heads, Hkv = d.n_kv_heads;
+    const int T = rows.T;
+    QkvRows x = rows;
+    PageView pv{table, pd.n_seq, pd.max_pages, pd.n_pages, 31 - __builtin_clz(pd.page_size)};
+    RopeTurns rope = rope_turns(d.rope_base);
+    bf16 *qp = static_cast<bf16 *>(q);
+    uint8_t *k8 = static_cast<uint8_t *>(kp), *v8 = static_cast<uint8_t *>(vp);
+    unsigned *err = device_info().err;
+    int n_qb = (Hq + kAppQRows - 1) / kAppQRows * ((T + kAppQTokens - 1) / kAppQTokens);
+    int rpb = T <= 1024 ? 1 : 4;
+    int slots = T <= kAppGroup ? T : T <= 1024 ? 32 : 8;
+    const int groups = (T + kAppGroup - 1) / kAppGroup;
+    const int n_kb = groups * ((2 * Hkv + rpb - 1) / rpb) * slots;
+    const void *kern = in == kInBf16  ? append_kernel<kInBf16>(pd.page_size)
+                       : in == kInF32 ? append_kernel<kInF32>(pd.page_size)
+                                      : append_kernel<kInParts>(pd.page_size);
+    void *args[] = {&x,  &Hq, &Hkv, &pv, &rope, &seq, &pos,   &qp,
+                    &k8, &v8, &ks,  &vs, &n_qb, &rpb, &slots, &err};
+    LaunchScope ls("paged_append", st);
+    return launch_pdl(kern, dim3((unsigned)(n_qb + n_kb)), dim3(kAppThreads), 0, st, args);
+}
+
+// Attention, a block for each (token, key/value head): each of its warps takes
+// every fourth position, a lane four dims.
+template <int G>
+__global__ void __launch_bounds__(128)
+k_paged_attend(int Hkv, const PageView pv, const int32_t *__restrict__ seq,
+               const int32_t *__restrict__ pos, const bf16 *__restrict__ q,
+               const uint8_t *__restrict__ kp, const uint8_t *__restrict__ vp,
+               const float *__restrict__ ks, const float *__restrict__ vs, bf16 *__restrict__ ctx,
+               unsigned *err) {
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    __shared__ float sm_m[4][G], sm_l[4][G], sm_a[4][G][kPagedDh];
+    const int t = blockIdx.x, g = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int sq = seq[t], p = pos[t], ps = 1 << pv.shift;
+    const bool in = pv.inside(sq, p);
+    if (!in && sq >= 0 && g == 0 && threadIdx.x == 0) set_error(err, kErrIndex);
+    float qv[G][4], m[G], l[G], acc[G][4];
+    const size_t q0 = ((size_t)t * Hkv + g) * G * kPagedDh;
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+        const uint2 u = *reinterpret_cast<const uint2 *>(q + q0 + h * kPagedDh + 4 * lane);
+        unpack_bf16x2(u.x, qv[h][0], qv[h][1]);
+        unpack_bf16x2(u.y, qv[h][2], qv[h][3]);
+        m[h] = -1e30f;
+        l[h] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            acc[h][i] = 0.f;
+            qv[h][i] *= 0.08838834764831845f;
+        }
+    }
+    for (int j = warp; in && j <= p; j += 4) {
+        const int pg = pv.page(sq, j >> pv.shift);
+        if (pg < 0) {
+            if (lane == 0) set_error(err, kErrIndex);
+            continue;
+        }
+        const size_t row = (((size_t)pg * Hkv + g) * ps + (j & (ps - 1))) * kPagedDh + 4 * lane;
+        const uint32_t kw = *reinterpret_cast<const uint32_t *>(kp + row);
+        const uint32_t vw = *reinterpret_cast<const uint32_t *>(vp + row);
+        const float2 k0 = e4m3x2_to_float2(kw & 0xffffu), k1 = e4m3x2_to_float2(kw >> 16);
+        const float2 v0 = e4m3x2_to_float2(vw & 0xffffu), v1 = e4m3x2_to_float2(vw >> 16);
+        const float sk = ks[(size_t)pg * Hkv + g], sv = vs[(size_t)pg * Hkv + g];
+#pragma unroll
+        for (int h = 0; h < G; ++h) {
+            const float s = sk * warp_sum(qv[h][0] * k0.x + qv[h][1] * k0.y + qv[h][2] * k1.x +
+                                          qv[h][3] * k1.y);
+            const float mn = fmaxf(m[h], s);
+            const float c = expf(m[h] - mn), w = expf(s - mn);
+            m[h] = mn;
+            l[h] = l[h] * c + w;
+            acc[h][0] = acc[h][0] * c + w * sv * v0.x;
+            acc[h][1] = acc[h][1] * c + w * sv * v0.y;
+            acc[h][2] = acc[h][2] * c + w * sv * v1.x;
+            acc[h][3] = acc[h][3] * c + w * sv * v1.y;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+        if (lane == 0) {
+            sm_m[warp][h] = m[h];
+            sm_l[warp][h] = l[h];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sm_a[warp][h][4 * lane + i] = acc[h][i];
+    }
+    __syncthreads();
+    for (int h = 0; h < G; ++h) {
+        float M = -1e30f, L = 0.f, A = 0.f;
+        for (int w = 0; w < 4; ++w) M = fmaxf(M, sm_m[w][h]);
+        for (int w = 0; w < 4; ++w) {
+            const float c = expf(sm_m[w][h] - M);
+            L += c * sm_l[w][h];
+            A += c * sm_a[w][h][threadIdx.x];
+        }
+        ctx[q0 + h * kPagedDh + threadIdx.x] = __float2bfloat16_rn(L != 0.f ? A / L : 0.f);
+    }
+}
+
+// ---- host ------------------------------------------------------------------------
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool ok_ptr(const void *p) { return p != nullptr && aligned16(p); }
+moe_status cuda_status(cudaError_t e) { return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA; }
+
+moe_status check_paged(const moe_sa_dims *d, const moe_paged_dims *pd) {
+    size_t n = 0;
+    moe_status s = moe_sa_workspace_size(d, 0, &n);  // the shape's own limits
+    if (s != MOE_OK) return s;
+    if (!pd) return MOE_ERR_INVALID_ARG;
+    if (pd->n_pages < 1 || pd->n_seq < 1 || pd->max_pages < 1 || pd->page_size < 1)
+        return MOE_ERR_INVALID_ARG;
+    if (pd->page_size != 16 && pd->page_size != 32 && pd->page_size != 64 && pd->page_size != 128)
+        return MOE_ERR_UNSUPPORTED;
+    const int64_t most = (1LL << 31) - 1;
+    if ((int64_t)pd->n_pages * d->n_kv_heads * pd->page_size > most ||
+        (int64_t)pd->max_pages * pd->page_size > most)
+        return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
+moe_status check_paged_call(const moe_sa_dims *d, const moe_paged_dims *pd, int32_t T,
+                            const int32_t *seq, const int32_t *pos, const int32_t *table,
+                            const void *kp, const void *vp, const float *ks, const float *vs) {
+    moe_status s = check_paged(d, pd);
+    if (s != MOE_OK) return s;
+    if (T < 0 || T > kPagedMaxTokens) return MOE_ERR_INVALID_ARG;
+    if (T > 0 && (!ok_ptr(seq) || !ok_ptr(pos) || !ok_ptr(table) || !ok_ptr(kp) || !ok_ptr(vp) ||
+                  !ok_ptr(ks) || !ok_ptr(vs)))
+        return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
+}  // namespace
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" {
+
+moe_status moe_paged_workspace_size(const moe_sa_dims *dims, int32_t max_tokens, size_t *bytes) {
+    size_t n = 0;
+    moe_status s = moe_sa_workspace_size(dims, 0, &n);
+    if (s != MOE_OK) return s;
+    if (!bytes || max_tokens < 0 || max_tokens > kPagedMaxTokens) return MOE_ERR_INVALID_ARG;
+    *bytes = 256;
+    return MOE_OK;
+}
+
+moe_status moe_paged_append(const moe_sa_dims *dims, const moe_paged_dims *paged, int32_t T,
+                            const void *qkv, int32_t qkv_dtype, const int32_t *seq,
+                            const int32_t *pos, const int32_t *page_table, void *q, void *k_pages,
+                            void *v_pages, float *k_scale, float *v_scale, moe_stream_t stream) {
+    MOE_INJECT("moe_paged_append");
+    moe_status s = check_paged_call(dims, paged, T, seq, pos, page_table, k_pages, v_pages,
+                                    k_scale, v_scale);
+    if (s != MOE_OK) return s;
+    if (qkv_dtype != MOE_F32 && qkv_dtype != MOE_BF16) return MOE_ERR_INVALID_ARG;
+    if (T == 0) return MOE_OK;
+    if (!ok_ptr(qkv) || !ok_ptr(q)) return MOE_ERR_INVALID_ARG;
+    const QkvRows rows{qkv, (dims->n_heads + 2 * dims->n_kv_heads) * kPagedDh, T, 1, 0, {}};
+    return cuda_status(launch_append(rows, qkv_dtype == MOE_BF16 ? kInBf16 : kInF32, *dims, *paged,
+                                     seq, pos, page_table, q, k_pages, v_pages, k_scale, v_scale,
+                                     (cudaStream_t)stream));
+}
+
+moe_status moe_paged_attend(const moe_sa_dims *dims, const moe_paged_dims *paged, int32_t T,
+                            const void *q, const int32_t *seq, const int32_t *pos,
+                            const int32_t *page_table, const void *k_pages, const void *v_pages,
+                            const float *k_scale, const float *v_scale, void *ctx, void *ws,
+                            size_t ws_bytes, moe_stream_t stream) {
+    MOE_INJECT("moe_paged_attend");
+    moe_status s = check_paged_call(dims, paged, T, seq, pos, page_table, k_pages, v_pages,
+                                    k_scale, v_scale);
+    if (s != MOE_OK) return s;
+    if (T == 0) return MOE_OK;
+    if (!ok_ptr(q) || !ok_ptr(ctx)) return MOE_ERR_INVALID_ARG;
+    size_t need = 0;
+    if ((s = moe_paged_workspace_size(dims, T, &need)) != MOE_OK) return s;
+    if (!ok_ptr(ws) || ws_bytes < need) return MOE_ERR_WORKSPACE;
+    int Hkv = dims->n_kv_heads;
+    PageView pv{page_table, paged->n_seq, paged->max_pages, paged->n_pages,
+                31 - __builtin_clz(paged->page_size)};
+    const bf16 *qp = static_cast<const bf16 *>(q);
+    const uint8_t *k8 = static_cast<const uint8_t *>(k_pages),
+                  *v8 = static_cast<const uint8_t *>(v_pages);
+    bf16 *cp = static_cast<bf16 *>(ctx);
+    unsigned *err = device_info().err;
+    const void *kern;
+    switch (dims->n_heads / Hkv) {
+        case 1: kern = (const void *)k_paged_attend<1>; break;
+        case 2: kern = (const void *)k_paged_attend<2>; break;
+        case 3: kern = (const void *)k_paged_attend<3>; break;
+        case 4: kern = (const void *)k_paged_attend<4>; break;
+        case 5: kern = (const void *)k_paged_attend<5>; break;
+        case 6: kern = (const void *)k_paged_attend<6>; break;
+        case 7: kern = (const void *)k_paged_attend<7>; break;
+        default: kern = (const void *)k_paged_attend<8>; break;
+    }
+    void *args[] = {&Hkv, &pv, &seq, &pos, &qp, &k8, &v8, &k_scale, &v_scale, &cp, &err};
+    LaunchScope ls("paged_attend", (cudaStream_t)stream);
+    return cuda_status(launch_pdl(kern, dim3(T, Hkv), dim3(128), 0, (cudaStream_t)stream, args));
+}
+
+}  // extern "C"

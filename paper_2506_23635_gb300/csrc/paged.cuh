@@ -1,0 +1,54 @@
+// The paged 8-bit key/value cache: what its kernels share (paged.cu).
+#pragma once
+
+#include <stdint.h>
+
+#include "ptx.cuh"
+
+namespace moe {
+
+constexpr int kPagedDh = 128;        // head_dim
+constexpr int kPagedMaxGroup = 8;    // query heads per key/value head
+constexpr int kPagedMaxTokens = 65536;
+constexpr float kE4m3Max = 448.f;
+constexpr int kPagedMinExp = -100;   // scales are at least 2^-100
+
+// Where the positions of the sequences lie: page_table [n_seq, max_pages].
+struct PageView {
+    const int32_t *table;
+    int n_seq, max_pages, n_pages;
+    int shift;  // log2(page_size)
+
+    // token (sequence sq, position p) lies inside the table
+    __device__ __forceinline__ bool inside(int sq, int p) const {
+        return sq >= 0 && sq < n_seq && p >= 0 && (p >> shift) < max_pages;
+    }
+    // page of the sequence's page index i, or -1 where the table holds none
+    __device__ __forceinline__ int page(int sq, int i) const {
+        const int pg = table[(size_t)sq * max_pages + i];
+        return pg >= 0 && pg < n_pages ? pg : -1;
+    }
+};
+
+// Two floats -> two e4m3 (round to nearest even, largest magnitude 448; NaN
+// stays NaN), the first in the low byte; and back to two halves (exact).
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t v) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)v));
+    return r;
+}
+__device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t v) {
+    const uint32_t h = e4m3x2_to_f16x2(v);
+    float2 f;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}"
+        : "=f"(f.x), "=f"(f.y)
+        : "r"(h));
+    return f;
+}
+
+}  // namespace moe

@@ -8,6 +8,7 @@ import of the library raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -35,6 +36,7 @@ EXPORTS = (
     "moe_profile_reset", "moe_profile_read",
     "moe_sa_workspace_size", "moe_sa_qkv", "moe_sa_attend", "moe_sa_forward",
     "moe_decoder_workspace_size", "moe_decoder_forward",
+    "moe_paged_workspace_size", "moe_paged_append", "moe_paged_attend",
 )
 
 
@@ -66,6 +68,16 @@ class SaDims(ctypes.Structure):
                 f"dh={self.head_dim}, base={self.rope_base})")
 
 
+class PagedDims(ctypes.Structure):
+    """moe_paged_dims: a paged cache's shape."""
+    _fields_ = [("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("n_seq", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+    def __repr__(self):
+        return (f"PagedDims(page={self.page_size}, pages={self.n_pages}, seqs={self.n_seq}, "
+                f"max={self.max_pages})")
+
+
 class KernelStat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 48), ("launches", ctypes.c_int64),
                 ("total_ms", ctypes.c_double)]
@@ -90,6 +102,7 @@ def lib() -> ctypes.CDLL:
     P, I32, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
     DP = ctypes.POINTER(Dims)
     SP = ctypes.POINTER(SaDims)
+    GP = ctypes.POINTER(PagedDims)
     sigs = {
         "moe_workspace_size": [DP, I32, ctypes.POINTER(SZ)],
         "moe_route": [DP, I32, P, P, P, P, P, P],
@@ -119,6 +132,9 @@ def lib() -> ctypes.CDLL:
         "moe_decoder_workspace_size": [SP, DP, I32, ctypes.POINTER(SZ)],
         "moe_decoder_forward": [SP, DP, I32, I32, P, P, I32, I32, P] + [ctypes.POINTER(P)] * 8
                                + [ctypes.c_float, P, SZ, P],
+        "moe_paged_workspace_size": [SP, I32, ctypes.POINTER(SZ)],
+        "moe_paged_append": [SP, GP, I32, P, I32] + [P] * 9,
+        "moe_paged_attend": [SP, GP, I32] + [P] * 10 + [SZ, P],
     }
     for name, args in sigs.items():
         fn = getattr(L, name)
@@ -478,3 +494,123 @@ def decoder_forward(a: SaDims, d: Dims, weights: DecoderWeights, resid, seq, pos
                                      _ptr(ws), ws.numel(), _stream(stream)),
            "moe_decoder_forward")
     return resid
+
+
+# ---- paged key/value cache in 8 bits -----------------------------------------
+
+
+class PagedCache:
+    """A paged e4m3 cache (include/moe.h, moe_paged_dims): ``k_pages`` and
+    ``v_pages`` [n_pages, Hkv, page_size, 128] float8_e4m3fn, ``k_scale`` and
+    ``v_scale`` [n_pages, Hkv] float32, ``page_table`` [n_seq, max_pages]
+    int32.  The tensors are the caller's; the table may be rewritten between
+    calls (``page_table`` may be given anew for another batch of sequences)."""
+
+    def __init__(self, k_pages, v_pages, k_scale, v_scale, page_table):
+        n_pages, n_kv, page_size, dh = k_pages.shape
+        _want(k_pages, (n_pages, n_kv, page_size, dh), torch.float8_e4m3fn, "k_pages")
+        _want(v_pages, (n_pages, n_kv, page_size, dh), torch.float8_e4m3fn, "v_pages")
+        _want(k_scale, (n_pages, n_kv), torch.float32, "k_scale")
+        _want(v_scale, (n_pages, n_kv), torch.float32, "v_scale")
+        if page_table.dim() != 2:
+            raise ValueError("page_table must be [n_seq, max_pages]")
+        _want(page_table, tuple(page_table.shape), torch.int32, "page_table")
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.k_scale, self.v_scale = k_scale, v_scale
+        self.page_table = page_table
+        self.dims = PagedDims(page_size, n_pages, *page_table.shape)
+
+    @staticmethod
+    def alloc(a: SaDims, page_size: int, n_pages: int, page_table) -> "PagedCache":
+        """An empty cache of ``n_pages`` pages on the page table's device."""
+        dev = page_table.device
+        shape = (n_pages, a.n_kv_heads, page_size, a.head_dim)
+        pages = [torch.zeros(shape, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)
+                 for _ in range(2)]
+        scales = [torch.ones(shape[:2], dtype=torch.float32, device=dev) for _ in range(2)]
+        return PagedCache(*pages, *scales, page_table)
+
+    def _args(self, a: SaDims, T: int, seq, pos):
+        """Checks a call's tokens against the cache; the tensors of the call."""
+        if (self.dims.n_seq, self.dims.max_pages) != tuple(self.page_table.shape):
+            self.dims = PagedDims(self.dims.page_size, self.dims.n_pages, *self.page_table.shape)
+        if self.k_pages.shape[1] != a.n_kv_heads or self.k_pages.shape[3] != a.head_dim:
+            raise ValueError("the cache's heads are not those of the dims")
+        _want(seq, (T,), torch.int32, "seq")
+        _want(pos, (T,), torch.int32, "pos")
+        _want(self.page_table, (self.dims.n_seq, self.dims.max_pages), torch.int32, "page_table")
+        return (self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.page_table, seq, pos)
+
+
+def _want(t, shape, dtype, what: str):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype} {tuple(shape)}, is {t.dtype} {tuple(t.shape)}")
+
+
+def _one_device(tensors, stream):
+    """The call's tensors lie on one CUDA device, and it is the one that the
+    launches go to: the current one, with a stream of its own."""
+    dev = torch.device("cuda", torch.cuda.current_device())
+    if any(t.device != dev for t in tensors):
+        raise ValueError(f"tensors must be on the current device {dev}")
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"the stream must be of the current device {dev}")
+
+
+def _on(stream):
+    """Memory that a call allocates itself belongs to the stream that uses it."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def paged_workspace_size(a: SaDims, max_tokens: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().moe_paged_workspace_size(ctypes.byref(a), max_tokens, ctypes.byref(n)),
+           "moe_paged_workspace_size")
+    return int(n.value)
+
+
+def paged_alloc_workspace(a: SaDims, max_tokens: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(paged_workspace_size(a, max_tokens), 256), dtype=torch.uint8,
+                       device=device)
+
+
+def paged_append(a: SaDims, cache: PagedCache, qkv, seq, pos, q=None, stream=None):
+    """Rotated queries q [T, Hq, 128] (bf16) of the projection's rows qkv
+    [T, (Hq + 2 Hkv) 128] (bf16 or fp32); the T tokens' rotated keys and
+    their values quantised into the cache's pages at (seq[t], pos[t])."""
+    T = qkv.shape[0]
+    args = cache._args(a, T, seq, pos)
+    if qkv.dtype not in _DT:
+        raise ValueError("qkv must be bf16 or fp32")
+    _want(qkv, (T, (a.n_heads + 2 * a.n_kv_heads) * a.head_dim), qkv.dtype, "qkv")
+    with _on(stream):
+        if q is None:
+            q = torch.empty((T, a.n_heads, a.head_dim), dtype=torch.bfloat16, device=qkv.device)
+    _want(q, (T, a.n_heads, a.head_dim), torch.bfloat16, "q")
+    _one_device((*args, qkv, q), stream)
+    c = cache
+    _check(lib().moe_paged_append(ctypes.byref(a), ctypes.byref(c.dims), T, _ptr(qkv),
+                                  _DT[qkv.dtype], _ptr(seq), _ptr(pos), _ptr(c.page_table),
+                                  _ptr(q), _ptr(c.k_pages), _ptr(c.v_pages), _ptr(c.k_scale),
+                                  _ptr(c.v_scale), _stream(stream)), "moe_paged_append")
+    return q
+
+
+def paged_attend(a: SaDims, cache: PagedCache, q, seq, pos, ctx=None, ws=None, stream=None):
+    """ctx [T, Hq * 128] (bf16): causal attention of the queries q
+    [T, Hq, 128] (bf16) over positions 0..pos[t] of their sequences."""
+    T = q.shape[0]
+    args = cache._args(a, T, seq, pos)
+    _want(q, (T, a.n_heads, a.head_dim), torch.bfloat16, "q")
+    with _on(stream):
+        if ctx is None:
+            ctx = torch.empty((T, a.n_heads * a.head_dim), dtype=torch.bfloat16, device=q.device)
+        ws = paged_alloc_workspace(a, T, q.device) if ws is None else ws
+    _want(ctx, (T, a.n_heads * a.head_dim), torch.bfloat16, "ctx")
+    _one_device((*args, q, ctx, ws), stream)
+    c = cache
+    _check(lib().moe_paged_attend(ctypes.byref(a), ctypes.byref(c.dims), T, _ptr(q), _ptr(seq),
+                                  _ptr(pos), _ptr(c.page_table), _ptr(c.k_pages),
+                                  _ptr(c.v_pages), _ptr(c.k_scale), _ptr(c.v_scale), _ptr(ctx),
+                                  _ptr(ws), ws.numel(), _stream(stream)), "moe_paged_attend")
+    return ctx
