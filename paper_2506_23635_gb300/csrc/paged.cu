@@ -322,82 +322,54 @@ cudaError_t launch_append(const QkvRows &rows, int in, const moe_sa_dims &d,
     return launch_pdl(kern, dim3((unsigned)(n_qb + n_kb)), dim3(kAppThreads), 0, st, args);
 }
 
-// Attention, a block for each (token, key/value head): each of its warps takes
-// every fourth position, a lane four dims.
-template <int G>
-__global__ void __launch_bounds__(128)
-k_paged_attend(int Hkv, const PageView pv, const int32_t *__restrict__ seq,
-               const int32_t *__restrict__ pos, const bf16 *__restrict__ q,
-               const uint8_t *__restrict__ kp, const uint8_t *__restrict__ vp,
-               const float *__restrict__ ks, const float *__restrict__ vs, bf16 *__restrict__ ctx,
-               unsigned *err) {
+// The tokens that are attended one by one (in their order), the position tiles
+// ahead of each, and the decode attention's counters at zero.  One block.
+constexpr int kPlanThreads = 1024;
+
+__global__ void __launch_bounds__(kPlanThreads)
+k_paged_plan(int T, const PageView pv, const int32_t *__restrict__ seq,
+             const int32_t *__restrict__ pos, const PagedList l) {
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
-    __shared__ float sm_m[4][G], sm_l[4][G], sm_a[4][G][kPagedDh];
-    const int t = blockIdx.x, g = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int sq = seq[t], p = pos[t], ps = 1 << pv.shift;
-    const bool in = pv.inside(sq, p);
-    if (!in && sq >= 0 && g == 0 && threadIdx.x == 0) set_error(err, kErrIndex);
-    float qv[G][4], m[G], l[G], acc[G][4];
-    const size_t q0 = ((size_t)t * Hkv + g) * G * kPagedDh;
-#pragma unroll
-    for (int h = 0; h < G; ++h) {
-        const uint2 u = *reinterpret_cast<const uint2 *>(q + q0 + h * kPagedDh + 4 * lane);
-        unpack_bf16x2(u.x, qv[h][0], qv[h][1]);
-        unpack_bf16x2(u.y, qv[h][2], qv[h][3]);
-        m[h] = -1e30f;
-        l[h] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            acc[h][i] = 0.f;
-            qv[h][i] *= 0.08838834764831845f;
+    __shared__ long long sums[kPlanThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    for (int i = tid; i < kPagedMaxCtas; i += kPlanThreads) l.count[i] = 0;
+    const int n = T;
+    long long run = 0;
+    for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+        const int i = i0 + tid;
+        int nt = 0;
+        if (i < n) {
+            const int t = i, p = pos[t];
+            l.list[i] = t;
+            nt = pv.inside(seq[t], p) ? p / kPagedTile + 1 : 1;
         }
+        long long v = nt;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long u = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v += u;
+        }
+        if (lane == 31) sums[warp] = v;
+        __syncthreads();
+        if (warp == 0) {
+            long long s = sums[lane];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long u = __shfl_up_sync(0xffffffffu, s, o);
+                if (lane >= o) s += u;
+            }
+            sums[lane] = s;
+        }
+        __syncthreads();
+        const long long ahead = run + (warp > 0 ? sums[warp - 1] : 0) + v - nt;
+        if (i < n) l.before[i] = ahead;
+        run += sums[kPlanThreads / 32 - 1];
+        __syncthreads();
     }
-    for (int j = warp; in && j <= p; j += 4) {
-        const int pg = pv.page(sq, j >> pv.shift);
-        if (pg < 0) {
-            if (lane == 0) set_error(err, kErrIndex);
-            continue;
-        }
-        const size_t row = (((size_t)pg * Hkv + g) * ps + (j & (ps - 1))) * kPagedDh + 4 * lane;
-        const uint32_t kw = *reinterpret_cast<const uint32_t *>(kp + row);
-        const uint32_t vw = *reinterpret_cast<const uint32_t *>(vp + row);
-        const float2 k0 = e4m3x2_to_float2(kw & 0xffffu), k1 = e4m3x2_to_float2(kw >> 16);
-        const float2 v0 = e4m3x2_to_float2(vw & 0xffffu), v1 = e4m3x2_to_float2(vw >> 16);
-        const float sk = ks[(size_t)pg * Hkv + g], sv = vs[(size_t)pg * Hkv + g];
-#pragma unroll
-        for (int h = 0; h < G; ++h) {
-            const float s = sk * warp_sum(qv[h][0] * k0.x + qv[h][1] * k0.y + qv[h][2] * k1.x +
-                                          qv[h][3] * k1.y);
-            const float mn = fmaxf(m[h], s);
-            const float c = expf(m[h] - mn), w = expf(s - mn);
-            m[h] = mn;
-            l[h] = l[h] * c + w;
-            acc[h][0] = acc[h][0] * c + w * sv * v0.x;
-            acc[h][1] = acc[h][1] * c + w * sv * v0.y;
-            acc[h][2] = acc[h][2] * c + w * sv * v1.x;
-            acc[h][3] = acc[h][3] * c + w * sv * v1.y;
-        }
-    }
-#pragma unroll
-    for (int h = 0; h < G; ++h) {
-        if (lane == 0) {
-            sm_m[warp][h] = m[h];
-            sm_l[warp][h] = l[h];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sm_a[warp][h][4 * lane + i] = acc[h][i];
-    }
-    __syncthreads();
-    for (int h = 0; h < G; ++h) {
-        float M = -1e30f, L = 0.f, A = 0.f;
-        for (int w = 0; w < 4; ++w) M = fmaxf(M, sm_m[w][h]);
-        for (int w = 0; w < 4; ++w) {
-            const float c = expf(sm_m[w][h] - M);
-            L += c * sm_l[w][h];
-            A += c * sm_a[w][h][threadIdx.x];
-        }
-        ctx[q0 + h * kPagedDh + threadIdx.x] = __float2bfloat16_rn(L != 0.f ? A / L : 0.f);
+    if (tid == 0) {
+        l.before[n] = run;
+        *l.n_list = n;
     }
 }
 
@@ -406,6 +378,46 @@ k_paged_attend(int Hkv, const PageView pv, const int32_t *__restrict__ seq,
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool ok_ptr(const void *p) { return p != nullptr && aligned16(p); }
 moe_status cuda_status(cudaError_t e) { return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA; }
+
+// Workspace of moe_paged_attend.
+struct PagedWs {
+    size_t n_list, count, list, before, part, total;
+};
+
+PagedWs paged_ws(int64_t T) {
+    auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
+    PagedWs L{};
+    size_t o = 0;
+    L.n_list = o; o += up(4);
+    L.count = o; o += up(kPagedMaxCtas * 4);
+    L.list = o; o += up((size_t)T * 4);
+    L.before = o; o += up(((size_t)T + 1) * 8);
+    L.part = o; o += up(kPagedPartFloats * 4);
+    L.total = o;
+    return L;
+}
+
+template <typename P>
+P *at(void *ws, size_t off) {
+    return reinterpret_cast<P *>(static_cast<char *>(ws) + off);
+}
+
+cudaError_t attend(const PagedAttn &a, void *ws, cudaStream_t st) {
+    const PagedWs L = paged_ws(a.T);
+    PagedList l{at<int>(ws, L.n_list), at<int>(ws, L.list), at<long long>(ws, L.before),
+                at<int>(ws, L.count)};
+    {
+        int T = a.T;
+        PageView pv = a.pv;
+        const int32_t *seq = a.seq, *pos = a.pos;
+        void *args[] = {&T, &pv, &seq, &pos, &l};
+        LaunchScope ls("paged_plan", st);
+        cudaError_t e =
+            launch_pdl((const void *)k_paged_plan, dim3(1), dim3(kPlanThreads), 0, st, args);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_paged_decode_tc(a, l, at<float>(ws, L.part), st);
+}
 
 moe_status check_paged(const moe_sa_dims *d, const moe_paged_dims *pd) {
     size_t n = 0;
@@ -447,7 +459,7 @@ moe_status moe_paged_workspace_size(const moe_sa_dims *dims, int32_t max_tokens,
     moe_status s = moe_sa_workspace_size(dims, 0, &n);
     if (s != MOE_OK) return s;
     if (!bytes || max_tokens < 0 || max_tokens > kPagedMaxTokens) return MOE_ERR_INVALID_ARG;
-    *bytes = 256;
+    *bytes = paged_ws(max_tokens).total;
     return MOE_OK;
 }
 
@@ -482,28 +494,21 @@ moe_status moe_paged_attend(const moe_sa_dims *dims, const moe_paged_dims *paged
     size_t need = 0;
     if ((s = moe_paged_workspace_size(dims, T, &need)) != MOE_OK) return s;
     if (!ok_ptr(ws) || ws_bytes < need) return MOE_ERR_WORKSPACE;
-    int Hkv = dims->n_kv_heads;
-    PageView pv{page_table, paged->n_seq, paged->max_pages, paged->n_pages,
-                31 - __builtin_clz(paged->page_size)};
-    const bf16 *qp = static_cast<const bf16 *>(q);
-    const uint8_t *k8 = static_cast<const uint8_t *>(k_pages),
-                  *v8 = static_cast<const uint8_t *>(v_pages);
-    bf16 *cp = static_cast<bf16 *>(ctx);
-    unsigned *err = device_info().err;
-    const void *kern;
-    switch (dims->n_heads / Hkv) {
-        case 1: kern = (const void *)k_paged_attend<1>; break;
-        case 2: kern = (const void *)k_paged_attend<2>; break;
-        case 3: kern = (const void *)k_paged_attend<3>; break;
-        case 4: kern = (const void *)k_paged_attend<4>; break;
-        case 5: kern = (const void *)k_paged_attend<5>; break;
-        case 6: kern = (const void *)k_paged_attend<6>; break;
-        case 7: kern = (const void *)k_paged_attend<7>; break;
-        default: kern = (const void *)k_paged_attend<8>; break;
-    }
-    void *args[] = {&Hkv, &pv, &seq, &pos, &qp, &k8, &v8, &k_scale, &v_scale, &cp, &err};
-    LaunchScope ls("paged_attend", (cudaStream_t)stream);
-    return cuda_status(launch_pdl(kern, dim3(T, Hkv), dim3(128), 0, (cudaStream_t)stream, args));
+    const PagedAttn a{T,
+                      dims->n_heads,
+                      dims->n_kv_heads,
+                      paged->page_size,
+                      PageView{page_table, paged->n_seq, paged->max_pages, paged->n_pages,
+                               31 - __builtin_clz(paged->page_size)},
+                      seq,
+                      pos,
+                      q,
+                      k_pages,
+                      v_pages,
+                      k_scale,
+                      v_scale,
+                      ctx};
+    return cuda_status(attend(a, ws, (cudaStream_t)stream));
 }
 
 }  // extern "C"

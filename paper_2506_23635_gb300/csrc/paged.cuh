@@ -51,4 +51,34 @@ __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t v) {
     return f;
 }
 
+// The tokens that the decode attention takes one by one, made on the device
+// (k_paged_plan): list[i] is a token, before[i] the position tiles (of
+// kPagedTile positions, at least one) of the list's tokens ahead of it, entry
+// n_list those of all.  count: a counter of finished parts for each CTA, zero
+// at the start.
+constexpr int kPagedTile = 128;
+constexpr int kPagedMaxCtas = 320;
+struct PagedList {
+    int *n_list;
+    int *list;
+    long long *before;
+    int *count;
+};
+// a part's slot in the workspace: 8 rows of 128 sums, 8 pairs (base, sum); two
+// slots for each CTA
+constexpr int kPagedSlot = kPagedMaxGroup * (kPagedDh + 2);
+constexpr size_t kPagedPartFloats = (size_t)2 * kPagedMaxCtas * kPagedSlot;
+
+struct PagedAttn {
+    int T, Hq, Hkv, page_size;
+    PageView pv;
+    const int32_t *seq, *pos;
+    const void *q, *kp, *vp;
+    const float *ks, *vs;
+    void *ctx;
+};
+// Attention of the listed tokens over the 8-bit cache (paged_decode_tc.cu).
+cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part,
+                                   cudaStream_t st);
+
 }  // namespace moe
