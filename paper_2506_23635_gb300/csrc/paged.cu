@@ -19,6 +19,7 @@
 
 #include <algorithm>
 
+#include "attn_plan.cuh"
 #include "paged.cuh"
 
 namespace moe {
@@ -32,8 +33,12 @@ struct RopeTurns {
     uint64_t r[kPagedDh / 2];
 };
 
-RopeTurns rope_turns(float base) {
-    RopeTurns t;
+// (64 powers take longer than a launch: a thread keeps those of its last base)
+const RopeTurns &rope_turns(float base) {
+    static thread_local RopeTurns t;
+    static thread_local float of = 0.f;
+    if (of == base) return t;
+    of = base;
     for (int i = 0; i < kPagedDh / 2; ++i)
         t.r[i] = (uint64_t)llrint(pow((double)base, -2.0 * i / (double)kPagedDh) /
                                   6.283185307179586 * 9223372036854775808.0)
@@ -328,20 +333,25 @@ constexpr int kPlanThreads = 1024;
 
 __global__ void __launch_bounds__(kPlanThreads)
 k_paged_plan(int T, const PageView pv, const int32_t *__restrict__ seq,
-             const int32_t *__restrict__ pos, const PagedList l) {
+             const int32_t *__restrict__ pos, const PagedList l, const PlanArgs pa) {
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
     __shared__ long long sums[kPlanThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < kPagedMaxCtas; i += kPlanThreads) l.count[i] = 0;
-    const int n = T;
+    int n = T;
+    if (pa.plan.head) {  // only those that no tile holds
+        plan_attention<kPlanThreads>(T, pa);
+        __syncthreads();
+        n = pa.plan.head->n_left;
+    }
     long long run = 0;
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
         const int i = i0 + tid;
         int nt = 0;
         if (i < n) {
-            const int t = i, p = pos[t];
-            l.list[i] = t;
+            const int t = pa.plan.head ? pa.plan.left[i] : i, p = pos[t];
+            if (!pa.plan.head) l.list[i] = t;
             nt = pv.inside(seq[t], p) ? p / kPagedTile + 1 : 1;
         }
         long long v = nt;
@@ -381,7 +391,7 @@ moe_status cuda_status(cudaError_t e) { return e == cudaSuccess ? MOE_OK : MOE_E
 
 // Workspace of moe_paged_attend.
 struct PagedWs {
-    size_t n_list, count, list, before, part, total;
+    size_t n_list, count, list, before, head, tiles, part, total;
 };
 
 PagedWs paged_ws(int64_t T) {
@@ -392,6 +402,8 @@ PagedWs paged_ws(int64_t T) {
     L.count = o; o += up(kPagedMaxCtas * 4);
     L.list = o; o += up((size_t)T * 4);
     L.before = o; o += up(((size_t)T + 1) * 8);
+    L.head = o; o += up(sizeof(AttnPlanHead));
+    L.tiles = o; o += up((size_t)(T / kAttnTileMinRows) * sizeof(int4));
     L.part = o; o += up(kPagedPartFloats * 4);
     L.total = o;
     return L;
@@ -402,18 +414,29 @@ P *at(void *ws, size_t off) {
     return reinterpret_cast<P *>(static_cast<char *>(ws) + off);
 }
 
+// Whether a call's tokens are sorted into tiles and the rest (as in attn.cu).
+constexpr int kPagedPlanTokens = 48;  // beyond one for each sequence
+bool planned(int T, int n_seq) { return T >= kAttnTile || T - n_seq >= kPagedPlanTokens; }
+
 cudaError_t attend(const PagedAttn &a, void *ws, cudaStream_t st) {
     const PagedWs L = paged_ws(a.T);
     PagedList l{at<int>(ws, L.n_list), at<int>(ws, L.list), at<long long>(ws, L.before),
                 at<int>(ws, L.count)};
+    PlanArgs pa{a.seq, a.pos, a.pv.n_seq, a.pv.max_pages << a.pv.shift, {}};
+    if (planned(a.T, a.pv.n_seq))
+        pa.plan = AttnPlan{at<AttnPlanHead>(ws, L.head), at<int4>(ws, L.tiles), l.list};
     {
         int T = a.T;
         PageView pv = a.pv;
         const int32_t *seq = a.seq, *pos = a.pos;
-        void *args[] = {&T, &pv, &seq, &pos, &l};
+        void *args[] = {&T, &pv, &seq, &pos, &l, &pa};
         LaunchScope ls("paged_plan", st);
         cudaError_t e =
             launch_pdl((const void *)k_paged_plan, dim3(1), dim3(kPlanThreads), 0, st, args);
+        if (e != cudaSuccess) return e;
+    }
+    if (pa.plan.head) {
+        cudaError_t e = launch_paged_prefill_tc(a, pa.plan, st);
         if (e != cudaSuccess) return e;
     }
     return launch_paged_decode_tc(a, l, at<float>(ws, L.part), st);

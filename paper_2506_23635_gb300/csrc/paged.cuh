@@ -78,6 +78,8 @@ struct PagedAttn {
     void *ctx;
 };
 // Attention of the listed tokens over the 8-bit cache (paged_decode_tc.cu).
+// Attention of the plan's tiles (paged_prefill_tc.cu).
+cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, cudaStream_t st);
 cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part,
                                    cudaStream_t st);
 

@@ -1,0 +1,564 @@
+// Causal attention of prefill tiles over the paged 8-bit cache on the tcgen05
+// tensor cores.
+//
+// Tiles and units are those of attn_tc.cu: a tile is 16 to 128 consecutive
+// positions p0 .. p0 + rows - 1 of one sequence, a unit a (tile, pair of query
+// heads of one key/value head) over cache positions 0 .. p0 + rows - 1, taken by
+// one CTA an SM from a counter, longest first; the two heads share every key and
+// value tile of 128 positions and take turns on the tensor cores.
+//
+// 128 queries share a tile, so its e4m3 numbers are decoded once, to fp16, which
+// holds them exactly (half an instruction and four bytes of shared-memory traffic
+// each, against 2 x 256 multiply-adds); queries scaled by a power of two (the largest
+// of a row in [2^14, 2^15)) are exact in fp16 too, and so is what the products S =
+// Q K^T are made of.  A score is multiplied with its key page's scale, a
+// probability with its value page's, before it is rounded to fp16: 2^-11 of it, one
+// term, where bf16 would need two.  The row sum takes the probability itself.
+//
+//   warp 0      tensor memory (per head a score tile S and an output tile O of
+//               128 columns) and the MMAs: per head S_j = Q K_j^T, and once
+//               P_j has taken S_j's place, O += P_j V_j with P_j read from tensor
+//               memory and V_j MN-major as it lies;
+//   warp 1      key rows from their pages (16 bytes a lane, 16 loads in flight),
+//               decoded and written with the 128-byte swizzle into two stages; the
+//               tile's scales;
+//   warp 2      the same for value rows (rows past the tile's last query and of
+//               pages outside the pool are zeros);
+//   warps 4-7   head A, 8-11 head B: first their queries, then the online softmax,
+//               one thread per query row and all 128 columns; the exponent base
+//               moves only when a value passes it by more than 8.
+//
+// Every wait is bounded (ptx.cuh); a CTA one of whose waits gave up ends.
+#include <math.h>
+#include <stddef.h>
+
+#include <algorithm>
+
+#include <cuda_fp16.h>
+
+#include "paged.cuh"
+#include "tc.cuh"
+
+namespace moe {
+namespace {
+
+using namespace tc;
+
+constexpr int kPfRows = 128;
+constexpr int kPfThreads = 12 * 32;
+constexpr int kPfHeadWarp = 4;  // first softmax warp
+constexpr uint32_t kPfHalf = kPfRows * 128;  // 64 columns of a tile: 16 KB
+constexpr uint32_t kPfTile = 2 * kPfHalf;
+constexpr uint32_t kPfOffQ = 0;
+constexpr uint32_t kPfOffK = 2 * kPfTile;
+constexpr uint32_t kPfOffV = 4 * kPfTile;
+constexpr uint32_t kPfOffHdr = 6 * kPfTile;
+constexpr uint32_t kPfHdrBytes = 1024;
+constexpr size_t kPfSmem = 1024 + kPfOffHdr + kPfHdrBytes;
+static_assert(kPfSmem <= 227 * 1024, "shared memory");
+// kind::f16: fp16 A and B, fp32 D, M = N = 128; and with B MN-major (bit 16)
+constexpr uint32_t kPfIdesc = (1u << 4) | ((uint32_t)(kPfRows >> 3) << 17) | ((uint32_t)(kPfRows >> 4) << 24);
+constexpr uint32_t kPfIdescV = kPfIdesc | (1u << 16);
+constexpr uint32_t kPfTmemCols = 512, kPfColS = 0, kPfColO = 256;
+// probabilities are 2^kPfTop at the exponent base, at most 2^15 where it lags,
+// and keep their 11 bits down to 2^-21 of it (2^-32 in the end)
+constexpr float kPfTop = 7.f, kPfSlack = 8.f;
+constexpr float kPfNone = -1e30f;
+constexpr int kPfRing = 4;
+
+struct PfScales {
+    float ks[8], vs[8], lv[8];  // of 16 positions each; log2 of vs
+    unsigned ok;                // bit i: positions 16 i .. of a page inside the pool
+    int pad[7];
+};
+
+struct PfHeader {
+    uint64_t q_full[2];    // a head's queries written (four warps)
+    uint64_t k_full[2], k_empty[2];
+    uint64_t v_full[2], v_empty[2];
+    uint64_t t_full[kPfRing];  // a tile's scales written
+    uint64_t s_full[2], p_ready[2], o_full[2];  // per head
+    uint64_t done;
+    uint32_t tmem_base;
+    int next;
+    int gave_up;
+    alignas(16) PfScales sc[kPfRing];
+};
+constexpr int kPfBars = (int)((offsetof(PfHeader, done) - offsetof(PfHeader, q_full)) / 8) + 1;
+constexpr int kPfBarP = (int)((offsetof(PfHeader, p_ready) - offsetof(PfHeader, q_full)) / 8);
+static_assert(sizeof(PfHeader) <= kPfHdrBytes, "header");
+
+__device__ __forceinline__ bool pf_wait(uint64_t *bar, uint32_t parity, unsigned *err) {
+    return ptx::mbar_try_wait(bar, parity) || ptx::mbar_wait_hint(bar, parity, err);
+}
+// a whole warp's
+__device__ __forceinline__ bool pf_wait_all(uint64_t *bar, uint32_t parity, unsigned *err) {
+    return __all_sync(0xffffffffu, pf_wait(bar, parity, err));
+}
+
+__device__ __forceinline__ float pf_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// MN-major, 128-byte swizzle: 8 k 1024 bytes apart, the next 64 MN elements
+// 16 KB on.
+__device__ __forceinline__ uint64_t pf_desc_mn(uint32_t saddr) {
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(kPfHalf >> 4) << 16) |
+           ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+
+__device__ __forceinline__ void pf_issue_qk(uint32_t d, uint32_t q, uint32_t k) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const uint64_t ad = smem_desc(q + half * kPfHalf), bd = smem_desc(k + half * kPfHalf);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)  // (kind::f16: the types are the descriptor's)
+            mma_bf16(d, ad + 2 * kk, bd + 2 * kk, kPfIdesc, (half | kk) != 0 ? 1u : 0u);
+    }
+}
+
+__device__ __forceinline__ void pf_issue_pv(uint32_t d, uint32_t p_tmem, uint32_t v, bool add) {
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+            "r"(p_tmem + ks * 8), "l"(pf_desc_mn(v + ks * 16 * 128)), "r"(kPfIdescV),
+            "r"((add || ks != 0) ? 1u : 0u));
+}
+
+__device__ __forceinline__ void pf_tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+        "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]),
+        "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
+        "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]),
+        "r"(v[29]), "r"(v[30]), "r"(v[31])
+        : "memory");
+}
+__device__ __forceinline__ void pf_tmem_st_wait() {
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+struct PfArgs {
+    int Hq, Hkv;
+    PageView pv;
+    AttnPlan plan;
+    const bf16 *q;
+    const uint8_t *kp, *vp;
+    const float *ks, *vs;
+    bf16 *ctx;
+    unsigned *err;
+};
+
+struct PfUnit {
+    int t0, rows, p0, sq;  // the tile: first token, tokens, position, sequence
+    int g, h0, nh, n_kv;   // key/value head, first query head, heads, position tiles
+};
+
+// Rows of 128 positions from their pages into one operand's two stages; KEYS:
+// and the tiles' scales.  False: a wait gave up.
+template <bool KEYS>
+__device__ __forceinline__ bool pf_feed(const PfArgs &a, PfHeader *hd, unsigned char *smem,
+                                        const PfUnit &u) {
+    const int lane = threadIdx.x & 31;
+    const int shift = a.pv.shift, per = kPfRows >> shift;
+    const int last = u.p0 + u.rows - 1;
+    const uint8_t *src = KEYS ? a.kp : a.vp;
+    uint64_t *full = KEYS ? hd->k_full : hd->v_full, *empty = KEYS ? hd->k_empty : hd->v_empty;
+    unsigned char *ring = smem + (KEYS ? kPfOffK : kPfOffV);
+    auto page = [&](int j) {  // lane i: the tile's page i
+        const int p = j * kPfRows + (lane << shift);
+        return lane < per && p <= last ? a.pv.page(u.sq, p >> shift) : -1;
+    };
+    int pg = page(0);
+#pragma unroll 1
+    for (int j = 0; j < u.n_kv; ++j) {
+        const int b = j & 1;
+        if (KEYS) {
+            const int p = j * kPfRows + (lane << shift);
+            if (lane < per && p <= last && pg < 0) set_error(a.err, kErrIndex);
+        }
+        // the scales of 16 positions a lane (KEYS)
+        const int mine = __shfl_sync(0xffffffffu, pg, ((lane & 7) << 4) >> shift);
+        float ks = 0.f, vs = 0.f;
+        if (KEYS && lane < 8 && mine >= 0) {
+            ks = __ldg(a.ks + (size_t)mine * a.Hkv + u.g);
+            vs = __ldg(a.vs + (size_t)mine * a.Hkv + u.g);
+        }
+        const int pg1 = j + 1 < u.n_kv ? page(j + 1) : -1;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            uint4 w[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int row = half * 64 + k * 4 + (lane >> 3);
+                const int rp = __shfl_sync(0xffffffffu, pg, row >> shift);
+                w[k] = make_uint4(0u, 0u, 0u, 0u);
+                if (rp >= 0 && j * kPfRows + row <= last)
+                    w[k] = ld_stream16(src +
+                                       ((((size_t)rp * a.Hkv + u.g) << shift) +
+                                        (row & ((1 << shift) - 1))) * kPagedDh +
+                                       (lane & 7) * 16);
+            }
+            if (half == 0 && !pf_wait_all(&empty[b], ((uint32_t)(j >> 1) & 1u) ^ 1u, a.err))
+                return false;
+            // dims 16 c .. of a row: chunks 2c, 2c + 1 of its 64-dim half's row
+            unsigned char *box = ring + b * kPfTile + ((lane & 7) >> 2) * kPfHalf;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int row = half * 64 + k * 4 + (lane >> 3);
+                const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+                uint32_t y[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    y[2 * i] = e4m3x2_to_f16x2(x[i] & 0xffffu);
+                    y[2 * i + 1] = e4m3x2_to_f16x2(x[i] >> 16);
+                }
+                unsigned char *rowp = box + row * 128;
+                const uint32_t c = (lane & 3) * 2;
+                *reinterpret_cast<uint4 *>(rowp + ((c ^ (row & 7)) << 4)) =
+                    make_uint4(y[0], y[1], y[2], y[3]);
+                *reinterpret_cast<uint4 *>(rowp + (((c + 1) ^ (row & 7)) << 4)) =
+                    make_uint4(y[4], y[5], y[6], y[7]);
+            }
+        }
+        if (KEYS) {
+            PfScales *s = &hd->sc[j % kPfRing];
+            if (lane < 8) {
+                s->ks[lane] = ks;
+                s->vs[lane] = vs;
+                s->lv[lane] = log2f(fmaxf(vs, 7.888609052210118e-31f));  // 2^-100 at least
+            }
+            const unsigned ok = __ballot_sync(0xffffffffu, lane < 8 && mine >= 0);
+            if (lane == 0) s->ok = ok;
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            if (KEYS) ptx::mbar_arrive(&hd->t_full[j % kPfRing]);
+            ptx::mbar_arrive(&full[b]);
+        }
+        pg = pg1;
+    }
+    return true;
+}
+
+// The MMA issuer's part of a unit.  False: a wait gave up.
+__device__ __forceinline__ bool pf_issue(PfHeader *hd, uint32_t sbase, uint32_t tmem,
+                                         const PfUnit &u, unsigned *err) {
+    bool good = pf_wait(&hd->k_full[0], 0, err);
+    for (int x = 0; x < u.nh && good; ++x) {
+        if (!(good = pf_wait(&hd->q_full[x], 0, err))) break;
+        tc_fence_after();
+        pf_issue_qk(tmem + kPfColS + x * 128, sbase + kPfOffQ + x * kPfTile, sbase + kPfOffK);
+        mma_commit(&hd->s_full[x]);
+    }
+    if (good) mma_commit(&hd->k_empty[0]);
+    for (int j = 0; j < u.n_kv && good; ++j) {
+        const int b = j & 1;
+        if (!(good = pf_wait(&hd->v_full[b], (uint32_t)(j >> 1) & 1u, err))) break;
+        for (int x = 0; x < u.nh && good; ++x) {
+            if (!(good = pf_wait(&hd->p_ready[x], j & 1, err))) break;
+            tc_fence_after();
+            pf_issue_pv(tmem + kPfColO + x * 128, tmem + kPfColS + x * 128,
+                        sbase + kPfOffV + b * kPfTile, j != 0);
+            mma_commit(&hd->o_full[x]);
+            if (x == u.nh - 1) mma_commit(&hd->v_empty[b]);
+            if (j + 1 < u.n_kv) {
+                // S_{j+1} replaces P_j: only after P_j V_j has finished
+                const int b1 = (j + 1) & 1;
+                if (!(good = pf_wait(&hd->o_full[x], j & 1, err))) break;
+                if (x == 0 && !(good = pf_wait(&hd->k_full[b1], (uint32_t)((j + 1) >> 1) & 1u, err)))
+                    break;
+                tc_fence_after();
+                pf_issue_qk(tmem + kPfColS + x * 128, sbase + kPfOffQ + x * kPfTile,
+                            sbase + kPfOffK + b1 * kPfTile);
+                mma_commit(&hd->s_full[x]);
+                if (x == u.nh - 1) mma_commit(&hd->k_empty[b1]);
+            }
+        }
+    }
+    return good;
+}
+
+// Row r of head x's queries: scaled to fp16 in shared memory; what its scores
+// are to be multiplied with.
+__device__ __forceinline__ float pf_queries(const PfArgs &a, unsigned char *smem, const PfUnit &u,
+                                            int x, int r) {
+    uint4 w[16];
+    const bool in = r < u.rows;
+    const uint4 *src = reinterpret_cast<const uint4 *>(
+        a.q + ((size_t)(u.t0 + (in ? r : 0)) * a.Hq + u.h0 + x) * kPagedDh);
+    uint32_t mb = 0;
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+        w[c] = in ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+        // the larger magnitude of a pair of bf16
+        const uint32_t v[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mb = max(mb, max(v[i] & 0x7fff0000u, (v[i] & 0x7fffu) << 16));
+    }
+    const int e = min(max((int)(mb >> 23), 15), 254);
+    const float up = __uint_as_float((uint32_t)(254 + 14 - e) << 23);
+    unsigned char *q = smem + kPfOffQ + x * kPfTile + r * 128;
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+        const uint32_t v[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float lo, hi;
+            unpack_bf16x2(v[i], lo, hi);
+            y[i] = f16x2(lo * up, hi * up);
+        }
+        *reinterpret_cast<uint4 *>(q + (c >> 3) * kPfHalf + (((c & 7) ^ (r & 7)) << 4)) =
+            make_uint4(y[0], y[1], y[2], y[3]);
+    }
+    // log2(e) / sqrt(128)
+    return 0.12751743f * __uint_as_float((uint32_t)(e - 14) << 23);
+}
+
+// One row's softmax over a unit's tiles; l: the row sum.
+__device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_t o_col,
+                                           const PfUnit &u, int r, int x, float qs, float &l,
+                                           unsigned *err) {
+    const int lane = threadIdx.x & 31;
+    float m = kPfNone;
+    l = 0.f;
+    bool good = true;
+#pragma unroll 1
+    for (int j = 0; j < u.n_kv; ++j) {
+        const int lim = u.p0 + r - j * kPfRows;  // the row's last position in the tile
+        good = good && pf_wait_all(&hd->t_full[j % kPfRing], (uint32_t)(j / kPfRing) & 1u, err);
+        good = good && pf_wait_all(&hd->s_full[x], j & 1, err);
+        tc_fence_after();
+        float v[128];
+#pragma unroll
+        for (int c = 0; c < 128; c += 32)
+            tmem_ld32(s_col + c, *reinterpret_cast<float(*)[32]>(&v[c]));
+        tmem_ld_wait();
+        const PfScales *sc = &hd->sc[j % kPfRing];
+        const unsigned ok = sc->ok;
+        // (a tile holds no position past its last row's, so pages inside it are
+        // missing only there and where the table says nothing)
+        const bool full = j * kPfRows + kPfRows - 1 <= u.p0 && ok == 0xffu;
+        float mrow = kPfNone;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float m2[2] = {-INFINITY, -INFINITY};
+            if (full) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) m2[k & 1] = fmaxf(m2[k & 1], v[16 * i + k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 16; ++k)
+                    if (16 * i + k <= lim) m2[k & 1] = fmaxf(m2[k & 1], v[16 * i + k]);
+            }
+            const float mx = fmaxf(m2[0], m2[1]);
+            const float t = fmaf(mx, sc->ks[i] * qs, sc->lv[i]);
+            if (full || (16 * i <= lim && ((ok >> i) & 1u))) mrow = fmaxf(mrow, t);
+        }
+        const bool bump = mrow > m + kPfSlack;
+        const float corr = bump ? pf_exp2(m - mrow) : 1.f;
+        if (bump) m = mrow;
+        const float2 nm2 = make_float2(kPfTop - m, kPfTop - m);
+        float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            uint32_t pw[32];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int gi = half * 4 + i;
+                const float c1 = sc->ks[gi] * qs, v1 = sc->vs[gi];
+                const float2 c2 = make_float2(c1, c1), v2 = make_float2(v1, v1);
+                const bool page = (ok >> gi) & 1u;
+#pragma unroll
+                for (int k = 0; k < 16; k += 2) {
+                    const int c = 16 * gi + k;
+                    const float2 e = __ffma2_rn(make_float2(v[c], v[c + 1]), c2, nm2);
+                    float2 p = make_float2(pf_exp2(e.x), pf_exp2(e.y));
+                    if (!full) {
+                        if (c > lim || !page) p.x = 0.f;
+                        if (c + 1 > lim || !page) p.y = 0.f;
+                    }
+                    sum2[(k >> 1) & 1] = __fadd2_rn(sum2[(k >> 1) & 1], p);
+                    const float2 w = __fmul2_rn(p, v2);
+                    pw[i * 8 + (k >> 1)] = f16x2(w.x, w.y);
+                }
+            }
+            pf_tmem_st32(s_col + half * 32, pw);
+        }
+        // a new base rescales O: P_{j-1} V_{j-1} finished before S_j was issued,
+        // and P_j V_j waits for this warp's arrival
+        if (j >= 1 && __any_sync(0xffffffffu, bump) && good) {
+#pragma unroll 1
+            for (int c = 0; c < 128; c += 32) {
+                float ov[32];
+                uint32_t ow[32];
+                tmem_ld32(o_col + c, ov);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) ow[i] = __float_as_uint(ov[i] * corr);
+                pf_tmem_st32(o_col + c, ow);
+            }
+        }
+        pf_tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&hd->p_ready[x]);
+        l = l * corr + ((sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y));
+    }
+    return good;
+}
+
+// 384 threads: three warps a scheduler, so at most 168 registers a thread
+__global__ void __launch_bounds__(kPfThreads, 1)
+k_paged_prefill_tc(const PfArgs a) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = reinterpret_cast<unsigned char *>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    PfHeader *hd = reinterpret_cast<PfHeader *>(smem + kPfOffHdr);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int G = a.Hq / a.Hkv, pairs = (G + 1) / 2;
+    const uint32_t sbase = ptx::smem_u32(smem);
+    unsigned *err = a.err;
+
+    ptx::grid_dependency_wait();
+    ptx::launch_dependents();
+    const int n_tiles = __ldcg(&a.plan.head->n_tiles), n_left = __ldcg(&a.plan.head->n_left);
+    // few tiles: a unit holds one head, so that the longest is shorter
+    const bool single = n_left == 0 && 3 * n_tiles * a.Hq <= 4 * (int)gridDim.x;
+    const int per = single ? G : pairs;
+    const int n_units = n_tiles * a.Hkv * per;
+    int unit = (int)blockIdx.x;
+    if (unit >= n_units) return;
+    if (threadIdx.x == 0) hd->gave_up = 0;
+    if (warp == 0) tmem_alloc(&hd->tmem_base, kPfTmemCols);
+
+#pragma unroll 1
+    for (bool again = false;; again = true) {
+        if (threadIdx.x == 0) {
+            uint64_t *bars = hd->q_full;
+            if (again)
+                for (int i = 0; i < kPfBars; ++i) ptx::mbar_inval(bars + i);
+            for (int i = 0; i < kPfBars; ++i)
+                ptx::mbar_init(bars + i, i < 2 || (i >= kPfBarP && i < kPfBarP + 2) ? 4 : 1);
+            ptx::fence_barrier_init();
+        }
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        const uint32_t tmem = hd->tmem_base;
+        const int tile = unit / (a.Hkv * per), gp = unit - tile * a.Hkv * per;
+        const int4 td = __ldcg(&a.plan.tiles[tile]);
+        PfUnit u;
+        u.g = gp / per;
+        const int hp = gp - u.g * per;
+        u.h0 = u.g * G + (single ? hp : 2 * hp);
+        u.nh = !single && 2 * hp + 1 < G ? 2 : 1;
+        u.t0 = td.x;
+        u.rows = td.y;
+        u.p0 = td.z;
+        u.sq = td.w;
+        u.n_kv = (u.p0 + u.rows - 1) / kPfRows + 1;
+
+        if (warp == 0) {
+            if (lane == 0) {
+                bool good = pf_issue(hd, sbase, tmem, u, err);
+                mma_commit(&hd->done);
+                good &= pf_wait(&hd->done, 0, err);
+                // the MMAs' last arrivals, before the barriers start anew
+                for (int j = max(0, u.n_kv - 2); good && j < u.n_kv; ++j)
+                    good = pf_wait(&hd->k_empty[j & 1], (uint32_t)(j >> 1) & 1u, err) &&
+                           pf_wait(&hd->v_empty[j & 1], (uint32_t)(j >> 1) & 1u, err);
+                if (!good) hd->gave_up = 1;
+            }
+            __syncwarp();
+        } else if (warp == 1) {
+            const bool good = pf_feed<true>(a, hd, smem, u);
+            if (lane == 0) {
+                hd->next = (int)gridDim.x + atomicAdd(&a.plan.head->next, 1);
+                if (!good) hd->gave_up = 1;
+            }
+        } else if (warp == 2) {
+            const bool good = pf_feed<false>(a, hd, smem, u);
+            if (lane == 0 && !good) hd->gave_up = 1;
+        } else if (warp >= kPfHeadWarp && (warp - kPfHeadWarp) / 4 < u.nh) {
+            const int x = (warp - kPfHeadWarp) / 4;
+            const int q = warp & 3, r = q * 32 + lane;
+            const uint32_t lane_base = (uint32_t)(q * 32) << 16;
+            const uint32_t s_col = tmem + lane_base + kPfColS + (uint32_t)x * 128;
+            const uint32_t o_col = tmem + lane_base + kPfColO + (uint32_t)x * 128;
+            const float qs = pf_queries(a, smem, u, x, r);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&hd->q_full[x]);
+            float l = 0.f;
+            bool good = pf_softmax(hd, s_col, o_col, u, r, x, qs, l, err);
+            good = good && pf_wait_all(&hd->o_full[x], (u.n_kv - 1) & 1, err);
+            if (!good) hd->gave_up = 1;
+            if (good) {
+                tc_fence_after();
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                bf16 *dst = a.ctx + ((size_t)(u.t0 + r) * a.Hq + u.h0 + x) * kPagedDh;
+#pragma unroll
+                for (int c = 0; c < 128; c += 32) {
+                    float vv[32];
+                    tmem_ld32(o_col + c, vv);
+                    tmem_ld_wait();
+                    if (r >= u.rows) continue;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const __nv_bfloat162 p2 = __floats2bfloat162_rn(
+                                vv[i + 2 * e] * inv, vv[i + 2 * e + 1] * inv);
+                            w[e] = *reinterpret_cast<const uint32_t *>(&p2);
+                        }
+                        *reinterpret_cast<uint4 *>(dst + c + i) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+            }
+        }
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        unit = hd->next;
+        if (unit >= n_units || hd->gave_up) break;
+        __syncthreads();  // (read by all before the next unit's)
+    }
+    if (warp == 0) tmem_dealloc(hd->tmem_base, kPfTmemCols);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, cudaStream_t st) {
+    const void *kern = (const void *)k_paged_prefill_tc;
+    cudaError_t e =
+        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPfSmem);
+    if (e != cudaSuccess) return e;
+    PfArgs pa{a.Hq, a.Hkv, a.pv, plan, static_cast<const bf16 *>(a.q),
+              static_cast<const uint8_t *>(a.kp), static_cast<const uint8_t *>(a.vp), a.ks, a.vs,
+              static_cast<bf16 *>(a.ctx), device_info().err};
+    void *args[] = {&pa};
+    const long long most = (long long)a.Hq * (a.T / kAttnTileMinRows);
+    LaunchScope ls("paged_prefill_tc", st);
+    return launch_pdl(
+        kern, dim3((unsigned)std::max(1LL, std::min<long long>(most, device_info().sm_count))),
+        dim3(kPfThreads), kPfSmem, st, args);
+}
+
+}  // namespace moe

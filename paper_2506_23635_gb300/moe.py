@@ -8,7 +8,6 @@ import of the library raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -503,22 +502,35 @@ class PagedCache:
     """A paged e4m3 cache (include/moe.h, moe_paged_dims): ``k_pages`` and
     ``v_pages`` [n_pages, Hkv, page_size, 128] float8_e4m3fn, ``k_scale`` and
     ``v_scale`` [n_pages, Hkv] float32, ``page_table`` [n_seq, max_pages]
-    int32.  The tensors are the caller's; the table may be rewritten between
-    calls (``page_table`` may be given anew for another batch of sequences)."""
+    int32.  The tensors are the caller's; their contents may change between
+    calls, and ``page_table`` may be set to another tensor (a batch of other
+    sequences)."""
 
     def __init__(self, k_pages, v_pages, k_scale, v_scale, page_table):
         n_pages, n_kv, page_size, dh = k_pages.shape
-        _want(k_pages, (n_pages, n_kv, page_size, dh), torch.float8_e4m3fn, "k_pages")
-        _want(v_pages, (n_pages, n_kv, page_size, dh), torch.float8_e4m3fn, "v_pages")
-        _want(k_scale, (n_pages, n_kv), torch.float32, "k_scale")
-        _want(v_scale, (n_pages, n_kv), torch.float32, "v_scale")
-        if page_table.dim() != 2:
-            raise ValueError("page_table must be [n_seq, max_pages]")
-        _want(page_table, tuple(page_table.shape), torch.int32, "page_table")
+        self.device_index = k_pages.get_device()
+        self.n_kv_heads, self.head_dim = n_kv, dh
+        shape, dev = (n_pages, n_kv, page_size, dh), self.device_index
+        _want(k_pages, shape, torch.float8_e4m3fn, dev, "k_pages")
+        _want(v_pages, shape, torch.float8_e4m3fn, dev, "v_pages")
+        _want(k_scale, (n_pages, n_kv), torch.float32, dev, "k_scale")
+        _want(v_scale, (n_pages, n_kv), torch.float32, dev, "v_scale")
         self.k_pages, self.v_pages = k_pages, v_pages
         self.k_scale, self.v_scale = k_scale, v_scale
+        self.page_size, self.n_pages = page_size, n_pages
         self.page_table = page_table
-        self.dims = PagedDims(page_size, n_pages, *page_table.shape)
+
+    @property
+    def page_table(self):
+        return self._page_table
+
+    @page_table.setter
+    def page_table(self, page_table):
+        if page_table.dim() != 2:
+            raise ValueError("page_table must be [n_seq, max_pages]")
+        _want(page_table, page_table.shape, torch.int32, self.device_index, "page_table")
+        self._page_table = page_table
+        self.dims = PagedDims(self.page_size, self.n_pages, *page_table.shape)
 
     @staticmethod
     def alloc(a: SaDims, page_size: int, n_pages: int, page_table) -> "PagedCache":
@@ -530,36 +542,34 @@ class PagedCache:
         scales = [torch.ones(shape[:2], dtype=torch.float32, device=dev) for _ in range(2)]
         return PagedCache(*pages, *scales, page_table)
 
-    def _args(self, a: SaDims, T: int, seq, pos):
-        """Checks a call's tokens against the cache; the tensors of the call."""
-        if (self.dims.n_seq, self.dims.max_pages) != tuple(self.page_table.shape):
-            self.dims = PagedDims(self.dims.page_size, self.dims.n_pages, *self.page_table.shape)
-        if self.k_pages.shape[1] != a.n_kv_heads or self.k_pages.shape[3] != a.head_dim:
+    def _call(self, a: SaDims, T: int, seq, pos, stream) -> int:
+        """Checks a call's tokens against the cache; the stream it goes to."""
+        if self.n_kv_heads != a.n_kv_heads or self.head_dim != a.head_dim:
             raise ValueError("the cache's heads are not those of the dims")
-        _want(seq, (T,), torch.int32, "seq")
-        _want(pos, (T,), torch.int32, "pos")
-        _want(self.page_table, (self.dims.n_seq, self.dims.max_pages), torch.int32, "page_table")
-        return (self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.page_table, seq, pos)
+        dev = self.device_index
+        _want(seq, (T,), torch.int32, dev, "seq")
+        _want(pos, (T,), torch.int32, dev, "pos")
+        if dev != torch.cuda.current_device():
+            raise ValueError(f"the cache is on device {dev}, which is not the current one")
+        if stream is None:
+            return torch.cuda.current_stream(dev).cuda_stream
+        if stream.device_index != dev:
+            raise ValueError(f"the stream is not of the cache's device {dev}")
+        return stream.cuda_stream
 
 
-def _want(t, shape, dtype, what: str):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        raise ValueError(f"{what} must be {dtype} {tuple(shape)}, is {t.dtype} {tuple(t.shape)}")
+def _want(t, shape, dtype, device: int, what: str):
+    if t.shape != shape or t.dtype != dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous {dtype} {tuple(shape)} on device {device}, is "
+                         f"{t.dtype} {tuple(t.shape)} (strides {t.stride()}) on {t.device}")
 
 
-def _one_device(tensors, stream):
-    """The call's tensors lie on one CUDA device, and it is the one that the
-    launches go to: the current one, with a stream of its own."""
-    dev = torch.device("cuda", torch.cuda.current_device())
-    if any(t.device != dev for t in tensors):
-        raise ValueError(f"tensors must be on the current device {dev}")
-    if stream is not None and stream.device != dev:
-        raise ValueError(f"the stream must be of the current device {dev}")
-
-
-def _on(stream):
+def _new(shape, dtype, device, stream):
     """Memory that a call allocates itself belongs to the stream that uses it."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def paged_workspace_size(a: SaDims, max_tokens: int) -> int:
@@ -578,39 +588,42 @@ def paged_append(a: SaDims, cache: PagedCache, qkv, seq, pos, q=None, stream=Non
     """Rotated queries q [T, Hq, 128] (bf16) of the projection's rows qkv
     [T, (Hq + 2 Hkv) 128] (bf16 or fp32); the T tokens' rotated keys and
     their values quantised into the cache's pages at (seq[t], pos[t])."""
-    T = qkv.shape[0]
-    args = cache._args(a, T, seq, pos)
+    T, dev = qkv.shape[0], cache.device_index
     if qkv.dtype not in _DT:
         raise ValueError("qkv must be bf16 or fp32")
-    _want(qkv, (T, (a.n_heads + 2 * a.n_kv_heads) * a.head_dim), qkv.dtype, "qkv")
-    with _on(stream):
-        if q is None:
-            q = torch.empty((T, a.n_heads, a.head_dim), dtype=torch.bfloat16, device=qkv.device)
-    _want(q, (T, a.n_heads, a.head_dim), torch.bfloat16, "q")
-    _one_device((*args, qkv, q), stream)
+    _want(qkv, (T, (a.n_heads + 2 * a.n_kv_heads) * a.head_dim), qkv.dtype, dev, "qkv")
+    if q is not None:
+        _want(q, (T, a.n_heads, a.head_dim), torch.bfloat16, dev, "q")
+    st = cache._call(a, T, seq, pos, stream)
+    if q is None:
+        q = _new((T, a.n_heads, a.head_dim), torch.bfloat16, qkv.device, stream)
     c = cache
-    _check(lib().moe_paged_append(ctypes.byref(a), ctypes.byref(c.dims), T, _ptr(qkv),
-                                  _DT[qkv.dtype], _ptr(seq), _ptr(pos), _ptr(c.page_table),
-                                  _ptr(q), _ptr(c.k_pages), _ptr(c.v_pages), _ptr(c.k_scale),
-                                  _ptr(c.v_scale), _stream(stream)), "moe_paged_append")
+    _check(lib().moe_paged_append(a, c.dims, T, qkv.data_ptr(), _DT[qkv.dtype], seq.data_ptr(),
+                                  pos.data_ptr(), c._page_table.data_ptr(), q.data_ptr(),
+                                  c.k_pages.data_ptr(), c.v_pages.data_ptr(),
+                                  c.k_scale.data_ptr(), c.v_scale.data_ptr(), st),
+           "moe_paged_append")
     return q
 
 
 def paged_attend(a: SaDims, cache: PagedCache, q, seq, pos, ctx=None, ws=None, stream=None):
     """ctx [T, Hq * 128] (bf16): causal attention of the queries q
     [T, Hq, 128] (bf16) over positions 0..pos[t] of their sequences."""
-    T = q.shape[0]
-    args = cache._args(a, T, seq, pos)
-    _want(q, (T, a.n_heads, a.head_dim), torch.bfloat16, "q")
-    with _on(stream):
-        if ctx is None:
-            ctx = torch.empty((T, a.n_heads * a.head_dim), dtype=torch.bfloat16, device=q.device)
-        ws = paged_alloc_workspace(a, T, q.device) if ws is None else ws
-    _want(ctx, (T, a.n_heads * a.head_dim), torch.bfloat16, "ctx")
-    _one_device((*args, q, ctx, ws), stream)
+    T, dev = q.shape[0], cache.device_index
+    _want(q, (T, a.n_heads, a.head_dim), torch.bfloat16, dev, "q")
+    if ctx is not None:
+        _want(ctx, (T, a.n_heads * a.head_dim), torch.bfloat16, dev, "ctx")
+    if ws is not None:
+        _want(ws, ws.shape, torch.uint8, dev, "ws")
+    st = cache._call(a, T, seq, pos, stream)
+    if ctx is None:
+        ctx = _new((T, a.n_heads * a.head_dim), torch.bfloat16, q.device, stream)
+    if ws is None:
+        ws = _new((paged_workspace_size(a, T),), torch.uint8, q.device, stream)
     c = cache
-    _check(lib().moe_paged_attend(ctypes.byref(a), ctypes.byref(c.dims), T, _ptr(q), _ptr(seq),
-                                  _ptr(pos), _ptr(c.page_table), _ptr(c.k_pages),
-                                  _ptr(c.v_pages), _ptr(c.k_scale), _ptr(c.v_scale), _ptr(ctx),
-                                  _ptr(ws), ws.numel(), _stream(stream)), "moe_paged_attend")
+    _check(lib().moe_paged_attend(a, c.dims, T, q.data_ptr(), seq.data_ptr(), pos.data_ptr(),
+                                  c._page_table.data_ptr(), c.k_pages.data_ptr(),
+                                  c.v_pages.data_ptr(), c.k_scale.data_ptr(),
+                                  c.v_scale.data_ptr(), ctx.data_ptr(), ws.data_ptr(), ws.numel(),
+                                  st), "moe_paged_attend")
     return ctx
