@@ -12,21 +12,22 @@
 // each, against 2 x 256 multiply-adds); queries scaled by a power of two (the largest
 // of a row in [2^14, 2^15)) are exact in fp16 too, and so is what the products S =
 // Q K^T are made of.  A score is multiplied with its key page's scale, a
-// probability with its value page's, before it is rounded to fp16: 2^-11 of it, one
-// term, where bf16 would need two.  The row sum takes the probability itself.
+// probability with its value page's (log2 of it in the exponent) before it is rounded
+// to fp16: 2^-11 of it, one term, where bf16 would need two.  The row sum takes the
+// probability itself.
 //
 //   warp 0      tensor memory (per head a score tile S and an output tile O of
 //               128 columns) and the MMAs: per head S_j = Q K_j^T, and once
 //               P_j has taken S_j's place, O += P_j V_j with P_j read from tensor
 //               memory and V_j MN-major as it lies;
-//   warp 1      key rows from their pages (16 bytes a lane, 16 loads in flight),
-//               decoded and written with the 128-byte swizzle into two stages; the
-//               tile's scales;
-//   warp 2      the same for value rows (rows past the tile's last query and of
+//   warps 1-3   key rows from their pages (16 bytes a lane), decoded and written
+//               with the 128-byte swizzle into two stages; the tile's scales;
+//   warps 4-7   the same for value rows (rows past the tile's last query and of
 //               pages outside the pool are zeros);
-//   warps 4-7   head A, 8-11 head B: first their queries, then the online softmax,
-//               one thread per query row and all 128 columns; the exponent base
-//               moves only when a value passes it by more than 8.
+//   warps 8-11  head A, 12-15 head B: first their queries, then the online
+//               softmax, one thread per query row and all 128 columns; the exponent
+//               base moves only when a value passes it by more than 8.  They
+//               take over registers from the others.
 //
 // Every wait is bounded (ptx.cuh); a CTA one of whose waits gave up ends.
 #include <math.h>
@@ -45,8 +46,13 @@ namespace {
 using namespace tc;
 
 constexpr int kPfRows = 128;
-constexpr int kPfThreads = 12 * 32;
-constexpr int kPfHeadWarp = 4;  // first softmax warp
+constexpr int kPfThreads = 16 * 32;
+constexpr int kPfKeyWarps = 3, kPfValueWarps = 4;  // warps 1-3, 4-7
+constexpr int kPfHeadWarp = 8;                     // first softmax warp
+// registers a thread: 512 x 128 at the launch, then two warpgroups each of
+// these (2 x 72 + 2 x 184 = 4 x 128)
+constexpr int kPfRegsFeed = 72, kPfRegsSoftmax = 184;
+static_assert(kPfRegsFeed + kPfRegsSoftmax == 2 * 128, "the launch's registers");
 constexpr uint32_t kPfHalf = kPfRows * 128;  // 64 columns of a tile: 16 KB
 constexpr uint32_t kPfTile = 2 * kPfHalf;
 constexpr uint32_t kPfOffQ = 0;
@@ -64,11 +70,14 @@ constexpr uint32_t kPfTmemCols = 512, kPfColS = 0, kPfColO = 256;
 // and keep their 11 bits down to 2^-21 of it (2^-32 in the end)
 constexpr float kPfTop = 7.f, kPfSlack = 8.f;
 constexpr float kPfNone = -1e30f;
+constexpr float kPfLeast = 7.888609052210118e-31f;  // 2^-100: nothing times a score
 constexpr int kPfRing = 4;
 
 struct PfScales {
-    float ks[8], vs[8], lv[8];  // of 16 positions each; log2 of vs
-    unsigned ok;                // bit i: positions 16 i .. of a page inside the pool
+    // of 16 positions each: the key page's scale, log2 and reciprocal of the
+    // value page's
+    float ks[8], lv[8], iv[8];
+    unsigned ok;  // bit i: positions 16 i .. of a page inside the pool
     int pad[7];
 };
 
@@ -85,7 +94,10 @@ struct PfHeader {
     alignas(16) PfScales sc[kPfRing];
 };
 constexpr int kPfBars = (int)((offsetof(PfHeader, done) - offsetof(PfHeader, q_full)) / 8) + 1;
-constexpr int kPfBarP = (int)((offsetof(PfHeader, p_ready) - offsetof(PfHeader, q_full)) / 8);
+constexpr int pf_bar(size_t off) { return (int)((off - offsetof(PfHeader, q_full)) / 8); }
+constexpr int kPfBarP = pf_bar(offsetof(PfHeader, p_ready));
+constexpr int kPfBarKF = pf_bar(offsetof(PfHeader, k_full));
+constexpr int kPfBarVF = pf_bar(offsetof(PfHeader, v_full));
 static_assert(sizeof(PfHeader) <= kPfHdrBytes, "header");
 
 __device__ __forceinline__ bool pf_wait(uint64_t *bar, uint32_t parity, unsigned *err) {
@@ -167,11 +179,14 @@ struct PfUnit {
     int g, h0, nh, n_kv;   // key/value head, first query head, heads, position tiles
 };
 
-// Rows of 128 positions from their pages into one operand's two stages; KEYS:
-// and the tiles' scales.  False: a wait gave up.
+// Rows of 128 positions from their pages into one operand's two stages, four
+// rows a load of warp w of NW, every NW-th four of them; KEYS: warp 0 also the
+// tiles' scales.  False: a wait gave up.
 template <bool KEYS>
 __device__ __forceinline__ bool pf_feed(const PfArgs &a, PfHeader *hd, unsigned char *smem,
-                                        const PfUnit &u) {
+                                        const PfUnit &u, int w) {
+    constexpr int NW = KEYS ? kPfKeyWarps : kPfValueWarps;
+    constexpr int B = KEYS ? 6 : 8;  // loads in flight
     const int lane = threadIdx.x & 31;
     const int shift = a.pv.shift, per = kPfRows >> shift;
     const int last = u.p0 + u.rows - 1;
@@ -180,51 +195,58 @@ __device__ __forceinline__ bool pf_feed(const PfArgs &a, PfHeader *hd, unsigned 
     unsigned char *ring = smem + (KEYS ? kPfOffK : kPfOffV);
     auto page = [&](int j) {  // lane i: the tile's page i
         const int p = j * kPfRows + (lane << shift);
-        return lane < per && p <= last ? a.pv.page(u.sq, p >> shift) : -1;
+        int pg = lane < per && p <= last ? a.pv.page(u.sq, p >> shift) : -1;
+        // (values under a scale of zero are zeros)
+        if (!KEYS && pg >= 0 && __ldg(a.vs + (size_t)pg * a.Hkv + u.g) == 0.f) pg = -1;
+        return pg;
     };
     int pg = page(0);
 #pragma unroll 1
     for (int j = 0; j < u.n_kv; ++j) {
         const int b = j & 1;
-        if (KEYS) {
+        // the scales of 16 positions a lane
+        int mine = -1;
+        float ks = 0.f, vs = 0.f;
+        if (KEYS && w == 0) {
             const int p = j * kPfRows + (lane << shift);
             if (lane < per && p <= last && pg < 0) set_error(a.err, kErrIndex);
-        }
-        // the scales of 16 positions a lane (KEYS)
-        const int mine = __shfl_sync(0xffffffffu, pg, ((lane & 7) << 4) >> shift);
-        float ks = 0.f, vs = 0.f;
-        if (KEYS && lane < 8 && mine >= 0) {
-            ks = __ldg(a.ks + (size_t)mine * a.Hkv + u.g);
-            vs = __ldg(a.vs + (size_t)mine * a.Hkv + u.g);
+            mine = __shfl_sync(0xffffffffu, pg, ((lane & 7) << 4) >> shift);
+            if (lane < 8 && mine >= 0) {
+                ks = __ldg(a.ks + (size_t)mine * a.Hkv + u.g);
+                vs = __ldg(a.vs + (size_t)mine * a.Hkv + u.g);
+            }
         }
         const int pg1 = j + 1 < u.n_kv ? page(j + 1) : -1;
+        bool waited = false;
+#pragma unroll 1
+        for (int k0 = w; k0 < kPfRows / 4; k0 += B * NW) {
+            uint4 x[B];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            uint4 w[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const int row = half * 64 + k * 4 + (lane >> 3);
-                const int rp = __shfl_sync(0xffffffffu, pg, row >> shift);
-                w[k] = make_uint4(0u, 0u, 0u, 0u);
-                if (rp >= 0 && j * kPfRows + row <= last)
-                    w[k] = ld_stream16(src +
+            for (int k = 0; k < B; ++k) {
+                const int row = (k0 + k * NW) * 4 + (lane >> 3);
+                const int rp = __shfl_sync(0xffffffffu, pg, (row & (kPfRows - 1)) >> shift);
+                x[k] = make_uint4(0u, 0u, 0u, 0u);
+                if (row < kPfRows && rp >= 0 && j * kPfRows + row <= last)
+                    x[k] = ld_stream16(src +
                                        ((((size_t)rp * a.Hkv + u.g) << shift) +
                                         (row & ((1 << shift) - 1))) * kPagedDh +
                                        (lane & 7) * 16);
             }
-            if (half == 0 && !pf_wait_all(&empty[b], ((uint32_t)(j >> 1) & 1u) ^ 1u, a.err))
+            if (!waited && !pf_wait_all(&empty[b], ((uint32_t)(j >> 1) & 1u) ^ 1u, a.err))
                 return false;
+            waited = true;
             // dims 16 c .. of a row: chunks 2c, 2c + 1 of its 64-dim half's row
             unsigned char *box = ring + b * kPfTile + ((lane & 7) >> 2) * kPfHalf;
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const int row = half * 64 + k * 4 + (lane >> 3);
-                const uint32_t x[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+            for (int k = 0; k < B; ++k) {
+                const int row = (k0 + k * NW) * 4 + (lane >> 3);
+                if (row >= kPfRows) break;
+                const uint32_t v[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
                 uint32_t y[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    y[2 * i] = e4m3x2_to_f16x2(x[i] & 0xffffu);
-                    y[2 * i + 1] = e4m3x2_to_f16x2(x[i] >> 16);
+                    y[2 * i] = e4m3x2_to_f16x2(v[i] & 0xffffu);
+                    y[2 * i + 1] = e4m3x2_to_f16x2(v[i] >> 16);
                 }
                 unsigned char *rowp = box + row * 128;
                 const uint32_t c = (lane & 3) * 2;
@@ -234,12 +256,14 @@ __device__ __forceinline__ bool pf_feed(const PfArgs &a, PfHeader *hd, unsigned 
                     make_uint4(y[4], y[5], y[6], y[7]);
             }
         }
-        if (KEYS) {
+        if (KEYS && w == 0) {
             PfScales *s = &hd->sc[j % kPfRing];
             if (lane < 8) {
+                // (a value scale of zero leaves rows of zeros, whatever it
+                // counts for here)
                 s->ks[lane] = ks;
-                s->vs[lane] = vs;
-                s->lv[lane] = log2f(fmaxf(vs, 7.888609052210118e-31f));  // 2^-100 at least
+                s->lv[lane] = log2f(fmaxf(vs, kPfLeast));
+                s->iv[lane] = 1.f / fmaxf(vs, kPfLeast);
             }
             const unsigned ok = __ballot_sync(0xffffffffu, lane < 8 && mine >= 0);
             if (lane == 0) s->ok = ok;
@@ -247,7 +271,7 @@ __device__ __forceinline__ bool pf_feed(const PfArgs &a, PfHeader *hd, unsigned 
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-            if (KEYS) ptx::mbar_arrive(&hd->t_full[j % kPfRing]);
+            if (KEYS && w == 0) ptx::mbar_arrive(&hd->t_full[j % kPfRing]);
             ptx::mbar_arrive(&full[b]);
         }
         pg = pg1;
@@ -351,52 +375,57 @@ __device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_
         tmem_ld_wait();
         const PfScales *sc = &hd->sc[j % kPfRing];
         const unsigned ok = sc->ok;
-        // (a tile holds no position past its last row's, so pages inside it are
-        // missing only there and where the table says nothing)
-        const bool full = j * kPfRows + kPfRows - 1 <= u.p0 && ok == 0xffu;
+        float cs[8], lv[8], iv[8];
+        *reinterpret_cast<float4 *>(&cs[0]) = *reinterpret_cast<const float4 *>(&sc->ks[0]);
+        *reinterpret_cast<float4 *>(&cs[4]) = *reinterpret_cast<const float4 *>(&sc->ks[4]);
+        *reinterpret_cast<float4 *>(&lv[0]) = *reinterpret_cast<const float4 *>(&sc->lv[0]);
+        *reinterpret_cast<float4 *>(&lv[4]) = *reinterpret_cast<const float4 *>(&sc->lv[4]);
+        *reinterpret_cast<float4 *>(&iv[0]) = *reinterpret_cast<const float4 *>(&sc->iv[0]);
+        *reinterpret_cast<float4 *>(&iv[4]) = *reinterpret_cast<const float4 *>(&sc->iv[4]);
+        if (j * kPfRows + kPfRows - 1 > u.p0 || ok != 0xffu) {
+            // positions past the row's own, and without a page: their score is
+            // -inf (cs is positive)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int n = (ok >> i) & 1u ? lim - 16 * i : -1;
+#pragma unroll
+                for (int k = 0; k < 16; ++k)
+                    if (k > n) v[16 * i + k] = -INFINITY;
+            }
+        }
         float mrow = kPfNone;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float m2[2] = {-INFINITY, -INFINITY};
-            if (full) {
+            float m2[2] = {v[16 * i], v[16 * i + 1]};
 #pragma unroll
-                for (int k = 0; k < 16; ++k) m2[k & 1] = fmaxf(m2[k & 1], v[16 * i + k]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 16; ++k)
-                    if (16 * i + k <= lim) m2[k & 1] = fmaxf(m2[k & 1], v[16 * i + k]);
-            }
-            const float mx = fmaxf(m2[0], m2[1]);
-            const float t = fmaf(mx, sc->ks[i] * qs, sc->lv[i]);
-            if (full || (16 * i <= lim && ((ok >> i) & 1u))) mrow = fmaxf(mrow, t);
+            for (int k = 2; k < 16; ++k) m2[k & 1] = fmaxf(m2[k & 1], v[16 * i + k]);
+            cs[i] = fmaxf(cs[i] * qs, kPfLeast);
+            mrow = fmaxf(mrow, fmaf(fmaxf(m2[0], m2[1]), cs[i], lv[i]));
         }
         const bool bump = mrow > m + kPfSlack;
         const float corr = bump ? pf_exp2(m - mrow) : 1.f;
         if (bump) m = mrow;
-        const float2 nm2 = make_float2(kPfTop - m, kPfTop - m);
-        float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        float lt = 0.f;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             uint32_t pw[32];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int gi = half * 4 + i;
-                const float c1 = sc->ks[gi] * qs, v1 = sc->vs[gi];
-                const float2 c2 = make_float2(c1, c1), v2 = make_float2(v1, v1);
-                const bool page = (ok >> gi) & 1u;
+                // p vs: the value page's scale is part of the exponent; the row
+                // sum takes it out again
+                const float b = lv[gi] + (kPfTop - m);
+                const float2 c2 = make_float2(cs[gi], cs[gi]), b2 = make_float2(b, b);
+                float2 sum2[2];
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) {
                     const int c = 16 * gi + k;
-                    const float2 e = __ffma2_rn(make_float2(v[c], v[c + 1]), c2, nm2);
-                    float2 p = make_float2(pf_exp2(e.x), pf_exp2(e.y));
-                    if (!full) {
-                        if (c > lim || !page) p.x = 0.f;
-                        if (c + 1 > lim || !page) p.y = 0.f;
-                    }
-                    sum2[(k >> 1) & 1] = __fadd2_rn(sum2[(k >> 1) & 1], p);
-                    const float2 w = __fmul2_rn(p, v2);
+                    const float2 e = __ffma2_rn(make_float2(v[c], v[c + 1]), c2, b2);
+                    const float2 w = make_float2(pf_exp2(e.x), pf_exp2(e.y));
+                    sum2[(k >> 1) & 1] = k < 4 ? w : __fadd2_rn(sum2[(k >> 1) & 1], w);
                     pw[i * 8 + (k >> 1)] = f16x2(w.x, w.y);
                 }
+                lt = fmaf((sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y), iv[gi], lt);
             }
             pf_tmem_st32(s_col + half * 32, pw);
         }
@@ -418,12 +447,27 @@ __device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_
         tc_fence_before();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&hd->p_ready[x]);
-        l = l * corr + ((sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y));
+        l = l * corr + lt;
     }
     return good;
 }
 
-// 384 threads: three warps a scheduler, so at most 168 registers a thread
+__device__ __forceinline__ PfUnit pf_unit(const PfArgs &a, int unit, int G, int per, bool single) {
+    const int tile = unit / (a.Hkv * per), gp = unit - tile * a.Hkv * per;
+    const int4 td = __ldcg(&a.plan.tiles[tile]);
+    PfUnit u;
+    u.g = gp / per;
+    const int hp = gp - u.g * per;
+    u.h0 = u.g * G + (single ? hp : 2 * hp);
+    u.nh = !single && 2 * hp + 1 < G ? 2 : 1;
+    u.t0 = td.x;
+    u.rows = td.y;
+    u.p0 = td.z;
+    u.sq = td.w;
+    u.n_kv = (u.p0 + u.rows - 1) / kPfRows + 1;
+    return u;
+}
+
 __global__ void __launch_bounds__(kPfThreads, 1)
 k_paged_prefill_tc(const PfArgs a) {
     extern __shared__ unsigned char smem_raw[];
@@ -446,101 +490,112 @@ k_paged_prefill_tc(const PfArgs a) {
     if (unit >= n_units) return;
     if (threadIdx.x == 0) hd->gave_up = 0;
     if (warp == 0) tmem_alloc(&hd->tmem_base, kPfTmemCols);
-
-#pragma unroll 1
-    for (bool again = false;; again = true) {
+    // the barriers of a unit, before and after the block meets
+    auto begin = [&](bool again) {
         if (threadIdx.x == 0) {
             uint64_t *bars = hd->q_full;
             if (again)
                 for (int i = 0; i < kPfBars; ++i) ptx::mbar_inval(bars + i);
-            for (int i = 0; i < kPfBars; ++i)
-                ptx::mbar_init(bars + i, i < 2 || (i >= kPfBarP && i < kPfBarP + 2) ? 4 : 1);
+            for (int i = 0; i < kPfBars; ++i) {
+                const int n = i == kPfBarKF || i == kPfBarKF + 1   ? kPfKeyWarps
+                              : i == kPfBarVF || i == kPfBarVF + 1 ? kPfValueWarps
+                              : i < 2 || i == kPfBarP || i == kPfBarP + 1 ? 4
+                                                                          : 1;
+                ptx::mbar_init(bars + i, n);
+            }
             ptx::fence_barrier_init();
         }
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
-        const uint32_t tmem = hd->tmem_base;
-        const int tile = unit / (a.Hkv * per), gp = unit - tile * a.Hkv * per;
-        const int4 td = __ldcg(&a.plan.tiles[tile]);
-        PfUnit u;
-        u.g = gp / per;
-        const int hp = gp - u.g * per;
-        u.h0 = u.g * G + (single ? hp : 2 * hp);
-        u.nh = !single && 2 * hp + 1 < G ? 2 : 1;
-        u.t0 = td.x;
-        u.rows = td.y;
-        u.p0 = td.z;
-        u.sq = td.w;
-        u.n_kv = (u.p0 + u.rows - 1) / kPfRows + 1;
-
-        if (warp == 0) {
-            if (lane == 0) {
-                bool good = pf_issue(hd, sbase, tmem, u, err);
-                mma_commit(&hd->done);
-                good &= pf_wait(&hd->done, 0, err);
-                // the MMAs' last arrivals, before the barriers start anew
-                for (int j = max(0, u.n_kv - 2); good && j < u.n_kv; ++j)
-                    good = pf_wait(&hd->k_empty[j & 1], (uint32_t)(j >> 1) & 1u, err) &&
-                           pf_wait(&hd->v_empty[j & 1], (uint32_t)(j >> 1) & 1u, err);
-                if (!good) hd->gave_up = 1;
-            }
-            __syncwarp();
-        } else if (warp == 1) {
-            const bool good = pf_feed<true>(a, hd, smem, u);
-            if (lane == 0) {
-                hd->next = (int)gridDim.x + atomicAdd(&a.plan.head->next, 1);
-                if (!good) hd->gave_up = 1;
-            }
-        } else if (warp == 2) {
-            const bool good = pf_feed<false>(a, hd, smem, u);
-            if (lane == 0 && !good) hd->gave_up = 1;
-        } else if (warp >= kPfHeadWarp && (warp - kPfHeadWarp) / 4 < u.nh) {
-            const int x = (warp - kPfHeadWarp) / 4;
-            const int q = warp & 3, r = q * 32 + lane;
-            const uint32_t lane_base = (uint32_t)(q * 32) << 16;
-            const uint32_t s_col = tmem + lane_base + kPfColS + (uint32_t)x * 128;
-            const uint32_t o_col = tmem + lane_base + kPfColO + (uint32_t)x * 128;
-            const float qs = pf_queries(a, smem, u, x, r);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(&hd->q_full[x]);
-            float l = 0.f;
-            bool good = pf_softmax(hd, s_col, o_col, u, r, x, qs, l, err);
-            good = good && pf_wait_all(&hd->o_full[x], (u.n_kv - 1) & 1, err);
-            if (!good) hd->gave_up = 1;
-            if (good) {
-                tc_fence_after();
-                const float inv = l == 0.f ? 0.f : 1.f / l;
-                bf16 *dst = a.ctx + ((size_t)(u.t0 + r) * a.Hq + u.h0 + x) * kPagedDh;
-#pragma unroll
-                for (int c = 0; c < 128; c += 32) {
-                    float vv[32];
-                    tmem_ld32(o_col + c, vv);
-                    tmem_ld_wait();
-                    if (r >= u.rows) continue;
-#pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const __nv_bfloat162 p2 = __floats2bfloat162_rn(
-                                vv[i + 2 * e] * inv, vv[i + 2 * e + 1] * inv);
-                            w[e] = *reinterpret_cast<const uint32_t *>(&p2);
-                        }
-                        *reinterpret_cast<uint4 *>(dst + c + i) = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                }
-            }
-        }
+    };
+    // the next unit, for all; false: there is none
+    auto more = [&]() {
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
         unit = hd->next;
-        if (unit >= n_units || hd->gave_up) break;
+        const bool go = unit < n_units && !hd->gave_up;
         __syncthreads();  // (read by all before the next unit's)
+        return go;
+    };
+
+    if (warp < kPfHeadWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPfRegsFeed));
+#pragma unroll 1
+        for (bool again = false;; again = true) {
+            begin(again);
+            const PfUnit u = pf_unit(a, unit, G, per, single);
+            bool good = true;
+            if (warp == 0) {
+                if (lane == 0) {
+                    good = pf_issue(hd, sbase, hd->tmem_base, u, err);
+                    mma_commit(&hd->done);
+                    good &= pf_wait(&hd->done, 0, err);
+                    // the MMAs' last arrivals, before the barriers start anew
+                    for (int j = max(0, u.n_kv - 2); good && j < u.n_kv; ++j)
+                        good = pf_wait(&hd->k_empty[j & 1], (uint32_t)(j >> 1) & 1u, err) &&
+                               pf_wait(&hd->v_empty[j & 1], (uint32_t)(j >> 1) & 1u, err);
+                }
+                __syncwarp();
+            } else if (warp <= kPfKeyWarps) {
+                good = pf_feed<true>(a, hd, smem, u, warp - 1);
+                if (warp == 1 && lane == 0)
+                    hd->next = (int)gridDim.x + atomicAdd(&a.plan.head->next, 1);
+            } else {
+                good = pf_feed<false>(a, hd, smem, u, warp - 1 - kPfKeyWarps);
+            }
+            if (!good) hd->gave_up = 1;
+            if (!more()) break;
+        }
+        if (warp == 0) tmem_dealloc(hd->tmem_base, kPfTmemCols);
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPfRegsSoftmax));
+        const int x = (warp - kPfHeadWarp) / 4;
+        const int q = warp & 3, r = q * 32 + lane;
+#pragma unroll 1
+        for (bool again = false;; again = true) {
+            begin(again);
+            const PfUnit u = pf_unit(a, unit, G, per, single);
+            if (x < u.nh) {
+                const uint32_t at = hd->tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)x * 128;
+                const uint32_t s_col = at + kPfColS, o_col = at + kPfColO;
+                const float qs = pf_queries(a, smem, u, x, r);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&hd->q_full[x]);
+                float l = 0.f;
+                bool good = pf_softmax(hd, s_col, o_col, u, r, x, qs, l, err);
+                good = good && pf_wait_all(&hd->o_full[x], (u.n_kv - 1) & 1, err);
+                if (!good) hd->gave_up = 1;
+                if (good) {
+                    tc_fence_after();
+                    const float inv = l == 0.f ? 0.f : 1.f / l;
+                    bf16 *dst = a.ctx + ((size_t)(u.t0 + r) * a.Hq + u.h0 + x) * kPagedDh;
+#pragma unroll
+                    for (int c = 0; c < 128; c += 32) {
+                        float vv[32];
+                        tmem_ld32(o_col + c, vv);
+                        tmem_ld_wait();
+                        if (r >= u.rows) continue;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const __nv_bfloat162 p2 = __floats2bfloat162_rn(
+                                    vv[i + 2 * e] * inv, vv[i + 2 * e + 1] * inv);
+                                w[e] = *reinterpret_cast<const uint32_t *>(&p2);
+                            }
+                            *reinterpret_cast<uint4 *>(dst + c + i) =
+                                make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    }
+                }
+            }
+            if (!more()) break;
+        }
     }
-    if (warp == 0) tmem_dealloc(hd->tmem_base, kPfTmemCols);
 }
 
 }  // namespace
