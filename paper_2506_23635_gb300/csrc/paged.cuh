@@ -3,7 +3,7 @@
 
 #include <stdint.h>
 
-#include "ptx.cuh"
+#include "tc.cuh"
 
 namespace moe {
 
@@ -77,6 +77,20 @@ struct PagedAttn {
     const float *ks, *vs;
     void *ctx;
 };
+// A page's rows of one head as a box: 8-bit [rows, 128].
+inline bool paged_map(CUtensorMap *m, const void *base, const PagedAttn &a, bool swizzle128) {
+    auto fn = tc::encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {kPagedDh, (cuuint64_t)a.pv.n_pages * a.Hkv * a.page_size};
+    cuuint64_t strides[1] = {kPagedDh};
+    cuuint32_t box[2] = {kPagedDh, (cuuint32_t)a.page_size};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box,
+              estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              swizzle128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Attention of the listed tokens over the 8-bit cache (paged_decode_tc.cu).
 // Attention of the plan's tiles (paged_prefill_tc.cu).
 cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, cudaStream_t st);

@@ -53,7 +53,6 @@
 #include <algorithm>
 
 #include "paged.cuh"
-#include "tc.cuh"
 
 namespace moe {
 namespace {
@@ -795,27 +794,13 @@ const void *pd_kernel(int G) {
     }
 }
 
-// A page's rows of one head as a box: 8-bit [rows, 128], 128-byte swizzle.
-bool page_map(CUtensorMap *m, const void *base, uint64_t rows, int page_size) {
-    auto fn = encode_fn();
-    if (!fn) return false;
-    cuuint64_t dims[2] = {kPagedDh, rows};
-    cuuint64_t strides[1] = {kPagedDh};
-    cuuint32_t box[2] = {kPagedDh, (cuuint32_t)page_size};
-    cuuint32_t estr[2] = {1, 1};
-    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box,
-              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 }  // namespace
 
 cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part,
                                    cudaStream_t st) {
     const int G = a.Hq / a.Hkv;
     CUtensorMap mk, mv;
-    const uint64_t rows = (uint64_t)a.pv.n_pages * a.Hkv * a.page_size;
-    if (!page_map(&mk, a.kp, rows, a.page_size) || !page_map(&mv, a.vp, rows, a.page_size))
+    if (!paged_map(&mk, a.kp, a, true) || !paged_map(&mv, a.vp, a, true))
         return cudaErrorInvalidValue;
     const void *kern = pd_kernel(G);
     cudaError_t e =

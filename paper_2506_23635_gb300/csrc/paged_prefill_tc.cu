@@ -20,9 +20,9 @@
 //               128 columns) and the MMAs: per head S_j = Q K_j^T, and once
 //               P_j has taken S_j's place, O += P_j V_j with P_j read from tensor
 //               memory and V_j MN-major as it lies;
-//   warps 1-3   key rows from their pages (16 bytes a lane), decoded and written
-//               with the 128-byte swizzle into two stages; the tile's scales;
-//   warps 4-7   the same for value rows (rows past the tile's last query and of
+//   warp 1      a tile's pages by TMA, as they are, its scales;
+//   warps 2-4   key rows decoded into two stages with the 128-byte swizzle;
+//   warps 5-7   the same for value rows (rows past the tile's last query and of
 //               pages outside the pool are zeros);
 //   warps 8-11  head A, 12-15 head B: first their queries, then the online
 //               softmax, one thread per query row and all 128 columns; the exponent
@@ -38,7 +38,6 @@
 #include <cuda_fp16.h>
 
 #include "paged.cuh"
-#include "tc.cuh"
 
 namespace moe {
 namespace {
@@ -47,19 +46,22 @@ using namespace tc;
 
 constexpr int kPfRows = 128;
 constexpr int kPfThreads = 16 * 32;
-constexpr int kPfKeyWarps = 3, kPfValueWarps = 4;  // warps 1-3, 4-7
+constexpr int kPfDecWarps = 3;  // that decode keys (warps 2-4), and values (5-7)
 constexpr int kPfHeadWarp = 8;                     // first softmax warp
 // registers a thread: 512 x 128 at the launch, then two warpgroups each of
-// these (2 x 72 + 2 x 184 = 4 x 128)
-constexpr int kPfRegsFeed = 72, kPfRegsSoftmax = 184;
+// these (2 x 80 + 2 x 176 = 4 x 128)
+constexpr int kPfRegsFeed = 80, kPfRegsSoftmax = 176;
 static_assert(kPfRegsFeed + kPfRegsSoftmax == 2 * 128, "the launch's registers");
 constexpr uint32_t kPfHalf = kPfRows * 128;  // 64 columns of a tile: 16 KB
 constexpr uint32_t kPfTile = 2 * kPfHalf;
 constexpr uint32_t kPfOffQ = 0;
 constexpr uint32_t kPfOffK = 2 * kPfTile;
 constexpr uint32_t kPfOffV = 4 * kPfTile;
-constexpr uint32_t kPfOffHdr = 6 * kPfTile;
-constexpr uint32_t kPfHdrBytes = 1024;
+constexpr uint32_t kPfRaw = kPfRows * kPagedDh;  // a tile as the pages hold it: 16 KB
+constexpr uint32_t kPfOffRawK = 6 * kPfTile;
+constexpr uint32_t kPfOffRawV = kPfOffRawK + kPfRaw;
+constexpr uint32_t kPfOffHdr = kPfOffRawV + kPfRaw;
+constexpr uint32_t kPfHdrBytes = 2048;
 constexpr size_t kPfSmem = 1024 + kPfOffHdr + kPfHdrBytes;
 static_assert(kPfSmem <= 227 * 1024, "shared memory");
 // kind::f16: fp16 A and B, fp32 D, M = N = 128; and with B MN-major (bit 16)
@@ -71,14 +73,16 @@ constexpr uint32_t kPfTmemCols = 512, kPfColS = 0, kPfColO = 256;
 constexpr float kPfTop = 7.f, kPfSlack = 8.f;
 constexpr float kPfNone = -1e30f;
 constexpr float kPfLeast = 7.888609052210118e-31f;  // 2^-100: nothing times a score
-constexpr int kPfRing = 4;
+constexpr int kPfRing = 8;  // tiles' scales
 
 struct PfScales {
     // of 16 positions each: the key page's scale, log2 and reciprocal of the
     // value page's
     float ks[8], lv[8], iv[8];
-    unsigned ok;  // bit i: positions 16 i .. of a page inside the pool
-    int pad[7];
+    // bit i: positions 16 i .. of a page inside the pool; and of one whose
+    // values' scale is not zero
+    unsigned ok, values;
+    int pad[6];
 };
 
 struct PfHeader {
@@ -86,6 +90,7 @@ struct PfHeader {
     uint64_t k_full[2], k_empty[2];
     uint64_t v_full[2], v_empty[2];
     uint64_t t_full[kPfRing];  // a tile's scales written
+    uint64_t raw_full[2], raw_empty[2];  // keys', values' rows landed; read by their warps
     uint64_t s_full[2], p_ready[2], o_full[2];  // per head
     uint64_t done;
     uint32_t tmem_base;
@@ -97,6 +102,7 @@ constexpr int kPfBars = (int)((offsetof(PfHeader, done) - offsetof(PfHeader, q_f
 constexpr int pf_bar(size_t off) { return (int)((off - offsetof(PfHeader, q_full)) / 8); }
 constexpr int kPfBarP = pf_bar(offsetof(PfHeader, p_ready));
 constexpr int kPfBarKF = pf_bar(offsetof(PfHeader, k_full));
+constexpr int kPfBarRaw = pf_bar(offsetof(PfHeader, raw_empty));
 constexpr int kPfBarVF = pf_bar(offsetof(PfHeader, v_full));
 static_assert(sizeof(PfHeader) <= kPfHdrBytes, "header");
 
@@ -164,11 +170,11 @@ __device__ __forceinline__ void pf_tmem_st_wait() {
 }
 
 struct PfArgs {
+    CUtensorMap tmK, tmV;
     int Hq, Hkv;
     PageView pv;
     AttnPlan plan;
     const bf16 *q;
-    const uint8_t *kp, *vp;
     const float *ks, *vs;
     bf16 *ctx;
     unsigned *err;
@@ -179,68 +185,118 @@ struct PfUnit {
     int g, h0, nh, n_kv;   // key/value head, first query head, heads, position tiles
 };
 
-// Rows of 128 positions from their pages into one operand's two stages, four
-// rows a load of warp w of NW, every NW-th four of them; KEYS: warp 0 also the
-// tiles' scales.  False: a wait gave up.
-template <bool KEYS>
-__device__ __forceinline__ bool pf_feed(const PfArgs &a, PfHeader *hd, unsigned char *smem,
-                                        const PfUnit &u, int w) {
-    constexpr int NW = KEYS ? kPfKeyWarps : kPfValueWarps;
-    constexpr int B = KEYS ? 6 : 8;  // loads in flight
+// Every tile's pages by TMA, as they are, keys and values each into one buffer
+// that its decoding warps empty, and the tile's scales.  A lane a page.  False:
+// a wait gave up.
+__device__ __forceinline__ bool pf_fetch(const PfArgs &a, PfHeader *hd, unsigned char *smem,
+                                         const PfUnit &u) {
     const int lane = threadIdx.x & 31;
     const int shift = a.pv.shift, per = kPfRows >> shift;
     const int last = u.p0 + u.rows - 1;
-    const uint8_t *src = KEYS ? a.kp : a.vp;
-    uint64_t *full = KEYS ? hd->k_full : hd->v_full, *empty = KEYS ? hd->k_empty : hd->v_empty;
-    unsigned char *ring = smem + (KEYS ? kPfOffK : kPfOffV);
-    auto page = [&](int j) {  // lane i: the tile's page i
+    const uint64_t pol = ptx::policy_evict_last();
+    const int32_t *table = a.pv.table + (size_t)u.sq * a.pv.max_pages;
+    auto entry = [&](int j) {
         const int p = j * kPfRows + (lane << shift);
-        int pg = lane < per && p <= last ? a.pv.page(u.sq, p >> shift) : -1;
-        // (values under a scale of zero are zeros)
-        if (!KEYS && pg >= 0 && __ldg(a.vs + (size_t)pg * a.Hkv + u.g) == 0.f) pg = -1;
-        return pg;
+        return j < u.n_kv && lane < per && p <= last ? table[p >> shift] : -1;
     };
-    int pg = page(0);
+    int next = entry(0);
+    bool good = true;
+#pragma unroll 1
+    for (int j = 0; j < u.n_kv; ++j) {
+        const int pg = next >= 0 && next < a.pv.n_pages ? next : -1;
+        if (pg < 0 && lane < per && j * kPfRows + (lane << shift) <= last)
+            set_error(a.err, kErrIndex);
+        next = entry(j + 1);
+        // the scales of 16 positions a lane
+        const int mine = __shfl_sync(0xffffffffu, pg, ((lane & 7) << 4) >> shift);
+        float ks = 0.f, vs = 0.f;
+        if (mine >= 0 && lane < 8) {
+            ks = __ldg(a.ks + (size_t)mine * a.Hkv + u.g);
+            vs = __ldg(a.vs + (size_t)mine * a.Hkv + u.g);
+        }
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, pg >= 0)) *
+                               ((uint32_t)kPagedDh << shift);
+        const int row = (pg * a.Hkv + u.g) << shift;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            good = good && pf_wait_all(&hd->raw_empty[v], (uint32_t)(j & 1) ^ 1u, a.err);
+            if (!good) break;
+            if (lane == 0) ptx::mbar_arrive_expect_tx(&hd->raw_full[v], bytes);
+            __syncwarp();
+            if (pg >= 0)
+                ptx::tma_load_2d(smem + (v ? kPfOffRawV : kPfOffRawK) +
+                                     ((uint32_t)(lane * kPagedDh) << shift),
+                                 v ? &a.tmV : &a.tmK, 0, row, &hd->raw_full[v], pol);
+        }
+        PfScales *s = &hd->sc[j % kPfRing];
+        if (lane < 8) {
+            // (a value scale of zero leaves rows of zeros, whatever it counts for
+            // here)
+            s->ks[lane] = ks;
+            s->lv[lane] = log2f(fmaxf(vs, kPfLeast));
+            s->iv[lane] = 1.f / fmaxf(vs, kPfLeast);
+        }
+        const unsigned ok = __ballot_sync(0xffffffffu, lane < 8 && mine >= 0);
+        const unsigned values = __ballot_sync(0xffffffffu, lane < 8 && mine >= 0 && vs != 0.f);
+        if (lane == 0) {
+            s->ok = ok;
+            s->values = values;
+        }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&hd->t_full[j % kPfRing]);
+        if (!good) {
+            // (what was asked for lands before the block can exit)
+            if (j > 0) {
+                pf_wait_all(&hd->raw_full[0], (uint32_t)(j - 1) & 1u, a.err);
+                pf_wait_all(&hd->raw_full[1], (uint32_t)(j - 1) & 1u, a.err);
+            }
+            break;
+        }
+    }
+    return good;
+}
+
+// A tile's rows decoded into one operand's two stages, four rows a time of warp
+// w of three, every third four of them.  False: a wait gave up.
+template <bool KEYS>
+__device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigned char *smem,
+                                          const PfUnit &u, int w) {
+    constexpr int B = 6;  // fours of rows a batch; two batches
+    const int lane = threadIdx.x & 31;
+    const int last = u.p0 + u.rows - 1;
+    uint64_t *full = KEYS ? hd->k_full : hd->v_full, *empty = KEYS ? hd->k_empty : hd->v_empty;
+    uint64_t *raw_full = &hd->raw_full[KEYS ? 0 : 1], *raw_empty = &hd->raw_empty[KEYS ? 0 : 1];
+    const unsigned char *raw = smem + (KEYS ? kPfOffRawK : kPfOffRawV) + lane * 16;
 #pragma unroll 1
     for (int j = 0; j < u.n_kv; ++j) {
         const int b = j & 1;
-        // the scales of 16 positions a lane
-        int mine = -1;
-        float ks = 0.f, vs = 0.f;
-        if (KEYS && w == 0) {
-            const int p = j * kPfRows + (lane << shift);
-            if (lane < per && p <= last && pg < 0) set_error(a.err, kErrIndex);
-            mine = __shfl_sync(0xffffffffu, pg, ((lane & 7) << 4) >> shift);
-            if (lane < 8 && mine >= 0) {
-                ks = __ldg(a.ks + (size_t)mine * a.Hkv + u.g);
-                vs = __ldg(a.vs + (size_t)mine * a.Hkv + u.g);
-            }
-        }
-        const int pg1 = j + 1 < u.n_kv ? page(j + 1) : -1;
-        bool waited = false;
-#pragma unroll 1
-        for (int k0 = w; k0 < kPfRows / 4; k0 += B * NW) {
+        if (!pf_wait_all(&hd->t_full[j % kPfRing], (uint32_t)(j / kPfRing) & 1u, a.err) ||
+            !pf_wait_all(raw_full, j & 1, a.err) ||
+            !pf_wait_all(&empty[b], ((uint32_t)(j >> 1) & 1u) ^ 1u, a.err))
+            return false;
+        // rows that hold no position are zeros, as are values under a scale of zero
+        const unsigned ok = KEYS ? hd->sc[j % kPfRing].ok : hd->sc[j % kPfRing].values;
+        // dims 16 c .. of a row: chunks 2c, 2c + 1 of its 64-dim half's row
+        unsigned char *box = smem + (KEYS ? kPfOffK : kPfOffV) + b * kPfTile +
+                             ((lane & 7) >> 2) * kPfHalf;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
             uint4 x[B];
 #pragma unroll
             for (int k = 0; k < B; ++k) {
-                const int row = (k0 + k * NW) * 4 + (lane >> 3);
-                const int rp = __shfl_sync(0xffffffffu, pg, (row & (kPfRows - 1)) >> shift);
-                x[k] = make_uint4(0u, 0u, 0u, 0u);
-                if (row < kPfRows && rp >= 0 && j * kPfRows + row <= last)
-                    x[k] = ld_stream16(src +
-                                       ((((size_t)rp * a.Hkv + u.g) << shift) +
-                                        (row & ((1 << shift) - 1))) * kPagedDh +
-                                       (lane & 7) * 16);
+                const int r4 = w + (half * B + k) * kPfDecWarps;
+                if (r4 < kPfRows / 4) x[k] = *reinterpret_cast<const uint4 *>(raw + r4 * 512);
             }
-            if (!waited && !pf_wait_all(&empty[b], ((uint32_t)(j >> 1) & 1u) ^ 1u, a.err))
-                return false;
-            waited = true;
-            // dims 16 c .. of a row: chunks 2c, 2c + 1 of its 64-dim half's row
-            unsigned char *box = ring + b * kPfTile + ((lane & 7) >> 2) * kPfHalf;
+            if (half == 1) {
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(raw_empty);
+            }
 #pragma unroll
             for (int k = 0; k < B; ++k) {
-                const int row = (k0 + k * NW) * 4 + (lane >> 3);
-                if (row >= kPfRows) break;
+                const int r4 = w + (half * B + k) * kPfDecWarps, row = r4 * 4 + (lane >> 3);
+                if (r4 >= kPfRows / 4) break;
+                const bool live = j * kPfRows + row <= last && ((ok >> (row >> 4)) & 1u);
+                if (!live) x[k] = make_uint4(0u, 0u, 0u, 0u);
                 const uint32_t v[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
                 uint32_t y[8];
 #pragma unroll
@@ -256,25 +312,9 @@ __device__ __forceinline__ bool pf_feed(const PfArgs &a, PfHeader *hd, unsigned 
                     make_uint4(y[4], y[5], y[6], y[7]);
             }
         }
-        if (KEYS && w == 0) {
-            PfScales *s = &hd->sc[j % kPfRing];
-            if (lane < 8) {
-                // (a value scale of zero leaves rows of zeros, whatever it
-                // counts for here)
-                s->ks[lane] = ks;
-                s->lv[lane] = log2f(fmaxf(vs, kPfLeast));
-                s->iv[lane] = 1.f / fmaxf(vs, kPfLeast);
-            }
-            const unsigned ok = __ballot_sync(0xffffffffu, lane < 8 && mine >= 0);
-            if (lane == 0) s->ok = ok;
-        }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) {
-            if (KEYS && w == 0) ptx::mbar_arrive(&hd->t_full[j % kPfRing]);
-            ptx::mbar_arrive(&full[b]);
-        }
-        pg = pg1;
+        if (lane == 0) ptx::mbar_arrive(&full[b]);
     }
     return true;
 }
@@ -375,13 +415,11 @@ __device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_
         tmem_ld_wait();
         const PfScales *sc = &hd->sc[j % kPfRing];
         const unsigned ok = sc->ok;
-        float cs[8], lv[8], iv[8];
+        float cs[8], lv[8];
         *reinterpret_cast<float4 *>(&cs[0]) = *reinterpret_cast<const float4 *>(&sc->ks[0]);
         *reinterpret_cast<float4 *>(&cs[4]) = *reinterpret_cast<const float4 *>(&sc->ks[4]);
         *reinterpret_cast<float4 *>(&lv[0]) = *reinterpret_cast<const float4 *>(&sc->lv[0]);
         *reinterpret_cast<float4 *>(&lv[4]) = *reinterpret_cast<const float4 *>(&sc->lv[4]);
-        *reinterpret_cast<float4 *>(&iv[0]) = *reinterpret_cast<const float4 *>(&sc->iv[0]);
-        *reinterpret_cast<float4 *>(&iv[4]) = *reinterpret_cast<const float4 *>(&sc->iv[4]);
         if (j * kPfRows + kPfRows - 1 > u.p0 || ok != 0xffu) {
             // positions past the row's own, and without a page: their score is
             // -inf (cs is positive)
@@ -425,7 +463,7 @@ __device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_
                     sum2[(k >> 1) & 1] = k < 4 ? w : __fadd2_rn(sum2[(k >> 1) & 1], w);
                     pw[i * 8 + (k >> 1)] = f16x2(w.x, w.y);
                 }
-                lt = fmaf((sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y), iv[gi], lt);
+                lt = fmaf((sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y), sc->iv[gi], lt);
             }
             pf_tmem_st32(s_col + half * 32, pw);
         }
@@ -469,7 +507,7 @@ __device__ __forceinline__ PfUnit pf_unit(const PfArgs &a, int unit, int G, int 
 }
 
 __global__ void __launch_bounds__(kPfThreads, 1)
-k_paged_prefill_tc(const PfArgs a) {
+k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -497,10 +535,13 @@ k_paged_prefill_tc(const PfArgs a) {
             if (again)
                 for (int i = 0; i < kPfBars; ++i) ptx::mbar_inval(bars + i);
             for (int i = 0; i < kPfBars; ++i) {
-                const int n = i == kPfBarKF || i == kPfBarKF + 1   ? kPfKeyWarps
-                              : i == kPfBarVF || i == kPfBarVF + 1 ? kPfValueWarps
-                              : i < 2 || i == kPfBarP || i == kPfBarP + 1 ? 4
-                                                                          : 1;
+                // (q_full and p_ready: a head's four warps; k_full, v_full and
+                // raw_empty: the decoding ones)
+                const int n = i < 2 || i == kPfBarP || i == kPfBarP + 1 ? 4
+                              : i == kPfBarKF || i == kPfBarKF + 1 || i == kPfBarVF ||
+                                      i == kPfBarVF + 1 || i == kPfBarRaw || i == kPfBarRaw + 1
+                                  ? kPfDecWarps
+                                  : 1;
                 ptx::mbar_init(bars + i, n);
             }
             ptx::fence_barrier_init();
@@ -538,12 +579,13 @@ k_paged_prefill_tc(const PfArgs a) {
                                pf_wait(&hd->v_empty[j & 1], (uint32_t)(j >> 1) & 1u, err);
                 }
                 __syncwarp();
-            } else if (warp <= kPfKeyWarps) {
-                good = pf_feed<true>(a, hd, smem, u, warp - 1);
-                if (warp == 1 && lane == 0)
-                    hd->next = (int)gridDim.x + atomicAdd(&a.plan.head->next, 1);
+            } else if (warp == 1) {
+                good = pf_fetch(a, hd, smem, u);
+                if (lane == 0) hd->next = (int)gridDim.x + atomicAdd(&a.plan.head->next, 1);
+            } else if (warp < 2 + kPfDecWarps) {
+                good = pf_decode<true>(a, hd, smem, u, warp - 2);
             } else {
-                good = pf_feed<false>(a, hd, smem, u, warp - 1 - kPfKeyWarps);
+                good = pf_decode<false>(a, hd, smem, u, warp - 2 - kPfDecWarps);
             }
             if (!good) hd->gave_up = 1;
             if (!more()) break;
@@ -605,9 +647,10 @@ cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, cu
     cudaError_t e =
         cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPfSmem);
     if (e != cudaSuccess) return e;
-    PfArgs pa{a.Hq, a.Hkv, a.pv, plan, static_cast<const bf16 *>(a.q),
-              static_cast<const uint8_t *>(a.kp), static_cast<const uint8_t *>(a.vp), a.ks, a.vs,
+    PfArgs pa{{}, {}, a.Hq, a.Hkv, a.pv, plan, static_cast<const bf16 *>(a.q), a.ks, a.vs,
               static_cast<bf16 *>(a.ctx), device_info().err};
+    if (!paged_map(&pa.tmK, a.kp, a, false) || !paged_map(&pa.tmV, a.vp, a, false))
+        return cudaErrorInvalidValue;
     void *args[] = {&pa};
     const long long most = (long long)a.Hq * (a.T / kAttnTileMinRows);
     LaunchScope ls("paged_prefill_tc", st);
