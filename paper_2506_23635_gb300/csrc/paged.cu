@@ -64,30 +64,33 @@ struct QkvRows {
     ProjSplit split;
 };
 
-// Elements i, i + 1 (a) and i + 64, i + 65 (b) of head row hr of token t.
+// Elements i .. i + 3 (a) and i + 64 .. i + 67 (b) of head row hr of token t.
 template <int IN>
-__device__ __forceinline__ void load_pairs(const QkvRows &x, int t, int hr, int i, float2 &a,
-                                           float2 &b) {
+__device__ __forceinline__ void load_pairs(const QkvRows &x, int t, int hr, int i, float (&a)[4],
+                                           float (&b)[4]) {
     const size_t at = (size_t)t * x.width + (size_t)hr * kPagedDh + i;
     if constexpr (IN == kInBf16) {
-        const uint32_t *p = reinterpret_cast<const uint32_t *>(static_cast<const bf16 *>(x.p) + at);
-        const uint32_t u = p[0], v = p[kPagedDh / 4];
-        unpack_bf16x2(u, a.x, a.y);
-        unpack_bf16x2(v, b.x, b.y);
+        const bf16 *p = static_cast<const bf16 *>(x.p) + at;
+        const uint2 u = __ldg(reinterpret_cast<const uint2 *>(p));
+        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p + kPagedDh / 2));
+        unpack_bf16x2(u.x, a[0], a[1]);
+        unpack_bf16x2(u.y, a[2], a[3]);
+        unpack_bf16x2(v.x, b[0], b[1]);
+        unpack_bf16x2(v.y, b[2], b[3]);
     } else {
         const float *p = static_cast<const float *>(x.p) + at;
-        a = *reinterpret_cast<const float2 *>(p);
-        b = *reinterpret_cast<const float2 *>(p + kPagedDh / 2);
-        if constexpr (IN == kInParts) {
-            const int n = x.n_part > 0 ? x.n_part : x.split.parts(x.T, t, hr * kPagedDh);
-            for (int k = 1; k < n; ++k) {
-                const float2 c = *reinterpret_cast<const float2 *>(p + k * x.part_stride);
-                const float2 d =
-                    *reinterpret_cast<const float2 *>(p + k * x.part_stride + kPagedDh / 2);
-                a.x += c.x;
-                a.y += c.y;
-                b.x += d.x;
-                b.y += d.y;
+        const int n = IN == kInF32    ? 1
+                      : x.n_part > 0 ? x.n_part
+                                     : x.split.parts(x.T, t, hr * kPagedDh);
+        for (int k = 0; k < n; ++k) {
+            const float4 u = __ldg(reinterpret_cast<const float4 *>(p + k * x.part_stride));
+            const float4 v =
+                __ldg(reinterpret_cast<const float4 *>(p + k * x.part_stride + kPagedDh / 2));
+            const float w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                a[e] = k ? a[e] + w[e] : w[e];
+                b[e] = k ? b[e] + w[4 + e] : w[4 + e];
             }
         }
     }
@@ -112,79 +115,120 @@ __device__ __forceinline__ float storable(float x) {
 }
 
 constexpr int kAppThreads = 256;
-constexpr int kAppWarps = kAppThreads / 32;
-constexpr int kAppQTokens = 4;           // tokens x head rows of a block of the queries' part
-constexpr int kAppQRows = kAppWarps;
-constexpr int kAppGroup = 128;           // tokens among which a block looks for its pages' first ones
+constexpr int kAppHalves = kAppThreads / 16;  // half a warp takes a row, four pairs a lane
+constexpr int kAppQTokens = 4;                // tokens of a block of the queries' part
+constexpr int kAppGroup = 128;  // tokens among which a block looks for its pages' first ones
+constexpr int kAppRows = 16;    // key and value rows of a block at most
 
-// Blocks [0, n_qb): queries, kAppQRows head rows of kAppQTokens tokens, a warp
-// a row.  The others: keys and values.  The tokens of a call that lie in one
+// The pair's rotation.
+__device__ __forceinline__ void turn(float &a, float &b, float sn, float cs) {
+    const float u = a, v = b;
+    a = u * cs - v * sn;
+    b = v * cs + u * sn;
+}
+
+// Four numbers x / scale, as they are stored.
+__device__ __forceinline__ uint32_t quantise(const float (&x)[4], float scale) {
+    const float inv = 1.f / scale;
+    const bool pow2 = (__float_as_uint(scale) & 0x7fffffu) == 0;
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = storable(pow2 ? x[e] * inv : x[e] / scale);
+    return e4m3x2(y[0], y[1]) | e4m3x2(y[2], y[3]) << 16;
+}
+
+// Four stored numbers times ratio, rounded again.
+__device__ __forceinline__ uint32_t rescale(uint32_t v, float ratio) {
+    const float2 f0 = e4m3x2_to_float2(v & 0xffffu), f1 = e4m3x2_to_float2(v >> 16);
+    return e4m3x2(f0.x * ratio, f0.y * ratio) | e4m3x2(f1.x * ratio, f1.y * ratio) << 16;
+}
+
+// The n-th set bit of four words.
+__device__ __forceinline__ int nth_bit(const uint32_t (&w)[kAppGroup / 32], int n) {
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < kAppGroup / 32; ++i) {
+        const int c = __popc(w[i]);
+        if (n >= 0 && n < c) at = i * 32 + (int)__fns(w[i], 0, n + 1);
+        n -= c;
+    }
+    return at;
+}
+
+// Blocks [0, n_qb): queries, kAppHalves head rows of kAppQTokens tokens, half a
+// warp a row.  The others: keys and values.  The tokens of a call that lie in one
 // page are found from the first of them: a token leads its page if no earlier
 // token of the call lies there.  Only one that does not follow its
 // predecessor inside the page can (a start); starts look through the whole
 // call's tokens, which may come in any order.  Blocks (group of 128 tokens, rows
 // [rb rpb, (rb + 1) rpb) of the 2 Hkv key and value rows, slot): the starts of the
-// group are shared out among its slots.  A block holds a page's rows in
-// registers, a warp every eighth row, between the maximum and the
-// quantisation.
+// group are shared out among its slots.  A page with one token of the call
+// (decode): half a warp for each of the block's rows; else row by row, the
+// page's tokens in registers between their maximum and the quantisation.
 template <int IN, int PS>
 __global__ void __launch_bounds__(kAppThreads)
-k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv, const RopeTurns rope,
-               const int32_t *__restrict__ seq, const int32_t *__restrict__ pos,
-               bf16 *__restrict__ q, uint8_t *__restrict__ kp, uint8_t *__restrict__ vp,
-               float *__restrict__ ks, float *__restrict__ vs, int n_qb, int rpb, int slots,
-               unsigned *err) {
+k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
+               const __grid_constant__ RopeTurns rope, const int32_t *__restrict__ seq,
+               const int32_t *__restrict__ pos, bf16 *__restrict__ q, uint8_t *__restrict__ kp,
+               uint8_t *__restrict__ vp, float *__restrict__ ks, float *__restrict__ vs, int n_qb,
+               int rpb, int slots, unsigned *err) {
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
-    constexpr int H2 = kPagedDh / 2, R = PS / kAppWarps;
-    const int T = x.T, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int i = 2 * lane;
-    __shared__ __align__(8) float sn_s[kAppQTokens][H2], cs_s[kAppQTokens][H2];
+    constexpr int H2 = kPagedDh / 2, R = PS / kAppHalves;
+    const int T = x.T, tid = threadIdx.x, lane = tid & 31;
+    const int hw = tid / 16, i = 4 * (tid % 16);
+    __shared__ __align__(16) float sn_s[kAppQTokens][H2], cs_s[kAppQTokens][H2];
+    __shared__ int in_s[kAppQTokens];
     __shared__ int tok_at[PS];
     __shared__ uint32_t starts[kAppGroup / 32];
-    __shared__ float red[kAppWarps];
+    __shared__ float red[kAppHalves], ratio_s[kAppRows];
     int b = (int)blockIdx.x;
     if (b < n_qb) {
-        const int nrb = (Hq + kAppQRows - 1) / kAppQRows;
-        const int t0 = b / nrb * kAppQTokens, hr = b % nrb * kAppQRows + warp;
+        const int nrb = (Hq + kAppHalves - 1) / kAppHalves;
+        const int t0 = b / nrb * kAppQTokens, hr = b % nrb * kAppHalves + hw;
         const int nt = min(kAppQTokens, T - t0);
-        float2 av[kAppQTokens], bv[kAppQTokens];
+        float av[kAppQTokens][4], bv[kAppQTokens][4];
 #pragma unroll
         for (int u = 0; u < kAppQTokens; ++u)
             if (hr < Hq && u < nt) load_pairs<IN>(x, t0 + u, hr, i, av[u], bv[u]);
         static_assert(kAppQTokens * H2 == kAppThreads, "an angle a thread");
-        bool in = false;
         if (tid / H2 < nt) {
             const int t = t0 + tid / H2, sq = seq[t], p = pos[t];
-            in = pv.inside(sq, p);
+            const bool in = pv.inside(sq, p);
             rope_sincos(rope.r[tid % H2], in ? p : 0, sn_s[tid / H2][tid % H2],
                         cs_s[tid / H2][tid % H2]);
-            if (!in) {  // a row of zeros
-                sn_s[tid / H2][tid % H2] = 0.f;
-                cs_s[tid / H2][tid % H2] = __uint_as_float(0x7fffffffu);
+            if (tid % H2 == 0) {
+                in_s[tid / H2] = in;
+                // (seq < 0: a padding token, no error)
+                if (!in && sq >= 0 && b % nrb == 0) set_error(err, kErrIndex);
             }
-            // (seq < 0: a padding token, no error)
-            if (!in && sq >= 0 && b % nrb == 0 && tid % H2 == 0) set_error(err, kErrIndex);
         }
         __syncthreads();
         if (hr >= Hq) return;
 #pragma unroll
         for (int u = 0; u < kAppQTokens; ++u) {
             if (u >= nt) break;
-            const float2 sn = *reinterpret_cast<const float2 *>(&sn_s[u][i]);
-            const float2 cs = *reinterpret_cast<const float2 *>(&cs_s[u][i]);
-            float2 lo = make_float2(av[u].x * cs.x - bv[u].x * sn.x, av[u].y * cs.y - bv[u].y * sn.y);
-            float2 hi = make_float2(bv[u].x * cs.x + av[u].x * sn.x, bv[u].y * cs.y + av[u].y * sn.y);
-            if (isnan(cs.x)) lo = hi = make_float2(0.f, 0.f);
+            const float4 sn = *reinterpret_cast<const float4 *>(&sn_s[u][i]);
+            const float4 cs = *reinterpret_cast<const float4 *>(&cs_s[u][i]);
+            turn(av[u][0], bv[u][0], sn.x, cs.x);
+            turn(av[u][1], bv[u][1], sn.y, cs.y);
+            turn(av[u][2], bv[u][2], sn.z, cs.z);
+            turn(av[u][3], bv[u][3], sn.w, cs.w);
+            const bool in = in_s[u];  // else a row of zeros
             bf16 *o = q + ((size_t)(t0 + u) * Hq + hr) * kPagedDh + i;
-            *reinterpret_cast<__nv_bfloat162 *>(o) = __floats2bfloat162_rn(lo.x, lo.y);
-            *reinterpret_cast<__nv_bfloat162 *>(o + H2) = __floats2bfloat162_rn(hi.x, hi.y);
+            __nv_bfloat162 w[4] = {
+                __floats2bfloat162_rn(av[u][0], av[u][1]), __floats2bfloat162_rn(av[u][2], av[u][3]),
+                __floats2bfloat162_rn(bv[u][0], bv[u][1]), __floats2bfloat162_rn(bv[u][2], bv[u][3])};
+            const uint32_t *w4 = reinterpret_cast<const uint32_t *>(w);
+            *reinterpret_cast<uint2 *>(o) = in ? make_uint2(w4[0], w4[1]) : make_uint2(0u, 0u);
+            *reinterpret_cast<uint2 *>(o + H2) = in ? make_uint2(w4[2], w4[3]) : make_uint2(0u, 0u);
         }
         return;
     }
     b -= n_qb;
     const int nrb = (2 * Hkv + rpb - 1) / rpb;
     const int slot = b % slots, rb = b / slots % nrb, g0 = b / slots / nrb * kAppGroup;
+    const int r_end = min((rb + 1) * rpb, 2 * Hkv);
     if (tid < kAppGroup) {
         const int t = g0 + tid;
         bool start = false;
@@ -194,97 +238,163 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv, const RopeTu
                     !(t > 0 && (p & (PS - 1)) != 0 && seq[t - 1] == sq && pos[t - 1] == p - 1);
         }
         const uint32_t m = __ballot_sync(0xffffffffu, start);
-        if (lane == 0) starts[warp] = m;
+        if (lane == 0) starts[tid / 32] = m;
     }
+    if (tid < PS) tok_at[tid] = -1;
     __syncthreads();
-    int seen = 0;
-#pragma unroll 1
+    uint32_t words[kAppGroup / 32];
+    int n_starts = 0;
+#pragma unroll
     for (int w = 0; w < kAppGroup / 32; ++w) {
+        words[w] = starts[w];
+        n_starts += __popc(words[w]);
+    }
 #pragma unroll 1
-        for (uint32_t m = starts[w]; m; m &= m - 1) {
-            if (seen++ % slots != slot) continue;
-            const int t = g0 + w * 32 + __ffs(m) - 1;
-            const int sq = seq[t], pi = pos[t] / PS;
-            const int pg = pv.page(sq, pi);
-            if (pg < 0) {
-                if (rb == 0 && tid == 0) set_error(err, kErrIndex);
-                continue;
-            }
-            __syncthreads();  // (the rows of the start before are done with tok_at)
-            for (int o = tid; o < PS; o += kAppThreads) tok_at[o] = -1;
+    for (int s = slot; s < n_starts; s += slots) {
+        const int t = g0 + nth_bit(words, s);
+        const int sq = seq[t], p0 = pos[t], pi = p0 / PS;
+        const int pg = pv.page(sq, pi);
+        if (s != slot) {  // (the rows of the start before are done with tok_at)
             __syncthreads();
-            bool earlier = false;
-            for (int j = tid; j < T; j += kAppThreads) {
-                if (seq[j] != sq) continue;
-                const int p = pos[j];
-                if (p < 0 || p / PS != pi) continue;
-                earlier |= j < t;
-                atomicMax(&tok_at[p & (PS - 1)], j);
+            if (tid < PS) tok_at[tid] = -1;
+            __syncthreads();
+        }
+        bool earlier = false;
+        auto seen = [&](int j, int sj, int pj) {
+            if (j >= T || sj != sq || pj < 0 || pj / PS != pi) return;
+            earlier |= j < t;
+            atomicMax(&tok_at[pj & (PS - 1)], j);
+        };
+        // (four of them a load; the last may lie past the call's, not past the
+        // arrays' 16-byte units)
+        const int n4 = T / 4;
+#pragma unroll 4
+        for (int j = tid; j < n4; j += kAppThreads) {
+            const int4 s4 = __ldg(reinterpret_cast<const int4 *>(seq) + j);
+            const int4 p4 = __ldg(reinterpret_cast<const int4 *>(pos) + j);
+            seen(4 * j, s4.x, p4.x);
+            seen(4 * j + 1, s4.y, p4.y);
+            seen(4 * j + 2, s4.z, p4.z);
+            seen(4 * j + 3, s4.w, p4.w);
+        }
+        if (tid < T - 4 * n4) seen(4 * n4 + tid, seq[4 * n4 + tid], pos[4 * n4 + tid]);
+        if (__syncthreads_or(earlier)) continue;  // another start leads this page
+        const int n_in = __syncthreads_count(tid < PS && tok_at[tid] >= 0);
+        if (pg < 0) {
+            if (rb == 0 && tid == 0) set_error(err, kErrIndex);
+            continue;
+        }
+        const bool fresh = tok_at[0] >= 0;
+        // key or value row hr of the page: its scale, its numbers
+        auto scale_at = [&](int hr) {
+            return (hr < Hkv ? ks : vs) + (size_t)pg * Hkv + (hr < Hkv ? hr : hr - Hkv);
+        };
+        auto rows_at = [&](int hr) {
+            return (hr < Hkv ? kp : vp) +
+                   ((size_t)pg * Hkv + (hr < Hkv ? hr : hr - Hkv)) * PS * kPagedDh;
+        };
+        auto magnitude = [&](const float (&a)[4], const float (&c)[4], float mx) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(finite_abs(a[e]), finite_abs(c[e])));
+            return mx;
+        };
+        auto half_max = [&](float mx) {
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            return mx;
+        };
+        auto turn_key = [&](float (&a)[4], float (&c)[4], int p) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float sn, cs;
+                rope_sincos(rope.r[i + e], p, sn, cs);
+                turn(a[e], c[e], sn, cs);
             }
-            if (__syncthreads_or(earlier)) continue;  // another start leads this page
-            int tok[R];
+        };
+        if (n_in == 1) {
+            const int hr = rb * rpb + hw;  // (rpb is at most the halves)
+            const bool mine = hr < r_end;
+            float a[4] = {0.f, 0.f, 0.f, 0.f}, c[4] = {0.f, 0.f, 0.f, 0.f}, old = 1.f;
+            if (mine) {
+                load_pairs<IN>(x, t, Hq + hr, i, a, c);
+                old = *scale_at(hr);
+                if (hr < Hkv) turn_key(a, c, p0);
+            }
+            const float need = scale_for(half_max(magnitude(a, c, 0.f)));
+            const float scale = fresh ? need : fmaxf(old, need);
+            const bool grown = mine && !fresh && scale != old;
+            if (mine) {
+                uint8_t *row = rows_at(hr) + (size_t)(p0 & (PS - 1)) * kPagedDh + i;
+                *reinterpret_cast<uint32_t *>(row) = quantise(a, scale);
+                *reinterpret_cast<uint32_t *>(row + H2) = quantise(c, scale);
+                if (i == 0) {
+                    *scale_at(hr) = scale;
+                    ratio_s[hw] = grown ? old / scale : 1.f;
+                }
+            }
+            if (!__syncthreads_or(grown)) continue;
+            // the other rows of the pages that grew, by the whole block
+            for (int r = 0; r < r_end - rb * rpb; ++r) {
+                const float ratio = ratio_s[r];
+                if (ratio == 1.f) continue;
+                uint8_t *rows = rows_at(rb * rpb + r);
 #pragma unroll
-            for (int k = 0; k < R; ++k) tok[k] = tok_at[warp + k * kAppWarps];
-            const bool fresh = tok_at[0] >= 0;
+                for (int k = 0; k < R; ++k) {
+                    const int o = hw + k * kAppHalves;
+                    if (o == (p0 & (PS - 1))) continue;
+                    uint2 *p8 = reinterpret_cast<uint2 *>(rows + (size_t)o * kPagedDh + 2 * i);
+                    uint2 v = *p8;
+                    v.x = rescale(v.x, ratio);
+                    v.y = rescale(v.y, ratio);
+                    *p8 = v;
+                }
+            }
+            continue;
+        }
+        int tok[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) tok[k] = tok_at[hw + k * kAppHalves];
 #pragma unroll 1
-            for (int hr = rb * rpb; hr < min((rb + 1) * rpb, 2 * Hkv); ++hr) {
-                const bool key = hr < Hkv;
-                const int h = key ? hr : hr - Hkv;
-                float *sp = (key ? ks : vs) + (size_t)pg * Hkv + h;
-                uint8_t *rows = (key ? kp : vp) + ((size_t)pg * Hkv + h) * PS * kPagedDh;
-                const float old = *sp;
-                float2 a[R], c[R];
-                float mx = 0.f;
+        for (int hr = rb * rpb; hr < r_end; ++hr) {
+            uint8_t *rows = rows_at(hr);
+            const float old = *scale_at(hr);
+            float a[R][4], c[R][4];
+            float mx = 0.f;
 #pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    a[k] = c[k] = make_float2(0.f, 0.f);
-                    if (tok[k] >= 0) load_pairs<IN>(x, tok[k], Hq + hr, i, a[k], c[k]);
-                }
+            for (int k = 0; k < R; ++k) {
 #pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    if (tok[k] < 0) continue;
-                    if (key) {
-                        const int p = pi * PS + warp + k * kAppWarps;
-                        float s0, c0, s1, c1;
-                        rope_sincos(rope.r[i], p, s0, c0);
-                        rope_sincos(rope.r[i + 1], p, s1, c1);
-                        const float2 u = a[k], v = c[k];
-                        a[k] = make_float2(u.x * c0 - v.x * s0, u.y * c1 - v.y * s1);
-                        c[k] = make_float2(v.x * c0 + u.x * s0, v.y * c1 + u.y * s1);
-                    }
-                    mx = fmaxf(fmaxf(mx, fmaxf(finite_abs(a[k].x), finite_abs(a[k].y))),
-                               fmaxf(finite_abs(c[k].x), finite_abs(c[k].y)));
-                }
-                mx = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(mx)));
-                if (lane == 0) red[warp] = mx;
-                __syncthreads();
+                for (int e = 0; e < 4; ++e) a[k][e] = c[k][e] = 0.f;
+                if (tok[k] >= 0) load_pairs<IN>(x, tok[k], Hq + hr, i, a[k], c[k]);
+            }
 #pragma unroll
-                for (int u = 0; u < kAppWarps; ++u) mx = fmaxf(mx, red[u]);
-                __syncthreads();
-                const float need = scale_for(mx);
-                const float scale = fresh ? need : fmaxf(old, need);
-                if (tid == 0) *sp = scale;
-                const float inv = 1.f / scale;
-                const bool pow2 = (__float_as_uint(scale) & 0x7fffffu) == 0;
-                auto div = [&](float v) { return storable(pow2 ? v * inv : v / scale); };
-                const bool grown = !fresh && scale != old;
-                const float ratio = old / scale;
+            for (int k = 0; k < R; ++k) {
+                if (tok[k] < 0) continue;
+                if (hr < Hkv) turn_key(a[k], c[k], pi * PS + hw + k * kAppHalves);
+                mx = magnitude(a[k], c[k], mx);
+            }
+            mx = half_max(mx);
+            if (i == 0) red[hw] = mx;
+            __syncthreads();
 #pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    uint8_t *row = rows + (size_t)(warp + k * kAppWarps) * kPagedDh;
-                    if (tok[k] >= 0) {
-                        *reinterpret_cast<uint16_t *>(row + i) =
-                            (uint16_t)e4m3x2(div(a[k].x), div(a[k].y));
-                        *reinterpret_cast<uint16_t *>(row + H2 + i) =
-                            (uint16_t)e4m3x2(div(c[k].x), div(c[k].y));
-                    } else if (grown) {
-                        uint32_t *p4 = reinterpret_cast<uint32_t *>(row + 4 * lane);
-                        const uint32_t v = *p4;
-                        const float2 f0 = e4m3x2_to_float2(v & 0xffffu);
-                        const float2 f1 = e4m3x2_to_float2(v >> 16);
-                        *p4 = e4m3x2(f0.x * ratio, f0.y * ratio) |
-                              e4m3x2(f1.x * ratio, f1.y * ratio) << 16;
-                    }
+            for (int u = 0; u < kAppHalves; ++u) mx = fmaxf(mx, red[u]);
+            __syncthreads();
+            const float need = scale_for(mx);
+            const float scale = fresh ? need : fmaxf(old, need);
+            if (tid == 0) *scale_at(hr) = scale;
+            const bool grown = !fresh && scale != old;
+            const float ratio = old / scale;
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                uint8_t *row = rows + (size_t)(hw + k * kAppHalves) * kPagedDh;
+                if (tok[k] >= 0) {
+                    *reinterpret_cast<uint32_t *>(row + i) = quantise(a[k], scale);
+                    *reinterpret_cast<uint32_t *>(row + H2 + i) = quantise(c[k], scale);
+                } else if (grown) {
+                    uint2 *p8 = reinterpret_cast<uint2 *>(row + 2 * i);
+                    uint2 v = *p8;
+                    v.x = rescale(v.x, ratio);
+                    v.y = rescale(v.y, ratio);
+                    *p8 = v;
                 }
             }
         }
@@ -313,8 +423,11 @@ cudaError_t launch_append(const QkvRows &rows, int in, const moe_sa_dims &d,
     bf16 *qp = static_cast<bf16 *>(q);
     uint8_t *k8 = static_cast<uint8_t *>(kp), *v8 = static_cast<uint8_t *>(vp);
     unsigned *err = device_info().err;
-    int n_qb = (Hq + kAppQRows - 1) / kAppQRows * ((T + kAppQTokens - 1) / kAppQTokens);
-    int rpb = T <= 1024 ? 1 : 4;
+    int n_qb = (Hq + kAppHalves - 1) / kAppHalves * ((T + kAppQTokens - 1) / kAppQTokens);
+    // a decode batch: all rows of a token in one block; larger calls, which have
+    // more pages with many tokens: few rows, the look through the call shared by
+    // four of them where it is long
+    int rpb = T <= kAppGroup ? kAppRows : T <= 1024 ? 2 : 4;
     int slots = T <= kAppGroup ? T : T <= 1024 ? 32 : 8;
     const int groups = (T + kAppGroup - 1) / kAppGroup;
     const int n_kb = groups * ((2 * Hkv + rpb - 1) / rpb) * slots;
