@@ -114,11 +114,12 @@ __device__ __forceinline__ float storable(float x) {
     return fabsf(x) <= 3.402823466e38f ? x : __uint_as_float(0x7fffffffu);
 }
 
-constexpr int kAppThreads = 256;
+constexpr int kAppThreads = 512;
 constexpr int kAppHalves = kAppThreads / 16;  // half a warp takes a row, four pairs a lane
-constexpr int kAppQTokens = 4;                // tokens of a block of the queries' part
-constexpr int kAppGroup = 128;  // tokens among which a block looks for its pages' first ones
-constexpr int kAppRows = 16;    // key and value rows of a block at most
+constexpr int kAppQTokens = 8;                // tokens of a block of the queries' part,
+constexpr int kAppQRows = 16;                 // and head rows: a row of four of them a half
+constexpr int kAppQEach = kAppQTokens * kAppQRows / kAppHalves;
+constexpr int kAppMaxGroup = 128;  // tokens whose pages a block looks after, at most
 
 // The pair's rotation.
 __device__ __forceinline__ void turn(float &a, float &b, float sn, float cs) {
@@ -143,54 +144,42 @@ __device__ __forceinline__ uint32_t rescale(uint32_t v, float ratio) {
     return e4m3x2(f0.x * ratio, f0.y * ratio) | e4m3x2(f1.x * ratio, f1.y * ratio) << 16;
 }
 
-// The n-th set bit of four words.
-__device__ __forceinline__ int nth_bit(const uint32_t (&w)[kAppGroup / 32], int n) {
-    int at = 0;
-#pragma unroll
-    for (int i = 0; i < kAppGroup / 32; ++i) {
-        const int c = __popc(w[i]);
-        if (n >= 0 && n < c) at = i * 32 + (int)__fns(w[i], 0, n + 1);
-        n -= c;
-    }
-    return at;
-}
-
-// Blocks [0, n_qb): queries, kAppHalves head rows of kAppQTokens tokens, half a
-// warp a row.  The others: keys and values.  The tokens of a call that lie in one
-// page are found from the first of them: a token leads its page if no earlier
+// Blocks [0, n_kb): keys and values, each a row (key or value head) of the pages
+// that a group of gs consecutive tokens starts.  The tokens of a call that lie in
+// one page are found from the first of them: a token leads its page if no earlier
 // token of the call lies there.  Only one that does not follow its
-// predecessor inside the page can (a start); starts look through the whole
-// call's tokens, which may come in any order.  Blocks (group of 128 tokens, rows
-// [rb rpb, (rb + 1) rpb) of the 2 Hkv key and value rows, slot): the starts of the
-// group are shared out among its slots.  A page with one token of the call
-// (decode): half a warp for each of the block's rows; else row by row, the
-// page's tokens in registers between their maximum and the quantisation.
+// predecessor inside the page can (a start); the block compares the whole call's
+// tokens, which may come in any order, with the group's starts.  Pages with one
+// token (decode): half a warp each, all side by side; the others one after the
+// other, the page's tokens in registers between their maximum and the
+// quantisation.  The blocks after them: queries, kAppQRows head rows of
+// kAppQTokens tokens, half a warp a row of four of them.
+//
+// Bound: bytes, where there are many tokens, otherwise the chain of loads of a
+// start, its page and its row.
 template <int IN, int PS>
-__global__ void __launch_bounds__(kAppThreads)
+__global__ void __launch_bounds__(kAppThreads, 2)
 k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
                const __grid_constant__ RopeTurns rope, const int32_t *__restrict__ seq,
                const int32_t *__restrict__ pos, bf16 *__restrict__ q, uint8_t *__restrict__ kp,
-               uint8_t *__restrict__ vp, float *__restrict__ ks, float *__restrict__ vs, int n_qb,
-               int rpb, int slots, unsigned *err) {
+               uint8_t *__restrict__ vp, float *__restrict__ ks, float *__restrict__ vs, int n_kb,
+               int gs, unsigned *err) {
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
-    constexpr int H2 = kPagedDh / 2, R = PS / kAppHalves;
+    constexpr int H2 = kPagedDh / 2, R = (PS + kAppHalves - 1) / kAppHalves;
     const int T = x.T, tid = threadIdx.x, lane = tid & 31;
     const int hw = tid / 16, i = 4 * (tid % 16);
-    __shared__ __align__(16) float sn_s[kAppQTokens][H2], cs_s[kAppQTokens][H2];
-    __shared__ int in_s[kAppQTokens];
-    __shared__ int tok_at[PS];
-    __shared__ uint32_t starts[kAppGroup / 32];
-    __shared__ float red[kAppHalves], ratio_s[kAppRows];
-    int b = (int)blockIdx.x;
-    if (b < n_qb) {
-        const int nrb = (Hq + kAppHalves - 1) / kAppHalves;
-        const int t0 = b / nrb * kAppQTokens, hr = b % nrb * kAppHalves + hw;
-        const int nt = min(kAppQTokens, T - t0);
-        float av[kAppQTokens][4], bv[kAppQTokens][4];
+    if ((int)blockIdx.x >= n_kb) {
+        __shared__ __align__(16) float sn_s[kAppQTokens][H2], cs_s[kAppQTokens][H2];
+        __shared__ int in_s[kAppQTokens];
+        const int b = (int)blockIdx.x - n_kb;
+        const int nrb = (Hq + kAppQRows - 1) / kAppQRows;
+        const int t0 = b / nrb * kAppQTokens, hr = b % nrb * kAppQRows + hw % kAppQRows;
+        const int nt = min(kAppQTokens, T - t0), u0 = hw / kAppQRows * kAppQEach;
+        float av[kAppQEach][4], bv[kAppQEach][4];
 #pragma unroll
-        for (int u = 0; u < kAppQTokens; ++u)
-            if (hr < Hq && u < nt) load_pairs<IN>(x, t0 + u, hr, i, av[u], bv[u]);
+        for (int u = 0; u < kAppQEach; ++u)
+            if (hr < Hq && u0 + u < nt) load_pairs<IN>(x, t0 + u0 + u, hr, i, av[u], bv[u]);
         static_assert(kAppQTokens * H2 == kAppThreads, "an angle a thread");
         if (tid / H2 < nt) {
             const int t = t0 + tid / H2, sq = seq[t], p = pos[t];
@@ -206,16 +195,16 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
         __syncthreads();
         if (hr >= Hq) return;
 #pragma unroll
-        for (int u = 0; u < kAppQTokens; ++u) {
-            if (u >= nt) break;
-            const float4 sn = *reinterpret_cast<const float4 *>(&sn_s[u][i]);
-            const float4 cs = *reinterpret_cast<const float4 *>(&cs_s[u][i]);
+        for (int u = 0; u < kAppQEach; ++u) {
+            if (u0 + u >= nt) break;
+            const float4 sn = *reinterpret_cast<const float4 *>(&sn_s[u0 + u][i]);
+            const float4 cs = *reinterpret_cast<const float4 *>(&cs_s[u0 + u][i]);
             turn(av[u][0], bv[u][0], sn.x, cs.x);
             turn(av[u][1], bv[u][1], sn.y, cs.y);
             turn(av[u][2], bv[u][2], sn.z, cs.z);
             turn(av[u][3], bv[u][3], sn.w, cs.w);
-            const bool in = in_s[u];  // else a row of zeros
-            bf16 *o = q + ((size_t)(t0 + u) * Hq + hr) * kPagedDh + i;
+            const bool in = in_s[u0 + u];  // else a row of zeros
+            bf16 *o = q + ((size_t)(t0 + u0 + u) * Hq + hr) * kPagedDh + i;
             __nv_bfloat162 w[4] = {
                 __floats2bfloat162_rn(av[u][0], av[u][1]), __floats2bfloat162_rn(av[u][2], av[u][3]),
                 __floats2bfloat162_rn(bv[u][0], bv[u][1]), __floats2bfloat162_rn(bv[u][2], bv[u][3])};
@@ -225,179 +214,243 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
         }
         return;
     }
-    b -= n_qb;
-    const int nrb = (2 * Hkv + rpb - 1) / rpb;
-    const int slot = b % slots, rb = b / slots % nrb, g0 = b / slots / nrb * kAppGroup;
-    const int r_end = min((rb + 1) * rpb, 2 * Hkv);
-    if (tid < kAppGroup) {
-        const int t = g0 + tid;
-        bool start = false;
-        if (t < T) {
-            const int sq = seq[t], p = pos[t];
-            start = pv.inside(sq, p) &&
-                    !(t > 0 && (p & (PS - 1)) != 0 && seq[t - 1] == sq && pos[t - 1] == p - 1);
-        }
-        const uint32_t m = __ballot_sync(0xffffffffu, start);
-        if (lane == 0) starts[tid / 32] = m;
-    }
-    if (tid < PS) tok_at[tid] = -1;
-    __syncthreads();
-    uint32_t words[kAppGroup / 32];
-    int n_starts = 0;
+    __shared__ int n_s, n_grown;
+    __shared__ int t_s[kAppMaxGroup], page_s[kAppMaxGroup], count_s[kAppMaxGroup];
+    __shared__ int2 at_s[kAppMaxGroup];      // a start's sequence, page index
+    __shared__ int grown_s[kAppMaxGroup];    // starts whose page's scale grew
+    __shared__ float ratio_s[kAppMaxGroup];  // and by what
+    constexpr int kFew = 4;  // starts whose pages' tokens are found in one look
+    __shared__ int tok_at[kFew][PS];
+    __shared__ float red[kAppHalves];
+    const int hr = (int)blockIdx.x % (2 * Hkv), g0 = (int)blockIdx.x / (2 * Hkv) * gs;
+    const bool key = hr < Hkv;
+    const int h = key ? hr : hr - Hkv;
+    float *scales = (key ? ks : vs) + h;
+    uint8_t *pool = (key ? kp : vp) + (size_t)h * PS * kPagedDh;
+    auto rows_of = [&](int pg) { return pool + (size_t)pg * Hkv * PS * kPagedDh; };
+    // a lane's pairs' rates (read from the parameters by 16 different addresses a
+    // half warp, so once)
+    uint64_t rate[4] = {0, 0, 0, 0};
+    if (key) {
 #pragma unroll
-    for (int w = 0; w < kAppGroup / 32; ++w) {
-        words[w] = starts[w];
-        n_starts += __popc(words[w]);
-    }
-#pragma unroll 1
-    for (int s = slot; s < n_starts; s += slots) {
-        const int t = g0 + nth_bit(words, s);
-        const int sq = seq[t], p0 = pos[t], pi = p0 / PS;
-        const int pg = pv.page(sq, pi);
-        if (s != slot) {  // (the rows of the start before are done with tok_at)
-            __syncthreads();
-            if (tid < PS) tok_at[tid] = -1;
-            __syncthreads();
+        for (int e = 0; e < 4; ++e) {
+            rate[e] = rope.r[i + e];
+            asm volatile("" : "+l"(rate[e]));
         }
-        bool earlier = false;
-        auto seen = [&](int j, int sj, int pj) {
-            if (j >= T || sj != sq || pj < 0 || pj / PS != pi) return;
-            earlier |= j < t;
-            atomicMax(&tok_at[pj & (PS - 1)], j);
+    }
+    if (tid == 0) n_s = n_grown = 0;
+    for (int o = tid; o < kFew * PS; o += kAppThreads) (&tok_at[0][0])[o] = -1;
+    __syncthreads();
+    if (tid < gs && g0 + tid < T) {
+        const int t = g0 + tid, sq = seq[t], p = pos[t];
+        if (pv.inside(sq, p) &&
+            !(t > 0 && (p & (PS - 1)) != 0 && seq[t - 1] == sq && pos[t - 1] == p - 1)) {
+            const int s = atomicAdd(&n_s, 1);  // (in any order: nothing depends on it)
+            t_s[s] = t;
+            at_s[s] = make_int2(sq, p / PS);
+            count_s[s] = 0;
+            const int pg = pv.page(sq, p / PS);
+            page_s[s] = pg;
+            if (pg < 0 && hr == 0) set_error(err, kErrIndex);
+        }
+    }
+    __syncthreads();
+    const int n_starts = n_s;
+    if (n_starts == 0) return;
+    // how many tokens of the call lie in each start's page; where an earlier one
+    // does, that one leads the page and this start has none
+    const int n4 = T / 4;
+    if (n_starts <= kFew) {  // a thread a token, and the page's tokens right away
+        auto compare = [&](int t, int sq, int p) {
+            if (p < 0) return;
+            const int pi = p / PS;
+            for (int s = 0; s < n_starts; ++s) {
+                const int2 at = at_s[s];
+                if (at.x != sq || at.y != pi) continue;
+                if (t < t_s[s]) page_s[s] = -1;
+                atomicAdd(&count_s[s], 1);
+                atomicMax(&tok_at[s][p & (PS - 1)], t);
+            }
         };
-        // (four of them a load; the last may lie past the call's, not past the
-        // arrays' 16-byte units)
-        const int n4 = T / 4;
 #pragma unroll 4
         for (int j = tid; j < n4; j += kAppThreads) {
             const int4 s4 = __ldg(reinterpret_cast<const int4 *>(seq) + j);
             const int4 p4 = __ldg(reinterpret_cast<const int4 *>(pos) + j);
-            seen(4 * j, s4.x, p4.x);
-            seen(4 * j + 1, s4.y, p4.y);
-            seen(4 * j + 2, s4.z, p4.z);
-            seen(4 * j + 3, s4.w, p4.w);
+            compare(4 * j, s4.x, p4.x);
+            compare(4 * j + 1, s4.y, p4.y);
+            compare(4 * j + 2, s4.z, p4.z);
+            compare(4 * j + 3, s4.w, p4.w);
         }
-        if (tid < T - 4 * n4) seen(4 * n4 + tid, seq[4 * n4 + tid], pos[4 * n4 + tid]);
-        if (__syncthreads_or(earlier)) continue;  // another start leads this page
-        const int n_in = __syncthreads_count(tid < PS && tok_at[tid] >= 0);
-        if (pg < 0) {
-            if (rb == 0 && tid == 0) set_error(err, kErrIndex);
-            continue;
-        }
-        const bool fresh = tok_at[0] >= 0;
-        // key or value row hr of the page: its scale, its numbers
-        auto scale_at = [&](int hr) {
-            return (hr < Hkv ? ks : vs) + (size_t)pg * Hkv + (hr < Hkv ? hr : hr - Hkv);
-        };
-        auto rows_at = [&](int hr) {
-            return (hr < Hkv ? kp : vp) +
-                   ((size_t)pg * Hkv + (hr < Hkv ? hr : hr - Hkv)) * PS * kPagedDh;
-        };
-        auto magnitude = [&](const float (&a)[4], const float (&c)[4], float mx) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(finite_abs(a[e]), finite_abs(c[e])));
-            return mx;
-        };
-        auto half_max = [&](float mx) {
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            return mx;
-        };
-        auto turn_key = [&](float (&a)[4], float (&c)[4], int p) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float sn, cs;
-                rope_sincos(rope.r[i + e], p, sn, cs);
-                turn(a[e], c[e], sn, cs);
-            }
-        };
-        if (n_in == 1) {
-            const int hr = rb * rpb + hw;  // (rpb is at most the halves)
-            const bool mine = hr < r_end;
-            float a[4] = {0.f, 0.f, 0.f, 0.f}, c[4] = {0.f, 0.f, 0.f, 0.f}, old = 1.f;
-            if (mine) {
-                load_pairs<IN>(x, t, Hq + hr, i, a, c);
-                old = *scale_at(hr);
-                if (hr < Hkv) turn_key(a, c, p0);
-            }
-            const float need = scale_for(half_max(magnitude(a, c, 0.f)));
-            const float scale = fresh ? need : fmaxf(old, need);
-            const bool grown = mine && !fresh && scale != old;
-            if (mine) {
-                uint8_t *row = rows_at(hr) + (size_t)(p0 & (PS - 1)) * kPagedDh + i;
-                *reinterpret_cast<uint32_t *>(row) = quantise(a, scale);
-                *reinterpret_cast<uint32_t *>(row + H2) = quantise(c, scale);
-                if (i == 0) {
-                    *scale_at(hr) = scale;
-                    ratio_s[hw] = grown ? old / scale : 1.f;
+        if (tid < T - 4 * n4) compare(4 * n4 + tid, seq[4 * n4 + tid], pos[4 * n4 + tid]);
+    } else {  // a lane a start, a warp 32 tokens
+        for (int s0 = 0; s0 < n_starts; s0 += 32) {
+            const int s = s0 + lane;
+            const int2 at = s < n_starts ? at_s[s] : make_int2(-1, -1);
+            const int mine = s < n_starts ? t_s[s] : 0;
+            int n = 0;
+            bool early = false;
+            for (int j0 = tid - lane; j0 < T; j0 += kAppThreads) {
+                const int t = j0 + lane;
+                const int sq = t < T ? seq[t] : -2, pi = t < T ? pos[t] >> pv.shift : -2;
+#pragma unroll 8
+                for (int u = 0; u < 32; ++u) {
+                    // (every lane takes part in both)
+                    const int su = __shfl_sync(0xffffffffu, sq, u);
+                    const int pu = __shfl_sync(0xffffffffu, pi, u);
+                    const bool here = su == at.x && pu == at.y;
+                    n += here;
+                    early |= here && j0 + u < mine;
                 }
             }
-            if (!__syncthreads_or(grown)) continue;
-            // the other rows of the pages that grew, by the whole block
-            for (int r = 0; r < r_end - rb * rpb; ++r) {
-                const float ratio = ratio_s[r];
-                if (ratio == 1.f) continue;
-                uint8_t *rows = rows_at(rb * rpb + r);
-#pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    const int o = hw + k * kAppHalves;
-                    if (o == (p0 & (PS - 1))) continue;
-                    uint2 *p8 = reinterpret_cast<uint2 *>(rows + (size_t)o * kPagedDh + 2 * i);
-                    uint2 v = *p8;
-                    v.x = rescale(v.x, ratio);
-                    v.y = rescale(v.y, ratio);
-                    *p8 = v;
-                }
-            }
-            continue;
+            if (s < n_starts && n) atomicAdd(&count_s[s], n);
+            if (s < n_starts && early) page_s[s] = -1;
         }
+    }
+    __syncthreads();
+    auto magnitude = [&](const float (&a)[4], const float (&c)[4], float mx) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(finite_abs(a[e]), finite_abs(c[e])));
+        return mx;
+    };
+    auto half_max = [&](float mx) {
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        return mx;
+    };
+    auto turn_key = [&](float (&a)[4], float (&c)[4], int p) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float sn, cs;
+            rope_sincos(rate[e], p, sn, cs);
+            turn(a[e], c[e], sn, cs);
+        }
+    };
+    // pages with one token of the call
+#pragma unroll 1
+    for (int s0 = 0; s0 < n_starts; s0 += kAppHalves) {
+        const int s = s0 + hw;
+        const bool mine = s < n_starts && count_s[s] == 1 && page_s[s] >= 0;
+        float a[4] = {0.f, 0.f, 0.f, 0.f}, c[4] = {0.f, 0.f, 0.f, 0.f}, old = 1.f;
+        int p = 0, pg = 0;
+        if (mine) {
+            const int t = t_s[s];
+            pg = page_s[s];
+            load_pairs<IN>(x, t, Hq + hr, i, a, c);
+            old = scales[(size_t)pg * Hkv];
+            p = pos[t];
+            if (key) turn_key(a, c, p);
+        }
+        const float need = scale_for(half_max(magnitude(a, c, 0.f)));
+        if (!mine) continue;
+        const bool fresh = (p & (PS - 1)) == 0;
+        const float scale = fresh ? need : fmaxf(old, need);
+        uint8_t *row = rows_of(pg) + (size_t)(p & (PS - 1)) * kPagedDh + i;
+        *reinterpret_cast<uint32_t *>(row) = quantise(a, scale);
+        *reinterpret_cast<uint32_t *>(row + H2) = quantise(c, scale);
+        if (i == 0) {
+            scales[(size_t)pg * Hkv] = scale;
+            if (!fresh && scale != old) {
+                const int n = atomicAdd(&n_grown, 1);
+                grown_s[n] = s;
+                ratio_s[n] = old / scale;
+            }
+        }
+    }
+    __syncthreads();
+    // the other rows of those whose scale grew, by the whole block
+#pragma unroll 1
+    for (int r = hw; r < n_grown * PS; r += 4 * kAppHalves) {
+        uint2 v[4];
+        uint2 *p8[4];
+        float ratio[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int rr = r + u * kAppHalves, n = rr / PS, o = rr % PS;
+            p8[u] = nullptr;
+            if (n >= n_grown) continue;
+            const int s = grown_s[n];
+            if (o == (pos[t_s[s]] & (PS - 1))) continue;
+            ratio[u] = ratio_s[n];
+            p8[u] = reinterpret_cast<uint2 *>(rows_of(page_s[s]) + (size_t)o * kPagedDh + 2 * i);
+            v[u] = *p8[u];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (p8[u]) *p8[u] = make_uint2(rescale(v[u].x, ratio[u]), rescale(v[u].y, ratio[u]));
+    }
+    // the others
+#pragma unroll 1
+    for (int s = 0; s < n_starts; ++s) {
+        if (count_s[s] <= 1 || page_s[s] < 0) continue;
+        const int pg = page_s[s], sq = at_s[s].x, pi = at_s[s].y;
+        int *toks = tok_at[n_starts <= kFew ? s : 0];
+        if (n_starts > kFew) {
+            __syncthreads();
+            if (tid < PS) toks[tid] = -1;
+            __syncthreads();
+            auto seen = [&](int t, int st, int p) {
+                if (st == sq && p >= 0 && p / PS == pi) atomicMax(&toks[p & (PS - 1)], t);
+            };
+#pragma unroll 4
+            for (int j = tid; j < n4; j += kAppThreads) {
+                const int4 s4 = __ldg(reinterpret_cast<const int4 *>(seq) + j);
+                const int4 p4 = __ldg(reinterpret_cast<const int4 *>(pos) + j);
+                seen(4 * j, s4.x, p4.x);
+                seen(4 * j + 1, s4.y, p4.y);
+                seen(4 * j + 2, s4.z, p4.z);
+                seen(4 * j + 3, s4.w, p4.w);
+            }
+            if (tid < T - 4 * n4) seen(4 * n4 + tid, seq[4 * n4 + tid], pos[4 * n4 + tid]);
+            __syncthreads();
+        }
+        const bool fresh = toks[0] >= 0;
         int tok[R];
 #pragma unroll
-        for (int k = 0; k < R; ++k) tok[k] = tok_at[hw + k * kAppHalves];
-#pragma unroll 1
-        for (int hr = rb * rpb; hr < r_end; ++hr) {
-            uint8_t *rows = rows_at(hr);
-            const float old = *scale_at(hr);
-            float a[R][4], c[R][4];
-            float mx = 0.f;
+        for (int k = 0; k < R; ++k) {
+            const int o = hw + k * kAppHalves;
+            tok[k] = o < PS ? toks[o] : -1;
+        }
+        uint8_t *rows = rows_of(pg);
+        const float old = scales[(size_t)pg * Hkv];
+        float a[R][4], c[R][4];
+        float mx = 0.f;
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
+        for (int k = 0; k < R; ++k) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) a[k][e] = c[k][e] = 0.f;
-                if (tok[k] >= 0) load_pairs<IN>(x, tok[k], Hq + hr, i, a[k], c[k]);
-            }
+            for (int e = 0; e < 4; ++e) a[k][e] = c[k][e] = 0.f;
+            if (tok[k] >= 0) load_pairs<IN>(x, tok[k], Hq + hr, i, a[k], c[k]);
+        }
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
-                if (tok[k] < 0) continue;
-                if (hr < Hkv) turn_key(a[k], c[k], pi * PS + hw + k * kAppHalves);
-                mx = magnitude(a[k], c[k], mx);
-            }
-            mx = half_max(mx);
-            if (i == 0) red[hw] = mx;
-            __syncthreads();
+        for (int k = 0; k < R; ++k) {
+            if (tok[k] < 0) continue;
+            if (key) turn_key(a[k], c[k], pi * PS + hw + k * kAppHalves);
+            mx = magnitude(a[k], c[k], mx);
+        }
+        mx = half_max(mx);
+        if (i == 0) red[hw] = mx;
+        __syncthreads();
 #pragma unroll
-            for (int u = 0; u < kAppHalves; ++u) mx = fmaxf(mx, red[u]);
-            __syncthreads();
-            const float need = scale_for(mx);
-            const float scale = fresh ? need : fmaxf(old, need);
-            if (tid == 0) *scale_at(hr) = scale;
-            const bool grown = !fresh && scale != old;
-            const float ratio = old / scale;
+        for (int u = 0; u < kAppHalves; ++u) mx = fmaxf(mx, red[u]);
+        const float need = scale_for(mx);
+        const float scale = fresh ? need : fmaxf(old, need);
+        const bool grown = !fresh && scale != old;
+        const float ratio = old / scale;
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
-                uint8_t *row = rows + (size_t)(hw + k * kAppHalves) * kPagedDh;
-                if (tok[k] >= 0) {
-                    *reinterpret_cast<uint32_t *>(row + i) = quantise(a[k], scale);
-                    *reinterpret_cast<uint32_t *>(row + H2 + i) = quantise(c[k], scale);
-                } else if (grown) {
-                    uint2 *p8 = reinterpret_cast<uint2 *>(row + 2 * i);
-                    uint2 v = *p8;
-                    v.x = rescale(v.x, ratio);
-                    v.y = rescale(v.y, ratio);
-                    *p8 = v;
-                }
+        for (int k = 0; k < R; ++k) {
+            uint8_t *row = rows + (size_t)(hw + k * kAppHalves) * kPagedDh;
+            if (tok[k] >= 0) {
+                *reinterpret_cast<uint32_t *>(row + i) = quantise(a[k], scale);
+                *reinterpret_cast<uint32_t *>(row + H2 + i) = quantise(c[k], scale);
+            } else if (grown && hw + k * kAppHalves < PS) {
+                uint2 *p8 = reinterpret_cast<uint2 *>(row + 2 * i);
+                uint2 v = *p8;
+                v.x = rescale(v.x, ratio);
+                v.y = rescale(v.y, ratio);
+                *p8 = v;
             }
         }
+        __syncthreads();  // (the old scale is read by all, and red)
+        if (tid == 0) scales[(size_t)pg * Hkv] = scale;
     }
 }
 
@@ -423,19 +476,16 @@ cudaError_t launch_append(const QkvRows &rows, int in, const moe_sa_dims &d,
     bf16 *qp = static_cast<bf16 *>(q);
     uint8_t *k8 = static_cast<uint8_t *>(kp), *v8 = static_cast<uint8_t *>(vp);
     unsigned *err = device_info().err;
-    int n_qb = (Hq + kAppHalves - 1) / kAppHalves * ((T + kAppQTokens - 1) / kAppQTokens);
-    // a decode batch: all rows of a token in one block; larger calls, which have
-    // more pages with many tokens: few rows, the look through the call shared by
-    // four of them where it is long
-    int rpb = T <= kAppGroup ? kAppRows : T <= 1024 ? 2 : 4;
-    int slots = T <= kAppGroup ? T : T <= 1024 ? 32 : 8;
-    const int groups = (T + kAppGroup - 1) / kAppGroup;
-    const int n_kb = groups * ((2 * Hkv + rpb - 1) / rpb) * slots;
+    const int n_qb = (Hq + kAppQRows - 1) / kAppQRows * ((T + kAppQTokens - 1) / kAppQTokens);
+    // small groups where the tokens may all be starts; a page's worth of tokens
+    // holds one or two otherwise
+    int gs = T <= kAppMaxGroup ? kAppHalves : std::max(kAppHalves, (int)pd.page_size);
+    int n_kb = (T + gs - 1) / gs * 2 * Hkv;
     const void *kern = in == kInBf16  ? append_kernel<kInBf16>(pd.page_size)
                        : in == kInF32 ? append_kernel<kInF32>(pd.page_size)
                                       : append_kernel<kInParts>(pd.page_size);
     void *args[] = {&x,  &Hq, &Hkv, &pv, &rope, &seq, &pos,   &qp,
-                    &k8, &v8, &ks,  &vs, &n_qb, &rpb, &slots, &err};
+                    &k8, &v8, &ks,  &vs, &n_kb, &gs,  &err};
     LaunchScope ls("paged_append", st);
     return launch_pdl(kern, dim3((unsigned)(n_qb + n_kb)), dim3(kAppThreads), 0, st, args);
 }
