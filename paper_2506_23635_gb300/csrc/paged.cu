@@ -128,13 +128,12 @@ __device__ __forceinline__ void turn(float &a, float &b, float sn, float cs) {
     b = v * cs + u * sn;
 }
 
-// Four numbers x / scale, as they are stored.
-__device__ __forceinline__ uint32_t quantise(const float (&x)[4], float scale) {
-    const float inv = 1.f / scale;
-    const bool pow2 = (__float_as_uint(scale) & 0x7fffffu) == 0;
+// Four numbers x / scale, as they are stored.  (inv = 1 / scale: exact for the
+// powers of two that this kernel gives.)
+__device__ __forceinline__ uint32_t quantise(const float (&x)[4], float inv) {
     float y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = storable(pow2 ? x[e] * inv : x[e] / scale);
+    for (int e = 0; e < 4; ++e) y[e] = storable(x[e]) * inv;
     return e4m3x2(y[0], y[1]) | e4m3x2(y[2], y[3]) << 16;
 }
 
@@ -261,18 +260,23 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
     // does, that one leads the page and this start has none
     const int n4 = T / 4;
     if (n_starts <= kFew) {  // a thread a token, and the page's tokens right away
+        int2 at[kFew];
+#pragma unroll
+        for (int s = 0; s < kFew; ++s) at[s] = s < n_starts ? at_s[s] : make_int2(-1, -1);
         auto compare = [&](int t, int sq, int p) {
-            if (p < 0) return;
-            const int pi = p / PS;
+            const int pi = p >> pv.shift;  // (negative where p is)
+            bool any = false;
+#pragma unroll
+            for (int s = 0; s < kFew; ++s) any = any || (at[s].x == sq && at[s].y == pi);
+            if (!any || sq < 0) return;
             for (int s = 0; s < n_starts; ++s) {
-                const int2 at = at_s[s];
-                if (at.x != sq || at.y != pi) continue;
+                if (at_s[s].x != sq || at_s[s].y != pi) continue;
                 if (t < t_s[s]) page_s[s] = -1;
                 atomicAdd(&count_s[s], 1);
                 atomicMax(&tok_at[s][p & (PS - 1)], t);
             }
         };
-#pragma unroll 4
+#pragma unroll 2
         for (int j = tid; j < n4; j += kAppThreads) {
             const int4 s4 = __ldg(reinterpret_cast<const int4 *>(seq) + j);
             const int4 p4 = __ldg(reinterpret_cast<const int4 *>(pos) + j);
@@ -307,9 +311,12 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
         }
     }
     __syncthreads();
-    auto magnitude = [&](const float (&a)[4], const float (&c)[4], float mx) {
+    // the largest magnitude; infinities are left out where there are any
+    auto magnitude = [&](const float (&a)[4], const float (&c)[4], float mx, bool all) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(finite_abs(a[e]), finite_abs(c[e])));
+        for (int e = 0; e < 4; ++e)
+            mx = all ? fmaxf(mx, fmaxf(fabsf(a[e]), fabsf(c[e])))
+                     : fmaxf(mx, fmaxf(finite_abs(a[e]), finite_abs(c[e])));
         return mx;
     };
     auto half_max = [&](float mx) {
@@ -329,6 +336,7 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
 #pragma unroll 1
     for (int s0 = 0; s0 < n_starts; s0 += kAppHalves) {
         const int s = s0 + hw;
+        if (!__any_sync(0xffffffffu, s < n_starts && count_s[s] == 1)) continue;
         const bool mine = s < n_starts && count_s[s] == 1 && page_s[s] >= 0;
         float a[4] = {0.f, 0.f, 0.f, 0.f}, c[4] = {0.f, 0.f, 0.f, 0.f}, old = 1.f;
         int p = 0, pg = 0;
@@ -340,13 +348,15 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
             p = pos[t];
             if (key) turn_key(a, c, p);
         }
-        const float need = scale_for(half_max(magnitude(a, c, 0.f)));
+        float mx = half_max(magnitude(a, c, 0.f, true));
+        if (__any_sync(0xffffffffu, mx == INFINITY)) mx = half_max(magnitude(a, c, 0.f, false));
+        const float need = scale_for(mx);
         if (!mine) continue;
         const bool fresh = (p & (PS - 1)) == 0;
         const float scale = fresh ? need : fmaxf(old, need);
         uint8_t *row = rows_of(pg) + (size_t)(p & (PS - 1)) * kPagedDh + i;
-        *reinterpret_cast<uint32_t *>(row) = quantise(a, scale);
-        *reinterpret_cast<uint32_t *>(row + H2) = quantise(c, scale);
+        *reinterpret_cast<uint32_t *>(row) = quantise(a, 1.f / scale);
+        *reinterpret_cast<uint32_t *>(row + H2) = quantise(c, 1.f / scale);
         if (i == 0) {
             scales[(size_t)pg * Hkv] = scale;
             if (!fresh && scale != old) {
@@ -424,23 +434,33 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
         for (int k = 0; k < R; ++k) {
             if (tok[k] < 0) continue;
             if (key) turn_key(a[k], c[k], pi * PS + hw + k * kAppHalves);
-            mx = magnitude(a[k], c[k], mx);
+            mx = magnitude(a[k], c[k], mx, true);
         }
-        mx = half_max(mx);
-        if (i == 0) red[hw] = mx;
-        __syncthreads();
+        auto block_max = [&]() {
+            mx = half_max(mx);
+            if (i == 0) red[hw] = mx;
+            __syncthreads();
 #pragma unroll
-        for (int u = 0; u < kAppHalves; ++u) mx = fmaxf(mx, red[u]);
+            for (int u = 0; u < kAppHalves; ++u) mx = fmaxf(mx, red[u]);
+        };
+        block_max();
+        if (mx == INFINITY) {  // (the same in every thread)
+            __syncthreads();
+            mx = 0.f;
+#pragma unroll
+            for (int k = 0; k < R; ++k) mx = magnitude(a[k], c[k], mx, false);
+            block_max();
+        }
         const float need = scale_for(mx);
         const float scale = fresh ? need : fmaxf(old, need);
         const bool grown = !fresh && scale != old;
-        const float ratio = old / scale;
+        const float ratio = old / scale, inv = 1.f / scale;
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             uint8_t *row = rows + (size_t)(hw + k * kAppHalves) * kPagedDh;
             if (tok[k] >= 0) {
-                *reinterpret_cast<uint32_t *>(row + i) = quantise(a[k], scale);
-                *reinterpret_cast<uint32_t *>(row + H2 + i) = quantise(c[k], scale);
+                *reinterpret_cast<uint32_t *>(row + i) = quantise(a[k], inv);
+                *reinterpret_cast<uint32_t *>(row + H2 + i) = quantise(c[k], inv);
             } else if (grown && hw + k * kAppHalves < PS) {
                 uint2 *p8 = reinterpret_cast<uint2 *>(row + 2 * i);
                 uint2 v = *p8;
