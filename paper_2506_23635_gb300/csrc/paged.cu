@@ -516,12 +516,14 @@ constexpr int kPlanThreads = 1024;
 
 __global__ void __launch_bounds__(kPlanThreads)
 k_paged_plan(int T, const PageView pv, const int32_t *__restrict__ seq,
-             const int32_t *__restrict__ pos, const PagedList l, const PlanArgs pa) {
-    ptx::launch_dependents();
+             const int32_t *__restrict__ pos, const PagedList l, const PlanArgs pa, bool small) {
     ptx::grid_dependency_wait();
+    // (after the wait: what starts now finds all that is ahead of the call complete)
+    ptx::launch_dependents();
     __shared__ long long sums[kPlanThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    for (int i = tid; i < kPagedMaxCtas; i += kPlanThreads) l.count[i] = 0;
+    for (int i = tid; i < 2 * kPagedMaxCtas; i += kPlanThreads) l.count[i] = 0;
+    if (small) return;
     int n = T;
     if (pa.plan.head) {  // only those that no tile holds
         plan_attention<kPlanThreads>(T, pa);
@@ -582,7 +584,7 @@ PagedWs paged_ws(int64_t T) {
     PagedWs L{};
     size_t o = 0;
     L.n_list = o; o += up(4);
-    L.count = o; o += up(kPagedMaxCtas * 4);
+    L.count = o; o += up(2 * kPagedMaxCtas * 4);
     L.list = o; o += up((size_t)T * 4);
     L.before = o; o += up(((size_t)T + 1) * 8);
     L.head = o; o += up(sizeof(AttnPlanHead));
@@ -606,13 +608,14 @@ cudaError_t attend(const PagedAttn &a, void *ws, cudaStream_t st) {
     PagedList l{at<int>(ws, L.n_list), at<int>(ws, L.list), at<long long>(ws, L.before),
                 at<int>(ws, L.count)};
     PlanArgs pa{a.seq, a.pos, a.pv.n_seq, a.pv.max_pages << a.pv.shift, {}};
+    bool small = a.T <= kPagedSmall && !planned(a.T, a.pv.n_seq);
     if (planned(a.T, a.pv.n_seq))
         pa.plan = AttnPlan{at<AttnPlanHead>(ws, L.head), at<int4>(ws, L.tiles), l.list};
     {
         int T = a.T;
         PageView pv = a.pv;
         const int32_t *seq = a.seq, *pos = a.pos;
-        void *args[] = {&T, &pv, &seq, &pos, &l, &pa};
+        void *args[] = {&T, &pv, &seq, &pos, &l, &pa, &small};
         LaunchScope ls("paged_plan", st);
         cudaError_t e =
             launch_pdl((const void *)k_paged_plan, dim3(1), dim3(kPlanThreads), 0, st, args);
@@ -622,7 +625,7 @@ cudaError_t attend(const PagedAttn &a, void *ws, cudaStream_t st) {
         cudaError_t e = launch_paged_prefill_tc(a, pa.plan, st);
         if (e != cudaSuccess) return e;
     }
-    return launch_paged_decode_tc(a, l, at<float>(ws, L.part), st);
+    return launch_paged_decode_tc(a, l, at<float>(ws, L.part), small, st);
 }
 
 moe_status check_paged(const moe_sa_dims *d, const moe_paged_dims *pd) {

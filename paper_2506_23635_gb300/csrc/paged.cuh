@@ -54,8 +54,9 @@ __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t v) {
 // The tokens that the decode attention takes one by one, made on the device
 // (k_paged_plan): list[i] is a token, before[i] the position tiles (of
 // kPagedTile positions, at least one) of the list's tokens ahead of it, entry
-// n_list those of all.  count: a counter of finished parts for each CTA, zero
+// n_list those of all.  count: counters of finished parts, two for each CTA, zero
 // at the start.
+constexpr int kPagedSmall = 128;
 constexpr int kPagedTile = 128;
 constexpr int kPagedMaxCtas = 320;
 struct PagedList {
@@ -94,7 +95,9 @@ inline bool paged_map(CUtensorMap *m, const void *base, const PagedAttn &a, bool
 // Attention of the listed tokens over the 8-bit cache (paged_decode_tc.cu).
 // Attention of the plan's tiles (paged_prefill_tc.cu).
 cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, cudaStream_t st);
-cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part,
+// small: a call of up to kPagedSmall tokens, all taken one by one; the kernel
+// then lists them itself, and only the counters are the plan's.
+cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, bool small,
                                    cudaStream_t st);
 
 }  // namespace moe

@@ -62,6 +62,12 @@ using namespace tc;
 constexpr int kPdThreads = 7 * 32;
 constexpr int kPdStages = 3;
 constexpr int kPdRing = 8;  // tile descriptions
+constexpr int kPdSmall = kPagedSmall;
+// a share's tiles at least: a second tile's copies are in flight with the
+// first's, a part to merge costs 1-2 us
+constexpr int kPdMinTiles = 2;
+// parts that one CTA merges: more are merged in groups first
+constexpr int kPdGroup = 16;
 constexpr int kPdMaxG = kPagedMaxGroup;
 constexpr int kPdMaxPages = kPagedTile / 16;  // pages of a tile at most
 constexpr uint32_t kPdTile = kPagedTile * kPagedDh;  // 16 KB
@@ -110,11 +116,14 @@ struct PdHeader {
     uint64_t t_full[kPdRing];         // description of tile j published
     uint64_t done;
     uint32_t tmem_base;
-    int last;  // this CTA counted last on its first (1), last (2) piece
+    int last;  // this CTA counted last
     float qs[2][kPdMaxG];  // queries: what a score is to be multiplied with
     float red[4][kPdMaxG];
     float lsum[4][kPdMaxG];
     alignas(16) PdDesc desc[kPdRing];
+    // a call of up to kPdSmall tokens, all of them listed: their sequences,
+    // positions attended to, and the tiles of those ahead of each
+    int seq[kPdSmall], n[kPdSmall], before[kPdSmall + 1];
 };
 static_assert(sizeof(PdHeader) <= kPdHdrBytes, "header");
 
@@ -213,6 +222,22 @@ __device__ __forceinline__ int pd_owner(long long x, long long W, int G) {
 }
 static_assert(kPagedMaxCtas < 1024, "the 32-bit products of pd_start and pd_owner");
 
+// The listed tokens: those of the plan, or all of a small call (in shared
+// memory, so that nothing waits for another kernel).
+struct PdTokens {
+    const PagedList &l;
+    const PdHeader *hd;
+    const int32_t *seq, *pos;
+    const PageView &pv;
+    int T;  // of a small call; 0: as listed
+
+    __device__ __forceinline__ int count() const { return T > 0 ? T : __ldcg(l.n_list); }
+    __device__ __forceinline__ long long before(int i) const {
+        return T > 0 ? hd->before[i] : __ldcg(&l.before[i]);
+    }
+    __device__ __forceinline__ int token(int i) const { return T > 0 ? i : __ldcg(&l.list[i]); }
+};
+
 // Where a share begins, and the walk through its (token, head)s.
 struct PdWalk {
     long long W;
@@ -222,14 +247,14 @@ struct PdWalk {
     int i, g, nt;         // present list entry, key/value head, its tiles
 };
 
-// The last entry with before[i] * Hkv <= x, by a warp.
-__device__ __forceinline__ int pd_find(const PagedList &l, int n, int Hkv, long long x) {
+// The last entry with before(i) * Hkv <= x, by a warp.
+__device__ __forceinline__ int pd_find(const PdTokens &l, int n, int Hkv, long long x) {
     const int lane = threadIdx.x & 31;
     int lo = 0, len = n;  // the answer is in [lo, lo + len)
     while (len > 1) {
         const int step = (len + 31) / 32;
         const int i = lo + lane * step;
-        const bool le = lane * step < len && __ldcg(&l.before[i]) * Hkv <= x;
+        const bool le = lane * step < len && l.before(i) * Hkv <= x;
         const uint32_t m = __ballot_sync(0xffffffffu, le);
         const int k = 31 - __clz(m);  // (entry lo itself always is)
         lo += k * step;
@@ -238,19 +263,19 @@ __device__ __forceinline__ int pd_find(const PagedList &l, int n, int Hkv, long 
     return lo;
 }
 
-__device__ __forceinline__ PdWalk pd_begin(const PagedList &l, int Hkv, int cta, int G) {
+__device__ __forceinline__ PdWalk pd_begin(const PdTokens &l, int Hkv, int cta, int G) {
     PdWalk w;
     w.Hkv = Hkv;
-    w.n_list = __ldcg(l.n_list);
-    w.W = w.n_list > 0 ? __ldcg(&l.before[w.n_list]) * Hkv : 0;
-    w.n_share = (int)min((long long)G, w.W);
+    w.n_list = l.count();
+    w.W = w.n_list > 0 ? l.before(w.n_list) * Hkv : 0;
+    w.n_share = (int)min((long long)G, (w.W + kPdMinTiles - 1) / kPdMinTiles);
     w.lo = w.hi = 0;
     if (cta >= w.n_share) return w;
     w.lo = pd_start(w.W, cta, w.n_share);
     w.hi = pd_start(w.W, cta + 1, w.n_share);
     w.i = pd_find(l, w.n_list, Hkv, w.lo);
-    const long long b = __ldcg(&l.before[w.i]);
-    w.nt = (int)(__ldcg(&l.before[w.i + 1]) - b);
+    const long long b = l.before(w.i);
+    w.nt = (int)(l.before(w.i + 1) - b);
     const long long in = w.lo - b * Hkv;
     w.g = in < (1 << 30) ? (int)((unsigned)in / (unsigned)w.nt) : (int)(in / w.nt);
     w.first = b * Hkv + (long long)w.g * w.nt;
@@ -258,67 +283,78 @@ __device__ __forceinline__ PdWalk pd_begin(const PagedList &l, int Hkv, int cta,
 }
 
 // On to the next (token, head).
-__device__ __forceinline__ void pd_next(const PagedList &l, PdWalk &w) {
+__device__ __forceinline__ void pd_next(const PdTokens &l, PdWalk &w) {
     w.first += w.nt;
     if (++w.g == w.Hkv) {
         w.g = 0;
         ++w.i;
-        if (w.first < w.hi)
-            w.nt = (int)(__ldcg(&l.before[w.i + 1]) - __ldcg(&l.before[w.i]));
+        if (w.first < w.hi) w.nt = (int)(l.before(w.i + 1) - l.before(w.i));
     }
 }
 
 __device__ __forceinline__ float pd_mean(float a, float s) { return s == 0.f ? 0.f : a / s; }
 
-// The parts of a (token, head) in the workspace, merged in order, thread r its
-// dim: part q is CTA b0 + q's, in its first slot (the start of the (token,
-// head), which ends CTA b0's share, in its second).
-template <int G>
-__device__ __forceinline__ void pd_merge(const float *part, int b0, int parts, int r, bf16 *dst) {
+// Parts in the workspace merged in order, thread r its dim: part k lies in slot
+// slot(k).  The result goes to dst (row 0 of the group's heads in ctx), or to the
+// slot `into`, which may be one of them.  Four parts' loads go out together, past
+// L1 (fewer with many heads).
+template <int G, typename Slot>
+__device__ __forceinline__ void pd_merge(float *part, Slot slot, int parts, int r, bf16 *dst,
+                                         float *into) {
+    constexpr int U = G > 6 ? 2 : G > 5 ? 3 : 4;  // (no register spills)
     float M[G], A[G], S[G];
 #pragma unroll
     for (int h = 0; h < G; ++h) {
         M[h] = kPdNone;
         A[h] = S[h] = 0.f;
     }
-    for (int q0 = 0; q0 < parts; q0 += 4) {
-        float2 bl[4][G];
-        float ov[4][G];
+#pragma unroll 1
+    for (int q0 = 0; q0 < parts; q0 += U) {
+        float2 bl[U][G];
+        float ov[U][G];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int q = q0 + u;
-            const float *pq = part + (size_t)(2 * (b0 + q) + (q == 0 ? 1 : 0)) * kPagedSlot;
+        for (int u = 0; u < U; ++u) {
+            const float *pq = part + (size_t)slot(min(q0 + u, parts - 1)) * kPagedSlot;
 #pragma unroll
             for (int h = 0; h < G; ++h) {
-                bl[u][h] = make_float2(kPdNone, 0.f);
-                ov[u][h] = 0.f;
-                if (q < parts) {
-                    bl[u][h] = __ldcg(reinterpret_cast<const float2 *>(pq + kPdMaxG * 128 + 2 * h));
-                    ov[u][h] = __ldcg(pq + h * 128 + r);
-                }
+                bl[u][h] = __ldcg(reinterpret_cast<const float2 *>(pq + kPdMaxG * 128 + 2 * h));
+                ov[u][h] = __ldcg(pq + h * 128 + r);
             }
         }
 #pragma unroll
         for (int h = 0; h < G; ++h) {
-            const float mn = fmaxf(M[h], fmaxf(fmaxf(bl[0][h].x, bl[1][h].x),
-                                               fmaxf(bl[2][h].x, bl[3][h].x)));
+            float mn = M[h];
+#pragma unroll
+            for (int u = 0; u < U; ++u) mn = fmaxf(mn, bl[u][h].x);
             const float c = pd_exp2(M[h] - mn);
             M[h] = mn;
             A[h] *= c;
             S[h] *= c;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < U; ++u) {
+                if (q0 + u >= parts) break;
                 const float w = pd_exp2(bl[u][h].x - mn);
                 S[h] = fmaf(w, bl[u][h].y, S[h]);
                 A[h] = fmaf(w, ov[u][h], A[h]);
             }
         }
     }
+    if (into) {
+        ptx::named_bar_sync(1, 128);  // all have read the slot
+#pragma unroll
+        for (int h = 0; h < G; ++h) {
+            into[h * 128 + r] = A[h];
+            if (r == 0)
+                *reinterpret_cast<float2 *>(into + kPdMaxG * 128 + 2 * h) = make_float2(M[h], S[h]);
+        }
+        return;
+    }
 #pragma unroll
     for (int h = 0; h < G; ++h) dst[h * 128] = __float2bfloat16_rn(pd_mean(A[h], S[h]));
 }
 
 struct PdArgs {
+    int T;  // tokens of a small call, all of them listed; 0: as the plan lists them
     int Hq, Hkv;
     PageView pv;
     PagedList list;
@@ -342,6 +378,9 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     const int cta = (int)blockIdx.x, n_cta = (int)gridDim.x, Hkv = a.Hkv;
     unsigned *err = a.err;
     ptx::launch_dependents();
+    // (the launch ahead, k_paged_plan, lets this one start once all that is ahead
+    // of the call is complete; a small call waits for it before it counts only)
+    const bool small = a.T > 0;
     if (threadIdx.x == 0) {
         for (int b = 0; b < kPdStages; ++b) {
             ptx::mbar_init(&hd->k_full[b], 1);
@@ -364,50 +403,94 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         ptx::prefetch_tmap(&tmV);
     }
     if (warp == 1) tmem_alloc(&hd->tmem_base, kPdTmemCols);
+    if (warp == 2 && small) {
+        // the tiles before each token; one outside the table has one, with no
+        // position: its ctx is zero
+        constexpr int E = kPdSmall / 32;
+        int nt[E], sum = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int t = E * lane + e;
+            const int sq = t < a.T ? a.seq[t] : -1, p = t < a.T ? a.pos[t] : -1;
+            const bool in = a.pv.inside(sq, p);
+            hd->seq[t] = sq;
+            hd->n[t] = in ? p + 1 : 0;
+            nt[e] = t < a.T ? (in ? p / kPagedTile + 1 : 1) : 0;
+            sum += nt[e];
+        }
+        int incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        int run = incl - sum;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            hd->before[E * lane + e] = run;
+            run += nt[e];
+        }
+        if (lane == 31) hd->before[kPdSmall] = run;
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    ptx::grid_dependency_wait();
+    if (!small) ptx::grid_dependency_wait();
+    const PdTokens tokens{a.list, hd, a.seq, a.pos, a.pv, a.T};
     const uint32_t tmem = hd->tmem_base;
     const uint32_t sbase = ptx::smem_u32(smem);
 
     if (warp == 0) {
         // ------------------------------------------------------------ pages
         const uint64_t pol = ptx::policy_evict_first();  // a tile is read once
-        PdWalk w = pd_begin(a.list, Hkv, cta, n_cta);
-        const int per = kPagedTile >> a.pv.shift;  // pages of a tile
-        const uint32_t page_bytes = (uint32_t)kPagedDh << a.pv.shift;
+        PdWalk w = pd_begin(tokens, Hkv, cta, n_cta);
+        const int shift = a.pv.shift, per = kPagedTile >> shift;  // pages of a tile
+        const uint32_t page_bytes = (uint32_t)kPagedDh << shift;
         bool good = true;
-        int j = 0, sent_k = 0, sent_v = 0, tok_of = -1, sq = 0, n = 0, tok = 0;
+        int j = 0, sent_k = 0, sent_v = 0, of = -1;
+        // a tile of the walk, looked up one ahead of its turn
+        struct Ahead {
+            int tok, sq, n, g, tile, nt;
+            long long first;
+            int entry;  // its page `lane`, as the table has it
+        } next = {};
+        auto look = [&](long long x) {
+            if (x == w.first + w.nt) pd_next(tokens, w);
+            if (w.i != of) {
+                of = w.i;
+                next.tok = tokens.token(w.i);
+                next.sq = small ? hd->seq[w.i] : a.seq[next.tok];
+                const int p = small ? hd->n[w.i] - 1 : a.pos[next.tok];
+                const bool in = a.pv.inside(next.sq, p);
+                next.n = in ? p + 1 : 0;
+                if (!in && next.sq >= 0 && lane == 0) set_error(err, kErrIndex);
+            }
+            next.g = w.g;
+            next.first = w.first;
+            next.nt = w.nt;
+            next.tile = (int)(x - w.first);
+            const int p = next.tile * kPagedTile + (lane << shift);
+            next.entry = lane < per && p < next.n
+                             ? a.pv.table[(size_t)next.sq * a.pv.max_pages + (p >> shift)]
+                             : -1;
+        };
+        if (w.lo < w.hi) look(w.lo);
         for (long long x = w.lo; x < w.hi; ++x, ++j) {
-            if (x == w.first + w.nt) pd_next(a.list, w);
-            const int tile = (int)(x - w.first);
-            if (w.i != tok_of) {
-                tok_of = w.i;
-                tok = __ldcg(&a.list.list[w.i]);
-                sq = a.seq[tok];
-                const int p = a.pos[tok];
-                const bool in = a.pv.inside(sq, p);
-                n = in ? p + 1 : 0;
-                if (!in && sq >= 0 && lane == 0) set_error(err, kErrIndex);
-            }
-            const int left = n - tile * kPagedTile;  // positions from the tile's first on
-            const int np = min(per, (max(left, 0) + (1 << a.pv.shift) - 1) >> a.pv.shift);
-            int pg = -1;
+            const Ahead c = next;
+            if (x + 1 < w.hi) look(x + 1);
+            const int pg = c.entry >= 0 && c.entry < a.pv.n_pages ? c.entry : -1;
+            const int left = c.n - c.tile * kPagedTile;  // positions from the tile's first on
+            if (pg < 0 && lane < per && (lane << shift) < left) set_error(err, kErrIndex);
             float ks = 0.f, vs = 0.f;
-            if (lane < np) {
-                pg = a.pv.page(sq, tile * per + lane);
-                if (pg < 0) set_error(err, kErrIndex);
-            }
             if (pg >= 0) {
-                ks = __ldg(a.ks + (size_t)pg * Hkv + w.g);
-                vs = __ldg(a.vs + (size_t)pg * Hkv + w.g);
+                ks = __ldg(a.ks + (size_t)pg * Hkv + c.g);
+                vs = __ldg(a.vs + (size_t)pg * Hkv + c.g);
             }
             const unsigned valid = __ballot_sync(0xffffffffu, pg >= 0);
             const uint32_t bytes = (uint32_t)__popc(valid) * page_bytes;
             const int st = j % kPdStages;
             const uint32_t ph = (uint32_t)(j / kPdStages) & 1u;
-            const int row = (pg * Hkv + w.g) << a.pv.shift;
+            const int row = (pg * Hkv + c.g) << shift;
             if (!(good = pd_wait(&hd->k_empty[st], ph ^ 1u, err))) break;
             if (lane == 0) ptx::mbar_arrive_expect_tx(&hd->k_full[st], bytes);
             __syncwarp();
@@ -415,6 +498,13 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             if (pg >= 0)
                 ptx::tma_load_2d(smem + kPdOffK + st * kPdTile + lane * page_bytes, &tmK, 0, row,
                                  &hd->k_full[st], pol);
+            if (!(good = pd_wait(&hd->v_empty[st], ph ^ 1u, err))) break;
+            if (lane == 0) ptx::mbar_arrive_expect_tx(&hd->v_full[st], bytes);
+            __syncwarp();
+            sent_v = j + 1;
+            if (pg >= 0)
+                ptx::tma_load_2d(smem + kPdOffV + st * kPdTile + lane * page_bytes, &tmV, 0, row,
+                                 &hd->v_full[st], pol);
             PdDesc *d = &hd->desc[j % kPdRing];
             if (lane < per) {
                 d->ks[lane] = ks;
@@ -424,32 +514,23 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 d->lv[lane] = log2f(fmaxf(vs, 7.888609052210118e-31f));
             }
             if (lane == 0) {
-                const bool whole = w.first >= w.lo && w.first + w.nt <= w.hi;
-                const bool first = tile == 0 || x == w.lo, last = tile == w.nt - 1 || x == w.hi - 1;
-                d->tile = tile;
-                d->tg = tok * Hkv + w.g;
-                d->n = n;
+                const bool whole = c.first >= w.lo && c.first + c.nt <= w.hi;
+                const bool first = c.tile == 0 || x == w.lo;
+                const bool last = c.tile == c.nt - 1 || x == w.hi - 1;
+                d->tile = c.tile;
+                d->tg = c.tok * Hkv + c.g;
+                d->n = c.n;
                 d->valid = valid;
                 d->flags = (first ? kPdFirst : 0) | (last ? kPdLast : 0) | (whole ? kPdWhole : 0) |
                            (x == w.hi - 1 ? kPdEnd : 0) |
                            (left < kPagedTile || (int)__popc(valid) < per ? kPdClip : 0);
                 if (!whole && last) {
-                    d->b0 = pd_owner(w.first, w.W, w.n_share);
-                    d->parts = pd_owner(w.first + w.nt - 1, w.W, w.n_share) - d->b0 + 1;
+                    d->b0 = pd_owner(c.first, w.W, w.n_share);
+                    d->parts = pd_owner(c.first + c.nt - 1, w.W, w.n_share) - d->b0 + 1;
                 }
             }
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&hd->t_full[j % kPdRing]);
-            if (!(good = pd_wait(&hd->v_empty[st], ph ^ 1u, err))) {
-                ++j;  // (published)
-                break;
-            }
-            if (lane == 0) ptx::mbar_arrive_expect_tx(&hd->v_full[st], bytes);
-            __syncwarp();
-            sent_v = j + 1;
-            if (pg >= 0)
-                ptx::tma_load_2d(smem + kPdOffV + st * kPdTile + lane * page_bytes, &tmV, 0, row,
-                                 &hd->v_full[st], pol);
         }
         // the end of the share, also where a wait gave up
         if (lane == 0) {
@@ -520,10 +601,10 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         __syncwarp();
     } else if (warp == 6) {
         // ------------------------------------------------------------ queries
-        PdWalk w = pd_begin(a.list, Hkv, cta, n_cta);
+        PdWalk w = pd_begin(tokens, Hkv, cta, n_cta);
         bool good = true;
         for (int piece = 0; w.lo < w.hi && w.first < w.hi && good; ++piece) {
-            const int tok = __ldcg(&a.list.list[w.i]);
+            const int tok = tokens.token(w.i);
             const bf16 *src = a.q + ((size_t)tok * a.Hq + w.g * G) * kPagedDh + 4 * lane;
             uint2 u[G];
 #pragma unroll
@@ -565,7 +646,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&hd->q_full[b]);
-            pd_next(a.list, w);
+            pd_next(tokens, w);
         }
     } else {
         // ------------------------------------------------------------ softmax
@@ -580,7 +661,10 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             l[h] = qs[h] = 0.f;
         }
         bool good = true;
-        int piece = -1, pend_tg[2] = {0, 0}, pend_b0[2] = {0, 0}, pend_parts[2] = {0, 0};
+        int piece = -1;
+        // parts to count at the end of the share: of the (token, head) that it
+        // begins inside, and of the one that it ends inside
+        int pend_tg0 = 0, pend_b0 = 0, pend_parts0 = 0, pend_tg1 = 0, pend_b1 = 0, pend_parts1 = 0;
 #pragma unroll 1
         for (int j = 0;; ++j) {
             // (a wait that gave up ends the loop of all four warps: they
@@ -746,39 +830,59 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                         *reinterpret_cast<float2 *>(mine + kPdMaxG * 128 + 2 * h) =
                             make_float2(base[h], L[h]);
                 }
-                pend_tg[slot] = tg;
-                pend_b0[slot] = b0;
-                pend_parts[slot] = parts;
+                if (slot) pend_tg1 = tg, pend_b1 = b0, pend_parts1 = parts;
+                else pend_tg0 = tg, pend_b0 = b0, pend_parts0 = parts;
             }
-            if (!(flags & kPdEnd) || (pend_parts[0] == 0 && pend_parts[1] == 0)) continue;
+            if (!(flags & kPdEnd) || (pend_parts0 == 0 && pend_parts1 == 0)) continue;
             // the share is done: its parts are counted, and the CTA that counts
-            // last on a (token, head) finds every part of it stored
-            ptx::named_bar_sync(1, 128);
-            if (r == 0) {
-                __threadfence();
-                int last = 0;
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (pend_parts[i] > 0 &&
-                        atomicAdd(&a.list.count[pend_b0[i]], 1) == pend_parts[i] - 1)
-                        last |= 1 << i;
-                hd->last = last;
-                __threadfence();
-            }
-            ptx::named_bar_sync(1, 128);
+            // last on a (token, head) finds every part of it stored; more than
+            // kPdGroup parts are counted and merged in groups of that many first
+            // (200,001 positions of one head over 304 CTAs: 96 us, all parts by one
+            // CTA, PD_LONG so)
+            if (small) ptx::grid_dependency_wait();  // the counters are zero
 #pragma unroll 1
-            for (int i = 0; i < 2; ++i)
-                if ((hd->last >> i) & 1) {
-                    const int t2 = pend_tg[i] / Hkv, g2 = pend_tg[i] - t2 * Hkv;
-                    pd_merge<G>(a.part, pend_b0[i], pend_parts[i], r,
-                                a.ctx + ((size_t)t2 * a.Hq + g2 * G) * kPagedDh + r);
+            for (int i = 0; i < 2; ++i) {
+                const int parts2 = i ? pend_parts1 : pend_parts0;
+                if (parts2 == 0) continue;
+                const int b2 = i ? pend_b1 : pend_b0, tg2 = i ? pend_tg1 : pend_tg0;
+                const int t2 = tg2 / Hkv, g2 = tg2 - t2 * Hkv;
+                bf16 *dst2 = a.ctx + ((size_t)t2 * a.Hq + g2 * G) * kPagedDh + r;
+                // part k: the first slot of CTA b2 + k, but its second where the
+                // (token, head) starts
+                auto slot = [&](int k) { return 2 * (b2 + k) + (k == 0 ? 1 : 0); };
+                // the last of n to count on counter `at`, with all they stored
+                auto last_of = [&](int at, int n) {
+                    ptx::named_bar_sync(1, 128);
+                    if (r == 0) {
+                        __threadfence();
+                        hd->last = atomicAdd(&a.list.count[at], 1) == n - 1;
+                        __threadfence();
+                    }
+                    ptx::named_bar_sync(1, 128);
+                    return hd->last != 0;
+                };
+                if (parts2 > kPdGroup) {
+                    const int k0 = (cta - b2) / kPdGroup * kPdGroup;
+                    const int n = min(kPdGroup, parts2 - k0);
+                    // (a counter by the group's last CTA: only the last one
+                    // of a (token, head) may start another)
+                    if (!last_of(kPagedMaxCtas + b2 + k0 + n - 1, n)) continue;
+                    float *into = a.part + (size_t)slot(k0) * kPagedSlot;
+                    pd_merge<G>(a.part, [&](int k) { return slot(k0 + k); }, n, r, nullptr, into);
                 }
+                const int groups = parts2 > kPdGroup ? (parts2 + kPdGroup - 1) / kPdGroup : parts2;
+                if (!last_of(b2, groups)) continue;
+                pd_merge<G>(
+                    a.part, [&](int k) { return slot(parts2 > kPdGroup ? k * kPdGroup : k); },
+                    groups, r, dst2, nullptr);
+            }
         }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (warp == 1) tmem_dealloc(tmem, kPdTmemCols);
+    if (small) ptx::grid_dependency_wait();  // (complete only after what is ahead is)
 }
 
 const void *pd_kernel(int G) {
@@ -796,7 +900,7 @@ const void *pd_kernel(int G) {
 
 }  // namespace
 
-cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part,
+cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, bool small,
                                    cudaStream_t st) {
     const int G = a.Hq / a.Hkv;
     CUtensorMap mk, mv;
@@ -806,11 +910,13 @@ cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float
     cudaError_t e =
         cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPdSmem);
     if (e != cudaSuccess) return e;
-    PdArgs pa{a.Hq, a.Hkv, a.pv, l, a.seq, a.pos, static_cast<const bf16 *>(a.q), a.ks, a.vs,
+    PdArgs pa{small ? a.T : 0, a.Hq, a.Hkv, a.pv, l, a.seq, a.pos, static_cast<const bf16 *>(a.q), a.ks, a.vs,
               static_cast<bf16 *>(a.ctx), part, device_info().err};
     void *args[] = {&mk, &mv, &pa};
-    const long long most = (long long)a.T * a.Hkv *
-                           (((long long)a.pv.max_pages * a.page_size + kPagedTile - 1) / kPagedTile);
+    // as many CTAs as the largest positions give shares
+    const long long tiles = (long long)a.T * a.Hkv *
+                            (((long long)a.pv.max_pages * a.page_size + kPagedTile - 1) / kPagedTile);
+    const long long most = (tiles + kPdMinTiles - 1) / kPdMinTiles;
     const int ctas = std::min(2 * device_info().sm_count, kPagedMaxCtas);
     LaunchScope ls("paged_decode_tc", st);
     return launch_pdl(kern, dim3((unsigned)std::min<long long>(most, ctas)), dim3(kPdThreads), kPdSmem,
