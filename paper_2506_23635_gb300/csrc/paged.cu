@@ -537,7 +537,7 @@ k_paged_plan(int T, const PageView pv, const int32_t *__restrict__ seq,
         if (i < n) {
             const int t = pa.plan.head ? pa.plan.left[i] : i, p = pos[t];
             if (!pa.plan.head) l.list[i] = t;
-            nt = pv.inside(seq[t], p) ? p / kPagedTile + 1 : 1;
+            nt = pv.inside(seq[t], p) ? p / kPagedTile + 1 : 0;
         }
         long long v = nt;
 #pragma unroll

@@ -53,8 +53,8 @@ __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t v) {
 
 // The tokens that the decode attention takes one by one, made on the device
 // (k_paged_plan): list[i] is a token, before[i] the position tiles (of
-// kPagedTile positions, at least one) of the list's tokens ahead of it, entry
-// n_list those of all.  count: counters of finished parts, two for each CTA, zero
+// kPagedTile positions; none for a token outside the table) of the list's tokens
+// ahead of it, entry n_list those of all.  count: counters of finished parts, two for each CTA, zero
 // at the start.
 constexpr int kPagedSmall = 128;
 constexpr int kPagedTile = 128;

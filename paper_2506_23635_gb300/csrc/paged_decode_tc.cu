@@ -67,7 +67,8 @@ constexpr int kPdSmall = kPagedSmall;
 // first's, a part to merge costs 1-2 us
 constexpr int kPdMinTiles = 2;
 // parts that one CTA merges: more are merged in groups first
-constexpr int kPdGroup = 16;
+constexpr int kPdGroup = 18;
+static_assert(kPagedMaxCtas <= kPdGroup * kPdGroup && kPdGroup <= 32, "two levels of merging");
 constexpr int kPdMaxG = kPagedMaxGroup;
 constexpr int kPdMaxPages = kPagedTile / 16;  // pages of a tile at most
 constexpr uint32_t kPdTile = kPagedTile * kPagedDh;  // 16 KB
@@ -287,70 +288,69 @@ __device__ __forceinline__ void pd_next(const PdTokens &l, PdWalk &w) {
     w.first += w.nt;
     if (++w.g == w.Hkv) {
         w.g = 0;
-        ++w.i;
-        if (w.first < w.hi) w.nt = (int)(l.before(w.i + 1) - l.before(w.i));
+        if (w.first < w.hi) do {
+                ++w.i;
+                w.nt = (int)(l.before(w.i + 1) - l.before(w.i));
+            } while (w.nt == 0);
     }
 }
 
 __device__ __forceinline__ float pd_mean(float a, float s) { return s == 0.f ? 0.f : a / s; }
 
-// Parts in the workspace merged in order, thread r its dim: part k lies in slot
-// slot(k).  The result goes to dst (row 0 of the group's heads in ctx), or to the
-// slot `into`, which may be one of them.  Four parts' loads go out together, past
-// L1 (fewer with many heads).
+// Up to 32 parts in the workspace merged in order: part k lies in slot slot(k).
+// A warp of the four takes every fourth head, a lane four dims; eight parts' loads
+// go out together, past L1.  The result goes to dst (the group's heads in ctx), or
+// to the slot `into`, which may be one of them (only the warp itself reads its
+// heads there).  (A thread a dim with all heads, three parts at a time: 3.4 us for
+// 8 parts of 6 heads, PD_MERGE us so.)
 template <int G, typename Slot>
-__device__ __forceinline__ void pd_merge(float *part, Slot slot, int parts, int r, bf16 *dst,
+__device__ __forceinline__ void pd_merge(const float *part, Slot slot, int parts, int w, bf16 *dst,
                                          float *into) {
-    constexpr int U = G > 6 ? 2 : G > 5 ? 3 : 4;  // (no register spills)
-    float M[G], A[G], S[G];
-#pragma unroll
-    for (int h = 0; h < G; ++h) {
-        M[h] = kPdNone;
-        A[h] = S[h] = 0.f;
-    }
+    const int lane = threadIdx.x & 31;
 #pragma unroll 1
-    for (int q0 = 0; q0 < parts; q0 += U) {
-        float2 bl[U][G];
-        float ov[U][G];
+    for (int h = w; h < G; h += 4) {
+        float2 bl = make_float2(kPdNone, 0.f);
+        if (lane < parts)
+            bl = __ldcg(reinterpret_cast<const float2 *>(part + (size_t)slot(lane) * kPagedSlot +
+                                                         kPdMaxG * 128 + 2 * h));
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float M = 0.f, wt = 0.f, S = 0.f;
+#pragma unroll 1
+        for (int q0 = 0; q0 < parts; q0 += 8) {
+            float4 v[8];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const float *pq = part + (size_t)slot(min(q0 + u, parts - 1)) * kPagedSlot;
+            for (int u = 0; u < 8; ++u) {
+                const int q = min(q0 + u, parts - 1);
+                v[u] = __ldcg(reinterpret_cast<const float4 *>(
+                    part + (size_t)slot(q) * kPagedSlot + h * 128 + 4 * lane));
+            }
+            if (q0 == 0) {
+                M = pd_warp_max(bl.x);
+                wt = lane < parts ? pd_exp2(bl.x - M) : 0.f;
+                S = warp_sum(wt * bl.y);
+            }
 #pragma unroll
-            for (int h = 0; h < G; ++h) {
-                bl[u][h] = __ldcg(reinterpret_cast<const float2 *>(pq + kPdMaxG * 128 + 2 * h));
-                ov[u][h] = __ldcg(pq + h * 128 + r);
+            for (int u = 0; u < 8; ++u) {
+                const float c = __shfl_sync(0xffffffffu, wt, (q0 + u) & 31);
+                if (q0 + u >= parts) continue;
+                acc.x = fmaf(c, v[u].x, acc.x);
+                acc.y = fmaf(c, v[u].y, acc.y);
+                acc.z = fmaf(c, v[u].z, acc.z);
+                acc.w = fmaf(c, v[u].w, acc.w);
             }
         }
-#pragma unroll
-        for (int h = 0; h < G; ++h) {
-            float mn = M[h];
-#pragma unroll
-            for (int u = 0; u < U; ++u) mn = fmaxf(mn, bl[u][h].x);
-            const float c = pd_exp2(M[h] - mn);
-            M[h] = mn;
-            A[h] *= c;
-            S[h] *= c;
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (q0 + u >= parts) break;
-                const float w = pd_exp2(bl[u][h].x - mn);
-                S[h] = fmaf(w, bl[u][h].y, S[h]);
-                A[h] = fmaf(w, ov[u][h], A[h]);
-            }
+        if (into) {
+            __syncwarp();
+            *reinterpret_cast<float4 *>(into + h * 128 + 4 * lane) = acc;
+            if (lane == 0)
+                *reinterpret_cast<float2 *>(into + kPdMaxG * 128 + 2 * h) = make_float2(M, S);
+            continue;
         }
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(pd_mean(acc.x, S), pd_mean(acc.y, S));
+        const __nv_bfloat162 hi = __floats2bfloat162_rn(pd_mean(acc.z, S), pd_mean(acc.w, S));
+        *reinterpret_cast<uint2 *>(dst + h * kPagedDh + 4 * lane) =
+            make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
     }
-    if (into) {
-        ptx::named_bar_sync(1, 128);  // all have read the slot
-#pragma unroll
-        for (int h = 0; h < G; ++h) {
-            into[h * 128 + r] = A[h];
-            if (r == 0)
-                *reinterpret_cast<float2 *>(into + kPdMaxG * 128 + 2 * h) = make_float2(M[h], S[h]);
-        }
-        return;
-    }
-#pragma unroll
-    for (int h = 0; h < G; ++h) dst[h * 128] = __float2bfloat16_rn(pd_mean(A[h], S[h]));
 }
 
 struct PdArgs {
@@ -404,8 +404,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     }
     if (warp == 1) tmem_alloc(&hd->tmem_base, kPdTmemCols);
     if (warp == 2 && small) {
-        // the tiles before each token; one outside the table has one, with no
-        // position: its ctx is zero
+        // the tiles before each token; one outside the table has none
         constexpr int E = kPdSmall / 32;
         int nt[E], sum = 0;
 #pragma unroll
@@ -415,7 +414,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             const bool in = a.pv.inside(sq, p);
             hd->seq[t] = sq;
             hd->n[t] = in ? p + 1 : 0;
-            nt[e] = t < a.T ? (in ? p / kPagedTile + 1 : 1) : 0;
+            nt[e] = in ? p / kPagedTile + 1 : 0;
             sum += nt[e];
         }
         int incl = sum;
@@ -461,9 +460,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 next.tok = tokens.token(w.i);
                 next.sq = small ? hd->seq[w.i] : a.seq[next.tok];
                 const int p = small ? hd->n[w.i] - 1 : a.pos[next.tok];
-                const bool in = a.pv.inside(next.sq, p);
-                next.n = in ? p + 1 : 0;
-                if (!in && next.sq >= 0 && lane == 0) set_error(err, kErrIndex);
+                next.n = p + 1;  // (a token with tiles lies inside the table)
             }
             next.g = w.g;
             next.first = w.first;
@@ -647,6 +644,14 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&hd->q_full[b]);
             pd_next(tokens, w);
+        }
+        // tokens with no position (padding, or outside the table): zeros
+        for (int i = cta; i < w.n_list; i += n_cta) {
+            if (tokens.before(i + 1) != tokens.before(i)) continue;
+            uint4 *row = reinterpret_cast<uint4 *>(a.ctx + (size_t)tokens.token(i) * a.Hq * kPagedDh);
+            for (int c = lane; c < a.Hq * kPagedDh / 8; c += 32) row[c] = make_uint4(0u, 0u, 0u, 0u);
+            const int t = tokens.token(i);
+            if (lane == 0 && a.seq[t] >= 0) set_error(err, kErrIndex);
         }
     } else {
         // ------------------------------------------------------------ softmax
@@ -846,7 +851,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 if (parts2 == 0) continue;
                 const int b2 = i ? pend_b1 : pend_b0, tg2 = i ? pend_tg1 : pend_tg0;
                 const int t2 = tg2 / Hkv, g2 = tg2 - t2 * Hkv;
-                bf16 *dst2 = a.ctx + ((size_t)t2 * a.Hq + g2 * G) * kPagedDh + r;
+                bf16 *dst2 = a.ctx + ((size_t)t2 * a.Hq + g2 * G) * kPagedDh;
                 // part k: the first slot of CTA b2 + k, but its second where the
                 // (token, head) starts
                 auto slot = [&](int k) { return 2 * (b2 + k) + (k == 0 ? 1 : 0); };
@@ -868,13 +873,13 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                     // of a (token, head) may start another)
                     if (!last_of(kPagedMaxCtas + b2 + k0 + n - 1, n)) continue;
                     float *into = a.part + (size_t)slot(k0) * kPagedSlot;
-                    pd_merge<G>(a.part, [&](int k) { return slot(k0 + k); }, n, r, nullptr, into);
+                    pd_merge<G>(a.part, [&](int k) { return slot(k0 + k); }, n, warp - 2, nullptr, into);
                 }
                 const int groups = parts2 > kPdGroup ? (parts2 + kPdGroup - 1) / kPdGroup : parts2;
                 if (!last_of(b2, groups)) continue;
                 pd_merge<G>(
                     a.part, [&](int k) { return slot(parts2 > kPdGroup ? k * kPdGroup : k); },
-                    groups, r, dst2, nullptr);
+                    groups, warp - 2, dst2, nullptr);
             }
         }
     }
