@@ -3,6 +3,8 @@
 
 #include <stdint.h>
 
+#include <atomic>
+
 #include "tc.cuh"
 
 namespace moe {
@@ -50,6 +52,21 @@ __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t v) {
         : "r"(h));
     return f;
 }
+
+// A kernel's dynamic shared memory, asked for once per device.
+struct SmemOnce {
+    std::atomic<uint64_t> done{0};  // bit: device
+    cudaError_t set(const void *kern, size_t bytes) {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+        if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+        return e;
+    }
+};
 
 // The tokens that the decode attention takes one by one, made on the device
 // (k_paged_plan): list[i] is a token, before[i] the position tiles (of

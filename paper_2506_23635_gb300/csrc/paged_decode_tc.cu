@@ -912,8 +912,8 @@ cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float
     if (!paged_map(&mk, a.kp, a, true) || !paged_map(&mv, a.vp, a, true))
         return cudaErrorInvalidValue;
     const void *kern = pd_kernel(G);
-    cudaError_t e =
-        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPdSmem);
+    static SmemOnce once[kPdMaxG];
+    cudaError_t e = once[G - 1].set(kern, kPdSmem);
     if (e != cudaSuccess) return e;
     PdArgs pa{small ? a.T : 0, a.Hq, a.Hkv, a.pv, l, a.seq, a.pos, static_cast<const bf16 *>(a.q), a.ks, a.vs,
               static_cast<bf16 *>(a.ctx), part, device_info().err};

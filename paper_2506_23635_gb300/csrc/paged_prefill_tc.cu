@@ -644,8 +644,8 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
 
 cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, cudaStream_t st) {
     const void *kern = (const void *)k_paged_prefill_tc;
-    cudaError_t e =
-        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPfSmem);
+    static SmemOnce once;
+    cudaError_t e = once.set(kern, kPfSmem);
     if (e != cudaSuccess) return e;
     PfArgs pa{{}, {}, a.Hq, a.Hkv, a.pv, plan, static_cast<const bf16 *>(a.q), a.ks, a.vs,
               static_cast<bf16 *>(a.ctx), device_info().err};

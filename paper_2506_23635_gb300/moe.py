@@ -549,10 +549,10 @@ class PagedCache:
         dev = self.device_index
         _want(seq, (T,), torch.int32, dev, "seq")
         _want(pos, (T,), torch.int32, dev, "pos")
-        if dev != torch.cuda.current_device():
+        if dev < 0 or dev != torch._C._cuda_getDevice():
             raise ValueError(f"the cache is on device {dev}, which is not the current one")
-        if stream is None:
-            return torch.cuda.current_stream(dev).cuda_stream
+        if stream is None:  # (what torch.cuda.current_stream wraps, 3 us less)
+            return torch._C._cuda_getCurrentRawStream(dev)
         if stream.device_index != dev:
             raise ValueError(f"the stream is not of the cache's device {dev}")
         return stream.cuda_stream
