@@ -516,7 +516,8 @@ constexpr int kPlanThreads = 1024;
 
 __global__ void __launch_bounds__(kPlanThreads)
 k_paged_plan(int T, const PageView pv, const int32_t *__restrict__ seq,
-             const int32_t *__restrict__ pos, const PagedList l, const PlanArgs pa, bool small) {
+             const int32_t *__restrict__ pos, const PagedList l, const PlanArgs pa,
+             int *unit_count, bool small) {
     ptx::grid_dependency_wait();
     // (after the wait: what starts now finds all that is ahead of the call complete)
     ptx::launch_dependents();
@@ -524,6 +525,8 @@ k_paged_plan(int T, const PageView pv, const int32_t *__restrict__ seq,
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < 2 * kPagedMaxCtas; i += kPlanThreads) l.count[i] = 0;
     if (small) return;
+    if (pa.plan.head)
+        for (int i = tid; i < 2 * kPagedUnitParts; i += kPlanThreads) unit_count[i] = 0;
     int n = T;
     if (pa.plan.head) {  // only those that no tile holds
         plan_attention<kPlanThreads>(T, pa);
@@ -576,7 +579,7 @@ moe_status cuda_status(cudaError_t e) { return e == cudaSuccess ? MOE_OK : MOE_E
 
 // Workspace of moe_paged_attend.
 struct PagedWs {
-    size_t n_list, count, list, before, head, tiles, part, total;
+    size_t n_list, count, list, before, head, tiles, unit_count, part, unit_part, total;
 };
 
 PagedWs paged_ws(int64_t T) {
@@ -589,7 +592,10 @@ PagedWs paged_ws(int64_t T) {
     L.before = o; o += up(((size_t)T + 1) * 8);
     L.head = o; o += up(sizeof(AttnPlanHead));
     L.tiles = o; o += up((size_t)(T / kAttnTileMinRows) * sizeof(int4));
+    L.unit_count = o; o += up(2 * kPagedUnitParts * 4);
     L.part = o; o += up(kPagedPartFloats * 4);
+    // (calls of fewer tokens hold no tile)
+    L.unit_part = o; o += T >= kAttnTileMinRows ? up(kPagedUnitPartFloats * 4) : 0;
     L.total = o;
     return L;
 }
@@ -615,17 +621,23 @@ cudaError_t attend(const PagedAttn &a, void *ws, cudaStream_t st) {
         int T = a.T;
         PageView pv = a.pv;
         const int32_t *seq = a.seq, *pos = a.pos;
-        void *args[] = {&T, &pv, &seq, &pos, &l, &pa, &small};
+        int *unit_count = at<int>(ws, L.unit_count);
+        void *args[] = {&T, &pv, &seq, &pos, &l, &pa, &unit_count, &small};
         LaunchScope ls("paged_plan", st);
         cudaError_t e =
             launch_pdl((const void *)k_paged_plan, dim3(1), dim3(kPlanThreads), 0, st, args);
         if (e != cudaSuccess) return e;
     }
     if (pa.plan.head) {
-        cudaError_t e = launch_paged_prefill_tc(a, pa.plan, st);
+        cudaError_t e = launch_paged_prefill_tc(a, pa.plan, at<float>(ws, L.unit_part),
+                                                at<int>(ws, L.unit_count), st);
         if (e != cudaSuccess) return e;
     }
-    return launch_paged_decode_tc(a, l, at<float>(ws, L.part), small, st);
+    return launch_paged_decode_tc(a, l, at<float>(ws, L.part),
+                                  small            ? kPagedAheadZero
+                                  : pa.plan.head ? kPagedAheadPrefill
+                                                   : kPagedAheadPlan,
+                                  st);
 }
 
 moe_status check_paged(const moe_sa_dims *d, const moe_paged_dims *pd) {

@@ -110,11 +110,19 @@ inline bool paged_map(CUtensorMap *m, const void *base, const PagedAttn &a, bool
 }
 
 // Attention of the listed tokens over the 8-bit cache (paged_decode_tc.cu).
-// Attention of the plan's tiles (paged_prefill_tc.cu).
-cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, cudaStream_t st);
-// small: a call of up to kPagedSmall tokens, all taken one by one; the kernel
-// then lists them itself, and only the counters are the plan's.
-cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, bool small,
+// Attention of the plan's tiles (paged_prefill_tc.cu).  part, count: where a unit
+// of work is shared by several CTAs; 2 counters a part, zero at the start.
+constexpr int kPagedUnitParts = 160;  // one for each SM
+constexpr size_t kPagedUnitPartFloats = (size_t)kPagedUnitParts * 2 * 128 * (128 + 2);
+cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, float *part,
+                                    int *count, cudaStream_t st);
+// ahead: what the launch ahead is.  kPagedAheadZero: k_paged_plan for a call of up
+// to kPagedSmall tokens, all taken one by one: the kernel lists them itself, and
+// only the counters are the plan's.  kPagedAheadPlan: k_paged_plan.
+// kPagedAheadPrefill: the prefill attention, whose results are not read here:
+// this kernel runs beside it, as that one leaves SMs.
+enum : int { kPagedAheadZero = 0, kPagedAheadPlan = 1, kPagedAheadPrefill = 2 };
+cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, int ahead,
                                    cudaStream_t st);
 
 }  // namespace moe

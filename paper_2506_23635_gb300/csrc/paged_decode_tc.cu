@@ -355,6 +355,7 @@ __device__ __forceinline__ void pd_merge(const float *part, Slot slot, int parts
 
 struct PdArgs {
     int T;  // tokens of a small call, all of them listed; 0: as the plan lists them
+    int ahead;
     int Hq, Hkv;
     PageView pv;
     PagedList list;
@@ -378,8 +379,9 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     const int cta = (int)blockIdx.x, n_cta = (int)gridDim.x, Hkv = a.Hkv;
     unsigned *err = a.err;
     ptx::launch_dependents();
-    // (the launch ahead, k_paged_plan, lets this one start once all that is ahead
-    // of the call is complete; a small call waits for it before it counts only)
+    // (k_paged_plan lets this one start once all that is ahead of the call is
+    // complete; a small call waits for it only before it counts.  The prefill
+    // attention starts after the plan is complete, and lets this one start then)
     const bool small = a.T > 0;
     if (threadIdx.x == 0) {
         for (int b = 0; b < kPdStages; ++b) {
@@ -434,7 +436,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (!small) ptx::grid_dependency_wait();
+    if (a.ahead == kPagedAheadPlan) ptx::grid_dependency_wait();
     const PdTokens tokens{a.list, hd, a.seq, a.pos, a.pv, a.T};
     const uint32_t tmem = hd->tmem_base;
     const uint32_t sbase = ptx::smem_u32(smem);
@@ -887,7 +889,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     __syncthreads();
     tc_fence_after();
     if (warp == 1) tmem_dealloc(tmem, kPdTmemCols);
-    if (small) ptx::grid_dependency_wait();  // (complete only after what is ahead is)
+    if (a.ahead != kPagedAheadPlan) ptx::grid_dependency_wait();  // (complete after what is ahead)
 }
 
 const void *pd_kernel(int G) {
@@ -905,7 +907,7 @@ const void *pd_kernel(int G) {
 
 }  // namespace
 
-cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, bool small,
+cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, int ahead,
                                    cudaStream_t st) {
     const int G = a.Hq / a.Hkv;
     CUtensorMap mk, mv;
@@ -915,7 +917,7 @@ cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float
     static SmemOnce once[kPdMaxG];
     cudaError_t e = once[G - 1].set(kern, kPdSmem);
     if (e != cudaSuccess) return e;
-    PdArgs pa{small ? a.T : 0, a.Hq, a.Hkv, a.pv, l, a.seq, a.pos, static_cast<const bf16 *>(a.q), a.ks, a.vs,
+    PdArgs pa{ahead == kPagedAheadZero ? a.T : 0, ahead, a.Hq, a.Hkv, a.pv, l, a.seq, a.pos, static_cast<const bf16 *>(a.q), a.ks, a.vs,
               static_cast<bf16 *>(a.ctx), part, device_info().err};
     void *args[] = {&mk, &mv, &pa};
     // as many CTAs as the largest positions give shares

@@ -73,6 +73,7 @@ constexpr uint32_t kPfTmemCols = 512, kPfColS = 0, kPfColO = 256;
 constexpr float kPfTop = 7.f, kPfSlack = 8.f;
 constexpr float kPfNone = -1e30f;
 constexpr float kPfLeast = 7.888609052210118e-31f;  // 2^-100: nothing times a score
+constexpr int kPfMaxParts = 16, kPfMinTiles = 6;  // of a unit; of a part
 constexpr int kPfRing = 8;  // tiles' scales
 
 struct PfScales {
@@ -96,6 +97,7 @@ struct PfHeader {
     uint32_t tmem_base;
     int next;
     int gave_up;
+    int last[2];  // a head's part was counted last
     alignas(16) PfScales sc[kPfRing];
 };
 constexpr int kPfBars = (int)((offsetof(PfHeader, done) - offsetof(PfHeader, q_full)) / 8) + 1;
@@ -177,12 +179,16 @@ struct PfArgs {
     const bf16 *q;
     const float *ks, *vs;
     bf16 *ctx;
+    float *part;  // kPagedUnitParts parts
+    int *count;   // of finished parts, a (unit, head of it) each; zero at the start
     unsigned *err;
 };
 
 struct PfUnit {
     int t0, rows, p0, sq;  // the tile: first token, tokens, position, sequence
-    int g, h0, nh, n_kv;   // key/value head, first query head, heads, position tiles
+    int g, h0, nh;         // key/value head, first query head, heads
+    int j0, n_kv;          // first position tile, position tiles
+    int parts, slot0, c;   // its parts, the first one's slot, which one this is
 };
 
 // Every tile's pages by TMA, as they are, keys and values each into one buffer
@@ -196,7 +202,7 @@ __device__ __forceinline__ bool pf_fetch(const PfArgs &a, PfHeader *hd, unsigned
     const uint64_t pol = ptx::policy_evict_last();
     const int32_t *table = a.pv.table + (size_t)u.sq * a.pv.max_pages;
     auto entry = [&](int j) {
-        const int p = j * kPfRows + (lane << shift);
+        const int p = (u.j0 + j) * kPfRows + (lane << shift);
         return j < u.n_kv && lane < per && p <= last ? table[p >> shift] : -1;
     };
     int next = entry(0);
@@ -204,7 +210,7 @@ __device__ __forceinline__ bool pf_fetch(const PfArgs &a, PfHeader *hd, unsigned
 #pragma unroll 1
     for (int j = 0; j < u.n_kv; ++j) {
         const int pg = next >= 0 && next < a.pv.n_pages ? next : -1;
-        if (pg < 0 && lane < per && j * kPfRows + (lane << shift) <= last)
+        if (pg < 0 && lane < per && (u.j0 + j) * kPfRows + (lane << shift) <= last)
             set_error(a.err, kErrIndex);
         next = entry(j + 1);
         // the scales of 16 positions a lane
@@ -295,7 +301,7 @@ __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigne
             for (int k = 0; k < B; ++k) {
                 const int r4 = w + (half * B + k) * kPfDecWarps, row = r4 * 4 + (lane >> 3);
                 if (r4 >= kPfRows / 4) break;
-                const bool live = j * kPfRows + row <= last && ((ok >> (row >> 4)) & 1u);
+                const bool live = (u.j0 + j) * kPfRows + row <= last && ((ok >> (row >> 4)) & 1u);
                 if (!live) x[k] = make_uint4(0u, 0u, 0u, 0u);
                 const uint32_t v[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
                 uint32_t y[8];
@@ -394,17 +400,17 @@ __device__ __forceinline__ float pf_queries(const PfArgs &a, unsigned char *smem
     return 0.12751743f * __uint_as_float((uint32_t)(e - 14) << 23);
 }
 
-// One row's softmax over a unit's tiles; l: the row sum.
+// One row's softmax over a unit's tiles; m, l: its exponent base, its sum.
 __device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_t o_col,
-                                           const PfUnit &u, int r, int x, float qs, float &l,
-                                           unsigned *err) {
+                                           const PfUnit &u, int r, int x, float qs, float &m,
+                                           float &l, unsigned *err) {
     const int lane = threadIdx.x & 31;
-    float m = kPfNone;
+    m = kPfNone;
     l = 0.f;
     bool good = true;
 #pragma unroll 1
     for (int j = 0; j < u.n_kv; ++j) {
-        const int lim = u.p0 + r - j * kPfRows;  // the row's last position in the tile
+        const int lim = u.p0 + r - (u.j0 + j) * kPfRows;  // the row's last position in the tile
         good = good && pf_wait_all(&hd->t_full[j % kPfRing], (uint32_t)(j / kPfRing) & 1u, err);
         good = good && pf_wait_all(&hd->s_full[x], j & 1, err);
         tc_fence_after();
@@ -420,7 +426,7 @@ __device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_
         *reinterpret_cast<float4 *>(&cs[4]) = *reinterpret_cast<const float4 *>(&sc->ks[4]);
         *reinterpret_cast<float4 *>(&lv[0]) = *reinterpret_cast<const float4 *>(&sc->lv[0]);
         *reinterpret_cast<float4 *>(&lv[4]) = *reinterpret_cast<const float4 *>(&sc->lv[4]);
-        if (j * kPfRows + kPfRows - 1 > u.p0 || ok != 0xffu) {
+        if ((u.j0 + j) * kPfRows + kPfRows - 1 > u.p0 || ok != 0xffu) {
             // positions past the row's own, and without a page: their score is
             // -inf (cs is positive)
 #pragma unroll
@@ -490,10 +496,15 @@ __device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_
     return good;
 }
 
-__device__ __forceinline__ PfUnit pf_unit(const PfArgs &a, int unit, int G, int per, bool single) {
-    const int tile = unit / (a.Hkv * per), gp = unit - tile * a.Hkv * per;
-    const int4 td = __ldcg(&a.plan.tiles[tile]);
+// Unit `unit` of S parts of each (tile, heads).
+__device__ __forceinline__ PfUnit pf_unit(const PfArgs &a, int unit, int G, int per, bool single,
+                                          int S) {
     PfUnit u;
+    const int whole = unit / S;
+    u.c = unit - whole * S;
+    u.slot0 = whole * S;
+    const int tile = whole / (a.Hkv * per), gp = whole - tile * a.Hkv * per;
+    const int4 td = __ldcg(&a.plan.tiles[tile]);
     u.g = gp / per;
     const int hp = gp - u.g * per;
     u.h0 = u.g * G + (single ? hp : 2 * hp);
@@ -502,8 +513,85 @@ __device__ __forceinline__ PfUnit pf_unit(const PfArgs &a, int unit, int G, int 
     u.rows = td.y;
     u.p0 = td.z;
     u.sq = td.w;
-    u.n_kv = (u.p0 + u.rows - 1) / kPfRows + 1;
+    const int n = (u.p0 + u.rows - 1) / kPfRows + 1;
+    u.parts = min(S, n);
+    // (a unit of fewer tiles than parts has nothing for the last ones)
+    u.j0 = u.c < u.parts ? (int)((long long)u.c * n / u.parts) : n;
+    u.n_kv = u.c < u.parts ? (int)((long long)(u.c + 1) * n / u.parts) - u.j0 : 0;
     return u;
+}
+
+// A part of a head's rows left in the workspace, a column's rows side by side;
+// the part that is counted last merges them all.  Thread r its row.
+__device__ __noinline__ void pf_part(const PfArgs &a, PfHeader *hd, const PfUnit &u, int x, int r,
+                                        uint32_t o_col, float m, float l) {
+    constexpr size_t kHead = (size_t)kPfRows * (128 + 2);  // a head's part
+    auto at = [&](int c) { return a.part + ((size_t)(u.slot0 + c) * 2 + x) * kHead; };
+    float *mine = at(u.c);
+#pragma unroll 1
+    for (int c = 0; c < 128; c += 32) {
+        float v[32];
+        tmem_ld32(o_col + c, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) mine[(c + i) * kPfRows + r] = v[i];
+    }
+    reinterpret_cast<float2 *>(mine + 128 * kPfRows)[r] = make_float2(m, l);
+    auto meet = [&]() {  // the head's threads
+        if (x == 0) ptx::named_bar_sync(1, 128);
+        else ptx::named_bar_sync(2, 128);
+    };
+    meet();
+    if (r == 0) {
+        __threadfence();
+        hd->last[x] = atomicAdd(&a.count[u.slot0 * 2 + x], 1) == u.parts - 1;
+        __threadfence();
+    }
+    meet();
+    if (!hd->last[x] || r >= u.rows) return;
+    float M = kPfNone, L = 0.f;
+    {
+        float2 ml[kPfMaxParts];
+#pragma unroll
+        for (int c = 0; c < kPfMaxParts; ++c)
+            ml[c] = __ldcg(reinterpret_cast<const float2 *>(at(min(c, u.parts - 1)) + 128 * kPfRows) + r);
+#pragma unroll
+        for (int c = 0; c < kPfMaxParts; ++c) M = fmaxf(M, ml[c].x);
+#pragma unroll
+        for (int c = 0; c < kPfMaxParts; ++c)
+            L = c < u.parts ? fmaf(pf_exp2(ml[c].x - M), ml[c].y, L) : L;
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    bf16 *dst = a.ctx + ((size_t)(u.t0 + r) * a.Hq + u.h0 + x) * kPagedDh;
+    // (64 columns' loads go out together: with eight 20 us for three parts)
+#pragma unroll 1
+    for (int c0 = 0; c0 < 128; c0 += 64) {
+        float s[64];
+#pragma unroll
+        for (int i = 0; i < 64; ++i) s[i] = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < u.parts; ++c) {
+            const float *p = at(c) + c0 * kPfRows + r;
+            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(at(c) + 128 * kPfRows) + r);
+            float v[64];
+#pragma unroll
+            for (int i = 0; i < 64; ++i) v[i] = __ldcg(p + i * kPfRows);
+            const float w = pf_exp2(ml.x - M);
+#pragma unroll
+            for (int i = 0; i < 64; ++i) s[i] = fmaf(w, v[i], s[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 64; i += 8) {
+            uint32_t o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const __nv_bfloat162 p2 =
+                    __floats2bfloat162_rn(s[i + 2 * e] * inv, s[i + 2 * e + 1] * inv);
+                o[e] = *reinterpret_cast<const uint32_t *>(&p2);
+            }
+            *reinterpret_cast<uint4 *>(dst + c0 + i) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    }
 }
 
 __global__ void __launch_bounds__(kPfThreads, 1)
@@ -523,7 +611,18 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
     // few tiles: a unit holds one head, so that the longest is shorter
     const bool single = n_left == 0 && 3 * n_tiles * a.Hq <= 4 * (int)gridDim.x;
     const int per = single ? G : pairs;
-    const int n_units = n_tiles * a.Hkv * per;
+    // and where there are at least two CTAs to each unit, it is cut along the
+    // positions into as many parts, of kPfMinTiles tiles or more (a part costs ~7 us
+    // to start and leave, its merge 2-3: 512 tokens at position 5000, 96 units of 40
+    // to 44 tiles on 152 SMs, take 127 us whole, 125 in three parts each)
+    const int n_whole = n_tiles * a.Hkv * per;
+    int S = 1;
+    if (n_whole > 0 && 2 * n_whole <= (int)gridDim.x) {
+        const int4 longest = __ldcg(&a.plan.tiles[0]);
+        S = min(min(kPfMaxParts, (int)gridDim.x / n_whole),
+                max(1, ((longest.z + longest.y - 1) / kPfRows + 1) / kPfMinTiles));
+    }
+    const int n_units = n_whole * S;
     int unit = (int)blockIdx.x;
     if (unit >= n_units) return;
     if (threadIdx.x == 0) hd->gave_up = 0;
@@ -566,10 +665,10 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
 #pragma unroll 1
         for (bool again = false;; again = true) {
             begin(again);
-            const PfUnit u = pf_unit(a, unit, G, per, single);
+            const PfUnit u = pf_unit(a, unit, G, per, single, S);
             bool good = true;
             if (warp == 0) {
-                if (lane == 0) {
+                if (lane == 0 && u.n_kv > 0) {
                     good = pf_issue(hd, sbase, hd->tmem_base, u, err);
                     mma_commit(&hd->done);
                     good &= pf_wait(&hd->done, 0, err);
@@ -598,20 +697,22 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
 #pragma unroll 1
         for (bool again = false;; again = true) {
             begin(again);
-            const PfUnit u = pf_unit(a, unit, G, per, single);
-            if (x < u.nh) {
+            const PfUnit u = pf_unit(a, unit, G, per, single, S);
+            if (x < u.nh && u.n_kv > 0) {
                 const uint32_t at = hd->tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)x * 128;
                 const uint32_t s_col = at + kPfColS, o_col = at + kPfColO;
                 const float qs = pf_queries(a, smem, u, x, r);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&hd->q_full[x]);
-                float l = 0.f;
-                bool good = pf_softmax(hd, s_col, o_col, u, r, x, qs, l, err);
+                float m = kPfNone, l = 0.f;
+                bool good = pf_softmax(hd, s_col, o_col, u, r, x, qs, m, l, err);
                 good = good && pf_wait_all(&hd->o_full[x], (u.n_kv - 1) & 1, err);
                 if (!good) hd->gave_up = 1;
-                if (good) {
-                    tc_fence_after();
+                if (good) tc_fence_after();
+                if (good && u.parts > 1) {
+                    pf_part(a, hd, u, x, r, o_col, m, l);
+                } else if (good) {
                     const float inv = l == 0.f ? 0.f : 1.f / l;
                     bf16 *dst = a.ctx + ((size_t)(u.t0 + r) * a.Hq + u.h0 + x) * kPagedDh;
 #pragma unroll
@@ -642,20 +743,22 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
 
 }  // namespace
 
-cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, cudaStream_t st) {
+cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, float *part,
+                                    int *count, cudaStream_t st) {
     const void *kern = (const void *)k_paged_prefill_tc;
     static SmemOnce once;
     cudaError_t e = once.set(kern, kPfSmem);
     if (e != cudaSuccess) return e;
     PfArgs pa{{}, {}, a.Hq, a.Hkv, a.pv, plan, static_cast<const bf16 *>(a.q), a.ks, a.vs,
-              static_cast<bf16 *>(a.ctx), device_info().err};
+              static_cast<bf16 *>(a.ctx), part, count, device_info().err};
     if (!paged_map(&pa.tmK, a.kp, a, false) || !paged_map(&pa.tmV, a.vp, a, false))
         return cudaErrorInvalidValue;
     void *args[] = {&pa};
-    const long long most = (long long)a.Hq * (a.T / kAttnTileMinRows);
+    const int ctas = std::min(device_info().sm_count, kPagedUnitParts);
+    const long long most = (long long)kPfMaxParts * a.Hq * (a.T / kAttnTileMinRows);
     LaunchScope ls("paged_prefill_tc", st);
     return launch_pdl(
-        kern, dim3((unsigned)std::max(1LL, std::min<long long>(most, device_info().sm_count))),
+        kern, dim3((unsigned)std::max(1LL, std::min<long long>(most, ctas))),
         dim3(kPfThreads), kPfSmem, st, args);
 }
 

@@ -266,6 +266,7 @@ ATTEND = {
     "two_chunks": [(0, 100, 300), (1, 0, 205)] + [(2 + i, 40 * i, 1) for i in range(24)],
     "full_tiles": [(0, 0, 384)],
     "late_chunk": [(0, 1900, 129)],
+    "far_chunks": [(0, 7000, 40), (1, 100, 20), (2, 3000, 130)],  # units cut into parts
     "short_runs": [(i, 50 + i, 15) for i in range(10)],
     "chunks_of_16": [(i, 100 * i, 16) for i in range(12)],
 }
