@@ -298,7 +298,8 @@ moe_status moe_get_last_error(moe_stream_t stream);
  * moe_layer_forward_experts, moe_prenorm, moe_stack_forward,
  * moe_layer_forward_noalloc, moe_sa_qkv,
  * moe_sa_attend, moe_sa_forward, moe_decoder_forward, moe_paged_append,
- * moe_paged_attend) returns that status at once without launching.
+ * moe_paged_attend, moe_paged_sa_forward, moe_paged_decoder_forward) returns
+ * that status at once without launching.
  * With MOE_WM_SINGLE_CTA=1 the prefill expert GEMMs (batches whose experts
  * hold 128 or more slots on average) run one CTA per tile, the form used on
  * devices that cannot keep CTA pairs resident, instead of CTA pairs. */
@@ -483,6 +484,34 @@ moe_status moe_paged_attend(const moe_sa_dims *dims, const moe_paged_dims *paged
                             const int32_t *page_table, const void *k_pages, const void *v_pages,
                             const float *k_scale, const float *v_scale, void *ctx, void *ws,
                             size_t ws_bytes, moe_stream_t stream);
+
+/* moe_paged_sa_forward: moe_sa_forward over the paged cache, in place on resid:
+ * resid += w_o . Attn(RMSNorm0(resid)), the projection's rows appended as by
+ * moe_paged_append, then attended to as by moe_paged_attend.  A padding token's
+ * row of resid is unchanged but for w_o . 0.  ws: moe_paged_sa_workspace_size
+ * bytes. */
+moe_status moe_paged_sa_workspace_size(const moe_sa_dims *dims, int32_t max_tokens, size_t *bytes);
+moe_status moe_paged_sa_forward(const moe_sa_dims *dims, const moe_paged_dims *paged, int32_t T,
+                                const int32_t *seq, const int32_t *pos, const int32_t *page_table,
+                                float *resid, const void *w_qkv, const void *w_o, void *k_pages,
+                                void *v_pages, float *k_scale, float *v_scale, float eps, void *ws,
+                                size_t ws_bytes, moe_stream_t stream);
+
+/* moe_paged_decoder_forward: moe_decoder_forward over paged caches, one for each
+ * layer (HOST arrays of n_layers DEVICE pointers), all with the same page
+ * table.  ws: moe_paged_decoder_workspace_size bytes. */
+moe_status moe_paged_decoder_workspace_size(const moe_sa_dims *attn, const moe_dims *moe,
+                                            int32_t max_tokens, size_t *bytes);
+moe_status moe_paged_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe,
+                                     const moe_paged_dims *paged, int32_t n_layers, int32_t T,
+                                     const int32_t *seq, const int32_t *pos,
+                                     const int32_t *page_table, float *resid,
+                                     const void *const *w_qkv, const void *const *w_o,
+                                     const void *const *w_router, const void *const *w1,
+                                     const void *const *v1, const void *const *w2,
+                                     void *const *k_pages, void *const *v_pages,
+                                     float *const *k_scale, float *const *v_scale, float eps,
+                                     void *ws, size_t ws_bytes, moe_stream_t stream);
 
 #ifdef __cplusplus
 }

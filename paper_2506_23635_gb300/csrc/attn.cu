@@ -44,6 +44,7 @@
 #include <algorithm>
 
 #include "attn_plan.cuh"
+#include "paged.cuh"
 
 namespace moe {
 namespace {
@@ -733,26 +734,34 @@ struct SaCall {
     int nr() const { return (d.n_heads + 2 * d.n_kv_heads) * kHeadDim; }
 };
 
-// W_qkv . xn -> qkv (fp32), then the rotary embedding and the cache writes.
-cudaError_t qkv_rope(const SaCall &c, const void *xn, const void *w_qkv, const int32_t *seq,
-                     const int32_t *pos, int n_seq, int L, float *q, void *kc, void *vc,
-                     bf16 *q16 = nullptr) {
+// W_qkv . xn -> qkv (fp32, in the workspace): n_part partial sums, T * nr floats
+// apart, or, n_part 0, as many as `split` says of each.
+cudaError_t qkv_project(const SaCall &c, const void *xn, const void *w_qkv, int *n_part,
+                        ProjSplit *split) {
     const moe_dims pd = proj_dims(c.nr(), c.d.d_model);
     const int32_t *offsets = at<int32_t>(c.ws, c.L.offsets);
     float *qkv = at<float>(c.ws, c.L.qkv);
-    cudaError_t e;
+    *n_part = 1;
+    if (proj_split(c.T, c.d.d_model, c.nr(), split)) {
+        *n_part = 0;
+        return launch_proj_wm(c.T, c.d.d_model, c.nr(), xn, w_qkv, qkv, *split, c.st, "qkv_gemm_tc");
+    }
+    if (gemm_rows_fits(c.T, c.nr())) {
+        *n_part = gemm_rows_parts(c.T, c.d.d_model, c.nr());
+        return launch_gemm_rows_tc(c.T, c.d.d_model, c.nr(), xn, w_qkv, *n_part, qkv, c.st,
+                                   "qkv_rows_tc");
+    }
+    return launch_gemm_down_wm(pd, c.T, xn, offsets, w_qkv, qkv, c.st, "qkv_gemm_tc");
+}
+
+// The projection, then the rotary embedding and the cache writes.
+cudaError_t qkv_rope(const SaCall &c, const void *xn, const void *w_qkv, const int32_t *seq,
+                     const int32_t *pos, int n_seq, int L, float *q, void *kc, void *vc,
+                     bf16 *q16 = nullptr) {
+    const float *qkv = at<float>(c.ws, c.L.qkv);
     int n_part = 1;
     ProjSplit split{};
-    if (proj_split(c.T, c.d.d_model, c.nr(), &split)) {
-        n_part = 0;
-        e = launch_proj_wm(c.T, c.d.d_model, c.nr(), xn, w_qkv, qkv, split, c.st, "qkv_gemm_tc");
-    } else if (gemm_rows_fits(c.T, c.nr())) {
-        n_part = gemm_rows_parts(c.T, c.d.d_model, c.nr());
-        e = launch_gemm_rows_tc(c.T, c.d.d_model, c.nr(), xn, w_qkv, n_part, qkv, c.st,
-                                "qkv_rows_tc");
-    } else {
-        e = launch_gemm_down_wm(pd, c.T, xn, offsets, w_qkv, qkv, c.st, "qkv_gemm_tc");
-    }
+    const cudaError_t e = qkv_project(c, xn, w_qkv, &n_part, &split);
     if (e != cudaSuccess) return e;
     long long pstride = (long long)c.T * c.nr();
     int Hq = c.d.n_heads, Hkv = c.d.n_kv_heads, ns = n_seq, Lv = L;
@@ -910,6 +919,21 @@ cudaError_t out_proj(const SaCall &c, const void *ctx, const void *w_o, float *r
     return launch_pdl((const void *)k_residual_add, dim3(grid), dim3(256), 0, c.st, args);
 }
 
+// RMSNorm0 of the residual -> the workspace's xn, and the attention's plan.
+cudaError_t launch_prenorm(const SaCall &c, const float *resid, float eps, PlanArgs pa) {
+    int Tv = c.T, D = c.d.d_model;
+    bf16 *xn = at<bf16>(c.ws, c.L.xn);
+    int32_t *off = at<int32_t>(c.ws, c.L.offsets);
+    void *args[] = {&Tv, &D, &resid, &xn, &eps, &off, &pa};
+    const dim3 grid(c.T + (pa.plan.head ? 1 : 0));
+    LaunchScope ls("sa_prenorm", c.st);
+    return c.T >= kNormWideMinTokens
+               ? launch_pdl((const void *)k_sa_prenorm<kNormThreadsWide, kNormMaxVec>, grid,
+                            dim3(kNormThreadsWide), 0, c.st, args)
+               : launch_pdl((const void *)k_sa_prenorm<kNormThreads, 4>, grid, dim3(kNormThreads),
+                            0, c.st, args);
+}
+
 moe_status check_ws(const moe_sa_dims *d, int T, void *ws, size_t ws_bytes) {
     size_t need = sa_ws(*d, T).total;
     if (!ws || !aligned16(ws) || ws_bytes < need) return MOE_ERR_WORKSPACE;
@@ -950,22 +974,8 @@ moe_status sa_forward_impl(const moe_sa_dims *dims, int32_t T, const int32_t *se
     bf16 *xn = at<bf16>(ws, c.L.xn);
     float *q = at<float>(ws, c.L.q);
     bf16 *ctx = at<bf16>(ws, c.L.ctx);
-    {
-        int Tv = T, D = dims->d_model;
-        const float *rc = resid;
-        int32_t *off = at<int32_t>(ws, c.L.offsets);
-        PlanArgs pa = plan_args(c, seq, pos, n_seq, max_len);
-        void *args[] = {&Tv, &D, &rc, &xn, &eps, &off, &pa};
-        const dim3 grid(T + (pa.plan.head ? 1 : 0));
-        LaunchScope ls("sa_prenorm", c.st);
-        const cudaError_t e =
-            T >= kNormWideMinTokens
-                ? launch_pdl((const void *)k_sa_prenorm<kNormThreadsWide, kNormMaxVec>, grid,
-                             dim3(kNormThreadsWide), 0, c.st, args)
-                : launch_pdl((const void *)k_sa_prenorm<kNormThreads, 4>, grid,
-                             dim3(kNormThreads), 0, c.st, args);
-        if (e != cudaSuccess) return MOE_ERR_CUDA;
-    }
+    if (launch_prenorm(c, resid, eps, plan_args(c, seq, pos, n_seq, max_len)) != cudaSuccess)
+        return MOE_ERR_CUDA;
     bf16 *q16 = wants_q16(T, n_seq) ? at<bf16>(ws, c.L.q16) : nullptr;
     // (only the CUDA-core attention reads the fp32 queries)
     cudaError_t e = qkv_rope(c, xn, w_qkv, seq, pos, n_seq, max_len, decode_tc() ? nullptr : q,
@@ -973,6 +983,75 @@ moe_status sa_forward_impl(const moe_sa_dims *dims, int32_t T, const int32_t *se
     if (e == cudaSuccess) e = attend(c, q, seq, pos, n_seq, max_len, k_cache, v_cache, ctx, q16);
     if (e == cudaSuccess) e = out_proj(c, ctx, w_o, resid, xn_next, eps);
     return cuda_status(e);
+}
+
+// The block over the paged cache: scratch of the projections, then of the
+// attention.
+moe_status paged_sa_impl(const moe_sa_dims *dims, const moe_paged_dims *paged, int32_t T,
+                         const int32_t *seq, const int32_t *pos, const int32_t *table, float *resid,
+                         const void *w_qkv, const void *w_o, void *kp, void *vp, float *ks,
+                         float *vs, float eps, void *ws, size_t ws_bytes, moe_stream_t stream,
+                         bf16 *xn_next) {
+    moe_status s = check_paged_call(dims, paged, T, seq, pos, table, kp, vp, ks, vs);
+    if (s != MOE_OK) return s;
+    if (!(eps > 0.f)) return MOE_ERR_INVALID_ARG;
+    if (T == 0) return MOE_OK;
+    if (!ok_ptr(resid) || !ok_ptr(w_qkv) || !ok_ptr(w_o)) return MOE_ERR_INVALID_ARG;
+    size_t need = 0;
+    if ((s = moe_paged_sa_workspace_size(dims, T, &need)) != MOE_OK) return s;
+    if (!ws || !aligned16(ws) || ws_bytes < need) return MOE_ERR_WORKSPACE;
+    SaCall c{*dims, T, (cudaStream_t)stream, ws, sa_ws(*dims, T)};
+    if (!tc_path_ok(proj_dims(c.nr(), dims->d_model)) ||
+        !tc_path_ok(proj_dims(dims->d_model, c.nq())))
+        return MOE_ERR_UNSUPPORTED;
+    void *attn_ws = static_cast<char *>(ws) + c.L.total;
+    bf16 *q = at<bf16>(ws, c.L.q16), *ctx = at<bf16>(ws, c.L.ctx);
+    int n_part = 1;
+    ProjSplit split{};
+    cudaError_t e = launch_prenorm(c, resid, eps, PlanArgs{});
+    if (e == cudaSuccess) e = qkv_project(c, at<bf16>(ws, c.L.xn), w_qkv, &n_part, &split);
+    if (e == cudaSuccess)
+        e = launch_paged_append(*dims, *paged, T, at<float>(ws, c.L.qkv), n_part,
+                                (long long)T * c.nr(), split, seq, pos, table, q, kp, vp, ks, vs,
+                                c.st);
+    if (e == cudaSuccess)
+        e = launch_paged_attend(*dims, *paged, T, q, seq, pos, table, kp, vp, ks, vs, ctx, attn_ws,
+                                c.st);
+    if (e == cudaSuccess) e = out_proj(c, ctx, w_o, resid, xn_next, eps);
+    return cuda_status(e);
+}
+
+// Decoder layers in place on resid; block(l, scratch, its bytes, xn) is layer l's
+// attention block, which leaves the MoE block's input in xn if that is not null.
+template <typename Block>
+moe_status decoder_layers(const moe_sa_dims *attn, const moe_dims *moe_d, int32_t n_layers,
+                          int32_t T, float *resid, const void *const *w_router,
+                          const void *const *w1, const void *const *v1, const void *const *w2,
+                          float eps, void *ws, size_t ws_bytes, moe_stream_t stream, Block block) {
+    // the attention block's residual add and the MoE block's pre-norm run as
+    // one kernel when a row fits its registers; otherwise as the stack does
+    const bool fused = attn->d_model <= kResNormCap;
+    const size_t xn_bytes = ((size_t)T * attn->d_model * 2 + 255) & ~size_t(255);
+    bf16 *xn = static_cast<bf16 *>(ws);
+    void *inner = static_cast<char *>(ws) + xn_bytes;
+    for (int l = 0; l < n_layers; ++l) {
+        moe_status s;
+        if (fused) {
+            s = block(l, inner, ws_bytes - xn_bytes, xn);
+            if (s != MOE_OK) return s;
+            // resid <- resid + MoE_l(xn): the combine reads each residual
+            // element before it writes the same element
+            s = moe_layer_forward(moe_d, T, xn, w_router[l], w1[l], v1[l], w2[l], resid, resid,
+                                  inner, ws_bytes - xn_bytes, stream);
+        } else {
+            s = block(l, ws, ws_bytes, nullptr);
+            if (s != MOE_OK) return s;
+            s = moe_stack_forward(moe_d, 1, T, &w_router[l], &w1[l], &v1[l], &w2[l], resid, eps,
+                                  ws, ws_bytes, stream);
+        }
+        if (s != MOE_OK) return s;
+    }
+    return MOE_OK;
 }
 
 }  // namespace
@@ -1081,32 +1160,78 @@ moe_status moe_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe_d, i
     size_t need = 0;
     if ((s = moe_decoder_workspace_size(attn, moe_d, T, &need)) != MOE_OK) return s;
     if (!ws || !aligned16(ws) || ws_bytes < need) return MOE_ERR_WORKSPACE;
-    // the attention block's residual add and the MoE block's pre-norm run as
-    // one kernel when a row fits its registers; otherwise as the stack does
-    const bool fused = attn->d_model <= kResNormCap;
-    const size_t xn_bytes = ((size_t)T * attn->d_model * 2 + 255) & ~size_t(255);
-    bf16 *xn = static_cast<bf16 *>(ws);
-    void *inner = static_cast<char *>(ws) + xn_bytes;
-    for (int l = 0; l < n_layers; ++l) {
-        if (fused) {
-            s = sa_forward_impl(attn, T, seq, pos, n_seq, max_len, resid, w_qkv[l], w_o[l],
-                                k_cache[l], v_cache[l], eps, inner, ws_bytes - xn_bytes, stream,
-                                xn);
-            if (s != MOE_OK) return s;
-            // resid <- resid + MoE_l(xn): the combine reads each residual
-            // element before it writes the same element
-            s = moe_layer_forward(moe_d, T, xn, w_router[l], w1[l], v1[l], w2[l], resid, resid,
-                                  inner, ws_bytes - xn_bytes, stream);
-        } else {
-            s = moe_sa_forward(attn, T, seq, pos, n_seq, max_len, resid, w_qkv[l], w_o[l],
-                               k_cache[l], v_cache[l], eps, ws, ws_bytes, stream);
-            if (s != MOE_OK) return s;
-            s = moe_stack_forward(moe_d, 1, T, &w_router[l], &w1[l], &v1[l], &w2[l], resid, eps,
-                                  ws, ws_bytes, stream);
-        }
-        if (s != MOE_OK) return s;
-    }
+    return decoder_layers(
+        attn, moe_d, n_layers, T, resid, w_router, w1, v1, w2, eps, ws, ws_bytes, stream,
+        [&](int l, void *aws, size_t bytes, bf16 *xn) {
+            return sa_forward_impl(attn, T, seq, pos, n_seq, max_len, resid, w_qkv[l], w_o[l],
+                                   k_cache[l], v_cache[l], eps, aws, bytes, stream, xn);
+        });
+}
+
+moe_status moe_paged_sa_workspace_size(const moe_sa_dims *dims, int32_t max_tokens, size_t *bytes) {
+    size_t a = 0, b = 0;
+    moe_status s = moe_sa_workspace_size(dims, max_tokens, &a);
+    if (s != MOE_OK) return s;
+    if ((s = moe_paged_workspace_size(dims, max_tokens, &b)) != MOE_OK) return s;
+    if (!bytes) return MOE_ERR_INVALID_ARG;
+    *bytes = a + b;
     return MOE_OK;
+}
+
+moe_status moe_paged_sa_forward(const moe_sa_dims *dims, const moe_paged_dims *paged, int32_t T,
+                                const int32_t *seq, const int32_t *pos, const int32_t *page_table,
+                                float *resid, const void *w_qkv, const void *w_o, void *k_pages,
+                                void *v_pages, float *k_scale, float *v_scale, float eps, void *ws,
+                                size_t ws_bytes, moe_stream_t stream) {
+    MOE_INJECT("moe_paged_sa_forward");
+    return paged_sa_impl(dims, paged, T, seq, pos, page_table, resid, w_qkv, w_o, k_pages, v_pages,
+                         k_scale, v_scale, eps, ws, ws_bytes, stream, nullptr);
+}
+
+moe_status moe_paged_decoder_workspace_size(const moe_sa_dims *attn, const moe_dims *moe_d,
+                                            int32_t max_tokens, size_t *bytes) {
+    size_t a = 0, d = 0, p = 0;
+    moe_status s = moe_decoder_workspace_size(attn, moe_d, max_tokens, &d);
+    if (s != MOE_OK) return s;
+    if ((s = moe_paged_sa_workspace_size(attn, max_tokens, &a)) != MOE_OK) return s;
+    if (!bytes) return MOE_ERR_INVALID_ARG;
+    // (the attention block's scratch beside the MoE block's input)
+    p = ((size_t)max_tokens * attn->d_model * 2 + 255) & ~size_t(255);
+    *bytes = std::max(d, p + a);
+    return MOE_OK;
+}
+
+moe_status moe_paged_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe_d,
+                                     const moe_paged_dims *paged, int32_t n_layers, int32_t T,
+                                     const int32_t *seq, const int32_t *pos,
+                                     const int32_t *page_table, float *resid,
+                                     const void *const *w_qkv, const void *const *w_o,
+                                     const void *const *w_router, const void *const *w1,
+                                     const void *const *v1, const void *const *w2,
+                                     void *const *k_pages, void *const *v_pages,
+                                     float *const *k_scale, float *const *v_scale, float eps,
+                                     void *ws, size_t ws_bytes, moe_stream_t stream) {
+    MOE_INJECT("moe_paged_decoder_forward");
+    moe_status s = check_paged(attn, paged);
+    if (s != MOE_OK) return s;
+    if (!moe_d || moe_d->d_model != attn->d_model || moe_d->w_dtype != MOE_BF16 ||
+        moe_d->x_dtype != MOE_BF16 || moe_d->out_dtype != MOE_F32 || n_layers < 0 || T < 0 ||
+        T > kMaxSaTokens || !(eps > 0.f))
+        return MOE_ERR_INVALID_ARG;
+    if (T == 0 || n_layers == 0) return MOE_OK;
+    if (!ok_ptr(seq) || !ok_ptr(pos) || !ok_ptr(page_table) || !ok_ptr(resid) || !w_qkv || !w_o ||
+        !w_router || !w1 || !v1 || !w2 || !k_pages || !v_pages || !k_scale || !v_scale)
+        return MOE_ERR_INVALID_ARG;
+    size_t need = 0;
+    if ((s = moe_paged_decoder_workspace_size(attn, moe_d, T, &need)) != MOE_OK) return s;
+    if (!ws || !aligned16(ws) || ws_bytes < need) return MOE_ERR_WORKSPACE;
+    return decoder_layers(
+        attn, moe_d, n_layers, T, resid, w_router, w1, v1, w2, eps, ws, ws_bytes, stream,
+        [&](int l, void *aws, size_t bytes, bf16 *xn) {
+            return paged_sa_impl(attn, paged, T, seq, pos, page_table, resid, w_qkv[l], w_o[l],
+                                 k_pages[l], v_pages[l], k_scale[l], v_scale[l], eps, aws, bytes,
+                                 stream, xn);
+        });
 }
 
 }  // extern "C"

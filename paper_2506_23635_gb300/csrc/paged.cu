@@ -640,6 +640,8 @@ cudaError_t attend(const PagedAttn &a, void *ws, cudaStream_t st) {
                                   st);
 }
 
+}  // namespace
+
 moe_status check_paged(const moe_sa_dims *d, const moe_paged_dims *pd) {
     size_t n = 0;
     moe_status s = moe_sa_workspace_size(d, 0, &n);  // the shape's own limits
@@ -668,7 +670,38 @@ moe_status check_paged_call(const moe_sa_dims *d, const moe_paged_dims *pd, int3
     return MOE_OK;
 }
 
-}  // namespace
+cudaError_t launch_paged_append(const moe_sa_dims &d, const moe_paged_dims &pd, int T,
+                                const float *qkv, int n_part, long long part_stride,
+                                const ProjSplit &split, const int32_t *seq, const int32_t *pos,
+                                const int32_t *table, void *q, void *kp, void *vp, float *ks,
+                                float *vs, cudaStream_t st) {
+    const QkvRows rows{qkv, (d.n_heads + 2 * d.n_kv_heads) * kPagedDh, T, n_part, part_stride, split};
+    return launch_append(rows, n_part == 1 ? kInF32 : kInParts, d, pd, seq, pos, table, q, kp, vp,
+                         ks, vs, st);
+}
+
+cudaError_t launch_paged_attend(const moe_sa_dims &d, const moe_paged_dims &pd, int T,
+                                const void *q, const int32_t *seq, const int32_t *pos,
+                                const int32_t *table, const void *kp, const void *vp,
+                                const float *ks, const float *vs, void *ctx, void *ws,
+                                cudaStream_t st) {
+    const PagedAttn a{T,
+                      d.n_heads,
+                      d.n_kv_heads,
+                      pd.page_size,
+                      PageView{table, pd.n_seq, pd.max_pages, pd.n_pages,
+                               31 - __builtin_clz(pd.page_size)},
+                      seq,
+                      pos,
+                      q,
+                      kp,
+                      vp,
+                      ks,
+                      vs,
+                      ctx};
+    return attend(a, ws, st);
+}
+
 }  // namespace moe
 
 using namespace moe;
@@ -715,21 +748,9 @@ moe_status moe_paged_attend(const moe_sa_dims *dims, const moe_paged_dims *paged
     size_t need = 0;
     if ((s = moe_paged_workspace_size(dims, T, &need)) != MOE_OK) return s;
     if (!ok_ptr(ws) || ws_bytes < need) return MOE_ERR_WORKSPACE;
-    const PagedAttn a{T,
-                      dims->n_heads,
-                      dims->n_kv_heads,
-                      paged->page_size,
-                      PageView{page_table, paged->n_seq, paged->max_pages, paged->n_pages,
-                               31 - __builtin_clz(paged->page_size)},
-                      seq,
-                      pos,
-                      q,
-                      k_pages,
-                      v_pages,
-                      k_scale,
-                      v_scale,
-                      ctx};
-    return cuda_status(attend(a, ws, (cudaStream_t)stream));
+    return cuda_status(launch_paged_attend(*dims, *paged, T, q, seq, pos, page_table, k_pages,
+                                           v_pages, k_scale, v_scale, ctx, ws,
+                                           (cudaStream_t)stream));
 }
 
 }  // extern "C"

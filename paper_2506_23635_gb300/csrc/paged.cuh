@@ -125,4 +125,24 @@ enum : int { kPagedAheadZero = 0, kPagedAheadPlan = 1, kPagedAheadPrefill = 2 };
 cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, int ahead,
                                    cudaStream_t st);
 
+
+// ---- host side (paged.cu), for the attention block over the paged cache --------
+
+// What the shape and the call's pointers have to be.
+moe_status check_paged(const moe_sa_dims *d, const moe_paged_dims *pd);
+moe_status check_paged_call(const moe_sa_dims *d, const moe_paged_dims *pd, int32_t T,
+                            const int32_t *seq, const int32_t *pos, const int32_t *table,
+                            const void *kp, const void *vp, const float *ks, const float *vs);
+// moe_paged_append of an fp32 projection in n_part parts (0: as `split` says).
+cudaError_t launch_paged_append(const moe_sa_dims &d, const moe_paged_dims &pd, int T,
+                                const float *qkv, int n_part, long long part_stride,
+                                const ProjSplit &split, const int32_t *seq, const int32_t *pos,
+                                const int32_t *table, void *q, void *kp, void *vp, float *ks,
+                                float *vs, cudaStream_t st);
+cudaError_t launch_paged_attend(const moe_sa_dims &d, const moe_paged_dims &pd, int T,
+                                const void *q, const int32_t *seq, const int32_t *pos,
+                                const int32_t *table, const void *kp, const void *vp,
+                                const float *ks, const float *vs, void *ctx, void *ws,
+                                cudaStream_t st);
+
 }  // namespace moe

@@ -36,6 +36,8 @@ EXPORTS = (
     "moe_sa_workspace_size", "moe_sa_qkv", "moe_sa_attend", "moe_sa_forward",
     "moe_decoder_workspace_size", "moe_decoder_forward",
     "moe_paged_workspace_size", "moe_paged_append", "moe_paged_attend",
+    "moe_paged_sa_workspace_size", "moe_paged_sa_forward",
+    "moe_paged_decoder_workspace_size", "moe_paged_decoder_forward",
 )
 
 
@@ -134,6 +136,11 @@ def lib() -> ctypes.CDLL:
         "moe_paged_workspace_size": [SP, I32, ctypes.POINTER(SZ)],
         "moe_paged_append": [SP, GP, I32, P, I32] + [P] * 9,
         "moe_paged_attend": [SP, GP, I32] + [P] * 10 + [SZ, P],
+        "moe_paged_sa_workspace_size": [SP, I32, ctypes.POINTER(SZ)],
+        "moe_paged_sa_forward": [SP, GP, I32] + [P] * 10 + [ctypes.c_float, P, SZ, P],
+        "moe_paged_decoder_workspace_size": [SP, DP, I32, ctypes.POINTER(SZ)],
+        "moe_paged_decoder_forward": [SP, DP, GP, I32, I32] + [P] * 4 + [ctypes.POINTER(P)] * 10
+                                     + [ctypes.c_float, P, SZ, P],
     }
     for name, args in sigs.items():
         fn = getattr(L, name)
@@ -627,3 +634,85 @@ def paged_attend(a: SaDims, cache: PagedCache, q, seq, pos, ctx=None, ws=None, s
                                   c.v_scale.data_ptr(), ctx.data_ptr(), ws.data_ptr(), ws.numel(),
                                   st), "moe_paged_attend")
     return ctx
+
+
+def paged_sa_workspace_size(a: SaDims, max_tokens: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().moe_paged_sa_workspace_size(ctypes.byref(a), max_tokens, ctypes.byref(n)),
+           "moe_paged_sa_workspace_size")
+    return int(n.value)
+
+
+def paged_sa_forward(a: SaDims, cache: PagedCache, resid, w_qkv, w_o, seq, pos,
+                     eps: float = STACK_EPS, ws=None, stream=None):
+    """resid <- resid + W_o . Attn(RMSNorm0(resid)) in place (fp32 [T, D]), over
+    a paged cache that takes the tokens' keys and values."""
+    T, dev = resid.shape[0], cache.device_index
+    D, nq, nkv = a.d_model, a.n_heads * a.head_dim, a.n_kv_heads * a.head_dim
+    _want(resid, (T, D), torch.float32, dev, "resid")
+    _want(w_qkv, (nq + 2 * nkv, D), torch.bfloat16, dev, "w_qkv")
+    _want(w_o, (D, nq), torch.bfloat16, dev, "w_o")
+    if ws is not None:
+        _want(ws, ws.shape, torch.uint8, dev, "ws")
+    st = cache._call(a, T, seq, pos, stream)
+    if ws is None:
+        ws = _new((paged_sa_workspace_size(a, T),), torch.uint8, resid.device, stream)
+    c = cache
+    _check(lib().moe_paged_sa_forward(a, c.dims, T, seq.data_ptr(), pos.data_ptr(),
+                                      c._page_table.data_ptr(), resid.data_ptr(),
+                                      w_qkv.data_ptr(), w_o.data_ptr(), c.k_pages.data_ptr(),
+                                      c.v_pages.data_ptr(), c.k_scale.data_ptr(),
+                                      c.v_scale.data_ptr(), eps, ws.data_ptr(), ws.numel(), st),
+           "moe_paged_sa_forward")
+    return resid
+
+
+def paged_decoder_workspace_size(a: SaDims, d: Dims, max_tokens: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().moe_paged_decoder_workspace_size(ctypes.byref(a), ctypes.byref(d), max_tokens,
+                                                  ctypes.byref(n)),
+           "moe_paged_decoder_workspace_size")
+    return int(n.value)
+
+
+class PagedDecoderWeights:
+    """Device pointers of every decoder layer's tensors as C arrays: per layer
+    (w_qkv, w_o, w_r, w1, v1, w2, cache), the caches PagedCaches of one shape.
+    The page table of a call is the first layer's.  The tensors must outlive
+    this object's use."""
+
+    def __init__(self, layers):
+        n = len(layers)
+        self.n = n
+        self.layers = layers
+        self.cache = layers[0][6]
+        shape = self.cache.k_pages.shape
+        if any(l[6].k_pages.shape != shape or l[6].device_index != self.cache.device_index
+               for l in layers):
+            raise ValueError("the layers' caches have one shape and one device")
+        arr = lambda ts: (ctypes.c_void_p * n)(*[ctypes.c_void_p(t.data_ptr()) for t in ts])
+        (self.w_qkv, self.w_o, self.w_r, self.w1, self.v1,
+         self.w2) = (arr([l[i] for l in layers]) for i in range(6))
+        (self.k_pages, self.v_pages, self.k_scale, self.v_scale) = (
+            arr([getattr(l[6], name) for l in layers])
+            for name in ("k_pages", "v_pages", "k_scale", "v_scale"))
+
+
+def paged_decoder_forward(a: SaDims, d: Dims, weights: PagedDecoderWeights, resid, seq, pos,
+                          eps: float = STACK_EPS, ws=None, stream=None):
+    """Every decoder layer in order, in place on resid (fp32 [T, D]), over paged
+    caches: resid += W_o . Attn(RMSNorm0(resid)); resid += MoE(RMSNorm0(resid))."""
+    W, c = weights, weights.cache
+    T, dev = resid.shape[0], c.device_index
+    _want(resid, (T, a.d_model), torch.float32, dev, "resid")
+    if ws is not None:
+        _want(ws, ws.shape, torch.uint8, dev, "ws")
+    st = c._call(a, T, seq, pos, stream)
+    if ws is None:
+        ws = _new((paged_decoder_workspace_size(a, d, T),), torch.uint8, resid.device, stream)
+    _check(lib().moe_paged_decoder_forward(a, d, c.dims, W.n, T, seq.data_ptr(), pos.data_ptr(),
+                                           c._page_table.data_ptr(), resid.data_ptr(), W.w_qkv,
+                                           W.w_o, W.w_r, W.w1, W.v1, W.w2, W.k_pages, W.v_pages,
+                                           W.k_scale, W.v_scale, eps, ws.data_ptr(), ws.numel(),
+                                           st), "moe_paged_decoder_forward")
+    return resid

@@ -107,6 +107,35 @@ def test_refusals(lib):
     assert app(dt=2) == 1 and app(dt=-1) == 1
     assert att(ctx=None) == 1 and att(ctx=MIS) == 1
     assert att(ws=None) == 3 and att(ws=MIS) == 3 and att(nb=need - 1) == 3
+    block = ctypes.c_size_t(0)
+    assert L.moe_paged_sa_workspace_size(ctypes.byref(a), 8, ctypes.byref(block)) == 0
+    assert block.value > need
+    assert L.moe_paged_sa_workspace_size(ctypes.byref(a), 65537, ctypes.byref(block)) == 1
+
+    def blk(T=8, d=a, p=P(64, 100, 4, 10), resid=A, w=A, eps=1e-6, ws=A, nb=1 << 40, seq=A, k=A):
+        return L.moe_paged_sa_forward(ctypes.byref(d), ctypes.byref(p), T, seq, A, A, resid, w, A, k,
+                                      A, A, A, eps, ws, nb, None)
+
+    assert blk(T=0) == 0 and blk(T=0, p=P(24, 100, 4, 10)) == 2
+    for kw in (dict(resid=None), dict(resid=MIS), dict(w=None), dict(seq=None), dict(k=MIS),
+               dict(eps=0.0), dict(T=-1), dict(p=P(64, 0, 4, 10))):
+        assert blk(**kw) == 1, kw
+    assert blk(ws=None) == 3 and blk(ws=MIS) == 3 and blk(nb=1024) == 3
+    m = lib.dims(6144, 10752, 16, 4, out_dtype=torch.float32)
+    assert L.moe_paged_decoder_workspace_size(ctypes.byref(a), ctypes.byref(m), 8,
+                                              ctypes.byref(block)) == 0
+    arr = (ctypes.c_void_p * 1)(A)
+
+    def dec(T=8, d=a, mo=m, p=P(64, 100, 4, 10), resid=A, seq=A, ks=arr, n=1, ws=A, nb=1 << 40):
+        return L.moe_paged_decoder_forward(ctypes.byref(d), ctypes.byref(mo), ctypes.byref(p), n, T,
+                                           seq, A, A, resid, arr, arr, arr, arr, arr, arr, arr, arr,
+                                           ks, arr, 1e-6, ws, nb, None)
+
+    assert dec(T=0) == 0 and dec(n=0) == 0
+    for kw in (dict(mo=lib.dims(6144, 10752, 16, 4)), dict(d=lib.sa_dims(4096, 32, 8)), dict(n=-1),
+               dict(T=-1), dict(resid=None), dict(seq=MIS), dict(ks=None), dict(p=P(64, 100, 0, 1))):
+        assert dec(**kw) == 1, kw
+    assert dec(ws=None) == 3 and dec(nb=4096) == 3
     assert L.moe_paged_append(None, None, 0, *[None, 1] + [None] * 9) == 1
     assert L.moe_paged_append(ctypes.byref(a), None, 0, *[None, 1] + [None] * 9) == 1
 
