@@ -218,7 +218,7 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
     __shared__ int2 at_s[kAppMaxGroup];      // a start's sequence, page index
     __shared__ int grown_s[kAppMaxGroup];    // starts whose page's scale grew
     __shared__ float ratio_s[kAppMaxGroup];  // and by what
-    constexpr int kFew = 4;  // starts whose pages' tokens are found in one look
+    constexpr int kFew = 2;  // starts whose pages' tokens are found in one look
     __shared__ int tok_at[kFew][PS];
     __shared__ float red[kAppHalves];
     const int hr = (int)blockIdx.x % (2 * Hkv), g0 = (int)blockIdx.x / (2 * Hkv) * gs;
