@@ -63,9 +63,6 @@ constexpr int kPdThreads = 7 * 32;
 constexpr int kPdStages = 3;
 constexpr int kPdRing = 8;  // tile descriptions
 constexpr int kPdSmall = kPagedSmall;
-// a share's tiles at least: a second tile's copies are in flight with the
-// first's, a part to merge costs 1-2 us
-constexpr int kPdMinTiles = 2;
 // parts that one CTA merges: more are merged in groups first
 constexpr int kPdGroup = 18;
 static_assert(kPagedMaxCtas <= kPdGroup * kPdGroup && kPdGroup <= 32, "two levels of merging");
@@ -269,7 +266,7 @@ __device__ __forceinline__ PdWalk pd_begin(const PdTokens &l, int Hkv, int cta, 
     w.Hkv = Hkv;
     w.n_list = l.count();
     w.W = w.n_list > 0 ? l.before(w.n_list) * Hkv : 0;
-    w.n_share = (int)min((long long)G, (w.W + kPdMinTiles - 1) / kPdMinTiles);
+    w.n_share = (int)min((long long)G, w.W);
     w.lo = w.hi = 0;
     if (cta >= w.n_share) return w;
     w.lo = pd_start(w.W, cta, w.n_share);
@@ -860,10 +857,13 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 // the last of n to count on counter `at`, with all they stored
                 auto last_of = [&](int at, int n) {
                     ptx::named_bar_sync(1, 128);
-                    if (r == 0) {
-                        __threadfence();
-                        hd->last = atomicAdd(&a.list.count[at], 1) == n - 1;
-                        __threadfence();
+                    if (r == 0) {  // (releases what the barrier has ordered before it)
+                        int old;
+                        asm volatile("atom.add.acq_rel.gpu.s32 %0, [%1], 1;"
+                                     : "=r"(old)
+                                     : "l"(a.list.count + at)
+                                     : "memory");
+                        hd->last = old == n - 1;
                     }
                     ptx::named_bar_sync(1, 128);
                     return hd->last != 0;
@@ -920,10 +920,9 @@ cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float
     PdArgs pa{ahead == kPagedAheadZero ? a.T : 0, ahead, a.Hq, a.Hkv, a.pv, l, a.seq, a.pos, static_cast<const bf16 *>(a.q), a.ks, a.vs,
               static_cast<bf16 *>(a.ctx), part, device_info().err};
     void *args[] = {&mk, &mv, &pa};
-    // as many CTAs as the largest positions give shares
-    const long long tiles = (long long)a.T * a.Hkv *
-                            (((long long)a.pv.max_pages * a.page_size + kPagedTile - 1) / kPagedTile);
-    const long long most = (tiles + kPdMinTiles - 1) / kPdMinTiles;
+    // as many CTAs as the largest positions give tiles
+    const long long most = (long long)a.T * a.Hkv *
+                           (((long long)a.pv.max_pages * a.page_size + kPagedTile - 1) / kPagedTile);
     const int ctas = std::min(2 * device_info().sm_count, kPagedMaxCtas);
     LaunchScope ls("paged_decode_tc", st);
     return launch_pdl(kern, dim3((unsigned)std::min<long long>(most, ctas)), dim3(kPdThreads), kPdSmem,
