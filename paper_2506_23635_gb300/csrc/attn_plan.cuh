@@ -19,14 +19,14 @@ struct PlanArgs {
 // The plan of an attention call, by one block of NT threads.  A run is the
 // longest stretch of tokens that are consecutive positions of one sequence;
 // its tiles are cut from its first token on.  Tiles of at least
-// kAttnTileMinRows tokens are listed by falling length (a counting sort over
+// MIN_ROWS tokens are listed by falling length (a counting sort over
 // their key/value tiles; tiles of the same length in any order: no result
 // depends on it), the tokens of the others in ascending order.  Run starts are
 // kept as one bit a token.  It runs beside the pre-norm's other blocks and is
 // done before the projection after them ends.
 constexpr int kPlanBins = 256;
 
-template <int NT>
+template <int NT, int MIN_ROWS = kAttnTileMinRows>
 __device__ void plan_attention(int T, const PlanArgs &a) {
     static_assert(NT >= kPlanBins && NT % 32 == 0, "a thread for each bin");
     __shared__ uint32_t brk[kMaxSaTokens / 32];  // bit t: a run starts at token t
@@ -87,7 +87,7 @@ __device__ void plan_attention(int T, const PlanArgs &a) {
         if (t < T) {
             int ts, rows;
             tile_of(t, ts, rows);
-            left = rows < kAttnTileMinRows;
+            left = rows < MIN_ROWS;
             if (!left && t == ts) atomicAdd(&bins[bin_of(ts, rows)], 1);
         }
         const uint32_t m = __ballot_sync(0xffffffffu, left);
@@ -120,7 +120,7 @@ __device__ void plan_attention(int T, const PlanArgs &a) {
     for (int t = tid; t < T; t += NT) {
         int ts, rows;
         tile_of(t, ts, rows);
-        if (t == ts && rows >= kAttnTileMinRows)
+        if (t == ts && rows >= MIN_ROWS)
             a.plan.tiles[atomicAdd(&bins[bin_of(ts, rows)], 1)] =
                 make_int4(ts, rows, a.pos[ts], a.seq[ts]);
     }

@@ -529,7 +529,7 @@ k_paged_plan(int T, const PageView pv, const int32_t *__restrict__ seq,
         for (int i = tid; i < 2 * kPagedUnitParts; i += kPlanThreads) unit_count[i] = 0;
     int n = T;
     if (pa.plan.head) {  // only those that no tile holds
-        plan_attention<kPlanThreads>(T, pa);
+        plan_attention<kPlanThreads, kPagedTileMinRows>(T, pa);
         __syncthreads();
         n = pa.plan.head->n_left;
     }
@@ -591,11 +591,11 @@ PagedWs paged_ws(int64_t T) {
     L.list = o; o += up((size_t)T * 4);
     L.before = o; o += up(((size_t)T + 1) * 8);
     L.head = o; o += up(sizeof(AttnPlanHead));
-    L.tiles = o; o += up((size_t)(T / kAttnTileMinRows) * sizeof(int4));
+    L.tiles = o; o += up((size_t)(T / kPagedTileMinRows) * sizeof(int4));
     L.unit_count = o; o += up(2 * kPagedUnitParts * 4);
     L.part = o; o += up(kPagedPartFloats * 4);
     // (calls of fewer tokens hold no tile)
-    L.unit_part = o; o += T >= kAttnTileMinRows ? up(kPagedUnitPartFloats * 4) : 0;
+    L.unit_part = o; o += T >= kPagedTileMinRows ? up(kPagedUnitPartFloats * 4) : 0;
     L.total = o;
     return L;
 }

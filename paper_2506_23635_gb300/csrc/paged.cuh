@@ -110,6 +110,11 @@ inline bool paged_map(CUtensorMap *m, const void *base, const PagedAttn &a, bool
 }
 
 // Attention of the listed tokens over the 8-bit cache (paged_decode_tc.cu).
+// Fewer consecutive tokens than this are attended one by one: a tile costs its
+// heads 2.4 us of an SM for each 128 positions whatever its rows, a token its
+// key/value heads 0.55 (DBRX's heads break even at 24).
+constexpr int kPagedTileMinRows = 24;
+
 // Attention of the plan's tiles (paged_prefill_tc.cu).  part, count: where a unit
 // of work is shared by several CTAs; 2 counters a part, zero at the start.
 constexpr int kPagedUnitParts = 160;  // one for each SM

@@ -1,7 +1,7 @@
 // Causal attention of prefill tiles over the paged 8-bit cache on the tcgen05
 // tensor cores.
 //
-// Tiles and units are those of attn_tc.cu: a tile is 16 to 128 consecutive
+// Tiles and units are those of attn_tc.cu: a tile is 24 to 128 consecutive
 // positions p0 .. p0 + rows - 1 of one sequence, a unit a (tile, pair of query
 // heads of one key/value head) over cache positions 0 .. p0 + rows - 1, taken by
 // one CTA an SM from a counter, longest first; the two heads share every key and
@@ -607,21 +607,35 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
 
     ptx::grid_dependency_wait();
     ptx::launch_dependents();
-    const int n_tiles = __ldcg(&a.plan.head->n_tiles), n_left = __ldcg(&a.plan.head->n_left);
-    // few tiles: a unit holds one head, so that the longest is shorter
-    const bool single = n_left == 0 && 3 * n_tiles * a.Hq <= 4 * (int)gridDim.x;
-    const int per = single ? G : pairs;
-    // and where there are at least two CTAs to each unit, it is cut along the
-    // positions into as many parts, of kPfMinTiles tiles or more (a part costs ~7 us
-    // to start and leave, its merge 2-3: 512 tokens at position 5000, 96 units of 40
-    // to 44 tiles on 152 SMs, take 127 us whole, 125 in three parts each)
-    const int n_whole = n_tiles * a.Hkv * per;
-    int S = 1;
-    if (n_whole > 0 && 2 * n_whole <= (int)gridDim.x) {
-        const int4 longest = __ldcg(&a.plan.tiles[0]);
-        S = min(min(kPfMaxParts, (int)gridDim.x / n_whole),
-                max(1, ((longest.z + longest.y - 1) / kPfRows + 1) / kPfMinTiles));
+    const int n_tiles = __ldcg(&a.plan.head->n_tiles);
+    // Two heads a unit or one, and a unit whole or, where there are at least two CTAs
+    // to each, cut along the positions into up to kPfMaxParts parts of kPfMinTiles
+    // tiles or more: whichever ends first for units as long as the longest, counting
+    // 2.75 us for a position tile of two heads, 2.4 of one, 5 us to start and leave a
+    // unit, and 8 and 1 for each part where they are merged (measured: 512 tokens at
+    // position 5000, 44 tiles, 4 x 48 heads on 152 SMs, 140 us in pairs, 214 alone).
+    const int4 longest = n_tiles > 0 ? __ldcg(&a.plan.tiles[0]) : make_int4(0, 1, 0, 0);
+    const int n_long = (longest.z + longest.y - 1) / kPfRows + 1;
+    bool single = false;
+    int S = 1, best = 0x7fffffff;
+    for (int one = 0; one < 2; ++one) {
+        const int units = max(1, n_tiles * a.Hkv * (one ? G : pairs)), cost = one ? 48 : 55;
+        const int most = min(min(kPfMaxParts, (int)gridDim.x / units), n_long / kPfMinTiles);
+        for (int whole = 1; whole >= 0; --whole) {
+            const int parts = whole ? 1 : most;
+            if (parts < 1 || (!whole && parts == 1)) continue;
+            const int rounds = (units * parts + (int)gridDim.x - 1) / (int)gridDim.x;
+            const long long us20 = (long long)rounds * ((n_long + parts - 1) / parts * cost + 100) +
+                                   (whole ? 0 : 160 + 20 * parts);
+            if (us20 < best) {
+                best = (int)us20;
+                single = one;
+                S = parts;
+            }
+        }
     }
+    const int per = single ? G : pairs;
+    const int n_whole = n_tiles * a.Hkv * per;
     const int n_units = n_whole * S;
     int unit = (int)blockIdx.x;
     if (unit >= n_units) return;
@@ -755,7 +769,7 @@ cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, fl
         return cudaErrorInvalidValue;
     void *args[] = {&pa};
     const int ctas = std::min(device_info().sm_count, kPagedUnitParts);
-    const long long most = (long long)kPfMaxParts * a.Hq * (a.T / kAttnTileMinRows);
+    const long long most = (long long)kPfMaxParts * a.Hq * (a.T / kPagedTileMinRows);
     LaunchScope ls("paged_prefill_tc", st);
     return launch_pdl(
         kern, dim3((unsigned)std::max(1LL, std::min<long long>(most, ctas))),

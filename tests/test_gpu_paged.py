@@ -268,6 +268,7 @@ ATTEND = {
     "late_chunk": [(0, 1900, 129)],
     "far_chunks": [(0, 7000, 40), (1, 100, 20), (2, 3000, 130)],  # units cut into parts
     "short_runs": [(i, 50 + i, 15) for i in range(10)],
+    "chunks_of_24": [(i, 100 * i, 23 + i % 3) for i in range(12)],
     "chunks_of_16": [(i, 100 * i, 16) for i in range(12)],
 }
 
