@@ -889,7 +889,10 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     __syncthreads();
     tc_fence_after();
     if (warp == 1) tmem_dealloc(tmem, kPdTmemCols);
-    if (a.ahead != kPagedAheadPlan) ptx::grid_dependency_wait();  // (complete after what is ahead)
+    // this grid is complete only after what is ahead: one CTA sees to it (the others
+    // would keep their SMs from those that wait for one: 512 tokens at position
+    // 5000 beside 24 of up to 2048 positions PD_ONE instead of 144 us)
+    if (a.ahead != kPagedAheadPlan && cta == n_cta - 1) ptx::grid_dependency_wait();
 }
 
 const void *pd_kernel(int G) {
