@@ -98,6 +98,7 @@ struct PfHeader {
     int next;
     int gave_up;
     int last[2];  // a head's part was counted last
+    uint32_t nan_rows[kPfRows / 32];  // bit p: NaN among the values of position p0 + p
     alignas(16) PfScales sc[kPfRing];
 };
 constexpr int kPfBars = (int)((offsetof(PfHeader, done) - offsetof(PfHeader, q_full)) / 8) + 1;
@@ -177,6 +178,7 @@ struct PfArgs {
     PageView pv;
     AttnPlan plan;
     const bf16 *q;
+    const uint8_t *vp;
     const float *ks, *vs;
     bf16 *ctx;
     float *part;  // kPagedUnitParts parts
@@ -262,17 +264,71 @@ __device__ __forceinline__ bool pf_fetch(const PfArgs &a, PfHeader *hd, unsigned
     return good;
 }
 
-// A tile's rows decoded into one operand's two stages, four rows a time of warp
-// w of three, every third four of them.  False: a wait gave up.
+// A value row that only the tile's rows from p on may see: 0 x NaN is NaN, so its
+// NaN become zeros for the product, and pf_show_nan puts them where they belong.
+__device__ __forceinline__ void pf_hide_nan(PfHeader *hd, int p, uint4 &x) {
+    const uint32_t n[4] = {__vcmpeq4(x.x & 0x7f7f7f7fu, 0x7f7f7f7fu), __vcmpeq4(x.y & 0x7f7f7f7fu, 0x7f7f7f7fu),
+                           __vcmpeq4(x.z & 0x7f7f7f7fu, 0x7f7f7f7fu), __vcmpeq4(x.w & 0x7f7f7f7fu, 0x7f7f7f7fu)};
+    if ((n[0] | n[1] | n[2] | n[3]) == 0) return;
+    x = make_uint4(x.x & ~n[0], x.y & ~n[1], x.z & ~n[2], x.w & ~n[3]);
+    atomicOr(&hd->nan_rows[p >> 5], 1u << (p & 31));
+}
+
+// Columns c .. c + 31 of row r's O: NaN where a hidden one lies at a position that
+// the row sees.
+__device__ __noinline__ void pf_show_nan(const PfArgs &a, const PfHeader *hd, const PfUnit &u, int r,
+                                         int c, float (&v)[32]) {
+    for (int w = 0; w <= r >> 5; ++w)
+        for (uint32_t m = hd->nan_rows[w]; m; m &= m - 1) {
+            const int p = w * 32 + __ffs(m) - 1;
+            if (p > r) return;
+            const int pos = u.p0 + p, pg = a.pv.page(u.sq, pos >> a.pv.shift);
+            const uint8_t *row =
+                a.vp + ((((size_t)pg * a.Hkv + u.g) << a.pv.shift) + (pos & ((1 << a.pv.shift) - 1))) * kPagedDh + c;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if ((row[i] & 0x7f) == 0x7f) v[i] = __uint_as_float(0x7fffffffu);
+        }
+}
+__device__ __forceinline__ bool pf_any_nan(const PfHeader *hd) {
+    return (hd->nan_rows[0] | hd->nan_rows[1] | hd->nan_rows[2] | hd->nan_rows[3]) != 0;
+}
+
+// 16 e4m3 numbers -> fp16, as chunks 2c, 2c + 1 of a row of 64 dims.
+__device__ __forceinline__ void pf_decode16(const uint4 &x, unsigned char *d0, unsigned char *d1) {
+    const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+    uint32_t y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        y[2 * i] = e4m3x2_to_f16x2(v[i] & 0xffffu);
+        y[2 * i + 1] = e4m3x2_to_f16x2(v[i] >> 16);
+    }
+    *reinterpret_cast<uint4 *>(d0) = make_uint4(y[0], y[1], y[2], y[3]);
+    *reinterpret_cast<uint4 *>(d1) = make_uint4(y[4], y[5], y[6], y[7]);
+}
+
+// A tile's rows decoded into one operand's two stages, four rows (a quarter warp
+// each) a time of warp w of three, every third four of them.  These warps' issue
+// slots are what the kernel has least of, so a tile whose rows every query sees
+// takes nothing but a load, the conversions and two stores at offsets that a lane
+// forms once (checks in the same loop: 512 tokens at position 5000 163 us, PF_DEC us
+// so).  False: a wait gave up.
 template <bool KEYS>
 __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigned char *smem,
                                           const PfUnit &u, int w) {
-    constexpr int B = 6;  // fours of rows a batch; two batches
+    constexpr int B = 6;                                   // fours of rows a batch
+    constexpr int N = (kPfRows / 4 + kPfDecWarps - 1) / kPfDecWarps;  // two batches of N at most
     const int lane = threadIdx.x & 31;
     const int last = u.p0 + u.rows - 1;
     uint64_t *full = KEYS ? hd->k_full : hd->v_full, *empty = KEYS ? hd->k_empty : hd->v_empty;
     uint64_t *raw_full = &hd->raw_full[KEYS ? 0 : 1], *raw_empty = &hd->raw_empty[KEYS ? 0 : 1];
-    const unsigned char *raw = smem + (KEYS ? kPfOffRawK : kPfOffRawV) + lane * 16;
+    const unsigned char *raw = smem + (KEYS ? kPfOffRawK : kPfOffRawV) + w * 512 + lane * 16;
+    // row 4 f + lane / 8, dims 16 (lane % 8) ..: its chunks in the 64-dim half's row,
+    // in fours f of even and of odd distance from w
+    const uint32_t row0 = w * 4 + (lane >> 3), c = (lane & 3) * 2;
+    unsigned char *dst = smem + (KEYS ? kPfOffK : kPfOffV) + ((lane & 7) >> 2) * kPfHalf + row0 * 128;
+    const uint32_t e0 = (c ^ (row0 & 7)) << 4, e1 = ((c + 1) ^ (row0 & 7)) << 4;
+    const uint32_t o0 = e0 ^ 64u, o1 = e1 ^ 64u;  // (4 rows on: bit 2 of the row)
 #pragma unroll 1
     for (int j = 0; j < u.n_kv; ++j) {
         const int b = j & 1;
@@ -282,41 +338,42 @@ __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigne
             return false;
         // rows that hold no position are zeros, as are values under a scale of zero
         const unsigned ok = KEYS ? hd->sc[j % kPfRing].ok : hd->sc[j % kPfRing].values;
-        // dims 16 c .. of a row: chunks 2c, 2c + 1 of its 64-dim half's row
-        unsigned char *box = smem + (KEYS ? kPfOffK : kPfOffV) + b * kPfTile +
-                             ((lane & 7) >> 2) * kPfHalf;
+        const int at = (u.j0 + j) * kPfRows;
+        unsigned char *d = dst + b * kPfTile;
+        if (ok == 0xffu && at + kPfRows - 1 <= (KEYS ? last : u.p0)) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            uint4 x[B];
+            for (int half = 0; half < 2; ++half) {
+                uint4 x[B];
 #pragma unroll
-            for (int k = 0; k < B; ++k) {
-                const int r4 = w + (half * B + k) * kPfDecWarps;
-                if (r4 < kPfRows / 4) x[k] = *reinterpret_cast<const uint4 *>(raw + r4 * 512);
-            }
-            if (half == 1) {
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(raw_empty);
-            }
-#pragma unroll
-            for (int k = 0; k < B; ++k) {
-                const int r4 = w + (half * B + k) * kPfDecWarps, row = r4 * 4 + (lane >> 3);
-                if (r4 >= kPfRows / 4) break;
-                const bool live = (u.j0 + j) * kPfRows + row <= last && ((ok >> (row >> 4)) & 1u);
-                if (!live) x[k] = make_uint4(0u, 0u, 0u, 0u);
-                const uint32_t v[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
-                uint32_t y[8];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    y[2 * i] = e4m3x2_to_f16x2(v[i] & 0xffffu);
-                    y[2 * i + 1] = e4m3x2_to_f16x2(v[i] >> 16);
+                for (int k = 0; k < B; ++k) {
+                    const int n = half * B + k;
+                    if (n < N - 1 || (n < N && w + n * kPfDecWarps < kPfRows / 4))
+                        x[k] = *reinterpret_cast<const uint4 *>(raw + n * kPfDecWarps * 512);
                 }
-                unsigned char *rowp = box + row * 128;
-                const uint32_t c = (lane & 3) * 2;
-                *reinterpret_cast<uint4 *>(rowp + ((c ^ (row & 7)) << 4)) =
-                    make_uint4(y[0], y[1], y[2], y[3]);
-                *reinterpret_cast<uint4 *>(rowp + (((c + 1) ^ (row & 7)) << 4)) =
-                    make_uint4(y[4], y[5], y[6], y[7]);
+                if (half == 1) {
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(raw_empty);
+                }
+#pragma unroll
+                for (int k = 0; k < B; ++k) {
+                    const int n = half * B + k;
+                    if (n < N - 1 || (n < N && w + n * kPfDecWarps < kPfRows / 4))
+                        pf_decode16(x[k], d + n * kPfDecWarps * 512 + (n & 1 ? o0 : e0),
+                                    d + n * kPfDecWarps * 512 + (n & 1 ? o1 : e1));
+                }
             }
+        } else {
+#pragma unroll 1
+            for (int n = 0; w + n * kPfDecWarps < kPfRows / 4; ++n) {
+                const int row = (w + n * kPfDecWarps) * 4 + (lane >> 3);
+                uint4 x = *reinterpret_cast<const uint4 *>(raw + n * kPfDecWarps * 512);
+                if (at + row > last || !((ok >> (row >> 4)) & 1u)) x = make_uint4(0u, 0u, 0u, 0u);
+                if (!KEYS && at + row > u.p0) pf_hide_nan(hd, at + row - u.p0, x);
+                pf_decode16(x, d + n * kPfDecWarps * 512 + (n & 1 ? o0 : e0),
+                            d + n * kPfDecWarps * 512 + (n & 1 ? o1 : e1));
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(raw_empty);
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -324,6 +381,7 @@ __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigne
     }
     return true;
 }
+static_assert(kPfDecWarps % 2 == 1, "the fours of a warp alternate in their rows' bit 2");
 
 // The MMA issuer's part of a unit.  False: a wait gave up.
 __device__ __forceinline__ bool pf_issue(PfHeader *hd, uint32_t sbase, uint32_t tmem,
@@ -533,6 +591,7 @@ __device__ __noinline__ void pf_part(const PfArgs &a, PfHeader *hd, const PfUnit
         float v[32];
         tmem_ld32(o_col + c, v);
         tmem_ld_wait();
+        if (pf_any_nan(hd)) pf_show_nan(a, hd, u, r, c, v);
 #pragma unroll
         for (int i = 0; i < 32; ++i) mine[(c + i) * kPfRows + r] = v[i];
     }
@@ -657,6 +716,7 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
                                   : 1;
                 ptx::mbar_init(bars + i, n);
             }
+            for (int i = 0; i < kPfRows / 32; ++i) hd->nan_rows[i] = 0u;
             ptx::fence_barrier_init();
         }
         tc_fence_before();
@@ -734,6 +794,7 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
                         float vv[32];
                         tmem_ld32(o_col + c, vv);
                         tmem_ld_wait();
+                        if (pf_any_nan(hd)) pf_show_nan(a, hd, u, r, c, vv);
                         if (r >= u.rows) continue;
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {
@@ -763,8 +824,8 @@ cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, fl
     static SmemOnce once;
     cudaError_t e = once.set(kern, kPfSmem);
     if (e != cudaSuccess) return e;
-    PfArgs pa{{}, {}, a.Hq, a.Hkv, a.pv, plan, static_cast<const bf16 *>(a.q), a.ks, a.vs,
-              static_cast<bf16 *>(a.ctx), part, count, device_info().err};
+    PfArgs pa{{}, {}, a.Hq, a.Hkv, a.pv, plan, static_cast<const bf16 *>(a.q),
+              static_cast<const uint8_t *>(a.vp), a.ks, a.vs, static_cast<bf16 *>(a.ctx), part, count, device_info().err};
     if (!paged_map(&pa.tmK, a.kp, a, false) || !paged_map(&pa.tmV, a.vp, a, false))
         return cudaErrorInvalidValue;
     void *args[] = {&pa};

@@ -377,6 +377,57 @@ def test_attend_nan_stays_with_its_sequence():
     assert np.array_equal(np.isnan(got), nan)
 
 
+@pytest.mark.parametrize("first,n", [(0, 100), (300, 200), (2000, 60), (5, 20)])
+def test_attend_nan_inside_a_chunk(first, n):
+    """NaN in the values and in the keys of tokens inside a chunk: the tokens
+    before them do not see them, those after do (in the values' dims, in all for
+    a key); NaN ahead of the chunk reaches every token."""
+    m = moe()
+    for ahead in (False, True):
+        c = ref.call(6, 2, 32, [(0, first, n), (1, 40, 1)], seed=45)
+        at = lambda p: (ref.page_of(c, 0, p), p % 32)
+        pv, pk = first + n // 3, first + n // 2
+        pg, off = at(pv)
+        c["v"][pg, 1, off, [7, 40, 127]] = [0x7f, 0xff, 0x7f]
+        pg, off = at(pk)
+        c["k"][pg, 0, off, 3] = 0xff
+        if ahead and first:
+            pg, off = at(first - 1)
+            c["v"][pg, 0, off, 99] = 0x7f
+        d = Dev(m, c)
+        q = queries(c)
+        got = m.paged_attend(d.a, d.cache, q, d.seq, d.pos).double().cpu().numpy().reshape(-1, 6, 128)
+        assert m.get_last_error() == 0
+        nan = np.zeros((n + 1, 6, 128), bool)
+        nan[n // 3:n, 3:, [7, 40, 127]] = True
+        nan[n // 2:n, :3] = True
+        if ahead and first:
+            nan[:n, :3, 99] = True
+        np.testing.assert_array_equal(np.isnan(got), nan)
+        # and the rest is as if they were not there
+        for x in ("k", "v"):
+            c[x][(c[x] & 0x7f) == 0x7f] = 0
+        clean = Dev(m, c)
+        want = m.paged_attend(d.a, clean.cache, q, d.seq, d.pos).double().cpu().numpy().reshape(got.shape)
+        seen = ~nan
+        seen[n // 3:n, 3:] = False  # (whose weights the zeros have changed)
+        seen[:n, :3] &= not (ahead and first)
+        np.testing.assert_array_equal(got[seen], want[seen])
+
+
+def test_padding_beside_prompts_and_many_tokens():
+    """Padding tokens in calls that are planned, and one of nothing else."""
+    c = ref.call(6, 2, 32, [(0, 0, 150), (1, 77, 1)], seed=46, pad=200, order="given")
+    run_attend(c)
+    c = ref.call(4, 4, 16, [(i, 3 * i, 1) for i in range(140)], seed=47, pad=60, order="shuffled")
+    run_append(c)
+    run_attend(c)
+    c = ref.call(6, 2, 32, [(0, 0, 1)], seed=48, pad=300)
+    c["seq"][:] = -1
+    run_append(c)
+    run_attend(c)
+
+
 def test_shared_pages_are_read():
     """Two sequences with the same first pages (a shared prompt)."""
     c = ref.call(6, 2, 16, [(0, 70, 1), (1, 90, 1)], seed=39)
