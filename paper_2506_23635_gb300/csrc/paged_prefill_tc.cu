@@ -34,8 +34,7 @@
 #include <stddef.h>
 
 #include <algorithm>
-
-#include <cuda_fp16.h>
+#include <type_traits>
 
 #include "paged.cuh"
 
@@ -274,20 +273,20 @@ __device__ __forceinline__ void pf_hide_nan(PfHeader *hd, int p, uint4 &x) {
     atomicOr(&hd->nan_rows[p >> 5], 1u << (p & 31));
 }
 
-// Columns c .. c + 31 of row r's O: NaN where a hidden one lies at a position that
-// the row sees.
+// Row r of what has been stored, NaN where a hidden one lies at a position that the
+// row sees: dim c at dst + c * step.
+template <typename T>
 __device__ __noinline__ void pf_show_nan(const PfArgs &a, const PfHeader *hd, const PfUnit &u, int r,
-                                         int c, float (&v)[32]) {
+                                         T *dst, int step) {
     for (int w = 0; w <= r >> 5; ++w)
         for (uint32_t m = hd->nan_rows[w]; m; m &= m - 1) {
             const int p = w * 32 + __ffs(m) - 1;
             if (p > r) return;
             const int pos = u.p0 + p, pg = a.pv.page(u.sq, pos >> a.pv.shift);
-            const uint8_t *row =
-                a.vp + ((((size_t)pg * a.Hkv + u.g) << a.pv.shift) + (pos & ((1 << a.pv.shift) - 1))) * kPagedDh + c;
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if ((row[i] & 0x7f) == 0x7f) v[i] = __uint_as_float(0x7fffffffu);
+            const uint8_t *row = a.vp + ((((size_t)pg * a.Hkv + u.g) << a.pv.shift) +
+                                         (pos & ((1 << a.pv.shift) - 1))) * kPagedDh;
+            for (int c = 0; c < kPagedDh; ++c)
+                if ((row[c] & 0x7f) == 0x7f) dst[c * step] = from_f<T>(__uint_as_float(0x7fffffffu));
         }
 }
 __device__ __forceinline__ bool pf_any_nan(const PfHeader *hd) {
@@ -340,7 +339,7 @@ __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigne
         const unsigned ok = KEYS ? hd->sc[j % kPfRing].ok : hd->sc[j % kPfRing].values;
         const int at = (u.j0 + j) * kPfRows;
         unsigned char *d = dst + b * kPfTile;
-        if (ok == 0xffu && at + kPfRows - 1 <= (KEYS ? last : u.p0)) {
+        auto rows = [&](auto check) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 uint4 x[B];
@@ -357,24 +356,22 @@ __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigne
 #pragma unroll
                 for (int k = 0; k < B; ++k) {
                     const int n = half * B + k;
-                    if (n < N - 1 || (n < N && w + n * kPfDecWarps < kPfRows / 4))
-                        pf_decode16(x[k], d + n * kPfDecWarps * 512 + (n & 1 ? o0 : e0),
-                                    d + n * kPfDecWarps * 512 + (n & 1 ? o1 : e1));
+                    if (!(n < N - 1 || (n < N && w + n * kPfDecWarps < kPfRows / 4))) continue;
+                    if constexpr (decltype(check)::value) {
+                        const int row = row0 + n * kPfDecWarps * 4;
+                        if (at + row > last || !((ok >> (row >> 4)) & 1u))
+                            x[k] = make_uint4(0u, 0u, 0u, 0u);
+                        if (!KEYS && at + row > u.p0) pf_hide_nan(hd, at + row - u.p0, x[k]);
+                    }
+                    pf_decode16(x[k], d + n * kPfDecWarps * 512 + (n & 1 ? o0 : e0),
+                                d + n * kPfDecWarps * 512 + (n & 1 ? o1 : e1));
                 }
             }
-        } else {
-#pragma unroll 1
-            for (int n = 0; w + n * kPfDecWarps < kPfRows / 4; ++n) {
-                const int row = (w + n * kPfDecWarps) * 4 + (lane >> 3);
-                uint4 x = *reinterpret_cast<const uint4 *>(raw + n * kPfDecWarps * 512);
-                if (at + row > last || !((ok >> (row >> 4)) & 1u)) x = make_uint4(0u, 0u, 0u, 0u);
-                if (!KEYS && at + row > u.p0) pf_hide_nan(hd, at + row - u.p0, x);
-                pf_decode16(x, d + n * kPfDecWarps * 512 + (n & 1 ? o0 : e0),
-                            d + n * kPfDecWarps * 512 + (n & 1 ? o1 : e1));
-            }
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(raw_empty);
-        }
+        };
+        if (ok == 0xffu && at + kPfRows - 1 <= (KEYS ? last : u.p0))
+            rows(std::false_type());
+        else
+            rows(std::true_type());
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&full[b]);
@@ -591,10 +588,10 @@ __device__ __noinline__ void pf_part(const PfArgs &a, PfHeader *hd, const PfUnit
         float v[32];
         tmem_ld32(o_col + c, v);
         tmem_ld_wait();
-        if (pf_any_nan(hd)) pf_show_nan(a, hd, u, r, c, v);
 #pragma unroll
         for (int i = 0; i < 32; ++i) mine[(c + i) * kPfRows + r] = v[i];
     }
+    if (pf_any_nan(hd)) pf_show_nan(a, hd, u, r, mine + r, kPfRows);
     reinterpret_cast<float2 *>(mine + 128 * kPfRows)[r] = make_float2(m, l);
     auto meet = [&]() {  // the head's threads
         if (x == 0) ptx::named_bar_sync(1, 128);
@@ -794,7 +791,6 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
                         float vv[32];
                         tmem_ld32(o_col + c, vv);
                         tmem_ld_wait();
-                        if (pf_any_nan(hd)) pf_show_nan(a, hd, u, r, c, vv);
                         if (r >= u.rows) continue;
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {
@@ -809,6 +805,7 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
                                 make_uint4(w[0], w[1], w[2], w[3]);
                         }
                     }
+                    if (pf_any_nan(hd) && r < u.rows) pf_show_nan(a, hd, u, r, dst, 1);
                 }
             }
             if (!more()) break;
