@@ -431,14 +431,16 @@ moe_status moe_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe, int
  * its layout.)
  *
  * Layouts: k_pages, v_pages [n_pages, Hkv, page_size, 128] e4m3 (a byte each);
- * k_scale, v_scale [n_pages, Hkv] float32, positive; page_table [n_seq,
+ * k_scale, v_scale [n_pages, Hkv] float32, finite, 2^-100 or more (zero: the
+ * page's numbers count as zeros); page_table [n_seq,
  * max_pages] int32: position p of sequence s lies in page page_table[s, p /
  * page_size], row p % page_size.  Entries that no position of a call needs may
  * hold anything.  A page may be in several sequences' tables while nothing is
  * appended to it.
  *
  * Tokens: (seq[t], pos[t]) as in moe_sa_*; the (seq, pos) pairs of a call are
- * distinct, in any order.  seq[t] < 0 is a padding token: it writes nothing to
+ * distinct, in any order (of one that occurs twice, the later token's row is
+ * stored).  seq[t] < 0 is a padding token: it writes nothing to
  * the cache, its rows of q and ctx are zero, and it is no error.  A token with
  * seq >= n_seq or pos outside [0, max_pages page_size) is recorded as
  * MOE_ERR_DEVICE_INDEX and otherwise treated so; a page_table entry that is
@@ -446,8 +448,8 @@ moe_status moe_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe, int
  * neither written nor attended to.
  *
  * Limits: head_dim 128, up to 8 query heads per key/value head, T <= 65536 (as
- * moe_sa_*); page_size 16, 32, 64 or 128; n_pages Hkv page_size and max_pages
- * page_size below 2^31. */
+ * moe_sa_*); page_size 16, 32, 64 or 128; n_pages Hkv page_size below
+ * 2^31, max_pages page_size up to 2^30. */
 typedef struct {
     int32_t page_size; /* positions of a page */
     int32_t n_pages;   /* pages of the pool */
@@ -476,7 +478,9 @@ moe_status moe_paged_append(const moe_sa_dims *dims, const moe_paged_dims *paged
                             void *v_pages, float *k_scale, float *v_scale, moe_stream_t stream);
 
 /* moe_paged_attend: ctx[t, h dh .. (h+1) dh) = softmax over positions 0..pos[t]
- * of q[t,h] . K / sqrt(dh), applied to V, bf16 out; q [T, Hq, 128] bf16.
+ * of q[t,h] . K / sqrt(dh), applied to V, bf16 out; q [T, Hq, 128] bf16.  NaN in
+ * a key or value reaches the tokens that attend to its position (a value's in its
+ * own dim), NaN or an infinity in a query its row.  ctx may not overlap q.
  *   ws  workspace of at least moe_paged_workspace_size(dims, T) bytes; calls
  *       that run at the same time need workspaces of their own. */
 moe_status moe_paged_attend(const moe_sa_dims *dims, const moe_paged_dims *paged, int32_t T,

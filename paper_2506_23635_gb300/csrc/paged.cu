@@ -651,9 +651,10 @@ moe_status check_paged(const moe_sa_dims *d, const moe_paged_dims *pd) {
         return MOE_ERR_INVALID_ARG;
     if (pd->page_size != 16 && pd->page_size != 32 && pd->page_size != 64 && pd->page_size != 128)
         return MOE_ERR_UNSUPPORTED;
-    const int64_t most = (1LL << 31) - 1;
-    if ((int64_t)pd->n_pages * d->n_kv_heads * pd->page_size > most ||
-        (int64_t)pd->max_pages * pd->page_size > most)
+    // (a cache row's number is a TMA coordinate; the tiles of kPagedSmall tokens are
+    // counted in 32 bits)
+    if ((int64_t)pd->n_pages * d->n_kv_heads * pd->page_size > (1LL << 31) - 1 ||
+        (int64_t)pd->max_pages * pd->page_size > 1LL << 30)
         return MOE_ERR_INVALID_ARG;
     return MOE_OK;
 }

@@ -299,7 +299,7 @@ __device__ __forceinline__ float pd_mean(float a, float s) { return s == 0.f ? 0
 // go out together, past L1.  The result goes to dst (the group's heads in ctx), or
 // to the slot `into`, which may be one of them (only the warp itself reads its
 // heads there).  (A thread a dim with all heads, three parts at a time: 3.4 us for
-// 8 parts of 6 heads, PD_MERGE us so.)
+// 8 parts of 6 heads, and one token over 2048 positions 11.7 us instead of 10.4.)
 template <int G, typename Slot>
 __device__ __forceinline__ void pd_merge(const float *part, Slot slot, int parts, int w, bf16 *dst,
                                          float *into) {
@@ -842,7 +842,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             // last on a (token, head) finds every part of it stored; more than
             // kPdGroup parts are counted and merged in groups of that many first
             // (200,001 positions of one head over 304 CTAs: 96 us, all parts by one
-            // CTA, PD_LONG so)
+            // CTA, 22.7 so)
             if (small) ptx::grid_dependency_wait();  // the counters are zero
 #pragma unroll 1
             for (int i = 0; i < 2; ++i) {
@@ -891,7 +891,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     if (warp == 1) tmem_dealloc(tmem, kPdTmemCols);
     // this grid is complete only after what is ahead: one CTA sees to it (the others
     // would keep their SMs from those that wait for one: 512 tokens at position
-    // 5000 beside 24 of up to 2048 positions PD_ONE instead of 144 us)
+    // 5000 beside 24 of up to 2048 positions 144 us, 126 so)
     if (a.ahead != kPagedAheadPlan && cta == n_cta - 1) ptx::grid_dependency_wait();
 }
 

@@ -5,7 +5,9 @@
 // positions p0 .. p0 + rows - 1 of one sequence, a unit a (tile, pair of query
 // heads of one key/value head) over cache positions 0 .. p0 + rows - 1, taken by
 // one CTA an SM from a counter, longest first; the two heads share every key and
-// value tile of 128 positions and take turns on the tensor cores.
+// value tile of 128 positions and take turns on the tensor cores.  Where that leaves
+// SMs idle a unit is one head's, or a part of the positions, merged by the part
+// that ends last.
 //
 // 128 queries share a tile, so its e4m3 numbers are decoded once, to fp16, which
 // holds them exactly (half an instruction and four bytes of shared-memory traffic
@@ -36,6 +38,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "attn_plan.cuh"
 #include "paged.cuh"
 
 namespace moe {
@@ -208,6 +211,7 @@ __device__ __forceinline__ bool pf_fetch(const PfArgs &a, PfHeader *hd, unsigned
     };
     int next = entry(0);
     bool good = true;
+    int asked[2] = {0, 0};  // tiles
 #pragma unroll 1
     for (int j = 0; j < u.n_kv; ++j) {
         const int pg = next >= 0 && next < a.pv.n_pages ? next : -1;
@@ -234,6 +238,7 @@ __device__ __forceinline__ bool pf_fetch(const PfArgs &a, PfHeader *hd, unsigned
                 ptx::tma_load_2d(smem + (v ? kPfOffRawV : kPfOffRawK) +
                                      ((uint32_t)(lane * kPagedDh) << shift),
                                  v ? &a.tmV : &a.tmK, 0, row, &hd->raw_full[v], pol);
+            ++asked[v];
         }
         PfScales *s = &hd->sc[j % kPfRing];
         if (lane < 8) {
@@ -253,10 +258,9 @@ __device__ __forceinline__ bool pf_fetch(const PfArgs &a, PfHeader *hd, unsigned
         if (lane == 0) ptx::mbar_arrive(&hd->t_full[j % kPfRing]);
         if (!good) {
             // (what was asked for lands before the block can exit)
-            if (j > 0) {
-                pf_wait_all(&hd->raw_full[0], (uint32_t)(j - 1) & 1u, a.err);
-                pf_wait_all(&hd->raw_full[1], (uint32_t)(j - 1) & 1u, a.err);
-            }
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+                if (asked[v] > 0) pf_wait_all(&hd->raw_full[v], (uint32_t)(asked[v] - 1) & 1u, a.err);
             break;
         }
     }
@@ -310,8 +314,8 @@ __device__ __forceinline__ void pf_decode16(const uint4 &x, unsigned char *d0, u
 // each) a time of warp w of three, every third four of them.  These warps' issue
 // slots are what the kernel has least of, so a tile whose rows every query sees
 // takes nothing but a load, the conversions and two stores at offsets that a lane
-// forms once (checks in the same loop: 512 tokens at position 5000 163 us, PF_DEC us
-// so).  False: a wait gave up.
+// forms once (checks in the same loop: 512 tokens at position 5000 163 us, 115 so).
+// False: a wait gave up.
 template <bool KEYS>
 __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigned char *smem,
                                           const PfUnit &u, int w) {
@@ -436,7 +440,8 @@ __device__ __forceinline__ float pf_queries(const PfArgs &a, unsigned char *smem
         for (int i = 0; i < 4; ++i) mb = max(mb, max(v[i] & 0x7fff0000u, (v[i] & 0x7fffu) << 16));
     }
     const int e = min(max((int)(mb >> 23), 15), 254);
-    const float up = __uint_as_float((uint32_t)(254 + 14 - e) << 23);
+    // (a row with NaN or an infinity: NaN)
+    const float up = __uint_as_float(mb < 0x7f800000u ? (uint32_t)(254 + 14 - e) << 23 : 0x7fffffffu);
     unsigned char *q = smem + kPfOffQ + x * kPfTile + r * 128;
 #pragma unroll
     for (int c = 0; c < 16; ++c) {
@@ -671,7 +676,9 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
     // unit, and 8 and 1 for each part where they are merged (measured: 512 tokens at
     // position 5000, 44 tiles, 4 x 48 heads on 152 SMs, 140 us in pairs, 214 alone).
     const int4 longest = n_tiles > 0 ? __ldcg(&a.plan.tiles[0]) : make_int4(0, 1, 0, 0);
-    const int n_long = (longest.z + longest.y - 1) / kPfRows + 1;
+    // (the plan's last bin holds tiles of any length from there on, in any order, and
+    // the choice decides what is added first)
+    const int n_long = min((longest.z + longest.y - 1) / kPfRows + 1, kPlanBins);
     bool single = false;
     int S = 1, best = 0x7fffffff;
     for (int one = 0; one < 2; ++one) {

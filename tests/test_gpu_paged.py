@@ -548,3 +548,88 @@ def test_the_binding_refuses_other_devices_and_strides():
         m.paged_attend(d.a, d.cache, q.transpose(0, 1).contiguous().transpose(0, 1), d.seq, d.pos)
     with pytest.raises(ValueError):
         m.paged_append(d.a, d.cache, torch.empty((4, 1280)), d.seq, d.pos)
+
+
+@pytest.mark.parametrize("runs", ["ends", "mixed"])
+def test_attend_queries_not_finite(runs):
+    """NaN or an infinity in a query: its row is NaN, and no other."""
+    m = moe()
+    c = ref.call(6, 2, 32, RUNS[runs], seed=50, pad=2)
+    d = Dev(m, c)
+    q = queries(c)
+    bad = q.clone()
+    at = [(0, 1, 5, float("inf")), (3, 0, 127, float("nan")), (4, 5, 64, -float("inf"))]
+    for t, h, i, x in at:
+        bad[t, h, i] = x
+    got = m.paged_attend(d.a, d.cache, bad, d.seq, d.pos).reshape(-1, 6, 128)
+    assert m.get_last_error() == 0
+    for t, h, _, _ in at:
+        assert bool(got[t, h].isnan().all())
+        got[t, h] = 0
+    want, room = ref.attend(c, q.double().cpu().numpy(), *d.host())
+    for t, h, _, _ in at:
+        want[t, h] = 0
+    err = np.abs(got.double().cpu().numpy() - want) - (2.0 ** -8 * np.abs(want) + 2.0 ** -10 * room)
+    assert np.max(err) <= 0
+
+
+@pytest.mark.parametrize("n", [20, 300])
+def test_append_of_the_same_position_twice(n):
+    """The later token's row is stored, as if the earlier were padding."""
+    m = moe()
+    c = ref.call(6, 2, 32, [(0, 3, n), (1, 64, 2)], seed=51)
+    twice = [(7, 2), (n - 1, 5), (n + 1, n)]  # token, and an earlier one
+    caches = []
+    x, _ = rows_for(c, "f32")
+    for padded in (False, True):
+        e = dict(c, seq=c["seq"].copy(), pos=c["pos"].copy())
+        for t, u in twice:
+            e["seq"][u], e["pos"][u] = (-1, 0) if padded else (c["seq"][t], c["pos"][t])
+        d = Dev(m, e)
+        m.paged_append(d.a, d.cache, x, d.seq, d.pos)
+        assert m.get_last_error() == 0
+        caches.append(d.host())
+    for got, want in zip(*caches):
+        np.testing.assert_array_equal(got, want)
+
+
+@pytest.mark.parametrize("runs", ["ends", "two_chunks", "many"])
+def test_two_calls_at_once(runs):
+    """On two streams, each with a workspace of its own, over one cache."""
+    m = moe()
+    c = ref.call(12, 2, 32, {**RUNS, **ATTEND}[runs], seed=52)
+    d = Dev(m, c)
+    q = [queries(c), queries(c)]
+    want = [m.paged_attend(d.a, d.cache, x, d.seq, d.pos) for x in q]
+    streams = [torch.cuda.Stream() for _ in q]
+    ws = [m.paged_alloc_workspace(d.a, len(c["seq"])) for _ in q]
+    got = [torch.empty_like(x) for x in want]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            m.paged_attend(d.a, d.cache, q[i], d.seq, d.pos, ctx=got[i], ws=ws[i], stream=streams[i])
+    torch.cuda.synchronize()
+    assert m.get_last_error() == 0
+    for g, w in zip(got, want):
+        assert torch.equal(g, w)
+
+
+def test_long_chunks_in_either_order():
+    """Chunks behind tens of thousands of positions: the same bits whichever of
+    them comes first in the call."""
+    m = moe()
+    c = ref.call(3, 1, 128, [(0, 40000, 26), (1, 33000, 30), (2, 50, 1)], seed=53)
+    d, q, got = run_attend(c)
+    turn = np.concatenate([np.arange(26, 56), np.arange(26), [56]])
+    index = torch.from_numpy(turn).cuda()
+    again = m.paged_attend(d.a, d.cache, q[index].contiguous(), d.seq[index], d.pos[index])
+    assert torch.equal(again[:56], got[index][:56])
+
+
+def test_largest_call():
+    """65536 tokens, most of them padding, in between and behind the others."""
+    c = ref.call(2, 1, 16, [(0, 0, 300), (1, 40, 1), (2, 5, 35)], seed=54, pad=65536 - 336)
+    order = np.concatenate([np.arange(336, 33000), np.arange(336), np.arange(33000, 65536)])
+    c["seq"], c["pos"] = c["seq"][order], c["pos"][order]
+    run_append(c)
+    run_attend(c)

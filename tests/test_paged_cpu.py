@@ -181,3 +181,17 @@ def test_the_binding_refuses(lib):
         with pytest.raises(ValueError):
             lib.paged_attend(**{**dict(a=a, cache=c, q=q, seq=seq, pos=pos,
                                        ws=torch.empty(4096, dtype=torch.uint8)), **kw})
+
+
+@no_gpu
+def test_limits_of_the_table_and_the_pool(lib):
+    L = lib.lib()
+    a = lib.sa_dims(6144, 48, 8)
+
+    def app(page, n_pages, max_pages):
+        p = lib.PagedDims(page, n_pages, 4, max_pages)
+        return L.moe_paged_append(ctypes.byref(a), ctypes.byref(p), 0, A, 1, *[A] * 8, None)
+
+    assert app(128, 10, 1 << 23) == 0 and app(128, 10, (1 << 23) + 1) == 1
+    assert app(16, 10, 1 << 26) == 0 and app(16, 10, (1 << 26) + 1) == 1
+    assert app(128, (1 << 21) - 1, 10) == 0 and app(128, 1 << 21, 10) == 1
