@@ -18,10 +18,10 @@
 // to fp16: 2^-11 of it, one term, where bf16 would need two.  The row sum takes the
 // probability itself.
 //
-//   warp 0      tensor memory (per head a score tile S and an output tile O of
-//               128 columns) and the MMAs: per head S_j = Q K_j^T, and once
-//               P_j has taken S_j's place, O += P_j V_j with P_j read from tensor
-//               memory and V_j MN-major as it lies;
+//   warp 0      tensor memory (two score tiles S, a head each or one head's by
+//               turns, and an output tile O per head, of 128 columns) and the MMAs:
+//               S_j = Q K_j^T, and once P_j has taken S_j's place, O += P_j V_j with
+//               P_j read from tensor memory and V_j MN-major as it lies;
 //   warp 1      a tile's pages by TMA, as they are, its scales;
 //   warps 2-4   key rows decoded into two stages with the 128-byte swizzle;
 //   warps 5-7   the same for value rows (rows past the tile's last query and of
@@ -94,7 +94,8 @@ struct PfHeader {
     uint64_t v_full[2], v_empty[2];
     uint64_t t_full[kPfRing];  // a tile's scales written
     uint64_t raw_full[2], raw_empty[2];  // keys', values' rows landed; read by their warps
-    uint64_t s_full[2], p_ready[2], o_full[2];  // per head
+    // per slot (a head's of two, else a tile's by turns): S written, P, P V finished
+    uint64_t s_full[2], p_ready[2], o_full[2];
     uint64_t done;
     uint32_t tmem_base;
     int next;
@@ -131,31 +132,43 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
     return r;
 }
 
-// MN-major, 128-byte swizzle: 8 k 1024 bytes apart, the next 64 MN elements
-// 16 KB on.
-__device__ __forceinline__ uint64_t pf_desc_mn(uint32_t saddr) {
-    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(kPfHalf >> 4) << 16) |
-           ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+// Shared-memory descriptors, 128-byte swizzle, 8 rows 1024 bytes apart: their upper
+// half, and the lower one's fields beside the address: K-major, and MN-major with
+// the next 64 elements 16 KB on.
+constexpr uint32_t kPfDescHi = (1024 >> 4) | 1u << 14 | 2u << 29;
+constexpr uint32_t kPfDescK = 1u << 16, kPfDescMn = (kPfHalf >> 4) << 16;
+
+// One lane of the warp, always the same.
+__device__ __forceinline__ bool pf_elect() {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
 }
 
 __device__ __forceinline__ void pf_issue_qk(uint32_t d, uint32_t q, uint32_t k) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const uint64_t ad = smem_desc(q + half * kPfHalf), bd = smem_desc(k + half * kPfHalf);
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk)  // (kind::f16: the types are the descriptor's)
-            mma_bf16(d, ad + 2 * kk, bd + 2 * kk, kPfIdesc, (half | kk) != 0 ? 1u : 0u);
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t at = (i >> 2) * (kPfHalf >> 4) + (i & 3) * 2;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+            "mov.b64 a, {%1, %4};\n\tmov.b64 b, {%2, %4};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+            "r"(q + at), "r"(k + at), "r"(kPfIdesc), "r"(kPfDescHi), "r"(i != 0 ? 1u : 0u)
+            : "memory");
     }
 }
-
-__device__ __forceinline__ void pf_issue_pv(uint32_t d, uint32_t p_tmem, uint32_t v, bool add) {
+__device__ __forceinline__ void pf_issue_pv(uint32_t d, uint32_t p_tmem, uint32_t v, uint32_t add) {
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks)
+    for (int i = 0; i < 8; ++i)
         asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-            "r"(p_tmem + ks * 8), "l"(pf_desc_mn(v + ks * 16 * 128)), "r"(kPfIdescV),
-            "r"((add || ks != 0) ? 1u : 0u));
+            "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+            "mov.b64 b, {%2, %4};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d),
+            "r"(p_tmem + i * 8), "r"(v + i * (16 * 128 >> 4)), "r"(kPfIdescV), "r"(kPfDescHi),
+            "r"(i != 0 ? 1u : add)
+            : "memory");
 }
 
 __device__ __forceinline__ void pf_tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
@@ -270,8 +283,9 @@ __device__ __forceinline__ bool pf_fetch(const PfArgs &a, PfHeader *hd, unsigned
 // A value row that only the tile's rows from p on may see: 0 x NaN is NaN, so its
 // NaN become zeros for the product, and pf_show_nan puts them where they belong.
 __device__ __forceinline__ void pf_hide_nan(PfHeader *hd, int p, uint4 &x) {
-    const uint32_t n[4] = {__vcmpeq4(x.x & 0x7f7f7f7fu, 0x7f7f7f7fu), __vcmpeq4(x.y & 0x7f7f7f7fu, 0x7f7f7f7fu),
-                           __vcmpeq4(x.z & 0x7f7f7f7fu, 0x7f7f7f7fu), __vcmpeq4(x.w & 0x7f7f7f7fu, 0x7f7f7f7fu)};
+    constexpr uint32_t m = 0x7f7f7f7fu;
+    const uint32_t n[4] = {__vcmpeq4(x.x & m, m), __vcmpeq4(x.y & m, m), __vcmpeq4(x.z & m, m),
+                           __vcmpeq4(x.w & m, m)};
     if ((n[0] | n[1] | n[2] | n[3]) == 0) return;
     x = make_uint4(x.x & ~n[0], x.y & ~n[1], x.z & ~n[2], x.w & ~n[3]);
     atomicOr(&hd->nan_rows[p >> 5], 1u << (p & 31));
@@ -316,20 +330,19 @@ __device__ __forceinline__ void pf_decode16(const uint4 &x, unsigned char *d0, u
 // takes nothing but a load, the conversions and two stores at offsets that a lane
 // forms once (checks in the same loop: 512 tokens at position 5000 163 us, 115 so).
 // False: a wait gave up.
-template <bool KEYS>
 __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigned char *smem,
-                                          const PfUnit &u, int w) {
+                                          const PfUnit &u, bool keys, int w) {
     constexpr int B = 6;                                   // fours of rows a batch
     constexpr int N = (kPfRows / 4 + kPfDecWarps - 1) / kPfDecWarps;  // two batches of N at most
     const int lane = threadIdx.x & 31;
     const int last = u.p0 + u.rows - 1;
-    uint64_t *full = KEYS ? hd->k_full : hd->v_full, *empty = KEYS ? hd->k_empty : hd->v_empty;
-    uint64_t *raw_full = &hd->raw_full[KEYS ? 0 : 1], *raw_empty = &hd->raw_empty[KEYS ? 0 : 1];
-    const unsigned char *raw = smem + (KEYS ? kPfOffRawK : kPfOffRawV) + w * 512 + lane * 16;
+    uint64_t *full = keys ? hd->k_full : hd->v_full, *empty = keys ? hd->k_empty : hd->v_empty;
+    uint64_t *raw_full = &hd->raw_full[keys ? 0 : 1], *raw_empty = &hd->raw_empty[keys ? 0 : 1];
+    const unsigned char *raw = smem + (keys ? kPfOffRawK : kPfOffRawV) + w * 512 + lane * 16;
     // row 4 f + lane / 8, dims 16 (lane % 8) ..: its chunks in the 64-dim half's row,
     // in fours f of even and of odd distance from w
     const uint32_t row0 = w * 4 + (lane >> 3), c = (lane & 3) * 2;
-    unsigned char *dst = smem + (KEYS ? kPfOffK : kPfOffV) + ((lane & 7) >> 2) * kPfHalf + row0 * 128;
+    unsigned char *dst = smem + (keys ? kPfOffK : kPfOffV) + ((lane & 7) >> 2) * kPfHalf + row0 * 128;
     const uint32_t e0 = (c ^ (row0 & 7)) << 4, e1 = ((c + 1) ^ (row0 & 7)) << 4;
     const uint32_t o0 = e0 ^ 64u, o1 = e1 ^ 64u;  // (4 rows on: bit 2 of the row)
 #pragma unroll 1
@@ -340,17 +353,17 @@ __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigne
             !pf_wait_all(&empty[b], ((uint32_t)(j >> 1) & 1u) ^ 1u, a.err))
             return false;
         // rows that hold no position are zeros, as are values under a scale of zero
-        const unsigned ok = KEYS ? hd->sc[j % kPfRing].ok : hd->sc[j % kPfRing].values;
+        const unsigned ok = keys ? hd->sc[j % kPfRing].ok : hd->sc[j % kPfRing].values;
         const int at = (u.j0 + j) * kPfRows;
         unsigned char *d = dst + b * kPfTile;
         auto rows = [&](auto check) {
-#pragma unroll
+#pragma unroll 1
             for (int half = 0; half < 2; ++half) {
                 uint4 x[B];
 #pragma unroll
                 for (int k = 0; k < B; ++k) {
                     const int n = half * B + k;
-                    if (n < N - 1 || (n < N && w + n * kPfDecWarps < kPfRows / 4))
+                    if (k < N - B - 1 || w + n * kPfDecWarps < kPfRows / 4)
                         x[k] = *reinterpret_cast<const uint4 *>(raw + n * kPfDecWarps * 512);
                 }
                 if (half == 1) {
@@ -360,19 +373,19 @@ __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigne
 #pragma unroll
                 for (int k = 0; k < B; ++k) {
                     const int n = half * B + k;
-                    if (!(n < N - 1 || (n < N && w + n * kPfDecWarps < kPfRows / 4))) continue;
+                    if (!(k < N - B - 1 || w + n * kPfDecWarps < kPfRows / 4)) continue;
                     if constexpr (decltype(check)::value) {
                         const int row = row0 + n * kPfDecWarps * 4;
                         if (at + row > last || !((ok >> (row >> 4)) & 1u))
                             x[k] = make_uint4(0u, 0u, 0u, 0u);
-                        if (!KEYS && at + row > u.p0) pf_hide_nan(hd, at + row - u.p0, x[k]);
+                        if (!keys && at + row > u.p0) pf_hide_nan(hd, at + row - u.p0, x[k]);
                     }
-                    pf_decode16(x[k], d + n * kPfDecWarps * 512 + (n & 1 ? o0 : e0),
-                                d + n * kPfDecWarps * 512 + (n & 1 ? o1 : e1));
+                    pf_decode16(x[k], d + n * kPfDecWarps * 512 + (k & 1 ? o0 : e0),
+                                d + n * kPfDecWarps * 512 + (k & 1 ? o1 : e1));
                 }
             }
         };
-        if (ok == 0xffu && at + kPfRows - 1 <= (KEYS ? last : u.p0))
+        if (ok == 0xffu && at + kPfRows - 1 <= (keys ? last : u.p0))
             rows(std::false_type());
         else
             rows(std::true_type());
@@ -382,86 +395,164 @@ __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigne
     }
     return true;
 }
-static_assert(kPfDecWarps % 2 == 1, "the fours of a warp alternate in their rows' bit 2");
+static_assert(kPfDecWarps % 2 == 1 /* and B even */, "the fours of a warp alternate in their rows' bit 2");
 
-// The MMA issuer's part of a unit.  False: a wait gave up.
-__device__ __forceinline__ bool pf_issue(PfHeader *hd, uint32_t sbase, uint32_t tmem,
-                                         const PfUnit &u, unsigned *err) {
-    bool good = pf_wait(&hd->k_full[0], 0, err);
-    for (int x = 0; x < u.nh && good; ++x) {
-        if (!(good = pf_wait(&hd->q_full[x], 0, err))) break;
-        tc_fence_after();
-        pf_issue_qk(tmem + kPfColS + x * 128, sbase + kPfOffQ + x * kPfTile, sbase + kPfOffK);
-        mma_commit(&hd->s_full[x]);
-    }
-    if (good) mma_commit(&hd->k_empty[0]);
-    for (int j = 0; j < u.n_kv && good; ++j) {
-        const int b = j & 1;
-        if (!(good = pf_wait(&hd->v_full[b], (uint32_t)(j >> 1) & 1u, err))) break;
-        for (int x = 0; x < u.nh && good; ++x) {
-            if (!(good = pf_wait(&hd->p_ready[x], j & 1, err))) break;
-            tc_fence_after();
-            pf_issue_pv(tmem + kPfColO + x * 128, tmem + kPfColS + x * 128,
-                        sbase + kPfOffV + b * kPfTile, j != 0);
-            mma_commit(&hd->o_full[x]);
-            if (x == u.nh - 1) mma_commit(&hd->v_empty[b]);
-            if (j + 1 < u.n_kv) {
-                // S_{j+1} replaces P_j: only after P_j V_j has finished
-                const int b1 = (j + 1) & 1;
-                if (!(good = pf_wait(&hd->o_full[x], j & 1, err))) break;
-                if (x == 0 && !(good = pf_wait(&hd->k_full[b1], (uint32_t)((j + 1) >> 1) & 1u, err)))
-                    break;
+// The MMA issuer's part of a unit: P_k V_k, then S of the tile after next for one
+// head, which has two places (slots) for S and P and its softmax no pause, or of the
+// next for two, each of which has one place and works while the other's products
+// run.  S replaces P only after P V has finished.  (Two places of 64 positions each for
+// two heads: products of N = 64 take as long as those of 128, 133 us for 512 tokens
+// at position 5000 instead of 94.  P V of 64 positions at a time, as soon as their P is
+// there: the warp waits for the second half instead of starting the other head's,
+// 98.)
+//
+// The whole warp runs it and one lane issues: operands that are the same in every
+// lane by the code go to the uniform registers that the instructions take them from
+// at once.  A branch of one lane's moves each there first, 85 cycles an instruction
+// of 64: 117 us.  False: a wait gave up.
+__device__ __forceinline__ bool pf_issue(PfHeader *hd, uint32_t sbase, const PfUnit &u,
+                                         unsigned *err) {
+    const int n = __shfl_sync(0xffffffffu, u.n_kv, 0), nh = __shfl_sync(0xffffffffu, u.nh, 0);
+    const uint32_t tmem = __shfl_sync(0xffffffffu, hd->tmem_base, 0);
+    const uint32_t q0 = ((sbase + kPfOffQ) >> 4) | kPfDescK, k0 = ((sbase + kPfOffK) >> 4) | kPfDescK;
+    const uint32_t v0 = ((sbase + kPfOffV) >> 4) | kPfDescMn;
+    const bool lead = pf_elect();
+    auto slot = [&](int x, int k) { return nh == 2 ? x : k & 1; };
+    auto phase = [&](int k) { return (uint32_t)(nh == 2 ? k : k >> 1) & 1u; };
+    const int ahead = 3 - nh;  // of S
+#pragma unroll 1
+    for (int k = -ahead; k < n; ++k)
+#pragma unroll 1
+        for (int x = 0; x < nh; ++x) {
+            if (k >= 0) {
+                const int b = k & 1, s = slot(x, k);
+                if (x == 0 && !pf_wait_all(&hd->v_full[b], (uint32_t)(k >> 1) & 1u, err)) return false;
+                if (!pf_wait_all(&hd->p_ready[s], phase(k), err)) return false;
                 tc_fence_after();
-                pf_issue_qk(tmem + kPfColS + x * 128, sbase + kPfOffQ + x * kPfTile,
-                            sbase + kPfOffK + b1 * kPfTile);
-                mma_commit(&hd->s_full[x]);
-                if (x == u.nh - 1) mma_commit(&hd->k_empty[b1]);
+                if (lead) {
+                    pf_issue_pv(tmem + kPfColO + x * 128, tmem + kPfColS + s * 128, v0 + b * (kPfTile >> 4), k != 0);
+                    mma_commit(&hd->o_full[s]);
+                    if (x == nh - 1) mma_commit(&hd->v_empty[b]);
+                }
+                __syncwarp();
+            }
+            const int i = k + ahead;
+            if (i < n) {
+                const int b = i & 1, s = slot(x, i);
+                if (i == 0 && !pf_wait_all(&hd->q_full[x], 0, err)) return false;
+                if (x == 0 && !pf_wait_all(&hd->k_full[b], (uint32_t)(i >> 1) & 1u, err)) return false;
+                if (k >= 0 && !pf_wait_all(&hd->o_full[s], phase(k), err)) return false;
+                tc_fence_after();
+                if (lead) {
+                    pf_issue_qk(tmem + kPfColS + s * 128, q0 + x * (kPfTile >> 4), k0 + b * (kPfTile >> 4));
+                    mma_commit(&hd->s_full[s]);
+                    if (x == nh - 1) mma_commit(&hd->k_empty[b]);
+                }
+                __syncwarp();
             }
         }
-    }
-    return good;
+    return true;
 }
 
-// Row r of head x's queries: scaled to fp16 in shared memory; what its scores
-// are to be multiplied with.
+// Head x's queries, scaled to fp16 in shared memory, by the head's four warps: 32
+// rows a warp, two of them (16 lanes each) at a time.  What row r's scores are to
+// be multiplied with, r the thread's.  (A row a thread, 16 loads of 32 lines each,
+// kept the first tiles' loads waiting, and pf_store's stores alike: a prompt of 1000
+// tokens 39.0 us, 33.5 with both so.)
 __device__ __forceinline__ float pf_queries(const PfArgs &a, unsigned char *smem, const PfUnit &u,
                                             int x, int r) {
-    uint4 w[16];
-    const bool in = r < u.rows;
+    const int lane = r & 31, r0 = r - lane, half = lane >> 4, c = lane & 15;
     const uint4 *src = reinterpret_cast<const uint4 *>(
-        a.q + ((size_t)(u.t0 + (in ? r : 0)) * a.Hq + u.h0 + x) * kPagedDh);
-    uint32_t mb = 0;
+                           a.q + ((size_t)u.t0 * a.Hq + u.h0 + x) * kPagedDh) + c;
+    const size_t step = (size_t)a.Hq * (kPagedDh / 8);
+    uint4 w[16];
 #pragma unroll
-    for (int c = 0; c < 16; ++c) {
-        w[c] = in ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-        // the larger magnitude of a pair of bf16
-        const uint32_t v[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mb = max(mb, max(v[i] & 0x7fff0000u, (v[i] & 0x7fffu) << 16));
+    for (int i = 0; i < 16; ++i) {
+        const int row = r0 + 2 * i + half;
+        w[i] = row < u.rows ? src[row * step] : make_uint4(0u, 0u, 0u, 0u);
     }
-    const int e = min(max((int)(mb >> 23), 15), 254);
-    // (a row with NaN or an infinity: NaN)
-    const float up = __uint_as_float(mb < 0x7f800000u ? (uint32_t)(254 + 14 - e) << 23 : 0x7fffffffu);
-    unsigned char *q = smem + kPfOffQ + x * kPfTile + r * 128;
+    // a row's largest magnitude, as bf16; rows of i and i + 8 side by side
+    uint32_t m[8];
 #pragma unroll
-    for (int c = 0; c < 16; ++c) {
-        const uint32_t v[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+    for (int i = 0; i < 8; ++i) {
+        uint32_t p[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint4 v = w[i + 8 * k];
+            p[k] = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu),
+                            __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+        }
+        m[i] = __vmaxu2(__byte_perm(p[0], p[1], 0x5410), __byte_perm(p[0], p[1], 0x7632));
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) m[i] = __vmaxu2(m[i], __shfl_xor_sync(0xffffffffu, m[i], o));
+    }
+    unsigned char *q = smem + kPfOffQ + x * kPfTile + (c >> 3) * kPfHalf;
+    uint32_t mine = 0;  // the thread's own row's
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const uint32_t mb = i < 8 ? m[i] & 0xffffu : m[i - 8] >> 16;
+        const int e = min(max((int)(mb >> 7), 15), 254);
+        // (a row with NaN or an infinity: NaN)
+        const float up = __uint_as_float(mb < 0x7f80u ? (uint32_t)(254 + 14 - e) << 23 : 0x7fffffffu);
+        const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
         uint32_t y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int k = 0; k < 4; ++k) {
             float lo, hi;
-            unpack_bf16x2(v[i], lo, hi);
-            y[i] = f16x2(lo * up, hi * up);
+            unpack_bf16x2(v[k], lo, hi);
+            y[k] = f16x2(lo * up, hi * up);
         }
-        *reinterpret_cast<uint4 *>(q + (c >> 3) * kPfHalf + (((c & 7) ^ (r & 7)) << 4)) =
+        const int row = r0 + 2 * i + half;
+        *reinterpret_cast<uint4 *>(q + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
             make_uint4(y[0], y[1], y[2], y[3]);
+        const uint32_t of = __shfl_sync(0xffffffffu, (uint32_t)e, (lane & 1) << 4);
+        mine = (lane >> 1) == i ? of : mine;
     }
     // log2(e) / sqrt(128)
-    return 0.12751743f * __uint_as_float((uint32_t)(e - 14) << 23);
+    return 0.12751743f * __uint_as_float((mine - 14u) << 23);
+}
+
+// Rows of head x's O, divided by their sums, to ctx: a row's bf16 go through the
+// head's queries' place (no product reads them any more), so that 16 lanes store a
+// row.
+__device__ __forceinline__ void pf_store(const PfArgs &a, unsigned char *smem, const PfUnit &u,
+                                         int x, int r, uint32_t o_col, float l) {
+    const int lane = r & 31, r0 = r - lane;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    unsigned char *s = smem + kPfOffQ + x * kPfTile;
+#pragma unroll
+    for (int c = 0; c < 128; c += 32) {
+        float v[32];
+        tmem_ld32(o_col + c, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const __nv_bfloat162 p2 =
+                    __floats2bfloat162_rn(v[i + 2 * e] * inv, v[i + 2 * e + 1] * inv);
+                w[e] = *reinterpret_cast<const uint32_t *>(&p2);
+            }
+            *reinterpret_cast<uint4 *>(s + r * 256 + ((((c + i) >> 3) ^ (r & 7)) << 4)) =
+                make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    __syncwarp();
+    const int ch = lane & 15;
+    bf16 *dst = a.ctx + ((size_t)u.t0 * a.Hq + u.h0 + x) * kPagedDh + ch * 8;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int row = r0 + 2 * i + (lane >> 4);
+        if (row < u.rows)
+            *reinterpret_cast<uint4 *>(dst + (size_t)row * a.Hq * kPagedDh) =
+                *reinterpret_cast<const uint4 *>(s + row * 256 + ((ch ^ (row & 7)) << 4));
+    }
+    __syncwarp();  // (before pf_show_nan, and the next unit's queries)
 }
 
 // One row's softmax over a unit's tiles; m, l: its exponent base, its sum.
-__device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_t o_col,
+__device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_cols, uint32_t o_col,
                                            const PfUnit &u, int r, int x, float qs, float &m,
                                            float &l, unsigned *err) {
     const int lane = threadIdx.x & 31;
@@ -470,9 +561,11 @@ __device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_
     bool good = true;
 #pragma unroll 1
     for (int j = 0; j < u.n_kv; ++j) {
+        const int slot = u.nh == 2 ? x : j & 1;
+        const uint32_t phase = (uint32_t)(u.nh == 2 ? j : j >> 1) & 1u, s_col = s_cols + slot * 128;
         const int lim = u.p0 + r - (u.j0 + j) * kPfRows;  // the row's last position in the tile
         good = good && pf_wait_all(&hd->t_full[j % kPfRing], (uint32_t)(j / kPfRing) & 1u, err);
-        good = good && pf_wait_all(&hd->s_full[x], j & 1, err);
+        good = good && pf_wait_all(&hd->s_full[slot], phase, err);
         tc_fence_after();
         float v[128];
 #pragma unroll
@@ -509,6 +602,7 @@ __device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_
         const bool bump = mrow > m + kPfSlack;
         const float corr = bump ? pf_exp2(m - mrow) : 1.f;
         if (bump) m = mrow;
+        const bool rescale = __any_sync(0xffffffffu, bump) && j >= 1 && good;
         float lt = 0.f;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -535,7 +629,11 @@ __device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_
         }
         // a new base rescales O: P_{j-1} V_{j-1} finished before S_j was issued,
         // and P_j V_j waits for this warp's arrival
-        if (j >= 1 && __any_sync(0xffffffffu, bump) && good) {
+        if (rescale) {
+            // (one head's S_j is issued ahead of P_{j-1} V_{j-1})
+            if (u.nh == 1)
+                good = pf_wait_all(&hd->o_full[slot ^ 1], (uint32_t)((j - 1) >> 1) & 1u, err);
+            tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < 128; c += 32) {
                 float ov[32];
@@ -550,7 +648,7 @@ __device__ __forceinline__ bool pf_softmax(PfHeader *hd, uint32_t s_col, uint32_
         pf_tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&hd->p_ready[x]);
+        if (lane == 0) ptx::mbar_arrive(&hd->p_ready[slot]);
         l = l * corr + lt;
     }
     return good;
@@ -666,157 +764,137 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
     const uint32_t sbase = ptx::smem_u32(smem);
     unsigned *err = a.err;
 
+    // ahead of the wait: what needs nothing of the plan
+    if (threadIdx.x == 0) {
+        hd->gave_up = 0;
+        ptx::prefetch_tmap(&a.tmK);
+        ptx::prefetch_tmap(&a.tmV);
+    }
+    if (warp == 0) tmem_alloc(&hd->tmem_base, kPfTmemCols);
+    // the barriers of a unit, before and after the block meets
+    auto begin = [&](bool again) {
+        if (threadIdx.x < kPfBars) {
+            const int i = threadIdx.x;
+            if (again) ptx::mbar_inval(hd->q_full + i);
+            // (q_full and p_ready: a head's four warps; k_full, v_full and
+            // raw_empty: the decoding ones)
+            auto of = [&](int first, int n) { return i >= first && i < first + n; };
+            ptx::mbar_init(hd->q_full + i, of(0, 2) || of(kPfBarP, 2) ? 4
+                                           : of(kPfBarKF, 2) || of(kPfBarVF, 2) || of(kPfBarRaw, 2)
+                                               ? kPfDecWarps
+                                               : 1);
+            ptx::fence_barrier_init();
+        }
+        if (threadIdx.x < kPfRows / 32) hd->nan_rows[threadIdx.x] = 0u;
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+    };
+    begin(false);
     ptx::grid_dependency_wait();
     ptx::launch_dependents();
     const int n_tiles = __ldcg(&a.plan.head->n_tiles);
+    const int4 longest = __ldcg(&a.plan.tiles[0]);  // (read whether there is one or not)
     // Two heads a unit or one, and a unit whole or, where there are at least two CTAs
     // to each, cut along the positions into up to kPfMaxParts parts of kPfMinTiles
     // tiles or more: whichever ends first for units as long as the longest, counting
-    // 2.75 us for a position tile of two heads, 2.4 of one, 5 us to start and leave a
+    // 1.85 us for a position tile of two heads, 1.3 of one, 5 us to start and leave a
     // unit, and 8 and 1 for each part where they are merged (measured: 512 tokens at
-    // position 5000, 44 tiles, 4 x 48 heads on 152 SMs, 140 us in pairs, 214 alone).
-    const int4 longest = n_tiles > 0 ? __ldcg(&a.plan.tiles[0]) : make_int4(0, 1, 0, 0);
+    // position 5000, 44 tiles, 4 x 48 heads on 152 SMs, 94 us in pairs, 133 alone).
+    // A lane a choice.
     // (the plan's last bin holds tiles of any length from there on, in any order, and
     // the choice decides what is added first)
-    const int n_long = min((longest.z + longest.y - 1) / kPfRows + 1, kPlanBins);
-    bool single = false;
-    int S = 1, best = 0x7fffffff;
-    for (int one = 0; one < 2; ++one) {
-        const int units = max(1, n_tiles * a.Hkv * (one ? G : pairs)), cost = one ? 48 : 55;
+    const int n_long = n_tiles > 0 ? min((longest.z + longest.y - 1) / kPfRows + 1, kPlanBins) : 1;
+    bool single;
+    int S;
+    {
+        const bool one = lane & 2, whole = !(lane & 1);
+        const int units = max(1, n_tiles * a.Hkv * (one ? G : pairs)), cost = one ? 26 : 37;
         const int most = min(min(kPfMaxParts, (int)gridDim.x / units), n_long / kPfMinTiles);
-        for (int whole = 1; whole >= 0; --whole) {
-            const int parts = whole ? 1 : most;
-            if (parts < 1 || (!whole && parts == 1)) continue;
-            const int rounds = (units * parts + (int)gridDim.x - 1) / (int)gridDim.x;
-            const long long us20 = (long long)rounds * ((n_long + parts - 1) / parts * cost + 100) +
-                                   (whole ? 0 : 160 + 20 * parts);
-            if (us20 < best) {
-                best = (int)us20;
-                single = one;
-                S = parts;
-            }
-        }
+        const int parts = whole ? 1 : max(most, 1);
+        const int rounds = (units * parts + (int)gridDim.x - 1) / (int)gridDim.x;
+        const long long us20 = (long long)rounds * ((n_long + parts - 1) / parts * cost + 100) +
+                               (whole ? 0 : 160 + 20 * parts);
+        const unsigned key = (unsigned)min(us20, (1LL << 29) - 1) << 2 | (lane & 3);
+        const unsigned best = __reduce_min_sync(0xffffffffu, whole || most > 1 ? key : 0xffffffffu);
+        single = best & 2;
+        S = __shfl_sync(0xffffffffu, parts, best & 3);
     }
     const int per = single ? G : pairs;
     const int n_whole = n_tiles * a.Hkv * per;
     const int n_units = n_whole * S;
     int unit = (int)blockIdx.x;
-    if (unit >= n_units) return;
-    if (threadIdx.x == 0) hd->gave_up = 0;
-    if (warp == 0) tmem_alloc(&hd->tmem_base, kPfTmemCols);
-    // the barriers of a unit, before and after the block meets
-    auto begin = [&](bool again) {
-        if (threadIdx.x == 0) {
-            uint64_t *bars = hd->q_full;
-            if (again)
-                for (int i = 0; i < kPfBars; ++i) ptx::mbar_inval(bars + i);
-            for (int i = 0; i < kPfBars; ++i) {
-                // (q_full and p_ready: a head's four warps; k_full, v_full and
-                // raw_empty: the decoding ones)
-                const int n = i < 2 || i == kPfBarP || i == kPfBarP + 1 ? 4
-                              : i == kPfBarKF || i == kPfBarKF + 1 || i == kPfBarVF ||
-                                      i == kPfBarVF + 1 || i == kPfBarRaw || i == kPfBarRaw + 1
-                                  ? kPfDecWarps
-                                  : 1;
-                ptx::mbar_init(bars + i, n);
-            }
-            for (int i = 0; i < kPfRows / 32; ++i) hd->nan_rows[i] = 0u;
-            ptx::fence_barrier_init();
-        }
-        tc_fence_before();
-        __syncthreads();
-        tc_fence_after();
-    };
-    // the next unit, for all; false: there is none
+    if (unit >= n_units) {
+        if (warp == 0) tmem_dealloc(hd->tmem_base, kPfTmemCols);
+        return;
+    }
+    // the next unit, for all, its barriers made; false: there is none
     auto more = [&]() {
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
         unit = hd->next;
-        const bool go = unit < n_units && !hd->gave_up;
-        __syncthreads();  // (read by all before the next unit's)
-        return go;
+        if (unit >= n_units || hd->gave_up) return false;
+        begin(true);  // (meets: all have read what the next unit writes)
+        return true;
     };
 
     if (warp < kPfHeadWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPfRegsFeed));
 #pragma unroll 1
-        for (bool again = false;; again = true) {
-            begin(again);
+        do {
             const PfUnit u = pf_unit(a, unit, G, per, single, S);
             bool good = true;
             if (warp == 0) {
-                if (lane == 0 && u.n_kv > 0) {
-                    good = pf_issue(hd, sbase, hd->tmem_base, u, err);
-                    mma_commit(&hd->done);
-                    good &= pf_wait(&hd->done, 0, err);
+                if (u.n_kv > 0) {
+                    good = pf_issue(hd, sbase, u, err);
+                    if (pf_elect()) mma_commit(&hd->done);
+                    good &= pf_wait_all(&hd->done, 0, err);
                     // the MMAs' last arrivals, before the barriers start anew
                     for (int j = max(0, u.n_kv - 2); good && j < u.n_kv; ++j)
-                        good = pf_wait(&hd->k_empty[j & 1], (uint32_t)(j >> 1) & 1u, err) &&
-                               pf_wait(&hd->v_empty[j & 1], (uint32_t)(j >> 1) & 1u, err);
+                        good = pf_wait_all(&hd->k_empty[j & 1], (uint32_t)(j >> 1) & 1u, err) &&
+                               pf_wait_all(&hd->v_empty[j & 1], (uint32_t)(j >> 1) & 1u, err);
                 }
-                __syncwarp();
             } else if (warp == 1) {
                 good = pf_fetch(a, hd, smem, u);
                 if (lane == 0) hd->next = (int)gridDim.x + atomicAdd(&a.plan.head->next, 1);
-            } else if (warp < 2 + kPfDecWarps) {
-                good = pf_decode<true>(a, hd, smem, u, warp - 2);
             } else {
-                good = pf_decode<false>(a, hd, smem, u, warp - 2 - kPfDecWarps);
+                const bool keys = warp < 2 + kPfDecWarps;
+                good = pf_decode(a, hd, smem, u, keys, warp - (keys ? 2 : 2 + kPfDecWarps));
             }
             if (!good) hd->gave_up = 1;
-            if (!more()) break;
-        }
+        } while (more());
         if (warp == 0) tmem_dealloc(hd->tmem_base, kPfTmemCols);
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPfRegsSoftmax));
         const int x = (warp - kPfHeadWarp) / 4;
         const int q = warp & 3, r = q * 32 + lane;
 #pragma unroll 1
-        for (bool again = false;; again = true) {
-            begin(again);
+        do {
             const PfUnit u = pf_unit(a, unit, G, per, single, S);
             if (x < u.nh && u.n_kv > 0) {
-                const uint32_t at = hd->tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)x * 128;
-                const uint32_t s_col = at + kPfColS, o_col = at + kPfColO;
+                const uint32_t at = hd->tmem_base + ((uint32_t)(q * 32) << 16);
+                const uint32_t o_col = at + kPfColO + x * 128;
                 const float qs = pf_queries(a, smem, u, x, r);
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&hd->q_full[x]);
                 float m = kPfNone, l = 0.f;
-                bool good = pf_softmax(hd, s_col, o_col, u, r, x, qs, m, l, err);
-                good = good && pf_wait_all(&hd->o_full[x], (u.n_kv - 1) & 1, err);
+                bool good = pf_softmax(hd, at + kPfColS, o_col, u, r, x, qs, m, l, err);
+                good = good && pf_wait_all(&hd->o_full[u.nh == 2 ? x : (u.n_kv - 1) & 1],
+                                           (uint32_t)(u.nh == 2 ? u.n_kv - 1 : (u.n_kv - 1) >> 1) & 1u, err);
                 if (!good) hd->gave_up = 1;
                 if (good) tc_fence_after();
                 if (good && u.parts > 1) {
                     pf_part(a, hd, u, x, r, o_col, m, l);
                 } else if (good) {
-                    const float inv = l == 0.f ? 0.f : 1.f / l;
-                    bf16 *dst = a.ctx + ((size_t)(u.t0 + r) * a.Hq + u.h0 + x) * kPagedDh;
-#pragma unroll
-                    for (int c = 0; c < 128; c += 32) {
-                        float vv[32];
-                        tmem_ld32(o_col + c, vv);
-                        tmem_ld_wait();
-                        if (r >= u.rows) continue;
-#pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const __nv_bfloat162 p2 = __floats2bfloat162_rn(
-                                    vv[i + 2 * e] * inv, vv[i + 2 * e + 1] * inv);
-                                w[e] = *reinterpret_cast<const uint32_t *>(&p2);
-                            }
-                            *reinterpret_cast<uint4 *>(dst + c + i) =
-                                make_uint4(w[0], w[1], w[2], w[3]);
-                        }
-                    }
-                    if (pf_any_nan(hd) && r < u.rows) pf_show_nan(a, hd, u, r, dst, 1);
+                    pf_store(a, smem, u, x, r, o_col, l);
+                    if (pf_any_nan(hd) && r < u.rows)
+                        pf_show_nan(a, hd, u, r,
+                                    a.ctx + ((size_t)(u.t0 + r) * a.Hq + u.h0 + x) * kPagedDh, 1);
                 }
             }
-            if (!more()) break;
-        }
+        } while (more());
     }
 }
 
@@ -829,7 +907,8 @@ cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, fl
     cudaError_t e = once.set(kern, kPfSmem);
     if (e != cudaSuccess) return e;
     PfArgs pa{{}, {}, a.Hq, a.Hkv, a.pv, plan, static_cast<const bf16 *>(a.q),
-              static_cast<const uint8_t *>(a.vp), a.ks, a.vs, static_cast<bf16 *>(a.ctx), part, count, device_info().err};
+              static_cast<const uint8_t *>(a.vp), a.ks, a.vs, static_cast<bf16 *>(a.ctx), part,
+              count, device_info().err};
     if (!paged_map(&pa.tmK, a.kp, a, false) || !paged_map(&pa.tmV, a.vp, a, false))
         return cudaErrorInvalidValue;
     void *args[] = {&pa};
