@@ -71,8 +71,8 @@ struct SmemOnce {
 // The tokens that the decode attention takes one by one, made on the device
 // (k_paged_plan): list[i] is a token, before[i] the position tiles (of
 // kPagedTile positions; none for a token outside the table) of the list's tokens
-// ahead of it, entry n_list those of all.  count: counters of finished parts, two for each CTA, zero
-// at the start.
+// ahead of it, entry n_list those of all.  count: counters of finished parts, two
+// for each CTA, zero at the start.
 constexpr int kPagedSmall = 128;
 constexpr int kPagedTile = 128;
 constexpr int kPagedMaxCtas = 320;
@@ -109,7 +109,6 @@ inline bool paged_map(CUtensorMap *m, const void *base, const PagedAttn &a, bool
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Attention of the listed tokens over the 8-bit cache (paged_decode_tc.cu).
 // Fewer consecutive tokens than this are attended one by one: a tile costs its
 // heads 2.4 us of an SM for each 128 positions whatever its rows, a token its
 // key/value heads 0.55 (DBRX's heads break even at 24).
@@ -121,6 +120,7 @@ constexpr int kPagedUnitParts = 160;  // one for each SM
 constexpr size_t kPagedUnitPartFloats = (size_t)kPagedUnitParts * 2 * 128 * (128 + 2);
 cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, float *part,
                                     int *count, cudaStream_t st);
+// Attention of the listed tokens (paged_decode_tc.cu).
 // ahead: what the launch ahead is.  kPagedAheadZero: k_paged_plan for a call of up
 // to kPagedSmall tokens, all taken one by one: the kernel lists them itself, and
 // only the counters are the plan's.  kPagedAheadPlan: k_paged_plan.

@@ -131,23 +131,33 @@ __device__ __forceinline__ float pd_exp2(float x) {
     return y;
 }
 
-// D[tmem] (+)= A[smem] * B[smem], 8-bit operands, one instruction of K = 32.
-__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
-                                       uint32_t idesc, uint32_t accumulate) {
+// Shared-memory descriptors.  Their upper half: 128-byte swizzle, 8 rows 1024 bytes
+// apart (queries and keys, K-major; values, MN-major: the next 8 rows, of k), and
+// 32-byte swizzle, 8 rows 256 bytes apart (probabilities, MN-major); the lower one's
+// field beside the address.  No operand is wider than a row.
+constexpr uint32_t kPdDescHi = (1024 >> 4) | 1u << 14 | 2u << 29;
+constexpr uint32_t kPdDescPHi = (256 >> 4) | 1u << 14 | 6u << 29;
+constexpr uint32_t kPdDescLo = 1u << 16;
+
+// One lane of the warp, always the same.
+__device__ __forceinline__ bool pd_elect() {
+    uint32_t r;
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
+        "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
 }
 
-// MN-major operands: rows of 128 bytes (128-byte swizzle, 8 rows 1024 bytes) or
-// of 32 (32-byte swizzle, 8 rows 256 bytes): the stride offset is that of the
-// next 8 rows (k); no operand is wider than a row.
-__device__ __forceinline__ uint64_t pd_desc_v(uint32_t saddr) { return smem_desc(saddr); }
-__device__ __forceinline__ uint64_t pd_desc_p(uint32_t saddr) {
-    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) |
-           ((uint64_t)(256 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)6 << 61);
+// D[tmem] (+)= A[smem] * B[smem], 8-bit operands, one instruction of K = 32; a, b:
+// the descriptors' lower halves.
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint32_t a, uint32_t b, uint32_t b_hi,
+                                       uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "mov.b64 da, {%1, %4};\n\tmov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a), "r"(b), "r"(idesc), "r"(kPdDescHi), "r"(b_hi), "r"(accumulate)
+        : "memory");
 }
 
 // A whole warp's wait: the answer is the same in every lane.
@@ -540,61 +550,67 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA
-        if (lane == 0) {
-            bool good = true;
-            int piece = -1;
-            uint32_t acc = 0, acc1 = 0;  // tile j, tile j - 1 adds to O
-            for (int j = 0; good; ++j) {
-                if (!(good = ptx::mbar_wait(&hd->t_full[j % kPdRing], (uint32_t)(j / kPdRing) & 1u,
-                                            err)))
-                    break;
-                const PdDesc *d = &hd->desc[j % kPdRing];
-                const bool more = d->tile >= 0;
-                if (more) {
-                    const int flags = d->flags, st = j % kPdStages;
-                    acc = flags & kPdFirst ? 0u : 1u;
-                    if (flags & kPdFirst) {
-                        ++piece;
-                        good = ptx::mbar_wait(&hd->q_full[piece & 1], (uint32_t)(piece >> 1) & 1u, err);
-                    }
-                    good = good &&
-                           ptx::mbar_wait(&hd->k_full[st], (uint32_t)(j / kPdStages) & 1u, err) &&
-                           ptx::mbar_wait(&hd->s_empty[j & 1], ((uint32_t)(j >> 1) & 1u) ^ 1u, err);
-                    if (!good) break;
-                    tc_fence_after();
-                    const uint64_t ad = smem_desc(sbase + kPdOffK + st * kPdTile);
-                    const uint64_t bd = smem_desc(sbase + kPdOffQ + (piece & 1) * kPdQ);
+        // The whole warp runs it and one lane issues: operands that are the same in
+        // every lane by the code go to uniform registers, which the instructions take
+        // them from, at once (a branch of one lane's moves each there first).
+        bool good = true;
+        int piece = -1;
+        uint32_t acc = 0, acc1 = 0;  // tile j, tile j - 1 adds to O
+        const bool lead = pd_elect();
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+        const uint32_t k0 = ((sbase + kPdOffK) >> 4) | kPdDescLo, q0 = ((sbase + kPdOffQ) >> 4) | kPdDescLo;
+        const uint32_t v0 = ((sbase + kPdOffV) >> 4) | kPdDescLo, p0 = ((sbase + kPdOffP) >> 4) | kPdDescLo;
+#pragma unroll 1
+        for (int j = 0; good; ++j) {
+            if (!(good = pd_wait(&hd->t_full[j % kPdRing], (uint32_t)(j / kPdRing) & 1u, err))) break;
+            const PdDesc *d = &hd->desc[j % kPdRing];
+            const bool more = __shfl_sync(0xffffffffu, d->tile, 0) >= 0;
+            if (more) {
+                const int flags = __shfl_sync(0xffffffffu, d->flags, 0), st = j % kPdStages;
+                acc = flags & kPdFirst ? 0u : 1u;
+                if (flags & kPdFirst) {
+                    ++piece;
+                    good = pd_wait(&hd->q_full[piece & 1], (uint32_t)(piece >> 1) & 1u, err);
+                }
+                good = good && pd_wait(&hd->k_full[st], (uint32_t)(j / kPdStages) & 1u, err) &&
+                       pd_wait(&hd->s_empty[j & 1], ((uint32_t)(j >> 1) & 1u) ^ 1u, err);
+                if (!good) break;
+                tc_fence_after();
+                if (lead) {
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
-                        mma_f8(tmem + kPdColS + (j & 1) * 16, ad + 2 * kk, bd + 2 * kk, kPdIdescQK,
+                        mma_f8(tm + kPdColS + (j & 1) * 16, k0 + ((st * kPdTile) >> 4) + 2 * kk,
+                               q0 + (((piece & 1) * kPdQ) >> 4) + 2 * kk, kPdDescHi, kPdIdescQK,
                                kk != 0);
                     mma_commit(&hd->s_full[j & 1]);
                     mma_commit(&hd->k_empty[st]);
                     if (flags & kPdLast) mma_commit(&hd->q_empty[piece & 1]);
                 }
-                if (j > 0) {  // P_{j-1} V_{j-1}
-                    const int u = j - 1, st = u % kPdStages;
-                    good = ptx::mbar_wait(&hd->v_full[st], (uint32_t)(u / kPdStages) & 1u, err) &&
-                           ptx::mbar_wait(&hd->p_ready[u & 1], (uint32_t)(u >> 1) & 1u, err);
-                    if (!good) break;
-                    tc_fence_after();
+                __syncwarp();
+            }
+            if (j > 0) {  // P_{j-1} V_{j-1}
+                const int u = j - 1, st = u % kPdStages;
+                good = pd_wait(&hd->v_full[st], (uint32_t)(u / kPdStages) & 1u, err) &&
+                       pd_wait(&hd->p_ready[u & 1], (uint32_t)(u >> 1) & 1u, err);
+                if (!good) break;
+                tc_fence_after();
+                if (lead) {
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
-                        mma_f8(tmem + kPdColO,
-                               pd_desc_v(sbase + kPdOffV + st * kPdTile + kk * 32 * kPagedDh),
-                               pd_desc_p(sbase + kPdOffP + (u & 1) * kPdP + kk * 32 * 32),
-                               kPdIdescPV, (acc1 | (uint32_t)(kk != 0)));
+                        mma_f8(tm + kPdColO, v0 + ((st * kPdTile + kk * 32 * kPagedDh) >> 4),
+                               p0 + (((u & 1) * kPdP + kk * 32 * 32) >> 4), kPdDescPHi, kPdIdescPV,
+                               kk != 0 ? 1u : acc1);
                     mma_commit(&hd->p_empty[u & 1]);
                     mma_commit(&hd->v_empty[st]);
                 }
-                acc1 = acc;
-                if (!more) break;
+                __syncwarp();
             }
-            // every MMA has finished before tensor memory is freed
-            mma_commit(&hd->done);
-            ptx::mbar_wait(&hd->done, 0, err);
+            acc1 = acc;
+            if (!more) break;
         }
-        __syncwarp();
+        // every MMA has finished before tensor memory is freed
+        if (lead) mma_commit(&hd->done);
+        pd_wait(&hd->done, 0, err);
     } else if (warp == 6) {
         // ------------------------------------------------------------ queries
         PdWalk w = pd_begin(tokens, Hkv, cta, n_cta);
@@ -920,8 +936,9 @@ cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float
     static SmemOnce once[kPdMaxG];
     cudaError_t e = once[G - 1].set(kern, kPdSmem);
     if (e != cudaSuccess) return e;
-    PdArgs pa{ahead == kPagedAheadZero ? a.T : 0, ahead, a.Hq, a.Hkv, a.pv, l, a.seq, a.pos, static_cast<const bf16 *>(a.q), a.ks, a.vs,
-              static_cast<bf16 *>(a.ctx), part, device_info().err};
+    PdArgs pa{ahead == kPagedAheadZero ? a.T : 0, ahead, a.Hq, a.Hkv, a.pv, l, a.seq, a.pos,
+              static_cast<const bf16 *>(a.q), a.ks, a.vs, static_cast<bf16 *>(a.ctx), part,
+              device_info().err};
     void *args[] = {&mk, &mv, &pa};
     // as many CTAs as the largest positions give tiles
     const long long most = (long long)a.T * a.Hkv *
