@@ -633,3 +633,13 @@ def test_largest_call():
     c["seq"], c["pos"] = c["seq"][order], c["pos"][order]
     run_append(c)
     run_attend(c)
+
+
+@pytest.mark.parametrize("page,runs,order", [
+    (16, [(0, 5, 1000), (1, 0, 340)], "shuffled"),
+    (16, [(0, 5, 2000), (1, 48, 620), (2, 9, 1)], "given"),
+    (128, [(0, 70, 6000), (1, 0, 3000), (2, 128, 800)], "given"),
+], ids=str)
+def test_append_several_rows_a_block(page, runs, order):
+    """Calls with blocks enough for each to take some of the heads' rows."""
+    run_append(ref.call(8, 8, page, runs, seed=55, order=order, pad=3))
