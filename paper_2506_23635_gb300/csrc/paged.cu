@@ -529,13 +529,15 @@ cudaError_t launch_append(const QkvRows &rows, int in, const moe_sa_dims &d,
     // small groups where the tokens may all be starts; a page's worth of tokens
     // holds one or two otherwise
     int gs = T <= kAppMaxGroup ? kAppHalves : std::max(kAppHalves, (int)pd.page_size);
-    // several rows a block where there are blocks enough: what a block finds out of its
-    // pages is half of its time (12,000 tokens, pages of 128: 92.5 us with one row,
-    // 87.5 with four)
+    // several rows a block, up to four, where there are blocks enough, one for each SM:
+    // what a block finds out of its pages is half of its time (12,000 tokens, pages of
+    // 128: one row 92.5 us, four 87.2, eight 99; 2048 tokens, pages of 64: one row 18.1
+    // us, two 16.4, four, 128 blocks, 19.6; 529 tokens: one row 9.2, two, 136 blocks,
+    // 13.8)
     const int groups = (T + gs - 1) / gs;
     int per = 1;
     while (per < 4 && 2 * Hkv % (2 * per) == 0 &&
-           (long long)groups * 2 * Hkv / (2 * per) >= 2 * device_info().sm_count)
+           (long long)groups * 2 * Hkv / (2 * per) >= device_info().sm_count)
         per *= 2;
     int n_kb = groups * (2 * Hkv / per);
     const void *kern = per > 1 ? append_kernel<true>(in, pd.page_size)
