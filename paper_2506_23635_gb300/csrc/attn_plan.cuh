@@ -26,9 +26,10 @@ struct PlanArgs {
 // done before the projection after them ends.
 constexpr int kPlanBins = 256;
 
+// Returns the number of tokens left, in every thread.
 template <int NT, int MIN_ROWS = kAttnTileMinRows>
-__device__ void plan_attention(int T, const PlanArgs &a) {
-    static_assert(NT >= kPlanBins && NT % 32 == 0, "a thread for each bin");
+__device__ int plan_attention(int T, const PlanArgs &a) {
+    static_assert(NT >= kPlanBins && NT % 32 == 0 && NT <= 1024, "a thread for each bin, a lane a warp");
     __shared__ uint32_t brk[kMaxSaTokens / 32];  // bit t: a run starts at token t
     __shared__ int last[kMaxSaTokens / 32];      // the last run start ahead of each word
     __shared__ int bins[kPlanBins];
@@ -94,27 +95,33 @@ __device__ void plan_attention(int T, const PlanArgs &a) {
         if (lane == 0) wsum[warp] = __popc(m);
         __syncthreads();
         int at = n_left + __popc(m & ((1u << lane) - 1u));
-        for (int w = 0; w < NT / 32; ++w) {
-            at += w < warp ? wsum[w] : 0;
-            n_left += wsum[w];
-        }
+        const int c = lane < NT / 32 ? wsum[lane] : 0;
+        at += __reduce_add_sync(0xffffffffu, lane < warp ? c : 0);
+        n_left += __reduce_add_sync(0xffffffffu, c);
         if (left) a.plan.left[at] = t;
         __syncthreads();
     }
-    if (warp == 0) {  // bins -> first place of each
-        int run = 0;
-        for (int b0 = 0; b0 < kPlanBins; b0 += 32) {
-            const int c = bins[b0 + lane];
-            int v = c;
+    if (warp == 0) {  // bins -> first place of each, a lane a few in a row
+        constexpr int B = kPlanBins / 32;
+        int c[B], v = 0;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int u = __shfl_up_sync(0xffffffffu, v, o);
-                if (lane >= o) v += u;
-            }
-            bins[b0 + lane] = run + v - c;
-            run += __shfl_sync(0xffffffffu, v, 31);
+        for (int b = 0; b < B; ++b) {
+            c[b] = bins[lane * B + b];
+            v += c[b];
         }
-        if (lane == 0) *a.plan.head = AttnPlanHead{run, n_left, 0, 0};
+        const int mine = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v += u;
+        }
+        if (lane == 31) *a.plan.head = AttnPlanHead{v, n_left, 0, 0};
+        v -= mine;
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            bins[lane * B + b] = v;
+            v += c[b];
+        }
     }
     __syncthreads();
     for (int t = tid; t < T; t += NT) {
@@ -124,6 +131,7 @@ __device__ void plan_attention(int T, const PlanArgs &a) {
             a.plan.tiles[atomicAdd(&bins[bin_of(ts, rows)], 1)] =
                 make_int4(ts, rows, a.pos[ts], a.seq[ts]);
     }
+    return n_left;
 }
 
 }  // namespace moe

@@ -567,9 +567,8 @@ k_paged_plan(int T, const PageView pv, const int32_t *__restrict__ seq,
         for (int i = tid; i < 2 * kPagedUnitParts; i += kPlanThreads) unit_count[i] = 0;
     int n = T;
     if (pa.plan.head) {  // only those that no tile holds
-        plan_attention<kPlanThreads, kPagedTileMinRows>(T, pa);
+        n = plan_attention<kPlanThreads, kPagedTileMinRows>(T, pa);
         __syncthreads();
-        n = pa.plan.head->n_left;
     }
     long long run = 0;
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
