@@ -390,6 +390,12 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     // complete; a small call waits for it only before it counts.  The prefill
     // attention starts after the plan is complete, and lets this one start then)
     const bool small = a.T > 0;
+    // (nothing listed beside the prefill's tiles: 2000 tokens of 16 heads 40.9 us, 40.3
+    // so)
+    if (a.ahead == kPagedAheadPrefill && __ldcg(a.list.n_list) == 0) {
+        if (cta == n_cta - 1) ptx::grid_dependency_wait();
+        return;
+    }
     if (threadIdx.x == 0) {
         for (int b = 0; b < kPdStages; ++b) {
             ptx::mbar_init(&hd->k_full[b], 1);
