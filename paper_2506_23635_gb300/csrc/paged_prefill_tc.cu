@@ -126,6 +126,18 @@ __device__ __forceinline__ float pf_exp2(float x) {
     return y;
 }
 
+// Barrier over head x's softmax threads that also tells whether any of them had p.
+__device__ __forceinline__ bool pf_any(int x, bool p) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)p), "r"(1 + x)
+        : "memory");
+    return r != 0;
+}
+
 __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -696,10 +708,7 @@ __device__ __noinline__ void pf_part(const PfArgs &a, PfHeader *hd, const PfUnit
     }
     if (pf_any_nan(hd)) pf_show_nan(a, hd, u, r, mine + r, kPfRows);
     reinterpret_cast<float2 *>(mine + 128 * kPfRows)[r] = make_float2(m, l);
-    auto meet = [&]() {  // the head's threads
-        if (x == 0) ptx::named_bar_sync(1, 128);
-        else ptx::named_bar_sync(2, 128);
-    };
+    auto meet = [&]() { pf_any(x, false); };  // the head's threads
     meet();
     if (r == 0) {
         __threadfence();
@@ -884,6 +893,8 @@ k_paged_prefill_tc(const __grid_constant__ PfArgs a) {
                 good = good && pf_wait_all(&hd->o_full[u.nh == 2 ? x : (u.n_kv - 1) & 1],
                                            (uint32_t)(u.nh == 2 ? u.n_kv - 1 : (u.n_kv - 1) >> 1) & 1u, err);
                 if (!good) hd->gave_up = 1;
+                // (the head's warps meet in pf_part: one that gave up, none goes there)
+                if (u.parts > 1 && pf_any(x, !good)) good = false;
                 if (good) tc_fence_after();
                 if (good && u.parts > 1) {
                     pf_part(a, hd, u, x, r, o_col, m, l);
