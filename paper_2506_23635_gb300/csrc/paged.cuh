@@ -109,10 +109,11 @@ inline bool paged_map(CUtensorMap *m, const void *base, const PagedAttn &a, bool
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Fewer consecutive tokens than this are attended one by one: a tile costs its
-// heads 2.4 us of an SM for each 128 positions whatever its rows, a token its
-// key/value heads 0.55 (DBRX's heads break even at 24).
-constexpr int kPagedTileMinRows = 24;
+// Fewer consecutive tokens than this are attended one by one: a tile costs the same
+// whatever its rows (24 chunks at position 2000, DBRX's heads: 151 us; one by one 196
+// for 16 tokens each, 244 for 20; four at position 3000: 55 and 61 for 16, so that 12
+// to 14 break even).
+constexpr int kPagedTileMinRows = 16;
 
 // Attention of the plan's tiles (paged_prefill_tc.cu).  part, count: where a unit
 // of work is shared by several CTAs; 2 counters a part, zero at the start.

@@ -1,7 +1,7 @@
 // Causal attention of prefill tiles over the paged 8-bit cache on the tcgen05
 // tensor cores.
 //
-// Tiles and units are those of attn_tc.cu: a tile is 24 to 128 consecutive
+// Tiles and units are those of attn_tc.cu: a tile is 16 to 128 consecutive
 // positions p0 .. p0 + rows - 1 of one sequence, a unit a (tile, pair of query
 // heads of one key/value head) over cache positions 0 .. p0 + rows - 1, taken by
 // one CTA an SM from a counter, longest first; the two heads share every key and
