@@ -89,7 +89,9 @@ typedef struct {
 } moe_dims;
 
 /* Bytes of workspace moe_layer_forward and moe_expert_ffn need for up to
- * max_tokens tokens (a multiple of 256).  Writes *bytes; MOE_ERR_INVALID_ARG
+ * max_tokens tokens (a multiple of 256).  This and the other
+ * moe_*_workspace_size never fall as max_tokens grows: a workspace takes every
+ * smaller call.  Writes *bytes; MOE_ERR_INVALID_ARG
  * for bad dims or max_tokens < 0. */
 moe_status moe_workspace_size(const moe_dims *dims, int32_t max_tokens,
                               size_t *bytes);
@@ -252,7 +254,8 @@ moe_status moe_stack_forward(const moe_dims *dims, int32_t n_layers, int32_t T,
  * scratch space is a fixed array of MOE_NOALLOC_SCRATCH_BYTES bytes in device
  * memory owned by the library.  Every GPU that loads this part of the
  * library holds that array until the process exits.
- *   - Limit: a call is accepted when moe_workspace_size(dims, T) is at most
+ *   - Limit: a call is accepted when what T tokens take (moe_workspace_size(dims,
+ *     T), or less where fewer tokens take more) is at most
  *     MOE_NOALLOC_SCRATCH_BYTES (24 MiB: the DBRX-shaped layer, D = 6144,
  *     F = 10752, E = 16, K = 4, fits at every T from 1 to 64, whose largest
  *     workspace is 20.25 MiB at T = 64); a larger workspace returns

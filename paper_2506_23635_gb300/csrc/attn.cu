@@ -645,15 +645,20 @@ k_residual_prenorm(int T, int D, int n_part, float *__restrict__ resid, const fl
 // ---- host ------------------------------------------------------------------------
 
 struct SaWs {
-    size_t offsets, xn, qkv, q, q16, plan_head, plan_tiles, plan_left, part_ml, part_acc,
-        dec_count, dec_part, ctx, total;
+    size_t offsets, xn, qkv, q16, ctx, q, plan_head, plan_tiles, plan_left, part_ml, part_acc,
+        dec_count, dec_part, total;
 };
 
-SaWs sa_ws(const moe_sa_dims &d, int64_t T) {
+// (paged: the block over the paged cache, whose attention has scratch of its own)
+SaWs sa_ws(const moe_sa_dims &d, int64_t T, bool paged = false) {
     auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
     const size_t nq = (size_t)d.n_heads * kHeadDim;
     const size_t nr = nq + 2 * (size_t)d.n_kv_heads * kHeadDim;
-    const size_t splits = (size_t)T * d.n_heads * split_cap((int)T, d.n_kv_heads);
+    // as many as any call of up to T tokens has: T Hq split_cap(T) falls wherever
+    // the cap does (48 / 8 heads: 256 tokens 24,576, 257 tokens 12,336)
+    const size_t splits =
+        std::min((size_t)T * d.n_heads * kMaxSplit,
+                 std::max((size_t)T * d.n_heads, (size_t)kMaxSplitCtas * (d.n_heads / d.n_kv_heads)));
     SaWs L{};
     size_t o = 0;
     L.offsets = o; o += up(2 * 4);
@@ -667,8 +672,11 @@ SaWs sa_ws(const moe_sa_dims &d, int64_t T) {
         std::max({(size_t)T, (size_t)kRowsMaxParts * std::min<int64_t>(T, kRowsMaxTokens),
                   (size_t)2 * std::min<int64_t>(T, kProjSplitMaxTokens)});
     L.qkv = o; o += up(part_rows * std::max(nr, (size_t)d.d_model) * 4);
-    L.q = o; o += up((size_t)T * nq * 4);
     L.q16 = o; o += up((size_t)T * nq * 2);
+    L.ctx = o; o += up((size_t)T * nq * 2);
+    L.total = o;
+    if (paged) return L;
+    L.q = o; o += up((size_t)T * nq * 4);
     L.plan_head = o; o += up(sizeof(AttnPlanHead));
     L.plan_tiles = o; o += up((size_t)(T / kAttnTileMinRows) * sizeof(int4));
     L.plan_left = o; o += up((size_t)T * 4);
@@ -676,7 +684,6 @@ SaWs sa_ws(const moe_sa_dims &d, int64_t T) {
     L.part_acc = o; o += up(splits * kHeadDim * 4);
     L.dec_count = o; o += up(kAttnDecodeCounts * 4);
     L.dec_part = o; o += up(kAttnDecodePartFloats * 4);
-    L.ctx = o; o += up((size_t)T * nq * 2);
     L.total = o;
     return L;
 }
@@ -1000,7 +1007,7 @@ moe_status paged_sa_impl(const moe_sa_dims *dims, const moe_paged_dims *paged, i
     size_t need = 0;
     if ((s = moe_paged_sa_workspace_size(dims, T, &need)) != MOE_OK) return s;
     if (!ws || !aligned16(ws) || ws_bytes < need) return MOE_ERR_WORKSPACE;
-    SaCall c{*dims, T, (cudaStream_t)stream, ws, sa_ws(*dims, T)};
+    SaCall c{*dims, T, (cudaStream_t)stream, ws, sa_ws(*dims, T, true)};
     if (!tc_path_ok(proj_dims(c.nr(), dims->d_model)) ||
         !tc_path_ok(proj_dims(dims->d_model, c.nq())))
         return MOE_ERR_UNSUPPORTED;
@@ -1019,6 +1026,20 @@ moe_status paged_sa_impl(const moe_sa_dims *dims, const moe_paged_dims *paged, i
                                 c.st);
     if (e == cudaSuccess) e = out_proj(c, ctx, w_o, resid, xn_next, eps);
     return cuda_status(e);
+}
+
+// Scratch of decoder layers whose attention block's is a.
+moe_status decoder_ws(const moe_sa_dims *attn, const moe_dims *moe_d, int32_t max_tokens, size_t a,
+                      size_t *bytes) {
+    size_t b = 0, c = 0;
+    moe_status s = moe_workspace_size(moe_d, max_tokens, &b);
+    if (s != MOE_OK) return s;
+    if ((s = moe_stack_workspace_size(moe_d, max_tokens, &c)) != MOE_OK) return s;
+    // the MoE block's normalised input, then the attention block's or the
+    // MoE layer's scratch (never live together)
+    const size_t xn = ((size_t)max_tokens * attn->d_model * 2 + 255) & ~size_t(255);
+    *bytes = std::max(xn + std::max(a, b), std::max(a, c));
+    return MOE_OK;
 }
 
 // Decoder layers in place on resid; block(l, scratch, its bytes, xn) is layer l's
@@ -1128,16 +1149,10 @@ moe_status moe_sa_forward(const moe_sa_dims *dims, int32_t T, const int32_t *seq
 moe_status moe_decoder_workspace_size(const moe_sa_dims *attn, const moe_dims *moe_d,
                                       int32_t max_tokens, size_t *bytes) {
     if (!bytes) return MOE_ERR_INVALID_ARG;
-    size_t a = 0, b = 0, c = 0;
+    size_t a = 0;
     moe_status s = moe_sa_workspace_size(attn, max_tokens, &a);
     if (s != MOE_OK) return s;
-    if ((s = moe_workspace_size(moe_d, max_tokens, &b)) != MOE_OK) return s;
-    if ((s = moe_stack_workspace_size(moe_d, max_tokens, &c)) != MOE_OK) return s;
-    // the MoE block's normalised input, then the attention block's or the
-    // MoE layer's scratch (never live together)
-    const size_t xn = ((size_t)max_tokens * attn->d_model * 2 + 255) & ~size_t(255);
-    *bytes = std::max(xn + std::max(a, b), std::max(a, c));
-    return MOE_OK;
+    return decoder_ws(attn, moe_d, max_tokens, a, bytes);
 }
 
 moe_status moe_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe_d, int32_t n_layers,
@@ -1169,12 +1184,11 @@ moe_status moe_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe_d, i
 }
 
 moe_status moe_paged_sa_workspace_size(const moe_sa_dims *dims, int32_t max_tokens, size_t *bytes) {
-    size_t a = 0, b = 0;
-    moe_status s = moe_sa_workspace_size(dims, max_tokens, &a);
+    size_t attn = 0;
+    moe_status s = moe_paged_workspace_size(dims, max_tokens, &attn);
     if (s != MOE_OK) return s;
-    if ((s = moe_paged_workspace_size(dims, max_tokens, &b)) != MOE_OK) return s;
     if (!bytes) return MOE_ERR_INVALID_ARG;
-    *bytes = a + b;
+    *bytes = sa_ws(*dims, max_tokens, true).total + attn;
     return MOE_OK;
 }
 
@@ -1190,15 +1204,11 @@ moe_status moe_paged_sa_forward(const moe_sa_dims *dims, const moe_paged_dims *p
 
 moe_status moe_paged_decoder_workspace_size(const moe_sa_dims *attn, const moe_dims *moe_d,
                                             int32_t max_tokens, size_t *bytes) {
-    size_t a = 0, d = 0, p = 0;
-    moe_status s = moe_decoder_workspace_size(attn, moe_d, max_tokens, &d);
-    if (s != MOE_OK) return s;
-    if ((s = moe_paged_sa_workspace_size(attn, max_tokens, &a)) != MOE_OK) return s;
     if (!bytes) return MOE_ERR_INVALID_ARG;
-    // (the attention block's scratch beside the MoE block's input)
-    p = ((size_t)max_tokens * attn->d_model * 2 + 255) & ~size_t(255);
-    *bytes = std::max(d, p + a);
-    return MOE_OK;
+    size_t a = 0;
+    moe_status s = moe_paged_sa_workspace_size(attn, max_tokens, &a);
+    if (s != MOE_OK) return s;
+    return decoder_ws(attn, moe_d, max_tokens, a, bytes);
 }
 
 moe_status moe_paged_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe_d,

@@ -56,6 +56,7 @@ extern "C" moe_status moe_layer_forward_noalloc(const moe_dims *dims, int32_t T,
     moe_status s = moe_workspace_size(dims, T < 0 ? 0 : T, &need);
     if (s != MOE_OK) return s;
     if (T < 0) return MOE_ERR_INVALID_ARG;
+    need = moe::ws_layout(*dims, T).total;  // (of just these tokens)
     if (need > (size_t)MOE_NOALLOC_SCRATCH_BYTES) return MOE_ERR_WORKSPACE;
     if (T == 0) return MOE_OK;
     // the same pointer rules as moe_layer_forward, checked here too so that a
