@@ -435,7 +435,7 @@ moe_status moe_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe, int
  *
  * Layouts: k_pages, v_pages [n_pages, Hkv, page_size, 128] e4m3 (a byte each);
  * k_scale, v_scale [n_pages, Hkv] float32, finite, 2^-100 or more (zero: the
- * page's numbers count as zeros); page_table [n_seq,
+ * page's numbers count as zeros, NaN among them); page_table [n_seq,
  * max_pages] int32: position p of sequence s lies in page page_table[s, p /
  * page_size], row p % page_size.  Entries that no position of a call needs may
  * hold anything.  A page may be in several sequences' tables while nothing is

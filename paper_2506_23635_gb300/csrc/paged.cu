@@ -137,8 +137,15 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[4], float inv) {
     return e4m3x2(y[0], y[1]) | e4m3x2(y[2], y[3]) << 16;
 }
 
+// The multiplier of a page's other rows; negative where they were zeros, NaN
+// among them, under a scale of zero.
+__device__ __forceinline__ float growth(float old, float scale) {
+    return old == 0.f ? -1.f : old / scale;
+}
+
 // Four stored numbers times ratio, rounded again.
 __device__ __forceinline__ uint32_t rescale(uint32_t v, float ratio) {
+    if (ratio < 0.f) return 0u;
     const float2 f0 = e4m3x2_to_float2(v & 0xffffu), f1 = e4m3x2_to_float2(v >> 16);
     return e4m3x2(f0.x * ratio, f0.y * ratio) | e4m3x2(f1.x * ratio, f1.y * ratio) << 16;
 }
@@ -384,7 +391,7 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
                 if (!fresh && scale != old) {
                     const int n = atomicAdd(&n_grown, 1);
                     grown_s[n] = s;
-                    ratio_s[n] = old / scale;
+                    ratio_s[n] = growth(old, scale);
                 }
             }
         }
@@ -476,7 +483,7 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
             const float need = scale_for(mx);
             const float scale = fresh ? need : fmaxf(old, need);
             const bool grown = !fresh && scale != old;
-            const float ratio = old / scale, inv = 1.f / scale;
+            const float ratio = growth(old, scale), inv = 1.f / scale;
 #pragma unroll
             for (int k = 0; k < R; ++k) {
                 uint8_t *row = rows + (size_t)(hw + k * kAppHalves) * kPagedDh;

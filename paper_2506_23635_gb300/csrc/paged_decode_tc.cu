@@ -43,7 +43,8 @@
 //               O^T is rescaled in tensor memory, a thread its dim's row); the
 //               four terms of its probabilities, 32 bytes, go to P_j, positions
 //               as rows (MN-major, 32-byte swizzle); rows of V_j that hold no
-//               position of the token are zeroed (0 x NaN is NaN);
+//               position of the token, or whose scale is zero, are zeroed (0 x NaN is
+//               NaN);
 //   warp 6      the next piece's queries, split into terms.
 //
 // Every wait is bounded (ptx.cuh); once one gives up the thread skips the later
@@ -91,14 +92,15 @@ constexpr uint32_t kPdColS = 0, kPdColO = 32;  // S^T twice 16 columns, O^T 32
 constexpr float kPdTop = 7.f, kPdSlack = 1.75f;
 constexpr float kPdNone = -1e30f;  // base of nothing
 
-enum : int { kPdFirst = 1, kPdLast = 2, kPdWhole = 4, kPdEnd = 8, kPdClip = 16 };
+enum : int { kPdFirst = 1, kPdLast = 2, kPdWhole = 4, kPdEnd = 8, kPdClear = 16 };
 
 struct PdDesc {
     int tile;     // -1: the share has ended
     int tg;       // token * Hkv + key/value head
     int n;        // positions the token attends to
     int flags;    // kPdFirst, kPdLast: of its piece; kPdWhole: the piece is the whole
-                  // (token, head); kPdEnd: of its share; kPdClip: some rows hold no position
+                  // (token, head); kPdEnd: of its share; kPdClear: some value rows count as
+                  // zeros (no position there, or a scale of zero)
     int b0, parts;  // not whole: the first share with a piece of it, and how many have one
     unsigned valid;  // bit i: page i of the tile holds positions
     int pad;
@@ -518,6 +520,8 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 ptx::tma_load_2d(smem + kPdOffV + st * kPdTile + lane * page_bytes, &tmV, 0, row,
                                  &hd->v_full[st], pol);
             PdDesc *d = &hd->desc[j % kPdRing];
+            // (asked for after the loads: the scales are long in coming)
+            const unsigned sound = __ballot_sync(0xffffffffu, pg >= 0 && vs != 0.f);
             if (lane < per) {
                 d->ks[lane] = ks;
                 d->vs[lane] = vs;
@@ -535,7 +539,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 d->valid = valid;
                 d->flags = (first ? kPdFirst : 0) | (last ? kPdLast : 0) | (whole ? kPdWhole : 0) |
                            (x == w.hi - 1 ? kPdEnd : 0) |
-                           (left < kPagedTile || (int)__popc(valid) < per ? kPdClip : 0);
+                           (left < kPagedTile || (int)__popc(sound) < per ? kPdClear : 0);
                 if (!whole && last) {
                     d->b0 = pd_owner(c.first, w.W, w.n_share);
                     d->parts = pd_owner(c.first + c.nt - 1, w.W, w.n_share) - d->b0 + 1;
@@ -635,8 +639,9 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 float f[4];
                 unpack_bf16x2(u[h].x, f[0], f[1]);
                 unpack_bf16x2(u[h].y, f[2], f[3]);
-                const float mx = fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3])));
-                const uint32_t mb = __reduce_max_sync(0xffffffffu, __float_as_uint(mx));
+                // (as integers: NaN is the largest)
+                const uint32_t m2 = __vmaxu2(u[h].x & 0x7fff7fffu, u[h].y & 0x7fff7fffu);
+                const uint32_t mb = __reduce_max_sync(0xffffffffu, max(m2 & 0xffffu, m2 >> 16)) << 16;
                 // 2^(7 - x) for a largest of 2^x to 2^(x+1) (x >= -119: what
                 // lies below does not count)
                 const int e = min(max((int)(mb >> 23), 8), 254);
@@ -658,8 +663,12 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 const uint32_t at = h * 128 + (((lane >> 2) ^ h) << 4) + (lane & 3) * 4;
                 *reinterpret_cast<uint32_t *>(qb + at) = w1;
                 *reinterpret_cast<uint32_t *>(qb + 1024 + at) = w2;
-                // log2(e) / sqrt(128)
-                if (lane == 0) hd->qs[b][h] = 0.12751743f * __uint_as_float((uint32_t)(e - 7) << 23);
+                // log2(e) / sqrt(128); NaN where the query is not finite, for keys under a
+                // scale of zero
+                if (lane == 0)
+                    hd->qs[b][h] = mb < 0x7f800000u
+                                       ? 0.12751743f * __uint_as_float((uint32_t)(e - 7) << 23)
+                                       : __uint_as_float(0x7fffffffu);
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -727,7 +736,9 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 if (lane == 0) ptx::mbar_arrive(&hd->s_empty[j & 1]);
 #pragma unroll
                 for (int h = 0; h < G; ++h) {
-                    s[h] = fmaf(v[8 + h], 0.0625f, v[h]) * (ks * qs[h]);
+                    // (keys under a scale of zero are zeros, whatever they hold)
+                    const float f = ks * qs[h];
+                    s[h] = ks == 0.f ? f : fmaf(v[8 + h], 0.0625f, v[h]) * f;
                     past = past || (live && s[h] + lv > base[h] + kPdSlack);
                 }
             }
@@ -800,13 +811,14 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 *reinterpret_cast<uint4 *>(pb + ((sw ^ 1u) << 4)) =
                     make_uint4(word[4], word[5], word[6], word[7]);
             }
-            if (flags & kPdClip) {
+            if (flags & kPdClear) {
                 good = good &&
                        pd_wait(&hd->v_full[j % kPdStages], (uint32_t)(j / kPdStages) & 1u, err);
                 unsigned char *vr = smem + kPdOffV + (j % kPdStages) * kPdTile + r * kPagedDh;
 #pragma unroll
                 for (int c = 0; c < kPagedDh; c += 16)
-                    if (!live) *reinterpret_cast<uint4 *>(vr + c) = make_uint4(0u, 0u, 0u, 0u);
+                    if (!live || vs == 0.f)
+                        *reinterpret_cast<uint4 *>(vr + c) = make_uint4(0u, 0u, 0u, 0u);
             }
             fence_proxy_async_smem();
             tc_fence_before();

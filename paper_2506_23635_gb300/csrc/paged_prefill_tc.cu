@@ -82,10 +82,10 @@ struct PfScales {
     // of 16 positions each: the key page's scale, log2 and reciprocal of the
     // value page's
     float ks[8], lv[8], iv[8];
-    // bit i: positions 16 i .. of a page inside the pool; and of one whose
+    // bit i: positions 16 i .. of a page inside the pool; and of one whose keys',
     // values' scale is not zero
-    unsigned ok, values;
-    int pad[6];
+    unsigned ok, keys, values;
+    int pad[5];
 };
 
 struct PfHeader {
@@ -267,17 +267,18 @@ __device__ __forceinline__ bool pf_fetch(const PfArgs &a, PfHeader *hd, unsigned
         }
         PfScales *s = &hd->sc[j % kPfRing];
         if (lane < 8) {
-            // (a value scale of zero leaves rows of zeros, whatever it counts for
-            // here)
+            // (a scale of zero leaves rows of zeros, whatever it counts for here)
             s->ks[lane] = ks;
             s->lv[lane] = log2f(fmaxf(vs, kPfLeast));
             s->iv[lane] = 1.f / fmaxf(vs, kPfLeast);
         }
         const unsigned ok = __ballot_sync(0xffffffffu, lane < 8 && mine >= 0);
-        const unsigned values = __ballot_sync(0xffffffffu, lane < 8 && mine >= 0 && vs != 0.f);
+        const unsigned with_keys = __ballot_sync(0xffffffffu, lane < 8 && mine >= 0 && ks != 0.f);
+        const unsigned with_values = __ballot_sync(0xffffffffu, lane < 8 && mine >= 0 && vs != 0.f);
         if (lane == 0) {
             s->ok = ok;
-            s->values = values;
+            s->keys = with_keys;
+            s->values = with_values;
         }
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&hd->t_full[j % kPfRing]);
@@ -364,8 +365,8 @@ __device__ __forceinline__ bool pf_decode(const PfArgs &a, PfHeader *hd, unsigne
             !pf_wait_all(raw_full, j & 1, a.err) ||
             !pf_wait_all(&empty[b], ((uint32_t)(j >> 1) & 1u) ^ 1u, a.err))
             return false;
-        // rows that hold no position are zeros, as are values under a scale of zero
-        const unsigned ok = keys ? hd->sc[j % kPfRing].ok : hd->sc[j % kPfRing].values;
+        // rows that hold no position are zeros, as are those under a scale of zero
+        const unsigned ok = keys ? hd->sc[j % kPfRing].keys : hd->sc[j % kPfRing].values;
         const int at = (u.j0 + j) * kPfRows;
         unsigned char *d = dst + b * kPfTile;
         auto rows = [&](auto check) {
