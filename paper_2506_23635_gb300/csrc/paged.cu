@@ -128,8 +128,28 @@ __device__ __forceinline__ void turn(float &a, float &b, float sn, float cs) {
     b = v * cs + u * sn;
 }
 
-// Four numbers x / scale, as they are stored.  (inv = 1 / scale: exact for the
-// powers of two that this kernel gives.)
+// A result y that was cut off, its last bit set where something was: rounded to a
+// few bits it gives what the exact result does (after a rounding to nearest it may
+// not).
+__device__ __forceinline__ float sticky(float y, bool inexact) {
+    return inexact ? __uint_as_float(__float_as_uint(y) | 1u) : y;
+}
+
+// All scales that this kernel gives are powers of two, division by which is exact as
+// a product; a caller's own cache may hold others, by which numbers are divided (q
+// the quotient cut off; x - q scale is exact; NaN and infinities give NaN).
+__device__ __forceinline__ bool power_of_two(float scale) {
+    return (__float_as_uint(scale) & 0x7fffffu) == 0;
+}
+__device__ __forceinline__ void divide(float (&x)[4], float scale) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float q = __fdiv_rz(x[e], scale);
+        x[e] = sticky(q, fmaf(-q, scale, x[e]) != 0.f);
+    }
+}
+
+// Four numbers x inv, as they are stored.
 __device__ __forceinline__ uint32_t quantise(const float (&x)[4], float inv) {
     float y[4];
 #pragma unroll
@@ -143,11 +163,16 @@ __device__ __forceinline__ float growth(float old, float scale) {
     return old == 0.f ? -1.f : old / scale;
 }
 
-// Four stored numbers times ratio, rounded again.
+// Four stored numbers times ratio, rounded again, once.
+__device__ __forceinline__ float times(float x, float ratio) {
+    const float y = __fmul_rz(x, ratio);
+    return sticky(y, fmaf(x, ratio, -y) != 0.f);
+}
 __device__ __forceinline__ uint32_t rescale(uint32_t v, float ratio) {
     if (ratio < 0.f) return 0u;
     const float2 f0 = e4m3x2_to_float2(v & 0xffffu), f1 = e4m3x2_to_float2(v >> 16);
-    return e4m3x2(f0.x * ratio, f0.y * ratio) | e4m3x2(f1.x * ratio, f1.y * ratio) << 16;
+    return e4m3x2(times(f0.x, ratio), times(f0.y, ratio)) |
+           e4m3x2(times(f1.x, ratio), times(f1.y, ratio)) << 16;
 }
 
 // Blocks [0, n_kb): keys and values, each a row (key or value head) of the pages
@@ -384,8 +409,14 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
             const bool fresh = (p & (PS - 1)) == 0;
             const float scale = fresh ? need : fmaxf(old, need);
             uint8_t *row = rows_of(pg) + (size_t)(p & (PS - 1)) * kPagedDh + i;
-            *reinterpret_cast<uint32_t *>(row) = quantise(a, 1.f / scale);
-            *reinterpret_cast<uint32_t *>(row + H2) = quantise(c, 1.f / scale);
+            float inv = 1.f / scale;
+            if (!power_of_two(scale)) {
+                divide(a, scale);
+                divide(c, scale);
+                inv = 1.f;
+            }
+            *reinterpret_cast<uint32_t *>(row) = quantise(a, inv);
+            *reinterpret_cast<uint32_t *>(row + H2) = quantise(c, inv);
             if (i == 0) {
                 scales[(size_t)pg * Hkv] = scale;
                 if (!fresh && scale != old) {
@@ -483,7 +514,16 @@ k_paged_append(const QkvRows x, int Hq, int Hkv, const PageView pv,
             const float need = scale_for(mx);
             const float scale = fresh ? need : fmaxf(old, need);
             const bool grown = !fresh && scale != old;
-            const float ratio = growth(old, scale), inv = 1.f / scale;
+            const float ratio = growth(old, scale);
+            float inv = 1.f / scale;
+            if (!power_of_two(scale)) {
+#pragma unroll
+                for (int k = 0; k < R; ++k) {
+                    divide(a[k], scale);
+                    divide(c[k], scale);
+                }
+                inv = 1.f;
+            }
 #pragma unroll
             for (int k = 0; k < R; ++k) {
                 uint8_t *row = rows + (size_t)(hw + k * kAppHalves) * kPagedDh;

@@ -97,3 +97,81 @@ def test_query_not_finite_over_zero_scales(n):
     nan = np.zeros((n, 6, 128), bool)
     nan[0, 1] = nan[n - 1, 4] = True
     np.testing.assert_array_equal(got, nan)
+
+
+# ---- earlier scales that are no powers of two ------------------------------------------
+
+
+def _near_ties(rng, scale, n):
+    """n numbers x whose x / scale lies within 2^-22 of the middle between two e4m3
+    numbers, on either side of it and on it (up to 224: need stays below a scale of
+    any mantissa)."""
+    pos = ref.E4M3[:119]
+    mid = ((pos[:-1] + pos[1:]) / 2)[8:]
+    assert mid[-1] < 224
+    x = (rng.choice(mid, n) * float(scale)).astype(np.float32)
+    step = rng.integers(-2, 3, n)
+    for _ in range(2):
+        x = np.where(step < 0, np.nextafter(x, np.float32(0)), np.where(step > 0, np.nextafter(x, np.float32(np.inf)), x))
+        step -= np.sign(step)
+    return x * rng.choice([-1.0, 1.0], n).astype(np.float32)
+
+
+@pytest.mark.parametrize("page,runs", [(16, [(i, 3 + i, 1) for i in range(8)]), (64, [(0, 5, 40), (1, 70, 9)]),
+                                       (128, [(0, 1, 127), (1, 130, 1)])], ids=["alone", "chunks", "page"])
+def test_append_rounds_the_quotient_once(page, runs):
+    """Values next to the middle of two e4m3 numbers under an old scale that stays:
+    x / scale, rounded once.  (float64: x / scale of 24-bit numbers is either that
+    middle, of five bits, or farther from it than 2^-30 of it, so it lies on its
+    right side.)"""
+    m = moe()
+    c = ref.call(4, 2, page, runs, seed=page + 62)
+    rng = np.random.default_rng(page)
+    c["vs"] = (rng.uniform(1.0, 2.0, c["vs"].shape) * 2.0 ** rng.integers(-4, 4, c["vs"].shape)).astype(np.float32)
+    c["vs"][:, 1] = 1.0  # (and one that is)
+    d = Dev(m, c)
+    T = len(c["seq"])
+    x = np.zeros((T, 8, 128), np.float32)
+    for t in range(T):
+        pg = ref.page_of(c, c["seq"][t], c["pos"][t])
+        for h in range(2):
+            x[t, 6 + h] = _near_ties(rng, c["vs"][pg, h], 128)
+    before = d.host()
+    m.paged_append(d.a, d.cache, torch.from_numpy(x.reshape(T, -1)).cuda(), d.seq, d.pos)
+    assert m.get_last_error() == 0
+    _, v, _, vs = d.host()
+    np.testing.assert_array_equal(vs, before[3])
+    for t in range(T):
+        pg, off = ref.page_of(c, c["seq"][t], c["pos"][t]), c["pos"][t] % page
+        want = ref.encode(x[t, 6:].astype(np.float64) / vs[pg].astype(np.float64)[:, None])
+        np.testing.assert_array_equal(v[pg, :, off], want, err_msg=f"token {t}")
+
+
+@pytest.mark.parametrize("tokens", [1, 5])
+def test_append_rounds_the_earlier_rows_once(tokens):
+    """A page that grows from a scale that is no power of two: its earlier numbers
+    times old / new, rounded once, for multipliers that put products next to the
+    middle of two e4m3 numbers."""
+    m = moe()
+    n = 96
+    c = ref.call(2, 1, 64, [(i, 20, tokens) for i in range(n)], seed=63)
+    rng = np.random.default_rng(64)
+    pos = ref.E4M3[:120]
+    mid, num = ((pos[:-1] + pos[1:]) / 2)[40:100], np.arange(9, 16, 2)
+    ratio = (rng.choice(mid, c["vs"].shape) / rng.choice(num, c["vs"].shape)).astype(np.float32)
+    frac = np.frexp(ratio)[0].astype(np.float32)  # [1/2, 1)
+    c["vs"][...] = frac * np.float32(2.0 ** -3)
+    d = Dev(m, c)
+    T = len(c["seq"])
+    x = np.zeros((T, 4, 128), np.float32)
+    x[:, 3, 0] = 448.0  # (need = 1)
+    before = d.host()
+    m.paged_append(d.a, d.cache, torch.from_numpy(x.reshape(T, -1)).cuda(), d.seq, d.pos)
+    assert m.get_last_error() == 0
+    _, v, _, vs = d.host()
+    for s in range(n):
+        pg = ref.page_of(c, s, 20)
+        assert vs[pg, 0] == 1.0
+        rest = [o for o in range(64) if not 20 <= o < 20 + tokens]
+        y = ref.decode(before[1][pg, 0, rest]) * float(before[3][pg, 0])  # (28 bits: exact)
+        np.testing.assert_array_equal(v[pg, 0, rest] & 0x7f, ref.encode(y) & 0x7f)
