@@ -71,13 +71,15 @@ struct SmemOnce {
 // The tokens that the decode attention takes one by one, made on the device
 // (k_paged_plan): list[i] is a token, before[i] the position tiles (of
 // kPagedTile positions; none for a token outside the table) of the list's tokens
-// ahead of it, entry n_list those of all.  count: counters of finished parts, two
+// ahead of it, entry n_list those of all.  released: n_list + 1, stored with release
+// semantics once all of it is (zero before): who acquires that sees the list and
+// whatever was complete ahead of the plan.  count: counters of finished parts, two
 // for each CTA, zero at the start.
 constexpr int kPagedSmall = 128;
 constexpr int kPagedTile = 128;
 constexpr int kPagedMaxCtas = 320;
 struct PagedList {
-    int *n_list;
+    int *n_list, *released;
     int *list;
     long long *before;
     int *count;
@@ -126,7 +128,7 @@ cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, fl
 // to kPagedSmall tokens, all taken one by one: the kernel lists them itself, and
 // only the counters are the plan's.  kPagedAheadPlan: k_paged_plan.
 // kPagedAheadPrefill: the prefill attention, whose results are not read here:
-// this kernel runs beside it, as that one leaves SMs.
+// this kernel runs beside it, as that one leaves SMs, on what the plan has released.
 enum : int { kPagedAheadZero = 0, kPagedAheadPlan = 1, kPagedAheadPrefill = 2 };
 cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, int ahead,
                                    cudaStream_t st);

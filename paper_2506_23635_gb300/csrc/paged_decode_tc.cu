@@ -162,6 +162,16 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint32_t a, uint32_t b, 
         : "memory");
 }
 
+__device__ __forceinline__ int pd_acquire(const int *p) {
+    int v;
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+// What has been acquired, for the TMA loads that follow.
+__device__ __forceinline__ void pd_fence_proxy_async() {
+    asm volatile("fence.proxy.async.global;" ::: "memory");
+}
+
 // A whole warp's wait: the answer is the same in every lane.
 __device__ __forceinline__ bool pd_wait(uint64_t *bar, uint32_t parity, unsigned *err) {
     return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, err));
@@ -388,15 +398,23 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     const int cta = (int)blockIdx.x, n_cta = (int)gridDim.x, Hkv = a.Hkv;
     unsigned *err = a.err;
     ptx::launch_dependents();
-    // (k_paged_plan lets this one start once all that is ahead of the call is
-    // complete; a small call waits for it only before it counts.  The prefill
-    // attention starts after the plan is complete, and lets this one start then)
     const bool small = a.T > 0;
-    // (nothing listed beside the prefill's tiles: 2000 tokens of 16 heads 40.9 us, 40.3
-    // so)
-    if (a.ahead == kPagedAheadPrefill && __ldcg(a.list.n_list) == 0) {
-        if (cta == n_cta - 1) ptx::grid_dependency_wait();
-        return;
+    // Beside the prefill attention: that one starts when the plan is complete and lets
+    // this one start then, so what the plan has released, its own list and all that
+    // was complete ahead of it, is acquired from it, not waited for (a wait for
+    // the prefill: 512 tokens at position 5000 beside 24 others 94 us, 117 so).
+    if (a.ahead == kPagedAheadPrefill) {
+        int n = pd_acquire(a.list.released) - 1;
+        if (n < 0) {
+            ptx::grid_dependency_wait();
+            n = __ldcg(a.list.n_list);
+        }
+        pd_fence_proxy_async();
+        // (nothing listed beside the tiles: 2000 tokens of 16 heads 40.9 us, 40.3 so)
+        if (n == 0) {
+            if (cta == n_cta - 1) ptx::grid_dependency_wait();
+            return;
+        }
     }
     if (threadIdx.x == 0) {
         for (int b = 0; b < kPdStages; ++b) {
@@ -420,6 +438,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         ptx::prefetch_tmap(&tmV);
     }
     if (warp == 1) tmem_alloc(&hd->tmem_base, kPdTmemCols);
+    if (a.ahead != kPagedAheadPrefill) ptx::grid_dependency_wait();
     if (warp == 2 && small) {
         // the tiles before each token; one outside the table has none
         constexpr int E = kPdSmall / 32;
@@ -451,7 +470,6 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (a.ahead == kPagedAheadPlan) ptx::grid_dependency_wait();
     const PdTokens tokens{a.list, hd, a.seq, a.pos, a.pv, a.T};
     const uint32_t tmem = hd->tmem_base;
     const uint32_t sbase = ptx::smem_u32(smem);
@@ -877,7 +895,6 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             // kPdGroup parts are counted and merged in groups of that many first
             // (200,001 positions of one head over 304 CTAs: 96 us, all parts by one
             // CTA, 22.7 so)
-            if (small) ptx::grid_dependency_wait();  // the counters are zero
 #pragma unroll 1
             for (int i = 0; i < 2; ++i) {
                 const int parts2 = i ? pend_parts1 : pend_parts0;
@@ -926,7 +943,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     // this grid is complete only after what is ahead: one CTA sees to it (the others
     // would keep their SMs from those that wait for one: 512 tokens at position
     // 5000 beside 24 of up to 2048 positions 144 us, 126 so)
-    if (a.ahead != kPagedAheadPlan && cta == n_cta - 1) ptx::grid_dependency_wait();
+    if (a.ahead == kPagedAheadPrefill && cta == n_cta - 1) ptx::grid_dependency_wait();
 }
 
 const void *pd_kernel(int G) {

@@ -175,3 +175,47 @@ def test_append_rounds_the_earlier_rows_once(tokens):
         rest = [o for o in range(64) if not 20 <= o < 20 + tokens]
         y = ref.decode(before[1][pg, 0, rest]) * float(before[3][pg, 0])  # (28 bits: exact)
         np.testing.assert_array_equal(v[pg, 0, rest] & 0x7f, ref.encode(y) & 0x7f)
+
+
+# ---- right behind what writes the inputs -------------------------------------------------
+
+
+@pytest.mark.parametrize("runs", ["one", "ends", "mixed", "two_chunks", "many"])
+def test_attend_right_behind_the_append(runs):
+    """Appends and attentions without a pause, on rows, queries and tables that the
+    kernels just ahead have written: the bits of calls that are waited for."""
+    m = moe()
+    c = ref.call(12, 2, 32, {**RUNS, **ATTEND}[runs], seed=66, pad=2)
+    T = len(c["seq"])
+    rows = [rows_for(c, "bf16")[0] for _ in range(6)]
+    ws = m.paged_alloc_workspace(Dev(m, c).a, T)
+
+    def run(wait):
+        d = Dev(m, c)
+        table, seq, pos = d.cache.page_table.clone(), d.seq.clone(), d.pos.clone()
+        x = torch.empty_like(rows[0])
+        outs = []
+        torch.cuda.synchronize()
+        for r in rows:
+            x.copy_(r)
+            d.cache.page_table.copy_(table)
+            d.seq.copy_(seq)
+            d.pos.copy_(pos)
+            if wait:
+                torch.cuda.synchronize()
+            q = m.paged_append(d.a, d.cache, x, d.seq, d.pos)
+            if wait:
+                torch.cuda.synchronize()
+            outs.append(m.paged_attend(d.a, d.cache, q, d.seq, d.pos, ws=ws))
+            if wait:
+                torch.cuda.synchronize()
+            d.cache.page_table.fill_(-1)
+            d.seq.fill_(-1)
+        torch.cuda.synchronize()
+        return outs
+
+    want = run(True)
+    for _ in range(3):
+        for a, b in zip(run(False), want):
+            assert torch.equal(a, b)
+    assert m.get_last_error() == 0
