@@ -596,35 +596,31 @@ cudaError_t launch_append(const QkvRows &rows, int in, const moe_sa_dims &d,
 }
 
 // The tokens that are attended one by one (in their order), the position tiles
-// ahead of each, and the decode attention's counters at zero.  One block.
+// ahead of each, and the attention's counters at zero; in a call that is not sorted
+// the decode attention's counters only.  One block.
 constexpr int kPlanThreads = 1024;
 
 __global__ void __launch_bounds__(kPlanThreads)
 k_paged_plan(int T, const PageView pv, const int32_t *__restrict__ seq,
              const int32_t *__restrict__ pos, const PagedList l, const PlanArgs pa,
-             int *unit_count, bool small) {
+             int *unit_count) {
     ptx::grid_dependency_wait();
     // (after the wait: ahead of it one token of 2048 positions takes 10.4 us, 9.8 so)
     ptx::launch_dependents();
     __shared__ long long sums[kPlanThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < 2 * kPagedMaxCtas; i += kPlanThreads) l.count[i] = 0;
-    if (small) return;
+    if (!pa.plan.head) return;
     if (tid == 0) *l.released = 0;
-    if (pa.plan.head)
-        for (int i = tid; i < 2 * kPagedUnitParts; i += kPlanThreads) unit_count[i] = 0;
-    int n = T;
-    if (pa.plan.head) {  // only those that no tile holds
-        n = plan_attention<kPlanThreads, kPagedTileMinRows>(T, pa);
-        __syncthreads();
-    }
+    for (int i = tid; i < 2 * kPagedUnitParts; i += kPlanThreads) unit_count[i] = 0;
+    const int n = plan_attention<kPlanThreads, kPagedTileMinRows>(T, pa);
+    __syncthreads();
     long long run = 0;
     for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
         const int i = i0 + tid;
         int nt = 0;
         if (i < n) {
-            const int t = pa.plan.head ? pa.plan.left[i] : i, p = pos[t];
-            if (!pa.plan.head) l.list[i] = t;
+            const int t = l.list[i], p = pos[t];  // (where the plan has put them)
             nt = pv.inside(seq[t], p) ? p / kPagedTile + 1 : 0;
         }
         long long v = nt;
@@ -704,30 +700,27 @@ cudaError_t attend(const PagedAttn &a, void *ws, cudaStream_t st) {
     PagedList l{at<int>(ws, L.n_list), at<int>(ws, L.n_list) + 1, at<int>(ws, L.list),
                 at<long long>(ws, L.before), at<int>(ws, L.count)};
     PlanArgs pa{a.seq, a.pos, a.pv.n_seq, a.pv.max_pages << a.pv.shift, {}};
-    bool small = a.T <= kPagedSmall && !planned(a.T, a.pv.n_seq);
-    if (planned(a.T, a.pv.n_seq))
+    static_assert(kAttnTile <= kPagedSmall, "a call that is not sorted needs no list");
+    const bool sorted = planned(a.T, a.pv.n_seq);
+    if (sorted)
         pa.plan = AttnPlan{at<AttnPlanHead>(ws, L.head), at<int4>(ws, L.tiles), l.list};
     {
         int T = a.T;
         PageView pv = a.pv;
         const int32_t *seq = a.seq, *pos = a.pos;
         int *unit_count = at<int>(ws, L.unit_count);
-        void *args[] = {&T, &pv, &seq, &pos, &l, &pa, &unit_count, &small};
+        void *args[] = {&T, &pv, &seq, &pos, &l, &pa, &unit_count};
         LaunchScope ls("paged_plan", st);
         cudaError_t e =
             launch_pdl((const void *)k_paged_plan, dim3(1), dim3(kPlanThreads), 0, st, args);
         if (e != cudaSuccess) return e;
     }
-    if (pa.plan.head) {
+    if (sorted) {
         cudaError_t e = launch_paged_prefill_tc(a, pa.plan, at<float>(ws, L.unit_part),
                                                 at<int>(ws, L.unit_count), st);
         if (e != cudaSuccess) return e;
     }
-    return launch_paged_decode_tc(a, l, at<float>(ws, L.part),
-                                  small            ? kPagedAheadZero
-                                  : pa.plan.head ? kPagedAheadPrefill
-                                                   : kPagedAheadPlan,
-                                  st);
+    return launch_paged_decode_tc(a, l, at<float>(ws, L.part), !sorted, st);
 }
 
 }  // namespace
@@ -754,7 +747,7 @@ moe_status check_paged_call(const moe_sa_dims *d, const moe_paged_dims *pd, int3
                             const void *kp, const void *vp, const float *ks, const float *vs) {
     moe_status s = check_paged(d, pd);
     if (s != MOE_OK) return s;
-    if (T < 0 || T > kPagedMaxTokens) return MOE_ERR_INVALID_ARG;
+    if (T < 0 || T > kMaxSaTokens) return MOE_ERR_INVALID_ARG;
     if (T > 0 && (!ok_ptr(seq) || !ok_ptr(pos) || !ok_ptr(table) || !ok_ptr(kp) || !ok_ptr(vp) ||
                   !ok_ptr(ks) || !ok_ptr(vs)))
         return MOE_ERR_INVALID_ARG;
@@ -803,7 +796,7 @@ moe_status moe_paged_workspace_size(const moe_sa_dims *dims, int32_t max_tokens,
     size_t n = 0;
     moe_status s = moe_sa_workspace_size(dims, 0, &n);
     if (s != MOE_OK) return s;
-    if (!bytes || max_tokens < 0 || max_tokens > kPagedMaxTokens) return MOE_ERR_INVALID_ARG;
+    if (!bytes || max_tokens < 0 || max_tokens > kMaxSaTokens) return MOE_ERR_INVALID_ARG;
     *bytes = paged_ws(max_tokens).total;
     return MOE_OK;
 }

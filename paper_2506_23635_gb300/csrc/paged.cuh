@@ -11,8 +11,6 @@ namespace moe {
 
 constexpr int kPagedDh = 128;        // head_dim
 constexpr int kPagedMaxGroup = 8;    // query heads per key/value head
-constexpr int kPagedMaxTokens = 65536;
-constexpr float kE4m3Max = 448.f;
 constexpr int kPagedMinExp = -100;   // scales are at least 2^-100
 
 // Where the positions of the sequences lie: page_table [n_seq, max_pages].
@@ -75,7 +73,7 @@ struct SmemOnce {
 // semantics once all of it is (zero before): who acquires that sees the list and
 // whatever was complete ahead of the plan.  count: counters of finished parts, two
 // for each CTA, zero at the start.
-constexpr int kPagedSmall = 128;
+constexpr int kPagedSmall = 128;  // tokens of a call that needs no list, at most
 constexpr int kPagedTile = 128;
 constexpr int kPagedMaxCtas = 320;
 struct PagedList {
@@ -123,14 +121,12 @@ constexpr int kPagedUnitParts = 160;  // one for each SM
 constexpr size_t kPagedUnitPartFloats = (size_t)kPagedUnitParts * 2 * 128 * (128 + 2);
 cudaError_t launch_paged_prefill_tc(const PagedAttn &a, const AttnPlan &plan, float *part,
                                     int *count, cudaStream_t st);
-// Attention of the listed tokens (paged_decode_tc.cu).
-// ahead: what the launch ahead is.  kPagedAheadZero: k_paged_plan for a call of up
-// to kPagedSmall tokens, all taken one by one: the kernel lists them itself, and
-// only the counters are the plan's.  kPagedAheadPlan: k_paged_plan.
-// kPagedAheadPrefill: the prefill attention, whose results are not read here:
-// this kernel runs beside it, as that one leaves SMs, on what the plan has released.
-enum : int { kPagedAheadZero = 0, kPagedAheadPlan = 1, kPagedAheadPrefill = 2 };
-cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, int ahead,
+// Attention of single tokens (paged_decode_tc.cu).  small: up to kPagedSmall tokens,
+// all taken one by one, right behind k_paged_plan: the kernel lists them itself, and only
+// the counters are the plan's.  Otherwise of the listed tokens, behind the prefill
+// attention, whose results are not read here: this kernel runs beside it, as that
+// one leaves SMs, on what the plan has released.
+cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, bool small,
                                    cudaStream_t st);
 
 

@@ -374,7 +374,6 @@ __device__ __forceinline__ void pd_merge(const float *part, Slot slot, int parts
 
 struct PdArgs {
     int T;  // tokens of a small call, all of them listed; 0: as the plan lists them
-    int ahead;
     int Hq, Hkv;
     PageView pv;
     PagedList list;
@@ -403,7 +402,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     // this one start then, so what the plan has released, its own list and all that
     // was complete ahead of it, is acquired from it, not waited for (a wait for
     // the prefill: 512 tokens at position 5000 beside 24 others 94 us, 117 so).
-    if (a.ahead == kPagedAheadPrefill) {
+    if (!small) {
         int n = pd_acquire(a.list.released) - 1;
         if (n < 0) {
             ptx::grid_dependency_wait();
@@ -438,7 +437,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         ptx::prefetch_tmap(&tmV);
     }
     if (warp == 1) tmem_alloc(&hd->tmem_base, kPdTmemCols);
-    if (a.ahead != kPagedAheadPrefill) ptx::grid_dependency_wait();
+    if (small) ptx::grid_dependency_wait();
     if (warp == 2 && small) {
         // the tiles before each token; one outside the table has none
         constexpr int E = kPdSmall / 32;
@@ -943,7 +942,7 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     // this grid is complete only after what is ahead: one CTA sees to it (the others
     // would keep their SMs from those that wait for one: 512 tokens at position
     // 5000 beside 24 of up to 2048 positions 144 us, 126 so)
-    if (a.ahead == kPagedAheadPrefill && cta == n_cta - 1) ptx::grid_dependency_wait();
+    if (!small && cta == n_cta - 1) ptx::grid_dependency_wait();
 }
 
 const void *pd_kernel(int G) {
@@ -961,7 +960,7 @@ const void *pd_kernel(int G) {
 
 }  // namespace
 
-cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, int ahead,
+cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float *part, bool small,
                                    cudaStream_t st) {
     const int G = a.Hq / a.Hkv;
     CUtensorMap mk, mv;
@@ -971,7 +970,7 @@ cudaError_t launch_paged_decode_tc(const PagedAttn &a, const PagedList &l, float
     static SmemOnce once[kPdMaxG];
     cudaError_t e = once[G - 1].set(kern, kPdSmem);
     if (e != cudaSuccess) return e;
-    PdArgs pa{ahead == kPagedAheadZero ? a.T : 0, ahead, a.Hq, a.Hkv, a.pv, l, a.seq, a.pos,
+    PdArgs pa{small ? a.T : 0, a.Hq, a.Hkv, a.pv, l, a.seq, a.pos,
               static_cast<const bf16 *>(a.q), a.ks, a.vs, static_cast<bf16 *>(a.ctx), part,
               device_info().err};
     void *args[] = {&mk, &mv, &pa};
