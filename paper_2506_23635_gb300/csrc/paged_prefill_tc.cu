@@ -282,14 +282,14 @@ __device__ __forceinline__ bool pf_fetch(const PfArgs &a, PfHeader *hd, unsigned
         }
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(&hd->t_full[j % kPfRing]);
-        if (!good) {
-            // (what was asked for lands before the block can exit)
-#pragma unroll
-            for (int v = 0; v < 2; ++v)
-                if (asked[v] > 0) pf_wait_all(&hd->raw_full[v], (uint32_t)(asked[v] - 1) & 1u, a.err);
-            break;
-        }
+        if (!good) break;
     }
+    // what was asked for lands before the block can exit, also where only the
+    // warps that decode it have given up
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+        if (asked[v] > 0)
+            good = pf_wait_all(&hd->raw_full[v], (uint32_t)(asked[v] - 1) & 1u, a.err) && good;
     return good;
 }
 
