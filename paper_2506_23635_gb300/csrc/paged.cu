@@ -28,7 +28,10 @@ namespace {
 // Rotary angles: pair i of position p turns by p base^(-2i/128) =
 // 2 pi (p r_i), r_i in turns as a 64-bit fixed-point fraction, so that p r_i
 // modulo one turn is a product of integers (no 64-bit floating point, of which
-// the SMs do little); its upper 32 bits are the angle to 2^-32 of a turn.
+// the SMs do little).  r_i comes from a power and a division of 53 bits, to 2^-54.6 of
+// a turn (base 500000: 2^-55.5), so the angle is off by p times that, by 2^-32 where
+// the product is cut to 32 bits and by 2^-26 where those become fp32: below 2^-24 of
+// a turn (2^-21.4 in radians) at the last position of all, 2^30.
 struct RopeTurns {
     uint64_t r[kPagedDh / 2];
 };

@@ -9,7 +9,7 @@
 //                     the group's (up to 8) query heads, 8 + h the second, 16
 //                     times as large; K = 128 dims.  A bf16 query scaled by a power
 //                     of two so that its row's largest is in [128, 256) is the sum
-//                     of its two terms but for 2^-22 of that largest.
+//                     of its two terms but for 2^-21 of that largest.
 //   O^T += V^T P^T    M = 128 dims, N = 32: columns 8 i + h the i-th term of head
 //                     h's probabilities, 16^i times as large; K = 128 positions; V
 //                     as it lies in the page (dims contiguous: an MN-major

@@ -1,5 +1,7 @@
 """The paged 8-bit cache at the edges of what its header allows.  Bounds as in
 tests/test_gpu_paged.py unless a test derives its own."""
+from decimal import Decimal, getcontext
+
 import numpy as np
 import pytest
 import torch
@@ -175,6 +177,58 @@ def test_append_rounds_the_earlier_rows_once(tokens):
         rest = [o for o in range(64) if not 20 <= o < 20 + tokens]
         y = ref.decode(before[1][pg, 0, rest]) * float(before[3][pg, 0])  # (28 bits: exact)
         np.testing.assert_array_equal(v[pg, 0, rest] & 0x7f, ref.encode(y) & 0x7f)
+
+
+# ---- far positions -------------------------------------------------------------------
+
+
+def _turns(base, pos):
+    """[positions, 64]: the angles' fractions of a turn, exact but for the last
+    rounding to float64."""
+    getcontext().prec = 60
+    two_pi = 2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494")
+    rate = [(-(Decimal(2 * i) / 128) * Decimal(base).ln()).exp() / two_pi for i in range(64)]
+    return np.array([[float((int(p) * r) % 1) for r in rate] for p in pos])
+
+
+@pytest.mark.parametrize("base", [10000.0, 500000.0])
+@pytest.mark.parametrize("first", [(1 << 20) - 20, (1 << 24) - 7, (1 << 27) + 3, (1 << 30) - 40])
+def test_append_at_far_positions(base, first):
+    """Queries and keys at positions up to the last one of the largest table.  Their
+    angles: 2^-55.5 of a turn a position (64 bits of the rate, of which the 53-bit
+    logarithm and division leave that), 2^-26 of a turn where the fraction becomes
+    fp32 and 2^-32 where it is cut; at 2^30 2^-25.5 + 2^-26 + 2^-32 of a turn,
+    2^-22.0 as an angle; sine and cosine 2^-23, the two products and their sum
+    2^-23: 2^-20.9 of the pair's magnitudes, 2^-20 allowed."""
+    m = moe()
+    page, n = 128, 40
+    pos = np.arange(first, first + n, dtype=np.int32)
+    table = torch.full((1, (1 << 30) // page), -1, dtype=torch.int32, device="cuda")
+    lo, hi = first // page, (first + n - 1) // page
+    for i in range(lo, hi + 1):
+        table[0, i] = i - lo
+    a = m.sa_dims(768, 2, 1, 128, base)
+    cache = m.PagedCache.alloc(a, page, 2, table)
+    g = torch.Generator().manual_seed(first)
+    x = torch.randn((n, 4 * 128), generator=g)
+    seq = torch.zeros(n, dtype=torch.int32, device="cuda")
+    q = m.paged_append(a, cache, x.cuda(), seq, torch.from_numpy(pos).cuda()).double().cpu().numpy()
+    assert m.get_last_error() == 0
+    xh = x.double().numpy().reshape(n, 4, 128)
+    w = 2 * np.pi * _turns(base, pos)[:, None, :]
+    lo_, hi_ = xh[:, :3, :64], xh[:, :3, 64:]
+    turned = np.concatenate([lo_ * np.cos(w) - hi_ * np.sin(w), hi_ * np.cos(w) + lo_ * np.sin(w)], -1)
+    mag = np.abs(lo_) + np.abs(hi_)
+    room = 2.0 ** -20 * np.concatenate([mag, mag], -1)
+    err = np.abs(q - turned[:, :2]) - (2.0 ** -8 * np.abs(turned[:, :2]) + room[:, :2])
+    assert np.max(err) <= 0, f"queries past their bound by {np.max(err):.3e}"
+    k, ks = cache.k_pages.view(torch.uint8).cpu().numpy(), cache.k_scale.cpu().numpy()
+    for t in range(n):
+        pg, off = pos[t] // page - lo, pos[t] % page
+        s = float(ks[pg, 0])
+        y = turned[t, 2] / s
+        lim = np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10) + room[t, 2] / s
+        assert np.all(np.abs(ref.decode(k[pg, 0, off]) - y) <= lim), t
 
 
 # ---- right behind what writes the inputs -------------------------------------------------
