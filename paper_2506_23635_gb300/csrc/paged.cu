@@ -664,6 +664,12 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 bool ok_ptr(const void *p) { return p != nullptr && aligned16(p); }
 moe_status cuda_status(cudaError_t e) { return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA; }
 
+// Whether a call's tokens are sorted into tiles and the rest: the plan and the
+// prefill attention's start cost 6 us and more beside tokens taken one by one (32
+// tokens at position 3000: 33.0 us sorted, 33.7 not, beside 24 others 52.8 and 44.0).
+constexpr int kPagedPlanTokens = 48;  // beyond one for each sequence
+bool planned(int T, int n_seq) { return T >= kAttnTile || T - n_seq >= kPagedPlanTokens; }
+
 // Workspace of moe_paged_attend.
 struct PagedWs {
     size_t n_list, count, list, before, head, tiles, unit_count, part, unit_part, total;
@@ -681,8 +687,8 @@ PagedWs paged_ws(int64_t T) {
     L.tiles = o; o += up((size_t)(T / kPagedTileMinRows) * sizeof(int4));
     L.unit_count = o; o += up(2 * kPagedUnitParts * 4);
     L.part = o; o += up(kPagedPartFloats * 4);
-    // (calls of fewer tokens hold no tile)
-    L.unit_part = o; o += T >= kPagedTileMinRows ? up(kPagedUnitPartFloats * 4) : 0;
+    // (a call of fewer tokens is not sorted, whatever its table)
+    L.unit_part = o; o += planned((int)T, 1) ? up(kPagedUnitPartFloats * 4) : 0;
     L.total = o;
     return L;
 }
@@ -691,12 +697,6 @@ template <typename P>
 P *at(void *ws, size_t off) {
     return reinterpret_cast<P *>(static_cast<char *>(ws) + off);
 }
-
-// Whether a call's tokens are sorted into tiles and the rest: the plan and the
-// prefill attention's start cost 6 us and more beside tokens taken one by one (32
-// tokens at position 3000: 33.0 us sorted, 33.7 not, beside 24 others 52.8 and 44.0).
-constexpr int kPagedPlanTokens = 48;  // beyond one for each sequence
-bool planned(int T, int n_seq) { return T >= kAttnTile || T - n_seq >= kPagedPlanTokens; }
 
 cudaError_t attend(const PagedAttn &a, void *ws, cudaStream_t st) {
     const PagedWs L = paged_ws(a.T);

@@ -52,3 +52,12 @@ def test_layer_sizes(lib, D, ffn, types):
     L, d = lib.lib(), lib.dims(D, *ffn, *types)
     for name in ("moe_workspace_size", "moe_stack_workspace_size", "moe_dense_workspace_size"):
         _never_falls(lambda T, n: getattr(L, name)(ctypes.byref(d), T, n), name)
+
+
+def test_small_paged_calls_have_no_scratch_for_tiles(lib):
+    """The parts of prefill units (20.3 MiB) are for calls that can be sorted into
+    tiles: those of 49 tokens or more (48 beyond a table of one row)."""
+    a = lib.sa_dims(6144, 48, 8)
+    parts = 160 * 2 * 128 * 130 * 4
+    assert lib.paged_workspace_size(a, 48) < 4 << 20
+    assert lib.paged_workspace_size(a, 49) >= parts
