@@ -452,7 +452,10 @@ moe_status moe_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe, int
  *
  * Limits: head_dim 128, up to 8 query heads per key/value head, T <= 65536 (as
  * moe_sa_*); page_size 16, 32, 64 or 128; n_pages Hkv page_size below
- * 2^31, max_pages page_size up to 2^30. */
+ * 2^31, max_pages page_size up to 2^30.  Where the value scales of a sequence's
+ * pages differ, by 2^k in a head, positions under the smaller ones whose weight
+ * is below 2^(k - 133) of the largest may count as zero in the attention's
+ * weights, and any of them beyond k = 120. */
 typedef struct {
     int32_t page_size; /* positions of a page */
     int32_t n_pages;   /* pages of the pool */

@@ -75,12 +75,15 @@ constexpr uint32_t kPfTmemCols = 512, kPfColS = 0, kPfColO = 256;
 constexpr float kPfTop = 7.f, kPfSlack = 8.f;
 constexpr float kPfNone = -1e30f;
 constexpr float kPfLeast = 7.888609052210118e-31f;  // 2^-100: nothing times a score
+// What row sums are multiplied with: a weight under a value scale of 2^-100 counts as
+// up to 2^115 there (2^15 where the base lags), and 2^29 of them stay in range so.
+constexpr float kPfSum = 7.62939453125e-6f;  // 2^-17
 constexpr int kPfMaxParts = 16, kPfMinTiles = 6;  // of a unit; of a part
 constexpr int kPfRing = 8;  // tiles' scales
 
 struct PfScales {
-    // of 16 positions each: the key page's scale, log2 and reciprocal of the
-    // value page's
+    // of 16 positions each: the key page's scale, log2 and reciprocal (times
+    // kPfSum) of the value page's
     float ks[8], lv[8], iv[8];
     // bit i: positions 16 i .. of a page inside the pool; and of one whose keys',
     // values' scale is not zero
@@ -270,7 +273,7 @@ __device__ __forceinline__ bool pf_fetch(const PfArgs &a, PfHeader *hd, unsigned
             // (a scale of zero leaves rows of zeros, whatever it counts for here)
             s->ks[lane] = ks;
             s->lv[lane] = log2f(fmaxf(vs, kPfLeast));
-            s->iv[lane] = 1.f / fmaxf(vs, kPfLeast);
+            s->iv[lane] = kPfSum / fmaxf(vs, kPfLeast);
         }
         const unsigned ok = __ballot_sync(0xffffffffu, lane < 8 && mine >= 0);
         const unsigned with_keys = __ballot_sync(0xffffffffu, lane < 8 && mine >= 0 && ks != 0.f);
@@ -531,7 +534,7 @@ __device__ __forceinline__ float pf_queries(const PfArgs &a, unsigned char *smem
 __device__ __forceinline__ void pf_store(const PfArgs &a, unsigned char *smem, const PfUnit &u,
                                          int x, int r, uint32_t o_col, float l) {
     const int lane = r & 31, r0 = r - lane;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = l == 0.f ? 0.f : kPfSum / l;
     unsigned char *s = smem + kPfOffQ + x * kPfTile;
 #pragma unroll
     for (int c = 0; c < 128; c += 32) {
@@ -730,7 +733,7 @@ __device__ __noinline__ void pf_part(const PfArgs &a, PfHeader *hd, const PfUnit
         for (int c = 0; c < kPfMaxParts; ++c)
             L = c < u.parts ? fmaf(pf_exp2(ml[c].x - M), ml[c].y, L) : L;
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;
+    const float inv = L == 0.f ? 0.f : kPfSum / L;
     bf16 *dst = a.ctx + ((size_t)(u.t0 + r) * a.Hq + u.h0 + x) * kPagedDh;
     // (64 columns' loads go out together: with eight 20 us for three parts)
 #pragma unroll 1

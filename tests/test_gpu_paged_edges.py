@@ -7,7 +7,8 @@ import pytest
 import torch
 
 from tests import paged_ref as ref
-from tests.test_gpu_paged import ATTEND, RUNS, Dev, check_append, moe, queries, rows_for
+from tests.test_gpu_paged import (ATTEND, RUNS, Dev, bf16, check_append, check_attend, moe, queries,
+                                  rows_for)
 
 pytestmark = pytest.mark.gpu
 
@@ -229,6 +230,52 @@ def test_append_at_far_positions(base, first):
         y = turned[t, 2] / s
         lim = np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10) + room[t, 2] / s
         assert np.all(np.abs(ref.decode(k[pg, 0, off]) - y) <= lim), t
+
+
+# ---- value scales far apart -------------------------------------------------------------
+
+
+@pytest.mark.parametrize("runs", ["ends", "mixed", "two_chunks", "far_chunks", "long"])
+@pytest.mark.parametrize("span", [(-100, 0), (-60, 40), (-10, 90)], ids=str)
+def test_attend_value_scales_far_apart(runs, span):
+    """Value pages of scales up to 2^100 apart in one sequence: a position counts in
+    the weights whatever its page's scale."""
+    m = moe()
+    c = ref.call(6, 2, 16, {**RUNS, **ATTEND}[runs], seed=65)
+    c["vs"][...] = 2.0 ** c["rng"].choice([span[0], span[0] + 1, span[1]], c["vs"].shape)
+    d = Dev(m, c)
+    q = queries(c, 1.0)
+    got = m.paged_attend(d.a, d.cache, q, d.seq, d.pos)
+    assert m.get_last_error() == 0
+    check_attend(c, d, q, got)
+
+
+@pytest.mark.parametrize("chunk,n_seq", [(1, 1), (1, 40), (140, 1), (17, 160)])
+def test_attend_after_many_zero_values(chunk, n_seq):
+    """16,384 positions of values that are all zeros, appended as such (scales of
+    2^-100), whose scores rise once by less than what moves the exponent's base; then
+    positions with values.  The sum of the weights stays in range.  (Several sequences
+    read the same pages, so that no CTA's work is cut along the positions.)"""
+    m = moe()
+    n = 16384
+    c = ref.call(1, 1, 128, [(0, n, chunk)], seed=67)
+    c["k"][...] = ref.encode(np.ones(128))
+    c["ks"][...] = 1.0
+    for p in range(0, n, 128):
+        pg = ref.page_of(c, 0, p)
+        c["v"][pg], c["vs"][pg] = 0, 2.0 ** -100
+    c["k"][ref.page_of(c, 0, 0)] = 0
+    w = 7.5 * np.log(2.0) / np.sqrt(128)
+    q = bf16(np.full((chunk, 1, 128), w)).cuda()
+    want, room = ref.attend(c, q.double().cpu().numpy(), c["k"], c["v"], c["ks"], c["vs"])
+    many = dict(c, seq=np.repeat(np.arange(n_seq, dtype=np.int32), chunk), pos=np.tile(c["pos"], n_seq),
+                table=np.tile(c["table"], (n_seq, 1)))
+    d = Dev(m, many)
+    got = m.paged_attend(d.a, d.cache, q.repeat(n_seq, 1, 1), d.seq, d.pos)
+    assert m.get_last_error() == 0
+    got = got.double().cpu().numpy().reshape(n_seq, chunk, 1, 128)
+    assert np.all(np.isfinite(got))
+    assert np.max(np.abs(got - want) - (2.0 ** -8 * np.abs(want) + 2.0 ** -10 * room)) <= 0
 
 
 # ---- right behind what writes the inputs -------------------------------------------------
