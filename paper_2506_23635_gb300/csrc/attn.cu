@@ -42,6 +42,7 @@
 #include <stdlib.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "attn_plan.cuh"
 #include "paged.cuh"
@@ -1042,6 +1043,14 @@ moe_status decoder_ws(const moe_sa_dims *attn, const moe_dims *moe_d, int32_t ma
     return MOE_OK;
 }
 
+// Every layer's pointers of each array, before any layer is launched.
+bool ok_layers(int32_t n_layers, std::initializer_list<const void *const *> arrays) {
+    for (const void *const *a : arrays)
+        for (int l = 0; l < n_layers; ++l)
+            if (!ok_ptr(a[l])) return false;
+    return true;
+}
+
 // Decoder layers in place on resid; block(l, scratch, its bytes, xn) is layer l's
 // attention block, which leaves the MoE block's input in xn if that is not null.
 template <typename Block>
@@ -1170,7 +1179,8 @@ moe_status moe_decoder_forward(const moe_sa_dims *attn, const moe_dims *moe_d, i
         moe_d->x_dtype != MOE_BF16 || moe_d->out_dtype != MOE_F32 || n_layers < 0)
         return MOE_ERR_INVALID_ARG;
     if (T == 0 || n_layers == 0) return MOE_OK;
-    if (!w_qkv || !w_o || !w_router || !w1 || !v1 || !w2 || !k_cache || !v_cache)
+    if (!w_qkv || !w_o || !w_router || !w1 || !v1 || !w2 || !k_cache || !v_cache ||
+        !ok_layers(n_layers, {w_qkv, w_o, w_router, w1, v1, w2, k_cache, v_cache}))
         return MOE_ERR_INVALID_ARG;
     size_t need = 0;
     if ((s = moe_decoder_workspace_size(attn, moe_d, T, &need)) != MOE_OK) return s;
@@ -1230,7 +1240,10 @@ moe_status moe_paged_decoder_forward(const moe_sa_dims *attn, const moe_dims *mo
         return MOE_ERR_INVALID_ARG;
     if (T == 0 || n_layers == 0) return MOE_OK;
     if (!ok_ptr(seq) || !ok_ptr(pos) || !ok_ptr(page_table) || !ok_ptr(resid) || !w_qkv || !w_o ||
-        !w_router || !w1 || !v1 || !w2 || !k_pages || !v_pages || !k_scale || !v_scale)
+        !w_router || !w1 || !v1 || !w2 || !k_pages || !v_pages || !k_scale || !v_scale ||
+        !ok_layers(n_layers, {w_qkv, w_o, w_router, w1, v1, w2, k_pages, v_pages,
+                              reinterpret_cast<const void *const *>(k_scale),
+                              reinterpret_cast<const void *const *>(v_scale)}))
         return MOE_ERR_INVALID_ARG;
     size_t need = 0;
     if ((s = moe_paged_decoder_workspace_size(attn, moe_d, T, &need)) != MOE_OK) return s;
