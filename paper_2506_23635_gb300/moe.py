@@ -505,6 +505,9 @@ def decoder_forward(a: SaDims, d: Dims, weights: DecoderWeights, resid, seq, pos
 # ---- paged key/value cache in 8 bits -----------------------------------------
 
 
+_tables_set = 0  # page tables given to any cache so far
+
+
 class PagedCache:
     """A paged e4m3 cache (include/moe.h, moe_paged_dims): ``k_pages`` and
     ``v_pages`` [n_pages, Hkv, page_size, 128] float8_e4m3fn, ``k_scale`` and
@@ -536,6 +539,8 @@ class PagedCache:
         if page_table.dim() != 2:
             raise ValueError("page_table must be [n_seq, max_pages]")
         _want(page_table, page_table.shape, torch.int32, self.device_index, "page_table")
+        global _tables_set
+        _tables_set += 1
         self._page_table = page_table
         self.dims = PagedDims(self.page_size, self.n_pages, *page_table.shape)
 
@@ -678,8 +683,9 @@ def paged_decoder_workspace_size(a: SaDims, d: Dims, max_tokens: int) -> int:
 class PagedDecoderWeights:
     """Device pointers of every decoder layer's tensors as C arrays: per layer
     (w_qkv, w_o, w_r, w1, v1, w2, cache), the caches PagedCaches of one shape.
-    The page table of a call is the first layer's.  The tensors must outlive
-    this object's use."""
+    The page table of a call is the first layer's cache's, whatever the others
+    have; one that was set on another layer's since, and not on the first's, is
+    refused.  The tensors must outlive this object's use."""
 
     def __init__(self, layers):
         n = len(layers)
@@ -690,6 +696,7 @@ class PagedDecoderWeights:
         if any(l[6].k_pages.shape != shape or l[6].device_index != self.cache.device_index
                for l in layers):
             raise ValueError("the layers' caches have one shape and one device")
+        self._tables, self._tables_at = [l[6]._page_table for l in layers], _tables_set
         arr = lambda ts: (ctypes.c_void_p * n)(*[ctypes.c_void_p(t.data_ptr()) for t in ts])
         (self.w_qkv, self.w_o, self.w_r, self.w1, self.v1,
          self.w2) = (arr([l[i] for l in layers]) for i in range(6))
@@ -697,12 +704,23 @@ class PagedDecoderWeights:
             arr([getattr(l[6], name) for l in layers])
             for name in ("k_pages", "v_pages", "k_scale", "v_scale"))
 
+    def _check_tables(self):
+        if self._tables_at == _tables_set:  # (no cache has been given one since)
+            return
+        first, now = self.cache._page_table, [l[6]._page_table for l in self.layers]
+        for i, (t, known) in enumerate(zip(now, self._tables)):
+            if t is not known and t is not first:
+                raise ValueError(f"layer {i}'s cache was given a page table that the first layer's was "
+                                 "not: a call's table is the first layer's")
+        self._tables, self._tables_at = now, _tables_set
+
 
 def paged_decoder_forward(a: SaDims, d: Dims, weights: PagedDecoderWeights, resid, seq, pos,
                           eps: float = STACK_EPS, ws=None, stream=None):
     """Every decoder layer in order, in place on resid (fp32 [T, D]), over paged
     caches: resid += W_o . Attn(RMSNorm0(resid)); resid += MoE(RMSNorm0(resid))."""
     W, c = weights, weights.cache
+    W._check_tables()
     T, dev = resid.shape[0], c.device_index
     _want(resid, (T, a.d_model), torch.float32, dev, "resid")
     if ws is not None:
