@@ -320,3 +320,23 @@ def test_attend_right_behind_the_append(runs):
         for a, b in zip(run(False), want):
             assert torch.equal(a, b)
     assert m.get_last_error() == 0
+
+
+# ---- tables with rows that a call does not use -----------------------------------------------
+
+
+@pytest.mark.parametrize("rows", [1, 64, 300])
+@pytest.mark.parametrize("n", [16, 48, 49, 100, 127, 128])
+def test_attend_a_chunk_in_a_table_with_idle_rows(n, rows):
+    """A chunk of one sequence, taken in tiles or token by token as the table's rows
+    decide, its sequence the table's last."""
+    m = moe()
+    c = ref.call(6, 2, 32, [(0, 700, n)], seed=68, pad=2)
+    c["table"] = np.concatenate([np.full((rows - 1, c["table"].shape[1]), 1 << 30, np.int32), c["table"]])
+    c["seq"] = np.where(c["seq"] == 0, rows - 1, -1).astype(np.int32)
+    d = Dev(m, c)
+    q = queries(c)
+    got = m.paged_attend(d.a, d.cache, q, d.seq, d.pos)
+    assert m.get_last_error() == 0
+    check_attend(c, d, q, got)
+    assert not got[n:].any()
