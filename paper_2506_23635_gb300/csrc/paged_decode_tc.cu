@@ -514,8 +514,9 @@ k_paged_decode_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             if (pg < 0 && lane < per && (lane << shift) < left) set_error(err, kErrIndex);
             float ks = 0.f, vs = 0.f;
             if (pg >= 0) {
-                ks = __ldg(a.ks + (size_t)pg * Hkv + c.g);
-                vs = __ldg(a.vs + (size_t)pg * Hkv + c.g);
+                // (not __ldg: its loads are outside of what an acquire orders)
+                ks = __ldcg(a.ks + (size_t)pg * Hkv + c.g);
+                vs = __ldcg(a.vs + (size_t)pg * Hkv + c.g);
             }
             const unsigned valid = __ballot_sync(0xffffffffu, pg >= 0);
             const uint32_t bytes = (uint32_t)__popc(valid) * page_bytes;
