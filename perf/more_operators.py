@@ -315,7 +315,7 @@ def _held(x):
 
 
 def _power(amax):
-    mant, e = torch.frexp(amax / TOP)
+    mant, e = torch.frexp(torch.clamp(amax / TOP, min=2.0 ** -101))
     return _two_to(torch.where(mant == 0.5, e - 1, e).clamp(min=-100))
 
 
