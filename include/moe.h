@@ -279,6 +279,113 @@ moe_status moe_layer_forward_noalloc(const moe_dims *dims, int32_t T,
                                      const void *w2, const void *residual_opt,
                                      void *out, moe_stream_t stream);
 
+/* ---- 8-bit experts ---------------------------------------------------------
+ * Numbers of 8 bits are e4m3 (4 exponent and 3 mantissa bits, largest 448; one byte
+ * each), with one float32 scale for each 128 numbers: of an activation row (x_scale
+ * [rows, ceil(cols/128)]), or for each 128 x 128 block of a weight matrix (w_scale [n,
+ * ceil(rows/128), ceil(cols/128)]).  A number stands for q * scale.  The last block of
+ * a row or a column may be smaller.  Half the weights' bytes of bf16, which is what
+ * bounds the layer in decode.
+ *
+ * The quantisers' scales are the smallest power of two s with max|block| <= 448 s,
+ * and at least 2^-100: q = e4m3(x / s), one rounding to nearest even.  A block with a
+ * value that is not finite: scale and numbers NaN.  The products take any scales.
+ *
+ * moe_quantize_rows: x [rows, cols] x_dtype -> q [rows, cols], scale.
+ * moe_quantize_blocks: w [n, rows, cols] w_dtype -> q [n, rows, cols], scale; n
+ *   matrices, as the experts of a weight tensor.
+ * Limits: cols a multiple of 16, 16 to 65536; rows <= 16777216 (of a matrix a multiple
+ * of 8, 8 to 65536); n <= 256. */
+moe_status moe_quantize_rows(int32_t rows, int32_t cols, const void *x,
+                             int32_t x_dtype, void *q, float *scale,
+                             moe_stream_t stream);
+moe_status moe_quantize_blocks(int32_t n, int32_t rows, int32_t cols,
+                               const void *w, int32_t w_dtype, void *q,
+                               float *scale, moe_stream_t stream);
+
+/* Grouped product of 8-bit rows and 8-bit matrices:
+ *   y[j, n] = sum_b x_scale[j, b] w_scale[g, n/128, b] (sum_{k in block b} x[j, k] w[g, n, k])
+ * for the rows j in [offsets[g], offsets[g + 1]) of each group g.
+ *   x [S, n_in] e4m3, x_scale; w [n_groups, n_out, n_in] e4m3, w_scale
+ *   offsets_opt [n_groups + 1] int32 (moe_dispatch's), or NULL with one group: all rows
+ *   y [S, n_out] y_dtype; rows outside every group are left as they were
+ *   ws  moe_quant_product_workspace_size bytes (for up to max_rows rows)
+ * fp32 sums, block by block.  Offsets that fall, or leave [0, S], are recorded as
+ * MOE_ERR_DEVICE_INDEX and their group is left out.  Limits: n_groups <= 256; n_out a
+ * multiple of 8, n_in of 16, both <= 65536; S <= 16777216. */
+moe_status moe_quant_product_workspace_size(int32_t n_groups, int32_t n_out,
+                                            int32_t n_in, int32_t max_rows,
+                                            size_t *bytes);
+moe_status moe_quant_product(int32_t n_groups, int32_t n_out, int32_t n_in,
+                             int32_t S, const void *x, const float *x_scale,
+                             const int32_t *offsets_opt, const void *w,
+                             const float *w_scale, void *y, int32_t y_dtype,
+                             void *ws, size_t ws_bytes, moe_stream_t stream);
+
+/* Choice of experts from router logits.
+ *   score  s = softmax(logits) or sigmoid(logits)
+ *   key    the logits, or s + bias where a bias is given (a bias that balances the
+ *          experts' load: it decides who is chosen, not the weight)
+ *   groups n_groups runs of E / n_groups consecutive experts; a group's value is its
+ *          largest key (group_top 1) or the sum of its two largest (group_top 2; of
+ *          scores where there is no bias); experts outside the top_groups groups of the
+ *          largest values are out
+ *   topk_idx   the K largest keys that are left, descending, ties to the lower index
+ *   topk_gate  s of those, divided by their sum if renormalise is 1, times scale
+ * The choice is that of 64-bit arithmetic on the given logits and bias.  A NaN key ranks
+ * below every number, so that K distinct experts come out whatever the logits; a softmax
+ * with a NaN or +inf logit, or without a finite one, gives NaN gates.
+ *   logits [T, E] float32; bias_opt [E] float32; topk_idx, topk_gate [T, K]
+ * Errors: MOE_ERR_INVALID_ARG, also where the kept groups have fewer than K experts. */
+typedef enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 } moe_score;
+typedef struct {
+    int32_t score;       /* moe_score */
+    int32_t n_groups;    /* divides E; 1: no groups */
+    int32_t top_groups;  /* groups that are kept */
+    int32_t group_top;   /* 1 or 2 */
+    int32_t renormalise; /* 0 or 1 */
+    float scale;
+} moe_router;
+moe_status moe_route_select(const moe_dims *dims, const moe_router *router,
+                            int32_t T, const float *logits,
+                            const float *bias_opt, int32_t *topk_idx,
+                            float *topk_gate, moe_stream_t stream);
+
+/* The experts' FFN over 8-bit weights, and the whole layer:
+ *   x8 = quantised rows of x;  h = SiLU(x8.w1[e]^T) * (x8.v1[e]^T);
+ *   h8 = quantised rows of h;  y = h8.w2[e]^T;  out = residual + sum_k gate y
+ * with fp32 sums and h in fp32 before its rounding to 8 bits.
+ * moe_quant_experts: w1, v1 [E, F, D], w2 [E, D, F] e4m3 and their scales (DEVICE
+ *   pointers; the struct itself is read during the call only).
+ * moe_quant_experts_forward: the experts of a choice that is made already (topk_idx,
+ *   topk_gate [T, K], from moe_route or moe_route_select; an index outside [0, E) is
+ *   recorded as MOE_ERR_DEVICE_INDEX and its slot left out).
+ * moe_quant_layer_forward: routing too: moe_route's with router_opt NULL (bias_opt is
+ *   then NULL), else moe_route_select on moe_route's logits.  w_router [D, E] w_dtype.
+ * Other arguments, residual and errors as moe_layer_forward's; d_model and ffn_hidden
+ * are multiples of 16; ws: moe_quant_workspace_size bytes for both. */
+typedef struct {
+    const void *w1, *v1, *w2;
+    const float *w1_scale, *v1_scale, *w2_scale;
+} moe_quant_experts;
+moe_status moe_quant_workspace_size(const moe_dims *dims, int32_t max_tokens,
+                                    size_t *bytes);
+moe_status moe_quant_experts_forward(const moe_dims *dims, int32_t T,
+                                     const void *x, const int32_t *topk_idx,
+                                     const float *topk_gate,
+                                     const moe_quant_experts *experts,
+                                     const void *residual_opt, void *out,
+                                     void *ws, size_t ws_bytes,
+                                     moe_stream_t stream);
+moe_status moe_quant_layer_forward(const moe_dims *dims,
+                                   const moe_router *router_opt, int32_t T,
+                                   const void *x, const void *w_router,
+                                   const float *bias_opt,
+                                   const moe_quant_experts *experts,
+                                   const void *residual_opt, void *out,
+                                   void *ws, size_t ws_bytes,
+                                   moe_stream_t stream);
+
 /* Human-readable name of a status. */
 const char *moe_status_string(moe_status status);
 

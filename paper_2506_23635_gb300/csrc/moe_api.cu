@@ -1277,20 +1277,15 @@ int *stream_ctr(const moe_dims &d, int T, const WsLayout &L, void *ws) {
     return T == 1 && small_route_ok(d, T) ? at<int>(ws, L.ctr) : nullptr;
 }
 
-// Routing and dispatch of the whole layer into the workspace regions of L:
-// the fused one-CTA or one-cluster kernels for decode batches, else the
-// router (on the tensor cores for large batches) and the dispatch kernel.
-cudaError_t route_dispatch_ws(const moe_dims &d, int T, const void *x, const void *w_router,
-                              const WsLayout &L, void *ws, cudaStream_t st) {
-    int32_t *idx = at<int32_t>(ws, L.idx);
-    float *gate = at<float>(ws, L.gate);
-    int32_t *counts = at<int32_t>(ws, L.counts);
-    int32_t *offsets = at<int32_t>(ws, L.offsets);
-    int32_t *perm = at<int32_t>(ws, L.perm);
-    int32_t *inv = at<int32_t>(ws, L.inv_perm);
+// Routing and dispatch of the whole layer: the fused one-CTA or one-cluster
+// kernels for decode batches, else the router (on the tensor cores for large
+// batches) and the dispatch kernel.
+cudaError_t route_dispatch_any(const moe_dims &d, int T, const void *x, const void *w_router,
+                               int32_t *idx, float *gate, int32_t *counts, int32_t *offsets,
+                               int32_t *perm, int32_t *inv, int *ctr, cudaStream_t st) {
     if (T == 1 && small_route_ok(d, T))
         return route_dispatch_small_any(d, T, x, w_router, idx, gate, counts, offsets, perm, inv,
-                                        st, stream_ctr(d, T, L, ws));
+                                        st, ctr);
     if (cluster_route_ok(d, T))
         return route_dispatch_cluster_any(d, T, x, w_router, idx, gate, counts, offsets, perm,
                                           inv, st);
@@ -1302,7 +1297,44 @@ cudaError_t route_dispatch_ws(const moe_dims &d, int T, const void *x, const voi
     return e;
 }
 
+// The same into the workspace regions of L.
+cudaError_t route_dispatch_ws(const moe_dims &d, int T, const void *x, const void *w_router,
+                              const WsLayout &L, void *ws, cudaStream_t st) {
+    return route_dispatch_any(d, T, x, w_router, at<int32_t>(ws, L.idx), at<float>(ws, L.gate),
+                              at<int32_t>(ws, L.counts), at<int32_t>(ws, L.offsets),
+                              at<int32_t>(ws, L.perm), at<int32_t>(ws, L.inv_perm),
+                              stream_ctr(d, T, L, ws), st);
+}
+
 }  // namespace
+
+namespace moe {
+
+moe_status check_layer_dims(const moe_dims *d) { return check_dims(d); }
+moe_status check_layer_tokens(const moe_dims *d, int32_t T) { return check_T(d, T); }
+cudaError_t launch_layer_route(const moe_dims &d, int T, const void *x, const void *w_router,
+                               float *logits, int32_t *idx, float *gate, cudaStream_t st) {
+    return route_any(d, T, x, w_router, logits, idx, gate, st);
+}
+cudaError_t launch_layer_route_dispatch(const moe_dims &d, int T, const void *x,
+                                        const void *w_router, int32_t *idx, float *gate,
+                                        int32_t *counts, int32_t *offsets, int32_t *perm,
+                                        int32_t *inv_perm, cudaStream_t st) {
+    return route_dispatch_any(d, T, x, w_router, idx, gate, counts, offsets, perm, inv_perm,
+                              nullptr, st);
+}
+cudaError_t launch_layer_dispatch(const moe_dims &d, int T, const int32_t *idx, int32_t *counts,
+                                  int32_t *offsets, int32_t *perm, int32_t *inv_perm,
+                                  cudaStream_t st) {
+    return dispatch_any(d, T, idx, counts, offsets, perm, inv_perm, st);
+}
+cudaError_t launch_layer_combine(const moe_dims &d, int T, const float *y, const int32_t *inv_perm,
+                                 const float *gate, const void *residual, void *out,
+                                 cudaStream_t st) {
+    return combine_any(d, T, y, inv_perm, gate, residual, out, st);
+}
+
+}  // namespace moe
 
 extern "C" {
 

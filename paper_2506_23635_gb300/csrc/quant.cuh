@@ -1,0 +1,106 @@
+// 8-bit experts: what their kernels share.  Numbers are e4m3; a scale (fp32) belongs to
+// each 128 numbers of an activation row and to each 128 x 128 block of a weight matrix.
+#pragma once
+
+#include <stdint.h>
+
+#include "paged.cuh"  // (e4m3 conversions, SmemOnce)
+#include "tc.cuh"
+
+namespace moe {
+
+constexpr int kQBlock = 128;    // numbers that share a scale, along a row
+constexpr int kQMinExp = -100;  // the quantisers' scales are at least 2^-100
+constexpr int kQMaxCtas = 160;  // of the streaming kernel, one for each SM
+
+__host__ __device__ inline int q_blocks(int n) { return (n + kQBlock - 1) / kQBlock; }
+
+// The scale of a block whose largest magnitude has these bits: the smallest power
+// of two that holds it (448 = 1.75 2^8), and its reciprocal; NaN where the block has a
+// value that is not finite.
+__device__ __forceinline__ void q_scale(uint32_t amax_bits, float &scale, float &inv) {
+    if (amax_bits >= 0x7f800000u) {
+        scale = inv = __uint_as_float(0x7fffffffu);
+        return;
+    }
+    const int e = max((int)(amax_bits >> 23) - 127 - 8 + ((amax_bits & 0x7fffffu) > 0x600000u ? 1 : 0),
+                      kQMinExp);
+    scale = __uint_as_float((uint32_t)(e + 127) << 23);
+    inv = __uint_as_float((uint32_t)(127 - e) << 23);
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Four values times inv (a power of two: exact but for numbers far below the
+// block's smallest e4m3) rounded to e4m3, the first in the low byte.
+__device__ __forceinline__ uint32_t q_pack4(float a, float b, float c, float d, float inv) {
+    return e4m3x2(a * inv, b * inv) | e4m3x2(c * inv, d * inv) << 16;
+}
+
+// A grouped product of 8-bit operands: rows x8 [S, n_in] in groups given by offsets
+// [E+1] (null: one group of S rows) times each group's matrix w8 [E, n_out, n_in].
+struct QuantGemm {
+    int E, S, n_in, n_out;
+    const int32_t *offsets;
+    const void *x8;
+    const float *xs;  // [S, q_blocks(n_in)]
+};
+
+// What the streaming kernel (quant_stream_tc.cu) needs beside its operands: slots
+// for tiles that several CTAs share, and a counter for each CTA, zero at the start.
+struct QuantParts {
+    float *part;
+    int *count;
+};
+// rows of x8 that a tile of it takes: every expert has at most `rows` of them
+inline int q_stream_cols(long long rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+inline size_t q_part_floats(int cols, bool up) {
+    return (size_t)2 * kQMaxCtas * 128 * cols * (up ? 2 : 1);
+}
+
+// up: h8, hs = quantised SiLU(x.w1) (x.v1); else y (fp32 or bf16) = x.w
+struct QuantUp {
+    const void *w1, *v1;
+    const float *s1, *sv;
+    void *h8;
+    float *hs;
+};
+struct QuantDown {
+    const void *w;
+    const float *s;
+    void *y;
+    int y_bf16;
+};
+cudaError_t launch_quant_stream_up(const QuantGemm &g, const QuantUp &u, const QuantParts &p,
+                                   int cols, cudaStream_t st);
+cudaError_t launch_quant_stream_down(const QuantGemm &g, const QuantDown &u, const QuantParts &p,
+                                     int cols, cudaStream_t st);
+
+// 8-bit weights [n, rows, cols]: boxes of 128 x 128, zeros outside each matrix.
+inline bool q_weight_map(CUtensorMap *m, const void *base, uint64_t n, uint64_t rows,
+                         uint64_t cols) {
+    auto fn = tc::encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {cols, rows, n};
+    cuuint64_t strides[2] = {cols, rows * cols};
+    cuuint32_t box[3] = {128u, 128u, 1u};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(base), dims, strides, box,
+              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// 8-bit rows [rows, cols]: boxes of box_rows x 128, zeros outside.
+inline bool q_row_map(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols,
+                      uint32_t box_rows) {
+    auto fn = tc::encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {cols, rows};
+    cuuint64_t strides[1] = {cols};
+    cuuint32_t box[2] = {128u, box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box,
+              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace moe

@@ -38,6 +38,9 @@ EXPORTS = (
     "moe_paged_workspace_size", "moe_paged_append", "moe_paged_attend",
     "moe_paged_sa_workspace_size", "moe_paged_sa_forward",
     "moe_paged_decoder_workspace_size", "moe_paged_decoder_forward",
+    "moe_quantize_rows", "moe_quantize_blocks", "moe_quant_product_workspace_size",
+    "moe_quant_product", "moe_route_select", "moe_quant_workspace_size",
+    "moe_quant_experts_forward", "moe_quant_layer_forward",
 )
 
 
@@ -79,6 +82,21 @@ class PagedDims(ctypes.Structure):
                 f"max={self.max_pages})")
 
 
+class Router(ctypes.Structure):
+    """moe_router: how experts are chosen from logits."""
+    _fields_ = [("score", ctypes.c_int32), ("n_groups", ctypes.c_int32),
+                ("top_groups", ctypes.c_int32), ("group_top", ctypes.c_int32),
+                ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+    def __repr__(self):
+        return (f"Router(score={self.score}, groups={self.n_groups}, top={self.top_groups}, "
+                f"group_top={self.group_top}, renormalise={self.renormalise}, scale={self.scale})")
+
+
+class _QuantExperts(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w1", "v1", "w2", "s1", "sv", "s2")]
+
+
 class KernelStat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 48), ("launches", ctypes.c_int64),
                 ("total_ms", ctypes.c_double)]
@@ -104,6 +122,7 @@ def lib() -> ctypes.CDLL:
     DP = ctypes.POINTER(Dims)
     SP = ctypes.POINTER(SaDims)
     GP = ctypes.POINTER(PagedDims)
+    RP, QP = ctypes.POINTER(Router), ctypes.POINTER(_QuantExperts)
     sigs = {
         "moe_workspace_size": [DP, I32, ctypes.POINTER(SZ)],
         "moe_route": [DP, I32, P, P, P, P, P, P],
@@ -141,6 +160,14 @@ def lib() -> ctypes.CDLL:
         "moe_paged_decoder_workspace_size": [SP, DP, I32, ctypes.POINTER(SZ)],
         "moe_paged_decoder_forward": [SP, DP, GP, I32, I32] + [P] * 4 + [ctypes.POINTER(P)] * 10
                                      + [ctypes.c_float, P, SZ, P],
+        "moe_quantize_rows": [I32, I32, P, I32, P, P, P],
+        "moe_quantize_blocks": [I32, I32, I32, P, I32, P, P, P],
+        "moe_quant_product_workspace_size": [I32, I32, I32, I32, ctypes.POINTER(SZ)],
+        "moe_quant_product": [I32] * 4 + [P] * 6 + [I32, P, SZ, P],
+        "moe_route_select": [DP, RP, I32, P, P, P, P, P],
+        "moe_quant_workspace_size": [DP, I32, ctypes.POINTER(SZ)],
+        "moe_quant_experts_forward": [DP, I32, P, P, P, QP, P, P, P, SZ, P],
+        "moe_quant_layer_forward": [DP, RP, I32, P, P, P, QP, P, P, P, SZ, P],
     }
     for name, args in sigs.items():
         fn = getattr(L, name)
@@ -734,3 +761,232 @@ def paged_decoder_forward(a: SaDims, d: Dims, weights: PagedDecoderWeights, resi
                                            W.k_scale, W.v_scale, eps, ws.data_ptr(), ws.numel(),
                                            st), "moe_paged_decoder_forward")
     return resid
+
+
+# ---- 8-bit experts --------------------------------------------------------------
+
+E4M3 = torch.float8_e4m3fn
+QUANT_BLOCK = 128  # numbers of a row that share a scale
+
+
+def _blocks(n: int) -> int:
+    return -(-n // QUANT_BLOCK)
+
+
+def _raw_stream(device: int, stream) -> int:
+    """The stream a call on ``device`` goes to: that device has to be the current one."""
+    if device < 0 or device != torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors are on device {device}, which is not the current one")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise ValueError(f"the stream is not of device {device}")
+    return stream.cuda_stream
+
+
+def _opt(t):
+    return None if t is None else t.data_ptr()
+
+
+def _quantize(x, scale_shape, q, scale, stream, name, sizes):
+    dev = x.get_device()
+    if x.dtype not in _DT:
+        raise ValueError("the numbers to quantise must be bf16 or fp32")
+    _want(x, x.shape, x.dtype, dev, "x")
+    if q is not None:
+        _want(q, x.shape, E4M3, dev, "q")
+    if scale is not None:
+        _want(scale, scale_shape, torch.float32, dev, "scale")
+    st = _raw_stream(dev, stream)
+    if q is None:
+        q = _new(x.shape, E4M3, x.device, stream)
+    if scale is None:
+        scale = _new(scale_shape, torch.float32, x.device, stream)
+    _check(getattr(lib(), name)(*sizes, x.data_ptr(), _DT[x.dtype], q.data_ptr(), scale.data_ptr(),
+                                st), name)
+    return q, scale
+
+
+def quantize_rows(x, q=None, scale=None, stream=None):
+    """e4m3 numbers and their scales [rows, ceil(cols/128)] (fp32 powers of two) of
+    x [rows, cols] (bf16 or fp32)."""
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, cols]")
+    rows, cols = x.shape
+    return _quantize(x, (rows, _blocks(cols)), q, scale, stream, "moe_quantize_rows", (rows, cols))
+
+
+def quantize_blocks(w, q=None, scale=None, stream=None):
+    """e4m3 numbers and their scales [n, ceil(rows/128), ceil(cols/128)] of n matrices
+    w [n, rows, cols] (bf16 or fp32), as an expert weight tensor holds them."""
+    if w.dim() != 3:
+        raise ValueError("w must be [n, rows, cols]")
+    n, rows, cols = w.shape
+    return _quantize(w, (n, _blocks(rows), _blocks(cols)), q, scale, stream, "moe_quantize_blocks",
+                     (n, rows, cols))
+
+
+def quant_product_workspace_size(n_groups: int, n_out: int, n_in: int, max_rows: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().moe_quant_product_workspace_size(n_groups, n_out, n_in, max_rows, ctypes.byref(n)),
+           "moe_quant_product_workspace_size")
+    return int(n.value)
+
+
+def quant_product_alloc_workspace(n_groups: int, n_out: int, n_in: int, max_rows: int,
+                                  device="cuda") -> torch.Tensor:
+    return torch.empty(quant_product_workspace_size(n_groups, n_out, n_in, max_rows),
+                       dtype=torch.uint8, device=device)
+
+
+def quant_product(x, x_scale, w, w_scale, offsets=None, out_dtype=torch.bfloat16, out=None, ws=None,
+                  stream=None):
+    """y [S, n_out] of 8-bit rows x [S, n_in] and matrices w [n_groups, n_out, n_in]: the
+    rows offsets[g]..offsets[g + 1] - 1 (int32 [n_groups + 1]) times matrix g; without
+    offsets one group of all rows.  Rows of ``out`` outside every group stay as they were
+    (of a result that this call allocates: undefined)."""
+    if x.dim() != 2 or w.dim() != 3:
+        raise ValueError("x must be [S, n_in] and w [n_groups, n_out, n_in]")
+    (S, n_in), (n, n_out, _), dev = x.shape, w.shape, w.get_device()
+    if out_dtype not in _DT:
+        raise ValueError("the result is bf16 or fp32")
+    _want(x, (S, n_in), E4M3, dev, "x")
+    _want(x_scale, (S, _blocks(n_in)), torch.float32, dev, "x_scale")
+    _want(w, (n, n_out, n_in), E4M3, dev, "w")
+    _want(w_scale, (n, _blocks(n_out), _blocks(n_in)), torch.float32, dev, "w_scale")
+    if offsets is not None:
+        _want(offsets, (n + 1,), torch.int32, dev, "offsets")
+    elif n != 1:
+        raise ValueError("several groups need offsets")
+    if out is not None:
+        _want(out, (S, n_out), out_dtype, dev, "out")
+    if ws is not None:
+        _want(ws, ws.shape, torch.uint8, dev, "ws")
+    st = _raw_stream(dev, stream)
+    if out is None:
+        out = _new((S, n_out), out_dtype, x.device, stream)
+    if ws is None:
+        ws = _new((quant_product_workspace_size(n, n_out, n_in, S),), torch.uint8, x.device, stream)
+    _check(lib().moe_quant_product(n, n_out, n_in, S, x.data_ptr(), x_scale.data_ptr(), _opt(offsets),
+                                   w.data_ptr(), w_scale.data_ptr(), out.data_ptr(), _DT[out_dtype],
+                                   ws.data_ptr(), ws.numel(), st), "moe_quant_product")
+    return out
+
+
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def router(score: str = "softmax", n_groups: int = 1, top_groups: int = 1, group_top: int = 1,
+           renormalise: bool = True, scale: float = 1.0) -> Router:
+    """How experts are chosen from logits (include/moe.h, moe_router)."""
+    if score not in _SCORES:
+        raise ValueError(f"score is one of {sorted(_SCORES)}")
+    return Router(_SCORES[score], n_groups, top_groups, group_top, int(bool(renormalise)), scale)
+
+
+def route_select(d: Dims, r: Router, logits, bias=None, idx=None, gate=None, stream=None):
+    """(topk_idx int32 [T, K], topk_gate fp32 [T, K]) of router logits [T, E] (fp32) and
+    a bias [E] (fp32) that takes part in the choice only."""
+    T, dev = logits.shape[0], logits.get_device()
+    _want(logits, (T, d.n_experts), torch.float32, dev, "logits")
+    if bias is not None:
+        _want(bias, (d.n_experts,), torch.float32, dev, "bias")
+    if idx is not None:
+        _want(idx, (T, d.top_k), torch.int32, dev, "idx")
+    if gate is not None:
+        _want(gate, (T, d.top_k), torch.float32, dev, "gate")
+    st = _raw_stream(dev, stream)
+    if idx is None:
+        idx = _new((T, d.top_k), torch.int32, logits.device, stream)
+    if gate is None:
+        gate = _new((T, d.top_k), torch.float32, logits.device, stream)
+    _check(lib().moe_route_select(d, r, T, logits.data_ptr(), _opt(bias), idx.data_ptr(),
+                                  gate.data_ptr(), st), "moe_route_select")
+    return idx, gate
+
+
+class QuantExperts:
+    """8-bit expert weights: w1, v1 [E, F, D], w2 [E, D, F] (float8_e4m3fn) and their scales
+    [E, ceil(rows/128), ceil(cols/128)] (fp32).  The tensors are the caller's; their
+    contents may change between calls."""
+
+    def __init__(self, w1, w1_scale, v1, v1_scale, w2, w2_scale):
+        if w1.dim() != 3:
+            raise ValueError("w1 must be [E, F, D]")
+        E, F, D = w1.shape
+        dev = self.device_index = w1.get_device()
+        for name, t, rows, cols in (("w1", w1, F, D), ("v1", v1, F, D), ("w2", w2, D, F)):
+            _want(t, (E, rows, cols), E4M3, dev, name)
+        for name, t, rows, cols in (("w1_scale", w1_scale, F, D), ("v1_scale", v1_scale, F, D),
+                                    ("w2_scale", w2_scale, D, F)):
+            _want(t, (E, _blocks(rows), _blocks(cols)), torch.float32, dev, name)
+        self.shape = (E, F, D)
+        self.tensors = (w1, v1, w2, w1_scale, v1_scale, w2_scale)
+        self.c = _QuantExperts(*[t.data_ptr() for t in self.tensors])
+
+    @staticmethod
+    def quantize(w1, v1, w2, stream=None) -> "QuantExperts":
+        """From bf16 or fp32 weights."""
+        (a, sa), (b, sb), (c, sc) = (quantize_blocks(t, stream=stream) for t in (w1, v1, w2))
+        return QuantExperts(a, sa, b, sb, c, sc)
+
+    def _call(self, d: Dims, x, residual, out, ws, stream):
+        """Checks a call's tensors against the weights; the stream it goes to, out and ws."""
+        if (d.n_experts, d.ffn_hidden, d.d_model) != self.shape:
+            raise ValueError(f"the weights are {self.shape} (E, F, D), the dims {d}")
+        T, dev = x.shape[0], self.device_index
+        _want(x, (T, d.d_model), _tdt(d.x_dtype), dev, "x")
+        for name, t in (("residual", residual), ("out", out)):
+            if t is not None:
+                _want(t, (T, d.d_model), _tdt(d.out_dtype), dev, name)
+        if ws is not None:
+            _want(ws, ws.shape, torch.uint8, dev, "ws")
+        st = _raw_stream(dev, stream)
+        if out is None:
+            out = _new((T, d.d_model), _tdt(d.out_dtype), x.device, stream)
+        if ws is None:
+            ws = _new((quant_workspace_size(d, T),), torch.uint8, x.device, stream)
+        return st, out, ws
+
+
+def quant_workspace_size(d: Dims, max_tokens: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().moe_quant_workspace_size(ctypes.byref(d), max_tokens, ctypes.byref(n)),
+           "moe_quant_workspace_size")
+    return int(n.value)
+
+
+def quant_alloc_workspace(d: Dims, max_tokens: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(quant_workspace_size(d, max_tokens), 256), dtype=torch.uint8, device=device)
+
+
+def quant_experts_forward(d: Dims, experts: QuantExperts, x, topk_idx, topk_gate, residual=None,
+                          out=None, ws=None, stream=None):
+    """The experts' part of the layer over 8-bit weights, for a choice that is made:
+    out [T, D] (out_dtype) = residual + sum_k gate[t, k] FFN_{idx[t, k]}(x[t])."""
+    T = x.shape[0]
+    _want(topk_idx, (T, d.top_k), torch.int32, experts.device_index, "topk_idx")
+    _want(topk_gate, (T, d.top_k), torch.float32, experts.device_index, "topk_gate")
+    st, out, ws = experts._call(d, x, residual, out, ws, stream)
+    _check(lib().moe_quant_experts_forward(d, T, x.data_ptr(), topk_idx.data_ptr(),
+                                           topk_gate.data_ptr(), experts.c, _opt(residual),
+                                           out.data_ptr(), ws.data_ptr(), ws.numel(), st),
+           "moe_quant_experts_forward")
+    return out
+
+
+def quant_layer_forward(d: Dims, experts: QuantExperts, x, w_r, router: Optional[Router] = None,
+                        bias=None, residual=None, out=None, ws=None, stream=None):
+    """The whole layer over 8-bit experts; returns out [T, D] (out_dtype).  Without a
+    ``router`` it chooses as ``route`` does, with one as ``route_select`` does."""
+    T, dev = x.shape[0], experts.device_index
+    _want(w_r, (d.d_model, d.n_experts), _tdt(d.w_dtype), dev, "w_r")
+    if bias is not None:
+        _want(bias, (d.n_experts,), torch.float32, dev, "bias")
+        if router is None:
+            raise ValueError("a bias needs a router")
+    st, out, ws = experts._call(d, x, residual, out, ws, stream)
+    _check(lib().moe_quant_layer_forward(d, router, T, x.data_ptr(), w_r.data_ptr(), _opt(bias),
+                                         experts.c, _opt(residual), out.data_ptr(), ws.data_ptr(),
+                                         ws.numel(), st), "moe_quant_layer_forward")
+    return out
