@@ -10,7 +10,8 @@ namespace {
 // ===========================================================================
 // Quantising rows: 16 lanes take a block of 128 numbers, eight each.  Bound by memory.
 // With K > 0 the rows are tokens, each written to the K sorted positions of its
-// slots (inv_perm; -1: left out), so that a token is read and quantised once.
+// slots (inv_perm; -1: left out), so that a token is read and quantised once, and
+// the scales block by block ([blocks, rows * K]), as the products read them.
 // ===========================================================================
 constexpr int kRowsThreads = 256;
 constexpr int kRowsUnroll = 4;
@@ -60,7 +61,7 @@ k_quant_rows(int rows, int cols, int K, const TX *__restrict__ x,
                 const int j = K > 0 ? inv_perm[(size_t)row * K + k] : row;
                 if (j < 0) continue;
                 if (c < cols) *reinterpret_cast<uint2 *>(q + (size_t)j * cols + c) = w;
-                if (sub == 0) scale[(size_t)j * nb + b] = sc;
+                if (sub == 0) scale[K > 0 ? (size_t)b * rows * K + j : (size_t)j * nb + b] = sc;
             }
         }
     }
@@ -110,10 +111,26 @@ k_quant_blocks(int rows, int cols, const TX *__restrict__ w, uint8_t *__restrict
     }
 }
 
-__global__ void k_quant_zero(int *count, int n) {
+// Ahead of a product: its rows' scales [S, nb] block by block, counters of zero.
+__global__ void __launch_bounds__(256)
+k_quant_scales(int S, int nb, const float *__restrict__ in, float *__restrict__ out, int *count,
+               int n_count) {
+    __shared__ float tile[32][33];
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
-    for (int i = threadIdx.x; i < n; i += blockDim.x) count[i] = 0;
+    if (blockIdx.x == 0 && blockIdx.y == 0)
+        for (int i = threadIdx.x; i < n_count; i += 256) count[i] = 0;
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, b0 = blockIdx.y * 32;
+    for (int s0 = blockIdx.x * 32; s0 < S; s0 += gridDim.x * 32) {
+#pragma unroll
+        for (int i = y; i < 32; i += 8)
+            if (s0 + i < S && b0 + x < nb) tile[i][x] = in[(size_t)(s0 + i) * nb + b0 + x];
+        __syncthreads();
+#pragma unroll
+        for (int i = y; i < 32; i += 8)
+            if (b0 + i < nb && s0 + x < S) out[(size_t)(b0 + i) * S + s0 + x] = tile[x][i];
+        __syncthreads();
+    }
 }
 
 // ===========================================================================
@@ -475,6 +492,9 @@ bool experts_ok(const moe_quant_experts *w) {
            q_aligned(w->v1_scale) && q_aligned(w->w2_scale);
 }
 
+// Rows enough for the CTA pairs.
+bool many_rows(int E, long long S) { return S >= 128LL * E; }
+
 // The experts' products of slots that are dispatched already, and their combine.
 cudaError_t quant_experts(const moe_dims &d, int T, const void *x, const moe_quant_experts &w,
                           const float *gate, const QuantLayout &L, void *ws, const void *residual,
@@ -490,16 +510,37 @@ cudaError_t quant_experts(const moe_dims &d, int T, const void *x, const moe_qua
     const QuantGemm gd{E, S, F, D, offsets, at<void>(ws, L.h8), at<float>(ws, L.hs)};
     const QuantDown down{w.w2, w.w2_scale, at<void>(ws, L.y), 0};
     const QuantParts pu{at<float>(ws, L.part), count}, pd{at<float>(ws, L.part), count + kQMaxCtas};
-    e = launch_quant_stream_up(gu, up, pu, L.cols, st);
-    if (e == cudaSuccess) e = launch_quant_stream_down(gd, down, pd, L.cols, st);
+    if (many_rows(E, S) && quant_pair_ok()) {
+        e = launch_quant_pair_up(gu, up, st);
+        if (e == cudaSuccess) e = launch_quant_pair_down(gd, down, st);
+    } else {
+        e = launch_quant_stream_up(gu, up, pu, L.cols, st);
+        if (e == cudaSuccess) e = launch_quant_stream_down(gd, down, pd, L.cols, st);
+    }
     if (e == cudaSuccess)
         e = launch_layer_combine(d, T, at<float>(ws, L.y), inv, gate, residual, out, st);
     return e;
 }
 
-size_t product_part_bytes(int cols) { return ((q_part_floats(cols, false) * 4) + 255) & ~size_t(255); }
 int product_cols(int E, int S) {
     return q_stream_cols(E == 1 ? S : std::min<long long>(S, 2LL * ((S + E - 1) / E)));
+}
+
+// Workspace of a product for up to S rows: scales, counters, parts.
+struct ProductLayout {
+    size_t xs, count, part, total;
+    int cols;
+};
+ProductLayout product_layout(int E, int n_in, int S) {
+    auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
+    ProductLayout L{};
+    L.cols = product_cols(E, S);
+    size_t o = 0;
+    L.xs = o; o += up((size_t)S * q_blocks(n_in) * 4);
+    L.count = o; o += up(kQMaxCtas * 4);
+    L.part = o; o += up(q_part_floats(L.cols, false) * 4);
+    L.total = o;
+    return L;
 }
 
 moe_status check_product(int32_t E, int32_t n_out, int32_t n_in, int32_t S) {
@@ -568,7 +609,7 @@ moe_status moe_quant_product_workspace_size(int32_t n_groups, int32_t n_out, int
     moe_status s = check_product(n_groups, n_out, n_in, max_rows);
     if (s != MOE_OK) return s;
     if (!bytes) return MOE_ERR_INVALID_ARG;
-    *bytes = product_part_bytes(product_cols(n_groups, max_rows)) + 1024;
+    *bytes = product_layout(n_groups, n_in, max_rows).total;
     return MOE_OK;
 }
 
@@ -583,21 +624,25 @@ moe_status moe_quant_product(int32_t n_groups, int32_t n_out, int32_t n_in, int3
     if (S == 0) return MOE_OK;
     if (!q_aligned(x) || !q_aligned(x_scale) || !q_aligned(w) || !q_aligned(w_scale) || !q_aligned(y))
         return MOE_ERR_INVALID_ARG;
-    const int cols = product_cols(n_groups, S);
-    const size_t part = product_part_bytes(cols);
-    if (!q_aligned(ws) || ws_bytes < part + 1024) return MOE_ERR_WORKSPACE;
+    const ProductLayout L = product_layout(n_groups, n_in, S);
+    if (!q_aligned(ws) || ws_bytes < L.total) return MOE_ERR_WORKSPACE;
     cudaStream_t st = (cudaStream_t)stream;
-    int *count = at<int>(ws, part);
+    int *count = at<int>(ws, L.count);
+    float *xs = at<float>(ws, L.xs);
     {
-        int n = kQMaxCtas;
-        void *args[] = {&count, &n};
-        LaunchScope ls("quant_zero", st);
-        cudaError_t e = launch_pdl((const void *)k_quant_zero, dim3(1), dim3(kQMaxCtas), 0, st, args);
-        if (e != cudaSuccess) return MOE_ERR_CUDA;
+        int nb = q_blocks(n_in), n = kQMaxCtas;
+        void *args[] = {&S, &nb, &x_scale, &xs, &count, &n};
+        LaunchScope ls("quant_scales", st);
+        if (launch_pdl((const void *)k_quant_scales,
+                       dim3(std::min((S + 31) / 32, 1024), (nb + 31) / 32), dim3(256), 0, st,
+                       args) != cudaSuccess)
+            return MOE_ERR_CUDA;
     }
-    const QuantGemm g{n_groups, S, n_in, n_out, offsets_opt, x, x_scale};
+    const QuantGemm g{n_groups, S, n_in, n_out, offsets_opt, x, xs};
     const QuantDown down{w, w_scale, y, y_dtype == MOE_BF16};
-    return q_status(launch_quant_stream_down(g, down, QuantParts{static_cast<float *>(ws), count}, cols,
+    if (many_rows(n_groups, S) && quant_pair_ok())
+        return q_status(launch_quant_pair_down(g, down, st));
+    return q_status(launch_quant_stream_down(g, down, QuantParts{at<float>(ws, L.part), count}, L.cols,
                                              st));
 }
 

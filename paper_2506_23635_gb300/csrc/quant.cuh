@@ -37,13 +37,53 @@ __device__ __forceinline__ uint32_t q_pack4(float a, float b, float c, float d, 
     return e4m3x2(a * inv, b * inv) | e4m3x2(c * inv, d * inv) << 16;
 }
 
+// 16 consecutive fp32 columns of this warp's 32 tensor-memory lanes.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+          "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// A wait that is over soon: the clock is looked at after 256 tries only.
+__device__ __forceinline__ bool wait_soon(uint64_t *bar, uint32_t parity, unsigned *err) {
+    uint64_t t0 = 0;
+    for (uint32_t it = 1;; ++it) {
+        if (ptx::mbar_try_wait(bar, parity)) return true;
+        if ((it & 255u) == 0) {
+            const uint64_t now = ptx::globaltimer();
+            if (t0 == 0) t0 = now;
+            if (now - t0 > ptx::kWaitLimitNs) {
+                set_error(err, kErrTimeout);
+                return false;
+            }
+        }
+    }
+}
+
+// One lane of the warp, always the same.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
+}
+
 // A grouped product of 8-bit operands: rows x8 [S, n_in] in groups given by offsets
 // [E+1] (null: one group of S rows) times each group's matrix w8 [E, n_out, n_in].
 struct QuantGemm {
     int E, S, n_in, n_out;
     const int32_t *offsets;
     const void *x8;
-    const float *xs;  // [S, q_blocks(n_in)]
+    const float *xs;  // [q_blocks(n_in), S]: the rows' scales of one k-block side by side
 };
 
 // What the streaming kernel (quant_stream_tc.cu) needs beside its operands: slots
@@ -63,7 +103,7 @@ struct QuantUp {
     const void *w1, *v1;
     const float *s1, *sv;
     void *h8;
-    float *hs;
+    float *hs;  // [q_blocks(n_out), S]
 };
 struct QuantDown {
     const void *w;
@@ -75,6 +115,12 @@ cudaError_t launch_quant_stream_up(const QuantGemm &g, const QuantUp &u, const Q
                                    int cols, cudaStream_t st);
 cudaError_t launch_quant_stream_down(const QuantGemm &g, const QuantDown &u, const QuantParts &p,
                                      int cols, cudaStream_t st);
+
+// The same for many rows a group, on CTA pairs (quant_pair_tc.cu), where the device
+// keeps such pairs resident.
+bool quant_pair_ok();
+cudaError_t launch_quant_pair_up(const QuantGemm &g, const QuantUp &u, cudaStream_t st);
+cudaError_t launch_quant_pair_down(const QuantGemm &g, const QuantDown &u, cudaStream_t st);
 
 // 8-bit weights [n, rows, cols]: boxes of 128 x 128, zeros outside each matrix.
 inline bool q_weight_map(CUtensorMap *m, const void *base, uint64_t n, uint64_t rows,

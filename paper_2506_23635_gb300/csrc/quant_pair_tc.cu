@@ -1,0 +1,458 @@
+// Grouped products of 8-bit operands for many rows a group: CTA pairs that share every
+// MMA (cta_group::2), 256 rows of x as its M, 256 weight rows as its N.
+//
+//   DOWN:  y[j, n] = sum_b xs[j, b] ws[e, n/128, b] (sum_{k in block b} x8[j, k] w8[e, n, k])
+//   UP:    a, b = the same with w1 and v1;  h = SiLU(a) b, quantised in blocks of 128
+//
+// Bound by the tensor cores.  A k-block of 128 is an accumulator of its own (two of 256
+// columns fill the tensor memory); eight epilogue warps take turns with the MMAs, which
+// write one accumulator while the other is multiplied with the block's scales and added to
+// the sums in registers.  The rows of x are the lanes, so that a thread needs one scale of
+// x and one or two of the weights for each k-block: with the weights as lanes every
+// column would need its own, 32 lanes reading the same word of shared memory.
+//
+// N: for UP 128 rows of W1 (loaded by the even CTA) and the same 128 of V1 (by the
+// odd one), for DOWN 256 rows of the weights.  Epilogue warp (q, half): lanes 32 q .. and
+// half of the columns (UP: 64 of a and the same 64 of b), 128 sums a thread.
+//
+// Units are (expert, weight tile, run of 256 rows), runs innermost, so that units that run
+// together share weight tiles in L2; pair p of P takes units p, p + P, ...
+#include "quant.cuh"
+
+namespace moe {
+namespace {
+
+using namespace tc;
+
+// warp 0 loads, warp 1 issues the MMAs, warps 4-11 are the epilogue.  Registers of the
+// launch: 168 a thread, 64,512; what the first four warps give up the others take:
+// 128 (72 + 2 * 216) = 64,512.
+constexpr int kQpThreads = 384;
+constexpr int kQpEpilogue = 4;  // first warp of it
+constexpr int kQpStages = 6;
+constexpr uint32_t kQpTile = 128 * 128;
+constexpr uint32_t kQpStage = 2 * kQpTile;  // of a CTA: 128 rows of x, 128 weight rows
+constexpr int kQpRows = 256;
+// kind::f8f6f4: e4m3 A and B, fp32 D, both K-major, M = 256, N = 256
+constexpr uint32_t kQpIdesc = (1u << 4) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
+
+struct QpHeader {
+    uint64_t full[kQpStages], empty[kQpStages];
+    uint64_t tfull[2], tempty[2];
+    uint64_t done;
+    uint32_t tmem_base;
+    int prefix[257];
+    uint32_t amax[2][2][128];  // (UP) of a row's 64 columns: tile in turn, half
+};
+constexpr uint32_t kQpHdrBytes = 6144;
+static_assert(sizeof(QpHeader) <= kQpHdrBytes, "header");
+constexpr size_t kQpSmem = 1024 + kQpStages * kQpStage + kQpHdrBytes;
+static_assert(kQpSmem <= 227 * 1024, "shared memory");
+
+__device__ __forceinline__ void mma_f8_pair(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc,
+                                            uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// Tensor copies that complete on the mbarrier at cluster address `bar`, the even CTA's.
+__device__ __forceinline__ void tma_2d_pair(void *dst, const CUtensorMap *m, int32_t x, int32_t y,
+                                            uint32_t bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        ".cta_group::2.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(ptx::smem_u32(dst)),
+        "l"(m), "r"(x), "r"(y), "r"(bar), "l"(policy)
+        : "memory");
+}
+__device__ __forceinline__ void tma_3d_pair(void *dst, const CUtensorMap *m, int32_t x, int32_t y,
+                                            int32_t z, uint32_t bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        ".cta_group::2.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(ptx::smem_u32(dst)),
+        "l"(m), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy)
+        : "memory");
+}
+
+// Arrive on an mbarrier of the even CTA.  No memory is handed over (only tensor memory,
+// whose reads have completed), so nothing of this thread's has to be seen at cluster
+// scope first: with a release there a k-block took 1.36 us instead of 0.75.
+__device__ __forceinline__ void arrive_remote(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// Two fp32 at once: acc += v * s.
+__device__ __forceinline__ void fma2(uint64_t &acc, float v0, float v1, uint64_t s) {
+    asm("{\n\t.reg .b64 v;\n\tmov.b64 v, {%1, %2};\n\tfma.rn.f32x2 %0, v, %3, %0;\n\t}"
+        : "+l"(acc)
+        : "f"(v0), "f"(v1), "l"(s));
+}
+__device__ __forceinline__ uint64_t twice(float s) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(s));
+    return r;
+}
+__device__ __forceinline__ float2 both(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+
+struct QpTile {
+    int e, wt;
+    int s0, cnt;  // first row, rows of the run (at most 256)
+};
+
+__device__ __forceinline__ QpTile qp_tile(const int *prefix, const int32_t *offsets, int E, int S,
+                                          int u) {
+    QpTile t;
+    t.e = chunk_expert(prefix, E, u);
+    const int lo = offsets ? offsets[t.e] : 0, hi = offsets ? offsets[t.e + 1] : S;
+    const int nst = (hi - lo + kQpRows - 1) / kQpRows, r = u - prefix[t.e];
+    t.wt = r / nst;
+    const int st = r - t.wt * nst;
+    t.s0 = lo + st * kQpRows;
+    t.cnt = min(kQpRows, hi - t.s0);
+    return t;
+}
+
+// prefix[e]: units of the experts ahead of e.
+__device__ void qp_prefix(const int32_t *offsets, int E, int S, int nwt, int *prefix,
+                          unsigned *err) {
+    const int lane = threadIdx.x & 31;
+    int run = 0;
+    for (int base = 0; base < E; base += 32) {
+        const int e = base + lane;
+        int c = 0;
+        if (e < E) {
+            const int lo = offsets ? offsets[e] : 0, hi = offsets ? offsets[e + 1] : S;
+            if (lo < 0 || hi < lo || hi > S) set_error(err, kErrIndex);
+            else c = ((hi - lo + kQpRows - 1) / kQpRows) * nwt;
+        }
+        int incl = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (e < E) prefix[e] = run + incl - c;
+        run += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) prefix[E] = run;
+}
+
+struct QpArgs {
+    const int32_t *offsets;
+    int E, S, n_in, n_out;
+    const float *xs, *s0, *s1;  // scales of x [blocks, S], of w1 (or w), of v1
+    void *out;                  // h8 or y
+    float *out_scale;           // hs [blocks, S]
+    int y_bf16;
+    unsigned *err;
+};
+
+template <bool UP>
+__global__ void __launch_bounds__(kQpThreads, 1)
+k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ CUtensorMap tm_w1,
+             const __grid_constant__ CUtensorMap tm_x, const QpArgs a) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *smem = reinterpret_cast<unsigned char *>(
+        (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    QpHeader *hd = reinterpret_cast<QpHeader *>(smem + kQpStages * kQpStage);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = ptx::cluster_ctarank();
+    const bool even = rank == 0;
+    const int nk = q_blocks(a.n_in), nblk = q_blocks(a.n_out);
+    const int nwt = UP ? nblk : (nblk + 1) / 2;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kQpStages; ++s) {
+            ptx::mbar_init(&hd->full[s], 1);
+            ptx::mbar_init(&hd->empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            ptx::mbar_init(&hd->tfull[b], 1);
+            ptx::mbar_init(&hd->tempty[b], 16);
+        }
+        ptx::mbar_init(&hd->done, 1);
+        ptx::fence_barrier_init();
+        ptx::prefetch_tmap(&tm_w0);
+        if (UP) ptx::prefetch_tmap(&tm_w1);
+        ptx::prefetch_tmap(&tm_x);
+    }
+    if (warp == 1) tmem_alloc_pair(&hd->tmem_base, 512);
+    ptx::launch_dependents();
+    ptx::grid_dependency_wait();
+    if (warp == kQpEpilogue) qp_prefix(a.offsets, a.E, a.S, nwt, hd->prefix, a.err);
+    tc_fence_before();
+    ptx::cluster_sync_all();  // barriers initialised in both CTAs
+    tc_fence_after();
+    const uint32_t tmem = hd->tmem_base;
+    const int n_units = hd->prefix[a.E], u0 = blockIdx.x >> 1, du = gridDim.x >> 1;
+
+    if (warp < kQpEpilogue) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == 0) {
+            // ------------------------------------------------------------ loads
+            if (lane == 0) {
+                // (normal priority: a weight tile serves the runs of its expert)
+                const uint64_t pol_w = ptx::policy_evict_normal(), pol_x = ptx::policy_evict_last();
+                uint32_t it = 0;
+                bool ok = true;
+                for (int u = u0; ok && u < n_units; u += du) {
+                    const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, u);
+                    // a run of 128 rows or fewer leaves the odd CTA's rows as they lie: their
+                    // sums are not read
+                    const bool rows = even || t.cnt > 128;
+                    const uint32_t bytes = (t.cnt > 128 ? 4 : 3) * kQpTile;
+                    const int wy = UP ? t.wt * 128 : t.wt * 256 + (int)rank * 128;
+                    const CUtensorMap *wm = UP && !even ? &tm_w1 : &tm_w0;
+                    for (int kb = 0; kb < nk; ++kb, ++it) {
+                        const uint32_t s = it % kQpStages, ph = (it / kQpStages) & 1;
+                        if (!(ok = wait_soon(&hd->empty[s], ph ^ 1, a.err))) break;
+                        unsigned char *sp = smem + s * kQpStage;
+                        const uint32_t fb = ptx::map_rank(ptx::smem_u32(&hd->full[s]), 0);
+                        if (even) ptx::mbar_arrive_expect_tx(&hd->full[s], bytes);
+                        tma_3d_pair(sp + kQpTile, wm, kb * 128, wy, t.e, fb, pol_w);
+                        if (rows)
+                            tma_2d_pair(sp, &tm_x, kb * 128, t.s0 + (int)rank * 128, fb, pol_x);
+                    }
+                }
+                // copies in flight land before the block can end: the even CTA sees its
+                // stages fill, the odd one, whose copies complete there, sees them consumed
+                for (uint32_t k = (it > kQpStages ? it - kQpStages : 0); k < it; ++k)
+                    ptx::mbar_wait_hint(even ? &hd->full[k % kQpStages] : &hd->empty[k % kQpStages],
+                                        (k / kQpStages) & 1, a.err);
+            }
+            __syncwarp();
+        } else if (warp == 1) {
+            // ------------------------------------------------------------ MMAs
+            if (even && lane == 0) {
+                uint32_t it = 0;
+                bool ok = true;
+                for (int u = u0; ok && u < n_units; u += du) {
+                    for (int kb = 0; kb < nk; ++kb, ++it) {
+                        const uint32_t s = it % kQpStages, ph = (it / kQpStages) & 1;
+                        const uint32_t b = it & 1, bph = (it >> 1) & 1;
+                        // released by both CTAs' epilogues
+                        ok = wait_soon(&hd->full[s], ph, a.err) &&
+                             wait_soon(&hd->tempty[b], bph ^ 1, a.err);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t sa = ptx::smem_u32(smem + s * kQpStage);
+                        const uint64_t x = smem_desc(sa), w = smem_desc(sa + kQpTile);
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)
+                            mma_f8_pair(tmem + b * 256, x + 2 * kk, w + 2 * kk, kQpIdesc, kk != 0);
+                        mma_commit_pair(&hd->empty[s], 3);
+                        mma_commit_pair(&hd->tfull[b], 3);
+                    }
+                }
+                mma_commit_pair(&hd->done, 1);
+                ptx::mbar_wait(&hd->done, 0, a.err);
+            }
+            __syncwarp();
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        // ------------------------------------------------------------ epilogue
+        const int q = warp & 3, half = (warp - kQpEpilogue) >> 2;
+        const uint32_t tempty0 = ptx::map_rank(ptx::smem_u32(&hd->tempty[0]), 0);
+        bool dead = false;  // a wait gave up: keep the barriers, skip the work
+        uint32_t it = 0, tl = 0;
+        for (int u = u0; u < n_units; u += du, ++tl) {
+            const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, u);
+            const int r = (int)rank * 128 + q * 32 + lane;  // of the run
+            const bool mine = r < t.cnt;
+            const float *sx = a.xs + t.s0 + r;
+            const int blk = UP ? t.wt : min(t.wt * 2 + half, nblk - 1);
+            const float *sw0 = a.s0 + ((size_t)t.e * nblk + blk) * nk;
+            const float *sw1 = UP ? a.s1 + ((size_t)t.e * nblk + blk) * nk : sw0;
+            uint64_t acc[64];
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[i] = 0;
+            float nx = mine ? *sx : 0.f, n0 = sw0[0], n1 = UP ? sw1[0] : 0.f;
+            for (int kb = 0; kb < nk; ++kb, ++it) {
+                const uint32_t b = it & 1, bph = (it >> 1) & 1;
+                const uint64_t sc0 = twice(nx * n0), sc1 = UP ? twice(nx * n1) : sc0;
+                if (!dead) dead = !__all_sync(0xffffffffu, wait_soon(&hd->tfull[b], bph, a.err));
+                tc_fence_after();
+                const int kn = min(kb + 1, nk - 1);  // the next block's scales
+                nx = mine ? sx[(size_t)kn * a.S] : 0.f;
+                n0 = sw0[kn];
+                if (UP) n1 = sw1[kn];
+                const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + b * 256 +
+                                      (uint32_t)half * (UP ? 64 : 128);
+                if (!dead) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float v[2][32];
+                        tmem_ld32(base + c * (UP ? 128 : 64), v[0]);
+                        tmem_ld32(base + c * (UP ? 128 : 64) + 32, v[1]);
+                        tmem_ld_wait();
+                        if (c == 1) {  // the accumulator is read: the next MMAs may write it
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) {
+                                if (even) ptx::mbar_arrive(&hd->tempty[b]);
+                                else arrive_remote(tempty0 + b * (uint32_t)sizeof(uint64_t));
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            fma2(acc[c * 32 + i], v[i >> 4][2 * (i & 15)], v[i >> 4][2 * (i & 15) + 1],
+                                 c ? sc1 : sc0);
+                    }
+                }
+            }
+            if (UP) {
+                float h[64];
+                uint32_t m = 0;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const float2 x = both(acc[i]), y = both(acc[32 + i]);
+                    h[2 * i] = silu(x.x) * y.x;
+                    h[2 * i + 1] = silu(x.y) * y.y;
+                    m = max(m, max(abs_bits(h[2 * i]), abs_bits(h[2 * i + 1])));
+                }
+                hd->amax[tl & 1][half][q * 32 + lane] = m;
+                ptx::named_bar_sync(1 + q, 64);
+                m = max(m, hd->amax[tl & 1][half ^ 1][q * 32 + lane]);
+                float sc, inv;
+                q_scale(m, sc, inv);
+                if (mine && !dead) {
+                    const int col = t.wt * 128 + half * 64;
+                    uint8_t *hp = static_cast<uint8_t *>(a.out) + (size_t)(t.s0 + r) * a.n_out + col;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (col + 16 * i < a.n_out) {
+                            const float *g = h + 16 * i;
+                            *reinterpret_cast<uint4 *>(hp + 16 * i) =
+                                make_uint4(q_pack4(g[0], g[1], g[2], g[3], inv),
+                                           q_pack4(g[4], g[5], g[6], g[7], inv),
+                                           q_pack4(g[8], g[9], g[10], g[11], inv),
+                                           q_pack4(g[12], g[13], g[14], g[15], inv));
+                        }
+                    if (half == 0) a.out_scale[(size_t)t.wt * a.S + t.s0 + r] = sc;
+                }
+            } else if (mine && !dead) {
+                const int col = t.wt * 256 + half * 128;
+                if (a.y_bf16) {
+                    bf16 *y = static_cast<bf16 *>(a.out) + (size_t)(t.s0 + r) * a.n_out + col;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (col + 8 * i < a.n_out) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float2 v = both(acc[4 * i + j]);
+                                const __nv_bfloat162 p = __floats2bfloat162_rn(v.x, v.y);
+                                w[j] = *reinterpret_cast<const uint32_t *>(&p);
+                            }
+                            *reinterpret_cast<uint4 *>(y + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                } else {
+                    float *y = static_cast<float *>(a.out) + (size_t)(t.s0 + r) * a.n_out + col;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (col + 4 * i < a.n_out) {
+                            const float2 v = both(acc[2 * i]), w = both(acc[2 * i + 1]);
+                            *reinterpret_cast<float4 *>(y + 4 * i) = make_float4(v.x, v.y, w.x, w.y);
+                        }
+                }
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    ptx::cluster_sync_all();  // no CTA leaves while its pair may touch it
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc_pair(tmem, 512);
+}
+
+void pair_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&attr)[2], int grid) {
+    cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kQpThreads);
+    cfg.dynamicSmemBytes = kQpSmem;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+}
+
+// CTA pairs that the current device keeps resident (looked up once a device).
+template <bool UP>
+int resident_pairs() {
+    static int cached[64];
+    static std::once_flag once[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    std::call_once(once[dev], [dev] {
+        const void *kern = (const void *)k_quant_pair<UP>;
+        int pairs = 0;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kQpSmem) ==
+            cudaSuccess) {
+            cudaLaunchConfig_t cfg;
+            cudaLaunchAttribute attr[2];
+            pair_config(cfg, attr, device_info().sm_count & ~1);
+            if (cudaOccupancyMaxActiveClusters(&pairs, kern, &cfg) != cudaSuccess) pairs = 0;
+        }
+        (void)cudaGetLastError();
+        cached[dev] = std::min(pairs, device_info().sm_count / 2);
+    });
+    return cached[dev];
+}
+
+template <bool UP>
+cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QpArgs a, cudaStream_t st) {
+    const int pairs = resident_pairs<UP>();
+    CUtensorMap mw0, mw1, mx;
+    if (pairs < 1 || !q_weight_map(&mw0, w0, g.E, g.n_out, g.n_in) ||
+        !q_weight_map(&mw1, UP ? w1 : w0, g.E, g.n_out, g.n_in) ||
+        !q_row_map(&mx, g.x8, g.S, g.n_in, 128))
+        return cudaErrorInvalidValue;
+    a.offsets = g.offsets;
+    a.E = g.E;
+    a.S = g.S;
+    a.n_in = g.n_in;
+    a.n_out = g.n_out;
+    a.xs = g.xs;
+    a.err = device_info().err;
+    void *args[] = {&mw0, &mw1, &mx, &a};
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    pair_config(cfg, attr, 2 * pairs);
+    cfg.numAttrs = 2;
+    cfg.stream = st;
+    LaunchScope ls(UP ? "quant_up_pair" : "quant_down_pair", st);
+    return cudaLaunchKernelExC(&cfg, (const void *)k_quant_pair<UP>, args);
+}
+
+}  // namespace
+
+bool quant_pair_ok() { return resident_pairs<true>() > 0 && resident_pairs<false>() > 0; }
+
+cudaError_t launch_quant_pair_up(const QuantGemm &g, const QuantUp &u, cudaStream_t st) {
+    QpArgs a{};
+    a.s0 = u.s1;
+    a.s1 = u.sv;
+    a.out = u.h8;
+    a.out_scale = u.hs;
+    return launch<true>(g, u.w1, u.v1, a, st);
+}
+
+cudaError_t launch_quant_pair_down(const QuantGemm &g, const QuantDown &u, cudaStream_t st) {
+    QpArgs a{};
+    a.s0 = u.s;
+    a.out = u.y;
+    a.y_bf16 = u.y_bf16;
+    return launch<false>(g, u.w, nullptr, a, st);
+}
+
+}  // namespace moe

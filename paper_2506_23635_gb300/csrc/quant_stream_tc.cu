@@ -73,30 +73,6 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, 
         : "memory");
 }
 
-// 16 consecutive fp32 columns of this warp's 32 tensor-memory lanes.
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
-    uint32_t r[16];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
-          "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr)
-        : "memory");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-
-// One lane of the warp, always the same.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t r;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(r));
-    return r != 0;
-}
-
 struct QsTile {
     int e, wt;    // expert, 128 weight rows
     int s0, cnt;  // first row of x, rows
@@ -169,9 +145,9 @@ __device__ void qs_prefix(const int32_t *offsets, int E, int S, int nwt, int col
 struct QsArgs {
     const int32_t *offsets;
     int E, S, n_in, n_out;
-    const float *xs, *s0, *s1;  // scales of x, of w1 (or w), of v1
+    const float *xs, *s0, *s1;  // scales of x [blocks, S], of w1 (or w), of v1
     void *out;                  // h8 or y
-    float *out_scale;           // hs
+    float *out_scale;           // hs [blocks, S]
     int y_bf16;
     float *part;
     int *count;
@@ -227,7 +203,7 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
             while (ok && share.next(t, kb0, kb1, first, last)) {
                 for (int kb = kb0; kb < kb1; ++kb, ++it) {
                     const uint32_t s = it % kStages, ph = (it / kStages) & 1;
-                    if (!(ok = ptx::mbar_wait_hint(&hd->empty[s], ph ^ 1, a.err))) break;
+                    if (!(ok = wait_soon(&hd->empty[s], ph ^ 1, a.err))) break;
                     unsigned char *sp = smem + s * C::kStage;
                     ptx::mbar_arrive_expect_tx(&hd->full[s], C::kStage);
                     tma_3d(sp, &tm_w0, kb * 128, t.wt * 128, t.e, &hd->full[s], pol_w);
@@ -250,8 +226,8 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
             for (int kb = kb0; kb < kb1; ++kb, ++it) {
                 const uint32_t s = it % kStages, ph = (it / kStages) & 1;
                 const uint32_t b = it % kQsAcc, bph = (it / kQsAcc) & 1;
-                ok = ptx::mbar_wait(&hd->tempty[b], bph ^ 1, a.err) &&
-                     ptx::mbar_wait_hint(&hd->full[s], ph, a.err);
+                ok = wait_soon(&hd->full[s], ph, a.err) &&
+                     wait_soon(&hd->tempty[b], bph ^ 1, a.err);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -289,9 +265,9 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                 for (int i = 0; i < N; ++i) acc[m][i] = 0.f;
             const float *sw0 = a.s0 + ((size_t)t.e * nwt + t.wt) * nk;
             const float *sw1 = UP ? a.s1 + ((size_t)t.e * nwt + t.wt) * nk : nullptr;
-            const float *sx = a.xs + (size_t)(t.s0 + th) * nk;
+            const float *sx = a.xs + t.s0 + th;
             const bool mine = th < t.cnt;
-            float nx = mine ? sx[kb0] : 0.f, n0 = sw0[kb0], n1 = UP ? sw1[kb0] : 0.f;
+            float nx = mine ? sx[(size_t)kb0 * a.S] : 0.f, n0 = sw0[kb0], n1 = UP ? sw1[kb0] : 0.f;
             for (int kb = kb0; kb < kb1; ++kb, ++it) {
                 const uint32_t b = it % kQsAcc, bph = (it / kQsAcc) & 1;
                 if (th < N) {
@@ -299,12 +275,12 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                     if (UP) hd->scale[it & 1][1][th] = nx * n1;
                 }
                 if (kb + 1 < kb1) {
-                    nx = mine ? sx[kb + 1] : 0.f;
+                    nx = mine ? sx[(size_t)(kb + 1) * a.S] : 0.f;
                     n0 = sw0[kb + 1];
                     if (UP) n1 = sw1[kb + 1];
                 }
                 ptx::named_bar_sync(1, 128);
-                if (!dead) dead = !__all_sync(0xffffffffu, ptx::mbar_wait_hint(&hd->tfull[b], bph, a.err));
+                if (!dead) dead = !__all_sync(0xffffffffu, wait_soon(&hd->tfull[b], bph, a.err));
                 tc_fence_after();
                 const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + b * C::kCols;
 #pragma unroll
@@ -379,7 +355,7 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                         q_scale(m, sc, inv);
                         if (row < a.n_out && !dead)
                             h[(size_t)i * a.n_out] = (uint8_t)e4m3x2(acc[0][i] * inv, 0.f);
-                        if (th == i && !dead) a.out_scale[(size_t)(t.s0 + i) * nwt + t.wt] = sc;
+                        if (th == i && !dead) a.out_scale[(size_t)t.wt * a.S + t.s0 + i] = sc;
                     }
                 }
             } else if (row < a.n_out && !dead) {
