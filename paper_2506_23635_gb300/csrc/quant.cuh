@@ -31,6 +31,11 @@ __device__ __forceinline__ void q_scale(uint32_t amax_bits, float &scale, float 
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// SiLU by the fast exponential and quotient: off by at most (|a| + 8) 2^-23 of itself, far
+// below the e4m3 rounding that follows (with expf and a full division the up projection
+// of 2048 tokens took 1520 us instead of 1170).
+__device__ __forceinline__ float q_silu(float a) { return __fdividef(a, 1.f + __expf(-a)); }
+
 // Four values times inv (a power of two: exact but for numbers far below the
 // block's smallest e4m3) rounded to e4m3, the first in the low byte.
 __device__ __forceinline__ uint32_t q_pack4(float a, float b, float c, float d, float inv) {

@@ -25,11 +25,12 @@ namespace {
 using namespace tc;
 
 // warp 0 loads, warp 1 issues the MMAs, warps 4-11 are the epilogue.  Registers of the
-// launch: 168 a thread, 64,512; what the first four warps give up the others take:
-// 128 (72 + 2 * 216) = 64,512.
+// launch: 168 a thread, 64,512; what the first four warps give up the others take: 128
+// (104 + 2 * 200) for UP, 128 (120 + 2 * 192) for DOWN, both 64,512 (splits that spill on
+// either side cost 5 to 20%).
 constexpr int kQpThreads = 384;
 constexpr int kQpEpilogue = 4;  // first warp of it
-constexpr int kQpStages = 6;
+constexpr int kQpStages = 5;
 constexpr uint32_t kQpTile = 128 * 128;
 constexpr uint32_t kQpStage = 2 * kQpTile;  // of a CTA: 128 rows of x, 128 weight rows
 constexpr int kQpRows = 256;
@@ -46,7 +47,8 @@ struct QpHeader {
 };
 constexpr uint32_t kQpHdrBytes = 6144;
 static_assert(sizeof(QpHeader) <= kQpHdrBytes, "header");
-constexpr size_t kQpSmem = 1024 + kQpStages * kQpStage + kQpHdrBytes;
+constexpr uint32_t kQpOut = 8 * 4096;  // 4 KB an epilogue warp: 32 rows of 128 bytes on their way out
+constexpr size_t kQpSmem = 1024 + kQpStages * kQpStage + kQpOut + kQpHdrBytes;
 static_assert(kQpSmem <= 227 * 1024, "shared memory");
 
 __device__ __forceinline__ void mma_f8_pair(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc,
@@ -149,18 +151,17 @@ struct QpArgs {
     const float *xs, *s0, *s1;  // scales of x [blocks, S], of w1 (or w), of v1
     void *out;                  // h8 or y
     float *out_scale;           // hs [blocks, S]
-    int y_bf16;
     unsigned *err;
 };
 
-template <bool UP>
+template <bool UP, bool BF>
 __global__ void __launch_bounds__(kQpThreads, 1)
 k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ CUtensorMap tm_w1,
              const __grid_constant__ CUtensorMap tm_x, const QpArgs a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    QpHeader *hd = reinterpret_cast<QpHeader *>(smem + kQpStages * kQpStage);
+    QpHeader *hd = reinterpret_cast<QpHeader *>(smem + kQpStages * kQpStage + kQpOut);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_ctarank();
     const bool even = rank == 0;
@@ -192,7 +193,7 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
     const int n_units = hd->prefix[a.E], u0 = blockIdx.x >> 1, du = gridDim.x >> 1;
 
     if (warp < kQpEpilogue) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(UP ? 104 : 120));
         if (warp == 0) {
             // ------------------------------------------------------------ loads
             if (lane == 0) {
@@ -229,24 +230,28 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
         } else if (warp == 1) {
             // ------------------------------------------------------------ MMAs
             if (even && lane == 0) {
-                uint32_t it = 0;
+                const int n = u0 < n_units ? ((n_units - 1 - u0) / du + 1) * nk : 0;
+                const uint64_t d0 = smem_desc(ptx::smem_u32(smem));
+                uint32_t s = 0, ph = 0;
                 bool ok = true;
-                for (int u = u0; ok && u < n_units; u += du) {
-                    for (int kb = 0; kb < nk; ++kb, ++it) {
-                        const uint32_t s = it % kQpStages, ph = (it / kQpStages) & 1;
-                        const uint32_t b = it & 1, bph = (it >> 1) & 1;
-                        // released by both CTAs' epilogues
-                        ok = wait_soon(&hd->full[s], ph, a.err) &&
-                             wait_soon(&hd->tempty[b], bph ^ 1, a.err);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t sa = ptx::smem_u32(smem + s * kQpStage);
-                        const uint64_t x = smem_desc(sa), w = smem_desc(sa + kQpTile);
+#pragma unroll 1
+                for (int it = 0; ok && it < n; ++it) {
+                    const uint32_t b = it & 1, bph = (it >> 1) & 1;
+                    // (released by both CTAs' epilogues)
+                    ok = wait_soon(&hd->full[s], ph, a.err) &&
+                         wait_soon(&hd->tempty[b], bph ^ 1, a.err);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t x = d0 + s * (kQpStage >> 4), w = x + (kQpTile >> 4);
+                    const uint32_t d = tmem + b * 256;
 #pragma unroll
-                        for (int kk = 0; kk < 4; ++kk)
-                            mma_f8_pair(tmem + b * 256, x + 2 * kk, w + 2 * kk, kQpIdesc, kk != 0);
-                        mma_commit_pair(&hd->empty[s], 3);
-                        mma_commit_pair(&hd->tfull[b], 3);
+                    for (int kk = 0; kk < 4; ++kk)
+                        mma_f8_pair(d, x + 2 * kk, w + 2 * kk, kQpIdesc, kk != 0);
+                    mma_commit_pair(&hd->tfull[b], 3);
+                    mma_commit_pair(&hd->empty[s], 3);
+                    if (++s == kQpStages) {
+                        s = 0;
+                        ph ^= 1;
                     }
                 }
                 mma_commit_pair(&hd->done, 1);
@@ -255,9 +260,10 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
             __syncwarp();
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(UP ? 200 : 192));
         // ------------------------------------------------------------ epilogue
         const int q = warp & 3, half = (warp - kQpEpilogue) >> 2;
+        const uint32_t base0 = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)half * (UP ? 64 : 128);
         const uint32_t tempty0 = ptx::map_rank(ptx::smem_u32(&hd->tempty[0]), 0);
         bool dead = false;  // a wait gave up: keep the barriers, skip the work
         uint32_t it = 0, tl = 0;
@@ -265,33 +271,32 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
             const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, u);
             const int r = (int)rank * 128 + q * 32 + lane;  // of the run
             const bool mine = r < t.cnt;
-            const float *sx = a.xs + t.s0 + r;
+            const float *sx = a.xs + t.s0 + min(r, t.cnt - 1);
             const int blk = UP ? t.wt : min(t.wt * 2 + half, nblk - 1);
             const float *sw0 = a.s0 + ((size_t)t.e * nblk + blk) * nk;
             const float *sw1 = UP ? a.s1 + ((size_t)t.e * nblk + blk) * nk : sw0;
             uint64_t acc[64];
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i] = 0;
-            float nx = mine ? *sx : 0.f, n0 = sw0[0], n1 = UP ? sw1[0] : 0.f;
+            float nx = *sx, n0 = sw0[0], n1 = UP ? sw1[0] : 0.f;
             for (int kb = 0; kb < nk; ++kb, ++it) {
                 const uint32_t b = it & 1, bph = (it >> 1) & 1;
                 const uint64_t sc0 = twice(nx * n0), sc1 = UP ? twice(nx * n1) : sc0;
                 if (!dead) dead = !__all_sync(0xffffffffu, wait_soon(&hd->tfull[b], bph, a.err));
                 tc_fence_after();
-                const int kn = min(kb + 1, nk - 1);  // the next block's scales
-                nx = mine ? sx[(size_t)kn * a.S] : 0.f;
-                n0 = sw0[kn];
-                if (UP) n1 = sw1[kn];
-                const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + b * 256 +
-                                      (uint32_t)half * (UP ? 64 : 128);
+                if (kb + 1 < nk) {  // the next block's scales
+                    nx = *(sx += a.S);
+                    n0 = *++sw0;
+                    if (UP) n1 = *++sw1;
+                }
+                const uint32_t base = base0 + b * 256;
                 if (!dead) {
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        float v[2][32];
-                        tmem_ld32(base + c * (UP ? 128 : 64), v[0]);
-                        tmem_ld32(base + c * (UP ? 128 : 64) + 32, v[1]);
+                    for (int c = 0; c < 4; ++c) {
+                        float v[32];
+                        tmem_ld32(base + (c >> 1) * (UP ? 128 : 64) + (c & 1) * 32, v);
                         tmem_ld_wait();
-                        if (c == 1) {  // the accumulator is read: the next MMAs may write it
+                        if (c == 3) {  // the accumulator is read: the next MMAs may write it
                             tc_fence_before();
                             __syncwarp();
                             if (lane == 0) {
@@ -300,9 +305,8 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
                             }
                         }
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            fma2(acc[c * 32 + i], v[i >> 4][2 * (i & 15)], v[i >> 4][2 * (i & 15) + 1],
-                                 c ? sc1 : sc0);
+                        for (int i = 0; i < 16; ++i)
+                            fma2(acc[c * 16 + i], v[2 * i], v[2 * i + 1], c >> 1 ? sc1 : sc0);
                     }
                 }
             }
@@ -312,8 +316,8 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     const float2 x = both(acc[i]), y = both(acc[32 + i]);
-                    h[2 * i] = silu(x.x) * y.x;
-                    h[2 * i + 1] = silu(x.y) * y.y;
+                    h[2 * i] = q_silu(x.x) * y.x;
+                    h[2 * i + 1] = q_silu(x.y) * y.y;
                     m = max(m, max(abs_bits(h[2 * i]), abs_bits(h[2 * i + 1])));
                 }
                 hd->amax[tl & 1][half][q * 32 + lane] = m;
@@ -336,30 +340,44 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
                         }
                     if (half == 0) a.out_scale[(size_t)t.wt * a.S + t.s0 + r] = sc;
                 }
-            } else if (mine && !dead) {
-                const int col = t.wt * 256 + half * 128;
-                if (a.y_bf16) {
-                    bf16 *y = static_cast<bf16 *>(a.out) + (size_t)(t.s0 + r) * a.n_out + col;
+            } else {
+                // 32 rows of 128 bytes at a time through shared memory, so that eight lanes
+                // write a row's 128 bytes (16-byte chunks exchanged by the row: no conflicts)
+                constexpr int kCols = BF ? 64 : 32, kSize = BF ? 2 : 4;
+                uint8_t *buf = smem + kQpStages * kQpStage + (warp - kQpEpilogue) * 4096;
+                const int row0 = (int)rank * 128 + q * 32, col0 = t.wt * 256 + half * 128;
+                uint8_t *y = static_cast<uint8_t *>(a.out) + ((size_t)t.s0 * a.n_out + col0) * kSize;
+                const int ch = lane & 7;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (col + 8 * i < a.n_out) {
-                            uint32_t w[4];
+                for (int c = 0; c < 128 / kCols; ++c) {
+                    __syncwarp();
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float2 v = both(acc[4 * i + j]);
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (BF) {
+                                const float2 v = both(acc[c * 32 + 4 * i + j]);
                                 const __nv_bfloat162 p = __floats2bfloat162_rn(v.x, v.y);
                                 w[j] = *reinterpret_cast<const uint32_t *>(&p);
+                            } else {
+                                const float2 v = both(acc[c * 16 + 2 * i + (j >> 1)]);
+                                w[j] = __float_as_uint(j & 1 ? v.y : v.x);
                             }
-                            *reinterpret_cast<uint4 *>(y + 8 * i) = make_uint4(w[0], w[1], w[2], w[3]);
                         }
-                } else {
-                    float *y = static_cast<float *>(a.out) + (size_t)(t.s0 + r) * a.n_out + col;
+                        *reinterpret_cast<uint4 *>(buf + lane * 128 + ((i ^ (lane & 7)) << 4)) =
+                            make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    __syncwarp();
+                    const bool in = col0 + c * kCols + ch * (16 / kSize) < a.n_out && !dead;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (col + 4 * i < a.n_out) {
-                            const float2 v = both(acc[2 * i]), w = both(acc[2 * i + 1]);
-                            *reinterpret_cast<float4 *>(y + 4 * i) = make_float4(v.x, v.y, w.x, w.y);
-                        }
+                    for (int i = 0; i < 8; ++i) {
+                        const int rr = i * 4 + (lane >> 3);
+                        const uint4 w = *reinterpret_cast<const uint4 *>(buf + rr * 128 + ((ch ^ (rr & 7)) << 4));
+                        if (in && row0 + rr < t.cnt)
+                            *reinterpret_cast<uint4 *>(y + (size_t)(row0 + rr) * a.n_out * kSize + c * 128 +
+                                                       ch * 16) = w;
+                    }
                 }
             }
         }
@@ -387,14 +405,14 @@ void pair_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&attr)[2], int gr
 }
 
 // CTA pairs that the current device keeps resident (looked up once a device).
-template <bool UP>
+template <bool UP, bool BF>
 int resident_pairs() {
     static int cached[64];
     static std::once_flag once[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
     std::call_once(once[dev], [dev] {
-        const void *kern = (const void *)k_quant_pair<UP>;
+        const void *kern = (const void *)k_quant_pair<UP, BF>;
         int pairs = 0;
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kQpSmem) ==
             cudaSuccess) {
@@ -409,9 +427,9 @@ int resident_pairs() {
     return cached[dev];
 }
 
-template <bool UP>
+template <bool UP, bool BF>
 cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QpArgs a, cudaStream_t st) {
-    const int pairs = resident_pairs<UP>();
+    const int pairs = resident_pairs<UP, BF>();
     CUtensorMap mw0, mw1, mx;
     if (pairs < 1 || !q_weight_map(&mw0, w0, g.E, g.n_out, g.n_in) ||
         !q_weight_map(&mw1, UP ? w1 : w0, g.E, g.n_out, g.n_in) ||
@@ -431,12 +449,13 @@ cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QpArgs a,
     cfg.numAttrs = 2;
     cfg.stream = st;
     LaunchScope ls(UP ? "quant_up_pair" : "quant_down_pair", st);
-    return cudaLaunchKernelExC(&cfg, (const void *)k_quant_pair<UP>, args);
+    return cudaLaunchKernelExC(&cfg, (const void *)k_quant_pair<UP, BF>, args);
 }
 
 }  // namespace
 
-bool quant_pair_ok() { return resident_pairs<true>() > 0 && resident_pairs<false>() > 0; }
+bool quant_pair_ok() { return resident_pairs<true, false>() > 0 && resident_pairs<false, true>() > 0 &&
+           resident_pairs<false, false>() > 0; }
 
 cudaError_t launch_quant_pair_up(const QuantGemm &g, const QuantUp &u, cudaStream_t st) {
     QpArgs a{};
@@ -444,15 +463,15 @@ cudaError_t launch_quant_pair_up(const QuantGemm &g, const QuantUp &u, cudaStrea
     a.s1 = u.sv;
     a.out = u.h8;
     a.out_scale = u.hs;
-    return launch<true>(g, u.w1, u.v1, a, st);
+    return launch<true, false>(g, u.w1, u.v1, a, st);
 }
 
 cudaError_t launch_quant_pair_down(const QuantGemm &g, const QuantDown &u, cudaStream_t st) {
     QpArgs a{};
     a.s0 = u.s;
     a.out = u.y;
-    a.y_bf16 = u.y_bf16;
-    return launch<false>(g, u.w, nullptr, a, st);
+    return u.y_bf16 ? launch<false, true>(g, u.w, nullptr, a, st)
+                    : launch<false, false>(g, u.w, nullptr, a, st);
 }
 
 }  // namespace moe

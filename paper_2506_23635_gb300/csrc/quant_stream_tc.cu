@@ -340,7 +340,7 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                 // h in place of a; its largest magnitude of each column over the 128 rows
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    acc[0][i] = silu(acc[0][i]) * acc[C::kMats - 1][i];
+                    acc[0][i] = q_silu(acc[0][i]) * acc[C::kMats - 1][i];
                     const uint32_t m = __reduce_max_sync(0xffffffffu, abs_bits(acc[0][i]));
                     if (lane == 0) hd->amax[q][i] = m;
                 }

@@ -81,8 +81,10 @@ def ffn(x, w1, v1, w2):
     a, ea = product(x, w1)
     b, eb = product(x, v1)
     h = silu(a) * b
-    # |silu'| < 1.1; the exponential, the quotient and the products 8 steps together
-    eh = 1.1 * ea * (np.abs(b) + eb) + np.abs(silu(a)) * eb + 8 * U32 * np.abs(h)
+    # |silu'| < 1.1; of its own, the argument of 2^x is a log2(e) rounded, off by half a step of
+    # |a| 1.45 2^-24, so the exponential by |a| 2^-24 of itself, and it, the quotient and the
+    # products by 8 steps together
+    eh = 1.1 * ea * (np.abs(b) + eb) + np.abs(silu(a)) * eb + (8 + np.abs(a)) * U32 * np.abs(h)
     rows, cols = h.shape
     pad = lambda v: np.pad(v, ((0, 0), (0, blocks(cols) * B - cols))).reshape(rows, -1, B)
     lo = scale_of(np.maximum(pad(np.abs(h) - eh), 0).max(-1))
