@@ -21,8 +21,8 @@ __global__ void __launch_bounds__(kRowsThreads)
 k_quant_rows(int rows, int cols, int K, const TX *__restrict__ x,
              const int32_t *__restrict__ inv_perm, uint8_t *__restrict__ q,
              float *__restrict__ scale, int *__restrict__ count, int n_count) {
-    ptx::launch_dependents();
     ptx::grid_dependency_wait();
+    ptx::launch_dependents();  // (after the wait: the products read offsets and weights early)
     if (count && blockIdx.x == 0)
         for (int i = threadIdx.x; i < n_count; i += kRowsThreads) count[i] = 0;
     const int nb = q_blocks(cols), sub = threadIdx.x & 15;
@@ -116,8 +116,8 @@ __global__ void __launch_bounds__(256)
 k_quant_scales(int S, int nb, const float *__restrict__ in, float *__restrict__ out, int *count,
                int n_count) {
     __shared__ float tile[32][33];
-    ptx::launch_dependents();
     ptx::grid_dependency_wait();
+    ptx::launch_dependents();  // (after the wait: the product reads offsets and weights early)
     if (blockIdx.x == 0 && blockIdx.y == 0)
         for (int i = threadIdx.x; i < n_count; i += 256) count[i] = 0;
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5, b0 = blockIdx.y * 32;
@@ -457,7 +457,7 @@ QuantLayout quant_layout(const moe_dims &d, int64_t T) {
     const size_t S = (size_t)T * d.top_k;
     QuantLayout L{};
     size_t o = 0;
-    L.cols = q_stream_cols(T);
+    L.cols = q_stream_cols(d.n_experts, (long long)S);
     L.idx = o; o += up(S * 4);
     L.gate = o; o += up(S * 4);
     L.logits = o; o += up((size_t)T * d.n_experts * 4);
@@ -515,15 +515,11 @@ cudaError_t quant_experts(const moe_dims &d, int T, const void *x, const moe_qua
         if (e == cudaSuccess) e = launch_quant_pair_down(gd, down, st);
     } else {
         e = launch_quant_stream_up(gu, up, pu, L.cols, st);
-        if (e == cudaSuccess) e = launch_quant_stream_down(gd, down, pd, L.cols, st);
+        if (e == cudaSuccess) e = launch_quant_stream_down(gd, down, pd, L.cols, false, st);
     }
     if (e == cudaSuccess)
         e = launch_layer_combine(d, T, at<float>(ws, L.y), inv, gate, residual, out, st);
     return e;
-}
-
-int product_cols(int E, int S) {
-    return q_stream_cols(E == 1 ? S : std::min<long long>(S, 2LL * ((S + E - 1) / E)));
 }
 
 // Workspace of a product for up to S rows: scales, counters, parts.
@@ -534,7 +530,7 @@ struct ProductLayout {
 ProductLayout product_layout(int E, int n_in, int S) {
     auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
     ProductLayout L{};
-    L.cols = product_cols(E, S);
+    L.cols = q_stream_cols(E, S);
     size_t o = 0;
     L.xs = o; o += up((size_t)S * q_blocks(n_in) * 4);
     L.count = o; o += up(kQMaxCtas * 4);
@@ -643,7 +639,7 @@ moe_status moe_quant_product(int32_t n_groups, int32_t n_out, int32_t n_in, int3
     if (many_rows(n_groups, S) && quant_pair_ok())
         return q_status(launch_quant_pair_down(g, down, st));
     return q_status(launch_quant_stream_down(g, down, QuantParts{at<float>(ws, L.part), count}, L.cols,
-                                             st));
+                                             true, st));
 }
 
 moe_status moe_quant_workspace_size(const moe_dims *dims, int32_t max_tokens, size_t *bytes) {

@@ -82,6 +82,18 @@ __device__ __forceinline__ bool elect_one() {
     return r != 0;
 }
 
+// Two fp32 at once: acc += v * s.
+__device__ __forceinline__ void fma2(uint64_t &acc, float v0, float v1, uint64_t s) {
+    asm("{\n\t.reg .b64 v;\n\tmov.b64 v, {%1, %2};\n\tfma.rn.f32x2 %0, v, %3, %0;\n\t}"
+        : "+l"(acc)
+        : "f"(v0), "f"(v1), "l"(s));
+}
+__device__ __forceinline__ float2 both(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+
 // A grouped product of 8-bit operands: rows x8 [S, n_in] in groups given by offsets
 // [E+1] (null: one group of S rows) times each group's matrix w8 [E, n_out, n_in].
 struct QuantGemm {
@@ -97,8 +109,12 @@ struct QuantParts {
     float *part;
     int *count;
 };
-// rows of x8 that a tile of it takes: every expert has at most `rows` of them
-inline int q_stream_cols(long long rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+// Rows of x8 that a tile of the streaming kernel takes: half as many again as the
+// groups have on average (64 tokens of 4 experts of 16: 32), one group's own number.
+inline int q_stream_cols(int E, long long S) {
+    const long long rows = E == 1 ? S : (3 * S + 2 * E - 1) / (2 * E);
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+}
 inline size_t q_part_floats(int cols, bool up) {
     return (size_t)2 * kQMaxCtas * 128 * cols * (up ? 2 : 1);
 }
@@ -118,8 +134,11 @@ struct QuantDown {
 };
 cudaError_t launch_quant_stream_up(const QuantGemm &g, const QuantUp &u, const QuantParts &p,
                                    int cols, cudaStream_t st);
+// alone: not behind the up projection, whose CTAs it shares the SMs with otherwise.  The
+// launch ahead lets either start behind its own wait only (the offsets and weights are read
+// before this kernel's).
 cudaError_t launch_quant_stream_down(const QuantGemm &g, const QuantDown &u, const QuantParts &p,
-                                     int cols, cudaStream_t st);
+                                     int cols, bool alone, cudaStream_t st);
 
 // The same for many rows a group, on CTA pairs (quant_pair_tc.cu), where the device
 // keeps such pairs resident.

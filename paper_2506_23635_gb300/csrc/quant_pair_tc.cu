@@ -85,23 +85,11 @@ __device__ __forceinline__ void arrive_remote(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// Two fp32 at once: acc += v * s.
-__device__ __forceinline__ void fma2(uint64_t &acc, float v0, float v1, uint64_t s) {
-    asm("{\n\t.reg .b64 v;\n\tmov.b64 v, {%1, %2};\n\tfma.rn.f32x2 %0, v, %3, %0;\n\t}"
-        : "+l"(acc)
-        : "f"(v0), "f"(v1), "l"(s));
-}
 __device__ __forceinline__ uint64_t twice(float s) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(s));
     return r;
 }
-__device__ __forceinline__ float2 both(uint64_t v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-
 struct QpTile {
     int e, wt;
     int s0, cnt;  // first row, rows of the run (at most 256)

@@ -9,10 +9,10 @@
 // equally; a tile that several CTAs have a piece of is added up by the one that finishes
 // last, in the order of the k-blocks whoever that is.
 //
-// Each k-block is an accumulator of its own in tensor memory (4 of them in turn): the
+// Each k-block is an accumulator of its own in tensor memory (a few in turn): the
 // epilogue multiplies it with the block's scales as it adds it to the sum it keeps in
-// registers.  Warp 0 loads (TMA), warp 1 issues the MMAs, warps 2-5 are the epilogue, thread i
-// of lane quarter q = (128 weight rows) row 32 q + i.
+// registers.  Warp 0 loads (TMA), warp 1 issues the MMAs, the others are the epilogue: thread
+// i of a warp of lane quarter q has weight row 32 q + i.
 #include "quant.cuh"
 
 namespace moe {
@@ -20,40 +20,49 @@ namespace {
 
 using namespace tc;
 
-constexpr int kQsThreads = 192;
-constexpr int kQsAcc = 4;           // accumulators in tensor memory
 constexpr int kQsMinBlocks = 4;     // k-blocks of a CTA's share at least
 constexpr int kQsMaxStages = 12;
 constexpr uint32_t kQsTile = 128 * 128;
 
+constexpr uint32_t kQsHdrBytes = 4096;
 struct QsHeader {
     uint64_t full[kQsMaxStages], empty[kQsMaxStages];
-    uint64_t tfull[kQsAcc], tempty[kQsAcc];
+    uint64_t tfull[4], tempty[4];
     uint64_t done;
     uint32_t tmem_base;
-    int last;
+    int last, ready[2];  // (ready: pieces in turn)
     int prefix[257];       // tiles of the experts ahead
     alignas(16) float scale[2][2][64];  // of this k-block: x's times w1's (w's), times v1's
     uint32_t amax[4][64];
 };
-constexpr uint32_t kQsHdrBytes = 4096;
 static_assert(sizeof(QsHeader) <= kQsHdrBytes, "header");
 
 template <bool UP, int N>
 struct QsCfg {
     static constexpr int kMats = UP ? 2 : 1;
     static constexpr uint32_t kStage = kMats * kQsTile + N * 128;
-    static constexpr int kStages = (int)((200 * 1024) / kStage) < kQsMaxStages ? (int)((200 * 1024) / kStage)
-                                                                              : kQsMaxStages;
-    static constexpr size_t kSmem = 1024 + kStages * kStage + kQsHdrBytes;
+    // epilogue warps: 32 columns each at most, four warps side by side
+    static constexpr int kHalves = N == 64 ? 2 : 1, kEpi = 4 * kHalves, kThreads = 64 + 32 * kEpi;
+    static constexpr int kOwn = N / kHalves;  // columns of a warp
+    // Stages where the up and the down projection's CTAs share an SM, so that the down
+    // projection's first weights arrive during the up projection's end (not with 64 columns,
+    // which take too many registers); alone: as many as fit 200 KB.
+    static constexpr int kShared = N == 64 ? (UP ? 5 : 8) : UP ? 3 : N == 16 ? 6 : 5;
+    static constexpr int kAlone = (int)((200 * 1024) / kStage) < kQsMaxStages
+                                      ? (int)((200 * 1024) / kStage) : kQsMaxStages;
+    static constexpr int kAcc = N == 64 ? 2 : 4;  // accumulators in turn
     static constexpr uint32_t kCols = kMats * N;  // tensor-memory columns of an accumulator
-    static constexpr uint32_t kTmem = kQsAcc * kCols < 32 ? 32 : kQsAcc * kCols;
+    static constexpr uint32_t kTmem = kAcc * kCols;
     // kind::f8f6f4: e4m3 A and B, fp32 D, both K-major, M = 128
     static constexpr uint32_t kIdesc = (1u << 4) | ((128u >> 4) << 24) | ((uint32_t)(N >> 3) << 17);
+    static constexpr size_t smem(int stages) { return 1024 + stages * kStage + kQsHdrBytes; }
     static_assert(kStage % 1024 == 0, "stages stay 1024-byte aligned");
-    static_assert(kSmem <= 227 * 1024, "shared memory");
-    static_assert((kTmem & (kTmem - 1)) == 0 && kTmem <= 512, "tensor memory");
+    static_assert(smem(kAlone) <= 227 * 1024, "shared memory");
+    static_assert((kTmem & (kTmem - 1)) == 0 && kTmem >= 32 && kTmem <= 256, "tensor memory");
 };
+static_assert(QsCfg<true, 16>::smem(QsCfg<true, 16>::kShared) + QsCfg<false, 16>::smem(QsCfg<false, 16>::kShared) <= 226 * 1024 &&
+              QsCfg<true, 32>::smem(QsCfg<true, 32>::kShared) + QsCfg<false, 32>::smem(QsCfg<false, 32>::kShared) <= 226 * 1024,
+              "an up and a down projection's CTA on one SM");
 
 __device__ __forceinline__ void tma_3d(void *dst, const CUtensorMap *m, int32_t x, int32_t y,
                                        int32_t z, uint64_t *bar, uint64_t policy) {
@@ -71,6 +80,17 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, 
         "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
         "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
         : "memory");
+}
+
+__device__ __forceinline__ int load_acquire(const int *p) {
+    int v;
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ int add_acq_rel(int *p, int v) {
+    int r;
+    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], %2;" : "=r"(r) : "l"(p), "r"(v) : "memory");
+    return r;
 }
 
 struct QsTile {
@@ -149,31 +169,33 @@ struct QsArgs {
     void *out;                  // h8 or y
     float *out_scale;           // hs [blocks, S]
     int y_bf16;
+    int stages;
     float *part;
     int *count;
     unsigned *err;
 };
 
 template <bool UP, int N>
-__global__ void __launch_bounds__(kQsThreads, 1)
+__global__ void __launch_bounds__(QsCfg<UP, N>::kThreads, N == 64 ? 1 : 2)
 k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ CUtensorMap tm_w1,
                const __grid_constant__ CUtensorMap tm_x, const QsArgs a) {
     using C = QsCfg<UP, N>;
-    constexpr int kStages = C::kStages;
+    constexpr int kAcc = C::kAcc;
+    const int n_stage = a.stages;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    QsHeader *hd = reinterpret_cast<QsHeader *>(smem + kStages * C::kStage);
+    QsHeader *hd = reinterpret_cast<QsHeader *>(smem + n_stage * C::kStage);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nk = q_blocks(a.n_in), nwt = q_blocks(a.n_out);
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < n_stage; ++s) {
             ptx::mbar_init(&hd->full[s], 1);
             ptx::mbar_init(&hd->empty[s], 1);
         }
-        for (int b = 0; b < kQsAcc; ++b) {
+        for (int b = 0; b < kAcc; ++b) {
             ptx::mbar_init(&hd->tfull[b], 1);
-            ptx::mbar_init(&hd->tempty[b], 4);
+            ptx::mbar_init(&hd->tempty[b], C::kEpi);
         }
         ptx::mbar_init(&hd->done, 1);
         ptx::fence_barrier_init();
@@ -183,7 +205,8 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
     }
     if (warp == 1) tmem_alloc(&hd->tmem_base, C::kTmem);
     ptx::launch_dependents();
-    ptx::grid_dependency_wait();
+    // (the offsets are older than the launch ahead, which lets this one start behind its own
+    // wait only, or is started so itself)
     if (warp == 2) qs_prefix(a.offsets, a.E, a.S, nwt, N, hd->prefix, a.err);
     tc_fence_before();
     __syncthreads();
@@ -191,60 +214,78 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
     const uint32_t tmem = hd->tmem_base;
     QsShare share{hd->prefix, a.offsets, a.E, a.S, nk, N};
     share.start((int)gridDim.x, (int)blockIdx.x);
-    QsTile t;
+    QsTile t{};
     int kb0, kb1, first, last;
 
     if (warp == 0) {
         // ------------------------------------------------------------ loads
         if (lane == 0) {
             const uint64_t pol_w = ptx::policy_evict_first(), pol_x = ptx::policy_evict_last();
-            uint32_t it = 0;
+            auto weights = [&](int s, int kb) {
+                unsigned char *sp = smem + s * C::kStage;
+                ptx::mbar_arrive_expect_tx(&hd->full[s], C::kStage);
+                tma_3d(sp, &tm_w0, kb * 128, t.wt * 128, t.e, &hd->full[s], pol_w);
+                if (UP) tma_3d(sp + kQsTile, &tm_w1, kb * 128, t.wt * 128, t.e, &hd->full[s], pol_w);
+            };
+            // the first stages' weights, which no kernel ahead writes, before the wait
+            int early = 0;
+            for (QsShare peek = share; early < n_stage && peek.next(t, kb0, kb1, first, last);)
+                for (int kb = kb0; kb < kb1 && early < n_stage; ++kb, ++early) weights(early, kb);
+            ptx::grid_dependency_wait();
+            int s = 0, n = 0;
+            uint32_t ph = 1;
             bool ok = true;
             while (ok && share.next(t, kb0, kb1, first, last)) {
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const uint32_t s = it % kStages, ph = (it / kStages) & 1;
-                    if (!(ok = wait_soon(&hd->empty[s], ph ^ 1, a.err))) break;
-                    unsigned char *sp = smem + s * C::kStage;
-                    ptx::mbar_arrive_expect_tx(&hd->full[s], C::kStage);
-                    tma_3d(sp, &tm_w0, kb * 128, t.wt * 128, t.e, &hd->full[s], pol_w);
-                    if (UP) tma_3d(sp + kQsTile, &tm_w1, kb * 128, t.wt * 128, t.e, &hd->full[s], pol_w);
-                    ptx::tma_load_2d(sp + C::kMats * kQsTile, &tm_x, kb * 128, t.s0, &hd->full[s],
-                                     pol_x);
+                for (int kb = kb0; kb < kb1; ++kb, ++n) {
+                    if (!(ok = wait_soon(&hd->empty[s], ph, a.err))) break;
+                    if (n >= early) weights(s, kb);
+                    ptx::tma_load_2d(smem + s * C::kStage + C::kMats * kQsTile, &tm_x, kb * 128, t.s0,
+                                     &hd->full[s], pol_x);
+                    if (++s == n_stage) {
+                        s = 0;
+                        ph ^= 1;
+                    }
                 }
             }
-            // copies in flight land before the block can end
-            for (uint32_t k = (it > kStages ? it - kStages : 0); k < it; ++k)
-                ptx::mbar_wait_hint(&hd->full[k % kStages], (k / kStages) & 1, a.err);
+            // copies in flight land before the block can end: the stages that were filled
+            // last, whose barriers' phases are those of their last fills.  (Where a wait
+            // gave up, stages whose weights came early may wait for rows that do not come:
+            // these waits end too.)
+            const int total = max(n, early);
+            for (int k = max(0, total - n_stage); k < total; ++k)
+                ptx::mbar_wait_hint(&hd->full[k % n_stage], (k / n_stage) & 1, a.err);
         }
         __syncwarp();
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMAs
         const bool one = elect_one();
-        uint32_t it = 0;
+        const uint64_t d0 = smem_desc(ptx::smem_u32(smem));
+        int s = 0;
+        uint32_t ph = 0;
         bool ok = true;
-        while (ok && share.next(t, kb0, kb1, first, last)) {
-            for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                const uint32_t s = it % kStages, ph = (it / kStages) & 1;
-                const uint32_t b = it % kQsAcc, bph = (it / kQsAcc) & 1;
-                ok = wait_soon(&hd->full[s], ph, a.err) &&
-                     wait_soon(&hd->tempty[b], bph ^ 1, a.err);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t sa = ptx::smem_u32(smem + s * C::kStage);
-                const uint64_t w0 = smem_desc(sa), w1 = smem_desc(sa + kQsTile);
-                const uint64_t x = smem_desc(sa + C::kMats * kQsTile);
-                const uint32_t d = tmem + b * C::kCols;
-                if (one) {
+#pragma unroll 1
+        for (uint32_t it = 0, n = (uint32_t)(share.end - share.pos); ok && it < n; ++it) {
+            const uint32_t b = it % kAcc, bph = (it / kAcc) & 1;
+            ok = wait_soon(&hd->full[s], ph, a.err) && wait_soon(&hd->tempty[b], bph ^ 1, a.err);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t w0 = d0 + s * (C::kStage >> 4), w1 = w0 + (kQsTile >> 4);
+            const uint64_t x = w0 + C::kMats * (kQsTile >> 4);
+            const uint32_t d = tmem + b * C::kCols;
+            if (one) {
 #pragma unroll
-                    for (int kk = 0; kk < 4; ++kk) {
-                        mma_f8(d, w0 + 2 * kk, x + 2 * kk, C::kIdesc, kk != 0);
-                        if (UP) mma_f8(d + N, w1 + 2 * kk, x + 2 * kk, C::kIdesc, kk != 0);
-                    }
-                    mma_commit(&hd->empty[s]);
-                    mma_commit(&hd->tfull[b]);
+                for (int kk = 0; kk < 4; ++kk) {
+                    mma_f8(d, w0 + 2 * kk, x + 2 * kk, C::kIdesc, kk != 0);
+                    if (UP) mma_f8(d + N, w1 + 2 * kk, x + 2 * kk, C::kIdesc, kk != 0);
                 }
-                __syncwarp();
+                mma_commit(&hd->tfull[b]);
+                mma_commit(&hd->empty[s]);
+            }
+            __syncwarp();
+            if (++s == n_stage) {
+                s = 0;
+                ph ^= 1;
             }
         }
         if (one) {
@@ -254,121 +295,146 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
         __syncwarp();
     } else {
         // ------------------------------------------------------------ epilogue
-        const int q = warp & 3, th = q * 32 + lane;  // row of the weight tile
+        // th: row of the weight tile; columns c0 .. c0 + kOwn; et: thread of the epilogue
+        constexpr int kOwn = C::kOwn, kEt = 32 * C::kEpi;
+        const int q = warp & 3, th = q * 32 + lane, half = (warp - 2) >> 2, c0 = half * kOwn;
+        const int et = half * 128 + th;
         bool dead = false;  // a wait gave up: keep the barriers, skip the work
-        uint32_t it = 0;
-        while (share.next(t, kb0, kb1, first, last)) {
-            float acc[C::kMats][N];
+        uint32_t it = 0, piece = 0;
+        ptx::grid_dependency_wait();  // (x's scales; the result's last readers)
+        for (; share.next(t, kb0, kb1, first, last); ++piece) {
+            uint64_t sum[C::kMats][kOwn / 2];  // two columns each
 #pragma unroll
             for (int m = 0; m < C::kMats; ++m)
 #pragma unroll
-                for (int i = 0; i < N; ++i) acc[m][i] = 0.f;
+                for (int i = 0; i < kOwn / 2; ++i) sum[m][i] = 0;
             const float *sw0 = a.s0 + ((size_t)t.e * nwt + t.wt) * nk;
             const float *sw1 = UP ? a.s1 + ((size_t)t.e * nwt + t.wt) * nk : nullptr;
-            const float *sx = a.xs + t.s0 + th;
-            const bool mine = th < t.cnt;
+            const float *sx = a.xs + t.s0 + et;
+            const bool mine = et < t.cnt;
             float nx = mine ? sx[(size_t)kb0 * a.S] : 0.f, n0 = sw0[kb0], n1 = UP ? sw1[kb0] : 0.f;
             for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                const uint32_t b = it % kQsAcc, bph = (it / kQsAcc) & 1;
-                if (th < N) {
-                    hd->scale[it & 1][0][th] = nx * n0;
-                    if (UP) hd->scale[it & 1][1][th] = nx * n1;
+                const uint32_t b = it % kAcc, bph = (it / kAcc) & 1;
+                if (et < N) {
+                    hd->scale[it & 1][0][et] = nx * n0;
+                    if (UP) hd->scale[it & 1][1][et] = nx * n1;
                 }
                 if (kb + 1 < kb1) {
                     nx = mine ? sx[(size_t)(kb + 1) * a.S] : 0.f;
                     n0 = sw0[kb + 1];
                     if (UP) n1 = sw1[kb + 1];
+                } else if (first != last && et == 0) {
+                    // are the tile's other pieces all done?  (That of its first k-blocks is the
+                    // last of a CTA's share, the others the first ones of theirs.)
+                    hd->ready[piece & 1] = load_acquire(a.count + first) == last - first;
                 }
-                ptx::named_bar_sync(1, 128);
+                ptx::named_bar_sync(1, kEt);
                 if (!dead) dead = !__all_sync(0xffffffffu, wait_soon(&hd->tfull[b], bph, a.err));
                 tc_fence_after();
-                const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + b * C::kCols;
+                const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + b * C::kCols + c0;
+                if (!dead) {
 #pragma unroll
-                for (int m = 0; m < C::kMats; ++m)
-#pragma unroll
-                    for (int c = 0; c < N; c += 16) {
-                        float v[16];
-                        if (!dead) {
-                            tmem_ld16(base + m * N + c, v);
-                            tmem_ld_wait();
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) v[i] = 0.f;
+                    for (int m = 0; m < C::kMats; ++m) {
+                        float v[kOwn];
+                        if constexpr (kOwn == 16) tmem_ld16(base + m * N, v);
+                        else tmem_ld32(base + m * N, v);
+                        tmem_ld_wait();
+                        if (m == C::kMats - 1) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) ptx::mbar_arrive(&hd->tempty[b]);
                         }
+                        const ulonglong2 *sc =
+                            reinterpret_cast<const ulonglong2 *>(&hd->scale[it & 1][m][c0]);
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
-                            const float4 sc = *reinterpret_cast<const float4 *>(&hd->scale[it & 1][m][c + i]);
-                            acc[m][c + i] = fmaf(sc.x, v[i], acc[m][c + i]);
-                            acc[m][c + i + 1] = fmaf(sc.y, v[i + 1], acc[m][c + i + 1]);
-                            acc[m][c + i + 2] = fmaf(sc.z, v[i + 2], acc[m][c + i + 2]);
-                            acc[m][c + i + 3] = fmaf(sc.w, v[i + 3], acc[m][c + i + 3]);
+                        for (int i = 0; i < kOwn / 4; ++i) {
+                            const ulonglong2 f = sc[i];
+                            fma2(sum[m][2 * i], v[4 * i], v[4 * i + 1], f.x);
+                            fma2(sum[m][2 * i + 1], v[4 * i + 2], v[4 * i + 3], f.y);
                         }
                     }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(&hd->tempty[b]);
+                }
             }
+            float acc[C::kMats][kOwn];
+#pragma unroll
+            for (int m = 0; m < C::kMats; ++m)
+#pragma unroll
+                for (int i = 0; i < kOwn / 2; ++i) {
+                    const float2 f = both(sum[m][i]);
+                    acc[m][2 * i] = f.x;
+                    acc[m][2 * i + 1] = f.y;
+                }
             if (first != last) {
-                // this piece into its slot: a CTA's last piece may begin a tile that the next
-                // ones end, its others end or continue one
+                // Slots of pieces: a CTA's last piece may begin a tile that the next ones end, its
+                // others end or continue one.
                 constexpr size_t kSlot = (size_t)C::kMats * N * 128;
-                float *mine_p = a.part + (size_t)(2 * share.cta + (kb0 == 0 ? 1 : 0)) * kSlot + th;
-#pragma unroll
-                for (int m = 0; m < C::kMats; ++m)
-#pragma unroll
-                    for (int i = 0; i < N; ++i) mine_p[(m * N + i) * 128] = acc[m][i];
-                __threadfence();
-                ptx::named_bar_sync(1, 128);
-                if (th == 0) hd->last = atomicAdd(a.count + first, 1) == last - first;
-                ptx::named_bar_sync(1, 128);
-                if (!hd->last) continue;
-                __threadfence();
-#pragma unroll
-                for (int m = 0; m < C::kMats; ++m)
-#pragma unroll
-                    for (int i = 0; i < N; ++i) acc[m][i] = 0.f;
-                for (int c = first; c <= last; ++c) {
-                    const float *p = a.part + (size_t)(2 * c + (c == first ? 1 : 0)) * kSlot + th;
+                bool whole = hd->ready[piece & 1];
+                if (!whole) {
+                    float *to = a.part + (size_t)(2 * share.cta + (kb0 == 0 ? 1 : 0)) * kSlot + c0 * 128 + th;
 #pragma unroll
                     for (int m = 0; m < C::kMats; ++m)
 #pragma unroll
-                        for (int i = 0; i < N; ++i) acc[m][i] += __ldcg(p + (m * N + i) * 128);
+                        for (int i = 0; i < kOwn; ++i) to[(m * N + i) * 128] = acc[m][i];
+                    ptx::named_bar_sync(1, kEt);
+                    // (the barrier hands this thread the others' writes, its release all of them)
+                    if (et == 0) hd->last = add_acq_rel(a.count + first, 1) == last - first;
+                    ptx::named_bar_sync(1, kEt);
+                    whole = hd->last;
+                }
+                if (!whole) continue;
+                // in the order of the k-blocks, whoever adds: the sums are the same bits
+                float own[C::kMats][kOwn];
+#pragma unroll
+                for (int m = 0; m < C::kMats; ++m)
+#pragma unroll
+                    for (int i = 0; i < kOwn; ++i) {
+                        own[m][i] = acc[m][i];
+                        acc[m][i] = 0.f;
+                    }
+                for (int c = first; c <= last; ++c) {
+                    const float *p = a.part + (size_t)(2 * c + (c == first ? 1 : 0)) * kSlot + c0 * 128 + th;
+                    const bool me = c == share.cta;
+#pragma unroll
+                    for (int m = 0; m < C::kMats; ++m)
+#pragma unroll
+                        for (int i = 0; i < kOwn; ++i)
+                            acc[m][i] += me ? own[m][i] : __ldcg(p + (m * N + i) * 128);
                 }
             }
             const int row = t.wt * 128 + th;
             if (UP) {
                 // h in place of a; its largest magnitude of each column over the 128 rows
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
+                for (int i = 0; i < kOwn; ++i) {
                     acc[0][i] = q_silu(acc[0][i]) * acc[C::kMats - 1][i];
                     const uint32_t m = __reduce_max_sync(0xffffffffu, abs_bits(acc[0][i]));
-                    if (lane == 0) hd->amax[q][i] = m;
+                    if (lane == 0) hd->amax[q][c0 + i] = m;
                 }
-                ptx::named_bar_sync(1, 128);
-                uint8_t *h = static_cast<uint8_t *>(a.out) + (size_t)t.s0 * a.n_out + row;
+                ptx::named_bar_sync(1, kEt);
+                uint8_t *h = static_cast<uint8_t *>(a.out) + (size_t)(t.s0 + c0) * a.n_out + row;
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    if (i < t.cnt) {
-                        const uint32_t m = max(max(hd->amax[0][i], hd->amax[1][i]),
-                                               max(hd->amax[2][i], hd->amax[3][i]));
+                for (int i = 0; i < kOwn; ++i) {
+                    if (c0 + i < t.cnt) {
+                        const uint32_t m = max(max(hd->amax[0][c0 + i], hd->amax[1][c0 + i]),
+                                               max(hd->amax[2][c0 + i], hd->amax[3][c0 + i]));
                         float sc, inv;
                         q_scale(m, sc, inv);
                         if (row < a.n_out && !dead)
                             h[(size_t)i * a.n_out] = (uint8_t)e4m3x2(acc[0][i] * inv, 0.f);
-                        if (th == i && !dead) a.out_scale[(size_t)t.wt * a.S + t.s0 + i] = sc;
+                        if (th == i && !dead) a.out_scale[(size_t)t.wt * a.S + t.s0 + c0 + i] = sc;
                     }
                 }
             } else if (row < a.n_out && !dead) {
                 if (a.y_bf16) {
-                    bf16 *y = static_cast<bf16 *>(a.out) + (size_t)t.s0 * a.n_out + row;
+                    bf16 *y = static_cast<bf16 *>(a.out) + (size_t)(t.s0 + c0) * a.n_out + row;
 #pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (i < t.cnt) y[(size_t)i * a.n_out] = __float2bfloat16_rn(acc[0][i]);
+                    for (int i = 0; i < kOwn; ++i)
+                        if (c0 + i < t.cnt) y[(size_t)i * a.n_out] = __float2bfloat16_rn(acc[0][i]);
                 } else {
-                    float *y = static_cast<float *>(a.out) + (size_t)t.s0 * a.n_out + row;
+                    float *y = static_cast<float *>(a.out) + (size_t)(t.s0 + c0) * a.n_out + row;
 #pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (i < t.cnt) y[(size_t)i * a.n_out] = acc[0][i];
+                    for (int i = 0; i < kOwn; ++i)
+                        if (c0 + i < t.cnt) y[(size_t)i * a.n_out] = acc[0][i];
                 }
             }
         }
@@ -381,7 +447,8 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
 }
 
 template <bool UP, int N>
-cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QsArgs a, cudaStream_t st) {
+cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QsArgs a, bool alone,
+                   cudaStream_t st) {
     using C = QsCfg<UP, N>;
     CUtensorMap mw0, mw1, mx;
     if (!q_weight_map(&mw0, w0, g.E, g.n_out, g.n_in) ||
@@ -390,7 +457,7 @@ cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QsArgs a,
         return cudaErrorInvalidValue;
     const void *kern = (const void *)k_quant_stream<UP, N>;
     static SmemOnce smem;
-    cudaError_t e = smem.set(kern, C::kSmem);
+    cudaError_t e = smem.set(kern, C::smem(C::kAlone));
     if (e != cudaSuccess) return e;
     a.offsets = g.offsets;
     a.E = g.E;
@@ -398,11 +465,12 @@ cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QsArgs a,
     a.n_in = g.n_in;
     a.n_out = g.n_out;
     a.xs = g.xs;
+    a.stages = alone ? C::kAlone : C::kShared;
     a.err = device_info().err;
     void *args[] = {&mw0, &mw1, &mx, &a};
     LaunchScope ls(UP ? "quant_up_stream" : "quant_down_stream", st);
-    return launch_pdl(kern, dim3(std::min(device_info().sm_count, kQMaxCtas)), dim3(kQsThreads),
-                      C::kSmem, st, args);
+    return launch_pdl(kern, dim3(std::min(device_info().sm_count, kQMaxCtas)), dim3(C::kThreads),
+                      C::smem(a.stages), st, args);
 }
 
 }  // namespace
@@ -416,22 +484,22 @@ cudaError_t launch_quant_stream_up(const QuantGemm &g, const QuantUp &u, const Q
     a.out_scale = u.hs;
     a.part = p.part;
     a.count = p.count;
-    if (cols == 16) return launch<true, 16>(g, u.w1, u.v1, a, st);
-    if (cols == 32) return launch<true, 32>(g, u.w1, u.v1, a, st);
-    return launch<true, 64>(g, u.w1, u.v1, a, st);
+    if (cols == 16) return launch<true, 16>(g, u.w1, u.v1, a, false, st);
+    if (cols == 32) return launch<true, 32>(g, u.w1, u.v1, a, false, st);
+    return launch<true, 64>(g, u.w1, u.v1, a, false, st);
 }
 
 cudaError_t launch_quant_stream_down(const QuantGemm &g, const QuantDown &u, const QuantParts &p,
-                                     int cols, cudaStream_t st) {
+                                     int cols, bool alone, cudaStream_t st) {
     QsArgs a{};
     a.s0 = u.s;
     a.out = u.y;
     a.y_bf16 = u.y_bf16;
     a.part = p.part;
     a.count = p.count;
-    if (cols == 16) return launch<false, 16>(g, u.w, nullptr, a, st);
-    if (cols == 32) return launch<false, 32>(g, u.w, nullptr, a, st);
-    return launch<false, 64>(g, u.w, nullptr, a, st);
+    if (cols == 16) return launch<false, 16>(g, u.w, nullptr, a, alone, st);
+    if (cols == 32) return launch<false, 32>(g, u.w, nullptr, a, alone, st);
+    return launch<false, 64>(g, u.w, nullptr, a, alone, st);
 }
 
 }  // namespace moe
