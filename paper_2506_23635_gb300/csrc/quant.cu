@@ -14,9 +14,8 @@ namespace {
 // the scales block by block ([blocks, rows * K]), as the products read them.
 // ===========================================================================
 constexpr int kRowsThreads = 256;
-constexpr int kRowsUnroll = 4;
 
-template <typename TX>
+template <typename TX, int U>
 __global__ void __launch_bounds__(kRowsThreads)
 k_quant_rows(int rows, int cols, int K, const TX *__restrict__ x,
              const int32_t *__restrict__ inv_perm, uint8_t *__restrict__ q,
@@ -26,73 +25,101 @@ k_quant_rows(int rows, int cols, int K, const TX *__restrict__ x,
     if (count && blockIdx.x == 0)
         for (int i = threadIdx.x; i < n_count; i += kRowsThreads) count[i] = 0;
     const int nb = q_blocks(cols), sub = threadIdx.x & 15;
-    const long long items = (long long)rows * nb;
-    const long long stride = (long long)gridDim.x * (kRowsThreads / 16);
-    long long it = (long long)blockIdx.x * (kRowsThreads / 16) + (threadIdx.x >> 4);
-    // every 16 lanes go through the same number of steps: the shuffles take whole warps
-    const long long steps = (items + stride * kRowsUnroll - 1) / (stride * kRowsUnroll);
-    for (long long s = 0; s < steps; ++s, it += stride * kRowsUnroll) {
-        float v[kRowsUnroll][8];
+    // blocks of a row in runs of U; 16 lanes take a run (the shuffles take whole warps, so
+    // both halves of a warp go on to its last run)
+    const unsigned runs = (unsigned)(nb + U - 1) / U;
+    const long long items = (long long)rows * runs, stride = (long long)gridDim.x * (kRowsThreads / 16);
+    const long long first = (long long)blockIdx.x * (kRowsThreads / 16) + (threadIdx.x >> 4);
+    for (long long i = first; i - (threadIdx.x >> 4 & 1) < items; i += stride) {
+        const bool in = i < items;
+        const int row = in ? (int)(i / runs) : 0, b0 = in ? (int)(i - (long long)row * runs) * U : nb;
+        const TX *src = x + (size_t)row * cols + sub * 8;
+        float v[U][8];
 #pragma unroll
-        for (int u = 0; u < kRowsUnroll; ++u) {
-            const long long i = it + u * stride;
-            const int row = (int)(i / nb), c = ((int)(i - (long long)row * nb) << 7) + sub * 8;
-            if (i < items && c < cols) load8(x + (size_t)row * cols + c, v[u]);
+        for (int u = 0; u < U; ++u) {
+            if ((b0 + u) * 128 + sub * 8 < cols) stream8(src + (b0 + u) * 128, v[u]);
             else
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[u][j] = 0.f;
         }
+        float sc[U];
+        uint2 w[U];
 #pragma unroll
-        for (int u = 0; u < kRowsUnroll; ++u) {
+        for (int u = 0; u < U; ++u) {
             uint32_t m = 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[u][j]));
 #pragma unroll
             for (int o = 1; o < 16; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-            float sc, inv;
-            q_scale(m, sc, inv);
-            const long long i = it + u * stride;
-            if (i >= items) continue;
-            const int row = (int)(i / nb), b = (int)(i - (long long)row * nb), c = (b << 7) + sub * 8;
-            const uint2 w = make_uint2(q_pack4(v[u][0], v[u][1], v[u][2], v[u][3], inv),
-                                       q_pack4(v[u][4], v[u][5], v[u][6], v[u][7], inv));
-            const int copies = K > 0 ? K : 1;
-            for (int k = 0; k < copies; ++k) {
-                const int j = K > 0 ? inv_perm[(size_t)row * K + k] : row;
-                if (j < 0) continue;
-                if (c < cols) *reinterpret_cast<uint2 *>(q + (size_t)j * cols + c) = w;
-                if (sub == 0) scale[K > 0 ? (size_t)b * rows * K + j : (size_t)j * nb + b] = sc;
+            float inv;
+            q_scale(m, sc[u], inv);
+            w[u] = make_uint2(q_pack4(v[u][0], v[u][1], v[u][2], v[u][3], inv),
+                              q_pack4(v[u][4], v[u][5], v[u][6], v[u][7], inv));
+        }
+        const int copies = K > 0 ? K : 1;
+        for (int k = 0; in && k < copies; ++k) {
+            const int j = K > 0 ? inv_perm[(size_t)row * K + k] : row;
+            if (j < 0) continue;
+            uint8_t *to = q + (size_t)j * cols + sub * 8;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int b = b0 + u;
+                if (b * 128 + sub * 8 < cols) *reinterpret_cast<uint2 *>(to + b * 128) = w[u];
+                if (sub == u && b < nb)
+                    scale[K > 0 ? (size_t)b * rows * K + j : (size_t)j * nb + b] = sc[u];
             }
         }
     }
 }
 
-// Quantising matrices: a block of 256 threads holds 128 x 128 numbers in registers.
+// Quantising matrices: a block of 256 threads holds 128 x 128 numbers in registers, as
+// they were loaded.
+__device__ __forceinline__ void hold8(const bf16 *p, uint4 (&r)[1]) { r[0] = ld_stream16(p); }
+__device__ __forceinline__ void hold8(const float *p, uint4 (&r)[2]) {
+    r[0] = ld_stream16(p);
+    r[1] = ld_stream16(p + 4);
+}
+__device__ __forceinline__ void held8(const uint4 (&r)[1], float (&o)[8]) {
+    unpack_bf16x2(r[0].x, o[0], o[1]);
+    unpack_bf16x2(r[0].y, o[2], o[3]);
+    unpack_bf16x2(r[0].z, o[4], o[5]);
+    unpack_bf16x2(r[0].w, o[6], o[7]);
+}
+__device__ __forceinline__ void held8(const uint4 (&r)[2], float (&o)[8]) {
+    o[0] = __uint_as_float(r[0].x); o[1] = __uint_as_float(r[0].y);
+    o[2] = __uint_as_float(r[0].z); o[3] = __uint_as_float(r[0].w);
+    o[4] = __uint_as_float(r[1].x); o[5] = __uint_as_float(r[1].y);
+    o[6] = __uint_as_float(r[1].z); o[7] = __uint_as_float(r[1].w);
+}
+
 template <typename TX>
 __global__ void __launch_bounds__(256)
 k_quant_blocks(int rows, int cols, const TX *__restrict__ w, uint8_t *__restrict__ q,
                float *__restrict__ scale) {
     __shared__ uint32_t red[8];
     const int nb = q_blocks(cols), nr = q_blocks(rows);
-    const long long blk = blockIdx.x;
+    const unsigned blk = blockIdx.x;
     const int b = (int)(blk % nb), r = (int)(blk / nb % nr);
-    const long long n = blk / nb / nr;
+    const unsigned n = blk / nb / nr;
     const int c = b * 128 + (threadIdx.x & 15) * 8, r0 = r * 128 + (threadIdx.x >> 4);
     const size_t base = (size_t)n * rows * cols + c;
-    float v[8][8];
+    uint4 v[8][sizeof(TX) / 2];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int row = r0 + 16 * i;
-        if (row < rows && c < cols) load8(w + base + (size_t)row * cols, v[i]);
+        if (row < rows && c < cols) hold8(w + base + (size_t)row * cols, v[i]);
         else
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+            for (int j = 0; j < (int)sizeof(TX) / 2; ++j) v[i][j] = make_uint4(0, 0, 0, 0);
     }
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 8; ++i) {
+        float f[8];
+        held8(v[i], f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[i][j]));
+        for (int j = 0; j < 8; ++j) m = max(m, abs_bits(f[j]));
+    }
     m = __reduce_max_sync(0xffffffffu, m);
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
     __syncthreads();
@@ -104,10 +131,12 @@ k_quant_blocks(int rows, int cols, const TX *__restrict__ w, uint8_t *__restrict
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int row = r0 + 16 * i;
-        if (row < rows && c < cols)
+        if (row < rows && c < cols) {
+            float f[8];
+            held8(v[i], f);
             *reinterpret_cast<uint2 *>(q + base + (size_t)row * cols) =
-                make_uint2(q_pack4(v[i][0], v[i][1], v[i][2], v[i][3], inv),
-                           q_pack4(v[i][4], v[i][5], v[i][6], v[i][7], inv));
+                make_uint2(q_pack4(f[0], f[1], f[2], f[3], inv), q_pack4(f[4], f[5], f[6], f[7], inv));
+        }
     }
 }
 
@@ -407,16 +436,20 @@ moe_status q_status(cudaError_t e) { return e == cudaSuccess ? MOE_OK : MOE_ERR_
 cudaError_t launch_rows(int rows, int cols, int K, const void *x, int32_t x_dtype,
                         const int32_t *inv, void *q, float *scale, int *count, int n_count,
                         cudaStream_t st) {
-    const long long items = (long long)rows * q_blocks(cols);
-    const long long per = (kRowsThreads / 16) * (long long)kRowsUnroll;
-    const int cap = device_info().sm_count * 8;
-    const int grid = (int)std::max(1LL, std::min<long long>((items + per - 1) / per, cap));
+    // runs of 4 blocks where that leaves every SM several, else single blocks
+    const int sms = device_info().sm_count, nb = q_blocks(cols);
+    const bool runs = (long long)rows * nb >= (long long)sms * 128;
+    const int U = runs ? 4 : 1;
+    const long long items = (long long)rows * ((nb + U - 1) / U);
+    const int grid = (int)std::max(1LL, std::min<long long>((items + kRowsThreads / 16 - 1) / (kRowsThreads / 16),
+                                                            sms * 8LL));
     uint8_t *qp = static_cast<uint8_t *>(q);
     void *args[] = {&rows, &cols, &K, &x, &inv, &qp, &scale, &count, &n_count};
     LaunchScope ls("quant_rows", st);
-    return launch_pdl(x_dtype == MOE_BF16 ? (const void *)k_quant_rows<bf16>
-                                          : (const void *)k_quant_rows<float>,
-                      dim3(grid), dim3(kRowsThreads), 0, st, args);
+    const void *kern = x_dtype == MOE_BF16
+                           ? (runs ? (const void *)k_quant_rows<bf16, 4> : (const void *)k_quant_rows<bf16, 1>)
+                           : (runs ? (const void *)k_quant_rows<float, 4> : (const void *)k_quant_rows<float, 1>);
+    return launch_pdl(kern, dim3(grid), dim3(kRowsThreads), 0, st, args);
 }
 
 moe_status check_router(const moe_dims &d, const moe_router *r) {
