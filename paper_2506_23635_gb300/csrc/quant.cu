@@ -163,9 +163,12 @@ k_quant_scales(int S, int nb, const float *__restrict__ in, float *__restrict__ 
 }
 
 // ===========================================================================
-// The choice of experts: one warp a token.  Scores and keys in 32 bits first; where two
-// of the keys that decide lie nearer to each other than the error of 32 bits, the warp
-// does the token again in 64 bits, so that the choice is that of 64 bits.
+// The choice of experts: one warp a token, lane i the experts [i NE, (i + 1) NE).  Scores
+// and keys in 32 bits first; where two of the keys that decide lie nearer to each other
+// than the error of 32 bits, the warp does the token again with more, so that the choice
+// is that of 64 bits (pairs of fp32 tell nearly always; fp64 itself takes 40 us a token).
+// Bound by the latency of its steps and the instructions of K
+// maxima over the warp.
 // ===========================================================================
 constexpr int kSelThreads = 128;
 constexpr int kSelWarps = kSelThreads / 32;
@@ -185,245 +188,612 @@ __device__ __forceinline__ uint32_t key_code(float v) {
     const uint32_t b = __float_as_uint(v + 0.f);
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float key_of(uint32_t code) {  // of a number's code
+    return __uint_as_float((code & 0x80000000u) ? code & 0x7fffffffu : ~code);
+}
 __device__ __forceinline__ unsigned long long key_code(double v) {
     if (isnan(v)) return 1ull;
     const unsigned long long b = (unsigned long long)__double_as_longlong(v + 0.0);
     return (b >> 63) ? ~b : b | 0x8000000000000000ull;
 }
-__device__ __forceinline__ uint32_t warp_max(uint32_t v) { return __reduce_max_sync(0xffffffffu, v); }
-__device__ __forceinline__ unsigned long long warp_max(unsigned long long v) {
+template <typename T> __device__ __forceinline__ T warp_most(T v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
-template <typename F> struct CodeOf;
-template <> struct CodeOf<float> { typedef uint32_t type; };
-template <> struct CodeOf<double> { typedef unsigned long long type; };
-
-__device__ __forceinline__ float sel_exp(float v) { return expf(v); }
-__device__ __forceinline__ double sel_exp(double v) { return exp(v); }
-template <typename F> __device__ __forceinline__ F warp_sum_of(F v) {
+__device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 
-// What 32 bits may be off by: of a score s = exp(d) / z or 1 / (1 + exp(d)), in units of
-// 2^-24: |d| of the subtraction's rounding, 4 of the exponential, 13 of the sum over 256,
-// 2 of the sum and the quotient, doubled for second orders below; of a key, its rounding.
+// What 32 bits may be off by, of a score s, in steps of 2^-24.  exp(d) / z: |d| of the
+// subtraction's rounding, 4 of the exponential, 4 + 13 of its sum over 256, 3 of the quotient
+// by a reciprocal.  1 / (1 + exp(-d)): 4 + 2.4 |d| of the fast exponential (2 + 1.18 |d| units
+// in the last place), 1 of the sum, 4 of the fast quotient.
 __device__ __forceinline__ float score_err(float s, float d) {
-    return s * ((24.f + fabsf(d)) * 5.9604645e-8f);
+    return s * ((28.f + 2.5f * fabsf(d)) * 5.9604645e-8f);
 }
+constexpr float kSumErr = 1.2e-7f;  // a key's or a sum's rounding, of either side
 
-template <typename F>
-struct SelWarp {
-    F score[256], key[256];
-    F group[256];  // values of the groups
-    int sel[257];
+// A warp's scratch; what 64 bits need takes the same place.
+struct alignas(16) SelScratch {
+    union {
+        struct {
+            float score[256], key[256], group[256];
+        } f;
+        struct {
+            float2 value[256], group[256];
+        } p;
+        struct {
+            double score[256], group[256];
+        } d;
+    };
+    int16_t sel[264];
 };
 
-// The K (and one more) experts of a token with the largest keys in F's precision;
-// false where 32 bits do not tell.
-template <int NE, typename F>
-__device__ bool select_token(const SelArgs &a, const float *l, SelWarp<F> &w, int lane) {
-    typedef typename CodeOf<F>::type Code;
-    constexpr bool kApprox = sizeof(F) == 4;
-    F v[NE], m = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < NE; ++i) {
-        const int e = i * 32 + lane;
-        v[i] = e < a.E ? (F)l[e] : (F)-INFINITY;
-        m = fmax(m, v[i]);
+// ---- numbers in pairs of fp32 (x + y, |y| at most half a step of x): about 44 bits at
+// fp32's rate, where fp64 runs at a sixtieth of it ------------------------------------
+
+__device__ __forceinline__ float2 pair_sum(float a, float b) {  // exact, any order
+    const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+    return make_float2(s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t)));
+}
+__device__ __forceinline__ float2 pair_norm(float a, float b) {  // |a| >= |b|
+    const float s = __fadd_rn(a, b);
+    return make_float2(s, __fsub_rn(b, __fsub_rn(s, a)));
+}
+__device__ __forceinline__ float2 pair_add(float2 a, float2 b) {
+    const float2 s = pair_sum(a.x, b.x);
+    return pair_norm(s.x, s.y + (a.y + b.y));
+}
+__device__ __forceinline__ float2 pair_div(float2 a, float2 b) {
+    const float r = 1.f / b.x, q = a.x * r;
+    const float rem = fmaf(-q, b.x, a.x) + (a.y - q * b.y);
+    return pair_norm(q, rem * r);
+}
+
+// exp(x) for |x| <= 80, to 2^-40 of itself: exp(x) = 2^(k/16) exp(r), k the nearest whole
+// number to 16 x / log 2, 2^(j/16) for j < 16 from a table (Tang's method, ACM TOMS 15, 1989),
+// exp(r), |r| < 0.022, by its series, the terms beyond r^2 in one fp32 (below 2^-19 and
+// so off by less than 2^-42).  log 2 / 16 in three parts, the first two of 12 bits, so that
+// their products with k are exact.
+__constant__ float2 kPairRoots[16] = {
+    {0x1.000000p+0f, 0.f},
+    {0x1.0b5586p+0f, 0x1.9f3122p-25f},
+    {0x1.172b84p+0f, -0x1.c15742p-27f},
+    {0x1.2387a6p+0f, 0x1.ceac48p-25f},
+    {0x1.306fe0p+0f, 0x1.4636e2p-25f},
+    {0x1.3dea64p+0f, 0x1.824684p-25f},
+    {0x1.4bfdaep+0f, -0x1.593abcp-25f},
+    {0x1.5ab07ep+0f, -0x1.5bd5ecp-27f},
+    {0x1.6a09e6p+0f, 0x1.9fcef4p-26f},
+    {0x1.7a1148p+0f, -0x1.829fd0p-25f},
+    {0x1.8ace54p+0f, 0x1.15506ep-27f},
+    {0x1.9c4918p+0f, 0x1.51f848p-27f},
+    {0x1.ae89fap+0f, -0x1.a94b14p-26f},
+    {0x1.c199bep+0f, -0x1.3d56b2p-27f},
+    {0x1.d5818ep+0f, -0x1.822dbcp-27f},
+    {0x1.ea4afap+0f, 0x1.52486cp-27f},
+};
+__device__ __forceinline__ float2 pair_exp(float2 x) {
+    const float k = rintf(x.x * 0x1.715476p+4f);
+    float2 r = pair_sum(fmaf(-k, 0x1.62e000p-5f, x.x), -k * 0x1.0be000p-19f);
+    r = pair_norm(r.x, r.y + (x.y - k * 0x1.be8e7cp-31f));
+    const float q = __fmul_rn(r.x, r.x), ql = fmaf(r.x, r.x, -q);
+    const float more = q * r.x * fmaf(r.x, fmaf(r.x, fmaf(r.x, 1.f / 720, 1.f / 120), 1.f / 24), 1.f / 6);
+    const float2 a = pair_norm(1.f, r.x), b = pair_norm(a.x, 0.5f * q);
+    const float low = ((r.y + fmaf(r.x, r.y, 0.5f * ql)) + (a.y + b.y)) + more;
+    const int n = (int)k;
+    const float2 t = kPairRoots[n & 15];
+    const float h = __fmul_rn(b.x, t.x);
+    const float2 e = pair_norm(h, fmaf(b.x, t.x, -h) + fmaf(b.x, t.y, low * t.x));
+    const float two = __uint_as_float((uint32_t)((n >> 4) + 127) << 23);
+    return make_float2(e.x * two, e.y * two);
+}
+
+__device__ __forceinline__ unsigned long long key_code(float2 v) {
+    const uint32_t hi = key_code(v.x);  // (NaN: nothing behind it counts)
+    return (unsigned long long)hi << 32 | (hi == 1u ? 0u : key_code(isnan(v.y) ? 0.f : v.y));
+}
+__device__ __forceinline__ bool pair_less(float2 a, float2 b) {
+    return a.x < b.x || (a.x == b.x && a.y < b.y);
+}
+// What a score in pairs may be off by, 16 times over.
+constexpr float kPairErr = 0x1p-36f;
+
+// Group g is one of the `top` with the largest values.
+template <typename F>
+__device__ __forceinline__ bool group_in(const F *value, int G, int top, int g) {
+    const auto mine = key_code(value[g]);
+    int before = 0;
+    for (int h = 0; h < G; ++h) {
+        const auto other = key_code(value[h]);
+        before += other > mine || (other == mine && h < g);
     }
-    F s[NE], err = 0;
-    if (a.sigmoid) {
-        m = 0;
-#pragma unroll
-        for (int i = 0; i < NE; ++i) s[i] = (F)1 / ((F)1 + sel_exp(-v[i]));
-    } else {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
-        F z = 0;
-#pragma unroll
-        for (int i = 0; i < NE; ++i) {
-            s[i] = i * 32 + lane < a.E ? sel_exp(v[i] - m) : (F)0;
-            z += s[i];
-        }
-        z = warp_sum_of(z);
-#pragma unroll
-        for (int i = 0; i < NE; ++i) s[i] /= z;
-    }
-    Code code[NE];
-#pragma unroll
-    for (int i = 0; i < NE; ++i) {
-        const int e = i * 32 + lane;
-        code[i] = 0;
-        if (e < a.E) {
-            const F key = a.bias ? s[i] + (F)a.bias[e] : v[i];
-            code[i] = key_code(key);
-            w.score[e] = s[i];
-            w.key[e] = key;
-            if (kApprox && a.G > 1)
-                err = fmax(err, (F)score_err((float)s[i], (float)(v[i] - m)) +
-                                    (a.bias ? (F)1.2e-7f * fabs((F)a.bias[e]) : (F)0));
-        }
+    return before < top;
+}
+
+// The score 1 / (1 + exp(-x)) in pairs; NaN stays.
+__device__ __forceinline__ float2 pair_sigmoid(float x) {
+    if (isnan(x)) return make_float2(x, 0.f);
+    if (x < -80.f) return make_float2(0.f, 0.f);
+    const float2 e = pair_exp(make_float2(-fminf(x, 80.f), 0.f)), t = pair_sum(1.f, e.x);
+    return pair_div(make_float2(1.f, 0.f), pair_norm(t.x, t.y + e.y));
+}
+
+// The K <= 32 experts chosen are the right ones, but some keys lie near to each other:
+// their order anew (sigmoid scores and a bias); false where pairs do not tell.
+__device__ __noinline__ bool order_pairs(const SelArgs &a, const float *l, SelScratch &w, int lane) {
+    const bool in = lane < a.K;
+    const int e = w.sel[in ? lane : 0];
+    const float x = l[e], b = a.bias[e];
+    const float2 s = pair_sigmoid(x), t = pair_sum(s.x, b);
+    const float2 key = isfinite(t.x) ? pair_norm(t.x, t.y + s.y) : make_float2(s.x + b, 0.f);
+    const unsigned long long mine = key_code(key);
+    int before = 0;
+    bool clear = true;
+    for (int k = 0; k < a.K; ++k) {
+        const float2 y = make_float2(__shfl_sync(0xffffffffu, key.x, k), __shfl_sync(0xffffffffu, key.y, k));
+        const float yx = __shfl_sync(0xffffffffu, x, k), yb = __shfl_sync(0xffffffffu, b, k);
+        const int f = __shfl_sync(0xffffffffu, e, k);
+        const unsigned long long other = key_code(y);
+        before += other > mine || (other == mine && f < e);
+        const bool same = __float_as_uint(yx) == __float_as_uint(x) && __float_as_uint(yb) == __float_as_uint(b);
+        if (in && k != lane && !same && isfinite(y.x) && isfinite(key.x) &&
+            fabsf((key.x - y.x) + (key.y - y.y)) <= 2.f * kPairErr * (1.f + 0x1p-8f * (fabsf(b) + fabsf(yb))))
+            clear = false;
     }
     __syncwarp();
+    if (in) w.sel[before] = (int16_t)e;
+    __syncwarp();
+    return __all_sync(0xffffffffu, clear);
+}
+
+// The token in pairs: its experts in w.sel; false where these do not tell either.
+template <int NE>
+__device__ __noinline__ bool select_pairs(const SelArgs &a, const float *l, SelScratch &w, int lane,
+                                          float m) {
+    // (a rare call finds its instructions far away: loops stay loops)
+    const int e0 = lane * NE;
+    const bool biased = a.bias != nullptr, by_score = !biased && a.group_top == 2 && a.G > 1;
+    float2 z = make_float2(0.f, 0.f);
+    __syncwarp();
+#pragma unroll 1
+    for (int e = lane; e < a.E; e += 32) {
+        const float x = l[e], d = x - m;
+        float2 s;
+        if (a.sigmoid) {
+            s = pair_sigmoid(x);
+        } else {
+            s = make_float2(isnan(d) ? d : 0.f, 0.f);
+            if (d >= -80.f) s = pair_exp(pair_sum(x, -m));
+            z = pair_add(z, s);
+        }
+        w.p.value[e] = s;
+    }
+    if (!a.sigmoid)
+#pragma unroll 1
+        for (int o = 16; o > 0; o >>= 1)
+            z = pair_add(z, make_float2(__shfl_xor_sync(0xffffffffu, z.x, o),
+                                        __shfl_xor_sync(0xffffffffu, z.y, o)));
+    float err = 0.f;
+#pragma unroll 1
+    for (int e = lane; e < a.E; e += 32) {
+        float2 s = w.p.value[e];
+        if (!a.sigmoid) s = pair_div(s, z);
+        const float b = biased ? a.bias[e] : 0.f;
+        err = fmaxf(err, kPairErr * (fabsf(s.x) + 0x1p-8f * fabsf(b)));
+        if (biased) {
+            const float2 t = pair_sum(s.x, b);
+            s = isfinite(t.x) ? pair_norm(t.x, t.y + s.y) : make_float2(s.x + b, 0.f);
+        } else if (!by_score) {
+            s = make_float2(l[e], 0.f);
+        }
+        w.p.value[e] = s;
+    }
+    err = warp_most(err) + 0x1p-100f;
+    __syncwarp();
     bool clear = true;
+    unsigned long long code[NE];
+#pragma unroll
+    for (int i = 0; i < NE; ++i)
+        code[i] = e0 + i >= a.E ? 0ull : by_score ? key_code(make_float2(l[e0 + i], 0.f))
+                                                  : key_code(w.p.value[e0 + i]);
     if (a.G > 1) {
         const int gs = a.E / a.G;
         int P = 1;
-        while (2 * P * a.G <= 32) P <<= 1;
-        const bool by_score = !a.bias && a.group_top == 2;
-        if (kApprox)
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) err = fmax(err, __shfl_xor_sync(0xffffffffu, err, o));
+        while (2 * P * a.G <= 32 && 2 * P <= gs) P <<= 1;
+        const float2 none = make_float2(-INFINITY, 0.f);
+#pragma unroll 1
         for (int g0 = 0; g0 < a.G; g0 += 32 / P) {
             const int g = g0 + lane / P;
-            F t1 = -INFINITY, t2 = -INFINITY;
-            if (g < a.G)
-                for (int i = lane % P; i < gs; i += P) {
-                    F k = by_score ? w.score[g * gs + i] : w.key[g * gs + i];
-                    if (isnan(k)) k = -INFINITY;
-                    t2 = fmax(t2, fmin(t1, k));
-                    t1 = fmax(t1, k);
+            float2 t1 = none, t2 = none;
+            auto take = [&](float2 k) {
+                if (isnan(k.x)) k = none;
+                if (pair_less(t1, k)) {
+                    t2 = t1;
+                    t1 = k;
+                } else if (pair_less(t2, k)) {
+                    t2 = k;
                 }
+            };
+            if (g < a.G)
+#pragma unroll 1
+                for (int i = lane & (P - 1); i < gs; i += P) take(w.p.value[g * gs + i]);
+#pragma unroll 1
             for (int o = 1; o < P; o <<= 1) {
-                const F o1 = __shfl_xor_sync(0xffffffffu, t1, o), o2 = __shfl_xor_sync(0xffffffffu, t2, o);
-                t2 = fmax(fmin(t1, o1), fmax(t2, o2));
-                t1 = fmax(t1, o1);
+                const float2 o1 = make_float2(__shfl_xor_sync(0xffffffffu, t1.x, o),
+                                              __shfl_xor_sync(0xffffffffu, t1.y, o));
+                const float2 o2 = make_float2(__shfl_xor_sync(0xffffffffu, t2.x, o),
+                                              __shfl_xor_sync(0xffffffffu, t2.y, o));
+                take(o1);
+                take(o2);
             }
-            if (g < a.G && lane % P == 0) w.group[g] = a.group_top == 2 ? t1 + t2 : t1;
+            if (g < a.G && (lane & (P - 1)) == 0) {
+                float2 v = t1;
+                if (a.group_top == 2)
+                    v = isfinite(t1.x) && isfinite(t2.x) ? pair_add(t1, t2) : make_float2(t1.x + t2.x, 0.f);
+                w.p.group[g] = v;
+            }
         }
         __syncwarp();
-        // a group's rank: how many are before it
-        uint32_t out = 0;  // of this lane's experts
-        F low = INFINITY, high = -INFINITY;  // the worst kept, the best left out
+        // the worst group kept, the best left out
+        float2 low = make_float2(INFINITY, 0.f), high = none;
+#pragma unroll 1
         for (int g0 = 0; g0 < a.G; g0 += 32) {
             const int g = g0 + lane;
             bool in = false;
             if (g < a.G) {
-                const F mine = w.group[g];
-                const Code cm = key_code(mine);
-                int before = 0;
-                for (int h = 0; h < a.G; ++h) {
-                    const Code ch = key_code(w.group[h]);
-                    before += ch > cm || (ch == cm && h < g);
-                }
-                in = before < a.top_groups;
-                const F x = isnan(mine) ? (F)-INFINITY : mine;
-                if (in) low = fmin(low, x);
-                else high = fmax(high, x);
+                in = group_in(w.p.group, a.G, a.top_groups, g);
+                float2 x = w.p.group[g];
+                if (isnan(x.x)) x = none;
+                if (in && pair_less(x, low)) low = x;
+                if (!in && pair_less(high, x)) high = x;
             }
             const uint32_t kept = __ballot_sync(0xffffffffu, in);
 #pragma unroll
             for (int i = 0; i < NE; ++i) {
-                const int e = i * 32 + lane, of = e / gs - g0;
-                if (e < a.E && of >= 0 && of < 32 && !((kept >> of) & 1u)) out |= 1u << i;
+                const int of_g = (e0 + i) / gs - g0;
+                if (of_g >= 0 && of_g < 32 && !((kept >> of_g) & 1u)) code[i] = 0;
             }
         }
-#pragma unroll
-        for (int i = 0; i < NE; ++i)
-            if ((out >> i) & 1u) code[i] = 0;
-        if (kApprox && (a.bias || a.group_top == 2) && a.top_groups < a.G) {
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                low = fmin(low, __shfl_xor_sync(0xffffffffu, low, o));
-                high = fmax(high, __shfl_xor_sync(0xffffffffu, high, o));
-            }
-            // both sides off by up to two keys each and their sum's rounding (infinite
-            // values are exact)
-            if (high > -INFINITY)
-                clear = low < INFINITY &&
-                        low - high > 4 * err + (F)1.2e-7f * (fabs(low) + fabs(high));
+#pragma unroll 1
+        for (int o = 16; o > 0; o >>= 1) {
+            const float2 x = make_float2(__shfl_xor_sync(0xffffffffu, low.x, o),
+                                         __shfl_xor_sync(0xffffffffu, low.y, o));
+            const float2 y = make_float2(__shfl_xor_sync(0xffffffffu, high.x, o),
+                                         __shfl_xor_sync(0xffffffffu, high.y, o));
+            if (pair_less(x, low)) low = x;
+            if (pair_less(high, y)) high = y;
         }
+        if ((biased || by_score) && high.x > -INFINITY)
+            clear = isfinite(low.x) && (low.x - high.x) + (low.y - high.y) > 4.f * err;
     }
-    const int n = kApprox && a.bias ? a.K + 1 : a.K;
+    const int n = biased ? a.K + 1 : a.K;
+#pragma unroll 1
     for (int k = 0; k < n; ++k) {
-        Code best = code[0];
-        int at = lane;
+        unsigned long long best = code[0];
+        int at = 0;
 #pragma unroll
         for (int i = 1; i < NE; ++i)
             if (code[i] > best) {
                 best = code[i];
-                at = i * 32 + lane;
+                at = i;
             }
-        const Code top = warp_max(best);
-        if (top == 0) {  // none is left (only for the one beyond K)
-            if (lane == 0) w.sel[k] = -1;
-            break;
-        }
-        const int e = (int)__reduce_min_sync(0xffffffffu, best == top ? (unsigned)at : 0xffffffffu);
+        const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32));
+        const bool mine = (uint32_t)(best >> 32) == hi;
+        const uint32_t lo = __reduce_max_sync(0xffffffffu, mine ? (uint32_t)best : 0u);
+        const int who = __ffs(__ballot_sync(0xffffffffu, mine && (uint32_t)best == lo)) - 1;
+        if (lane == who) {
+            w.sel[k] = (int16_t)(best ? e0 + at : -1);
 #pragma unroll
-        for (int i = 0; i < NE; ++i)
-            if (i * 32 + lane == e) code[i] = 0;
-        if (lane == 0) w.sel[k] = e;
+            for (int i = 0; i < NE; ++i)
+                if (i == at) code[i] = 0;
+        }
     }
     __syncwarp();
-    if (kApprox && a.bias)
+    if (biased)
         for (int k = lane; k < a.K; k += 32) {
             const int e = w.sel[k], f = w.sel[k + 1];
             if (f < 0) break;
-            const float le = l[e], lf = l[f], be = a.bias[e], bf = a.bias[f];
-            // the same numbers give the same keys
-            if (__float_as_uint(le) == __float_as_uint(lf) && __float_as_uint(be) == __float_as_uint(bf))
+            if (__float_as_uint(l[e]) == __float_as_uint(l[f]) &&
+                __float_as_uint(a.bias[e]) == __float_as_uint(a.bias[f]))
                 continue;
-            const float ke = (float)w.key[e], kf = (float)w.key[f];
-            // an infinite bias or none decides by itself; NaN is below everything
-            if (isnan(ke) || isnan(kf) || isinf(ke) || isinf(kf)) continue;
-            const float off = score_err((float)w.score[e], le - (float)m) +
-                              score_err((float)w.score[f], lf - (float)m) +
-                              1.2e-7f * (fabsf(be) + fabsf(bf));
-            if (!(ke - kf > off)) clear = false;
+            const float2 x = w.p.value[e], y = w.p.value[f];
+            if (isfinite(x.x) && isfinite(y.x) && !((x.x - y.x) + (x.y - y.y) > 2.f * err)) clear = false;
         }
     return __all_sync(0xffffffffu, clear);
 }
 
-template <typename F>
-__device__ void write_choice(const SelArgs &a, int t, SelWarp<F> &w, int lane) {
-    F sum = 0;
-    for (int k = lane; k < a.K; k += 32) sum += w.score[w.sel[k]];
-    sum = warp_sum_of(sum);
+// The token in 64 bits: any sizes, no haste (an equality that pairs leave open).
+__device__ __noinline__ void select_exact(const SelArgs &a, const float *l, SelScratch &w, int lane) {
+    double m = -INFINITY, z = 0;
+    if (!a.sigmoid) {
+        for (int e = lane; e < a.E; e += 32) m = fmax(m, (double)l[e]);
+        m = warp_most(m);
+        for (int e = lane; e < a.E; e += 32) {
+            w.d.score[e] = exp((double)l[e] - m);
+            z += w.d.score[e];
+        }
+        z = warp_sum(z);
+    }
+    for (int e = lane; e < a.E; e += 32) {
+        const double s = a.sigmoid ? 1.0 / (1.0 + exp(-(double)l[e])) : w.d.score[e] / z;
+        w.d.score[e] = s;
+    }
+    __syncwarp();
+    auto key = [&](int e) { return a.bias ? w.d.score[e] + (double)a.bias[e] : (double)l[e]; };
+    const int gs = a.E / a.G;
+    uint32_t out = 0;  // of the experts lane, lane + 32, ...: those out of the choice
+    if (a.G > 1) {
+        const bool by_score = !a.bias && a.group_top == 2;
+        for (int g = lane; g < a.G; g += 32) {
+            double t1 = -INFINITY, t2 = -INFINITY;
+            for (int i = 0; i < gs; ++i) {
+                double k = by_score ? w.d.score[g * gs + i] : key(g * gs + i);
+                if (isnan(k)) k = -INFINITY;
+                t2 = fmax(t2, fmin(t1, k));
+                t1 = fmax(t1, k);
+            }
+            w.d.group[g] = a.group_top == 2 ? t1 + t2 : t1;
+        }
+        __syncwarp();
+        for (int i = 0, e = lane; e < a.E; ++i, e += 32)
+            if (!group_in(w.d.group, a.G, a.top_groups, e / gs)) out |= 1u << i;
+    }
+    for (int k = 0; k < a.K; ++k) {
+        unsigned long long best = 0;
+        int at = 256;
+        for (int i = 0, e = lane; e < a.E; ++i, e += 32) {
+            const unsigned long long c = (out >> i) & 1u ? 0ull : key_code(key(e));
+            if (c > best) {
+                best = c;
+                at = e;
+            }
+        }
+        const unsigned long long top = warp_most(best);
+        const int e = (int)__reduce_min_sync(0xffffffffu, best == top ? (unsigned)at : 256u);
+        if ((e & 31) == lane) out |= 1u << (e >> 5);
+        if (lane == 0) w.sel[k] = (int16_t)e;
+    }
+    __syncwarp();
+}
+
+__device__ void write_exact(const SelArgs &a, int t, const SelScratch &w, int lane) {
+    double sum = 0;
+    for (int k = lane; k < a.K; k += 32) sum += w.d.score[w.sel[k]];
+    sum = warp_sum(sum);
     for (int k = lane; k < a.K; k += 32) {
-        const int e = w.sel[k];
-        const F s = w.score[e];
-        a.idx[(size_t)t * a.K + k] = e;
-        a.gate[(size_t)t * a.K + k] = (float)((a.renorm ? s / sum : s) * (F)a.scale);
+        const double s = w.d.score[w.sel[k]];
+        a.idx[(size_t)t * a.K + k] = w.sel[k];
+        a.gate[(size_t)t * a.K + k] = (float)((a.renorm ? s / sum : s) * (double)a.scale);
+    }
+}
+
+template <int NE>
+__device__ __forceinline__ void keep(float *to, const float (&v)[NE]) {
+    if constexpr (NE >= 4) {
+#pragma unroll
+        for (int i = 0; i < NE; i += 4)
+            *reinterpret_cast<float4 *>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < NE; ++i) to[i] = v[i];
     }
 }
 
 template <int NE>
 __global__ void __launch_bounds__(kSelThreads)
 k_select(const SelArgs a) {
-    __shared__ SelWarp<float> sw[kSelWarps];
-    __shared__ SelWarp<double> dw[1];
-    __shared__ int redo[kSelWarps];
+    __shared__ SelScratch scratch[kSelWarps];
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int t = blockIdx.x * kSelWarps + warp;
-    bool again = false;
-    if (t < a.T) {
-        again = !select_token<NE, float>(a, a.logits + (size_t)t * a.E, sw[warp], lane);
-        // weights whose sum 32 bits hold badly or not at all
-        if (!again && a.renorm) {
-            float sum = 0.f;
-            for (int k = lane; k < a.K; k += 32) sum += sw[warp].score[sw[warp].sel[k]];
-            again = warp_sum(sum) < 1e-30f;
-        }
-        if (!again) write_choice(a, t, sw[warp], lane);
-    }
-    if (lane == 0) redo[warp] = again;
-    __syncthreads();
-    // (rare: one warp after another, in one warp's worth of 64-bit scratch)
-    if (warp == 0)
-        for (int i = 0; i < kSelWarps; ++i)
-            if (redo[i]) {
-                const int u = blockIdx.x * kSelWarps + i;
-                select_token<NE, double>(a, a.logits + (size_t)u * a.E, dw[0], lane);
-                write_choice(a, u, dw[0], lane);
-                __syncwarp();
+    if (t >= a.T) return;
+    SelScratch &w = scratch[warp];
+    const float *l = a.logits + (size_t)t * a.E;
+    const int e0 = lane * NE;
+    const bool biased = a.bias != nullptr, by_score = !biased && a.group_top == 2 && a.G > 1;
+    float v[NE], s[NE], b[NE], m = 0.f, z = 1.f;
+#pragma unroll
+    for (int i = 0; i < NE; ++i) v[i] = -INFINITY;
+    if (NE >= 4 && a.E % 4 == 0) {  // (rows of 16-byte multiples)
+#pragma unroll
+        for (int i = 0; i + 4 <= NE; i += 4)
+            if (e0 + i < a.E) {
+                const float4 f = *reinterpret_cast<const float4 *>(l + e0 + i);
+                v[i] = f.x;
+                v[i + 1] = f.y;
+                v[i + 2] = f.z;
+                v[i + 3] = f.w;
             }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NE; ++i)
+            if (e0 + i < a.E) v[i] = l[e0 + i];
+    }
+#pragma unroll
+    for (int i = 0; i < NE; ++i) b[i] = biased && e0 + i < a.E ? a.bias[e0 + i] : 0.f;
+    if (!a.sigmoid) {
+        m = v[0];
+#pragma unroll
+        for (int i = 1; i < NE; ++i) m = fmaxf(m, v[i]);
+        m = warp_most(m);
+        z = 0.f;
+#pragma unroll
+        for (int i = 0; i < NE; ++i) {
+            s[i] = e0 + i < a.E ? expf(v[i] - m) : 0.f;
+            z += s[i];
+        }
+        z = moe::warp_sum(z);
+        const float inv = 1.f / z;
+#pragma unroll
+        for (int i = 0; i < NE; ++i) s[i] *= inv;
+    } else if (biased || by_score) {
+#pragma unroll
+        for (int i = 0; i < NE; ++i) s[i] = __fdividef(1.f, 1.f + __expf(-v[i]));
+    }
+    uint32_t code[NE];
+    float err = 0.f, kv[NE];  // of the keys
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+        const float key = biased ? s[i] + b[i] : v[i];
+        code[i] = e0 + i < a.E ? key_code(key) : 0u;
+        kv[i] = key;
+        if ((biased || by_score) && a.G > 1 && e0 + i < a.E)
+            err = fmaxf(err, score_err(s[i], v[i] - m) + kSumErr * fabsf(b[i]));
+    }
+    if (biased || by_score) keep<NE>(w.f.score + e0, s);
+    keep<NE>(w.f.key + e0, kv);
+    bool clear = true;
+    if (a.G > 1) {
+        const int gs = a.E / a.G;
+        __syncwarp();
+        // the two largest of each group: of a lane's own experts where it has no other group's
+        // (those of a group are P lanes then), else through shared memory
+        int P = gs / NE;
+        const bool own_group = P * NE == gs && (P & (P - 1)) == 0;
+        if (!own_group)
+            for (P = 1; 2 * P * a.G <= 32 && 2 * P <= gs;) P <<= 1;
+        const float *of = by_score ? w.f.score : w.f.key;
+        for (int g0 = 0; g0 < a.G; g0 += own_group ? a.G : 32 / P) {
+            const int g = g0 + lane / P;
+            float t1 = -INFINITY, t2 = -INFINITY;
+            auto take = [&](float k) {
+                if (isnan(k)) k = -INFINITY;
+                t2 = fmaxf(t2, fminf(t1, k));
+                t1 = fmaxf(t1, k);
+            };
+            if (own_group) {
+#pragma unroll
+                for (int i = 0; i < NE; ++i) take(by_score ? s[i] : kv[i]);
+            } else if (g < a.G) {
+                for (int i = lane & (P - 1); i < gs; i += P) take(of[g * gs + i]);
+            }
+            for (int o = 1; o < P; o <<= 1) {
+                const float o1 = __shfl_xor_sync(0xffffffffu, t1, o), o2 = __shfl_xor_sync(0xffffffffu, t2, o);
+                t2 = fmaxf(fminf(t1, o1), fmaxf(t2, o2));
+                t1 = fmaxf(t1, o1);
+            }
+            if (g < a.G && (lane & (P - 1)) == 0) w.f.group[g] = a.group_top == 2 ? t1 + t2 : t1;
+        }
+        __syncwarp();
+        uint32_t low = 0xffffffffu, high = 0u;  // the worst kept, the best left out
+        for (int g0 = 0; g0 < a.G; g0 += 32) {
+            const int g = g0 + lane;
+            bool in = false;
+            if (g < a.G) {
+                in = group_in(w.f.group, a.G, a.top_groups, g);
+                const uint32_t c = key_code(w.f.group[g]);
+                if (in) low = min(low, c);
+                else high = max(high, c);
+            }
+            const uint32_t kept = __ballot_sync(0xffffffffu, in);
+            if (own_group) {  // (32 groups at most)
+                if (!((kept >> (lane / P)) & 1u))
+#pragma unroll
+                    for (int i = 0; i < NE; ++i) code[i] = 0u;
+            } else {
+#pragma unroll
+                for (int i = 0; i < NE; ++i) {
+                    const int of_g = (e0 + i) / gs - g0;
+                    if (of_g >= 0 && of_g < 32 && !((kept >> of_g) & 1u)) code[i] = 0u;
+                }
+            }
+        }
+        if ((biased || by_score) && a.top_groups < a.G) {
+            low = __reduce_min_sync(0xffffffffu, low);
+            high = __reduce_max_sync(0xffffffffu, high);
+            err = warp_most(err);
+            // both sides off by up to two keys each and their sum's rounding; NaN and minus
+            // infinity are what they are in 64 bits too
+            if (high > key_code(-INFINITY)) {
+                const float lo = key_of(low), hi = key_of(high);
+                clear = lo < INFINITY && lo - hi > 4.f * err + kSumErr * (fabsf(lo) + fabsf(hi));
+            }
+        }
+    }
+    const int n = biased ? a.K + 1 : a.K;
+    for (int k = 0; k < n; ++k) {
+        uint32_t best = code[0];
+        int at = 0;
+#pragma unroll
+        for (int i = 1; i < NE; ++i)
+            if (code[i] > best) {
+                best = code[i];
+                at = i;
+            }
+        const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+        // (the lowest lane has the lowest experts)
+        const int who = __ffs(__ballot_sync(0xffffffffu, best == top)) - 1;
+        if (lane == who) {
+            w.sel[k] = (int16_t)(top ? e0 + at : -1);  // (none left: only for the one beyond K)
+#pragma unroll
+            for (int i = 0; i < NE; ++i)
+                if (i == at) code[i] = 0u;
+        }
+    }
+    __syncwarp();
+    // order: of the K is clear (clear: which they are); edge: the last one's key is also that
+    // of the first one left out, so that a change of order could change which they are
+    bool order = true, edge = false;
+    if (biased)
+        for (int k = lane; k < a.K; k += 32) {
+            const int e = w.sel[k], f = w.sel[k + 1];
+            if (f < 0) break;
+            const float le = l[e], lf = l[f], be = a.bias[e], bf = a.bias[f];
+            // the same numbers give the same keys
+            if (__float_as_uint(le) == __float_as_uint(lf) && __float_as_uint(be) == __float_as_uint(bf)) {
+                edge = k == a.K - 1;
+                continue;
+            }
+            const float ke = w.f.key[e], kf = w.f.key[f];
+            // an infinite bias decides by itself; NaN is below everything
+            if (isnan(ke) || isnan(kf) || isinf(ke) || isinf(kf)) continue;
+            const float off = score_err(w.f.score[e], le - m) + score_err(w.f.score[f], lf - m) +
+                              kSumErr * (fabsf(be) + fabsf(bf));
+            if (!(ke - kf > off)) (k == a.K - 1 ? clear : order) = false;
+        }
+    clear = __all_sync(0xffffffffu, clear);
+    order = __all_sync(0xffffffffu, order);
+    if (clear && !order) {
+        clear = a.sigmoid && a.K <= 32 && !__any_sync(0xffffffffu, edge);
+        if (clear) clear = order_pairs(a, l, w, lane);
+    }
+    // weights: the scores anew, with the full exponential and quotient
+    float sum = 0.f, own = 0.f;
+    auto weights = [&]() {
+        sum = 0.f;
+        for (int k = lane; k < a.K; k += 32) {
+            const float x = l[w.sel[k]];
+            own = a.sigmoid ? 1.f / (1.f + expf(-x)) : expf(x - m) / z;
+            sum += own;
+        }
+        sum = moe::warp_sum(sum);
+    };
+    weights();
+    // (a sum that 32 bits hold badly or not at all: 64 bits too)
+    const bool tiny = a.renorm && sum < 1e-30f;
+    if (!clear || tiny) {
+        if (tiny || !select_pairs<NE>(a, l, w, lane, m)) {
+            __syncwarp();
+            select_exact(a, l, w, lane);
+            write_exact(a, t, w, lane);
+            return;
+        }
+        weights();
+    }
+    for (int k = lane; k < a.K; k += 32) {
+        const int e = w.sel[k];
+        if (a.K > 32) {
+            const float x = l[e];
+            own = a.sigmoid ? 1.f / (1.f + expf(-x)) : expf(x - m) / z;
+        }
+        a.idx[(size_t)t * a.K + k] = e;
+        a.gate[(size_t)t * a.K + k] = (a.renorm ? own / sum : own) * a.scale;
+    }
 }
 
 // ---- host side ---------------------------------------------------------------
