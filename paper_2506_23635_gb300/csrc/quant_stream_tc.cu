@@ -11,7 +11,8 @@
 //
 // Each k-block is an accumulator of its own in tensor memory (a few in turn): the
 // epilogue multiplies it with the block's scales as it adds it to the sum it keeps in
-// registers.  Warp 0 loads (TMA), warp 1 issues the MMAs, the others are the epilogue: thread
+// registers.  Two sets of epilogue warps take the k-blocks in turn (one set alone took about
+// as long for a k-block as its weights take from memory) and are added at a piece's end.  Warp 0 loads (TMA), warp 1 issues the MMAs, the others are the epilogue: thread
 // i of a warp of lane quarter q has weight row 32 q + i.
 #include "quant.cuh"
 
@@ -24,7 +25,7 @@ constexpr int kQsMinBlocks = 4;     // k-blocks of a CTA's share at least
 constexpr int kQsMaxStages = 12;
 constexpr uint32_t kQsTile = 128 * 128;
 
-constexpr uint32_t kQsHdrBytes = 4096;
+constexpr uint32_t kQsHdrBytes = 7168;
 struct QsHeader {
     uint64_t full[kQsMaxStages], empty[kQsMaxStages];
     uint64_t tfull[4], tempty[4];
@@ -32,7 +33,7 @@ struct QsHeader {
     uint32_t tmem_base;
     int last, ready[2];  // (ready: pieces in turn)
     int prefix[257];       // tiles of the experts ahead
-    alignas(16) float scale[2][2][64];  // of this k-block: x's times w1's (w's), times v1's
+    alignas(16) float scale[8][2][2][32];  // warp, k-blocks in turn: x's times w1's (w's), v1's
     uint32_t amax[4][64];
 };
 static_assert(sizeof(QsHeader) <= kQsHdrBytes, "header");
@@ -41,27 +42,29 @@ template <bool UP, int N>
 struct QsCfg {
     static constexpr int kMats = UP ? 2 : 1;
     static constexpr uint32_t kStage = kMats * kQsTile + N * 128;
-    // epilogue warps: 32 columns each at most, four warps side by side
-    static constexpr int kHalves = N == 64 ? 2 : 1, kEpi = 4 * kHalves, kThreads = 64 + 32 * kEpi;
-    static constexpr int kOwn = N / kHalves;  // columns of a warp
-    // Stages where the up and the down projection's CTAs share an SM, so that the down
-    // projection's first weights arrive during the up projection's end (not with 64 columns,
-    // which take too many registers); alone: as many as fit 200 KB.
-    static constexpr int kShared = N == 64 ? (UP ? 5 : 8) : UP ? 3 : N == 16 ? 6 : 5;
-    static constexpr int kAlone = (int)((200 * 1024) / kStage) < kQsMaxStages
-                                      ? (int)((200 * 1024) / kStage) : kQsMaxStages;
+    // eight epilogue warps: two sets that take the k-blocks in turn, with 64 columns two
+    // halves of them
+    static constexpr int kSets = N == 64 ? 1 : 2, kThreads = 64 + 256;
+    static constexpr int kOwn = N == 64 ? 32 : N;  // columns of a warp
+    // the second set's sums on their way to the first
+    static constexpr uint32_t kSums = kSets == 2 ? kMats * N * 512 : 0;
+    // With 16 columns the up and the down projection's CTAs share an SM, so that the down
+    // projection's first weights arrive during the up projection's end (wider tiles take too many
+    // registers); alone: as many stages as fit.
+    static constexpr int kShared = N != 16 ? 0 : UP ? 3 : 4;
+    static constexpr int kFit = (int)((220 * 1024 - kSums - kQsHdrBytes) / kStage);
+    static constexpr int kAlone = kFit < kQsMaxStages ? kFit : kQsMaxStages;
     static constexpr int kAcc = N == 64 ? 2 : 4;  // accumulators in turn
     static constexpr uint32_t kCols = kMats * N;  // tensor-memory columns of an accumulator
     static constexpr uint32_t kTmem = kAcc * kCols;
     // kind::f8f6f4: e4m3 A and B, fp32 D, both K-major, M = 128
     static constexpr uint32_t kIdesc = (1u << 4) | ((128u >> 4) << 24) | ((uint32_t)(N >> 3) << 17);
-    static constexpr size_t smem(int stages) { return 1024 + stages * kStage + kQsHdrBytes; }
+    static constexpr size_t smem(int stages) { return 1024 + stages * kStage + kSums + kQsHdrBytes; }
     static_assert(kStage % 1024 == 0, "stages stay 1024-byte aligned");
     static_assert(smem(kAlone) <= 227 * 1024, "shared memory");
     static_assert((kTmem & (kTmem - 1)) == 0 && kTmem >= 32 && kTmem <= 256, "tensor memory");
 };
-static_assert(QsCfg<true, 16>::smem(QsCfg<true, 16>::kShared) + QsCfg<false, 16>::smem(QsCfg<false, 16>::kShared) <= 226 * 1024 &&
-              QsCfg<true, 32>::smem(QsCfg<true, 32>::kShared) + QsCfg<false, 32>::smem(QsCfg<false, 32>::kShared) <= 226 * 1024,
+static_assert(QsCfg<true, 16>::smem(QsCfg<true, 16>::kShared) + QsCfg<false, 16>::smem(QsCfg<false, 16>::kShared) <= 226 * 1024,
               "an up and a down projection's CTA on one SM");
 
 __device__ __forceinline__ void tma_3d(void *dst, const CUtensorMap *m, int32_t x, int32_t y,
@@ -93,6 +96,10 @@ __device__ __forceinline__ int add_acq_rel(int *p, int v) {
     return r;
 }
 
+__device__ __forceinline__ void bar_arrive(uint32_t id, uint32_t threads) {
+    asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
 struct QsTile {
     int e, wt;    // expert, 128 weight rows
     int s0, cnt;  // first row of x, rows
@@ -103,14 +110,14 @@ struct QsShare {
     const int *prefix;
     const int32_t *offsets;
     int E, S, nk, cols;
-    long long W, pos, end;
+    long long W, begin, pos, end;
     int ctas, cta;
 
     __device__ __forceinline__ void start(int n_ctas, int me) {
         W = (long long)prefix[E] * nk;
         ctas = (int)max(1LL, min((long long)n_ctas, W / kQsMinBlocks));
         cta = me;
-        pos = me < ctas ? W * me / ctas : W;
+        begin = pos = me < ctas ? W * me / ctas : W;
         end = me < ctas ? W * (me + 1) / ctas : W;
     }
     __device__ __forceinline__ int owner(long long block) const {
@@ -176,7 +183,7 @@ struct QsArgs {
 };
 
 template <bool UP, int N>
-__global__ void __launch_bounds__(QsCfg<UP, N>::kThreads, N == 64 ? 1 : 2)
+__global__ void __launch_bounds__(QsCfg<UP, N>::kThreads, N == 16 ? 2 : 1)
 k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ CUtensorMap tm_w1,
                const __grid_constant__ CUtensorMap tm_x, const QsArgs a) {
     using C = QsCfg<UP, N>;
@@ -185,7 +192,7 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    QsHeader *hd = reinterpret_cast<QsHeader *>(smem + n_stage * C::kStage);
+    QsHeader *hd = reinterpret_cast<QsHeader *>(smem + n_stage * C::kStage + C::kSums);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nk = q_blocks(a.n_in), nwt = q_blocks(a.n_out);
     if (threadIdx.x == 0) {
@@ -195,7 +202,7 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
         }
         for (int b = 0; b < kAcc; ++b) {
             ptx::mbar_init(&hd->tfull[b], 1);
-            ptx::mbar_init(&hd->tempty[b], C::kEpi);
+            ptx::mbar_init(&hd->tempty[b], 8 / C::kSets);
         }
         ptx::mbar_init(&hd->done, 1);
         ptx::fence_barrier_init();
@@ -295,12 +302,15 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
         __syncwarp();
     } else {
         // ------------------------------------------------------------ epilogue
-        // th: row of the weight tile; columns c0 .. c0 + kOwn; et: thread of the epilogue
-        constexpr int kOwn = C::kOwn, kEt = 32 * C::kEpi;
-        const int q = warp & 3, th = q * 32 + lane, half = (warp - 2) >> 2, c0 = half * kOwn;
-        const int et = half * 128 + th;
+        // th: row of the weight tile; columns c0 .. c0 + kOwn; et: thread of the set
+        constexpr int kOwn = C::kOwn, kSets = C::kSets, kEt = 256 / kSets;
+        const int q = warp & 3, th = q * 32 + lane;
+        const int set = kSets == 2 ? (warp - 2) >> 2 : 0, half = kSets == 2 ? 0 : (warp - 2) >> 2;
+        const int c0 = half * kOwn, et = half * 128 + th;
+        float(*scale)[2][32] = hd->scale[warp - 2];
+        float *sums = reinterpret_cast<float *>(smem + n_stage * C::kStage) + c0 * 128 + th;
         bool dead = false;  // a wait gave up: keep the barriers, skip the work
-        uint32_t it = 0, piece = 0;
+        uint32_t it = 0, piece = 0, turn = 0;
         ptx::grid_dependency_wait();  // (x's scales; the result's last readers)
         for (; share.next(t, kb0, kb1, first, last); ++piece) {
             uint64_t sum[C::kMats][kOwn / 2];  // two columns each
@@ -310,26 +320,33 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                 for (int i = 0; i < kOwn / 2; ++i) sum[m][i] = 0;
             const float *sw0 = a.s0 + ((size_t)t.e * nwt + t.wt) * nk;
             const float *sw1 = UP ? a.s1 + ((size_t)t.e * nwt + t.wt) * nk : nullptr;
-            const float *sx = a.xs + t.s0 + et;
-            const bool mine = et < t.cnt;
-            float nx = mine ? sx[(size_t)kb0 * a.S] : 0.f, n0 = sw0[kb0], n1 = UP ? sw1[kb0] : 0.f;
-            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+            // lane i: column c0 + i's scale
+            const bool mine = lane < kOwn && c0 + lane < t.cnt;
+            const float *sx = a.xs + t.s0 + c0 + (mine ? lane : 0);
+            int kb = kb0;
+            if (kSets == 2 && ((it ^ set) & 1)) {
+                ++kb;
+                ++it;
+            }
+            float nx = 0.f, n0 = 0.f, n1 = 0.f;
+            if (kb < kb1) {
+                nx = sx[(size_t)kb * a.S];
+                n0 = sw0[kb];
+                if (UP) n1 = sw1[kb];
+            }
+            for (; kb < kb1; kb += kSets, it += kSets, turn ^= 1) {
                 const uint32_t b = it % kAcc, bph = (it / kAcc) & 1;
-                if (et < N) {
-                    hd->scale[it & 1][0][et] = nx * n0;
-                    if (UP) hd->scale[it & 1][1][et] = nx * n1;
+                if (lane < kOwn) {
+                    scale[turn][0][lane] = nx * n0;
+                    if (UP) scale[turn][1][lane] = nx * n1;
                 }
-                if (kb + 1 < kb1) {
-                    nx = mine ? sx[(size_t)(kb + 1) * a.S] : 0.f;
-                    n0 = sw0[kb + 1];
-                    if (UP) n1 = sw1[kb + 1];
-                } else if (first != last && et == 0) {
-                    // are the tile's other pieces all done?  (That of its first k-blocks is the
-                    // last of a CTA's share, the others the first ones of theirs.)
-                    hd->ready[piece & 1] = load_acquire(a.count + first) == last - first;
+                if (kb + kSets < kb1) {
+                    nx = sx[(size_t)(kb + kSets) * a.S];
+                    n0 = sw0[kb + kSets];
+                    if (UP) n1 = sw1[kb + kSets];
                 }
-                ptx::named_bar_sync(1, kEt);
                 if (!dead) dead = !__all_sync(0xffffffffu, wait_soon(&hd->tfull[b], bph, a.err));
+                __syncwarp();
                 tc_fence_after();
                 const uint32_t base = tmem + ((uint32_t)(q * 32) << 16) + b * C::kCols + c0;
                 if (!dead) {
@@ -344,8 +361,7 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                             __syncwarp();
                             if (lane == 0) ptx::mbar_arrive(&hd->tempty[b]);
                         }
-                        const ulonglong2 *sc =
-                            reinterpret_cast<const ulonglong2 *>(&hd->scale[it & 1][m][c0]);
+                        const ulonglong2 *sc = reinterpret_cast<const ulonglong2 *>(scale[turn][m]);
 #pragma unroll
                         for (int i = 0; i < kOwn / 4; ++i) {
                             const ulonglong2 f = sc[i];
@@ -355,6 +371,26 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                     }
                 }
             }
+            it = (uint32_t)(share.pos - share.begin);  // k-blocks of the share so far
+            if (set == 1) {  // its sums to the first set
+                if (piece) ptx::named_bar_sync(2, 2 * kEt);  // (the last ones are read)
+#pragma unroll
+                for (int m = 0; m < C::kMats; ++m)
+#pragma unroll
+                    for (int i = 0; i < kOwn / 2; ++i) {
+                        const float2 f = both(sum[m][i]);
+                        sums[(m * N + 2 * i) * 128] = f.x;
+                        sums[(m * N + 2 * i + 1) * 128] = f.y;
+                    }
+                bar_arrive(1, 2 * kEt);
+                continue;
+            }
+            // are the tile's other pieces all done?  (That of its first k-blocks is the last of a
+            // CTA's share, the others the first ones of theirs.)
+            if (first != last && et == 0)
+                hd->ready[piece & 1] = load_acquire(a.count + first) == last - first;
+            if (kSets == 2) ptx::named_bar_sync(1, 2 * kEt);
+            else if (first != last) ptx::named_bar_sync(3, kEt);
             float acc[C::kMats][kOwn];
 #pragma unroll
             for (int m = 0; m < C::kMats; ++m)
@@ -363,7 +399,12 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                     const float2 f = both(sum[m][i]);
                     acc[m][2 * i] = f.x;
                     acc[m][2 * i + 1] = f.y;
+                    if (kSets == 2) {
+                        acc[m][2 * i] += sums[(m * N + 2 * i) * 128];
+                        acc[m][2 * i + 1] += sums[(m * N + 2 * i + 1) * 128];
+                    }
                 }
+            if (kSets == 2) bar_arrive(2, 2 * kEt);
             if (first != last) {
                 // Slots of pieces: a CTA's last piece may begin a tile that the next ones end, its
                 // others end or continue one.
@@ -375,31 +416,31 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                     for (int m = 0; m < C::kMats; ++m)
 #pragma unroll
                         for (int i = 0; i < kOwn; ++i) to[(m * N + i) * 128] = acc[m][i];
-                    ptx::named_bar_sync(1, kEt);
+                    ptx::named_bar_sync(3, kEt);
                     // (the barrier hands this thread the others' writes, its release all of them)
                     if (et == 0) hd->last = add_acq_rel(a.count + first, 1) == last - first;
-                    ptx::named_bar_sync(1, kEt);
+                    ptx::named_bar_sync(3, kEt);
                     whole = hd->last;
                 }
                 if (!whole) continue;
                 // in the order of the k-blocks, whoever adds: the sums are the same bits
-                float own[C::kMats][kOwn];
 #pragma unroll
                 for (int m = 0; m < C::kMats; ++m)
 #pragma unroll
-                    for (int i = 0; i < kOwn; ++i) {
-                        own[m][i] = acc[m][i];
-                        acc[m][i] = 0.f;
+                    for (int j = 0; j < kOwn; j += 16) {
+                        float all[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) all[i] = 0.f;
+                        for (int c = first; c <= last; ++c) {
+                            const float *p = a.part + (size_t)(2 * c + (c == first ? 1 : 0)) * kSlot +
+                                             (m * N + c0 + j) * 128 + th;
+                            const bool me = c == share.cta;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) all[i] += me ? acc[m][j + i] : __ldcg(p + i * 128);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[m][j + i] = all[i];
                     }
-                for (int c = first; c <= last; ++c) {
-                    const float *p = a.part + (size_t)(2 * c + (c == first ? 1 : 0)) * kSlot + c0 * 128 + th;
-                    const bool me = c == share.cta;
-#pragma unroll
-                    for (int m = 0; m < C::kMats; ++m)
-#pragma unroll
-                        for (int i = 0; i < kOwn; ++i)
-                            acc[m][i] += me ? own[m][i] : __ldcg(p + (m * N + i) * 128);
-                }
             }
             const int row = t.wt * 128 + th;
             if (UP) {
@@ -410,7 +451,7 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                     const uint32_t m = __reduce_max_sync(0xffffffffu, abs_bits(acc[0][i]));
                     if (lane == 0) hd->amax[q][c0 + i] = m;
                 }
-                ptx::named_bar_sync(1, kEt);
+                ptx::named_bar_sync(3, kEt);
                 uint8_t *h = static_cast<uint8_t *>(a.out) + (size_t)(t.s0 + c0) * a.n_out + row;
 #pragma unroll
                 for (int i = 0; i < kOwn; ++i) {
@@ -465,7 +506,7 @@ cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QsArgs a,
     a.n_in = g.n_in;
     a.n_out = g.n_out;
     a.xs = g.xs;
-    a.stages = alone ? C::kAlone : C::kShared;
+    a.stages = alone || C::kShared == 0 ? C::kAlone : C::kShared;
     a.err = device_info().err;
     void *args[] = {&mw0, &mw1, &mx, &a};
     LaunchScope ls(UP ? "quant_up_stream" : "quant_down_stream", st);
