@@ -896,13 +896,11 @@ bool experts_ok(const moe_quant_experts *w) {
 }
 
 // Rows enough for the CTA pairs, whose units of 256 rows cost the same however full they are:
-// 56 a group where the weight tiles alone fill the SMs (16 experts of 6144 x 10752: 48 rows 740 us
-// streamed and 783 by pairs, 64 rows 908 and 801), else more than 128 (one matrix of 8192 x
-// 6144: 64 rows 25 and 33 us, 128 rows 33 and 33, 200 rows 54 and 33).
-bool many_rows(int E, long long S, int n_out) {
-    const bool full = (long long)E * q_blocks(n_out) >= device_info().sm_count;
-    return full ? S >= 56LL * E : S > 128LL * E;
-}
+// 64 a group (16 experts of 6144 x 10752, streamed and by pairs: 48 rows 648 and 779 us, 64 rows
+// 802 and 798, 80 rows 870 and 806; 40 experts of 2000 x 1424: 45 rows 124 and 136, 63 rows 148
+// and 139), of a single matrix more than 144 (8192 x 6144: 128 rows 29 and 33 us, 160 rows 37
+// and 33).
+bool many_rows(int E, long long S) { return E == 1 ? S > 144 : S >= 64LL * E; }
 
 // The experts' products of slots that are dispatched already, and their combine.
 cudaError_t quant_experts(const moe_dims &d, int T, const void *x, const moe_quant_experts &w,
@@ -919,7 +917,7 @@ cudaError_t quant_experts(const moe_dims &d, int T, const void *x, const moe_qua
     const QuantGemm gd{E, S, F, D, offsets, at<void>(ws, L.h8), at<float>(ws, L.hs)};
     const QuantDown down{w.w2, w.w2_scale, at<void>(ws, L.y), 0};
     const QuantParts pu{at<float>(ws, L.part), count}, pd{at<float>(ws, L.part), count + kQMaxCtas};
-    if (many_rows(E, S, F) && quant_pair_ok()) {
+    if (many_rows(E, S) && quant_pair_ok()) {
         e = launch_quant_pair_up(gu, up, st);
         if (e == cudaSuccess) e = launch_quant_pair_down(gd, down, st);
     } else {
@@ -1045,7 +1043,7 @@ moe_status moe_quant_product(int32_t n_groups, int32_t n_out, int32_t n_in, int3
     }
     const QuantGemm g{n_groups, S, n_in, n_out, offsets_opt, x, xs};
     const QuantDown down{w, w_scale, y, y_dtype == MOE_BF16};
-    if (many_rows(n_groups, S, n_out) && quant_pair_ok())
+    if (many_rows(n_groups, S) && quant_pair_ok())
         return q_status(launch_quant_pair_down(g, down, st));
     return q_status(launch_quant_stream_down(g, down, QuantParts{at<float>(ws, L.part), count}, L.cols,
                                              true, st));

@@ -35,6 +35,7 @@ struct QsHeader {
     int prefix[257];       // tiles of the experts ahead
     alignas(16) float scale[8][2][2][32];  // warp, k-blocks in turn: x's times w1's (w's), v1's
     uint32_t amax[4][64];
+    alignas(16) float hinv[64];  // (UP) one over the scales of h's columns
 };
 static_assert(sizeof(QsHeader) <= kQsHdrBytes, "header");
 
@@ -54,7 +55,7 @@ struct QsCfg {
     static constexpr int kShared = N != 16 ? 0 : UP ? 3 : 4;
     static constexpr int kFit = (int)((220 * 1024 - kSums - kQsHdrBytes) / kStage);
     static constexpr int kAlone = kFit < kQsMaxStages ? kFit : kQsMaxStages;
-    static constexpr int kAcc = N == 64 ? 2 : 4;  // accumulators in turn
+    static constexpr int kAcc = 4;  // accumulators in turn
     static constexpr uint32_t kCols = kMats * N;  // tensor-memory columns of an accumulator
     static constexpr uint32_t kTmem = kAcc * kCols;
     // kind::f8f6f4: e4m3 A and B, fp32 D, both K-major, M = 128
@@ -62,7 +63,7 @@ struct QsCfg {
     static constexpr size_t smem(int stages) { return 1024 + stages * kStage + kSums + kQsHdrBytes; }
     static_assert(kStage % 1024 == 0, "stages stay 1024-byte aligned");
     static_assert(smem(kAlone) <= 227 * 1024, "shared memory");
-    static_assert((kTmem & (kTmem - 1)) == 0 && kTmem >= 32 && kTmem <= 256, "tensor memory");
+    static_assert((kTmem & (kTmem - 1)) == 0 && kTmem >= 32 && kTmem <= 512, "tensor memory");
 };
 static_assert(QsCfg<true, 16>::smem(QsCfg<true, 16>::kShared) + QsCfg<false, 16>::smem(QsCfg<false, 16>::kShared) <= 226 * 1024,
               "an up and a down projection's CTA on one SM");
@@ -452,18 +453,26 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                     if (lane == 0) hd->amax[q][c0 + i] = m;
                 }
                 ptx::named_bar_sync(3, kEt);
+                if (et < N) {
+                    const uint32_t m = max(max(hd->amax[0][et], hd->amax[1][et]),
+                                           max(hd->amax[2][et], hd->amax[3][et]));
+                    float sc, inv;
+                    q_scale(m, sc, inv);
+                    hd->hinv[et] = inv;
+                    if (et < t.cnt && !dead) a.out_scale[(size_t)t.wt * a.S + t.s0 + et] = sc;
+                }
+                ptx::named_bar_sync(3, kEt);
                 uint8_t *h = static_cast<uint8_t *>(a.out) + (size_t)(t.s0 + c0) * a.n_out + row;
+                const int left = row < a.n_out && !dead ? t.cnt - c0 : 0;
+                const float4 *inv4 = reinterpret_cast<const float4 *>(&hd->hinv[c0]);
 #pragma unroll
-                for (int i = 0; i < kOwn; ++i) {
-                    if (c0 + i < t.cnt) {
-                        const uint32_t m = max(max(hd->amax[0][c0 + i], hd->amax[1][c0 + i]),
-                                               max(hd->amax[2][c0 + i], hd->amax[3][c0 + i]));
-                        float sc, inv;
-                        q_scale(m, sc, inv);
-                        if (row < a.n_out && !dead)
-                            h[(size_t)i * a.n_out] = (uint8_t)e4m3x2(acc[0][i] * inv, 0.f);
-                        if (th == i && !dead) a.out_scale[(size_t)t.wt * a.S + t.s0 + c0 + i] = sc;
-                    }
+                for (int i = 0; i < kOwn; i += 4) {
+                    const float4 inv = inv4[i / 4];
+                    const uint32_t w = e4m3x2(acc[0][i] * inv.x, acc[0][i + 1] * inv.y) |
+                                       e4m3x2(acc[0][i + 2] * inv.z, acc[0][i + 3] * inv.w) << 16;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (i + j < left) h[(size_t)(i + j) * a.n_out] = (uint8_t)(w >> (8 * j));
                 }
             } else if (row < a.n_out && !dead) {
                 if (a.y_bf16) {

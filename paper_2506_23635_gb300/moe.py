@@ -788,42 +788,48 @@ def _opt(t):
     return None if t is None else t.data_ptr()
 
 
-def _quantize(x, scale_shape, q, scale, stream, name, sizes):
-    dev = x.get_device()
-    if x.dtype not in _DT:
-        raise ValueError("the numbers to quantise must be bf16 or fp32")
-    _want(x, x.shape, x.dtype, dev, "x")
-    if q is not None:
-        _want(q, x.shape, E4M3, dev, "q")
-    if scale is not None:
-        _want(scale, scale_shape, torch.float32, dev, "scale")
-    st = _raw_stream(dev, stream)
-    if q is None:
-        q = _new(x.shape, E4M3, x.device, stream)
-    if scale is None:
-        scale = _new(scale_shape, torch.float32, x.device, stream)
-    _check(getattr(lib(), name)(*sizes, x.data_ptr(), _DT[x.dtype], q.data_ptr(), scale.data_ptr(),
-                                st), name)
-    return q, scale
-
-
 def quantize_rows(x, q=None, scale=None, stream=None):
     """e4m3 numbers and their scales [rows, ceil(cols/128)] (fp32 powers of two) of
     x [rows, cols] (bf16 or fp32)."""
-    if x.dim() != 2:
-        raise ValueError("x must be [rows, cols]")
-    rows, cols = x.shape
-    return _quantize(x, (rows, _blocks(cols)), q, scale, stream, "moe_quantize_rows", (rows, cols))
+    dev, dt = x.get_device(), _DT.get(x.dtype)
+    if x.dim() != 2 or dt is None or not x.is_contiguous():
+        raise ValueError("x must be contiguous bf16 or fp32 [rows, cols]")
+    rows, cols = shape = x.shape
+    sshape = (rows, -(-cols // QUANT_BLOCK))
+    if q is not None:
+        _want(q, shape, E4M3, dev, "q")
+    if scale is not None:
+        _want(scale, sshape, torch.float32, dev, "scale")
+    st = _raw_stream(dev, stream)
+    if q is None:
+        q = _new(shape, E4M3, x.device, stream)
+    if scale is None:
+        scale = _new(sshape, torch.float32, x.device, stream)
+    _check(lib().moe_quantize_rows(rows, cols, x.data_ptr(), dt, q.data_ptr(), scale.data_ptr(), st),
+           "moe_quantize_rows")
+    return q, scale
 
 
 def quantize_blocks(w, q=None, scale=None, stream=None):
     """e4m3 numbers and their scales [n, ceil(rows/128), ceil(cols/128)] of n matrices
     w [n, rows, cols] (bf16 or fp32), as an expert weight tensor holds them."""
-    if w.dim() != 3:
-        raise ValueError("w must be [n, rows, cols]")
+    dev, dt = w.get_device(), _DT.get(w.dtype)
+    if w.dim() != 3 or dt is None or not w.is_contiguous():
+        raise ValueError("w must be contiguous bf16 or fp32 [n, rows, cols]")
     n, rows, cols = w.shape
-    return _quantize(w, (n, _blocks(rows), _blocks(cols)), q, scale, stream, "moe_quantize_blocks",
-                     (n, rows, cols))
+    sshape = (n, _blocks(rows), _blocks(cols))
+    if q is not None:
+        _want(q, w.shape, E4M3, dev, "q")
+    if scale is not None:
+        _want(scale, sshape, torch.float32, dev, "scale")
+    st = _raw_stream(dev, stream)
+    if q is None:
+        q = _new(w.shape, E4M3, w.device, stream)
+    if scale is None:
+        scale = _new(sshape, torch.float32, w.device, stream)
+    _check(lib().moe_quantize_blocks(n, rows, cols, w.data_ptr(), dt, q.data_ptr(), scale.data_ptr(),
+                                     st), "moe_quantize_blocks")
+    return q, scale
 
 
 def quant_product_workspace_size(n_groups: int, n_out: int, n_in: int, max_rows: int) -> int:
