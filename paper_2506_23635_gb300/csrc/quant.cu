@@ -209,10 +209,11 @@ __device__ __forceinline__ double warp_sum(double v) {
 
 // What 32 bits may be off by, of a score s, in steps of 2^-24.  exp(d) / z: |d| of the
 // subtraction's rounding, 4 of the exponential, 4 + 13 of its sum over 256, 3 of the quotient
-// by a reciprocal.  1 / (1 + exp(-d)): 4 + 2.4 |d| of the fast exponential (2 + 1.18 |d| units
-// in the last place), 1 of the sum, 4 of the fast quotient.
-__device__ __forceinline__ float score_err(float s, float d) {
-    return s * ((28.f + 2.5f * fabsf(d)) * 5.9604645e-8f);
+// by a reciprocal.  1 / (1 + exp(-d)): the fast exponential's 4 + 2.4 |d| (2 + 1.18 |d| units in
+// the last place), of which the share 1 - s arrives, 1 of the sum, 4 of the fast quotient.
+__device__ __forceinline__ float score_err(bool sigmoid, float s, float d) {
+    const float steps = sigmoid ? 6.f + (1.f - s) * (5.f + 2.5f * fabsf(d)) : 28.f + 1.1f * fabsf(d);
+    return s * steps * 5.9604645e-8f;
 }
 constexpr float kSumErr = 1.2e-7f;  // a key's or a sum's rounding, of either side
 
@@ -643,7 +644,7 @@ k_select(const SelArgs a) {
         code[i] = e0 + i < a.E ? key_code(key) : 0u;
         kv[i] = key;
         if ((biased || by_score) && a.G > 1 && e0 + i < a.E)
-            err = fmaxf(err, score_err(s[i], v[i] - m) + kSumErr * fabsf(b[i]));
+            err = fmaxf(err, score_err(a.sigmoid, s[i], v[i] - m) + kSumErr * fabsf(b[i]));
     }
     if (biased || by_score) keep<NE>(w.f.score + e0, s);
     keep<NE>(w.f.key + e0, kv);
@@ -752,7 +753,8 @@ k_select(const SelArgs a) {
             const float ke = w.f.key[e], kf = w.f.key[f];
             // an infinite bias decides by itself; NaN is below everything
             if (isnan(ke) || isnan(kf) || isinf(ke) || isinf(kf)) continue;
-            const float off = score_err(w.f.score[e], le - m) + score_err(w.f.score[f], lf - m) +
+            const float off = score_err(a.sigmoid, w.f.score[e], le - m) +
+                              score_err(a.sigmoid, w.f.score[f], lf - m) +
                               kSumErr * (fabsf(be) + fabsf(bf));
             if (!(ke - kf > off)) (k == a.K - 1 ? clear : order) = false;
         }
