@@ -491,3 +491,108 @@ def test_empty_calls():
     q, s = m.quantize_blocks(e(1, 128, 256))
     assert m.quant_product(e(0, 256, t=torch.float8_e4m3fn), e(0, 2), q, s).shape == (0, 128)
     assert m.get_last_error() == 0
+
+
+# ---- the launch directly ahead ----------------------------------------------------------
+
+
+def _behind(m, zero, write, fn):
+    """fn() right behind write(), whose kernel lets the next launch start before it has
+    written, gives what it gives once everything is there."""
+    write()
+    torch.cuda.synchronize()
+    want = fn().clone()
+    for _ in range(8):
+        zero.view(torch.uint8).zero_()
+        torch.cuda.synchronize()
+        write()
+        got = fn()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+    assert m.get_last_error() == 0
+
+
+@pytest.mark.parametrize("S", [1, 40, 400])
+def test_product_weights_and_rows_written_just_ahead(S):
+    m, g = moe(), torch.Generator(device="cuda").manual_seed(S)
+    n_out, n_in = 4096, 4096
+    src = torch.randn((n_out, n_in), device="cuda", generator=g)
+    q, s = m.quantize_rows(src)
+    ws = torch.rand((1, 32, 32), device="cuda", generator=g)
+    x, xs = m.quantize_rows(torch.randn((S, n_in), device="cuda", generator=g))
+    out, sp = torch.empty((S, n_out), device="cuda"), m.quant_product_alloc_workspace(1, n_out, n_in, S)
+    run = lambda: m.quant_product(x, xs, q.view(1, n_out, n_in), ws, None, torch.float32, out=out, ws=sp)
+    _behind(m, q, lambda: m.quantize_rows(src, q, s), run)
+    rows = torch.randn((S, n_in), device="cuda", generator=g)
+    _behind(m, x, lambda: m.quantize_rows(rows, x, xs), run)
+
+
+@pytest.mark.parametrize("T", [1, 40, 300])
+def test_experts_inputs_written_just_ahead(T):
+    """The choice, the down projection's weights and the tokens."""
+    m, g = moe(), torch.Generator(device="cuda").manual_seed(T)
+    E, K, D, F = 8, 2, 1024, 2048
+    mk = lambda *s: torch.randn(s, device="cuda", generator=g) * 0.05
+    ex = m.QuantExperts.quantize(mk(E, F, D), mk(E, F, D), mk(E, D, F))
+    d = m.dims(D, F, E, K, torch.float32)
+    x, logits, bias = mk(T, D) * 20, mk(T, E) * 20, mk(E)
+    idx, gate = m.route_select(d, m.router("sigmoid"), logits, bias)
+    out, ws = torch.empty_like(x), m.quant_alloc_workspace(d, T)
+    run = lambda: m.quant_experts_forward(d, ex, x, idx, gate, out=out, ws=ws)
+    _behind(m, gate, lambda: m.route_select(d, m.router("sigmoid"), logits, bias, idx, gate), run)
+    w2, src = ex.tensors[2], mk(E * D, F)
+    s = m.quantize_rows(src)[1]
+    _behind(m, w2, lambda: m.quantize_rows(src, w2.view(E * D, F), s), run)
+    inner = m.dims(D, F, E, K, torch.float32)
+    _behind(m, x, lambda: m.quant_experts_forward(inner, ex, logits.new_ones((T, D)), idx, gate, out=x), run)
+
+
+@pytest.mark.parametrize("T", [1, 16, 65, 300])
+def test_calls_back_to_back_share_a_workspace(T):
+    """Calls of different sizes behind each other on one stream, over one workspace."""
+    m, rng = moe(), np.random.default_rng(T)
+    D, F, E, K = 512, 656, 8, 2
+    ex, _ = _experts(m, rng, E, F, D)
+    d = m.dims(D, F, E, K, torch.bfloat16)
+    ws = m.quant_alloc_workspace(d, 400)
+    sizes = [T, 1, 400, 7, T, 33, 200, T]
+    x = torch.from_numpy(rng.normal(size=(400, D)).astype(np.float32)).bfloat16().cuda()
+    idx, gate = (cuda(a) for a in _routing(rng, 400, E, K))
+    want = []
+    for n in sizes:
+        want.append(m.quant_experts_forward(d, ex, x[:n], idx[:n], gate[:n]))
+        torch.cuda.synchronize()
+    got = [m.quant_experts_forward(d, ex, x[:n], idx[:n], gate[:n], ws=ws) for n in sizes]
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    assert m.get_last_error() == 0
+
+
+def test_large_offsets():
+    """Weights of more than 2^31 bytes, and rows whose outputs lie past 2^31 bytes."""
+    m, rng = moe(), np.random.default_rng(1)
+    E, n_out, n_in = 9, 16384, 16384
+    wq = torch.zeros((E, n_out, n_in), dtype=torch.uint8, device="cuda")
+    part, s = _matrices8(rng, 1, 256, n_in)
+    wq[E - 1, -256:] = torch.from_numpy(part[0]).cuda()
+    ws = torch.ones((E, 128, 128), device="cuda")
+    xq, xs = _rows8(rng, 3, n_in)
+    off = cuda(np.array([0] * E + [3], np.int32))
+    y = num(m.quant_product(e4m3(xq), cuda(xs), wq.view(torch.float8_e4m3fn), ws, off, torch.float32))
+    want, room = ref.product(ref.rows64(xq, xs), ref.decode(part[0]))
+    assert (np.abs(y[:, -256:] - want) <= room + 2.0 ** -24 * np.abs(want)).all() and (y[:, :-256] == 0).all()
+    del wq, ws
+    S, n_out, n_in = 40000, 16384, 128
+    wq, s = _matrices8(rng, 1, n_out, n_in)
+    x = torch.zeros((S, n_in), dtype=torch.uint8, device="cuda")
+    xq, xs1 = _rows8(rng, 300, n_in)
+    x[-300:] = torch.from_numpy(xq).cuda()
+    xs = torch.ones((S, 1), device="cuda")
+    xs[-300:] = cuda(xs1)
+    y = m.quant_product(x.view(torch.float8_e4m3fn), xs, e4m3(wq), cuda(s), None, torch.float32)
+    want, room = ref.product(ref.rows64(xq, xs1), ref.matrix64(wq[0], s[0]))
+    got = num(y[-300:])
+    assert (np.abs(got - want) <= room + 2.0 ** -24 * np.abs(want)).all()
+    assert not y[:-300].any()
+    assert m.get_last_error() == 0
