@@ -897,12 +897,12 @@ bool experts_ok(const moe_quant_experts *w) {
            q_aligned(w->v1_scale) && q_aligned(w->w2_scale);
 }
 
-// Rows enough for the CTA pairs, whose units of 256 rows cost the same however full they are:
-// 64 a group (16 experts of 6144 x 10752, streamed and by pairs: 48 rows 648 and 779 us, 64 rows
-// 802 and 798, 80 rows 870 and 806; 40 experts of 2000 x 1424: 45 rows 124 and 136, 63 rows 148
+// Rows enough for the CTA pairs, whose units of 256 rows cost nearly the same however full they
+// are: 60 a group (16 experts of 6144 x 10752, streamed and by pairs: 48 rows 648 and 715 us, 64 rows
+// 802 and 743, 80 rows 870 and 764; 40 experts of 2000 x 1424: 45 rows 115 and 136, 63 rows 148
 // and 139), of a single matrix more than 144 (8192 x 6144: 128 rows 29 and 33 us, 160 rows 37
-// and 33).
-bool many_rows(int E, long long S) { return E == 1 ? S > 144 : S >= 64LL * E; }
+// and 31).
+bool many_rows(int E, long long S) { return E == 1 ? S > 144 : S >= 60LL * E; }
 
 // The experts' products of slots that are dispatched already, and their combine.
 cudaError_t quant_experts(const moe_dims &d, int T, const void *x, const moe_quant_experts &w,

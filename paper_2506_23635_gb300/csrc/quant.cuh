@@ -94,20 +94,6 @@ __device__ __forceinline__ float2 both(uint64_t v) {
     return r;
 }
 
-// Four bytes into shared memory without waiting for them; groups of such copies.
-__device__ __forceinline__ void copy_ahead(uint32_t dst, const float *src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ float lds(uint32_t p) {
-    float v;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(p) : "memory");
-    return v;
-}
-
 // A grouped product of 8-bit operands: rows x8 [S, n_in] in groups given by offsets
 // [E+1] (null: one group of S rows) times each group's matrix w8 [E, n_out, n_in].
 struct QuantGemm {

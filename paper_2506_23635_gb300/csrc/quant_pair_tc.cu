@@ -8,8 +8,13 @@
 // columns fill the tensor memory); eight epilogue warps take turns with the MMAs, which
 // write one accumulator while the other is multiplied with the block's scales and added to
 // the sums in registers.  The rows of x are the lanes, so that a thread needs one scale of
-// x and one or two of the weights for each k-block: with the weights as lanes every
+// x times one or two of the weights for each k-block: with the weights as lanes every
 // column would need its own, 32 lanes reading the same word of shared memory.
+//
+// A k-block takes 1000 cycles (9728 rows of 8192 x 6144: 391 us, 2.5 PFLOP/s), its MMAs 512: the rest
+// is the way around, a buffer's sums 580 cycles in the epilogue, the arrivals to and from the
+// even CTA's MMA warp about 500 each.  With the arrivals taken out (in groups of eight k-blocks)
+// the MMAs alone took 304 us.
 //
 // N: for UP 128 rows of W1 (loaded by the even CTA) and the same 128 of V1 (by the
 // odd one), for DOWN 256 rows of the weights.  Epilogue warp (q, half): lanes 32 q .. and
@@ -24,11 +29,11 @@ namespace {
 
 using namespace tc;
 
-// warp 0 loads, warp 1 issues the MMAs, warps 4-11 are the epilogue.  Registers of the
-// launch: 168 a thread, 64,512; what the first four warps give up the others take: 128
-// (104 + 2 * 200) for UP, 128 (120 + 2 * 192) for DOWN, both 64,512 (splits that spill on
-// either side cost 5 to 20%).
+// warp 0 loads, warp 1 issues the MMAs, warps 2 and 3 prepare scales, warps 4-11 are the
+// epilogue.  Registers of the launch: 168 a thread, 64,512; what the first four warps give up the
+// others take: 128 (136 + 2 * 184) = 64,512 (splits that spill on either side cost 5 to 20%).
 constexpr int kQpThreads = 384;
+constexpr int kQpRegsFeed = 136, kQpRegsSums = 184;
 constexpr int kQpEpilogue = 4;  // first warp of it
 constexpr int kQpStages = 5;
 constexpr uint32_t kQpTile = 128 * 128;
@@ -43,24 +48,25 @@ struct QpHeader {
     uint64_t done;
     uint32_t tmem_base;
     int prefix[257];
+    float2 scale[4][128];      // steps in turn, row: x's times w1's and v1's (the tile's two blocks')
     uint32_t amax[2][2][128];  // (UP) of a row's 64 columns: tile in turn, half
 };
-constexpr uint32_t kQpHdrBytes = 6144;
+constexpr uint32_t kQpHdrBytes = 8192;
 static_assert(sizeof(QpHeader) <= kQpHdrBytes, "header");
 constexpr uint32_t kQpOut = 8 * 4096;  // 4 KB an epilogue warp: 32 rows of 128 bytes on their way out
-// (DOWN) The scales of the next k-blocks, copied ahead by the threads that use them (the
-// experts of 2048 tokens: 597 -> 540 us; UP, which keeps them in registers, lost 16% by it).
-constexpr int kQpAhead = 3, kQpRing = kQpAhead + 1;
-constexpr uint32_t kQpScales = 8 * kQpRing * 2 * 128;  // warp, k-block, x's, the weights': 32 lanes
-constexpr size_t kQpSmem = 1024 + kQpStages * kQpStage + kQpOut + kQpScales + kQpHdrBytes;
+constexpr size_t kQpSmem = 1024 + kQpStages * kQpStage + kQpOut + kQpHdrBytes;
 static_assert(kQpSmem <= 227 * 1024, "shared memory");
 
-__device__ __forceinline__ void mma_f8_pair(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc,
+// x, w: the lower halves of their descriptors (the upper: 128-byte swizzle, 8 rows 1024
+// bytes apart).
+__device__ __forceinline__ void mma_f8_pair(uint32_t d_tmem, uint32_t x, uint32_t w, uint32_t idesc,
                                             uint32_t accumulate) {
+    constexpr uint32_t kHi = (1024 >> 4) | 1u << 14 | 2u << 29;
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 dx, dw;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "mov.b64 dx, {%1, %5};\n\tmov.b64 dw, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], dx, dw, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(x), "r"(w), "r"(idesc), "r"(accumulate), "r"(kHi)
         : "memory");
 }
 
@@ -153,7 +159,7 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    QpHeader *hd = reinterpret_cast<QpHeader *>(smem + kQpStages * kQpStage + kQpOut + kQpScales);
+    QpHeader *hd = reinterpret_cast<QpHeader *>(smem + kQpStages * kQpStage + kQpOut);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_ctarank();
     const bool even = rank == 0;
@@ -165,7 +171,7 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
             ptx::mbar_init(&hd->empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
-            ptx::mbar_init(&hd->tfull[b], 1);
+            ptx::mbar_init(&hd->tfull[b], 3);  // (the MMAs; the two warps with the scales)
             ptx::mbar_init(&hd->tempty[b], 16);
         }
         ptx::mbar_init(&hd->done, 1);
@@ -185,7 +191,7 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
     const int n_units = hd->prefix[a.E], u0 = blockIdx.x >> 1, du = gridDim.x >> 1;
 
     if (warp < kQpEpilogue) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(UP ? 104 : 120));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kQpRegsFeed));
         if (warp == 0) {
             // ------------------------------------------------------------ loads
             if (lane == 0) {
@@ -221,9 +227,12 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
             __syncwarp();
         } else if (warp == 1) {
             // ------------------------------------------------------------ MMAs
-            if (even && lane == 0) {
+            // (all lanes go along and one issues: in a branch of a single lane every MMA costs a
+            // search for its operands' uniform registers)
+            if (even) {
+                const bool one = elect_one();
                 const int n = u0 < n_units ? ((n_units - 1 - u0) / du + 1) * nk : 0;
-                const uint64_t d0 = smem_desc(ptx::smem_u32(smem));
+                const uint32_t base = (ptx::smem_u32(smem) & 0x3FFFFu) >> 4 | 1u << 16;
                 uint32_t s = 0, ph = 0;
                 bool ok = true;
 #pragma unroll 1
@@ -232,84 +241,89 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
                     // (released by both CTAs' epilogues)
                     ok = wait_soon(&hd->full[s], ph, a.err) &&
                          wait_soon(&hd->tempty[b], bph ^ 1, a.err);
+                    ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint64_t x = d0 + s * (kQpStage >> 4), w = x + (kQpTile >> 4);
+                    const uint32_t x = base + s * (kQpStage >> 4), w = x + (kQpTile >> 4);
                     const uint32_t d = tmem + b * 256;
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)
-                        mma_f8_pair(d, x + 2 * kk, w + 2 * kk, kQpIdesc, kk != 0);
-                    mma_commit_pair(&hd->tfull[b], 3);
-                    mma_commit_pair(&hd->empty[s], 3);
+                    if (one) {
+                        mma_f8_pair(d, x, w, kQpIdesc, 0);
+                        mma_f8_pair(d, x + 2, w + 2, kQpIdesc, 1);
+                        mma_f8_pair(d, x + 4, w + 4, kQpIdesc, 1);
+                        mma_f8_pair(d, x + 6, w + 6, kQpIdesc, 1);
+                        mma_commit_pair(&hd->tfull[b], 3);
+                        mma_commit_pair(&hd->empty[s], 3);
+                    }
+                    __syncwarp();
                     if (++s == kQpStages) {
                         s = 0;
                         ph ^= 1;
                     }
                 }
-                mma_commit_pair(&hd->done, 1);
+                if (one) mma_commit_pair(&hd->done, 1);
                 ptx::mbar_wait(&hd->done, 0, a.err);
             }
             __syncwarp();
+        } else {
+            // ------------------------------------------------------------ scales
+            // warps 2 and 3: 64 rows each.  A step's scales take the slot of the step four ago,
+            // which both CTAs' epilogues have read once the MMAs of the step two ago are done.
+            const int r0 = (warp - 2) * 64 + lane;
+            uint32_t it = 0;
+            bool ok = true;
+            for (int u = u0; ok && u < n_units; u += du) {
+                const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, u);
+                const int row = (int)rank * 128 + r0;
+                const float *x0 = a.xs + t.s0 + min(row, t.cnt - 1);
+                const int x1 = min(row + 32, t.cnt - 1) - min(row, t.cnt - 1);
+                const int blk = UP ? t.wt : t.wt * 2, next = UP ? blk : min(blk + 1, nblk - 1);
+                const float *w0 = a.s0 + ((size_t)t.e * nblk + blk) * nk;
+                const float *w1 = (UP ? a.s1 : a.s0) + ((size_t)t.e * nblk + next) * nk;
+                float v[4], more[4];  // of this k-block, of the next one
+                auto fetch = [&](int kb) {
+                    more[0] = x0[(size_t)kb * a.S];
+                    more[1] = x0[(size_t)kb * a.S + x1];
+                    more[2] = w0[kb];
+                    more[3] = w1[kb];
+                };
+                fetch(0);
+#pragma unroll 1
+                for (int kb = 0; kb < nk; ++kb, ++it) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = more[j];
+                    if (kb + 1 < nk) fetch(kb + 1);
+                    if (it >= 2) ok = __all_sync(0xffffffffu, wait_soon(&hd->tfull[it & 1], ((it >> 1) - 1) & 1, a.err));
+                    if (!ok) break;
+                    hd->scale[it & 3][r0] = make_float2(v[0] * v[2], v[0] * v[3]);
+                    hd->scale[it & 3][r0 + 32] = make_float2(v[1] * v[2], v[1] * v[3]);
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(&hd->tfull[it & 1]);
+                }
+            }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(UP ? 200 : 192));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kQpRegsSums));
         // ------------------------------------------------------------ epilogue
         const int q = warp & 3, half = (warp - kQpEpilogue) >> 2;
         const uint32_t base0 = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)half * (UP ? 64 : 128);
         const uint32_t tempty0 = ptx::map_rank(ptx::smem_u32(&hd->tempty[0]), 0);
-        const uint32_t scales = ptx::smem_u32(smem + kQpStages * kQpStage + kQpOut) +
-                                (uint32_t)(warp - kQpEpilogue) * (kQpRing * 256) + lane * 4;
         bool dead = false;  // a wait gave up: keep the barriers, skip the work
         uint32_t it = 0, tl = 0;
         for (int u = u0; u < n_units; u += du, ++tl) {
             const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, u);
             const int r = (int)rank * 128 + q * 32 + lane;  // of the run
             const bool mine = r < t.cnt;
-            const float *sx = a.xs + t.s0 + min(r, t.cnt - 1);
-            const int blk = UP ? t.wt : min(t.wt * 2 + half, nblk - 1);
-            const float *sw0 = a.s0 + ((size_t)t.e * nblk + blk) * nk;
-            const float *sw1 = UP ? a.s1 + ((size_t)t.e * nblk + blk) * nk : sw0;
             uint64_t acc[64];
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i] = 0;
-            // DOWN: k-block kb's scales go to slot kb % kQpRing
-            auto fetch = [&](int kb) {
-                if (kb < nk) {
-                    const uint32_t to = scales + (uint32_t)(kb % kQpRing) * 256;
-                    copy_ahead(to, sx);
-                    copy_ahead(to + 128, sw0 + kb);
-                    sx += a.S;
-                }
-                copies_commit();
-            };
-            float nx = 0.f, n0 = 0.f, n1 = 0.f;
-            if (UP) {
-                nx = *sx;
-                n0 = *sw0;
-                n1 = *sw1;
-            } else {
-#pragma unroll
-                for (int i = 0; i < kQpAhead; ++i) fetch(i);
-            }
             for (int kb = 0; kb < nk; ++kb, ++it) {
                 const uint32_t b = it & 1, bph = (it >> 1) & 1;
-                float f0 = nx * n0, f1 = nx * n1;
-                if (!UP) {
-                    copies_wait<kQpAhead - 1>();
-                    const uint32_t from = scales + (uint32_t)(kb % kQpRing) * 256;
-                    f0 = lds(from) * lds(from + 128);
-                    fetch(kb + kQpAhead);
-                }
-                const uint64_t sc0 = twice(f0), sc1 = UP ? twice(f1) : sc0;
                 if (!dead) dead = !__all_sync(0xffffffffu, wait_soon(&hd->tfull[b], bph, a.err));
                 tc_fence_after();
-                if (UP && kb + 1 < nk) {  // the next block's scales
-                    nx = *(sx += a.S);
-                    n0 = *++sw0;
-                    n1 = *++sw1;
-                }
                 const uint32_t base = base0 + b * 256;
                 if (!dead) {
+                    const float2 f = hd->scale[it & 3][q * 32 + lane];
+                    const uint64_t sc0 = twice(UP || half == 0 ? f.x : f.y), sc1 = UP ? twice(f.y) : sc0;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         float v[32];
