@@ -8,7 +8,8 @@ namespace moe {
 namespace {
 
 // ===========================================================================
-// Quantising rows: 16 lanes take a block of 128 numbers, eight each.  Bound by memory.
+// Quantising rows: 16 lanes take a block of 128 numbers, eight each.  Bound by memory
+// (8190 x 6144 bf16: 27.5 us, 5.6 TB/s read and written, 0.82 of a copy's rate).
 // With K > 0 the rows are tokens, each written to the K sorted positions of its
 // slots (inv_perm; -1: left out), so that a token is read and quantised once, and
 // the scales block by block ([blocks, rows * K]), as the products read them.
@@ -73,7 +74,7 @@ k_quant_rows(int rows, int cols, int K, const TX *__restrict__ x,
 }
 
 // Quantising matrices: a block of 256 threads holds 128 x 128 numbers in registers, as
-// they were loaded.
+// they were loaded.  Bound by memory (four of 10752 x 6144 bf16: 121 us, 0.97 of a copy's rate).
 __device__ __forceinline__ void hold8(const bf16 *p, uint4 (&r)[1]) { r[0] = ld_stream16(p); }
 __device__ __forceinline__ void hold8(const float *p, uint4 (&r)[2]) {
     r[0] = ld_stream16(p);
@@ -167,8 +168,10 @@ k_quant_scales(int S, int nb, const float *__restrict__ in, float *__restrict__ 
 // and keys in 32 bits first; where two of the keys that decide lie nearer to each other
 // than the error of 32 bits, the warp does the token again with more, so that the choice
 // is that of 64 bits (pairs of fp32 tell nearly always; fp64 itself takes 40 us a token).
-// Bound by the latency of its steps and the instructions of K
-// maxima over the warp.
+// Bound by the latency of its steps and the instructions of K maxima over the warp: 8191
+// tokens of 256 experts in 8 groups, 8 chosen, 23 us, of which tokens done again are 8 at the
+// end; a token of 16 experts 2.2.  A grid that stays and takes tokens in turn took 33 us where
+// this took 30 (its loop's registers).
 // ===========================================================================
 constexpr int kSelThreads = 128;
 constexpr int kSelWarps = kSelThreads / 32;
