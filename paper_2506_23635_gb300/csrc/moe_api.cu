@@ -11,6 +11,7 @@
 
 #include <cooperative_groups.h>
 
+#include "layer_steps.cuh"
 #include "moe_internal.cuh"
 #include "ptx.cuh"
 

@@ -2,6 +2,7 @@
 // the C ABI of the grouped products and of the layer over them (include/moe.h).
 #include <math.h>
 
+#include "layer_steps.cuh"
 #include "quant.cuh"
 
 namespace moe {
