@@ -901,12 +901,18 @@ bool experts_ok(const moe_quant_experts *w) {
            q_aligned(w->v1_scale) && q_aligned(w->w2_scale);
 }
 
-// Rows enough for the CTA pairs, whose units of 256 rows cost nearly the same however full they
-// are: 60 a group (16 experts of 6144 x 10752, streamed and by pairs: 48 rows 648 and 715 us, 64 rows
-// 802 and 743, 80 rows 870 and 764; 40 experts of 2000 x 1424: 45 rows 115 and 136, 63 rows 148
-// and 139), of a single matrix more than 144 (8192 x 6144: 128 rows 29 and 33 us, 160 rows 37
-// and 31).
-bool many_rows(int E, long long S) { return E == 1 ? S > 144 : S >= 60LL * E; }
+// Rows enough for the CTA pairs, whose units of up to 128 rows x 512 weight rows cost the same
+// however few rows there are (us, streamed and by pairs).  More than 64 a group, where the
+// streaming kernel takes a second tile (8192 x 6144: 2 groups of 100 45 and 34, 8 of them 135 and
+// 80); of a single matrix, whose pairs are few, more than 128 (96 rows 29 and 30, 144 rows 37 and
+// 31).  From 34 on where the units go twice around (16 experts of 6144 x 10752: 32 rows 488 and
+// 504, 35 rows 533 and 520, 40 rows 548 and 511; 40 of 2000 x 1424: 30 rows 106 and 102, 45 rows 113
+// and 104; but 6 groups of 40 rows, 8192 x 6144, 96 units on 76 pairs: 61 and 72).
+bool many_rows(int E, long long S, int n_out) {
+    if (E == 1) return S > 128;
+    return S > 64LL * E ||
+           (S >= 34LL * E && (long long)E * ((n_out + 511) / 512) >= device_info().sm_count);
+}
 
 // The experts' products of slots that are dispatched already, and their combine.
 cudaError_t quant_experts(const moe_dims &d, int T, const void *x, const moe_quant_experts &w,
@@ -923,7 +929,7 @@ cudaError_t quant_experts(const moe_dims &d, int T, const void *x, const moe_qua
     const QuantGemm gd{E, S, F, D, offsets, at<void>(ws, L.h8), at<float>(ws, L.hs)};
     const QuantDown down{w.w2, w.w2_scale, at<void>(ws, L.y), 0};
     const QuantParts pu{at<float>(ws, L.part), count}, pd{at<float>(ws, L.part), count + kQMaxCtas};
-    if (many_rows(E, S) && quant_pair_ok()) {
+    if (many_rows(E, S, D) && quant_pair_ok()) {
         e = launch_quant_pair_up(gu, up, st);
         if (e == cudaSuccess) e = launch_quant_pair_down(gd, down, st);
     } else {
@@ -1049,7 +1055,7 @@ moe_status moe_quant_product(int32_t n_groups, int32_t n_out, int32_t n_in, int3
     }
     const QuantGemm g{n_groups, S, n_in, n_out, offsets_opt, x, xs};
     const QuantDown down{w, w_scale, y, y_dtype == MOE_BF16};
-    if (many_rows(n_groups, S) && quant_pair_ok())
+    if (many_rows(n_groups, S, n_out) && quant_pair_ok())
         return q_status(launch_quant_pair_down(g, down, st));
     return q_status(launch_quant_stream_down(g, down, QuantParts{at<float>(ws, L.part), count}, L.cols,
                                              true, st));

@@ -1,27 +1,32 @@
-// Grouped products of 8-bit operands for many rows a group: CTA pairs that share every
-// MMA (cta_group::2), 256 rows of x as its M, 256 weight rows as its N.
+// Grouped products of 8-bit operands for many rows a group: pairs of CTAs that share their
+// weight tiles, each 128 rows of x as its MMAs' M, 256 weight rows as their N.
 //
 //   DOWN:  y[j, n] = sum_b xs[j, b] ws[e, n/128, b] (sum_{k in block b} x8[j, k] w8[e, n, k])
 //   UP:    a, b = the same with w1 and v1;  h = SiLU(a) b, quantised in blocks of 128
 //
-// Bound by the tensor cores.  A k-block of 128 is an accumulator of its own (two of 256
-// columns fill the tensor memory); eight epilogue warps take turns with the MMAs, which
-// write one accumulator while the other is multiplied with the block's scales and added to
-// the sums in registers.  The rows of x are the lanes, so that a thread needs one scale of
-// x times one or two of the weights for each k-block: with the weights as lanes every
-// column would need its own, 32 lanes reading the same word of shared memory.
+// A k-block of 128 is an accumulator of its own (two of 256 columns fill the tensor memory);
+// eight epilogue warps take turns with the MMAs, which write one accumulator while the other
+// is multiplied with the block's scales and added to the sums in registers.  The rows of x
+// are the lanes, so that a thread needs one scale of x times one or two of the weights for
+// each k-block: with the weights as lanes every column would need its own, 32 lanes reading
+// the same word of shared memory.
 //
-// A k-block takes 1000 cycles (9728 rows of 8192 x 6144: 391 us, 2.5 PFLOP/s), its MMAs 512: the rest
-// is the way around, a buffer's sums 580 cycles in the epilogue, the arrivals to and from the
-// even CTA's MMA warp about 500 each.  With the arrivals taken out (in groups of eight k-blocks)
-// the MMAs alone took 304 us.
+// Bound by the way around: a k-block takes 950 cycles (9728 rows of 8192 x 6144: 375 to 380 us,
+// 2.6 PFLOP/s), its MMAs 512, what shared memory moves for it (48 KB in, 48 KB out) 750 at
+// least, a buffer's sums 580 in the epilogue, and an accumulator goes from one to the other and
+// back.  MMAs of both CTAs in one (cta_group::2) read half the weights each and wait for each
+// other: 388 us, 1033 and 562 instead of 1011 and 558 for the projections of 2048 tokens.
+// Scales of powers of two could go into the MMAs (kind::mxf8f6f4, no epilogue before the end):
+// 321 us, but any other scale needs this way, and the choice a look at all scales first.
 //
-// N: for UP 128 rows of W1 (loaded by the even CTA) and the same 128 of V1 (by the
-// odd one), for DOWN 256 rows of the weights.  Epilogue warp (q, half): lanes 32 q .. and
-// half of the columns (UP: 64 of a and the same 64 of b), 128 sums a thread.
+// N: 256 rows of the weights; for UP 128 rows of W1, then the same 128 of V1.  Each CTA loads
+// half of a shared tile for both.  Epilogue warp (q, half): lanes 32 q .. and half of the
+// columns (UP: 64 of a and the same 64 of b), 128 sums a thread.
 //
 // Units are (expert, weight tile, run of 256 rows), runs innermost, so that units that run
-// together share weight tiles in L2; pair p of P takes units p, p + P, ...
+// together share weight tiles in L2.  A last run of at most 128 rows leaves nothing to share:
+// there the CTAs of a pair take weight tiles side by side (2048 tokens on 16 experts 1022 and
+// 563 -> 957 and 534 us).  Pair p of P takes units p, p + P, ...
 #include "quant.cuh"
 
 namespace moe {
@@ -35,15 +40,14 @@ using namespace tc;
 constexpr int kQpThreads = 384;
 constexpr int kQpRegsFeed = 136, kQpRegsSums = 184;
 constexpr int kQpEpilogue = 4;  // first warp of it
-constexpr int kQpStages = 5;
 constexpr uint32_t kQpTile = 128 * 128;
-constexpr uint32_t kQpStage = 2 * kQpTile;  // of a CTA: 128 rows of x, 128 weight rows
-constexpr int kQpRows = 256;
-// kind::f8f6f4: e4m3 A and B, fp32 D, both K-major, M = 256, N = 256
-constexpr uint32_t kQpIdesc = (1u << 4) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
+constexpr uint32_t kQpStage = 3 * kQpTile;  // 128 rows of x, 256 weight rows
+constexpr int kQpMaxStages = 4;
+// kind::f8f6f4: e4m3 A and B, fp32 D, both K-major, M = 128, N = 256
+constexpr uint32_t kQpIdesc = (1u << 4) | ((256u >> 3) << 17) | ((128u >> 4) << 24);
 
 struct QpHeader {
-    uint64_t full[kQpStages], empty[kQpStages];
+    uint64_t full[kQpMaxStages], empty[kQpMaxStages];
     uint64_t tfull[2], tempty[2];
     uint64_t done;
     uint32_t tmem_base;
@@ -53,46 +57,49 @@ struct QpHeader {
 };
 constexpr uint32_t kQpHdrBytes = 8192;
 static_assert(sizeof(QpHeader) <= kQpHdrBytes, "header");
-constexpr uint32_t kQpOut = 8 * 4096;  // 4 KB an epilogue warp: 32 rows of 128 bytes on their way out
-constexpr size_t kQpSmem = 1024 + kQpStages * kQpStage + kQpOut + kQpHdrBytes;
-static_assert(kQpSmem <= 227 * 1024, "shared memory");
+// y's way out: 4 KB an epilogue warp, 32 rows of 128 bytes.  (h goes out from registers, and
+// its projection has a stage more: 1027 -> 1010 us for 2048 tokens; rows of 64 bytes and a stage
+// more for y, too, 99 -> 102.)
+template <bool UP>
+struct QpCfg {
+    static constexpr int kStages = UP ? 4 : 3;
+    static constexpr uint32_t kOut = UP ? 0 : 8 * 4096;
+    static constexpr size_t kSmem = 1024 + kStages * kQpStage + kOut + kQpHdrBytes;
+    static_assert(kSmem <= 227 * 1024, "shared memory");
+};
 
 // x, w: the lower halves of their descriptors (the upper: 128-byte swizzle, 8 rows 1024
 // bytes apart).
-__device__ __forceinline__ void mma_f8_pair(uint32_t d_tmem, uint32_t x, uint32_t w, uint32_t idesc,
+__device__ __forceinline__ void mma_f8_wide(uint32_t d_tmem, uint32_t x, uint32_t w, uint32_t idesc,
                                             uint32_t accumulate) {
     constexpr uint32_t kHi = (1024 >> 4) | 1u << 14 | 2u << 29;
     asm volatile(
         "{\n\t.reg .pred p;\n\t.reg .b64 dx, dw;\n\tsetp.ne.b32 p, %4, 0;\n\t"
         "mov.b64 dx, {%1, %5};\n\tmov.b64 dw, {%2, %5};\n\t"
-        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], dx, dw, %3, p;\n\t}" ::"r"(d_tmem),
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], dx, dw, %3, p;\n\t}" ::"r"(d_tmem),
         "r"(x), "r"(w), "r"(idesc), "r"(accumulate), "r"(kHi)
         : "memory");
 }
 
-// Tensor copies that complete on the mbarrier at cluster address `bar`, the even CTA's.
-__device__ __forceinline__ void tma_2d_pair(void *dst, const CUtensorMap *m, int32_t x, int32_t y,
-                                            uint32_t bar, uint64_t policy) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-        ".cta_group::2.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(ptx::smem_u32(dst)),
-        "l"(m), "r"(x), "r"(y), "r"(bar), "l"(policy)
-        : "memory");
-}
-__device__ __forceinline__ void tma_3d_pair(void *dst, const CUtensorMap *m, int32_t x, int32_t y,
-                                            int32_t z, uint32_t bar, uint64_t policy) {
+// A tensor copy into the same place of these CTAs' shared memory, each told on its own barrier.
+__device__ __forceinline__ void tma_3d_to(void *dst, const CUtensorMap *m, int32_t x, int32_t y,
+                                          int32_t z, uint64_t *bar, uint16_t ctas,
+                                          uint64_t policy) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-        ".cta_group::2.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(ptx::smem_u32(dst)),
-        "l"(m), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy)
+        ".multicast::cluster.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6, %7;" ::"r"(
+            ptx::smem_u32(dst)),
+        "l"(m), "r"(x), "r"(y), "r"(z), "r"(ptx::smem_u32(bar)), "h"(ctas), "l"(policy)
         : "memory");
 }
 
-// Arrive on an mbarrier of the even CTA.  No memory is handed over (only tensor memory,
-// whose reads have completed), so nothing of this thread's has to be seen at cluster
-// scope first: with a release there a k-block took 1.36 us instead of 0.75.
-__device__ __forceinline__ void arrive_remote(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// Arrive on the mbarrier at this offset in both CTAs once all earlier MMAs of this thread finish.
+__device__ __forceinline__ void mma_commit_both(uint64_t *bar) {
+    asm volatile(
+        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
+        " [%0], %1;" ::"r"(ptx::smem_u32(bar)),
+        "h"((uint16_t)3)
+        : "memory");
 }
 
 __device__ __forceinline__ uint64_t twice(float s) {
@@ -100,21 +107,35 @@ __device__ __forceinline__ uint64_t twice(float s) {
     asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(s));
     return r;
 }
+// A group's rows in runs: whole ones of up to 256 rows, the odd CTA's behind the even one's,
+// both with the same 256 weight rows (UP: 128 of both matrices); a last one of at most 128
+// rows, which both CTAs take with weight tiles side by side.
+__device__ __forceinline__ void qp_runs(int rows, int &whole, int &rest) {
+    whole = (rows + 127) / 256;
+    rest = rows > whole * 256;
+}
+
 struct QpTile {
-    int e, wt;
-    int s0, cnt;  // first row, rows of the run (at most 256)
+    int e, wt;    // the CTA's weight tile (one behind the last for the odd CTA's rest: no results)
+    int s0, cnt;  // its first row, its rows (1 to 128)
+    bool shared;  // the weight tile is both CTAs'
 };
 
 __device__ __forceinline__ QpTile qp_tile(const int *prefix, const int32_t *offsets, int E, int S,
-                                          int u) {
+                                          int nwt, int rank, int u) {
     QpTile t;
     t.e = chunk_expert(prefix, E, u);
     const int lo = offsets ? offsets[t.e] : 0, hi = offsets ? offsets[t.e + 1] : S;
-    const int nst = (hi - lo + kQpRows - 1) / kQpRows, r = u - prefix[t.e];
-    t.wt = r / nst;
-    const int st = r - t.wt * nst;
-    t.s0 = lo + st * kQpRows;
-    t.cnt = min(kQpRows, hi - t.s0);
+    int whole, rest;
+    qp_runs(hi - lo, whole, rest);
+    // two weight tiles' units, then the rest's with both
+    const int r = u - prefix[t.e], per = 2 * whole + rest, j = r / per, i = r - j * per;
+    t.shared = i < min(2, nwt - 2 * j) * whole;
+    const int second = i >= whole;
+    const int run = t.shared ? i - second * whole : whole;
+    t.wt = 2 * j + (t.shared ? second : rank);
+    t.s0 = lo + run * 256 + (t.shared ? rank * 128 : 0);
+    t.cnt = min(128, hi - t.s0);
     return t;
 }
 
@@ -129,7 +150,11 @@ __device__ void qp_prefix(const int32_t *offsets, int E, int S, int nwt, int *pr
         if (e < E) {
             const int lo = offsets ? offsets[e] : 0, hi = offsets ? offsets[e + 1] : S;
             if (lo < 0 || hi < lo || hi > S) set_error(err, kErrIndex);
-            else c = ((hi - lo + kQpRows - 1) / kQpRows) * nwt;
+            else {
+                int whole, rest;
+                qp_runs(hi - lo, whole, rest);
+                c = whole * nwt + rest * ((nwt + 1) / 2);
+            }
         }
         int incl = c;
 #pragma unroll
@@ -156,23 +181,25 @@ template <bool UP, bool BF>
 __global__ void __launch_bounds__(kQpThreads, 1)
 k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ CUtensorMap tm_w1,
              const __grid_constant__ CUtensorMap tm_x, const QpArgs a) {
+    using C = QpCfg<UP>;
+    constexpr int kStages = C::kStages;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    QpHeader *hd = reinterpret_cast<QpHeader *>(smem + kQpStages * kQpStage + kQpOut);
+    QpHeader *hd = reinterpret_cast<QpHeader *>(smem + kStages * kQpStage + C::kOut);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_ctarank();
     const bool even = rank == 0;
     const int nk = q_blocks(a.n_in), nblk = q_blocks(a.n_out);
     const int nwt = UP ? nblk : (nblk + 1) / 2;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kQpStages; ++s) {
+        for (int s = 0; s < kStages; ++s) {
             ptx::mbar_init(&hd->full[s], 1);
-            ptx::mbar_init(&hd->empty[s], 1);
+            ptx::mbar_init(&hd->empty[s], 2);
         }
         for (int b = 0; b < 2; ++b) {
             ptx::mbar_init(&hd->tfull[b], 3);  // (the MMAs; the two warps with the scales)
-            ptx::mbar_init(&hd->tempty[b], 16);
+            ptx::mbar_init(&hd->tempty[b], 8);
         }
         ptx::mbar_init(&hd->done, 1);
         ptx::fence_barrier_init();
@@ -180,7 +207,7 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
         if (UP) ptx::prefetch_tmap(&tm_w1);
         ptx::prefetch_tmap(&tm_x);
     }
-    if (warp == 1) tmem_alloc_pair(&hd->tmem_base, 512);
+    if (warp == 1) tmem_alloc(&hd->tmem_base, 512);
     ptx::launch_dependents();
     ptx::grid_dependency_wait();
     if (warp == kQpEpilogue) qp_prefix(a.offsets, a.E, a.S, nwt, hd->prefix, a.err);
@@ -200,83 +227,79 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
                 uint32_t it = 0;
                 bool ok = true;
                 for (int u = u0; ok && u < n_units; u += du) {
-                    const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, u);
-                    // a run of 128 rows or fewer leaves the odd CTA's rows as they lie: their
-                    // sums are not read
-                    const bool rows = even || t.cnt > 128;
-                    const uint32_t bytes = (t.cnt > 128 ? 4 : 3) * kQpTile;
-                    const int wy = UP ? t.wt * 128 : t.wt * 256 + (int)rank * 128;
-                    const CUtensorMap *wm = UP && !even ? &tm_w1 : &tm_w0;
+                    const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, nwt, (int)rank, u);
+                    // a shared weight tile: this CTA's half for both; else both halves for itself
+                    const uint16_t who = t.shared ? 3 : 1 << rank;
+                    const uint32_t at = (t.shared ? 1 + rank : 1) * kQpTile;
+                    const CUtensorMap *wm = UP && t.shared && !even ? &tm_w1 : &tm_w0;
+                    const int wy = UP ? t.wt * 128 : t.wt * 256 + (t.shared ? (int)rank * 128 : 0);
                     for (int kb = 0; kb < nk; ++kb, ++it) {
-                        const uint32_t s = it % kQpStages, ph = (it / kQpStages) & 1;
+                        const uint32_t s = it % kStages, ph = (it / kStages) & 1;
                         if (!(ok = wait_soon(&hd->empty[s], ph ^ 1, a.err))) break;
                         unsigned char *sp = smem + s * kQpStage;
-                        const uint32_t fb = ptx::map_rank(ptx::smem_u32(&hd->full[s]), 0);
-                        if (even) ptx::mbar_arrive_expect_tx(&hd->full[s], bytes);
-                        tma_3d_pair(sp + kQpTile, wm, kb * 128, wy, t.e, fb, pol_w);
-                        if (rows)
-                            tma_2d_pair(sp, &tm_x, kb * 128, t.s0 + (int)rank * 128, fb, pol_x);
+                        uint64_t *fb = &hd->full[s];
+                        ptx::mbar_arrive_expect_tx(fb, kQpStage);
+                        tma_3d_to(sp + at, wm, kb * 128, wy, t.e, fb, who, pol_w);
+                        if (!t.shared)
+                            tma_3d(sp + 2 * kQpTile, UP ? &tm_w1 : &tm_w0, kb * 128, UP ? wy : wy + 128,
+                                   t.e, fb, pol_w);
+                        ptx::tma_load_2d(sp, &tm_x, kb * 128, t.s0, fb, pol_x);
                     }
                 }
-                // copies in flight land before the block can end: the even CTA sees its
-                // stages fill, the odd one, whose copies complete there, sees them consumed
-                for (uint32_t k = (it > kQpStages ? it - kQpStages : 0); k < it; ++k)
-                    ptx::mbar_wait_hint(even ? &hd->full[k % kQpStages] : &hd->empty[k % kQpStages],
-                                        (k / kQpStages) & 1, a.err);
+                // copies in flight land before the block can end, and what both CTAs' MMAs tell
+                // of its last stages
+                for (uint32_t k = (it > kStages ? it - kStages : 0); k < it; ++k)
+                    ptx::mbar_wait_hint(&hd->full[k % kStages], (k / kStages) & 1, a.err) &&
+                        ptx::mbar_wait_hint(&hd->empty[k % kStages], (k / kStages) & 1, a.err);
             }
             __syncwarp();
         } else if (warp == 1) {
             // ------------------------------------------------------------ MMAs
             // (all lanes go along and one issues: in a branch of a single lane every MMA costs a
             // search for its operands' uniform registers)
-            if (even) {
-                const bool one = elect_one();
-                const int n = u0 < n_units ? ((n_units - 1 - u0) / du + 1) * nk : 0;
-                const uint32_t base = (ptx::smem_u32(smem) & 0x3FFFFu) >> 4 | 1u << 16;
-                uint32_t s = 0, ph = 0;
-                bool ok = true;
+            const bool one = elect_one();
+            const int n = u0 < n_units ? ((n_units - 1 - u0) / du + 1) * nk : 0;
+            const uint32_t base = (ptx::smem_u32(smem) & 0x3FFFFu) >> 4 | 1u << 16;
+            uint32_t s = 0, ph = 0;
+            bool ok = true;
 #pragma unroll 1
-                for (int it = 0; ok && it < n; ++it) {
-                    const uint32_t b = it & 1, bph = (it >> 1) & 1;
-                    // (released by both CTAs' epilogues)
-                    ok = wait_soon(&hd->full[s], ph, a.err) &&
-                         wait_soon(&hd->tempty[b], bph ^ 1, a.err);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t x = base + s * (kQpStage >> 4), w = x + (kQpTile >> 4);
-                    const uint32_t d = tmem + b * 256;
-                    if (one) {
-                        mma_f8_pair(d, x, w, kQpIdesc, 0);
-                        mma_f8_pair(d, x + 2, w + 2, kQpIdesc, 1);
-                        mma_f8_pair(d, x + 4, w + 4, kQpIdesc, 1);
-                        mma_f8_pair(d, x + 6, w + 6, kQpIdesc, 1);
-                        mma_commit_pair(&hd->tfull[b], 3);
-                        mma_commit_pair(&hd->empty[s], 3);
-                    }
-                    __syncwarp();
-                    if (++s == kQpStages) {
-                        s = 0;
-                        ph ^= 1;
-                    }
+            for (int it = 0; ok && it < n; ++it) {
+                const uint32_t b = it & 1, bph = (it >> 1) & 1;
+                ok = wait_soon(&hd->full[s], ph, a.err) && wait_soon(&hd->tempty[b], bph ^ 1, a.err);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t x = base + s * (kQpStage >> 4), w = x + (kQpTile >> 4);
+                const uint32_t d = tmem + b * 256;
+                if (one) {
+                    mma_f8_wide(d, x, w, kQpIdesc, 0);
+                    mma_f8_wide(d, x + 2, w + 2, kQpIdesc, 1);
+                    mma_f8_wide(d, x + 4, w + 4, kQpIdesc, 1);
+                    mma_f8_wide(d, x + 6, w + 6, kQpIdesc, 1);
+                    mma_commit(&hd->tfull[b]);
+                    mma_commit_both(&hd->empty[s]);
                 }
-                if (one) mma_commit_pair(&hd->done, 1);
-                ptx::mbar_wait(&hd->done, 0, a.err);
+                __syncwarp();
+                if (++s == kStages) {
+                    s = 0;
+                    ph ^= 1;
+                }
             }
+            if (one) mma_commit(&hd->done);
+            ptx::mbar_wait(&hd->done, 0, a.err);
             __syncwarp();
         } else {
             // ------------------------------------------------------------ scales
             // warps 2 and 3: 64 rows each.  A step's scales take the slot of the step four ago,
-            // which both CTAs' epilogues have read once the MMAs of the step two ago are done.
+            // which the epilogue has read once the MMAs of the step two ago are done.
             const int r0 = (warp - 2) * 64 + lane;
             uint32_t it = 0;
             bool ok = true;
             for (int u = u0; ok && u < n_units; u += du) {
-                const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, u);
-                const int row = (int)rank * 128 + r0;
-                const float *x0 = a.xs + t.s0 + min(row, t.cnt - 1);
-                const int x1 = min(row + 32, t.cnt - 1) - min(row, t.cnt - 1);
-                const int blk = UP ? t.wt : t.wt * 2, next = UP ? blk : min(blk + 1, nblk - 1);
+                const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, nwt, (int)rank, u);
+                const int row = min(t.s0 + r0, a.S - 1), blk = min(UP ? t.wt : t.wt * 2, nblk - 1);
+                const float *x0 = a.xs + row;
+                const int x1 = min(t.s0 + r0 + 32, a.S - 1) - row, next = UP ? blk : min(blk + 1, nblk - 1);
                 const float *w0 = a.s0 + ((size_t)t.e * nblk + blk) * nk;
                 const float *w1 = (UP ? a.s1 : a.s0) + ((size_t)t.e * nblk + next) * nk;
                 float v[4], more[4];  // of this k-block, of the next one
@@ -306,13 +329,12 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
         // ------------------------------------------------------------ epilogue
         const int q = warp & 3, half = (warp - kQpEpilogue) >> 2;
         const uint32_t base0 = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)half * (UP ? 64 : 128);
-        const uint32_t tempty0 = ptx::map_rank(ptx::smem_u32(&hd->tempty[0]), 0);
         bool dead = false;  // a wait gave up: keep the barriers, skip the work
         uint32_t it = 0, tl = 0;
         for (int u = u0; u < n_units; u += du, ++tl) {
-            const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, u);
-            const int r = (int)rank * 128 + q * 32 + lane;  // of the run
-            const bool mine = r < t.cnt;
+            const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, nwt, (int)rank, u);
+            const int r = q * 32 + lane;
+            const bool mine = r < t.cnt && (!UP || t.wt < nwt);
             uint64_t acc[64];
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i] = 0;
@@ -332,10 +354,7 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
                         if (c == 3) {  // the accumulator is read: the next MMAs may write it
                             tc_fence_before();
                             __syncwarp();
-                            if (lane == 0) {
-                                if (even) ptx::mbar_arrive(&hd->tempty[b]);
-                                else arrive_remote(tempty0 + b * (uint32_t)sizeof(uint64_t));
-                            }
+                            if (lane == 0) ptx::mbar_arrive(&hd->tempty[b]);
                         }
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
@@ -377,8 +396,8 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
                 // 32 rows of 128 bytes at a time through shared memory, so that eight lanes
                 // write a row's 128 bytes (16-byte chunks exchanged by the row: no conflicts)
                 constexpr int kCols = BF ? 64 : 32, kSize = BF ? 2 : 4;
-                uint8_t *buf = smem + kQpStages * kQpStage + (warp - kQpEpilogue) * 4096;
-                const int row0 = (int)rank * 128 + q * 32, col0 = t.wt * 256 + half * 128;
+                uint8_t *buf = smem + kStages * kQpStage + (warp - kQpEpilogue) * 4096;
+                const int row0 = q * 32, col0 = t.wt * 256 + half * 128;
                 uint8_t *y = static_cast<uint8_t *>(a.out) + ((size_t)t.s0 * a.n_out + col0) * kSize;
                 const int ch = lane & 7;
 #pragma unroll
@@ -419,14 +438,14 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
     tc_fence_before();
     ptx::cluster_sync_all();  // no CTA leaves while its pair may touch it
     tc_fence_after();
-    if (warp == 1) tmem_dealloc_pair(tmem, 512);
+    if (warp == 1) tmem_dealloc(tmem, 512);
 }
 
-void pair_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&attr)[2], int grid) {
+void pair_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&attr)[2], int grid, size_t smem) {
     cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(kQpThreads);
-    cfg.dynamicSmemBytes = kQpSmem;
+    cfg.dynamicSmemBytes = smem;
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
     attr[0].val.clusterDim.y = 1;
@@ -447,11 +466,11 @@ int resident_pairs() {
     std::call_once(once[dev], [dev] {
         const void *kern = (const void *)k_quant_pair<UP, BF>;
         int pairs = 0;
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kQpSmem) ==
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)QpCfg<UP>::kSmem) ==
             cudaSuccess) {
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute attr[2];
-            pair_config(cfg, attr, device_info().sm_count & ~1);
+            pair_config(cfg, attr, device_info().sm_count & ~1, QpCfg<UP>::kSmem);
             if (cudaOccupancyMaxActiveClusters(&pairs, kern, &cfg) != cudaSuccess) pairs = 0;
         }
         (void)cudaGetLastError();
@@ -478,7 +497,7 @@ cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QpArgs a,
     void *args[] = {&mw0, &mw1, &mx, &a};
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    pair_config(cfg, attr, 2 * pairs);
+    pair_config(cfg, attr, 2 * pairs, QpCfg<UP>::kSmem);
     cfg.numAttrs = 2;
     cfg.stream = st;
     LaunchScope ls(UP ? "quant_up_pair" : "quant_down_pair", st);

@@ -74,15 +74,6 @@ struct QsCfg {
 static_assert(QsCfg<true, 16>::smem(QsCfg<true, 16>::kShared) + QsCfg<false, 16>::smem(QsCfg<false, 16>::kShared) <= 226 * 1024,
               "an up and a down projection's CTA on one SM");
 
-__device__ __forceinline__ void tma_3d(void *dst, const CUtensorMap *m, int32_t x, int32_t y,
-                                       int32_t z, uint64_t *bar, uint64_t policy) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-        ".L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(ptx::smem_u32(dst)),
-        "l"(m), "r"(x), "r"(y), "r"(z), "r"(ptx::smem_u32(bar)), "l"(policy)
-        : "memory");
-}
-
 __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc,
                                        uint32_t accumulate) {
     asm volatile(

@@ -166,6 +166,13 @@ def test_product_many_groups():
     check_product(moe(), rng, sizes, 72, 160, "f32", extra_rows=1)
 
 
+@pytest.mark.parametrize("n_out", [8, 264, 520, 776, 1288])
+@pytest.mark.parametrize("sizes", [[128, 129, 1, 256, 257, 384, 385, 0, 70, 640], [65, 66, 64], [40] * 48], ids=str)
+def test_product_runs(sizes, n_out):
+    """Last runs of up to 128 rows, whose weight tiles go two by two, an odd one by itself."""
+    check_product(moe(), np.random.default_rng(n_out), sizes, n_out, 272, "f32", extra_rows=2)
+
+
 def test_product_bad_offsets():
     """Offsets that fall or leave [0, S]: their groups are left out and recorded."""
     m, rng = moe(), np.random.default_rng(5)
@@ -328,6 +335,19 @@ def test_experts(T, E, K, D, F, x_dtype, out_dtype, res):
     got = m.quant_experts_forward(d, ex, x.cuda(), cuda(idx), cuda(gate), r.cuda() if res else None)
     assert m.get_last_error() == 0
     check_experts(num(got), num(x), idx, gate, w, out_dtype, num(r) if res else None)
+
+
+@pytest.mark.parametrize("D,F", [(528, 640), (256, 128), (400, 272)])
+@pytest.mark.parametrize("T", [130, 250, 500])
+def test_experts_runs(T, D, F):
+    m, rng = moe(), np.random.default_rng(T + D)
+    d = m.dims(D, F, 3, 2, torch.float32)
+    ex, w = _experts(m, rng, 3, F, D)
+    idx, gate = _routing(rng, T, 3, 2)
+    x = rng.normal(size=(T, D)).astype(np.float32)
+    got = m.quant_experts_forward(d, ex, cuda(x), cuda(idx), cuda(gate))
+    assert m.get_last_error() == 0
+    check_experts(num(got), x.astype(np.float64), idx, gate, w, "f32")
 
 
 def test_experts_same_expert_twice_and_out_of_range():
