@@ -150,7 +150,7 @@ cudaError_t launch_quant_stream_down(const QuantGemm &g, const QuantDown &u, con
                                      int cols, bool alone, cudaStream_t st);
 
 // The same for many rows a group, on CTA pairs (quant_pair_tc.cu), where the device
-// keeps such pairs resident.
+// keeps such pairs resident; they, too, read offsets and weights early.
 bool quant_pair_ok();
 cudaError_t launch_quant_pair_up(const QuantGemm &g, const QuantUp &u, cudaStream_t st);
 cudaError_t launch_quant_pair_down(const QuantGemm &g, const QuantDown &u, cudaStream_t st);

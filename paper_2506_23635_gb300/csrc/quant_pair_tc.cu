@@ -209,7 +209,8 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
     }
     if (warp == 1) tmem_alloc(&hd->tmem_base, 512);
     ptx::launch_dependents();
-    ptx::grid_dependency_wait();
+    // (the offsets are older than the launch ahead, which lets this one start behind its own
+    // wait only, or is started so itself)
     if (warp == kQpEpilogue) qp_prefix(a.offsets, a.E, a.S, nwt, hd->prefix, a.err);
     tc_fence_before();
     ptx::cluster_sync_all();  // barriers initialised in both CTAs
@@ -224,30 +225,42 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
             if (lane == 0) {
                 // (normal priority: a weight tile serves the runs of its expert)
                 const uint64_t pol_w = ptx::policy_evict_normal(), pol_x = ptx::policy_evict_last();
+                auto weights = [&](const QpTile &t, uint32_t s, int kb) {
+                    // a shared weight tile: this CTA's half for both; else both halves for itself
+                    const CUtensorMap *wm = UP && t.shared && !even ? &tm_w1 : &tm_w0;
+                    const int wy = UP ? t.wt * 128 : t.wt * 256 + (t.shared ? (int)rank * 128 : 0);
+                    unsigned char *sp = smem + s * kQpStage;
+                    uint64_t *fb = &hd->full[s];
+                    ptx::mbar_arrive_expect_tx(fb, kQpStage);
+                    tma_3d_to(sp + (t.shared ? 1 + rank : 1) * kQpTile, wm, kb * 128, wy, t.e, fb,
+                              t.shared ? 3 : 1 << rank, pol_w);
+                    if (!t.shared)
+                        tma_3d(sp + 2 * kQpTile, UP ? &tm_w1 : &tm_w0, kb * 128, UP ? wy : wy + 128, t.e,
+                               fb, pol_w);
+                };
+                // the first stages' weights, which no kernel ahead writes, before the wait (300 tokens
+                // of 40 small experts 106 -> 103 us)
+                const uint32_t early = u0 < n_units ? min(kStages, nk) : 0;
+                if (early) {
+                    const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, nwt, (int)rank, u0);
+                    for (uint32_t k = 0; k < early; ++k) weights(t, k, k);
+                }
+                ptx::grid_dependency_wait();
                 uint32_t it = 0;
                 bool ok = true;
                 for (int u = u0; ok && u < n_units; u += du) {
                     const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, nwt, (int)rank, u);
-                    // a shared weight tile: this CTA's half for both; else both halves for itself
-                    const uint16_t who = t.shared ? 3 : 1 << rank;
-                    const uint32_t at = (t.shared ? 1 + rank : 1) * kQpTile;
-                    const CUtensorMap *wm = UP && t.shared && !even ? &tm_w1 : &tm_w0;
-                    const int wy = UP ? t.wt * 128 : t.wt * 256 + (t.shared ? (int)rank * 128 : 0);
                     for (int kb = 0; kb < nk; ++kb, ++it) {
                         const uint32_t s = it % kStages, ph = (it / kStages) & 1;
                         if (!(ok = wait_soon(&hd->empty[s], ph ^ 1, a.err))) break;
-                        unsigned char *sp = smem + s * kQpStage;
-                        uint64_t *fb = &hd->full[s];
-                        ptx::mbar_arrive_expect_tx(fb, kQpStage);
-                        tma_3d_to(sp + at, wm, kb * 128, wy, t.e, fb, who, pol_w);
-                        if (!t.shared)
-                            tma_3d(sp + 2 * kQpTile, UP ? &tm_w1 : &tm_w0, kb * 128, UP ? wy : wy + 128,
-                                   t.e, fb, pol_w);
-                        ptx::tma_load_2d(sp, &tm_x, kb * 128, t.s0, fb, pol_x);
+                        if (it >= early) weights(t, s, kb);
+                        ptx::tma_load_2d(smem + s * kQpStage, &tm_x, kb * 128, t.s0, &hd->full[s], pol_x);
                     }
                 }
                 // copies in flight land before the block can end, and what both CTAs' MMAs tell
-                // of its last stages
+                // of its last stages.  (Where a wait gave up, stages whose weights came early may
+                // wait for rows that do not come: these waits end too.)
+                it = max(it, early);
                 for (uint32_t k = (it > kStages ? it - kStages : 0); k < it; ++k)
                     ptx::mbar_wait_hint(&hd->full[k % kStages], (k / kStages) & 1, a.err) &&
                         ptx::mbar_wait_hint(&hd->empty[k % kStages], (k / kStages) & 1, a.err);
@@ -292,6 +305,7 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
             // ------------------------------------------------------------ scales
             // warps 2 and 3: 64 rows each.  A step's scales take the slot of the step four ago,
             // which the epilogue has read once the MMAs of the step two ago are done.
+            ptx::grid_dependency_wait();
             const int r0 = (warp - 2) * 64 + lane;
             uint32_t it = 0;
             bool ok = true;
@@ -330,6 +344,7 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
         const int q = warp & 3, half = (warp - kQpEpilogue) >> 2;
         const uint32_t base0 = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)half * (UP ? 64 : 128);
         bool dead = false;  // a wait gave up: keep the barriers, skip the work
+        ptx::grid_dependency_wait();  // (the result's last readers)
         uint32_t it = 0, tl = 0;
         for (int u = u0; u < n_units; u += du, ++tl) {
             const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, nwt, (int)rank, u);

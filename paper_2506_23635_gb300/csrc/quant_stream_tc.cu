@@ -18,8 +18,8 @@
 //
 // Measured: 16 rows of 38912 x 16384 100 us, 6.4 TB/s of weights (0.94 of a copy's rate); one row
 // of 8192 x 6144 14 us with the launch ahead (7.4 at the copy's rate); 16 experts of
-// 6144 x 10752, 16 rows each, up 314 us and down 159 (0.99 and 0.98); 40 of 2000 x 1424 with 45
-// rows each (64 columns) 63 and 41 us, the epilogue's.
+// 6144 x 10752, 16 rows each, up 314 us and down 159 (0.99 and 0.98); 40 of 2000 x 1424 with 30
+// rows each (64 columns) 63 and 43 us, the epilogue's.
 #include "quant.cuh"
 
 namespace moe {
