@@ -214,12 +214,20 @@ __device__ __forceinline__ double warp_sum(double v) {
 // What 32 bits may be off by, of a score s, in steps of 2^-24.  exp(d) / z: |d| of the
 // subtraction's rounding, 4 of the exponential, 4 + 13 of its sum over 256, 3 of the quotient
 // by a reciprocal.  1 / (1 + exp(-d)): the fast exponential's 4 + 2.4 |d| (2 + 1.18 |d| units in
-// the last place), of which the share 1 - s arrives, 1 of the sum, 4 of the fast quotient.
+// the last place), of which the share 1 - s arrives, 1 of the sum, 4 of the fast quotient.  Both:
+// 1 of the key's rounding, 1 of a bound's (key and error added).  (Beyond |d| = 104 s is 0 or 1.)
 __device__ __forceinline__ float score_err(bool sigmoid, float s, float d) {
-    const float steps = sigmoid ? 6.f + (1.f - s) * (5.f + 2.5f * fabsf(d)) : 28.f + 1.1f * fabsf(d);
+    d = fminf(fabsf(d), 128.f);
+    const float steps = sigmoid ? 7.f + (1.f - s) * (5.f + 2.5f * d) : 29.f + 1.1f * d;
     return s * steps * 5.9604645e-8f;
 }
-constexpr float kSumErr = 1.2e-7f;  // a key's or a sum's rounding, of either side
+constexpr float kSumErr = 1.2e-7f;  // the bias' part of a key's and a bound's rounding; a sum's
+
+// The same numbers give the same keys.
+__device__ __forceinline__ bool same_key(const float *l, const float *bias, int e, int f) {
+    return __float_as_uint(l[e]) == __float_as_uint(l[f]) &&
+           __float_as_uint(bias[e]) == __float_as_uint(bias[f]);
+}
 
 // A warp's scratch; what 64 bits need takes the same place.
 struct alignas(16) SelScratch {
@@ -388,7 +396,7 @@ __device__ __noinline__ bool select_pairs(const SelArgs &a, const float *l, SelS
         float2 s = w.p.value[e];
         if (!a.sigmoid) s = pair_div(s, z);
         const float b = biased ? a.bias[e] : 0.f;
-        err = fmaxf(err, kPairErr * (fabsf(s.x) + 0x1p-8f * fabsf(b)));
+        if (isfinite(b)) err = fmaxf(err, kPairErr * (fabsf(s.x) + 0x1p-8f * fabsf(b)));
         if (biased) {
             const float2 t = pair_sum(s.x, b);
             s = isfinite(t.x) ? pair_norm(t.x, t.y + s.y) : make_float2(s.x + b, 0.f);
@@ -475,9 +483,8 @@ __device__ __noinline__ bool select_pairs(const SelArgs &a, const float *l, SelS
         if ((biased || by_score) && high.x > -INFINITY)
             clear = isfinite(low.x) && (low.x - high.x) + (low.y - high.y) > 4.f * err;
     }
-    const int n = biased ? a.K + 1 : a.K;
 #pragma unroll 1
-    for (int k = 0; k < n; ++k) {
+    for (int k = 0; k < a.K; ++k) {
         unsigned long long best = code[0];
         int at = 0;
 #pragma unroll
@@ -491,23 +498,26 @@ __device__ __noinline__ bool select_pairs(const SelArgs &a, const float *l, SelS
         const uint32_t lo = __reduce_max_sync(0xffffffffu, mine ? (uint32_t)best : 0u);
         const int who = __ffs(__ballot_sync(0xffffffffu, mine && (uint32_t)best == lo)) - 1;
         if (lane == who) {
-            w.sel[k] = (int16_t)(best ? e0 + at : -1);
+            w.sel[k] = (int16_t)(e0 + at);
 #pragma unroll
             for (int i = 0; i < NE; ++i)
                 if (i == at) code[i] = 0;
         }
     }
     __syncwarp();
-    if (biased)
-        for (int k = lane; k < a.K; k += 32) {
-            const int e = w.sel[k], f = w.sel[k + 1];
-            if (f < 0) break;
-            if (__float_as_uint(l[e]) == __float_as_uint(l[f]) &&
-                __float_as_uint(a.bias[e]) == __float_as_uint(a.bias[f]))
-                continue;
+    if (biased) {
+        // neighbours among the K; the last of them and each one left out that is not its equal
+        auto apart = [&](int e, int f) {
             const float2 x = w.p.value[e], y = w.p.value[f];
-            if (isfinite(x.x) && isfinite(y.x) && !((x.x - y.x) + (x.y - y.y) > 2.f * err)) clear = false;
-        }
+            return !isfinite(x.x) || !isfinite(y.x) || (x.x - y.x) + (x.y - y.y) > 2.f * err ||
+                   same_key(l, a.bias, e, f);
+        };
+        for (int k = lane; k + 1 < a.K; k += 32) clear = clear && apart(w.sel[k], w.sel[k + 1]);
+        const int last = w.sel[a.K - 1];
+#pragma unroll
+        for (int i = 0; i < NE; ++i)
+            if (code[i]) clear = clear && apart(last, e0 + i);
+    }
     return __all_sync(0xffffffffu, clear);
 }
 
@@ -641,14 +651,18 @@ k_select(const SelArgs a) {
         for (int i = 0; i < NE; ++i) s[i] = __fdividef(1.f, 1.f + __expf(-v[i]));
     }
     uint32_t code[NE];
-    float err = 0.f, kv[NE];  // of the keys
+    float err = 0.f, kv[NE], up[NE];  // the largest error, keys, keys with their errors
 #pragma unroll
     for (int i = 0; i < NE; ++i) {
         const float key = biased ? s[i] + b[i] : v[i];
         code[i] = e0 + i < a.E ? key_code(key) : 0u;
         kv[i] = key;
-        if ((biased || by_score) && a.G > 1 && e0 + i < a.E)
-            err = fmaxf(err, score_err(a.sigmoid, s[i], v[i] - m) + kSumErr * fabsf(b[i]));
+        up[i] = -INFINITY;
+        if ((biased || by_score) && e0 + i < a.E && isfinite(key)) {
+            const float off = score_err(a.sigmoid, s[i], v[i] - m) + kSumErr * fabsf(b[i]);
+            err = fmaxf(err, off);
+            up[i] = key + off;
+        }
     }
     if (biased || by_score) keep<NE>(w.f.score + e0, s);
     keep<NE>(w.f.key + e0, kv);
@@ -720,8 +734,7 @@ k_select(const SelArgs a) {
             }
         }
     }
-    const int n = biased ? a.K + 1 : a.K;
-    for (int k = 0; k < n; ++k) {
+    for (int k = 0; k < a.K; ++k) {
         uint32_t best = code[0];
         int at = 0;
 #pragma unroll
@@ -734,40 +747,62 @@ k_select(const SelArgs a) {
         // (the lowest lane has the lowest experts)
         const int who = __ffs(__ballot_sync(0xffffffffu, best == top)) - 1;
         if (lane == who) {
-            w.sel[k] = (int16_t)(top ? e0 + at : -1);  // (none left: only for the one beyond K)
+            w.sel[k] = (int16_t)(e0 + at);
 #pragma unroll
             for (int i = 0; i < NE; ++i)
                 if (i == at) code[i] = 0u;
         }
     }
     __syncwarp();
-    // order: of the K is clear (clear: which they are); edge: the last one's key is also that
-    // of the first one left out, so that a change of order could change which they are
-    bool order = true, edge = false;
-    if (biased)
+    // clear: which the K are; order: theirs is clear too
+    bool order = true;
+    if (biased) {
+        float lo = INFINITY, hi = -INFINITY;  // the least that a key kept may be, the most of one left out
+        auto off = [&](int e) {
+            return score_err(a.sigmoid, w.f.score[e], l[e] - m) + kSumErr * fabsf(a.bias[e]);
+        };
         for (int k = lane; k < a.K; k += 32) {
-            const int e = w.sel[k], f = w.sel[k + 1];
-            if (f < 0) break;
-            const float le = l[e], lf = l[f], be = a.bias[e], bf = a.bias[f];
-            // the same numbers give the same keys
-            if (__float_as_uint(le) == __float_as_uint(lf) && __float_as_uint(be) == __float_as_uint(bf)) {
-                edge = k == a.K - 1;
-                continue;
-            }
-            const float ke = w.f.key[e], kf = w.f.key[f];
-            // an infinite bias decides by itself; NaN is below everything
-            if (isnan(ke) || isnan(kf) || isinf(ke) || isinf(kf)) continue;
-            const float off = score_err(a.sigmoid, w.f.score[e], le - m) +
-                              score_err(a.sigmoid, w.f.score[f], lf - m) +
-                              kSumErr * (fabsf(be) + fabsf(bf));
-            if (!(ke - kf > off)) (k == a.K - 1 ? clear : order) = false;
+            const int e = w.sel[k];
+            const float ke = w.f.key[e];
+            if (!isfinite(ke)) continue;  // an infinite bias decides by itself; NaN is below everything
+            lo = fminf(lo, ke - off(e));
+            if (k + 1 == a.K) continue;
+            const int f = w.sel[k + 1];
+            const float kf = w.f.key[f];
+            if (isfinite(kf) && !(ke - kf > off(e) + off(f)) && !same_key(l, a.bias, e, f)) order = false;
         }
+#pragma unroll
+        for (int i = 0; i < NE; ++i)
+            if (code[i]) hi = fmaxf(hi, up[i]);
+        const int last = w.sel[a.K - 1];
+        const float kl = w.f.key[last];
+        if (isfinite(kl)) {
+            lo = key_of(__reduce_min_sync(0xffffffffu, key_code(lo)));
+            hi = key_of(__reduce_max_sync(0xffffffffu, key_code(hi)));
+            if (!(lo > hi)) {
+                // Equals of the last one kept may be left out, by their index, where every other one kept
+                // is above them and every other one left out is below those kept.
+                bool fits = true, equal = false;
+#pragma unroll
+                for (int i = 0; i < NE; ++i)
+                    if (code[i]) {
+                        if (same_key(l, a.bias, last, e0 + i)) equal = true;
+                        else if (!(lo > up[i])) fits = false;
+                    }
+                if (__any_sync(0xffffffffu, equal))
+                    for (int k = lane; k < a.K; k += 32) {
+                        const int e = w.sel[k];
+                        const float ke = w.f.key[e];
+                        if (isfinite(ke) && !(ke - off(e) > kl + off(last)) && !same_key(l, a.bias, last, e))
+                            fits = false;
+                    }
+                if (!fits) clear = false;
+            }
+        }
+    }
     clear = __all_sync(0xffffffffu, clear);
     order = __all_sync(0xffffffffu, order);
-    if (clear && !order) {
-        clear = a.sigmoid && a.K <= 32 && !__any_sync(0xffffffffu, edge);
-        if (clear) clear = order_pairs(a, l, w, lane);
-    }
+    if (clear && !order) clear = a.sigmoid && a.K <= 32 && order_pairs(a, l, w, lane);
     // weights: the scores anew, with the full exponential and quotient
     float sum = 0.f, own = 0.f;
     auto weights = [&]() {

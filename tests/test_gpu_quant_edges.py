@@ -1,0 +1,65 @@
+"""8-bit experts on the GPU where their error bounds are at their ends: choices that near keys of
+unlike errors decide."""
+import numpy as np
+import pytest
+
+from tests.test_gpu_quant import check_select, moe
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- the choice of experts -----------------------------------------------------------
+
+
+@pytest.mark.parametrize("logits,K", [([20, 20, 21], 1), ([8, 8, 8.000001], 1), ([30, 20, 20, 20.5, 40], 2),
+                                      ([1, 20, 20, 20, 21, 2], 1), ([-5, 17, 17, 17.000002, 17.000002], 3)], ids=str)
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_select_equals_at_the_border(score, logits, K):
+    """The last one kept and the first left out are equal, another whose key 32 bits do not tell from
+    theirs lies behind."""
+    l = np.array([logits] * 5, np.float32)
+    l[1:] += np.array([[0], [-0.5], [0.25], [1]], np.float32)
+    check_select(moe(), l, np.zeros(l.shape[1]), K, score=score)
+
+
+def test_select_small_errors_beside_a_large_one():
+    """The two at the border are further apart than their own errors; a third, a score near one with a
+    bias that takes it to their size, has the largest key."""
+    for l, b in (([-6.9995, -6.9995036, 3.3423553], [0, 0, -0.96494204]),
+                 ([-7.143973, -7.8893886, 1.6407677], [.00121102, .00162542, -.83563936])):
+        l, b = np.array(l, np.float32), np.array(b, np.float32)
+        around = np.tile(l, (400, 1))  # (and neighbours of it, so that any exponential meets some)
+        around[:, 2] += np.float32(2.0 ** -23) * (np.arange(400) - 200)
+        check_select(moe(), around, b, 1, score="sigmoid")
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,K,G,kept", [(16, 1, 1, 1), (16, 2, 1, 1), (24, 5, 1, 1), (64, 3, 1, 1), (256, 8, 1, 1),
+                                        (24, 2, 4, 2), (256, 4, 8, 4)])
+def test_select_wide_biases(score, E, K, G, kept):
+    """Biases as wide as the scores, so that small and large scores meet at the same key: keys t + noise
+    of 1e-8 to 1e-5 for one t a token."""
+    rng = np.random.default_rng(E + K + G)
+    T = 2000
+    bias = np.where(rng.random(E) < 0.5, 0.0, -rng.random(E) * (0.95 if score == "sigmoid" else 1.6 / E))
+    bias = bias.astype(np.float32)
+    t = np.exp(rng.uniform(np.log(1e-4), np.log(0.02 if score == "sigmoid" else 0.3 / E), (T, 1)))
+    noise = rng.normal(size=(T, E)) * 10.0 ** rng.uniform(-8, -5, (T, 1)) * t ** 0.5
+    s = np.clip(t + noise - bias, 1e-7, 0.999)
+    if score == "sigmoid":
+        logits = np.log(s / (1 - s))
+    else:
+        s[:, 0] += np.maximum(1.0 - s.sum(1), 1e-3)  # (the rest of the sum: one large score)
+        logits = np.log(s / s.sum(1, keepdims=True)) + rng.normal(size=(T, 1))
+    check_select(moe(), logits, bias, K, score=score, n_groups=G, top_groups=kept, group_top=2 if G > 1 else 1)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_select_barred_experts(score):
+    """Biases of -1e9 bar experts; what rounding does to their keys decides nothing, but among themselves."""
+    rng = np.random.default_rng(1)
+    logits, bias = rng.normal(size=(500, 64)), rng.normal(size=64) * 0.05
+    bias[::3] = -1e9
+    check_select(moe(), logits, bias, 6, score=score)
+    check_select(moe(), logits, bias, 50, score=score)
+    check_select(moe(), logits, bias, 6, score=score, n_groups=8, top_groups=4, group_top=2)
