@@ -216,10 +216,11 @@ __device__ __forceinline__ double warp_sum(double v) {
 // by a reciprocal.  1 / (1 + exp(-d)): the fast exponential's 4 + 2.4 |d| (2 + 1.18 |d| units in
 // the last place), of which the share 1 - s arrives, 1 of the sum, 4 of the fast quotient.  Both:
 // 1 of the key's rounding, 1 of a bound's (key and error added).  (Beyond |d| = 104 s is 0 or 1.)
+// And 2^-126 at once: the fast quotient of a larger divisor is 0, smaller numbers have fixed steps.
 __device__ __forceinline__ float score_err(bool sigmoid, float s, float d) {
     d = fminf(fabsf(d), 128.f);
     const float steps = sigmoid ? 7.f + (1.f - s) * (5.f + 2.5f * d) : 29.f + 1.1f * d;
-    return s * steps * 5.9604645e-8f;
+    return fmaf(s * steps, 5.9604645e-8f, 0x1p-125f);
 }
 constexpr float kSumErr = 1.2e-7f;  // the bias' part of a key's and a bound's rounding; a sum's
 

@@ -63,3 +63,11 @@ def test_select_barred_experts(score):
     check_select(moe(), logits, bias, 6, score=score)
     check_select(moe(), logits, bias, 50, score=score)
     check_select(moe(), logits, bias, 6, score=score, n_groups=8, top_groups=4, group_top=2)
+
+
+def test_select_smallest_scores():
+    """Scores about 2^-126, where their 32-bit form may be zero, beside biases of that size."""
+    rng = np.random.default_rng(2)
+    logits = rng.uniform(-89.5, -86.5, size=(600, 12))
+    bias = rng.uniform(0, 2e-38, 12)
+    check_select(moe(), logits, bias, 3, score="sigmoid")
