@@ -587,6 +587,12 @@ __device__ void write_exact(const SelArgs &a, int t, const SelScratch &w, int la
     }
 }
 
+// 1 / (1 + exp(-x)), also where exp(-x) leaves the numbers of 32 bits.
+__device__ __forceinline__ float sigmoid(float x) {
+    const float e = expf(-fabsf(x));
+    return (x < 0.f ? e : 1.f) / (1.f + e);
+}
+
 template <int NE>
 __device__ __forceinline__ void keep(float *to, const float (&v)[NE]) {
     if constexpr (NE >= 4) {
@@ -810,7 +816,7 @@ k_select(const SelArgs a) {
         sum = 0.f;
         for (int k = lane; k < a.K; k += 32) {
             const float x = l[w.sel[k]];
-            own = a.sigmoid ? 1.f / (1.f + expf(-x)) : expf(x - m) / z;
+            own = a.sigmoid ? sigmoid(x) : expf(x - m) / z;
             sum += own;
         }
         sum = moe::warp_sum(sum);
@@ -831,7 +837,7 @@ k_select(const SelArgs a) {
         const int e = w.sel[k];
         if (a.K > 32) {
             const float x = l[e];
-            own = a.sigmoid ? 1.f / (1.f + expf(-x)) : expf(x - m) / z;
+            own = a.sigmoid ? sigmoid(x) : expf(x - m) / z;
         }
         a.idx[(size_t)t * a.K + k] = e;
         a.gate[(size_t)t * a.K + k] = (a.renorm ? own / sum : own) * a.scale;

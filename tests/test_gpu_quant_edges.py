@@ -71,3 +71,9 @@ def test_select_smallest_scores():
     logits = rng.uniform(-89.5, -86.5, size=(600, 12))
     bias = rng.uniform(0, 2e-38, 12)
     check_select(moe(), logits, bias, 3, score="sigmoid")
+
+
+def test_select_gates_of_the_smallest_scores():
+    """Sigmoids down to the smallest number of 32 bits, lifted by the scale."""
+    logits = -80.0 - np.arange(48).reshape(2, 24) * 0.5
+    check_select(moe(), logits, None, 24, score="sigmoid", renormalise=False, scale=1e30)
