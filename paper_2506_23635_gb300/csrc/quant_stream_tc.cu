@@ -37,7 +37,7 @@ struct QsHeader {
     uint64_t tfull[4], tempty[4];
     uint64_t done;
     uint32_t tmem_base;
-    int last, ready[2];  // (ready: pieces in turn)
+    int last, ready[2];  // (ready: of the shared piece that ends or continues a tile, that begins one)
     int prefix[257];       // tiles of the experts ahead
     alignas(16) float scale[8][2][2][32];  // warp, k-blocks in turn: x's times w1's (w's), v1's
     uint32_t amax[4][64];
@@ -384,9 +384,11 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                 continue;
             }
             // are the tile's other pieces all done?  (That of its first k-blocks is the last of a
-            // CTA's share, the others the first ones of theirs.)
+            // CTA's share, the others the first ones of theirs: each has a word of its own, as nothing
+            // holds the warps together at the pieces between them.)
+            const int begins = kb0 == 0;
             if (first != last && et == 0)
-                hd->ready[piece & 1] = load_acquire(a.count + first) == last - first;
+                hd->ready[begins] = load_acquire(a.count + first) == last - first;
             if (kSets == 2) ptx::named_bar_sync(1, 2 * kEt);
             else if (first != last) ptx::named_bar_sync(3, kEt);
             float acc[C::kMats][kOwn];
@@ -407,9 +409,9 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                 // Slots of pieces: a CTA's last piece may begin a tile that the next ones end, its
                 // others end or continue one.
                 constexpr size_t kSlot = (size_t)C::kMats * N * 128;
-                bool whole = hd->ready[piece & 1];
+                bool whole = hd->ready[begins];
                 if (!whole) {
-                    float *to = a.part + (size_t)(2 * share.cta + (kb0 == 0 ? 1 : 0)) * kSlot + c0 * 128 + th;
+                    float *to = a.part + (size_t)(2 * share.cta + begins) * kSlot + c0 * 128 + th;
 #pragma unroll
                     for (int m = 0; m < C::kMats; ++m)
 #pragma unroll

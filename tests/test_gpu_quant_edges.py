@@ -1,7 +1,8 @@
 """8-bit experts on the GPU where their error bounds are at their ends: choices that near keys of
-unlike errors decide."""
+unlike errors decide, shares of the streaming kernel that hold several tiles."""
 import numpy as np
 import pytest
+import torch
 
 from tests.test_gpu_quant import check_select, moe
 
@@ -77,3 +78,28 @@ def test_select_gates_of_the_smallest_scores():
     """Sigmoids down to the smallest number of 32 bits, lifted by the scale."""
     logits = -80.0 - np.arange(48).reshape(2, 24) * 0.5
     check_select(moe(), logits, None, 24, score="sigmoid", renormalise=False, scale=1e30)
+
+
+# ---- shares of the streaming kernel ------------------------------------------------------
+
+
+@pytest.mark.parametrize("n_in", [144, 256, 384, 512])
+@pytest.mark.parametrize("S", [1, 20, 33, 64])
+def test_product_shares_of_several_tiles(S, n_in):
+    """Tiles of few k-blocks: a CTA's share ends one that others began, has whole ones, and begins one that
+    others end.  Against 64 bits, and the same bits every time."""
+    m, g = moe(), torch.Generator(device="cuda").manual_seed(S + n_in)
+    n_out, nb = 40000, -(-n_in // 128)
+    f8 = lambda *s: (torch.randn(s, device="cuda", generator=g) * 100).clamp(-448, 448).to(torch.float8_e4m3fn)
+    x, w = f8(S, n_in), f8(1, n_out, n_in)
+    xs = torch.rand((S, nb), device="cuda", generator=g) + 0.5
+    s = torch.rand((1, -(-n_out // 128), nb), device="cuda", generator=g) + 0.5
+    x64 = x.double() * xs.double().repeat_interleave(128, 1)[:, :n_in]
+    w64 = w[0].double() * s[0].double().repeat_interleave(128, 0)[:n_out].repeat_interleave(128, 1)[:, :n_in]
+    want, room = x64 @ w64.t(), (n_in + 8) * 2.0 ** -23 * (x64.abs() @ w64.abs().t())
+    ws = m.quant_product_alloc_workspace(1, n_out, n_in, S)
+    first = m.quant_product(x, xs, w, s, None, torch.float32, ws=ws)
+    assert ((first.double() - want).abs() <= room).all()
+    for _ in range(20):
+        assert torch.equal(m.quant_product(x, xs, w, s, None, torch.float32, ws=ws), first)
+    assert m.get_last_error() == 0
