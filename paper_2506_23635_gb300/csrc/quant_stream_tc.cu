@@ -318,9 +318,9 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
                 for (int i = 0; i < kOwn / 2; ++i) sum[m][i] = 0;
             const float *sw0 = a.s0 + ((size_t)t.e * nwt + t.wt) * nk;
             const float *sw1 = UP ? a.s1 + ((size_t)t.e * nwt + t.wt) * nk : nullptr;
-            // lane i: column c0 + i's scale
+            // lane i: column c0 + i's scale (lanes behind the last row: the first row's, which count for nothing)
             const bool mine = lane < kOwn && c0 + lane < t.cnt;
-            const float *sx = a.xs + t.s0 + c0 + (mine ? lane : 0);
+            const float *sx = a.xs + t.s0 + (mine ? c0 + lane : 0);
             int kb = kb0;
             if (kSets == 2 && ((it ^ set) & 1)) {
                 ++kb;

@@ -103,3 +103,27 @@ def test_product_shares_of_several_tiles(S, n_in):
     for _ in range(20):
         assert torch.equal(m.quant_product(x, xs, w, s, None, torch.float32, ws=ws), first)
     assert m.get_last_error() == 0
+
+
+@pytest.mark.parametrize("S", [65, 70, 96, 100, 128])
+@pytest.mark.parametrize("n_in", [16, 272, 1024])
+def test_product_last_rows_of_a_wide_tile(S, n_in):
+    """Tiles of 64 rows with half of them or less: nothing behind the workspace's size is needed, and
+    its contents do not matter."""
+    m, g = moe(), torch.Generator(device="cuda").manual_seed(S + n_in)
+    n_out, nb = 264, -(-n_in // 128)
+    f8 = lambda *s: (torch.randn(s, device="cuda", generator=g) * 100).clamp(-448, 448).to(torch.float8_e4m3fn)
+    x, w = f8(S, n_in), f8(1, n_out, n_in)
+    xs = torch.rand((S, nb), device="cuda", generator=g) + 0.5
+    s = torch.rand((1, 3, nb), device="cuda", generator=g) + 0.5
+    x64 = x.double() * xs.double().repeat_interleave(128, 1)[:, :n_in]
+    w64 = w[0].double() * s[0].double().repeat_interleave(128, 0)[:n_out].repeat_interleave(128, 1)[:, :n_in]
+    want, room = x64 @ w64.t(), (n_in + 8) * 2.0 ** -23 * (x64.abs() @ w64.abs().t())
+    ws = m.quant_product_alloc_workspace(1, n_out, n_in, S)
+    assert ws.numel() == m.quant_product_workspace_size(1, n_out, n_in, S)
+    outs = []
+    for fill in (0x00, 0xff, 0x7f):
+        ws.fill_(fill)
+        outs.append(m.quant_product(x, xs, w, s, None, torch.float32, ws=ws))
+        assert ((outs[-1].double() - want).abs() <= room).all() and torch.equal(outs[-1], outs[0])
+    assert m.get_last_error() == 0
