@@ -943,13 +943,14 @@ bool experts_ok(const moe_quant_experts *w) {
            q_aligned(w->v1_scale) && q_aligned(w->w2_scale);
 }
 
-// Rows enough for the CTA pairs, whose units of up to 128 rows x 512 weight rows cost the same
-// however few rows there are (us, streamed and by pairs).  More than 64 a group, where the
-// streaming kernel takes a second tile (8192 x 6144: 2 groups of 100 45 and 34, 8 of them 135 and
-// 80); of a single matrix, whose pairs are few, more than 128 (96 rows 29 and 30, 144 rows 37 and
-// 31).  From 34 on where the units go twice around (16 experts of 6144 x 10752: 32 rows 488 and
-// 504, 35 rows 533 and 520, 40 rows 548 and 511; 40 of 2000 x 1424: 30 rows 106 and 102, 45 rows 113
-// and 104; but 6 groups of 40 rows, 8192 x 6144, 96 units on 76 pairs: 61 and 72).
+// Rows enough for the kernel of many rows, whose units of up to 128 rows x 256 weight rows cost the
+// same however few rows there are (us, streamed and by it).  More than 64 a group, where the
+// streaming kernel takes a second tile (8192 x 6144: 2 groups of 80 44 and 28, 8 of 100 145 and
+// 74); of a single matrix, whose units are few, more than 128 (8192 x 6144: 128 rows 26 and 26, 144
+// rows 35 and 26; 1024 x 8192: 128 rows 19 and 33).  From 34 on where the units go twice around
+// (16 experts of 6144 x 10752: 24 to 40 rows 505 to 513 and 498 to 507; 40 of 2000 x 1424: 30 rows
+// 107 and 99, 45 rows 109 and 100; but 6 groups of 40 rows, 8192 x 6144, 192 units on 152 SMs: 63
+// and 66).
 bool many_rows(int E, long long S, int n_out) {
     if (E == 1) return S > 128;
     return S > 64LL * E ||
@@ -971,9 +972,9 @@ cudaError_t quant_experts(const moe_dims &d, int T, const void *x, const moe_qua
     const QuantGemm gd{E, S, F, D, offsets, at<void>(ws, L.h8), at<float>(ws, L.hs)};
     const QuantDown down{w.w2, w.w2_scale, at<void>(ws, L.y), 0};
     const QuantParts pu{at<float>(ws, L.part), count}, pd{at<float>(ws, L.part), count + kQMaxCtas};
-    if (many_rows(E, S, D) && quant_pair_ok()) {
-        e = launch_quant_pair_up(gu, up, st);
-        if (e == cudaSuccess) e = launch_quant_pair_down(gd, down, st);
+    if (many_rows(E, S, D)) {
+        e = launch_quant_wide_up(gu, up, st);
+        if (e == cudaSuccess) e = launch_quant_wide_down(gd, down, st);
     } else {
         e = launch_quant_stream_up(gu, up, pu, L.cols, st);
         if (e == cudaSuccess) e = launch_quant_stream_down(gd, down, pd, L.cols, false, st);
@@ -1097,8 +1098,8 @@ moe_status moe_quant_product(int32_t n_groups, int32_t n_out, int32_t n_in, int3
     }
     const QuantGemm g{n_groups, S, n_in, n_out, offsets_opt, x, xs};
     const QuantDown down{w, w_scale, y, y_dtype == MOE_BF16};
-    if (many_rows(n_groups, S, n_out) && quant_pair_ok())
-        return q_status(launch_quant_pair_down(g, down, st));
+    if (many_rows(n_groups, S, n_out))
+        return q_status(launch_quant_wide_down(g, down, st));
     return q_status(launch_quant_stream_down(g, down, QuantParts{at<float>(ws, L.part), count}, L.cols,
                                              true, st));
 }

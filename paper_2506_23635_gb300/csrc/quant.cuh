@@ -103,6 +103,31 @@ __device__ __forceinline__ float2 both(uint64_t v) {
     return r;
 }
 
+// prefix[e]: tiles of the experts ahead of e, nwt for each run of `rows` rows (one warp).
+__device__ __forceinline__ void q_tile_prefix(const int32_t *offsets, int E, int S, int nwt, int rows,
+                                              int *prefix, unsigned *err) {
+    const int lane = threadIdx.x & 31;
+    int run = 0;
+    for (int base = 0; base < E; base += 32) {
+        const int e = base + lane;
+        int c = 0;
+        if (e < E) {
+            const int lo = offsets ? offsets[e] : 0, hi = offsets ? offsets[e + 1] : S;
+            if (lo < 0 || hi < lo || hi > S) set_error(err, kErrIndex);
+            else c = ((hi - lo + rows - 1) / rows) * nwt;
+        }
+        int incl = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (e < E) prefix[e] = run + incl - c;
+        run += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) prefix[E] = run;
+}
+
 // A grouped product of 8-bit operands: rows x8 [S, n_in] in groups given by offsets
 // [E+1] (null: one group of S rows) times each group's matrix w8 [E, n_out, n_in].
 struct QuantGemm {
@@ -149,11 +174,9 @@ cudaError_t launch_quant_stream_up(const QuantGemm &g, const QuantUp &u, const Q
 cudaError_t launch_quant_stream_down(const QuantGemm &g, const QuantDown &u, const QuantParts &p,
                                      int cols, bool alone, cudaStream_t st);
 
-// The same for many rows a group, on CTA pairs (quant_pair_tc.cu), where the device
-// keeps such pairs resident; they, too, read offsets and weights early.
-bool quant_pair_ok();
-cudaError_t launch_quant_pair_up(const QuantGemm &g, const QuantUp &u, cudaStream_t st);
-cudaError_t launch_quant_pair_down(const QuantGemm &g, const QuantDown &u, cudaStream_t st);
+// The same for many rows a group (quant_wide_tc.cu); it, too, reads offsets and weights early.
+cudaError_t launch_quant_wide_up(const QuantGemm &g, const QuantUp &u, cudaStream_t st);
+cudaError_t launch_quant_wide_down(const QuantGemm &g, const QuantDown &u, cudaStream_t st);
 
 // 8-bit weights [n, rows, cols]: boxes of 128 x 128, zeros outside each matrix.
 inline bool q_weight_map(CUtensorMap *m, const void *base, uint64_t n, uint64_t rows,

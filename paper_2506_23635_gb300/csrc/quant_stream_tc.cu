@@ -142,31 +142,6 @@ struct QsShare {
     }
 };
 
-// prefix[e]: tiles of the experts ahead of e.
-__device__ void qs_prefix(const int32_t *offsets, int E, int S, int nwt, int cols, int *prefix,
-                          unsigned *err) {
-    const int lane = threadIdx.x & 31;
-    int run = 0;
-    for (int base = 0; base < E; base += 32) {
-        const int e = base + lane;
-        int c = 0;
-        if (e < E) {
-            const int lo = offsets ? offsets[e] : 0, hi = offsets ? offsets[e + 1] : S;
-            if (lo < 0 || hi < lo || hi > S) set_error(err, kErrIndex);
-            else c = ((hi - lo + cols - 1) / cols) * nwt;
-        }
-        int incl = c;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
-        }
-        if (e < E) prefix[e] = run + incl - c;
-        run += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    if (lane == 0) prefix[E] = run;
-}
-
 struct QsArgs {
     const int32_t *offsets;
     int E, S, n_in, n_out;
@@ -212,7 +187,7 @@ k_quant_stream(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant_
     ptx::launch_dependents();
     // (the offsets are older than the launch ahead, which lets this one start behind its own
     // wait only, or is started so itself)
-    if (warp == 2) qs_prefix(a.offsets, a.E, a.S, nwt, N, hd->prefix, a.err);
+    if (warp == 2) q_tile_prefix(a.offsets, a.E, a.S, nwt, N, hd->prefix, a.err);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();

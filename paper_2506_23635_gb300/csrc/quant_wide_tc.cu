@@ -1,5 +1,5 @@
-// Grouped products of 8-bit operands for many rows a group: pairs of CTAs that share their
-// weight tiles, each 128 rows of x as its MMAs' M, 256 weight rows as their N.
+// Grouped products of 8-bit operands for many rows a group: CTAs of 128 rows of x as their MMAs'
+// M, 256 weight rows as their N.
 //
 //   DOWN:  y[j, n] = sum_b xs[j, b] ws[e, n/128, b] (sum_{k in block b} x8[j, k] w8[e, n, k])
 //   UP:    a, b = the same with w1 and v1;  h = SiLU(a) b, quantised in blocks of 128
@@ -11,22 +11,20 @@
 // each k-block: with the weights as lanes every column would need its own, 32 lanes reading
 // the same word of shared memory.
 //
-// Bound by the way around: a k-block takes 950 cycles (9728 rows of 8192 x 6144: 375 to 380 us,
-// 2.6 PFLOP/s), its MMAs 512, what shared memory moves for it (48 KB in, 48 KB out) 750 at
+// Bound by the way around: a k-block takes 0.51 us, about 970 cycles (9728 rows of 8192 x 6144:
+// 392 us, 2.5 PFLOP/s), its MMAs 512, what shared memory moves for it (48 KB in, 48 KB out) 750 at
 // least, a buffer's sums 580 in the epilogue, and an accumulator goes from one to the other and
-// back.  MMAs of both CTAs in one (cta_group::2) read half the weights each and wait for each
-// other: 388 us, 1033 and 562 instead of 1011 and 558 for the projections of 2048 tokens.
+// back.  Every CTA loads its weight tile by itself, from L2 where others take the same one.  Pairs of
+// CTAs that load half of a tile each for both of them (MMAs of two CTAs, cta_group::2): 388 us,
+// but runs of 256 rows, of which short groups fill less.
 // Scales of powers of two could go into the MMAs (kind::mxf8f6f4, no epilogue before the end):
 // 321 us, but any other scale needs this way, and the choice a look at all scales first.
 //
-// N: 256 rows of the weights; for UP 128 rows of W1, then the same 128 of V1.  Each CTA loads
-// half of a shared tile for both.  Epilogue warp (q, half): lanes 32 q .. and half of the
-// columns (UP: 64 of a and the same 64 of b), 128 sums a thread.
+// N: 256 rows of the weights; for UP 128 rows of W1, then the same 128 of V1.  Epilogue warp (q,
+// half): lanes 32 q .. and half of the columns (UP: 64 of a and the same 64 of b), 128 sums a thread.
 //
-// Units are (expert, weight tile, run of 256 rows), runs innermost, so that units that run
-// together share weight tiles in L2.  A last run of at most 128 rows leaves nothing to share:
-// there the CTAs of a pair take weight tiles side by side (2048 tokens on 16 experts 1022 and
-// 563 -> 957 and 534 us).  Pair p of P takes units p, p + P, ...
+// Units are (expert, weight tile, run of 128 rows), runs innermost, so that units that run
+// together share weight tiles in L2.  CTA c of C takes units c, c + C, ...
 #include "quant.cuh"
 
 namespace moe {
@@ -37,17 +35,17 @@ using namespace tc;
 // warp 0 loads, warp 1 issues the MMAs, warps 2 and 3 prepare scales, warps 4-11 are the
 // epilogue.  Registers of the launch: 168 a thread, 64,512; what the first four warps give up the
 // others take: 128 (136 + 2 * 184) = 64,512 (splits that spill on either side cost 5 to 20%).
-constexpr int kQpThreads = 384;
-constexpr int kQpRegsFeed = 136, kQpRegsSums = 184;
-constexpr int kQpEpilogue = 4;  // first warp of it
-constexpr uint32_t kQpTile = 128 * 128;
-constexpr uint32_t kQpStage = 3 * kQpTile;  // 128 rows of x, 256 weight rows
-constexpr int kQpMaxStages = 4;
+constexpr int kQwThreads = 384;
+constexpr int kQwRegsFeed = 136, kQwRegsSums = 184;
+constexpr int kQwEpilogue = 4;  // first warp of it
+constexpr uint32_t kQwTile = 128 * 128;
+constexpr uint32_t kQwStage = 3 * kQwTile;  // 128 rows of x, 256 weight rows
+constexpr int kQwMaxStages = 4;
 // kind::f8f6f4: e4m3 A and B, fp32 D, both K-major, M = 128, N = 256
-constexpr uint32_t kQpIdesc = (1u << 4) | ((256u >> 3) << 17) | ((128u >> 4) << 24);
+constexpr uint32_t kQwIdesc = (1u << 4) | ((256u >> 3) << 17) | ((128u >> 4) << 24);
 
-struct QpHeader {
-    uint64_t full[kQpMaxStages], empty[kQpMaxStages];
+struct QwHeader {
+    uint64_t full[kQwMaxStages], empty[kQwMaxStages];
     uint64_t tfull[2], tempty[2];
     uint64_t done;
     uint32_t tmem_base;
@@ -55,16 +53,16 @@ struct QpHeader {
     float2 scale[4][128];      // steps in turn, row: x's times w1's and v1's (the tile's two blocks')
     uint32_t amax[2][2][128];  // (UP) of a row's 64 columns: tile in turn, half
 };
-constexpr uint32_t kQpHdrBytes = 8192;
-static_assert(sizeof(QpHeader) <= kQpHdrBytes, "header");
+constexpr uint32_t kQwHdrBytes = 8192;
+static_assert(sizeof(QwHeader) <= kQwHdrBytes, "header");
 // y's way out: 4 KB an epilogue warp, 32 rows of 128 bytes.  (h goes out from registers, and
 // its projection has a stage more: 1027 -> 1010 us for 2048 tokens; rows of 64 bytes and a stage
 // more for y, too, 99 -> 102.)
 template <bool UP>
-struct QpCfg {
+struct QwCfg {
     static constexpr int kStages = UP ? 4 : 3;
     static constexpr uint32_t kOut = UP ? 0 : 8 * 4096;
-    static constexpr size_t kSmem = 1024 + kStages * kQpStage + kOut + kQpHdrBytes;
+    static constexpr size_t kSmem = 1024 + kStages * kQwStage + kOut + kQwHdrBytes;
     static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
@@ -81,94 +79,28 @@ __device__ __forceinline__ void mma_f8_wide(uint32_t d_tmem, uint32_t x, uint32_
         : "memory");
 }
 
-// A tensor copy into the same place of these CTAs' shared memory, each told on its own barrier.
-__device__ __forceinline__ void tma_3d_to(void *dst, const CUtensorMap *m, int32_t x, int32_t y,
-                                          int32_t z, uint64_t *bar, uint16_t ctas,
-                                          uint64_t policy) {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-        ".multicast::cluster.L2::cache_hint [%0], [%1, {%2, %3, %4}], [%5], %6, %7;" ::"r"(
-            ptx::smem_u32(dst)),
-        "l"(m), "r"(x), "r"(y), "r"(z), "r"(ptx::smem_u32(bar)), "h"(ctas), "l"(policy)
-        : "memory");
-}
-
-// Arrive on the mbarrier at this offset in both CTAs once all earlier MMAs of this thread finish.
-__device__ __forceinline__ void mma_commit_both(uint64_t *bar) {
-    asm volatile(
-        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
-        " [%0], %1;" ::"r"(ptx::smem_u32(bar)),
-        "h"((uint16_t)3)
-        : "memory");
-}
-
 __device__ __forceinline__ uint64_t twice(float s) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(s));
     return r;
 }
-// A group's rows in runs: whole ones of up to 256 rows, the odd CTA's behind the even one's,
-// both with the same 256 weight rows (UP: 128 of both matrices); a last one of at most 128
-// rows, which both CTAs take with weight tiles side by side.
-__device__ __forceinline__ void qp_runs(int rows, int &whole, int &rest) {
-    whole = (rows + 127) / 256;
-    rest = rows > whole * 256;
-}
-
-struct QpTile {
-    int e, wt;    // the CTA's weight tile (one behind the last for the odd CTA's rest: no results)
-    int s0, cnt;  // its first row, its rows (1 to 128)
-    bool shared;  // the weight tile is both CTAs'
+struct QwTile {
+    int e, wt;    // expert, weight tile
+    int s0, cnt;  // first row of x, rows (1 to 128)
 };
 
-__device__ __forceinline__ QpTile qp_tile(const int *prefix, const int32_t *offsets, int E, int S,
-                                          int nwt, int rank, int u) {
-    QpTile t;
+__device__ __forceinline__ QwTile qw_tile(const int *prefix, const int32_t *offsets, int E, int S, int u) {
+    QwTile t;
     t.e = chunk_expert(prefix, E, u);
     const int lo = offsets ? offsets[t.e] : 0, hi = offsets ? offsets[t.e + 1] : S;
-    int whole, rest;
-    qp_runs(hi - lo, whole, rest);
-    // two weight tiles' units, then the rest's with both
-    const int r = u - prefix[t.e], per = 2 * whole + rest, j = r / per, i = r - j * per;
-    t.shared = i < min(2, nwt - 2 * j) * whole;
-    const int second = i >= whole;
-    const int run = t.shared ? i - second * whole : whole;
-    t.wt = 2 * j + (t.shared ? second : rank);
-    t.s0 = lo + run * 256 + (t.shared ? rank * 128 : 0);
+    const int runs = (hi - lo + 127) / 128, r = u - prefix[t.e];
+    t.wt = r / runs;
+    t.s0 = lo + (r - t.wt * runs) * 128;
     t.cnt = min(128, hi - t.s0);
     return t;
 }
 
-// prefix[e]: units of the experts ahead of e.
-__device__ void qp_prefix(const int32_t *offsets, int E, int S, int nwt, int *prefix,
-                          unsigned *err) {
-    const int lane = threadIdx.x & 31;
-    int run = 0;
-    for (int base = 0; base < E; base += 32) {
-        const int e = base + lane;
-        int c = 0;
-        if (e < E) {
-            const int lo = offsets ? offsets[e] : 0, hi = offsets ? offsets[e + 1] : S;
-            if (lo < 0 || hi < lo || hi > S) set_error(err, kErrIndex);
-            else {
-                int whole, rest;
-                qp_runs(hi - lo, whole, rest);
-                c = whole * nwt + rest * ((nwt + 1) / 2);
-            }
-        }
-        int incl = c;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
-        }
-        if (e < E) prefix[e] = run + incl - c;
-        run += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    if (lane == 0) prefix[E] = run;
-}
-
-struct QpArgs {
+struct QwArgs {
     const int32_t *offsets;
     int E, S, n_in, n_out;
     const float *xs, *s0, *s1;  // scales of x [blocks, S], of w1 (or w), of v1
@@ -178,24 +110,22 @@ struct QpArgs {
 };
 
 template <bool UP, bool BF>
-__global__ void __launch_bounds__(kQpThreads, 1)
-k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ CUtensorMap tm_w1,
-             const __grid_constant__ CUtensorMap tm_x, const QpArgs a) {
-    using C = QpCfg<UP>;
+__global__ void __launch_bounds__(kQwThreads, 1)
+k_quant_wide(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ CUtensorMap tm_w1,
+             const __grid_constant__ CUtensorMap tm_x, const QwArgs a) {
+    using C = QwCfg<UP>;
     constexpr int kStages = C::kStages;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *smem = reinterpret_cast<unsigned char *>(
         (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    QpHeader *hd = reinterpret_cast<QpHeader *>(smem + kStages * kQpStage + C::kOut);
+    QwHeader *hd = reinterpret_cast<QwHeader *>(smem + kStages * kQwStage + C::kOut);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = ptx::cluster_ctarank();
-    const bool even = rank == 0;
     const int nk = q_blocks(a.n_in), nblk = q_blocks(a.n_out);
     const int nwt = UP ? nblk : (nblk + 1) / 2;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
             ptx::mbar_init(&hd->full[s], 1);
-            ptx::mbar_init(&hd->empty[s], 2);
+            ptx::mbar_init(&hd->empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             ptx::mbar_init(&hd->tfull[b], 3);  // (the MMAs; the two warps with the scales)
@@ -211,54 +141,49 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
     ptx::launch_dependents();
     // (the offsets are older than the launch ahead, which lets this one start behind its own
     // wait only, or is started so itself)
-    if (warp == kQpEpilogue) qp_prefix(a.offsets, a.E, a.S, nwt, hd->prefix, a.err);
+    if (warp == kQwEpilogue) q_tile_prefix(a.offsets, a.E, a.S, nwt, 128, hd->prefix, a.err);
     tc_fence_before();
-    ptx::cluster_sync_all();  // barriers initialised in both CTAs
+    __syncthreads();
     tc_fence_after();
     const uint32_t tmem = hd->tmem_base;
-    const int n_units = hd->prefix[a.E], u0 = blockIdx.x >> 1, du = gridDim.x >> 1;
+    const int n_units = hd->prefix[a.E], u0 = blockIdx.x, du = gridDim.x;
 
-    if (warp < kQpEpilogue) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kQpRegsFeed));
+    if (warp < kQwEpilogue) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kQwRegsFeed));
         if (warp == 0) {
             // ------------------------------------------------------------ loads
             if (lane == 0) {
-                // (normal priority: a weight tile serves the runs of its expert)
-                const uint64_t pol_w = ptx::policy_evict_normal(), pol_x = ptx::policy_evict_last();
-                auto weights = [&](const QpTile &t, uint32_t s, int kb) {
-                    // a shared weight tile: this CTA's half for both; else both halves for itself
-                    const CUtensorMap *wm = UP && t.shared && !even ? &tm_w1 : &tm_w0;
-                    const int wy = UP ? t.wt * 128 : t.wt * 256 + (t.shared ? (int)rank * 128 : 0);
-                    unsigned char *sp = smem + s * kQpStage;
+                // (both stay in L2: a weight tile serves the runs of its expert, x all weight tiles; with
+                // normal priority for the weights 2048 rows of 8192 x 6144 took 99.3 us instead of 97.3)
+                const uint64_t pol_w = ptx::policy_evict_last(), pol_x = ptx::policy_evict_last();
+                auto weights = [&](const QwTile &t, uint32_t s, int kb) {
+                    unsigned char *sp = smem + s * kQwStage + kQwTile;
                     uint64_t *fb = &hd->full[s];
-                    ptx::mbar_arrive_expect_tx(fb, kQpStage);
-                    tma_3d_to(sp + (t.shared ? 1 + rank : 1) * kQpTile, wm, kb * 128, wy, t.e, fb,
-                              t.shared ? 3 : 1 << rank, pol_w);
-                    if (!t.shared)
-                        tma_3d(sp + 2 * kQpTile, UP ? &tm_w1 : &tm_w0, kb * 128, UP ? wy : wy + 128, t.e,
-                               fb, pol_w);
+                    ptx::mbar_arrive_expect_tx(fb, kQwStage);
+                    tma_3d(sp, &tm_w0, kb * 128, t.wt * (UP ? 128 : 256), t.e, fb, pol_w);
+                    tma_3d(sp + kQwTile, UP ? &tm_w1 : &tm_w0, kb * 128, UP ? t.wt * 128 : t.wt * 256 + 128, t.e,
+                           fb, pol_w);
                 };
-                // the first stages' weights, which no kernel ahead writes, before the wait (300 tokens
-                // of 40 small experts 106 -> 103 us)
+                // the first stages' weights, which no kernel ahead writes, before the wait
                 const uint32_t early = u0 < n_units ? min(kStages, nk) : 0;
                 if (early) {
-                    const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, nwt, (int)rank, u0);
+                    const QwTile t = qw_tile(hd->prefix, a.offsets, a.E, a.S, u0);
                     for (uint32_t k = 0; k < early; ++k) weights(t, k, k);
                 }
                 ptx::grid_dependency_wait();
                 uint32_t it = 0;
                 bool ok = true;
                 for (int u = u0; ok && u < n_units; u += du) {
-                    const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, nwt, (int)rank, u);
+                    const QwTile t = qw_tile(hd->prefix, a.offsets, a.E, a.S, u);
                     for (int kb = 0; kb < nk; ++kb, ++it) {
                         const uint32_t s = it % kStages, ph = (it / kStages) & 1;
                         if (!(ok = wait_soon(&hd->empty[s], ph ^ 1, a.err))) break;
                         if (it >= early) weights(t, s, kb);
-                        ptx::tma_load_2d(smem + s * kQpStage, &tm_x, kb * 128, t.s0, &hd->full[s], pol_x);
+                        ptx::tma_load_2d(smem + s * kQwStage, &tm_x, kb * 128, t.s0, &hd->full[s], pol_x);
                     }
                 }
-                // copies in flight land before the block can end, and what both CTAs' MMAs tell
-                // of its last stages.  (Where a wait gave up, stages whose weights came early may
+                // copies in flight land before the block can end, and what the MMAs tell of its
+                // last stages.  (Where a wait gave up, stages whose weights came early may
                 // wait for rows that do not come: these waits end too.)
                 it = max(it, early);
                 for (uint32_t k = (it > kStages ? it - kStages : 0); k < it; ++k)
@@ -282,15 +207,15 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t x = base + s * (kQpStage >> 4), w = x + (kQpTile >> 4);
+                const uint32_t x = base + s * (kQwStage >> 4), w = x + (kQwTile >> 4);
                 const uint32_t d = tmem + b * 256;
                 if (one) {
-                    mma_f8_wide(d, x, w, kQpIdesc, 0);
-                    mma_f8_wide(d, x + 2, w + 2, kQpIdesc, 1);
-                    mma_f8_wide(d, x + 4, w + 4, kQpIdesc, 1);
-                    mma_f8_wide(d, x + 6, w + 6, kQpIdesc, 1);
+                    mma_f8_wide(d, x, w, kQwIdesc, 0);
+                    mma_f8_wide(d, x + 2, w + 2, kQwIdesc, 1);
+                    mma_f8_wide(d, x + 4, w + 4, kQwIdesc, 1);
+                    mma_f8_wide(d, x + 6, w + 6, kQwIdesc, 1);
                     mma_commit(&hd->tfull[b]);
-                    mma_commit_both(&hd->empty[s]);
+                    mma_commit(&hd->empty[s]);
                 }
                 __syncwarp();
                 if (++s == kStages) {
@@ -310,8 +235,8 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
             uint32_t it = 0;
             bool ok = true;
             for (int u = u0; ok && u < n_units; u += du) {
-                const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, nwt, (int)rank, u);
-                const int row = min(t.s0 + r0, a.S - 1), blk = min(UP ? t.wt : t.wt * 2, nblk - 1);
+                const QwTile t = qw_tile(hd->prefix, a.offsets, a.E, a.S, u);
+                const int row = min(t.s0 + r0, a.S - 1), blk = UP ? t.wt : t.wt * 2;
                 const float *x0 = a.xs + row;
                 const int x1 = min(t.s0 + r0 + 32, a.S - 1) - row, next = UP ? blk : min(blk + 1, nblk - 1);
                 const float *w0 = a.s0 + ((size_t)t.e * nblk + blk) * nk;
@@ -339,17 +264,17 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kQpRegsSums));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kQwRegsSums));
         // ------------------------------------------------------------ epilogue
-        const int q = warp & 3, half = (warp - kQpEpilogue) >> 2;
+        const int q = warp & 3, half = (warp - kQwEpilogue) >> 2;
         const uint32_t base0 = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)half * (UP ? 64 : 128);
         bool dead = false;  // a wait gave up: keep the barriers, skip the work
         ptx::grid_dependency_wait();  // (the result's last readers)
         uint32_t it = 0, tl = 0;
         for (int u = u0; u < n_units; u += du, ++tl) {
-            const QpTile t = qp_tile(hd->prefix, a.offsets, a.E, a.S, nwt, (int)rank, u);
+            const QwTile t = qw_tile(hd->prefix, a.offsets, a.E, a.S, u);
             const int r = q * 32 + lane;
-            const bool mine = r < t.cnt && (!UP || t.wt < nwt);
+            const bool mine = r < t.cnt;
             uint64_t acc[64];
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i] = 0;
@@ -411,7 +336,7 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
                 // 32 rows of 128 bytes at a time through shared memory, so that eight lanes
                 // write a row's 128 bytes (16-byte chunks exchanged by the row: no conflicts)
                 constexpr int kCols = BF ? 64 : 32, kSize = BF ? 2 : 4;
-                uint8_t *buf = smem + kStages * kQpStage + (warp - kQpEpilogue) * 4096;
+                uint8_t *buf = smem + kStages * kQwStage + (warp - kQwEpilogue) * 4096;
                 const int row0 = q * 32, col0 = t.wt * 256 + half * 128;
                 uint8_t *y = static_cast<uint8_t *>(a.out) + ((size_t)t.s0 * a.n_out + col0) * kSize;
                 const int ch = lane & 7;
@@ -451,57 +376,22 @@ k_quant_pair(const __grid_constant__ CUtensorMap tm_w0, const __grid_constant__ 
     }
     __syncwarp();
     tc_fence_before();
-    ptx::cluster_sync_all();  // no CTA leaves while its pair may touch it
+    __syncthreads();
     tc_fence_after();
     if (warp == 1) tmem_dealloc(tmem, 512);
 }
 
-void pair_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&attr)[2], int grid, size_t smem) {
-    cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(kQpThreads);
-    cfg.dynamicSmemBytes = smem;
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-}
-
-// CTA pairs that the current device keeps resident (looked up once a device).
 template <bool UP, bool BF>
-int resident_pairs() {
-    static int cached[64];
-    static std::once_flag once[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-    std::call_once(once[dev], [dev] {
-        const void *kern = (const void *)k_quant_pair<UP, BF>;
-        int pairs = 0;
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)QpCfg<UP>::kSmem) ==
-            cudaSuccess) {
-            cudaLaunchConfig_t cfg;
-            cudaLaunchAttribute attr[2];
-            pair_config(cfg, attr, device_info().sm_count & ~1, QpCfg<UP>::kSmem);
-            if (cudaOccupancyMaxActiveClusters(&pairs, kern, &cfg) != cudaSuccess) pairs = 0;
-        }
-        (void)cudaGetLastError();
-        cached[dev] = std::min(pairs, device_info().sm_count / 2);
-    });
-    return cached[dev];
-}
-
-template <bool UP, bool BF>
-cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QpArgs a, cudaStream_t st) {
-    const int pairs = resident_pairs<UP, BF>();
+cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QwArgs a, cudaStream_t st) {
     CUtensorMap mw0, mw1, mx;
-    if (pairs < 1 || !q_weight_map(&mw0, w0, g.E, g.n_out, g.n_in) ||
+    if (!q_weight_map(&mw0, w0, g.E, g.n_out, g.n_in) ||
         !q_weight_map(&mw1, UP ? w1 : w0, g.E, g.n_out, g.n_in) ||
         !q_row_map(&mx, g.x8, g.S, g.n_in, 128))
         return cudaErrorInvalidValue;
+    const void *kern = (const void *)k_quant_wide<UP, BF>;
+    static SmemOnce smem;
+    cudaError_t e = smem.set(kern, QwCfg<UP>::kSmem);
+    if (e != cudaSuccess) return e;
     a.offsets = g.offsets;
     a.E = g.E;
     a.S = g.S;
@@ -510,22 +400,14 @@ cudaError_t launch(const QuantGemm &g, const void *w0, const void *w1, QpArgs a,
     a.xs = g.xs;
     a.err = device_info().err;
     void *args[] = {&mw0, &mw1, &mx, &a};
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr[2];
-    pair_config(cfg, attr, 2 * pairs, QpCfg<UP>::kSmem);
-    cfg.numAttrs = 2;
-    cfg.stream = st;
-    LaunchScope ls(UP ? "quant_up_pair" : "quant_down_pair", st);
-    return cudaLaunchKernelExC(&cfg, (const void *)k_quant_pair<UP, BF>, args);
+    LaunchScope ls(UP ? "quant_up_wide" : "quant_down_wide", st);
+    return launch_pdl(kern, dim3(device_info().sm_count), dim3(kQwThreads), QwCfg<UP>::kSmem, st, args);
 }
 
 }  // namespace
 
-bool quant_pair_ok() { return resident_pairs<true, false>() > 0 && resident_pairs<false, true>() > 0 &&
-           resident_pairs<false, false>() > 0; }
-
-cudaError_t launch_quant_pair_up(const QuantGemm &g, const QuantUp &u, cudaStream_t st) {
-    QpArgs a{};
+cudaError_t launch_quant_wide_up(const QuantGemm &g, const QuantUp &u, cudaStream_t st) {
+    QwArgs a{};
     a.s0 = u.s1;
     a.s1 = u.sv;
     a.out = u.h8;
@@ -533,8 +415,8 @@ cudaError_t launch_quant_pair_up(const QuantGemm &g, const QuantUp &u, cudaStrea
     return launch<true, false>(g, u.w1, u.v1, a, st);
 }
 
-cudaError_t launch_quant_pair_down(const QuantGemm &g, const QuantDown &u, cudaStream_t st) {
-    QpArgs a{};
+cudaError_t launch_quant_wide_down(const QuantGemm &g, const QuantDown &u, cudaStream_t st) {
+    QwArgs a{};
     a.s0 = u.s;
     a.out = u.y;
     return u.y_bf16 ? launch<false, true>(g, u.w, nullptr, a, st)
