@@ -1,12 +1,47 @@
-"""8-bit experts on the GPU where their error bounds are at their ends: choices that near keys of
-unlike errors decide, shares of the streaming kernel that hold several tiles."""
+"""8-bit experts on the GPU where their error bounds are at their ends: SiLU of far negative
+numbers, choices that near keys of unlike errors decide, shares of the streaming kernel that
+hold several tiles."""
 import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_quant import check_select, moe
+from tests.paged_ref import encode
+from tests.test_gpu_quant import check_select, cuda, e4m3, moe, num
 
 pytestmark = pytest.mark.gpu
+
+
+# ---- SiLU ----------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("tens", [[-80.0, -88.0, -96.0], [-88.0, -96.0]], ids=["from80", "from88"])
+@pytest.mark.parametrize("T", [1, 20, 60, 200])
+def test_silu_of_far_negative_numbers(T, tens):
+    """SiLU(a) is a e^a there, not zero (b = 2^100 and more lifts h); a is exact in the products, as
+    is y, which is h's 8-bit number.  h: rounded to nearest by at most 2^-4 of itself, or half of the
+    smallest step, 2^-10 of its block's scale, which is at most its largest number / 224;
+    exponentials down to 2e-42 are numbers of 1450 steps of 2^-149, off by half a step (2^-11) and
+    their product with a by less; the rest below 2^-16."""
+    m = moe()
+    D = F = 128
+    x = np.zeros((T, D))
+    x[:, :2] = 1.0, 0.25
+    x[:, 2] = 2.0 ** (np.arange(T) % 5)
+    w1, v1 = np.zeros((1, F, D)), np.zeros((1, F, D))
+    w1[0, :, 0] = np.repeat(tens, 64)[:F] if len(tens) == 2 else np.repeat(tens, 43)[:F]
+    w1[0, :, 1] = (np.arange(F) % 4) * 2 * (w1[0, :, 0] > -96)
+    v1[0, :, 2] = 1.0
+    w2 = np.eye(D, F)[None]
+    one, big = np.ones((1, 1, 1), np.float32), np.full((1, 1, 1), 2.0 ** 100, np.float32)
+    ex = m.QuantExperts(e4m3(encode(w1)), cuda(one), e4m3(encode(v1)), cuda(big), e4m3(encode(w2)), cuda(one))
+    d = m.dims(D, F, 1, 1, torch.float32)
+    got = num(m.quant_experts_forward(d, ex, cuda(x.astype(np.float32)), cuda(np.zeros((T, 1), np.int32)),
+                                      cuda(np.ones((T, 1), np.float32))))
+    assert m.get_last_error() == 0
+    a = w1[0, :, 0] + 0.25 * w1[0, :, 1]
+    want = a * np.exp(a) / (1 + np.exp(a)) * x[:, 2:3] * 2.0 ** 100
+    step = np.abs(want).max(1, keepdims=True) / 224 * 2.0 ** -10
+    assert (np.abs(got - want) <= np.maximum(2.0 ** -4 * np.abs(want), step) + 2.0 ** -10 * np.abs(want)).all()
 
 
 # ---- the choice of experts -----------------------------------------------------------
