@@ -447,7 +447,9 @@ __device__ __noinline__ bool select_pairs(const SelArgs &a, const float *l, SelS
             if (g < a.G && (lane & (P - 1)) == 0) {
                 float2 v = t1;
                 if (a.group_top == 2)
-                    v = isfinite(t1.x) && isfinite(t2.x) ? pair_add(t1, t2) : make_float2(t1.x + t2.x, 0.f);
+                    v = isfinite(t1.x) && isfinite(t2.x)
+                            ? pair_add(make_float2(0.5f * t1.x, 0.5f * t1.y), make_float2(0.5f * t2.x, 0.5f * t2.y))
+                            : make_float2(t1.x + t2.x, 0.f);
                 w.p.group[g] = v;
             }
         }
@@ -482,7 +484,7 @@ __device__ __noinline__ bool select_pairs(const SelArgs &a, const float *l, SelS
             if (pair_less(high, y)) high = y;
         }
         if ((biased || by_score) && high.x > -INFINITY)
-            clear = isfinite(low.x) && (low.x - high.x) + (low.y - high.y) > 4.f * err;
+            clear = isfinite(low.x) && (low.x - high.x) + (low.y - high.y) > 2.f * err;
     }
 #pragma unroll 1
     for (int k = 0; k < a.K; ++k) {
@@ -703,7 +705,9 @@ k_select(const SelArgs a) {
                 t2 = fmaxf(fminf(t1, o1), fmaxf(t2, o2));
                 t1 = fmaxf(t1, o1);
             }
-            if (g < a.G && (lane & (P - 1)) == 0) w.f.group[g] = a.group_top == 2 ? t1 + t2 : t1;
+            // (half the sum, which stays in range where both are the type's lowest)
+            if (g < a.G && (lane & (P - 1)) == 0)
+                w.f.group[g] = a.group_top == 2 ? 0.5f * t1 + 0.5f * t2 : t1;
         }
         __syncwarp();
         uint32_t low = 0xffffffffu, high = 0u;  // the worst kept, the best left out
@@ -733,11 +737,11 @@ k_select(const SelArgs a) {
             low = __reduce_min_sync(0xffffffffu, low);
             high = __reduce_max_sync(0xffffffffu, high);
             err = warp_most(err);
-            // both sides off by up to two keys each and their sum's rounding; NaN and minus
+            // both sides off by up to a key (or the mean of two) and its rounding; NaN and minus
             // infinity are what they are in 64 bits too
             if (high > key_code(-INFINITY)) {
                 const float lo = key_of(low), hi = key_of(high);
-                clear = lo < INFINITY && lo - hi > 4.f * err + kSumErr * (fabsf(lo) + fabsf(hi));
+                clear = lo < INFINITY && lo - hi > 2.f * err + kSumErr * (fabsf(lo) + fabsf(hi));
             }
         }
     }

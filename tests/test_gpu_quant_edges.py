@@ -101,6 +101,19 @@ def test_select_barred_experts(score):
     check_select(moe(), logits, bias, 6, score=score, n_groups=8, top_groups=4, group_top=2)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("low,best", [(-np.inf, 2), (-np.inf, 1), (-3e38, 2)])
+def test_select_groups_barred_by_the_lowest_numbers(score, low, best):
+    """Groups whose biases are all the type's lowest rank above those of minus infinity (or by
+    how low they are), though the sum of two is no number of 32 bits."""
+    rng = np.random.default_rng(3)
+    logits, bias = rng.normal(size=(200, 16)), rng.normal(size=16) * 0.05
+    bias[:4], bias[4:8] = low, np.finfo(np.float32).min
+    if np.isfinite(low):
+        bias[:4], bias[4:8] = np.finfo(np.float32).min, low
+    check_select(moe(), logits, bias, 11, score=score, n_groups=4, top_groups=3, group_top=best)
+
+
 def test_select_smallest_scores():
     """Scores about 2^-126, where their 32-bit form may be zero, beside biases of that size."""
     rng = np.random.default_rng(2)
