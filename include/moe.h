@@ -289,7 +289,8 @@ moe_status moe_layer_forward_noalloc(const moe_dims *dims, int32_t T,
  *
  * The quantisers' scales are the smallest power of two s with max|block| <= 448 s,
  * and at least 2^-100: q = e4m3(x / s), one rounding to nearest even.  A block with a
- * value that is not finite: scale and numbers NaN.  The products take any scales.
+ * value that is not finite: scale and numbers NaN.  The products take any scales; a
+ * row's and a block's are multiplied first, in float32.
  *
  * moe_quantize_rows: x [rows, cols] x_dtype -> q [rows, cols], scale.
  * moe_quantize_blocks: w [n, rows, cols] w_dtype -> q [n, rows, cols], scale; n
