@@ -175,3 +175,98 @@ def test_product_last_rows_of_a_wide_tile(S, n_in):
         outs.append(m.quant_product(x, xs, w, s, None, torch.float32, ws=ws))
         assert ((outs[-1].double() - want).abs() <= room).all() and torch.equal(outs[-1], outs[0])
     assert m.get_last_error() == 0
+
+
+# ---- the largest calls ---------------------------------------------------------------------
+
+
+def test_largest_rows_and_products():
+    """16,777,216 rows: quantised, and times a matrix (whole numbers, so that every sum is exact)."""
+    m, rows = moe(), 1 << 24
+    x = (torch.arange(rows * 16, device="cuda") % 13 - 6).to(torch.bfloat16).view(rows, 16)
+    x[:, 0] = 7.0
+    q, s = m.quantize_rows(x)
+    assert (s == 2.0 ** -6).all()  # (7 = 448 / 64)
+    for part in range(0, rows, 1 << 22):
+        assert torch.equal(q[part:part + (1 << 22)].float() * 2.0 ** -6, x[part:part + (1 << 22)].float())
+    w = (torch.arange(8 * 16, device="cuda") % 5 - 2).float().view(1, 8, 16)
+    off = torch.tensor([5, rows - 3], dtype=torch.int32, device="cuda")
+    y = torch.full((rows, 8), 9.0, device="cuda")
+    m.quant_product(q, s, w.to(torch.float8_e4m3fn), torch.ones((1, 1, 1), device="cuda"), off, torch.float32, out=y)
+    want = x.float() @ w[0].t()  # (numbers of at most 16 * 14: exact in any order)
+    want[:5], want[-3:] = 9.0, 9.0
+    assert torch.equal(y, want)
+    assert m.get_last_error() == 0
+
+
+@pytest.mark.parametrize("T,E,K", [(20000, 4, 4), (1 << 20, 3, 1), (1 << 17, 200, 128)])
+def test_largest_experts(T, E, K):
+    """The most tokens and slots: one value a token and an expert, exact all the way."""
+    m, D = moe(), 16
+    g = torch.Generator(device="cuda").manual_seed(T)
+    d = m.dims(D, D, E, K, torch.float32)
+    w1, v1, w2 = (torch.zeros((E, D, D), device="cuda") for _ in range(3))
+    w1[:, 0, 0], v1[:, 0, 1], w2[:, 0, 0] = 64.0, 0.25, (torch.arange(E, device="cuda") % 7 + 1).float()
+    ex = m.QuantExperts.quantize(w1, v1, w2)
+    x = torch.zeros((T, D), device="cuda")
+    x[:, 0] = 1.0
+    x[:, 1] = (torch.randint(0, 8, (T,), device="cuda", generator=g) * 4).float()
+    idx = torch.argsort(torch.rand((T, E), device="cuda", generator=g), dim=1)[:, :K].int()
+    gate = torch.full((T, K), 0.5, device="cuda")
+    got = m.quant_experts_forward(d, ex, x, idx, gate)
+    assert m.get_last_error() == 0
+    # SiLU(64) is 64 in 32 bits; h = 64 v, v below 8: a number of 8 bits; sums of at most 128 * 7 * 448 halves
+    want = 0.5 * 64.0 * 0.25 * x[:, 1] * (idx % 7 + 1).sum(1)
+    assert torch.equal(got[:, 0], want) and not got[:, 1:].any()
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_largest_select(score):
+    """1,048,576 tokens, keys a step of 1/16 apart."""
+    m, T, E, K = moe(), 1 << 20, 16, 4
+    g = torch.Generator(device="cuda").manual_seed(0)
+    order = torch.argsort(torch.rand((T, E), device="cuda", generator=g), dim=1)
+    logits = torch.empty((T, E), device="cuda").scatter_(1, order, (-torch.arange(E, device="cuda") / 16.0).expand(T, E))
+    for bias in (None, torch.zeros(E, device="cuda")):
+        idx, gate = m.route_select(m.dims(1024, 1024, E, K, torch.bfloat16), m.router(score), logits, bias)
+        assert torch.equal(idx.long(), order[:, :K])
+        p = -torch.arange(E, device="cuda").double() / 16
+        s = (torch.softmax(p, 0) if score == "softmax" else torch.sigmoid(p))[:K]
+        assert ((gate.double() - s / s.sum()).abs() <= 130 * 2.0 ** -23 * s).all()
+    assert m.get_last_error() == 0
+
+
+def test_calls_of_both_kernels_at_once():
+    """Streamed calls and calls in tiles of 128 rows on four streams at once, launched and as graphs, each with
+    a workspace of its own."""
+    m, g = moe(), torch.Generator(device="cuda").manual_seed(3)
+    E, K, D, F = 6, 2, 1024, 1536
+    mk = lambda *s: torch.randn(s, device="cuda", generator=g) * 0.05
+    ex = m.QuantExperts.quantize(mk(E, F, D), mk(E, F, D), mk(E, D, F))
+    d, r = m.dims(D, F, E, K, torch.float32), m.router("sigmoid")
+    w_r, sizes = mk(D, E), (1, 40, 300, 1000)
+    xs = [mk(T, D) * 20 for T in sizes]
+    wss = [m.quant_alloc_workspace(d, T) for T in sizes]
+    want = [m.quant_layer_forward(d, ex, x, w_r, r, ws=ws) for x, ws in zip(xs, wss)]
+    outs, streams = [torch.zeros_like(x) for x in xs], [torch.cuda.Stream() for _ in sizes]
+    torch.cuda.synchronize()
+    graphs = []
+    for x, o, ws in zip(xs, outs, wss):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            m.quant_layer_forward(d, ex, x, w_r, r, out=o, ws=ws)
+    for graphed in (False, True):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for x, o, ws, st, gr in zip(xs, outs, wss, streams, graphs):
+                with torch.cuda.stream(st):
+                    if graphed:
+                        gr.replay()
+                    else:
+                        m.quant_layer_forward(d, ex, x, w_r, r, out=o, ws=ws)
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            assert torch.equal(o, w)
+    assert m.get_last_error() == 0
